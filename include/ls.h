@@ -63,6 +63,8 @@ enum {
 
 enum { LS_LOSS_SOFTMAX_CE = 0, LS_LOSS_MSE_HALF = 1 };
 enum { LS_GEMM_FP32 = 0, LS_GEMM_BF16 = 1 };
+/* Element type of the tensors of the operators on raw buffers (ls_layer_norm, ls_vocab_loss, ls_orthogonalize, ...). */
+enum { LS_DTYPE_FP32 = 0, LS_DTYPE_BF16 = 1 };
 /* What an averaging step does with the per-replica momentum buffers.
  * AVERAGE: replaced by their mean like the parameters (makes tau = 1 equal to
  *          synchronous momentum SGD on the m-fold batch).
@@ -394,6 +396,82 @@ int ls_philox4x32_10(const uint32_t counter[4], const uint32_t key[2], uint32_t 
 int ls_linear_loss_static(const float* W_dev, const float* bias_dev, const float* x_dev, const void* y_dev,
                           int64_t n_rows, int d_in, int d_out, int loss, int chunk_rows, float* chunk_loss_dev,
                           void* cuda_stream);
+
+/* ---- operators of a language model's last layers and its weight update, on raw buffers ------------------------
+ * Not passages of the paper: what a local-SGD job of a language model needs beside the averaging step.  Conventions:
+ *  - m replicas in one call; *_stride is the distance in elements between replicas of that tensor (ignored for m == 1),
+ *    inside a replica every tensor is dense and row-major.  Any size is allowed up to the limits stated; rows and
+ *    replicas that start on 16-byte boundaries are read in vectors, others element by element.
+ *  - dtype LS_DTYPE_*: the type of activations, operands and their gradients; sums, statistics and losses are fp32 or
+ *    wider, and an output of dtype is rounded once.
+ *  - ws_dev: the call's workspace, 256-byte aligned, at least *_ws_bytes() bytes (else LS_ERR_STATE_SIZE), contents
+ *    irrelevant.  Two calls that may overlap on the GPU (other streams, other captured graphs) need workspaces of
+ *    their own.  Nothing is kept in it between calls.
+ *  - Enqueued on cuda_stream of the current device; the call returns at once and may be captured into a graph (the
+ *    first call of an operator on a device outside any capture).  Results are the same bits on every run.
+ *  - Outputs must not overlap inputs or each other.
+ *  - Every wait inside a kernel is bounded; one that runs out is recorded per device and reported by
+ *    ls_device_status().  The results of that call are invalid. */
+
+/* Waits for cuda_stream, then returns LS_ERR_DEVICE_TIMEOUT once (and clears the record) if a wait of one of these operators ran
+ * out on the current device since the last call, else LS_OK. */
+int ls_device_status(void* cuda_stream);
+
+/* Layer norm of every row of x [m][rows][d]:  y = (x - mean) * rstd * weight + bias,  rstd = 1 / sqrt(var + eps), var the
+ * mean square of x - mean.  weight, bias (may be NULL): float [m][d], param_stride apart.  y like x.  mean, rstd
+ * (either may be NULL): float [m][rows], dense.  eps >= 0.  d <= 16384. */
+int ls_layer_norm(const void* x_dev, const float* weight_dev, const float* bias_dev, int m, int64_t rows, int d,
+                  int64_t x_stride, int64_t param_stride, int dtype, float eps, void* y_dev, int64_t y_stride,
+                  float* mean_dev, float* rstd_dev, void* cuda_stream);
+
+/* Its gradient, from dy, x and the mean and rstd that the forward call wrote:
+ *   dx = rstd * (t - <t> - xhat <t xhat>),  t = dy * weight, xhat = (x - mean) * rstd, <.> the mean over a row,
+ *   dweight = sum over rows of dy * xhat,  dbias (may be NULL) = sum over rows of dy
+ * dweight, dbias: float [m][d], dparam_stride apart, overwritten (zeros for rows == 0). */
+int ls_layer_norm_grad_ws_bytes(int m, int64_t rows, int d, size_t* bytes);
+int ls_layer_norm_grad(const void* dy_dev, const void* x_dev, const float* weight_dev, const float* mean_dev,
+                       const float* rstd_dev, int m, int64_t rows, int d, int64_t dy_stride, int64_t x_stride,
+                       int64_t param_stride, int dtype, void* dx_dev, int64_t dx_stride, float* dweight_dev,
+                       float* dbias_dev, int64_t dparam_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
+/* Softmax cross entropy of the logits h W^T of a wide output matrix, without storing the logits:
+ *   z_n = W h_n,  lse_n = log sum_v exp z_nv,  row_loss_n = lse_n - z_n,y(n),  loss = mean of row_loss over labelled rows
+ * h [m][rows][d], W [m][vocab][d] of dtype; labels int32 [m][rows], dense: a label outside [0, vocab) marks a row
+ * without one (padding), whose row_loss is 0 and which does not count (loss is 0 when no row counts).
+ * loss float [m]; row_loss, lse float [m][rows], dense, either may be NULL.
+ * vocab <= 2^24, d <= 65536.  When a row is whole 16-byte pieces (d a multiple of 8 for bf16, 4 for fp32), h, W, dh, dW
+ * and their strides must be 16-byte multiples (else LS_ERR_INVALID_ARG).
+ * In fp32 an infinite element of h or W counts as 3.39e38 with its sign.
+ * Workspace of the loss: a few numbers a row and 128 columns (and a copy of both operands for fp32 or d not a multiple
+ * of 8).  Of the gradient: also the probabilities of a piece of rows, at most about 1 GiB, and the fp32 sum
+ * of dW for bf16 when the rows take several pieces. */
+int ls_vocab_loss_ws_bytes(int m, int64_t rows, int64_t vocab, int d, int dtype, int grad, size_t* bytes);
+int ls_vocab_loss(const void* h_dev, const void* W_dev, const int32_t* labels_dev, int m, int64_t rows, int64_t vocab,
+                  int d, int64_t h_stride, int64_t w_stride, int dtype, float* loss_dev, float* row_loss_dev,
+                  float* lse_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
+/* The same losses, and the gradients of scale * loss: dh [m][rows][d] (zero in rows without a label), dW [m][vocab][d],
+ * both of dtype, overwritten.  h of rows without a label does not enter dW, whatever it holds. */
+int ls_vocab_loss_grad(const void* h_dev, const void* W_dev, const int32_t* labels_dev, int m, int64_t rows, int64_t vocab,
+                       int d, int64_t h_stride, int64_t w_stride, int dtype, float scale, float* loss_dev,
+                       float* row_loss_dev, float* lse_dev, void* dh_dev, int64_t dh_stride, void* dW_dev,
+                       int64_t dw_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
+/* Orthogonalisation of the matrices u [m][rows][cols] by `steps` (1..64) Newton-Schulz steps:
+ *   X = u / (|u|_F + 1e-7);  repeat: A = X X^T, X = 3.4445 X + (-4.7750 A + 2.0315 A A) X;  out = X
+ * (for rows > cols the same of the transpose, transposed back).  Products are accurate to about 22 bits.  out has u's
+ * dtype and shape.  rows, cols <= 32768.  The workspace also serves ls_muon_step. */
+int ls_orthogonalize_ws_bytes(int m, int rows, int cols, size_t* bytes);
+int ls_orthogonalize(const void* u_dev, int m, int rows, int cols, int64_t u_stride, int dtype, int steps, void* out_dev,
+                     int64_t out_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
+/* One orthogonalised momentum step (the Muon update) of the matrices w [m][rows][cols] with momentum buffers v, both
+ * fp32 (ls_state_view() of a handle gives such stacks), from gradients g of g_dtype:
+ *   v <- momentum * v + g;   u = nesterov ? g + momentum * v : v;   w <- w - lr * sqrt(max(1, rows / cols)) * O(u)
+ * with O the orthogonalisation above.  0 <= momentum < 1. */
+int ls_muon_step(float* w_dev, float* v_dev, const void* g_dev, int m, int rows, int cols, int64_t w_stride,
+                 int64_t v_stride, int64_t g_stride, int g_dtype, float lr, float momentum, int nesterov, int steps, void* ws_dev,
+                 size_t ws_bytes, void* cuda_stream);
 
 /* Per-kernel device timing.  Between ls_profile_begin() and ls_profile_end()
  * every launch of a kernel class selected by class_mask (bit c = class c; for

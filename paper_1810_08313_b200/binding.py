@@ -116,6 +116,20 @@ def _lib():
                                      vp, i64, P(i64), P(f32)]),
         "ls_get_lr": (C.c_int, [vp, P(f32)]),
         "ls_linear_loss_static": (C.c_int, [vp, vp, vp, vp, i64, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp]),
+        "ls_device_status": (C.c_int, [vp]),
+        "ls_layer_norm": (C.c_int, [vp, vp, vp, C.c_int, i64, C.c_int, i64, i64, C.c_int, f32, vp, i64, vp, vp, vp]),
+        "ls_layer_norm_grad_ws_bytes": (C.c_int, [C.c_int, i64, C.c_int, P(C.c_size_t)]),
+        "ls_layer_norm_grad": (C.c_int, [vp, vp, vp, vp, vp, C.c_int, i64, C.c_int, i64, i64, i64, C.c_int, vp, i64, vp, vp,
+                                         i64, vp, C.c_size_t, vp]),
+        "ls_vocab_loss_ws_bytes": (C.c_int, [C.c_int, i64, i64, C.c_int, C.c_int, C.c_int, P(C.c_size_t)]),
+        "ls_vocab_loss": (C.c_int, [vp, vp, vp, C.c_int, i64, i64, C.c_int, i64, i64, C.c_int, vp, vp, vp, vp, C.c_size_t,
+                                    vp]),
+        "ls_vocab_loss_grad": (C.c_int, [vp, vp, vp, C.c_int, i64, i64, C.c_int, i64, i64, C.c_int, f32, vp, vp, vp, vp, i64,
+                                         vp, i64, vp, C.c_size_t, vp]),
+        "ls_orthogonalize_ws_bytes": (C.c_int, [C.c_int, C.c_int, C.c_int, P(C.c_size_t)]),
+        "ls_orthogonalize": (C.c_int, [vp, C.c_int, C.c_int, C.c_int, i64, C.c_int, C.c_int, vp, i64, vp, C.c_size_t, vp]),
+        "ls_muon_step": (C.c_int, [vp, vp, vp, C.c_int, C.c_int, C.c_int, i64, i64, i64, C.c_int, f32, f32, C.c_int, C.c_int,
+                                   vp, C.c_size_t, vp]),
         "ls_shard_buffer_floats": (C.c_int, [vp, P(i64)]),
         "ls_set_shard": (C.c_int, [vp, C.c_int, C.c_int, vp, vp, EXCHANGE_FN, vp]),
         "ls_shard_partial_sum": (C.c_int, [vp, vp]),
@@ -293,6 +307,271 @@ def linear_loss_static(W, bias, x, y, chunk_rows: int, chunk_loss, loss: str = "
                                         y.data_ptr(), int(x.shape[0]), int(x.shape[1]), int(W.shape[0]), LOSS[loss],
                                         int(chunk_rows), chunk_loss.data_ptr(), _stream_ptr(stream)),
            "ls_linear_loss_static")
+
+
+# ---- operators of a language model's last layers and its weight update ---------------------------------------
+# Every tensor takes the replicas first ([m][rows][d], ...); one replica may leave that axis out.  A replica is dense,
+# the distance between replicas is free (views into packed replica vectors are fine).  Outputs that are not given are
+# allocated.  `workspace`: a uint8 tensor of the size the matching *_workspace function names, for callers that keep
+# one; calls that may overlap on the GPU need their own.  `stream`: a torch stream, the current one by default.
+
+def _op_dtype(t, name: str) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+
+
+class _Op:
+    """Checks the tensors of one call, lends out its workspace and keeps track of what the stream uses."""
+
+    def __init__(self, first, stream):
+        import torch
+        self.torch = torch
+        if not (isinstance(first, torch.Tensor) and first.is_cuda):
+            raise ValueError("CUDA tensors expected")
+        self.device = first.device
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        if self.stream.device != self.device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        self.side = self.stream != torch.cuda.current_stream(self.device)
+
+    def stack(self, t, name: str, tail, m: Optional[int], dtype=None):
+        """t as [m][*tail] (m None: from t); returns (pointer, m, stride between replicas)."""
+        torch = self.torch
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == self.device):
+            raise ValueError(f"{name} must be a tensor on {self.device}")
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+        tail = tuple(int(n) for n in tail)
+        if t.dim() == len(tail):
+            t = t.unsqueeze(0)
+        if t.dim() != len(tail) + 1 or tuple(t.shape[1:]) != tail or (m is not None and t.shape[0] != m):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{'m' if m is None else m}] + {list(tail)}")
+        want = 1
+        for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+            if size > 1 and step != want:
+                raise ValueError(f"{name}: a replica must be dense and row-major")
+            want *= size
+        if t.shape[0] > 1 and t.stride(0) < want:
+            raise ValueError(f"{name}: the replicas overlap")
+        if self.side:
+            t.record_stream(self.stream)
+        return t.data_ptr(), t.shape[0], t.stride(0) if t.shape[0] > 1 else want
+
+    def dense(self, t, name: str, shape, dtype):
+        """t as a dense tensor of this shape (one replica may leave the first axis out)."""
+        ptr, _, stride = self.stack(t, name, shape[1:], shape[0], dtype)
+        n = 1
+        for v in shape[1:]:
+            n *= int(v)
+        if shape[0] > 1 and n > 0 and stride != n:
+            raise ValueError(f"{name} must be contiguous")
+        return ptr
+
+    def new(self, shape, dtype):
+        t = self.torch.empty(shape, dtype=dtype, device=self.device)
+        if self.side:
+            t.record_stream(self.stream)
+        return t
+
+    def workspace(self, given, nbytes: int):
+        t = given
+        if t is None:
+            t = self.new((nbytes + 256,), self.torch.uint8)
+        elif not (t.is_cuda and t.device == self.device and t.dtype == self.torch.uint8 and t.is_contiguous()):
+            raise ValueError("workspace must be a contiguous uint8 tensor on the device of the call")
+        elif self.side:
+            t.record_stream(self.stream)
+        base = (t.data_ptr() + 255) // 256 * 256
+        return base, t.data_ptr() + t.numel() - base, t
+
+    def call(self, name: str, *args):
+        with self.torch.cuda.device(self.device):
+            _check(getattr(_lib(), name)(*args, int(self.stream.cuda_stream)), name)
+
+
+def _like(t, lead, out):
+    """An output without the replica axis when the call's first tensor had none."""
+    return out if t.dim() == lead else out.squeeze(0)
+
+
+def _ws_bytes(name: str, *args) -> int:
+    n = C.c_size_t()
+    _check(getattr(_lib(), name)(*args, C.byref(n)), name)
+    return n.value
+
+
+def device_status(stream=None) -> None:
+    """Wait for the stream; raises LsError(LS_ERR_DEVICE_TIMEOUT) if a bounded wait of an operator ran out on its
+    device since the last call (ls_device_status)."""
+    import torch
+    s = stream if stream is not None else torch.cuda.current_stream()
+    with torch.cuda.device(s.device):
+        _check(_lib().ls_device_status(int(s.cuda_stream)), "ls_device_status")
+
+
+def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None, mean=None, rstd=None, stream=None):
+    """Layer norm of the rows of x [m][rows][d] (float32 or bfloat16) with float32 weight and bias [m][d]
+    (ls_layer_norm).  Returns (y, mean, rstd), the last two float32 [m][rows]."""
+    op = _Op(x, stream)
+    dt = _op_dtype(x, "x")
+    if x.dim() not in (2, 3):
+        raise ValueError("x must be [m][rows][d] or [rows][d]")
+    rows, d = x.shape[-2:]
+    xp, m, xs = op.stack(x, "x", (rows, d), None)
+    f32 = op.torch.float32
+    wp, _, ws = op.stack(weight, "weight", (d,), m, f32)
+    bp = None
+    if bias is not None:
+        bp, _, bs = op.stack(bias, "bias", (d,), m, f32)
+        if m > 1 and bs != ws:
+            raise ValueError("weight and bias must have the same distance between replicas")
+    y = op.new((m, rows, d), x.dtype) if out is None else out
+    mean_t = op.new((m, rows), f32) if mean is None else mean
+    rstd_t = op.new((m, rows), f32) if rstd is None else rstd
+    yp, _, ys = op.stack(y, "out", (rows, d), m, x.dtype)
+    mp, rp = op.dense(mean_t, "mean", (m, rows), f32), op.dense(rstd_t, "rstd", (m, rows), f32)
+    op.call("ls_layer_norm", xp, wp, bp, m, rows, d, xs, ws, dt, float(eps), yp, ys, mp, rp)
+    return (y if out is not None else _like(x, 3, y), mean_t if mean is not None else _like(x, 3, mean_t),
+            rstd_t if rstd is not None else _like(x, 3, rstd_t))
+
+
+def layer_norm_grad_workspace(m: int, rows: int, d: int) -> int:
+    return _ws_bytes("ls_layer_norm_grad_ws_bytes", int(m), int(rows), int(d)) + 256
+
+
+def layer_norm_grad(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, workspace=None, stream=None):
+    """Gradient of layer_norm from dy, x and the forward call's mean and rstd (ls_layer_norm_grad).  Returns
+    (dx like x, dweight, dbias float32 [m][d])."""
+    op = _Op(x, stream)
+    dt = _op_dtype(x, "x")
+    if x.dim() not in (2, 3):
+        raise ValueError("x must be [m][rows][d] or [rows][d]")
+    rows, d = x.shape[-2:]
+    f32 = op.torch.float32
+    xp, m, xs = op.stack(x, "x", (rows, d), None)
+    dyp, _, dys = op.stack(dy, "dy", (rows, d), m, x.dtype)
+    wp, _, ws = op.stack(weight, "weight", (d,), m, f32)
+    mp, rp = op.dense(mean, "mean", (m, rows), f32), op.dense(rstd, "rstd", (m, rows), f32)
+    dx_t = op.new((m, rows, d), x.dtype) if dx is None else dx
+    dxp, _, dxs = op.stack(dx_t, "dx", (rows, d), m, x.dtype)
+    dw_t = op.new((m, d), f32) if dweight is None else dweight
+    dwp, _, dps = op.stack(dw_t, "dweight", (d,), m, f32)
+    if dbias is None:
+        # beside dweight, with its distance between replicas
+        db_t = op.torch.empty_strided((m, d), (dps, 1), dtype=f32, device=op.device)
+        if op.side:
+            db_t.record_stream(op.stream)
+    else:
+        db_t = dbias
+    dbp, _, dbs = op.stack(db_t, "dbias", (d,), m, f32)
+    if m > 1 and dbs != dps:
+        raise ValueError("dweight and dbias must have the same distance between replicas")
+    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_layer_norm_grad_ws_bytes", m, rows, d))
+    op.call("ls_layer_norm_grad", dyp, xp, wp, mp, rp, m, rows, d, dys, xs, ws, dt, dxp, dxs, dwp, dbp, dps, base, nbytes)
+    return (dx_t if dx is not None else _like(x, 3, dx_t), dw_t if dweight is not None else _like(x, 3, dw_t),
+            db_t if dbias is not None else _like(x, 3, db_t))
+
+
+def vocab_loss_workspace(m: int, rows: int, vocab: int, d: int, dtype: str = "bf16", grad: bool = False) -> int:
+    return _ws_bytes("ls_vocab_loss_ws_bytes", int(m), int(rows), int(vocab), int(d), GEMM[dtype], int(bool(grad))) + 256
+
+
+def _vocab_args(op, h, W, labels):
+    torch = op.torch
+    dt = _op_dtype(h, "h")
+    if h.dim() not in (2, 3):
+        raise ValueError("h must be [m][rows][d] or [rows][d]")
+    rows, d = h.shape[-2:]
+    hp, m, hs = op.stack(h, "h", (rows, d), None)
+    if W.dim() not in (2, 3) or W.shape[-1] != d:
+        raise ValueError(f"W must be [m][vocab][{d}]")
+    vocab = W.shape[-2]
+    wp, _, ws = op.stack(W, "W", (vocab, d), m, h.dtype)
+    lp = op.dense(labels, "labels", (m, rows), torch.int32)
+    return dt, m, rows, d, vocab, hp, hs, wp, ws, lp
+
+
+def vocab_loss(h, W, labels, loss=None, row_loss=None, lse=None, workspace=None, stream=None):
+    """Mean softmax cross entropy of the logits h W^T, h [m][rows][d], W [m][vocab][d] (both float32 or both
+    bfloat16), labels int32 [m][rows] (outside [0, vocab): no label), without storing the logits (ls_vocab_loss).
+    Returns (loss [m], row_loss [m][rows], log-sum-exp [m][rows]), float32."""
+    op = _Op(h, stream)
+    dt, m, rows, d, vocab, hp, hs, wp, ws, lp = _vocab_args(op, h, W, labels)
+    f32 = op.torch.float32
+    loss_t = op.new((m,), f32) if loss is None else loss
+    rl_t = op.new((m, rows), f32) if row_loss is None else row_loss
+    lse_t = op.new((m, rows), f32) if lse is None else lse
+    outs = (op.dense(loss_t, "loss", (m,), f32), op.dense(rl_t, "row_loss", (m, rows), f32),
+            op.dense(lse_t, "lse", (m, rows), f32))
+    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_vocab_loss_ws_bytes", m, rows, vocab, d, dt, 0))
+    op.call("ls_vocab_loss", hp, wp, lp, m, rows, vocab, d, hs, ws, dt, *outs, base, nbytes)
+    return (loss_t, rl_t if row_loss is not None else _like(h, 3, rl_t), lse_t if lse is not None else _like(h, 3, lse_t))
+
+
+def vocab_loss_grad(h, W, labels, scale: float = 1.0, dh=None, dW=None, loss=None, row_loss=None, lse=None,
+                    workspace=None, stream=None):
+    """vocab_loss and the gradients of scale * loss (ls_vocab_loss_grad).  Returns (loss, row_loss, lse, dh like h,
+    dW like W)."""
+    op = _Op(h, stream)
+    dt, m, rows, d, vocab, hp, hs, wp, ws, lp = _vocab_args(op, h, W, labels)
+    f32 = op.torch.float32
+    loss_t = op.new((m,), f32) if loss is None else loss
+    rl_t = op.new((m, rows), f32) if row_loss is None else row_loss
+    lse_t = op.new((m, rows), f32) if lse is None else lse
+    outs = (op.dense(loss_t, "loss", (m,), f32), op.dense(rl_t, "row_loss", (m, rows), f32),
+            op.dense(lse_t, "lse", (m, rows), f32))
+    dh_t = op.new((m, rows, d), h.dtype) if dh is None else dh
+    dW_t = op.new((m, vocab, d), h.dtype) if dW is None else dW
+    dhp, _, dhs = op.stack(dh_t, "dh", (rows, d), m, h.dtype)
+    dwp, _, dws = op.stack(dW_t, "dW", (vocab, d), m, h.dtype)
+    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_vocab_loss_ws_bytes", m, rows, vocab, d, dt, 1))
+    op.call("ls_vocab_loss_grad", hp, wp, lp, m, rows, vocab, d, hs, ws, dt, float(scale), *outs, dhp, dhs, dwp, dws, base,
+            nbytes)
+    return (loss_t, rl_t if row_loss is not None else _like(h, 3, rl_t), lse_t if lse is not None else _like(h, 3, lse_t),
+            dh_t if dh is not None else _like(h, 3, dh_t), dW_t if dW is not None else _like(h, 3, dW_t))
+
+
+def orthogonalize_workspace(m: int, rows: int, cols: int) -> int:
+    """Workspace of orthogonalize and muon_step."""
+    return _ws_bytes("ls_orthogonalize_ws_bytes", int(m), int(rows), int(cols)) + 256
+
+
+def orthogonalize(u, steps: int = 5, out=None, workspace=None, stream=None):
+    """Newton-Schulz orthogonalisation of the matrices u [m][rows][cols], float32 or bfloat16 (ls_orthogonalize)."""
+    op = _Op(u, stream)
+    dt = _op_dtype(u, "u")
+    if u.dim() not in (2, 3):
+        raise ValueError("u must be [m][rows][cols] or [rows][cols]")
+    rows, cols = u.shape[-2:]
+    up, m, us = op.stack(u, "u", (rows, cols), None)
+    o = op.new((m, rows, cols), u.dtype) if out is None else out
+    outp, _, outs = op.stack(o, "out", (rows, cols), m, u.dtype)
+    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
+    op.call("ls_orthogonalize", up, m, rows, cols, us, dt, int(steps), outp, outs, base, nbytes)
+    return o if out is not None else _like(u, 3, o)
+
+
+def muon_step(w, v, g, lr: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5, workspace=None,
+              stream=None) -> None:
+    """One orthogonalised momentum step of the float32 matrices w [m][rows][cols] with momentum buffers v, in place,
+    from gradients g (float32 or bfloat16) (ls_muon_step).  w and v may be views into packed replica vectors
+    (LocalSGD.state_view)."""
+    op = _Op(w, stream)
+    dt = _op_dtype(g, "g")
+    if w.dim() not in (2, 3):
+        raise ValueError("w must be [m][rows][cols] or [rows][cols]")
+    rows, cols = w.shape[-2:]
+    f32 = op.torch.float32
+    wp, m, ws = op.stack(w, "w", (rows, cols), None, f32)
+    vp, _, vs = op.stack(v, "v", (rows, cols), m, f32)
+    gp, _, gs = op.stack(g, "g", (rows, cols), m)
+    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
+    op.call("ls_muon_step", wp, vp, gp, m, rows, cols, ws, vs, gs, dt, float(lr), float(momentum), int(bool(nesterov)),
+            int(steps), base, nbytes)
 
 
 class LocalSGD:

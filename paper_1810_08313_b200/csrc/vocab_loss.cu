@@ -1,0 +1,565 @@
+// Softmax cross entropy of a wide output matrix and its gradient (ls_vocab_loss, ls_vocab_loss_grad).
+//
+//   z = h W^T  [rows][V];   loss_n = log sum_v exp z_nv - z_n,y(n);   loss = mean of the rows that have a label
+//   dz = exp(z - lse) - onehot(y);   dh = dz W / count;   dW = dz^T h / count
+//
+// The three products are 6 rows V d flops and bound the call; what must not be added to them is traffic of rows x V
+// numbers in fp32.  The logits never reach memory in the loss: the product's epilogue reduces every row of a 256 x 256 tile to
+// (maximum, sum of exponentials) per 128 columns, and a small kernel combines those.  The gradient needs the
+// normalised probabilities twice, as an operand of dh (contracted over V) and of dW (contracted over rows), and their
+// normaliser only when the last column is known.  Recomputing the logits would cost a third more flops; instead a piece
+// of rows (at most 2^29 elements of the piece's probabilities, 1 GiB) keeps exp(z - slice maximum) as fp16 numbers in
+// [0, 1], a streaming pass scales them to dz in bf16 in place (4 bytes a logit against 6 d flops), and both products
+// read them.  fp16 and not bf16 there because the number is rounded once more: 11 bits against 8, its error
+// disappears under the bf16 rounding of dz, which the tensor cores need and which is of the same size as the rounding
+// of the bf16 results.  At the label, exp(z_y - lse) - 1 is formed from the fp32 logit with expm1.  The factor
+// scale / count is applied to the fp32 accumulators: in dz it would give every uncertain row the same rounding error
+// of 1 / count, where -1 is exact.
+//
+// fp32 tensors: operands as three bf16 pieces (24 bits) and six products (gemm_op.cuh), logits kept in fp32 for a piece of rows, dz
+// in three pieces; sums over several pieces of rows are added into dW by the bulk-copy engine in fp32.
+//
+// The row sums, the loss and every accumulation are fp32 or wider and in a fixed order: results are
+// reproducible bit for bit.
+#include "gemm_op.cuh"
+
+#include <math.h>
+
+namespace ls {
+namespace {
+
+using gop::Params;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ bool has_label(int y, int V) { return y >= 0 && y < V; }
+
+// ---- number of rows with a label, per replica ----------------------------------------------------------------------
+__global__ void __launch_bounds__(1024) vocab_count_kernel(const int32_t* labels, int64_t rows, int V, float* inv_count) {
+  __shared__ long long red[32];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int32_t* y = labels + (int64_t)blockIdx.x * rows;
+  long long n = 0;
+  for (int64_t i = threadIdx.x; i < rows; i += 1024) n += has_label(y[i], V) ? 1 : 0;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    long long t = 0;
+    for (int i = 0; i < 32; ++i) t += red[i];
+    inv_count[blockIdx.x] = t > 0 ? (float)(1.0 / (double)t) : 0.f;
+  }
+}
+
+// ---- mean loss of every replica: double sums, thread by thread and then in thread order -----------------------------
+__global__ void __launch_bounds__(1024) vocab_mean_kernel(const float* row_loss, const int32_t* labels, int64_t rows, int V,
+                                                          float* loss) {
+  __shared__ double sum[32];
+  __shared__ long long cnt[32];
+  grid_dep_wait();
+  grid_dep_launch();
+  const float* l = row_loss + (int64_t)blockIdx.x * rows;
+  const int32_t* y = labels + (int64_t)blockIdx.x * rows;
+  double s = 0.0;
+  long long n = 0;
+  for (int64_t i = threadIdx.x; i < rows; i += 1024)
+    if (has_label(y[i], V)) { s += (double)l[i]; ++n; }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    s += __shfl_xor_sync(0xffffffffu, s, o);
+    n += __shfl_xor_sync(0xffffffffu, n, o);
+  }
+  if ((threadIdx.x & 31) == 0) { sum[threadIdx.x >> 5] = s; cnt[threadIdx.x >> 5] = n; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0; n = 0;
+    for (int i = 0; i < 32; ++i) { s += sum[i]; n += cnt[i]; }
+    loss[blockIdx.x] = n > 0 ? (float)(s / (double)n) : 0.f;
+  }
+}
+
+// ---- slices -> log-sum-exp and row loss: 32 rows per CTA, 32 warps take every 32nd slice ------------------------------
+__global__ void __launch_bounds__(1024)
+vocab_combine_kernel(const float* stat_max, const float* stat_sum, int64_t stat_ld, int slices, int rows, int V,
+                     const int32_t* labels, const float* label_logit, float* lse, float* row_loss) {
+  __shared__ float smax[32][33], ssum[32][33];
+  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
+  const int row = blockIdx.x * 32 + lane;
+  grid_dep_wait();
+  grid_dep_launch();
+  float m = -INFINITY, s = 0.f;
+  if (row < rows) {
+    for (int t = wp; t < slices; t += 32) {
+      const float tm = __ldcg(stat_max + (int64_t)t * stat_ld + row), ts = __ldcg(stat_sum + (int64_t)t * stat_ld + row);
+      if (tm > m) { s = s * gop::ex2(m - tm) + ts; m = tm; }
+      else if (tm == -INFINITY) s += ts;             // only -inf (nothing to add), or NaN
+      else s += ts * gop::ex2(tm - m);
+    }
+  }
+  smax[wp][lane] = m; ssum[wp][lane] = s;
+  __syncthreads();
+  if (wp == 0 && row < rows) {
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) M = fmaxf(M, smax[i][lane]);
+    float S = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float tm = smax[i][lane];
+      S += tm == -INFINITY ? ssum[i][lane] : ssum[i][lane] * gop::ex2(tm - M);
+    }
+    const float l = (M == -INFINITY ? 0.f : M * kLn2) + logf(S);
+    lse[row] = l;
+    row_loss[row] = has_label(labels[row], V) ? l - label_logit[row] : 0.f;
+  }
+}
+
+// ---- exponentials -> dz, eight columns per thread ------------------------------------------------------------------------
+// bf16: in place over the fp16 numbers.
+__global__ void __launch_bounds__(256)
+vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int V, const float* stat_max, int64_t stat_ld, const int32_t* labels,
+                     const float* label_logit, const float* lse) {
+  const int row = blockIdx.y;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  grid_dep_wait();
+  grid_dep_launch();
+  if (c >= V) return;
+  uint16_t* at = e + (int64_t)row * ld + c;
+  const int y = labels[row];
+  if (!has_label(y, V)) {
+    *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  const float l = lse[row];
+  const float f = gop::ex2(__ldg(stat_max + (int64_t)(c >> 7) * stat_ld + row) - l * kLog2e);
+  uint4 u = *reinterpret_cast<const uint4*>(at);
+  uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    v[2 * i] = t.x * f; v[2 * i + 1] = t.y * f;
+  }
+  const int d = y - c;
+  if (d >= 0 && d < 8) {
+    const float py = expm1f(label_logit[row] - l);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i == d) v[i] = py;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<uint32_t*>(&t);
+  }
+  *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// x = p0 + p1 + p2, each piece the bf16 rounding of what is left.  The first piece stays finite: the products pair every
+// piece with others that may be zero, and 0 * inf would be a NaN.  An infinite x counts as the largest bf16 number.
+__device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
+  const float kMax = 3.3895313892515355e38f;                  // 0x7f7f
+  p[0] = isnan(x) ? __float2bfloat16_rn(x) : __float2bfloat16_rn(fminf(fmaxf(x, -kMax), kMax));
+  const float r = isinf(x) ? 0.f : x - __bfloat162float(p[0]);
+  p[1] = __float2bfloat16_rn(r);
+  p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
+}
+
+// fp32: logits z -> three pieces of dz.
+__global__ void __launch_bounds__(256)
+vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t piece, int V, const int32_t* labels,
+                     const float* label_logit, const float* lse) {
+  const int row = blockIdx.y;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  grid_dep_wait();
+  grid_dep_launch();
+  if (c >= V) return;
+  const int64_t at = (int64_t)row * ld + c;
+  const int y = labels[row];
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (has_label(y, V)) {
+      const float l = lse[row];
+    const float4 u = *reinterpret_cast<const float4*>(z + at);
+    v[0] = expf(u.x - l); v[1] = expf(u.y - l); v[2] = expf(u.z - l); v[3] = expf(u.w - l);
+    const int d = y - c;
+    if (d >= 0 && d < 4) {
+      const float py = expm1f(label_logit[row] - l);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) if (i == d) v[i] = py;
+    }
+  }
+  __nv_bfloat16 p[4][3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) split3(v[i], p[i]);
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    uint2 w;
+    __nv_bfloat162 a = __halves2bfloat162(p[0][q], p[1][q]), b = __halves2bfloat162(p[2][q], p[3][q]);
+    w.x = *reinterpret_cast<uint32_t*>(&a); w.y = *reinterpret_cast<uint32_t*>(&b);
+    *reinterpret_cast<uint2*>(out + q * piece + at) = w;
+  }
+}
+
+// ---- operands into the workspace: rows padded to whole 16 bytes, fp32 cut into three pieces ------------------------------
+// labels (optional): rows without a label are written as zeros, so that whatever they hold stays out of dW.
+template <typename T>
+__global__ void __launch_bounds__(256)
+vocab_pack_kernel(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t ld, int64_t piece, const int32_t* labels,
+                  int V, bool vec) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int PER = F32 ? 4 : 8;
+  const int per_row = (d + PER - 1) / PER;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int64_t total = rows * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per_row;
+    const int c = (int)(i - row * per_row) * PER;
+    T v[PER];
+    if (labels != nullptr && !has_label(labels[row], V)) {
+#pragma unroll
+      for (int k = 0; k < PER; ++k) v[k] = (T)0.f;
+    } else if (vec) {
+      *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(src + row * d + c);
+    } else {
+#pragma unroll
+      for (int k = 0; k < PER; ++k) v[k] = c + k < d ? src[row * d + c + k] : (T)0.f;
+    }
+    if constexpr (F32) {
+      __nv_bfloat16 p[4][3];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) split3(v[k], p[k]);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        __nv_bfloat162 a = __halves2bfloat162(p[0][q], p[1][q]), b = __halves2bfloat162(p[2][q], p[3][q]);
+        *reinterpret_cast<uint2*>(dst + q * piece + row * ld + c) =
+            make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+      }
+    } else {
+      *reinterpret_cast<uint4*>(dst + row * ld + c) = *reinterpret_cast<const uint4*>(v);
+    }
+  }
+}
+
+// ---- sum of fp32 planes in index order, rounded to the output type --------------------------------------------------------
+template <typename T>
+__global__ void __launch_bounds__(256)
+vocab_fold_kernel(const float* part, int planes, int64_t plane, int64_t ld, int64_t rows, int d, T* out) {
+  const int per_row = (d + 3) / 4;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int64_t total = rows * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per_row;
+    const int c = (int)(i - row * per_row) * 4;
+    float4 s = *reinterpret_cast<const float4*>(part + row * ld + c);
+    for (int p = 1; p < planes; ++p) {
+      const float4 t = *reinterpret_cast<const float4*>(part + p * plane + row * ld + c);
+      s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+    }
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    T* o = out + row * d + c;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) if (c + k < d) o[k] = (T)v[k];
+  }
+}
+
+// ---- plan: what a call keeps in its workspace ---------------------------------------------------------------------------------
+constexpr int64_t kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+struct Plan {
+  bool f32, grad;
+  int np;
+  int64_t R;            // rows of a piece
+  int64_t pieces;
+  int64_t Vp, dp;       // padded row lengths: probabilities, packed operands
+  int64_t df;           // padded row length of fp32 sums
+  int slices;
+  int64_t stat_ld;
+  int splits;           // of the contraction over V in dh
+  bool dh_fold, dw_fold;   // dh, dW pass through an fp32 sum in the workspace (several parts, or rows of no whole 16 bytes)
+  size_t o_stat, o_logit, o_lse, o_rowloss, o_inv, o_e, o_dz, o_h, o_w, o_dh, o_dw, total;
+};
+
+int check_sizes(int m, int64_t rows, int64_t vocab, int d, int dtype) {
+  if (m < 1 || rows < 0 || vocab < 1 || d < 1) return LS_ERR_INVALID_ARG;
+  if (dtype != LS_DTYPE_FP32 && dtype != LS_DTYPE_BF16) return LS_ERR_INVALID_ARG;
+  if (m > 65535 || rows > 2147483647ll || vocab > kMaxVocab || d > kMaxWidth) return LS_ERR_TOO_LARGE;
+  return LS_OK;
+}
+
+Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
+  Plan p{};
+  p.f32 = dtype == LS_DTYPE_FP32;
+  p.grad = grad;
+  p.np = p.f32 ? 3 : 1;
+  p.Vp = round_up(V, 64);
+  p.dp = round_up(d, 8);
+  p.df = round_up(d, 4);
+  p.slices = (int)(2 * ((V + 255) / 256));
+  // rows of a piece: the probabilities of a piece of a gradient, or the statistics of a piece of a loss, stay bounded
+  const int64_t most = grad ? (p.f32 ? (int64_t)1 << 27 : (int64_t)1 << 29) / p.Vp : ((int64_t)1 << 25) / p.slices;
+  int64_t R = most / 256 * 256;
+  if (R < 256) R = 256;
+  p.pieces = rows > 0 ? (rows + R - 1) / R : 0;
+  p.R = rows > 0 ? round_up((rows + p.pieces - 1) / p.pieces, 256) : 0;
+  p.pieces = rows > 0 ? (rows + p.R - 1) / p.R : 0;
+  p.stat_ld = p.R;
+  const int64_t dh_tiles = ((p.R < rows ? p.R : rows) + 255) / 256 * ((d + 255) / 256);
+  p.splits = grad && rows > 0 ? gop::split_count(dh_tiles, V, 8) : 1;
+  const bool whole = d % (p.f32 ? 4 : 8) == 0;
+  p.dh_fold = grad && (p.splits > 1 || !whole);
+  p.dw_fold = grad && (!whole || (!p.f32 && p.pieces > 1));
+  size_t at = 0;
+  auto take = [&at](int64_t bytes) { size_t o = at; at += (size_t)round_up(bytes, 256); return o; };
+  p.o_stat = take(2 * p.slices * p.stat_ld * 4);
+  p.o_logit = take(m * rows * 4);
+  p.o_lse = take(m * rows * 4);
+  p.o_rowloss = take(m * rows * 4);
+  p.o_inv = take(m * 4);
+  // operands laid out anew: fp32 ones (as pieces), bf16 ones whose rows are no whole 16 bytes, and, for dW, h with the
+  // rows that have no label cleared
+  const bool lay = p.f32 || d % 8 != 0;
+  p.o_h = take(lay || grad ? p.np * p.R * p.dp * 2 : 0);
+  p.o_w = take(lay ? p.np * V * p.dp * 2 : 0);
+  if (grad) {
+    p.o_e = take(p.R * p.Vp * (p.f32 ? 4 : 2));
+    p.o_dz = p.f32 ? take(3 * p.R * p.Vp * 2) : p.o_e;
+    p.o_dh = take(p.dh_fold ? (int64_t)p.splits * p.R * p.df * 4 : 0);
+    p.o_dw = take(p.dw_fold ? V * p.df * 4 : 0);
+  }
+  p.total = at;
+  return p;
+}
+
+unsigned stream_grid(int64_t items) {
+  const int64_t g = (items + 255) / 256;
+  return (unsigned)(g < 148 * 8 ? (g < 1 ? 1 : g) : 148 * 8);
+}
+
+template <typename T>
+cudaError_t pack(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t ld, int64_t piece, const int32_t* labels,
+                 int V, cudaStream_t st) {
+  const int per = 16 / sizeof(T);
+  const bool vec = d % per == 0 && reinterpret_cast<uintptr_t>(src) % 16 == 0;
+  return launch_dep(vocab_pack_kernel<T>, dim3(stream_grid(rows * ((d + per - 1) / per))), dim3(256), 0, st, 1, src, rows, d,
+                    dst, ld, piece, labels, V, vec);
+}
+
+struct VocabArgs {
+  const void *h, *W;
+  const int32_t* labels;
+  int m;
+  int64_t rows, V;
+  int d;
+  int64_t h_stride, w_stride, dh_stride, dw_stride;
+  int dtype;
+  float scale;
+  float *loss, *row_loss, *lse;
+  void *dh, *dW;
+  char* ws;
+};
+
+#define LS_TRY(x)                                   \
+  do {                                              \
+    if ((x) != cudaSuccess) return LS_ERR_CUDA;     \
+  } while (0)
+
+// One replica.  T: element type of h, W, dh, dW.  NP: pieces an operand is given in.
+template <typename T, int NP>
+int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
+  constexpr bool F32 = NP == 3;
+  using bf = __nv_bfloat16;
+  const T* h = static_cast<const T*>(a.h) + rep * a.h_stride;
+  const T* W = static_cast<const T*>(a.W) + rep * a.w_stride;
+  const int32_t* labels = a.labels + rep * a.rows;
+  float* stat_max = reinterpret_cast<float*>(a.ws + p.o_stat);
+  float* stat_sum = stat_max + p.slices * p.stat_ld;
+  float* logit = reinterpret_cast<float*>(a.ws + p.o_logit) + rep * a.rows;
+  float* lse = (a.lse ? a.lse : reinterpret_cast<float*>(a.ws + p.o_lse)) + rep * a.rows;
+  float* row_loss = (a.row_loss ? a.row_loss : reinterpret_cast<float*>(a.ws + p.o_rowloss)) + rep * a.rows;
+  const float* inv = reinterpret_cast<const float*>(a.ws + p.o_inv) + rep;
+  bf* hpack = reinterpret_cast<bf*>(a.ws + p.o_h);
+  bf* wpack = reinterpret_cast<bf*>(a.ws + p.o_w);
+  const int64_t V = a.V;
+  const int d = a.d;
+  const bool lay = F32 || d % 8 != 0;
+  if (lay) LS_TRY(pack<T>(W, V, d, wpack, p.dp, V * p.dp, nullptr, 0, st));
+  const bf* wop = lay ? wpack : reinterpret_cast<const bf*>(W);
+  const int64_t wld = lay ? p.dp : d;
+  CUtensorMap mw_k, mw_mn;
+  LS_TRY(gop::make_stack_map(&mw_k, wop, gop::MAP_BF16, V, d, NP, wld, V * wld, 128));
+  LS_TRY(gop::make_stack_map(&mw_mn, wop, gop::MAP_BF16, V, d, NP, wld, V * wld, 64));
+  for (int64_t r0 = 0, piece = 0; r0 < a.rows; r0 += p.R, ++piece) {
+    const int64_t rn = a.rows - r0 < p.R ? a.rows - r0 : p.R;
+    const T* hr = h + r0 * d;
+    const int64_t hplane = p.R * p.dp;
+    if (lay) LS_TRY(pack<T>(hr, rn, d, hpack, p.dp, hplane, nullptr, 0, st));
+    const bf* hop = lay ? hpack : reinterpret_cast<const bf*>(hr);
+    const int64_t hld = lay ? p.dp : d;
+    CUtensorMap mh_k, me;
+    LS_TRY(gop::make_stack_map(&mh_k, hop, gop::MAP_BF16, rn, d, NP, hld, hplane, 128));
+    // logits
+    Params g{};
+    g.batch = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
+    g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld;
+    g.labels = labels + r0; g.label_logit = logit + r0;
+    if (!p.grad) {
+      LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(mh_k, mw_k, mh_k, mh_k, g, d, st)));
+    } else if (F32) {
+      LS_TRY(gop::make_stack_map(&me, a.ws + p.o_e, gop::MAP_F32, rn, V, 1, p.Vp, p.R * p.Vp, 32));
+      LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS_F32>(mh_k, mw_k, me, me, g, d, st)));
+    } else {
+      LS_TRY(gop::make_stack_map(&me, a.ws + p.o_e, gop::MAP_F16, rn, V, 1, p.Vp, p.R * p.Vp, 32));
+      LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS_F16>(mh_k, mw_k, me, me, g, d, st)));
+    }
+    LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((rn + 31) / 32)), dim3(1024), 0, st, 1, stat_max, stat_sum,
+                      p.stat_ld, p.slices, (int)rn, (int)V, labels + r0, logit + r0, lse + r0, row_loss + r0));
+    if (!p.grad) continue;
+    // dz
+    bf* dz = reinterpret_cast<bf*>(a.ws + p.o_dz);
+    // (grid.y is limited to 65535 rows a launch)
+    for (int64_t q0 = 0; q0 < rn; q0 += 65280) {
+      const unsigned qn = (unsigned)(rn - q0 < 65280 ? rn - q0 : 65280);
+      const int32_t* ly = labels + r0 + q0;
+      if (F32) {
+        LS_TRY(launch_dep(vocab_dz_fp32_kernel, dim3((unsigned)((V + 1023) / 1024), qn), dim3(256), 0, st, 1,
+                          reinterpret_cast<const float*>(a.ws + p.o_e) + q0 * p.Vp, dz + q0 * p.Vp, p.Vp, p.R * p.Vp, (int)V,
+                          ly, logit + r0 + q0, lse + r0 + q0));
+      } else {
+        LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + 2047) / 2048), qn), dim3(256), 0, st, 1,
+                          reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)V, stat_max + q0, p.stat_ld, ly,
+                          logit + r0 + q0, lse + r0 + q0));
+      }
+    }
+    CUtensorMap mz_k, mz_mn, mh_mn, mo;
+    LS_TRY(gop::make_stack_map(&mz_k, dz, gop::MAP_BF16, rn, V, NP, p.Vp, p.R * p.Vp, 128));
+    LS_TRY(gop::make_stack_map(&mz_mn, dz, gop::MAP_BF16, rn, V, NP, p.Vp, p.R * p.Vp, 64));
+    // dh = dz W
+    T* dh = static_cast<T*>(a.dh) + rep * a.dh_stride + r0 * d;
+    Params gh{};
+    gh.batch = 1; gh.splits = p.splits; gh.M = (int)rn; gh.N = d; gh.alpha = a.scale; gh.alpha_dev = inv; gh.n_fast = 1;
+    if (p.dh_fold) {
+      float* part = reinterpret_cast<float*>(a.ws + p.o_dh);
+      gh.c_zstep = p.splits;
+      LS_TRY(gop::make_stack_map(&mo, part, gop::MAP_F32, rn, d, p.splits, p.df, p.R * p.df, 32));
+      LS_TRY((gop::launch<NP, false, false, true, gop::EPI_F32>(mz_k, mw_mn, mo, mo, gh, V, st)));
+      LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(rn * ((d + 3) / 4))), dim3(256), 0, st, 1,
+                        static_cast<const float*>(part), p.splits, p.R * p.df, p.df, rn, d, dh));
+    } else {
+      LS_TRY(gop::make_stack_map(&mo, dh, F32 ? gop::MAP_F32 : gop::MAP_BF16, rn, d, 1, d, rn * d, 32));
+      LS_TRY((gop::launch<NP, false, false, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(mz_k, mw_mn, mo, mo, gh, V, st)));
+    }
+    // dW (+)= dz^T h, with the rows that have no label cleared
+    LS_TRY(pack<T>(hr, rn, d, hpack, p.dp, hplane, labels + r0, (int)V, st));
+    LS_TRY(gop::make_stack_map(&mh_mn, hpack, gop::MAP_BF16, rn, d, NP, p.dp, hplane, 64));
+    T* dW = static_cast<T*>(a.dW) + rep * a.dw_stride;
+    Params gw{};
+    gw.batch = 1; gw.splits = 1; gw.M = (int)V; gw.N = d; gw.alpha = a.scale; gw.alpha_dev = inv; gw.n_fast = 1;
+    gw.reduce = piece > 0;
+    if (p.dw_fold) {
+      float* sum = reinterpret_cast<float*>(a.ws + p.o_dw);
+      LS_TRY(gop::make_stack_map(&mo, sum, gop::MAP_F32, V, d, 1, p.df, V * p.df, 32));
+      LS_TRY((gop::launch<NP, false, true, true, gop::EPI_F32>(mz_mn, mh_mn, mo, mo, gw, rn, st)));
+      if (r0 + p.R >= a.rows)
+        LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(V * ((d + 3) / 4))), dim3(256), 0, st, 1,
+                          static_cast<const float*>(sum), 1, (int64_t)0, p.df, V, d, dW));
+    } else {
+      LS_TRY(gop::make_stack_map(&mo, dW, F32 ? gop::MAP_F32 : gop::MAP_BF16, V, d, 1, d, V * d, 32));
+      LS_TRY((gop::launch<NP, false, true, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(mz_mn, mh_mn, mo, mo, gw, rn, st)));
+    }
+  }
+  return LS_OK;
+}
+
+int run_vocab(const VocabArgs& a, bool grad, size_t ws_bytes, cudaStream_t st) {
+  const Plan p = make_plan(a.m, a.rows, a.V, a.d, a.dtype, grad);
+  if (ws_bytes < p.total || reinterpret_cast<uintptr_t>(a.ws) % 256 != 0) return LS_ERR_STATE_SIZE;
+  const size_t eb = a.dtype == LS_DTYPE_BF16 ? 2 : 4;
+  if (a.rows == 0) {
+    LS_TRY(cudaMemsetAsync(a.loss, 0, a.m * sizeof(float), st));
+    if (grad)
+      for (int i = 0; i < a.m; ++i)
+        LS_TRY(cudaMemsetAsync(static_cast<char*>(a.dW) + i * a.dw_stride * eb, 0, (size_t)a.V * a.d * eb, st));
+    return LS_OK;
+  }
+  if (grad)
+    LS_TRY(launch_dep(vocab_count_kernel, dim3(a.m), dim3(1024), 0, st, 1, a.labels, a.rows, (int)a.V,
+                      reinterpret_cast<float*>(a.ws + p.o_inv)));
+  for (int i = 0; i < a.m; ++i) {
+    const int rc = p.f32 ? run_replica<float, 3>(a, p, i, st) : run_replica<__nv_bfloat16, 1>(a, p, i, st);
+    if (rc != LS_OK) return rc;
+  }
+  const float* row_loss = a.row_loss ? a.row_loss : reinterpret_cast<const float*>(a.ws + p.o_rowloss);
+  LS_TRY(launch_dep(vocab_mean_kernel, dim3(a.m), dim3(1024), 0, st, 1, row_loss, a.labels, a.rows, (int)a.V, a.loss));
+  return LS_OK;
+}
+
+bool off(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+int check_call(const VocabArgs& a, bool grad) {
+  int rc = check_sizes(a.m, a.rows, a.V, a.d, a.dtype);
+  if (rc != LS_OK) return rc;
+  if (a.W == nullptr || a.loss == nullptr || a.ws == nullptr) return LS_ERR_INVALID_ARG;
+  if (a.rows > 0 && (a.h == nullptr || a.labels == nullptr)) return LS_ERR_INVALID_ARG;
+  const size_t eb = a.dtype == LS_DTYPE_BF16 ? 2 : 4;
+  if (off(a.h, eb) || off(a.W, eb) || off(a.labels, 4) || off(a.loss, 4) || off(a.row_loss, 4) || off(a.lse, 4))
+    return LS_ERR_INVALID_ARG;
+  if (a.m > 1 && (a.h_stride < a.rows * a.d || a.w_stride < a.V * a.d)) return LS_ERR_INVALID_ARG;
+  // rows of whole 16 bytes are moved by bulk copies, which start on 16-byte boundaries
+  const int per = a.dtype == LS_DTYPE_BF16 ? 8 : 4;
+  const bool whole = a.d % per == 0, many = a.m > 1;
+  if (whole && (off(a.h, 16) || off(a.W, 16) || (many && (a.h_stride % per != 0 || a.w_stride % per != 0))))
+    return LS_ERR_INVALID_ARG;
+  if (grad) {
+    if (a.dW == nullptr || (a.rows > 0 && a.dh == nullptr) || off(a.dW, eb) || off(a.dh, eb)) return LS_ERR_INVALID_ARG;
+    if (a.m > 1 && (a.dh_stride < a.rows * a.d || a.dw_stride < a.V * a.d)) return LS_ERR_INVALID_ARG;
+    if (whole && (off(a.dh, 16) || off(a.dW, 16) || (many && (a.dh_stride % per != 0 || a.dw_stride % per != 0))))
+      return LS_ERR_INVALID_ARG;
+    if (!isfinite(a.scale)) return LS_ERR_INVALID_ARG;
+  }
+  return LS_OK;
+}
+
+}  // namespace
+}  // namespace ls
+
+extern "C" int ls_vocab_loss_ws_bytes(int m, int64_t rows, int64_t vocab, int d, int dtype, int grad, size_t* bytes) {
+  using namespace ls;
+  int rc = check_sizes(m, rows, vocab, d, dtype);
+  if (rc != LS_OK) return rc;
+  if (bytes == nullptr) return LS_ERR_INVALID_ARG;
+  *bytes = make_plan(m, rows, vocab, d, dtype, grad != 0).total;
+  return LS_OK;
+}
+
+extern "C" int ls_vocab_loss(const void* h_dev, const void* W_dev, const int32_t* labels_dev, int m, int64_t rows,
+                             int64_t vocab, int d, int64_t h_stride, int64_t w_stride, int dtype, float* loss_dev,
+                             float* row_loss_dev, float* lse_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  using namespace ls;
+  VocabArgs a{};
+  a.h = h_dev; a.W = W_dev; a.labels = labels_dev; a.m = m; a.rows = rows; a.V = vocab; a.d = d;
+  a.h_stride = h_stride; a.w_stride = w_stride; a.dtype = dtype;
+  a.loss = loss_dev; a.row_loss = row_loss_dev; a.lse = lse_dev; a.ws = static_cast<char*>(ws_dev);
+  int rc = check_call(a, false);
+  return rc != LS_OK ? rc : run_vocab(a, false, ws_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" int ls_vocab_loss_grad(const void* h_dev, const void* W_dev, const int32_t* labels_dev, int m, int64_t rows,
+                                  int64_t vocab, int d, int64_t h_stride, int64_t w_stride, int dtype, float scale,
+                                  float* loss_dev, float* row_loss_dev, float* lse_dev, void* dh_dev, int64_t dh_stride,
+                                  void* dW_dev, int64_t dw_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  using namespace ls;
+  VocabArgs a{};
+  a.h = h_dev; a.W = W_dev; a.labels = labels_dev; a.m = m; a.rows = rows; a.V = vocab; a.d = d;
+  a.h_stride = h_stride; a.w_stride = w_stride; a.dh_stride = dh_stride; a.dw_stride = dw_stride; a.dtype = dtype;
+  a.scale = scale;
+  a.loss = loss_dev; a.row_loss = row_loss_dev; a.lse = lse_dev; a.dh = dh_dev; a.dW = dW_dev;
+  a.ws = static_cast<char*>(ws_dev);
+  int rc = check_call(a, true);
+  return rc != LS_OK ? rc : run_vocab(a, true, ws_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
