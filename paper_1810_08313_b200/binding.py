@@ -7,6 +7,7 @@ or loaded this module raises; there is no other implementation to fall back to.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -315,82 +316,112 @@ def linear_loss_static(W, bias, x, y, chunk_rows: int, chunk_loss, loss: str = "
 # allocated.  `workspace`: a uint8 tensor of the size the matching *_workspace function names, for callers that keep
 # one; calls that may overlap on the GPU need their own.  `stream`: a torch stream, the current one by default.
 
+_TORCH = None
+_OP_DTYPE = {}
+
+
+def _op_torch():
+    """torch, imported once (importing this module stays cheap)."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _OP_DTYPE.update({torch.float32: 0, torch.bfloat16: 1})
+        _TORCH = torch
+    return _TORCH
+
+
 def _op_dtype(t, name: str) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return 0
-    if t.dtype == torch.bfloat16:
-        return 1
-    raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    dt = _OP_DTYPE.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return dt
 
 
 class _Op:
-    """Checks the tensors of one call, lends out its workspace and keeps track of what the stream uses."""
+    """Checks the tensors of one call, lends out its workspace and keeps track of what the stream uses.  The common
+    case (contiguous tensors, the current stream and device) takes a few attribute reads per tensor: a call of a
+    small operator costs what its Python does."""
+
+    __slots__ = ("torch", "device", "stream", "raw")
 
     def __init__(self, first, stream):
-        import torch
-        self.torch = torch
+        self.torch = torch = _op_torch()
         if not (isinstance(first, torch.Tensor) and first.is_cuda):
             raise ValueError("CUDA tensors expected")
         self.device = first.device
-        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
-        if self.stream.device != self.device:
-            raise ValueError("the stream belongs to another device than the tensors")
-        self.side = self.stream != torch.cuda.current_stream(self.device)
+        if stream is None:
+            self.stream = None
+            self.raw = torch._C._cuda_getCurrentRawStream(self.device.index)
+        else:
+            if stream.device != self.device:
+                raise ValueError("the stream belongs to another device than the tensors")
+            self.raw = int(stream.cuda_stream)
+            # tensors of the current stream that another one uses
+            self.stream = stream if stream != torch.cuda.current_stream(self.device) else None
 
     def stack(self, t, name: str, tail, m: Optional[int], dtype=None):
         """t as [m][*tail] (m None: from t); returns (pointer, m, stride between replicas)."""
         torch = self.torch
-        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == self.device):
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
             raise ValueError(f"{name} must be a tensor on {self.device}")
         if dtype is not None and t.dtype != dtype:
             raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-        tail = tuple(int(n) for n in tail)
-        if t.dim() == len(tail):
-            t = t.unsqueeze(0)
-        if t.dim() != len(tail) + 1 or tuple(t.shape[1:]) != tail or (m is not None and t.shape[0] != m):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{'m' if m is None else m}] + {list(tail)}")
-        want = 1
-        for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-            if size > 1 and step != want:
-                raise ValueError(f"{name}: a replica must be dense and row-major")
-            want *= size
-        if t.shape[0] > 1 and t.stride(0) < want:
-            raise ValueError(f"{name}: the replicas overlap")
-        if self.side:
+        shape = tuple(t.shape)
+        lead = len(shape) - len(tail)
+        if lead not in (0, 1) or shape[lead:] != tail or (m is not None and (shape[0] if lead else 1) != m):
+            raise ValueError(f"{name} has shape {shape}, expected [{'m' if m is None else m}] + {list(tail)}")
+        n = 1
+        for size in tail:
+            n *= size
+        k = shape[0] if lead else 1
+        step = n
+        if not t.is_contiguous():
+            want = 1
+            for size, st in zip(reversed(tail), reversed(t.stride()[lead:])):
+                if size > 1 and st != want:
+                    raise ValueError(f"{name}: a replica must be dense and row-major")
+                want *= size
+            if k > 1:
+                step = t.stride(0)
+                if step < n:
+                    raise ValueError(f"{name}: the replicas overlap")
+        if self.stream is not None:
             t.record_stream(self.stream)
-        return t.data_ptr(), t.shape[0], t.stride(0) if t.shape[0] > 1 else want
+        return t.data_ptr(), k, step
 
     def dense(self, t, name: str, shape, dtype):
         """t as a dense tensor of this shape (one replica may leave the first axis out)."""
-        ptr, _, stride = self.stack(t, name, shape[1:], shape[0], dtype)
-        n = 1
-        for v in shape[1:]:
-            n *= int(v)
-        if shape[0] > 1 and n > 0 and stride != n:
+        if not (isinstance(t, self.torch.Tensor) and t.is_contiguous()):
             raise ValueError(f"{name} must be contiguous")
-        return ptr
+        return self.stack(t, name, shape[1:], shape[0], dtype)[0]
 
-    def new(self, shape, dtype):
-        t = self.torch.empty(shape, dtype=dtype, device=self.device)
-        if self.side:
+    def new(self, like, shape, dtype):
+        t = like.new_empty(shape, dtype=dtype)
+        if self.stream is not None:
             t.record_stream(self.stream)
         return t
 
-    def workspace(self, given, nbytes: int):
+    def workspace(self, like, given, nbytes: int):
         t = given
         if t is None:
-            t = self.new((nbytes + 256,), self.torch.uint8)
+            t = self.new(like, (nbytes + 256,), self.torch.uint8)
         elif not (t.is_cuda and t.device == self.device and t.dtype == self.torch.uint8 and t.is_contiguous()):
             raise ValueError("workspace must be a contiguous uint8 tensor on the device of the call")
-        elif self.side:
+        elif self.stream is not None:
             t.record_stream(self.stream)
-        base = (t.data_ptr() + 255) // 256 * 256
-        return base, t.data_ptr() + t.numel() - base, t
+        start = t.data_ptr()
+        base = (start + 255) & -256
+        return base, start + t.numel() - base, t
 
     def call(self, name: str, *args):
-        with self.torch.cuda.device(self.device):
-            _check(getattr(_lib(), name)(*args, int(self.stream.cuda_stream)), name)
+        fn = getattr(_LIB or _lib(), name)
+        if self.torch._C._cuda_getDevice() == self.device.index:
+            code = fn(*args, self.raw)
+        else:
+            with self.torch.cuda.device(self.device):
+                code = fn(*args, self.raw)
+        if code != LS_OK:
+            raise LsError(code, name)
 
 
 def _like(t, lead, out):
@@ -398,6 +429,7 @@ def _like(t, lead, out):
     return out if t.dim() == lead else out.squeeze(0)
 
 
+@functools.lru_cache(maxsize=256)
 def _ws_bytes(name: str, *args) -> int:
     n = C.c_size_t()
     _check(getattr(_lib(), name)(*args, C.byref(n)), name)
@@ -429,9 +461,9 @@ def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None, mean=None, rst
         bp, _, bs = op.stack(bias, "bias", (d,), m, f32)
         if m > 1 and bs != ws:
             raise ValueError("weight and bias must have the same distance between replicas")
-    y = op.new((m, rows, d), x.dtype) if out is None else out
-    mean_t = op.new((m, rows), f32) if mean is None else mean
-    rstd_t = op.new((m, rows), f32) if rstd is None else rstd
+    y = op.new(x, (m, rows, d), x.dtype) if out is None else out
+    mean_t = op.new(x, (m, rows), f32) if mean is None else mean
+    rstd_t = op.new(x, (m, rows), f32) if rstd is None else rstd
     yp, _, ys = op.stack(y, "out", (rows, d), m, x.dtype)
     mp, rp = op.dense(mean_t, "mean", (m, rows), f32), op.dense(rstd_t, "rstd", (m, rows), f32)
     op.call("ls_layer_norm", xp, wp, bp, m, rows, d, xs, ws, dt, float(eps), yp, ys, mp, rp)
@@ -456,21 +488,21 @@ def layer_norm_grad(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None
     dyp, _, dys = op.stack(dy, "dy", (rows, d), m, x.dtype)
     wp, _, ws = op.stack(weight, "weight", (d,), m, f32)
     mp, rp = op.dense(mean, "mean", (m, rows), f32), op.dense(rstd, "rstd", (m, rows), f32)
-    dx_t = op.new((m, rows, d), x.dtype) if dx is None else dx
+    dx_t = op.new(x, (m, rows, d), x.dtype) if dx is None else dx
     dxp, _, dxs = op.stack(dx_t, "dx", (rows, d), m, x.dtype)
-    dw_t = op.new((m, d), f32) if dweight is None else dweight
+    dw_t = op.new(x, (m, d), f32) if dweight is None else dweight
     dwp, _, dps = op.stack(dw_t, "dweight", (d,), m, f32)
     if dbias is None:
         # beside dweight, with its distance between replicas
         db_t = op.torch.empty_strided((m, d), (dps, 1), dtype=f32, device=op.device)
-        if op.side:
+        if op.stream is not None:
             db_t.record_stream(op.stream)
     else:
         db_t = dbias
     dbp, _, dbs = op.stack(db_t, "dbias", (d,), m, f32)
     if m > 1 and dbs != dps:
         raise ValueError("dweight and dbias must have the same distance between replicas")
-    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_layer_norm_grad_ws_bytes", m, rows, d))
+    base, nbytes, keep = op.workspace(x, workspace, _ws_bytes("ls_layer_norm_grad_ws_bytes", m, rows, d))
     op.call("ls_layer_norm_grad", dyp, xp, wp, mp, rp, m, rows, d, dys, xs, ws, dt, dxp, dxs, dwp, dbp, dps, base, nbytes)
     return (dx_t if dx is not None else _like(x, 3, dx_t), dw_t if dweight is not None else _like(x, 3, dw_t),
             db_t if dbias is not None else _like(x, 3, db_t))
@@ -502,12 +534,12 @@ def vocab_loss(h, W, labels, loss=None, row_loss=None, lse=None, workspace=None,
     op = _Op(h, stream)
     dt, m, rows, d, vocab, hp, hs, wp, ws, lp = _vocab_args(op, h, W, labels)
     f32 = op.torch.float32
-    loss_t = op.new((m,), f32) if loss is None else loss
-    rl_t = op.new((m, rows), f32) if row_loss is None else row_loss
-    lse_t = op.new((m, rows), f32) if lse is None else lse
+    loss_t = op.new(h, (m,), f32) if loss is None else loss
+    rl_t = op.new(h, (m, rows), f32) if row_loss is None else row_loss
+    lse_t = op.new(h, (m, rows), f32) if lse is None else lse
     outs = (op.dense(loss_t, "loss", (m,), f32), op.dense(rl_t, "row_loss", (m, rows), f32),
             op.dense(lse_t, "lse", (m, rows), f32))
-    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_vocab_loss_ws_bytes", m, rows, vocab, d, dt, 0))
+    base, nbytes, keep = op.workspace(h, workspace, _ws_bytes("ls_vocab_loss_ws_bytes", m, rows, vocab, d, dt, 0))
     op.call("ls_vocab_loss", hp, wp, lp, m, rows, vocab, d, hs, ws, dt, *outs, base, nbytes)
     return (loss_t, rl_t if row_loss is not None else _like(h, 3, rl_t), lse_t if lse is not None else _like(h, 3, lse_t))
 
@@ -519,16 +551,16 @@ def vocab_loss_grad(h, W, labels, scale: float = 1.0, dh=None, dW=None, loss=Non
     op = _Op(h, stream)
     dt, m, rows, d, vocab, hp, hs, wp, ws, lp = _vocab_args(op, h, W, labels)
     f32 = op.torch.float32
-    loss_t = op.new((m,), f32) if loss is None else loss
-    rl_t = op.new((m, rows), f32) if row_loss is None else row_loss
-    lse_t = op.new((m, rows), f32) if lse is None else lse
+    loss_t = op.new(h, (m,), f32) if loss is None else loss
+    rl_t = op.new(h, (m, rows), f32) if row_loss is None else row_loss
+    lse_t = op.new(h, (m, rows), f32) if lse is None else lse
     outs = (op.dense(loss_t, "loss", (m,), f32), op.dense(rl_t, "row_loss", (m, rows), f32),
             op.dense(lse_t, "lse", (m, rows), f32))
-    dh_t = op.new((m, rows, d), h.dtype) if dh is None else dh
-    dW_t = op.new((m, vocab, d), h.dtype) if dW is None else dW
+    dh_t = op.new(h, (m, rows, d), h.dtype) if dh is None else dh
+    dW_t = op.new(h, (m, vocab, d), h.dtype) if dW is None else dW
     dhp, _, dhs = op.stack(dh_t, "dh", (rows, d), m, h.dtype)
     dwp, _, dws = op.stack(dW_t, "dW", (vocab, d), m, h.dtype)
-    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_vocab_loss_ws_bytes", m, rows, vocab, d, dt, 1))
+    base, nbytes, keep = op.workspace(h, workspace, _ws_bytes("ls_vocab_loss_ws_bytes", m, rows, vocab, d, dt, 1))
     op.call("ls_vocab_loss_grad", hp, wp, lp, m, rows, vocab, d, hs, ws, dt, float(scale), *outs, dhp, dhs, dwp, dws, base,
             nbytes)
     return (loss_t, rl_t if row_loss is not None else _like(h, 3, rl_t), lse_t if lse is not None else _like(h, 3, lse_t),
@@ -548,9 +580,9 @@ def orthogonalize(u, steps: int = 5, out=None, workspace=None, stream=None):
         raise ValueError("u must be [m][rows][cols] or [rows][cols]")
     rows, cols = u.shape[-2:]
     up, m, us = op.stack(u, "u", (rows, cols), None)
-    o = op.new((m, rows, cols), u.dtype) if out is None else out
+    o = op.new(u, (m, rows, cols), u.dtype) if out is None else out
     outp, _, outs = op.stack(o, "out", (rows, cols), m, u.dtype)
-    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
+    base, nbytes, keep = op.workspace(u, workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
     op.call("ls_orthogonalize", up, m, rows, cols, us, dt, int(steps), outp, outs, base, nbytes)
     return o if out is not None else _like(u, 3, o)
 
@@ -569,7 +601,7 @@ def muon_step(w, v, g, lr: float, momentum: float = 0.95, nesterov: bool = True,
     wp, m, ws = op.stack(w, "w", (rows, cols), None, f32)
     vp, _, vs = op.stack(v, "v", (rows, cols), m, f32)
     gp, _, gs = op.stack(g, "g", (rows, cols), m)
-    base, nbytes, keep = op.workspace(workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
+    base, nbytes, keep = op.workspace(w, workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
     op.call("ls_muon_step", wp, vp, gp, m, rows, cols, ws, vs, gs, dt, float(lr), float(momentum), int(bool(nesterov)),
             int(steps), base, nbytes)
 
