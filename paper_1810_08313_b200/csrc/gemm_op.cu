@@ -37,24 +37,32 @@ int* device_error_word() {
   return g_error_addr[dev];
 }
 
-int make_stack_map(CUtensorMap* out, const void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
-                   int64_t plane, int box_rows) {
+static int make_map(CUtensorMap* out, const void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
+                    int64_t plane, int row_bytes, int box_rows, bool swizzled) {
   EncodeTiledFn fn = encode_fn();
   if (fn == nullptr) return cudaErrorNotSupported;
   const int64_t eb = type == MAP_F32 ? 4 : 2;
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
   cuuint64_t strides[2] = {(cuuint64_t)(ld * eb), (cuuint64_t)(plane * eb)};
-  cuuint32_t box[3] = {(cuuint32_t)((type >= MAP_F16_S ? 64 : 128) / eb), (cuuint32_t)box_rows, 1};
+  cuuint32_t box[3] = {(cuuint32_t)(row_bytes / eb), (cuuint32_t)box_rows, 1};
   cuuint32_t es[3] = {1, 1, 1};
   const CUtensorMapDataType dt = type == MAP_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                 : type != MAP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                 : type == MAP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                    : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  CUresult r = fn(out, dt, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  type == MAP_F16_T   ? CU_TENSOR_MAP_SWIZZLE_NONE
-                  : type == MAP_F16_S ? CU_TENSOR_MAP_SWIZZLE_64B
-                                      : CU_TENSOR_MAP_SWIZZLE_128B,
+  const CUtensorMapSwizzle sw = !swizzled          ? CU_TENSOR_MAP_SWIZZLE_NONE
+                                : row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B
+                                                   : CU_TENSOR_MAP_SWIZZLE_64B;
+  CUresult r = fn(out, dt, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+int make_operand_map(CUtensorMap* out, const void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
+                     int64_t plane) {
+  return make_map(out, base, type, rows, cols, planes, ld, plane, 128, 64, true);
+}
+int make_output_map(CUtensorMap* out, void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
+                    int64_t plane, int row_bytes, bool transposed) {
+  return make_map(out, base, type, rows, cols, planes, ld, plane, row_bytes, 32, !transposed);
 }
 
 }  // namespace gop

@@ -5,19 +5,25 @@
 // with A_i [M][K] and B_j [N][K] matrices of 16-bit numbers, K- or MN-major.  An operand is given as NP "pieces" whose
 // sum is the operand: one for a bf16 tensor, two fp16 pieces (22 significant bits, operands scaled into fp16's range by
 // the caller), three bf16 pieces (24 bits, all of fp32's range).  The products kept are those with i + j < NP (1, 3 or
-// 6 of them): the dropped ones are below the last bit kept.  A stage of the ring holds a 64-wide K block of all pieces
-// of both operands, so two pieces cost three products but only twice the operand traffic.
+// 6 of them): the dropped ones are below the last bit kept.  The ring's slots hold a 64-wide K block of one piece of both
+// operands; a K block's products are issued when its NP slots are there, so two pieces cost three products but only
+// twice the operand traffic.
 //
-// Persistent kernel on CTA pairs (cta_group::2), a 256 x 256 tile per pair:
-//   warp 0     TMA producer (each CTA brings its 128 rows of A and its 128 columns of B)
+// Persistent kernel on CTA pairs (cta_group::2), a 256 x NT tile per pair:
+//   warp 0     TMA producer (each CTA brings its 128 rows of A and its NT / 2 columns of B)
 //   warp 1     leader: issues the MMAs.  A tensor-memory accumulator is used for `chunk_kb` K blocks and then handed to
-//              the epilogue; two of them alternate, so that products run while the other one is collected
+//              the epilogue; 512 / NT of them take turns, so that products run while others are collected
 //   warps 2-9  epilogue: warp w owns TMEM lanes 32 (w % 4) .. + 31 (rows) and one half of the columns; a thread adds the
-//              chunks of its row's 128 columns in registers, rounding to nearest.  The tensor core's own fp32
+//              chunks of its row's NT / 2 columns in registers, rounding to nearest.  The tensor core's own fp32
 //              accumulation truncates, which biases a sum of a thousand MMAs by about 2e-5 of its value: short
 //              chunks keep that below the last bits that matter (see kChunk*), and since a tile's last chunk is
 //              collected like any other, the epilogue of a tile runs under the products of the next one.
-// Outputs leave through 4 KB of shared memory per warp and TMA stores, which clip at the tensor's edge; ragged M, N
+// NT = 256 for one piece: 64 bytes of operands per clock and SM at the full MMA rate, 1540 of 1709 TFLOP/s (2047 x 50001 x
+// 1024).  With several pieces the chunks are so short that collecting 128 columns a thread, eight dependent
+// tcgen05.ld of 16 registers, took longer than the products (52 % of the MMA rate at 2048^3 x 8): NT = 128 collects a chunk
+// with one wait and has four accumulators.
+//
+// Outputs leave through boxes of shared memory per warp and TMA stores, which clip at the tensor's edge; ragged M, N
 // and K are the zero fill of the loads and that clip.  A symmetric result is computed on and above the diagonal tiles and
 // stored twice, the second time from a transposed box.
 // Before a CTA exits, every arrival that the tensor core or the other CTA sends to its barriers has been waited for.
@@ -33,22 +39,28 @@ namespace gop {
 
 using namespace ptx;
 
-constexpr int kTile = 256;               // rows and columns of a pair's tile
+constexpr int kTileM = 256;              // rows of a pair's tile
 constexpr int kThreads = 320;            // warp 0 producer, warp 1 MMA issuer, warps 2-9 epilogue
-constexpr int kSlice = 128;              // columns of an epilogue thread: the unit of the row statistics
-constexpr int kStageBoxBytes = 4096;     // staging of one epilogue warp: 32 rows x 128 bytes
 
-template <int NP>
+// NP: pieces of an operand.  NT: columns of a pair's tile; half of them is a slice, the unit of the row statistics.
+template <int NP, int NT>
 struct Smem {
-  static constexpr int kOperand = 128 * 128;                       // 128 rows (or columns) x 64 numbers
-  static constexpr int kStage = 2 * NP * kOperand;
-  static constexpr int kStages = NP == 1 ? 6 : NP == 2 ? 3 : 2;
-  static constexpr int kRing = kStages * kStage;
-  static constexpr int kOut = 8 * kStageBoxBytes;
-  static constexpr int kBars = 2 * kStages + 4;
+  static constexpr int kA = 128 * 128;                             // 128 rows x 64 numbers
+  static constexpr int kB = NT / 2 * 128;
+  static constexpr int kSlot = kA + kB;
+  static constexpr int kSlots = NT == 256 ? 6 : 7;
+  static constexpr int kRing = kSlots * kSlot;
+  // boxes of an epilogue warp: 32 rows of kBoxRow bytes, kBoxes of them in turn
+  static constexpr int kBoxRow = NP == 1 ? 128 : 64;
+  static constexpr int kBox = 32 * kBoxRow;
+  static constexpr int kBoxes = NP == 1 ? 1 : NT == 256 ? 2 : 3;
+  static constexpr int kOut = 8 * kBoxes * kBox;
+  static constexpr int kAccs = 512 / NT;
+  static constexpr int kBars = 2 * kSlots + 2 * kAccs;
   static constexpr int kTotal = 1024 + kRing + kOut + kBars * 8 + 16;
   static_assert(kTotal <= 227 * 1024, "shared memory budget");
 };
+constexpr int box_row(int np) { return np == 1 ? 128 : 64; }
 
 enum Epi {
   EPI_F32,        // fp32 C = alpha acc (reduce: C += alpha acc)
@@ -64,6 +76,7 @@ struct Params {
   int num_kb, kb_per_split, chunk_kb;
   int total;                             // tiles of the launch
   int tri;                               // 1: only tiles on or above the diagonal (symmetric C)
+  int per, step;                         // tiles of one batch entry and split; 256 / NT
   int n_fast;                            // 1: neighbouring pairs take neighbouring columns, else neighbouring rows
   int a_z0, a_zstep, b_z0, b_zstep;      // plane of batch entry z: z0 + z * zstep (+ piece)
   int c_z0, c_zstep;
@@ -71,7 +84,7 @@ struct Params {
   float alpha;
   const float* alpha_dev;                // EPI_F32, EPI_BF16: a further factor of alpha in device memory, or null
   int reduce;                            // EPI_F32: C += instead of C =
-  // row statistics: slice t = column / 128 of row r at [t * stat_ld + r]
+  // row statistics: slice t = column / (NT / 2) of row r at [t * stat_ld + r]
   float* stat_max;                       // slice maximum * log2(e)
   float* stat_sum;                       // sum over the slice of exp(acc - slice maximum)
   int64_t stat_ld;
@@ -88,16 +101,16 @@ struct Tile { int m, n, split, z; };
 
 __device__ __forceinline__ Tile tile_of(const Params& p, int t) {
   Tile r;
-  const int per = p.tri ? p.m_tiles * (p.m_tiles + 1) / 2 : p.m_tiles * p.n_tiles;
+  const int per = p.per;
   const int q = t / per, i = t - q * per;
   r.z = q / p.splits;
   r.split = q - r.z * p.splits;
   if (p.tri) {
-    int n = (int)((sqrtf(8.f * (float)i + 1.f) - 1.f) * 0.5f);
-    while ((n + 1) * (n + 2) / 2 <= i) ++n;
-    while (n * (n + 1) / 2 > i) --n;
-    r.n = n;
-    r.m = i - n * (n + 1) / 2;
+    // row block m has the column blocks from its diagonal on: step * m .. n_tiles - 1, step = 256 / NT
+    int m = 0, left = i;
+    for (int w = p.n_tiles; left >= w; w -= p.step) { left -= w; ++m; }
+    r.m = m;
+    r.n = m * p.step + left;
   } else if (p.n_fast) {
     r.m = i / p.n_tiles;
     r.n = i - r.m * p.n_tiles;
@@ -126,9 +139,10 @@ __device__ __forceinline__ void add_box(const CUtensorMap* m, const void* src, i
                "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z)
                : "memory");
 }
-// the staging box may be written again: the bulk store has read it
+// The next of a warp's boxes may be written: the bulk store that used it last has read it.
+template <int NBOX>
 __device__ __forceinline__ void box_free(int lane) {
-  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(NBOX - 1) : "memory");
   __syncwarp();
 }
 // hand the box over: all lanes have written it
@@ -141,24 +155,37 @@ __device__ __forceinline__ void box_send(const CUtensorMap* m, const void* box, 
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
+// piece u of 16 bytes of this lane's row, as the tensor map's swizzle places it
+template <int ROW>
+__device__ __forceinline__ uint4* box_piece(uint8_t* box, int lane, int u) {
+  return reinterpret_cast<uint4*>(box + lane * ROW + ((ROW == 128 ? u ^ (lane & 7) : u ^ ((lane >> 1) & 3)) << 4));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<uint32_t*>(&h);
+}
 
-template <int NP, bool F16, bool A_MN, bool B_MN, int EPI>
+template <int NP, int NT, bool F16, bool A_MN, bool B_MN, int EPI>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmCT, const Params p) {
-  using L = Smem<NP>;
-  constexpr int STAGES = L::kStages;
-  constexpr uint32_t IDESC = make_idesc(F16 ? 0u : 1u, A_MN, B_MN, 256, 256);
+  using L = Smem<NP, NT>;
+  constexpr int SLOTS = L::kSlots, ACCS = L::kAccs, HALF = NT / 2;
+  constexpr uint32_t IDESC = make_idesc(F16 ? 0u : 1u, A_MN, B_MN, 256, NT);
   constexpr uint32_t TMEM_COLS = 512;
 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* out_base = smem + L::kRing;
   uint64_t* full = reinterpret_cast<uint64_t*>(out_base + L::kOut);
-  uint64_t* empty = full + STAGES;
-  uint64_t* acc_full = empty + STAGES;         // [2]
-  uint64_t* acc_empty = acc_full + 2;          // [2] leader's: sixteen epilogue warps of the pair
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  uint64_t* empty = full + SLOTS;
+  uint64_t* acc_full = empty + SLOTS;          // [ACCS]
+  uint64_t* acc_empty = acc_full + ACCS;       // [ACCS] leader's: sixteen epilogue warps of the pair
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + ACCS);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();
@@ -166,8 +193,8 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   bool failed = false;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], 16); }
+    for (int s = 0; s < SLOTS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int s = 0; s < ACCS; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], 16); }
     fence_mbar_init();
     prefetch_tmap(&tmA);
     prefetch_tmap(&tmB);
@@ -186,151 +213,195 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   grid_dep_wait();
   grid_dep_launch();
 
+  // The loops of warps 0 and 1 run in all lanes (the waits too), so that addresses and descriptors are warp-uniform values;
+  // one lane issues.  Slots and accumulators are counted with a place in the ring and the parity of the round.
   if (warp == 0) {
-    if (elect_one()) {
-      const uint64_t pol = l2_policy(0);
-      const uint32_t full_leader = map_to_rank(smem_u32(&full[0]), 0);
-      int it = 0;
-      for (int t = pair; t < p.total && !failed; t += pairs) {
-        const Tile tl = tile_of(p, t);
-        const int k0 = tl.split * p.kb_per_split;
-        const int k1 = min(p.num_kb, k0 + p.kb_per_split);
-        const int az = p.a_z0 + tl.z * p.a_zstep, bz = p.b_z0 + tl.z * p.b_zstep;
-        const int ma = tl.m * kTile + rank * 128, nb = tl.n * kTile + rank * 128;
-        for (int kb = k0; kb < k1; ++kb, ++it) {
-          const int s = it % STAGES;
-          if (it >= STAGES && !mbar_wait(&empty[s], ((it / STAGES) - 1) & 1)) { atomicExch(p.err, 31); failed = true; break; }
-          if (rank == 0) mbar_expect_tx(&full[s], 2 * L::kStage);      // both CTAs' bytes
-          const uint32_t bar = full_leader + (uint32_t)(s * 8);
-          uint8_t* sa = smem + s * L::kStage;
-          uint8_t* sb = sa + NP * L::kOperand;
+    const bool lead = elect_one();
+    const uint64_t pol = l2_policy(0);
+    const uint32_t full_leader = map_to_rank(smem_u32(&full[0]), 0);
+    int s = 0, round = 0;
+    for (int t = pair; t < p.total && !failed; t += pairs) {
+      const Tile tl = tile_of(p, t);
+      const int k0 = tl.split * p.kb_per_split;
+      const int k1 = min(p.num_kb, k0 + p.kb_per_split);
+      const int az = p.a_z0 + tl.z * p.a_zstep, bz = p.b_z0 + tl.z * p.b_zstep;
+      const int ma = tl.m * kTileM + rank * 128, nb = tl.n * NT + rank * HALF;
+      for (int kb = k0; kb < k1 && !failed; ++kb) {
 #pragma unroll
-          for (int q = 0; q < NP; ++q) {
+        for (int q = 0; q < NP; ++q) {
+          if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[s], (round - 1) & 1))) { failed = true; break; }
+          if (lead) {
+            if (rank == 0) mbar_expect_tx(&full[s], 2 * L::kSlot);      // both CTAs' bytes
+            const uint32_t bar = full_leader + (uint32_t)(s * 8);
+            uint8_t* sa = smem + s * L::kSlot;
+            uint8_t* sb = sa + L::kA;
             if (A_MN) {
-              tma_load_3d_pair(sa + q * L::kOperand, &tmA, bar, ma, kb * 64, az + q, pol);
-              tma_load_3d_pair(sa + q * L::kOperand + 8192, &tmA, bar, ma + 64, kb * 64, az + q, pol);
+              tma_load_3d_pair(sa, &tmA, bar, ma, kb * 64, az + q, pol);
+              tma_load_3d_pair(sa + 8192, &tmA, bar, ma + 64, kb * 64, az + q, pol);
             } else {
-              tma_load_3d_pair(sa + q * L::kOperand, &tmA, bar, kb * 64, ma, az + q, pol);
+              tma_load_3d_pair(sa, &tmA, bar, kb * 64, ma, az + q, pol);
+              tma_load_3d_pair(sa + 8192, &tmA, bar, kb * 64, ma + 64, az + q, pol);
             }
-            if (B_MN) {
-              tma_load_3d_pair(sb + q * L::kOperand, &tmB, bar, nb, kb * 64, bz + q, pol);
-              tma_load_3d_pair(sb + q * L::kOperand + 8192, &tmB, bar, nb + 64, kb * 64, bz + q, pol);
-            } else {
-              tma_load_3d_pair(sb + q * L::kOperand, &tmB, bar, kb * 64, nb, bz + q, pol);
+#pragma unroll
+            for (int c = 0; c < HALF / 64; ++c) {
+              if (B_MN) tma_load_3d_pair(sb + c * 8192, &tmB, bar, nb + c * 64, kb * 64, bz + q, pol);
+              else tma_load_3d_pair(sb + c * 8192, &tmB, bar, kb * 64, nb + c * 64, bz + q, pol);
             }
           }
+          __syncwarp();
+          if (++s == SLOTS) { s = 0; ++round; }
         }
       }
-      // the releases of the last stages arrive here from the leader's tensor core: wait for them before leaving
-      for (int s = 0; s < STAGES && s < it && !failed; ++s) {
-        const int uses = (it - 1 - s) / STAGES + 1;
-        if (!mbar_wait(&empty[s], (uses - 1) & 1)) { atomicExch(p.err, 35); failed = true; }
-      }
     }
+    // the releases of the last slots arrive here from the leader's tensor core: wait for them before leaving
+    for (int i = 0; i < SLOTS && !failed; ++i) {
+      const int uses = round + (i < s ? 1 : 0);
+      if (uses > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[i], (uses - 1) & 1))) failed = true;
+    }
+    if (failed && lane == 0) atomicExch(p.err, 31);
   } else if (warp == 1) {
-    if (rank == 0 && elect_one()) {
-      int it = 0, ch = 0;
+    if (rank == 0) {
+      const bool lead = elect_one();
+      constexpr uint32_t HI = smem_desc_hi(1024);
+      const uint32_t a_lo0 = smem_desc_lo(smem_u32(smem), A_MN ? 8192 : 16);
+      const uint32_t b_lo0 = smem_desc_lo(smem_u32(smem) + L::kA, B_MN ? 8192 : 16);
+      int s = 0, round = 0, acc = 0, acc_round = 0;
       for (int t = pair; t < p.total && !failed; t += pairs) {
         const Tile tl = tile_of(p, t);
         const int k0 = tl.split * p.kb_per_split;
         const int nk = min(p.num_kb, k0 + p.kb_per_split) - k0;
-        for (int kb = 0; kb < nk; ++kb, ++it) {
-          const int in_chunk = kb % p.chunk_kb;
-          if (in_chunk == 0 && ch >= 2 && !mbar_wait(&acc_empty[ch & 1], ((ch >> 1) - 1) & 1)) {
-            atomicExch(p.err, 32); failed = true; break;
+        int in_chunk = 0;
+        for (int kb = 0; kb < nk; ++kb) {
+          if (in_chunk == 0 && acc_round > 0 &&
+              !__all_sync(0xffffffffu, mbar_wait(&acc_empty[acc], (acc_round - 1) & 1))) { failed = true; break; }
+          uint32_t a_lo[NP], b_lo[NP];
+          int first_slot = s;
+          bool got = true;
+#pragma unroll
+          for (int q = 0; q < NP; ++q) {
+            a_lo[q] = a_lo0 + (uint32_t)(s * (L::kSlot >> 4));
+            b_lo[q] = b_lo0 + (uint32_t)(s * (L::kSlot >> 4));
+            got = got && mbar_wait(&full[s], round & 1);
+            if (++s == SLOTS) { s = 0; ++round; }
           }
-          const int s = it % STAGES;
-          if (!mbar_wait(&full[s], (it / STAGES) & 1)) { atomicExch(p.err, 33); failed = true; break; }
+          if (!__all_sync(0xffffffffu, got)) { failed = true; break; }
           tc_fence_after_sync();
-          const uint32_t d_tmem = tmem_base + (uint32_t)((ch & 1) * kTile);
-          const uint32_t a_addr = smem_u32(smem + s * L::kStage);
-          const uint32_t b_addr = a_addr + NP * L::kOperand;
-          bool first = in_chunk == 0;
-          // small products first
+          const bool last = in_chunk == p.chunk_kb - 1 || kb == nk - 1;
+          if (lead) {
+            const uint32_t d_tmem = tmem_base + (uint32_t)(acc * NT);
+            // small products first
 #pragma unroll
-          for (int i = NP - 1; i >= 0; --i)
+            for (int i = NP - 1; i >= 0; --i)
 #pragma unroll
-            for (int j = NP - 1 - i; j >= 0; --j)
+              for (int j = NP - 1 - i; j >= 0; --j)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const uint64_t da = make_smem_desc(a_addr + i * L::kOperand + (A_MN ? k * 2048 : k * 32), A_MN ? 8192 : 16, 1024);
-                const uint64_t db = make_smem_desc(b_addr + j * L::kOperand + (B_MN ? k * 2048 : k * 32), B_MN ? 8192 : 16, 1024);
-                mma_bf16_pair(d_tmem, da, db, IDESC, first ? 0u : 1u);
-                first = false;
-              }
-          mma_commit_pair(&empty[s]);
-          if (in_chunk == p.chunk_kb - 1 || kb == nk - 1) {
-            mma_commit_pair(&acc_full[ch & 1]);
-            ++ch;
+                for (int k = 0; k < 4; ++k) {
+                  const bool begin = i == NP - 1 && j == 0 && k == 0;
+                  mma_f16_pair_lo(d_tmem, a_lo[i] + (A_MN ? k * 128 : k * 2), b_lo[j] + (B_MN ? k * 128 : k * 2), HI, IDESC,
+                                  begin && in_chunk == 0 ? 0u : 1u);
+                }
+#pragma unroll
+            for (int q = 0; q < NP; ++q) {
+              mma_commit_pair(&empty[first_slot]);
+              if (++first_slot == SLOTS) first_slot = 0;
+            }
+            if (last) mma_commit_pair(&acc_full[acc]);
+          }
+          __syncwarp();
+          ++in_chunk;
+          if (last) {
+            in_chunk = 0;
+            if (++acc == ACCS) { acc = 0; ++acc_round; }
           }
         }
       }
       // both CTAs' epilogues have let go of the last accumulators
-      for (int b = 0; b < 2 && b < ch && !failed; ++b) {
-        const int uses = (ch - 1 - b) / 2 + 1;
-        if (!mbar_wait(&acc_empty[b], (uses - 1) & 1)) { atomicExch(p.err, 36); failed = true; }
+      for (int i = 0; i < ACCS && !failed; ++i) {
+        const int uses = acc_round + (i < acc ? 1 : 0);
+        if (uses > 0 && !__all_sync(0xffffffffu, mbar_wait(&acc_empty[i], (uses - 1) & 1))) failed = true;
       }
+      if (failed && lane == 0) atomicExch(p.err, 32);
     }
   } else {
+    constexpr int G = HALF / 32;             // groups of 32 columns of a thread
+    constexpr int ROW = L::kBoxRow, NBOX = L::kBoxes;
     const int q = warp & 3, cs = (warp - 2) >> 2;
-    const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(cs * kSlice);
-    uint8_t* box = out_base + (warp - 2) * kStageBoxBytes;
-    uint8_t* myrow = box + lane * 128;
+    const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(cs * HALF);
+    uint8_t* boxes = out_base + (warp - 2) * (NBOX * L::kBox);
+    int turn = 0;                            // which box is next
     const uint32_t empty_leader = map_to_rank(smem_u32(&acc_empty[0]), 0);
-    int ch = 0;
+    int buf = 0, round = 0;
     for (int t = pair; t < p.total && !failed; t += pairs) {
       const Tile tl = tile_of(p, t);
       const int k0 = tl.split * p.kb_per_split;
       const int nk = min(p.num_kb, k0 + p.kb_per_split) - k0;
       const int chunks = (nk + p.chunk_kb - 1) / p.chunk_kb;
-      uint32_t acc[4][32];
+      uint32_t acc[G][32];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < G; ++j)
 #pragma unroll
         for (int i = 0; i < 32; ++i) acc[j][i] = 0u;
-      for (int c = 0; c < chunks; ++c, ++ch) {
-        const int buf = ch & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (ch >> 1) & 1))) {
+      for (int c = 0; c < chunks; ++c) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&acc_full[buf], round & 1))) {
           if (lane == 0) atomicExch(p.err, 34);
           failed = true;
           break;
         }
         __syncwarp();
         tc_fence_after_sync();
-        const uint32_t at = taddr + (uint32_t)(buf * kTile);
+        const uint32_t at = taddr + (uint32_t)(buf * NT);
+        if constexpr (G <= 2) {
+          uint32_t r[G][32];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t r[16];
-          tmem_ld_32x16(at + j * 16, r);
+          for (int j = 0; j < G; ++j) tmem_ld_32x32(at + j * 32, r[j]);
           tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            uint32_t& sum = acc[j >> 1][(j & 1) * 16 + i];
-            sum = __float_as_uint(__uint_as_float(sum) + __uint_as_float(r[i]));
+          for (int j = 0; j < G; ++j)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              acc[j][i] = __float_as_uint(__uint_as_float(acc[j][i]) + __uint_as_float(r[j][i]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2 * G; ++j) {
+            uint32_t r[16];
+            tmem_ld_32x16(at + j * 16, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              uint32_t& sum = acc[j >> 1][(j & 1) * 16 + i];
+              sum = __float_as_uint(__uint_as_float(sum) + __uint_as_float(r[i]));
+            }
           }
         }
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(empty_leader + (uint32_t)(buf * 8));
         __syncwarp();
+        if (++buf == ACCS) { buf = 0; ++round; }
       }
       if (failed) break;
-      const int wr0 = tl.m * kTile + rank * 128 + q * 32;        // first row of the warp
+      const int wr0 = tl.m * kTileM + rank * 128 + q * 32;       // first row of the warp
       const int row = wr0 + lane;
-      const int col0 = tl.n * kTile + cs * kSlice;
+      const int col0 = tl.n * NT + cs * HALF;
       const int zc = p.c_z0 + tl.z * p.c_zstep + tl.split;
       if (wr0 >= p.M) continue;                                    // nothing of the warp's rows is inside
+      auto next_box = [&]() {
+        uint8_t* b = boxes + turn * L::kBox;
+        turn = turn + 1 == NBOX ? 0 : turn + 1;
+        box_free<NBOX>(lane);
+        return b;
+      };
       if constexpr (EPI == EPI_STATS || EPI == EPI_STATS_F16 || EPI == EPI_STATS_F32) {
-        if (col0 + kSlice > p.N) {                                 // the ragged end (or all) of the last slices
+        if (col0 + HALF > p.N) {                                   // the ragged end (or all) of the last slices
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < G; ++j)
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if (col0 + j * 32 + i >= p.N) acc[j][i] = 0xff800000u;
         }
         float mx = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < G; ++j)
 #pragma unroll
           for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(acc[j][i]));
         constexpr float kLog2e = 1.4426950408889634f;
@@ -339,11 +410,11 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const float ref = mx == -INFINITY ? 0.f : mx < 0.f ? fmaxf(mx * kLog2e, -3.4e38f) : mx * kLog2e;
         if (p.labels != nullptr) {
           const int lab = row < p.M ? p.labels[row] - col0 : -1;
-          const bool mine = lab >= 0 && lab < kSlice && lab + col0 < p.N;
+          const bool mine = lab >= 0 && lab < HALF && lab + col0 < p.N;
           if (__any_sync(0xffffffffu, mine)) {
             float zl = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < G; ++j)
 #pragma unroll
               for (int i = 0; i < 32; ++i)
                 if (lab == j * 32 + i) zl = __uint_as_float(acc[j][i]);
@@ -352,20 +423,23 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
         if constexpr (EPI == EPI_STATS_F32) {
           // the logits themselves leave; the exponentials are only summed
+          constexpr int W = ROW / 4;                               // columns of a box
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (col0 + j * 32 >= p.N) continue;
-            box_free(lane);
+          for (int j = 0; j < HALF / W; ++j) {
+            if (col0 + j * W >= p.N) continue;
+            uint8_t* box = next_box();
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-              *reinterpret_cast<uint4*>(myrow + ((u ^ (lane & 7)) << 4)) =
-                  make_uint4(acc[j][4 * u], acc[j][4 * u + 1], acc[j][4 * u + 2], acc[j][4 * u + 3]);
-            box_send(&tmC, box, lane, col0 + j * 32, wr0, zc, false);
+            for (int u = 0; u < ROW / 16; ++u) {
+              const int i = j * W + u * 4;
+              *box_piece<ROW>(box, lane, u) =
+                  make_uint4(acc[i >> 5][i & 31], acc[i >> 5][(i + 1) & 31], acc[i >> 5][(i + 2) & 31], acc[i >> 5][(i + 3) & 31]);
+            }
+            box_send(&tmC, box, lane, col0 + j * W, wr0, zc, false);
           }
         }
         float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < G; ++j)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const float e = ex2(fmaf(__uint_as_float(acc[j][i]), kLog2e, -ref));
@@ -377,75 +451,57 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           p.stat_max[at] = mx == -INFINITY ? -INFINITY : ref;
           p.stat_sum[at] = (part[0] + part[1]) + (part[2] + part[3]);
         }
-        if constexpr (EPI == EPI_STATS_F16) {
-#pragma unroll
-          for (int b2 = 0; b2 < 2; ++b2) {
-            if (col0 + b2 * 64 >= p.N) continue;
-            box_free(lane);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              uint32_t w[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int i = u * 8 + e * 2;
-                __half2 h = __floats2half2_rn(__uint_as_float(acc[b2 * 2 + (i >> 5)][i & 31]),
-                                              __uint_as_float(acc[b2 * 2 + ((i + 1) >> 5)][(i + 1) & 31]));
-                w[e] = *reinterpret_cast<uint32_t*>(&h);
-              }
-              *reinterpret_cast<uint4*>(myrow + ((u ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            box_send(&tmC, box, lane, col0 + b2 * 64, wr0, zc, false);
-          }
-        }
       }
-      const float alpha = (EPI == EPI_F32 || EPI == EPI_BF16) && p.alpha_dev != nullptr ? p.alpha * __ldg(p.alpha_dev) : p.alpha;
-      if constexpr (EPI == EPI_F32) {
+      if constexpr (EPI == EPI_STATS_F16 || EPI == EPI_BF16) {
+        const float alpha = EPI == EPI_BF16 && p.alpha_dev != nullptr ? p.alpha * __ldg(p.alpha_dev) : p.alpha;
+        constexpr int W = ROW / 2;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (col0 + j * 32 >= p.N) continue;
-          box_free(lane);
+        for (int j = 0; j < HALF / W; ++j) {
+          if (col0 + j * W >= p.N) continue;
+          uint8_t* box = next_box();
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            float4 v;
-            v.x = alpha * __uint_as_float(acc[j][4 * u]);
-            v.y = alpha * __uint_as_float(acc[j][4 * u + 1]);
-            v.z = alpha * __uint_as_float(acc[j][4 * u + 2]);
-            v.w = alpha * __uint_as_float(acc[j][4 * u + 3]);
-            *reinterpret_cast<float4*>(myrow + ((u ^ (lane & 7)) << 4)) = v;
-          }
-          box_send(&tmC, box, lane, col0 + j * 32, wr0, zc, p.reduce != 0);
-        }
-      }
-      if constexpr (EPI == EPI_BF16) {
-#pragma unroll
-        for (int b2 = 0; b2 < 2; ++b2) {
-          if (col0 + b2 * 64 >= p.N) continue;
-          box_free(lane);
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
+          for (int u = 0; u < ROW / 16; ++u) {
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int i = u * 8 + e * 2;
-              __nv_bfloat162 h = __floats2bfloat162_rn(alpha * __uint_as_float(acc[b2 * 2 + (i >> 5)][i & 31]),
-                                                       alpha * __uint_as_float(acc[b2 * 2 + ((i + 1) >> 5)][(i + 1) & 31]));
-              w[e] = *reinterpret_cast<uint32_t*>(&h);
+              const int i = j * W + u * 8 + e * 2;
+              const float a = __uint_as_float(acc[i >> 5][i & 31]), b = __uint_as_float(acc[i >> 5][(i + 1) & 31]);
+              w[e] = EPI == EPI_BF16 ? pack_bf16(alpha * a, alpha * b) : pack_f16(a, b);
             }
-            *reinterpret_cast<uint4*>(myrow + ((u ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            *box_piece<ROW>(box, lane, u) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          box_send(&tmC, box, lane, col0 + b2 * 64, wr0, zc, false);
+          box_send(&tmC, box, lane, col0 + j * W, wr0, zc, false);
+        }
+      }
+      if constexpr (EPI == EPI_F32) {
+        const float alpha = p.alpha_dev != nullptr ? p.alpha * __ldg(p.alpha_dev) : p.alpha;
+        constexpr int W = ROW / 4;
+#pragma unroll
+        for (int j = 0; j < HALF / W; ++j) {
+          if (col0 + j * W >= p.N) continue;
+          uint8_t* box = next_box();
+#pragma unroll
+          for (int u = 0; u < ROW / 16; ++u) {
+            const int i = j * W + u * 4;
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(alpha * __uint_as_float(acc[i >> 5][(i + e) & 31]));
+            *box_piece<ROW>(box, lane, u) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          box_send(&tmC, box, lane, col0 + j * W, wr0, zc, p.reduce != 0);
         }
       }
       if constexpr (EPI == EPI_PIECES) {
-        const bool flip = p.mirror != 0 && tl.m != tl.n;
+        static_assert(EPI != EPI_PIECES || ROW == 64, "boxes of 32 x 32 16-bit numbers");
+        const bool flip = p.mirror != 0 && tl.n >= (tl.m + 1) * p.step;          // strictly above the diagonal block
         for (int o = 0; o < p.n_out; ++o) {
           const float alpha_o = p.out_alpha[o], diag_o = p.out_diag[o];
           const int zp = zc + 2 * o;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < G; ++j) {
             const int c0 = col0 + j * 32;
             if (c0 >= p.N) continue;
-            // the first pieces of two columns in a word, and what they leave over: 32 x 32 boxes of 2 KB each
+            // the first pieces of two columns in a word, and what they leave over
             uint32_t hi[16], lo[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -453,31 +509,30 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
               const float v1 = fmaf(alpha_o, __uint_as_float(acc[j][2 * e + 1]), row == c0 + 2 * e + 1 ? diag_o : 0.f);
               const __half2 h = __floats2half2_rn(v0, v1);
               const float2 f = __half22float2(h);
-              const __half2 l = __floats2half2_rn(v0 - f.x, v1 - f.y);
               hi[e] = *reinterpret_cast<const uint32_t*>(&h);
-              lo[e] = *reinterpret_cast<const uint32_t*>(&l);
+              lo[e] = pack_f16(v0 - f.x, v1 - f.y);
             }
-            box_free(lane);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              uint8_t* at = box + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4);      // the 64-byte swizzle
-              *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * u], hi[4 * u + 1], hi[4 * u + 2], hi[4 * u + 3]);
-              *reinterpret_cast<uint4*>(at + 2048) = make_uint4(lo[4 * u], lo[4 * u + 1], lo[4 * u + 2], lo[4 * u + 3]);
+            for (int piece = 0; piece < 2; ++piece) {
+              uint8_t* box = next_box();
+              const uint32_t* w = piece == 0 ? hi : lo;
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                *box_piece<ROW>(box, lane, u) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+              box_send(&tmC, box, lane, c0, wr0, zp + piece, false);
             }
-            box_send(&tmC, box, lane, c0, wr0, zp, false);
-            box_send(&tmC, box + 2048, lane, c0, wr0, zp + 1, false);
             if (flip) {
-              box_free(lane);
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                uint8_t* at = box + 2 * e * 64 + lane * 2;
-                *reinterpret_cast<uint16_t*>(at) = (uint16_t)hi[e];
-                *reinterpret_cast<uint16_t*>(at + 64) = (uint16_t)(hi[e] >> 16);
-                *reinterpret_cast<uint16_t*>(at + 2048) = (uint16_t)lo[e];
-                *reinterpret_cast<uint16_t*>(at + 2112) = (uint16_t)(lo[e] >> 16);
+              for (int piece = 0; piece < 2; ++piece) {
+                uint8_t* box = next_box();
+                const uint32_t* w = piece == 0 ? hi : lo;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  *reinterpret_cast<uint16_t*>(box + 2 * e * 64 + lane * 2) = (uint16_t)w[e];
+                  *reinterpret_cast<uint16_t*>(box + (2 * e + 1) * 64 + lane * 2) = (uint16_t)(w[e] >> 16);
+                }
+                box_send(&tmCT, box, lane, wr0, c0, zp + piece, false);
               }
-              box_send(&tmCT, box, lane, wr0, c0, zp, false);
-              box_send(&tmCT, box + 2048, lane, wr0, c0, zp + 1, false);
             }
           }
         }
@@ -503,45 +558,64 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 // ---- host side ---------------------------------------------------------------------------------------------------
 
 // A stack of `planes` row-major matrices [rows][cols] of 16-bit or fp32 numbers (row pitch ld, plane pitch `plane`, in
-// elements, both 16-byte multiples), read or written in boxes of 128 bytes x box_rows rows with the 128-byte swizzle.
-// MAP_F16_S, MAP_F16_T: boxes of 64 bytes x box_rows rows with the 64-byte swizzle, or none (EPI_PIECES' straight and
-// transposed stores).
-enum MapType { MAP_BF16, MAP_F16, MAP_F32, MAP_F16_S, MAP_F16_T };
-int make_stack_map(CUtensorMap* out, const void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
-                   int64_t plane, int box_rows);
+// elements, both 16-byte multiples).  An operand is read in boxes of 64 rows x 128 bytes with the 128-byte swizzle; an output
+// is written in boxes of 32 rows x `row_bytes` (Smem::kBoxRow) with the swizzle of that width, or, transposed, none.
+enum MapType { MAP_BF16, MAP_F16, MAP_F32 };
+int make_operand_map(CUtensorMap* out, const void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
+                     int64_t plane);
+int make_output_map(CUtensorMap* out, void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
+                    int64_t plane, int row_bytes, bool transposed = false);
 // where a bounded wait that runs out is recorded (one word per device, read by ls_device_status); null on failure
 int* device_error_word();
 
-// K blocks per tensor-memory accumulator.  One MMA adds 16 products per element and truncates: 64 (24, 48) MMAs per chunk
-// bias a sum of equal signs by about 2e-6 (0.8e-6, 1.5e-6) of its value, and sums of mixed signs by far less.  The row
+// K blocks per tensor-memory accumulator.  One MMA adds 16 products per element and truncates: 64 (24) MMAs per chunk
+// bias a sum of equal signs by about 2e-6 (0.8e-6) of its value, and sums of mixed signs by far less.  The row
 // statistics of bf16 operands, which leave in fp32, take 32.
-constexpr int kChunk1 = 16, kChunk2 = 2, kChunk3 = 2;
+constexpr int kChunk1 = 16, kChunk2 = 2, kChunk3 = 1;
 constexpr int kPairs = 74;
 
 // Fills in the tile counts and launches.  p.splits, p.M, p.N, p.batch, p.tri, p.n_fast and the epilogue's fields are the
 // caller's; K is the contraction length.
-template <int NP, bool F16, bool A_MN, bool B_MN, int EPI>
-cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& ct, Params p, int64_t K,
-                   cudaStream_t st) {
-  auto kern = gemm_op_kernel<NP, F16, A_MN, B_MN, EPI>;
+template <int NP, int NT, bool F16, bool A_MN, bool B_MN, int EPI>
+cudaError_t launch_nt(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& ct, Params p,
+                      int64_t K, cudaStream_t st) {
+  auto kern = gemm_op_kernel<NP, NT, F16, A_MN, B_MN, EPI>;
   static uint64_t configured = 0;        // one bit per device
-  cudaError_t e = allow_dynamic_smem(kern, (int)Smem<NP>::kTotal, &configured);
+  cudaError_t e = allow_dynamic_smem(kern, (int)Smem<NP, NT>::kTotal, &configured);
   if (e != cudaSuccess) return e;
-  p.m_tiles = (p.M + kTile - 1) / kTile;
-  p.n_tiles = (p.N + kTile - 1) / kTile;
+  p.m_tiles = (p.M + kTileM - 1) / kTileM;
+  p.n_tiles = (p.N + NT - 1) / NT;
+  p.step = kTileM / NT;
   p.num_kb = (int)((K + 63) / 64);
   if (p.splits < 1) p.splits = 1;
   p.kb_per_split = (p.num_kb + p.splits - 1) / p.splits;
   p.splits = (p.num_kb + p.kb_per_split - 1) / p.kb_per_split;       // (callers ask split_count() first: no change here)
   p.chunk_kb = NP == 1 ? (EPI == EPI_F32 || EPI == EPI_BF16 ? kChunk1 : kChunk1 / 2) : NP == 2 ? kChunk2 : kChunk3;
-  const int64_t per = p.tri ? (int64_t)p.m_tiles * (p.m_tiles + 1) / 2 : (int64_t)p.m_tiles * p.n_tiles;
+  int64_t per = (int64_t)p.m_tiles * p.n_tiles;
+  if (p.tri) {
+    per = 0;
+    for (int m = 0; m < p.m_tiles; ++m) per += p.n_tiles - m * p.step;
+  }
   const int64_t total = per * p.splits * p.batch;
   if (total > 2000000000ll) return cudaErrorInvalidValue;
+  p.per = (int)per;
   p.total = (int)total;
   p.err = device_error_word();
   if (p.err == nullptr) return cudaErrorUnknown;
   const unsigned pairs = (unsigned)(total < kPairs ? total : kPairs);
-  return launch_dep(kern, dim3(2 * pairs), dim3(kThreads), Smem<NP>::kTotal, st, 2, a, b, c, ct, p);
+  return launch_dep(kern, dim3(2 * pairs), dim3(kThreads), Smem<NP, NT>::kTotal, st, 2, a, b, c, ct, p);
+}
+
+// Columns of a tile: 256, or 128 where that leaves pairs without a tile.
+inline int pick_nt(int64_t M, int64_t N, int64_t batch, bool tri) {
+  const int64_t mt = (M + 255) / 256, nt = (N + 255) / 256;
+  return (tri ? mt * (mt + 1) / 2 : mt * nt) * batch < kPairs ? 128 : 256;
+}
+template <int NP, bool F16, bool A_MN, bool B_MN, int EPI>
+cudaError_t launch(int nt, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& ct,
+                   const Params& p, int64_t K, cudaStream_t st) {
+  return nt == 256 ? launch_nt<NP, 256, F16, A_MN, B_MN, EPI>(a, b, c, ct, p, K, st)
+                   : launch_nt<NP, 128, F16, A_MN, B_MN, EPI>(a, b, c, ct, p, K, st);
 }
 
 // Into how many parts the contraction is cut when `tiles` output tiles leave pairs idle: enough parts to give each pair

@@ -29,7 +29,7 @@ constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kNsEps = 1e-7f;
 constexpr int kMaxSide = 1 << 15;
 constexpr int kMaxSteps = 64;
-constexpr int kSumBlocks = 296;        // at most: partial sums of squares of a matrix
+constexpr int kSumBlocks = 592;        // at most: partial sums of squares of a matrix
 // Scales of A, C and P in fp16.  Singular values stay below 1.25, so no entry of A exceeds 1.6, none of C |b| + 1.6 |c| < 8.1,
 // and P, whose eigenvalues lie between 0 and a, has none above 3.5.
 constexpr float kScaleA = 8192.f, kScaleC = 4096.f, kScaleP = 8192.f;
@@ -48,44 +48,91 @@ struct MatArgs {
   float scale_x;
 };
 
-template <typename G>
-__device__ __forceinline__ float load_g(const void* g, int64_t i) { return (float)static_cast<const G*>(g)[i]; }
+// The element-wise passes take a matrix in units of 512 columns of a row, one warp each; a lane has four groups of four
+// consecutive elements, read as 16 (bf16: 8) bytes where rows start on such boundaries (VEC), else one by one.
+constexpr int kUnit = 512;
+constexpr int kWarps = 8;                // per CTA
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void load4(const T* p, int left, float (&f)[4]) {
+  if constexpr (VEC && sizeof(T) == 4) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+  } else if constexpr (VEC) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xFFFF0000u);
+    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xFFFF0000u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = i < left ? (float)p[i] : 0.f;
+  }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store4(T* p, int left, const float (&f)[4]) {
+  if constexpr (VEC && sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  } else if constexpr (VEC) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(gop::pack_bf16(f[0], f[1]), gop::pack_bf16(f[2], f[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (i < left) p[i] = (T)f[i];
+  }
+}
+// f(offset in the matrix, row, column, elements left in the row) for every group of four of this warp's units
+template <typename F>
+__device__ __forceinline__ void for_groups(const MatArgs& a, F f) {
+  const int segs = (a.cols + kUnit - 1) / kUnit;
+  const int64_t units = (int64_t)a.rows * segs;
+  const int lane = threadIdx.x & 31;
+  for (int64_t u = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * kWarps) {
+    const int r = (int)(u / segs), c0 = (int)(u - (int64_t)r * segs) * kUnit;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = c0 + k * 128 + lane * 4;
+      if (c < a.cols) f((int64_t)r * a.cols + c, r, c, a.cols - c);
+    }
+  }
+}
 
 // v <- mu v + g, and the partial sums of squares of U in double
-template <typename G, bool MUON>
-__global__ void __launch_bounds__(512) ns_momentum_kernel(const MatArgs a) {
-  __shared__ double red[16];
+template <typename G, bool MUON, bool VEC>
+__global__ void __launch_bounds__(32 * kWarps) ns_momentum_kernel(const MatArgs a) {
+  __shared__ double red[kWarps];
   grid_dep_wait();
   grid_dep_launch();
-  const int64_t n = (int64_t)a.rows * a.cols;
   const int64_t z = blockIdx.y;
   double s = 0.0;
-  for (int64_t i = (int64_t)blockIdx.x * 512 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 512) {
-    const float g = load_g<G>(a.g, z * a.g_stride + i);
-    float u = g;
+  for_groups(a, [&](int64_t at, int, int, int left) {
+    float g[4];
+    load4<G, VEC>(static_cast<const G*>(a.g) + z * a.g_stride + at, left, g);
     if constexpr (MUON) {
-      float* v = a.v + z * a.v_stride + i;
-      const float nv = fmaf(a.mu, *v, g);
-      *v = nv;
-      u = a.nesterov ? fmaf(a.mu, nv, g) : nv;
+      float* vp = a.v + z * a.v_stride + at;
+      float v[4];
+      load4<float, VEC>(vp, left, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = fmaf(a.mu, v[i], g[i]);
+      store4<float, VEC>(vp, left, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = a.nesterov ? fmaf(a.mu, v[i], g[i]) : v[i];
     }
-    s += (double)u * (double)u;
-  }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s += (double)g[i] * (double)g[i];
+  });
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
     double t = 0.0;
-    for (int i = 0; i < 16; ++i) t += red[i];
+    for (int i = 0; i < kWarps; ++i) t += red[i];
     a.partial[z * kSumBlocks + blockIdx.x] = t;
   }
 }
 
 // X_0 = U / (|U| + eps) as two scaled pieces
-template <typename G, bool MUON>
-__global__ void __launch_bounds__(512) ns_start_kernel(const MatArgs a, __half* x) {
-  __shared__ float inv_s;
+template <typename G, bool MUON, bool VEC>
+__global__ void __launch_bounds__(32 * kWarps) ns_start_kernel(const MatArgs a, __half* x) {
+  __shared__ float norm_s;
   grid_dep_wait();
   grid_dep_launch();
   const int64_t z = blockIdx.y;
@@ -94,48 +141,68 @@ __global__ void __launch_bounds__(512) ns_start_kernel(const MatArgs a, __half* 
     for (int i = threadIdx.x; i < a.blocks; i += 32) t += a.partial[z * kSumBlocks + i];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-    if (threadIdx.x == 0) inv_s = (float)sqrt(t) + kNsEps;
+    if (threadIdx.x == 0) norm_s = (float)sqrt(t) + kNsEps;
   }
   __syncthreads();
-  const float norm = inv_s;
+  const float norm = norm_s;
   __half* hi = x + z * 2 * a.plane;
-  __half* lo = hi + a.plane;
-  const int64_t n = (int64_t)a.rows * a.cols;
-  for (int64_t i = (int64_t)blockIdx.x * 512 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 512) {
-    const float g = load_g<G>(a.g, z * a.g_stride + i);
-    float u = g;
+  for_groups(a, [&](int64_t at, int r, int c, int left) {
+    float g[4];
+    load4<G, VEC>(static_cast<const G*>(a.g) + z * a.g_stride + at, left, g);
     if constexpr (MUON) {
-      const float nv = a.v[z * a.v_stride + i];
-      u = a.nesterov ? fmaf(a.mu, nv, g) : nv;
+      float v[4];
+      load4<float, VEC>(a.v + z * a.v_stride + at, left, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = a.nesterov ? fmaf(a.mu, v[i], g[i]) : v[i];
     }
-    const float v = u / norm * a.scale_x;
-    const __half h = __float2half_rn(v);
-    const int64_t r = i / a.cols, at = r * a.ld + (i - r * a.cols);
-    hi[at] = h;
-    lo[at] = __float2half_rn(v - __half2float(h));
-  }
+    float l[4];
+    uint32_t hw[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g[i] = g[i] / norm * a.scale_x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const __half2 h = __floats2half2_rn(g[2 * i], g[2 * i + 1]);
+      const float2 f = __half22float2(h);
+      l[2 * i] = g[2 * i] - f.x; l[2 * i + 1] = g[2 * i + 1] - f.y;
+      hw[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    // (rows of X are padded to whole 64 elements: the group past the last column is written as it is)
+    __half* o = hi + (int64_t)r * a.ld + c;
+    *reinterpret_cast<uint2*>(o) = make_uint2(hw[0], hw[1]);
+    *reinterpret_cast<uint2*>(o + a.plane) = make_uint2(gop::pack_f16(l[0], l[1]), gop::pack_f16(l[2], l[3]));
+  });
 }
 
 // W <- W - step O, or out <- O, from the pieces of the last X
-template <typename G, bool MUON>
-__global__ void __launch_bounds__(512) ns_finish_kernel(const MatArgs a, const __half* x, float step) {
+template <typename G, bool MUON, bool VEC>
+__global__ void __launch_bounds__(32 * kWarps) ns_finish_kernel(const MatArgs a, const __half* x, float step) {
   grid_dep_wait();
   grid_dep_launch();
   const int64_t z = blockIdx.y;
   const __half* hi = x + z * 2 * a.plane;
-  const __half* lo = hi + a.plane;
   const float inv = 1.f / a.scale_x;
-  const int64_t n = (int64_t)a.rows * a.cols;
-  for (int64_t i = (int64_t)blockIdx.x * 512 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 512) {
-    const int64_t r = i / a.cols, at = r * a.ld + (i - r * a.cols);
-    const float o = (__half2float(hi[at]) + __half2float(lo[at])) * inv;
-    if constexpr (MUON) {
-      float* w = a.w + z * a.w_stride + i;
-      *w = fmaf(-step, o, *w);
-    } else {
-      static_cast<G*>(a.out)[z * a.out_stride + i] = (G)o;
+  for_groups(a, [&](int64_t at, int r, int c, int left) {
+    const __half* p = hi + (int64_t)r * a.ld + c;
+    const uint2 h = *reinterpret_cast<const uint2*>(p), l = *reinterpret_cast<const uint2*>(p + a.plane);
+    const uint32_t hw[2] = {h.x, h.y}, lw[2] = {l.x, l.y};
+    float o[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hw[i]));
+      const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&lw[i]));
+      o[2 * i] = (f.x + e.x) * inv; o[2 * i + 1] = (f.y + e.y) * inv;
     }
-  }
+    if constexpr (MUON) {
+      float* wp = a.w + z * a.w_stride + at;
+      float w[4];
+      load4<float, VEC>(wp, left, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = fmaf(-step, o[i], w[i]);
+      store4<float, VEC>(wp, left, w);
+    } else {
+      store4<G, VEC>(static_cast<G*>(a.out) + z * a.out_stride + at, left, o);
+    }
+  });
 }
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -172,7 +239,9 @@ Plan make_plan(int m, int rows, int cols) {
     if ((x) != cudaSuccess) return LS_ERR_CUDA;     \
   } while (0)
 
-template <typename G, bool MUON>
+bool off(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+template <typename G, bool MUON, bool VEC>
 int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
   const Plan p = make_plan(a.m, a.rows, a.cols);
   a.ld = p.ld; a.plane = p.plane;
@@ -181,32 +250,33 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
   // entries of X_0 of about 1: the root mean square of a matrix of Frobenius norm 1, inverted; none exceeds 2^14
   a.scale_x = exp2f(floorf(0.5f * log2f((float)n)));
   if (a.scale_x > 16384.f) a.scale_x = 16384.f;
-  int64_t blocks = (n + 2047) / 2048, share = 148 * 4 / a.m;
+  // (four resident CTAs per SM over all replicas)
+  int64_t blocks = ((int64_t)a.rows * ((a.cols + kUnit - 1) / kUnit) + kWarps - 1) / kWarps, share = 148 * 4 / a.m;
   if (share < 1) share = 1;
   if (blocks > share) blocks = share;
   if (blocks > kSumBlocks) blocks = kSumBlocks;
   a.blocks = (int)blocks;
   __half* x[2] = {reinterpret_cast<__half*>(ws + p.o_x[0]), reinterpret_cast<__half*>(ws + p.o_x[1])};
-  const void* ac = ws + p.o_ac;      // [m][A first, second piece, C first, second piece]
-  const void* pp = ws + p.o_p;
+  void* ac = ws + p.o_ac;      // [m][A first, second piece, C first, second piece]
+  void* pp = ws + p.o_p;
   const dim3 grid((unsigned)blocks, (unsigned)a.m);
-  LS_TRY(launch_dep(ns_momentum_kernel<G, MUON>, grid, dim3(512), 0, st, 1, a));
-  LS_TRY(launch_dep(ns_start_kernel<G, MUON>, grid, dim3(512), 0, st, 1, a, x[0]));
-  // maps: X as K-major and MN-major operand and as output; A, C and P as K-major operands (they are symmetric) and as
-  // outputs, straight and transposed
-  CUtensorMap xk[2], xm[2], xo[2], ack, aco, act, pk, po, pt;
+  LS_TRY(launch_dep(ns_momentum_kernel<G, MUON, VEC>, grid, dim3(32 * kWarps), 0, st, 1, a));
+  LS_TRY(launch_dep(ns_start_kernel<G, MUON, VEC>, grid, dim3(32 * kWarps), 0, st, 1, a, x[0]));
+  // maps: X as operand and as output; A, C and P as operands and as outputs, straight and transposed
+  constexpr int kRow = gop::box_row(2);
+  CUtensorMap xk[2], xo[2], ack, aco, act, pk, po, pt;
   const int64_t m = a.m;
   for (int i = 0; i < 2; ++i) {
-    LS_TRY(gop::make_stack_map(&xk[i], x[i], gop::MAP_F16, a.rows, a.cols, 2 * m, p.ld, p.plane, 128));
-    LS_TRY(gop::make_stack_map(&xm[i], x[i], gop::MAP_F16, a.rows, a.cols, 2 * m, p.ld, p.plane, 64));
-    LS_TRY(gop::make_stack_map(&xo[i], x[i], gop::MAP_F16_S, a.rows, a.cols, 2 * m, p.ld, p.plane, 32));
+    LS_TRY(gop::make_operand_map(&xk[i], x[i], gop::MAP_F16, a.rows, a.cols, 2 * m, p.ld, p.plane));
+    LS_TRY(gop::make_output_map(&xo[i], x[i], gop::MAP_F16, a.rows, a.cols, 2 * m, p.ld, p.plane, kRow));
   }
-  LS_TRY(gop::make_stack_map(&ack, ac, gop::MAP_F16, p.n, p.n, 4 * m, p.ldn, p.plane_n, 128));
-  LS_TRY(gop::make_stack_map(&aco, ac, gop::MAP_F16_S, p.n, p.n, 4 * m, p.ldn, p.plane_n, 32));
-  LS_TRY(gop::make_stack_map(&act, ac, gop::MAP_F16_T, p.n, p.n, 4 * m, p.ldn, p.plane_n, 32));
-  LS_TRY(gop::make_stack_map(&pk, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, 128));
-  LS_TRY(gop::make_stack_map(&po, pp, gop::MAP_F16_S, p.n, p.n, 2 * m, p.ldn, p.plane_n, 32));
-  LS_TRY(gop::make_stack_map(&pt, pp, gop::MAP_F16_T, p.n, p.n, 2 * m, p.ldn, p.plane_n, 32));
+  LS_TRY(gop::make_operand_map(&ack, ac, gop::MAP_F16, p.n, p.n, 4 * m, p.ldn, p.plane_n));
+  LS_TRY(gop::make_output_map(&aco, ac, gop::MAP_F16, p.n, p.n, 4 * m, p.ldn, p.plane_n, kRow));
+  LS_TRY(gop::make_output_map(&act, ac, gop::MAP_F16, p.n, p.n, 4 * m, p.ldn, p.plane_n, kRow, true));
+  LS_TRY(gop::make_operand_map(&pk, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n));
+  LS_TRY(gop::make_output_map(&po, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, kRow));
+  LS_TRY(gop::make_output_map(&pt, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, kRow, true));
+  const int nt_n = gop::pick_nt(p.n, p.n, m, true), nt_x = gop::pick_nt(a.rows, a.cols, m, false);
   int cur = 0;
   for (int s = 0; s < steps; ++s, cur ^= 1) {
     Params g{};
@@ -219,26 +289,35 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
     g.out_alpha[0] = kScaleA * unit;
     g.out_alpha[1] = kNsC * kScaleC * unit;
     g.out_diag[1] = kNsB * kScaleC;
-    if (p.tall) LS_TRY((gop::launch<2, true, true, true, gop::EPI_PIECES>(xm[cur], xm[cur], aco, act, g, p.k, st)));
-    else LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(xk[cur], xk[cur], aco, act, g, p.k, st)));
+    if (p.tall) LS_TRY((gop::launch<2, true, true, true, gop::EPI_PIECES>(nt_n, xk[cur], xk[cur], aco, act, g, p.k, st)));
+    else LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(nt_n, xk[cur], xk[cur], aco, act, g, p.k, st)));
     // P = a I + A C
     g.a_zstep = g.b_zstep = 4; g.b_z0 = 2; g.c_zstep = 2;
     g.n_out = 1;
     g.out_alpha[0] = kScaleP / (kScaleA * kScaleC);
     g.out_diag[0] = kNsA * kScaleP;
-    LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(ack, ack, po, pt, g, p.n, st)));
+    LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(nt_n, ack, ack, po, pt, g, p.n, st)));
     // X <- P X (wide) or X P (tall)
     g.a_zstep = g.b_zstep = g.c_zstep = 2; g.b_z0 = 0;
     g.tri = g.mirror = 0;
     g.M = a.rows; g.N = a.cols;
     g.out_alpha[0] = 1.f / kScaleP;
     g.out_diag[0] = 0.f;
-    if (p.tall) LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(xk[cur], pk, xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
-    else LS_TRY((gop::launch<2, true, false, true, gop::EPI_PIECES>(pk, xm[cur], xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
+    if (p.tall) LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(nt_x, xk[cur], pk, xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
+    else LS_TRY((gop::launch<2, true, false, true, gop::EPI_PIECES>(nt_x, pk, xk[cur], xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
   }
   const float step = a.lr * sqrtf(fmaxf(1.f, (float)a.rows / (float)a.cols));
-  LS_TRY(launch_dep(ns_finish_kernel<G, MUON>, grid, dim3(512), 0, st, 1, a, static_cast<const __half*>(x[cur]), step));
+  LS_TRY(launch_dep(ns_finish_kernel<G, MUON, VEC>, grid, dim3(32 * kWarps), 0, st, 1, a, static_cast<const __half*>(x[cur]), step));
   return LS_OK;
+}
+
+// 16-byte (bf16: 8-byte) accesses need every row and replica of every tensor of the call to start on such a boundary.
+template <typename G, bool MUON>
+int pick_ns(const MatArgs& a, int steps, char* ws, cudaStream_t st) {
+  const size_t e = sizeof(G) * 4;
+  bool vec = a.cols % 4 == 0 && !off(a.g, e) && !off(a.out, e) && !off(a.w, 16) && !off(a.v, 16);
+  if (a.m > 1) vec = vec && a.g_stride % 4 == 0 && a.out_stride % 4 == 0 && a.w_stride % 4 == 0 && a.v_stride % 4 == 0;
+  return vec ? run_ns<G, MUON, true>(a, steps, ws, st) : run_ns<G, MUON, false>(a, steps, ws, st);
 }
 
 int check_sizes(int m, int rows, int cols) {
@@ -246,7 +325,6 @@ int check_sizes(int m, int rows, int cols) {
   if (m > 65535 || rows > kMaxSide || cols > kMaxSide) return LS_ERR_TOO_LARGE;
   return LS_OK;
 }
-bool off(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
 int check_ws(int m, int rows, int cols, const void* ws, size_t ws_bytes) {
   if (ws == nullptr) return LS_ERR_INVALID_ARG;
@@ -282,8 +360,8 @@ extern "C" int ls_orthogonalize(const void* u_dev, int m, int rows, int cols, in
   a.g = u_dev; a.g_stride = u_stride; a.out = out_dev; a.out_stride = out_stride;
   a.m = m; a.rows = rows; a.cols = cols;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return dtype == LS_DTYPE_BF16 ? run_ns<__nv_bfloat16, false>(a, steps, static_cast<char*>(ws_dev), st)
-                                : run_ns<float, false>(a, steps, static_cast<char*>(ws_dev), st);
+  return dtype == LS_DTYPE_BF16 ? pick_ns<__nv_bfloat16, false>(a, steps, static_cast<char*>(ws_dev), st)
+                                : pick_ns<float, false>(a, steps, static_cast<char*>(ws_dev), st);
 }
 
 extern "C" int ls_muon_step(float* w_dev, float* v_dev, const void* g_dev, int m, int rows, int cols, int64_t w_stride,
@@ -304,6 +382,6 @@ extern "C" int ls_muon_step(float* w_dev, float* v_dev, const void* g_dev, int m
   a.g = g_dev; a.g_stride = g_stride; a.w = w_dev; a.v = v_dev; a.w_stride = w_stride; a.v_stride = v_stride;
   a.m = m; a.rows = rows; a.cols = cols; a.lr = lr; a.mu = momentum; a.nesterov = nesterov;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return g_dtype == LS_DTYPE_BF16 ? run_ns<__nv_bfloat16, true>(a, steps, static_cast<char*>(ws_dev), st)
-                                  : run_ns<float, true>(a, steps, static_cast<char*>(ws_dev), st);
+  return g_dtype == LS_DTYPE_BF16 ? pick_ns<__nv_bfloat16, true>(a, steps, static_cast<char*>(ws_dev), st)
+                                  : pick_ns<float, true>(a, steps, static_cast<char*>(ws_dev), st);
 }

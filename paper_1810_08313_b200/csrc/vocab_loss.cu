@@ -5,7 +5,7 @@
 //
 // The three products are 6 rows V d flops and bound the call; what must not be added to them is traffic of rows x V
 // numbers in fp32.  The logits never reach memory in the loss: the product's epilogue reduces every row of a 256 x 256 tile to
-// (maximum, sum of exponentials) per 128 columns, and a small kernel combines those.  The gradient needs the
+// (maximum, sum of exponentials) per slice of half a tile's columns, and a small kernel combines those.  The gradient needs the
 // normalised probabilities twice, as an operand of dh (contracted over V) and of dW (contracted over rows), and their
 // normaliser only when the last column is known.  Recomputing the logits would cost a third more flops; instead a piece
 // of rows (at most 2^29 elements of the piece's probabilities, 1 GiB) keeps exp(z - slice maximum) as fp16 numbers in
@@ -120,7 +120,7 @@ vocab_combine_kernel(const float* stat_max, const float* stat_sum, int64_t stat_
 // ---- exponentials -> dz, eight columns per thread ------------------------------------------------------------------------
 // bf16: in place over the fp16 numbers.
 __global__ void __launch_bounds__(256)
-vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int V, const float* stat_max, int64_t stat_ld, const int32_t* labels,
+vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int V, const float* stat_max, int64_t stat_ld, int slice, const int32_t* labels,
                      const float* label_logit, const float* lse) {
   const int row = blockIdx.y;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
@@ -134,7 +134,7 @@ vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int V, const float* stat_max, int6
     return;
   }
   const float l = lse[row];
-  const float f = gop::ex2(__ldg(stat_max + (int64_t)(c >> 7) * stat_ld + row) - l * kLog2e);
+  const float f = gop::ex2(__ldg(stat_max + (int64_t)(c / slice) * stat_ld + row) - l * kLog2e);
   uint4 u = *reinterpret_cast<const uint4*>(at);
   uint32_t w[4] = {u.x, u.y, u.z, u.w};
   float v[8];
@@ -278,6 +278,7 @@ struct Plan {
   int64_t pieces;
   int64_t Vp, dp;       // padded row lengths: probabilities, packed operands
   int64_t df;           // padded row length of fp32 sums
+  int nt, nt_dh, nt_dw;
   int slices;
   int64_t stat_ld;
   int splits;           // of the contraction over V in dh
@@ -300,16 +301,21 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.Vp = round_up(V, 64);
   p.dp = round_up(d, 8);
   p.df = round_up(d, 4);
-  p.slices = (int)(2 * ((V + 255) / 256));
   // rows of a piece: the probabilities of a piece of a gradient, or the statistics of a piece of a loss, stay bounded
-  const int64_t most = grad ? (p.f32 ? (int64_t)1 << 27 : (int64_t)1 << 29) / p.Vp : ((int64_t)1 << 25) / p.slices;
+  const int64_t most = grad ? (p.f32 ? (int64_t)1 << 27 : (int64_t)1 << 29) / p.Vp : ((int64_t)1 << 31) / p.Vp;
   int64_t R = most / 256 * 256;
   if (R < 256) R = 256;
   p.pieces = rows > 0 ? (rows + R - 1) / R : 0;
   p.R = rows > 0 ? round_up((rows + p.pieces - 1) / p.pieces, 256) : 0;
   p.pieces = rows > 0 ? (rows + p.R - 1) / p.R : 0;
   p.stat_ld = p.R;
-  const int64_t dh_tiles = ((p.R < rows ? p.R : rows) + 255) / 256 * ((d + 255) / 256);
+  // tile widths of the three products (a slice of the statistics is half a tile)
+  const int64_t most_rows = p.R < rows ? p.R : rows;
+  p.nt = gop::pick_nt(most_rows, V, 1, false);
+  p.nt_dh = gop::pick_nt(most_rows, d, 1, false);
+  p.nt_dw = gop::pick_nt(V, d, 1, false);
+  p.slices = (int)(2 * ((V + p.nt - 1) / p.nt));
+  const int64_t dh_tiles = (most_rows + 255) / 256 * ((d + p.nt_dh - 1) / p.nt_dh);
   p.splits = grad && rows > 0 ? gop::split_count(dh_tiles, V, 8) : 1;
   const bool whole = d % (p.f32 ? 4 : 8) == 0;
   p.dh_fold = grad && (p.splits > 1 || !whole);
@@ -373,6 +379,7 @@ struct VocabArgs {
 template <typename T, int NP>
 int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   constexpr bool F32 = NP == 3;
+  constexpr int kRow = gop::box_row(NP);
   using bf = __nv_bfloat16;
   const T* h = static_cast<const T*>(a.h) + rep * a.h_stride;
   const T* W = static_cast<const T*>(a.W) + rep * a.w_stride;
@@ -391,9 +398,8 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   if (lay) LS_TRY(pack<T>(W, V, d, wpack, p.dp, V * p.dp, nullptr, 0, st));
   const bf* wop = lay ? wpack : reinterpret_cast<const bf*>(W);
   const int64_t wld = lay ? p.dp : d;
-  CUtensorMap mw_k, mw_mn;
-  LS_TRY(gop::make_stack_map(&mw_k, wop, gop::MAP_BF16, V, d, NP, wld, V * wld, 128));
-  LS_TRY(gop::make_stack_map(&mw_mn, wop, gop::MAP_BF16, V, d, NP, wld, V * wld, 64));
+  CUtensorMap mw;
+  LS_TRY(gop::make_operand_map(&mw, wop, gop::MAP_BF16, V, d, NP, wld, V * wld));
   for (int64_t r0 = 0, piece = 0; r0 < a.rows; r0 += p.R, ++piece) {
     const int64_t rn = a.rows - r0 < p.R ? a.rows - r0 : p.R;
     const T* hr = h + r0 * d;
@@ -401,21 +407,19 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     if (lay) LS_TRY(pack<T>(hr, rn, d, hpack, p.dp, hplane, nullptr, 0, st));
     const bf* hop = lay ? hpack : reinterpret_cast<const bf*>(hr);
     const int64_t hld = lay ? p.dp : d;
-    CUtensorMap mh_k, me;
-    LS_TRY(gop::make_stack_map(&mh_k, hop, gop::MAP_BF16, rn, d, NP, hld, hplane, 128));
+    CUtensorMap mh, me;
+    LS_TRY(gop::make_operand_map(&mh, hop, gop::MAP_BF16, rn, d, NP, hld, hplane));
     // logits
     Params g{};
     g.batch = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
     g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld;
     g.labels = labels + r0; g.label_logit = logit + r0;
     if (!p.grad) {
-      LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(mh_k, mw_k, mh_k, mh_k, g, d, st)));
-    } else if (F32) {
-      LS_TRY(gop::make_stack_map(&me, a.ws + p.o_e, gop::MAP_F32, rn, V, 1, p.Vp, p.R * p.Vp, 32));
-      LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS_F32>(mh_k, mw_k, me, me, g, d, st)));
+      LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(p.nt, mh, mw, mh, mh, g, d, st)));
     } else {
-      LS_TRY(gop::make_stack_map(&me, a.ws + p.o_e, gop::MAP_F16, rn, V, 1, p.Vp, p.R * p.Vp, 32));
-      LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS_F16>(mh_k, mw_k, me, me, g, d, st)));
+      constexpr gop::Epi kEpi = F32 ? gop::EPI_STATS_F32 : gop::EPI_STATS_F16;
+      LS_TRY(gop::make_output_map(&me, a.ws + p.o_e, F32 ? gop::MAP_F32 : gop::MAP_F16, rn, V, 1, p.Vp, p.R * p.Vp, kRow));
+      LS_TRY((gop::launch<NP, false, false, false, kEpi>(p.nt, mh, mw, me, me, g, d, st)));
     }
     LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((rn + 31) / 32)), dim3(1024), 0, st, 1, stat_max, stat_sum,
                       p.stat_ld, p.slices, (int)rn, (int)V, labels + r0, logit + r0, lse + r0, row_loss + r0));
@@ -432,13 +436,12 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
                           ly, logit + r0 + q0, lse + r0 + q0));
       } else {
         LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + 2047) / 2048), qn), dim3(256), 0, st, 1,
-                          reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)V, stat_max + q0, p.stat_ld, ly,
+                          reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)V, stat_max + q0, p.stat_ld, p.nt / 2, ly,
                           logit + r0 + q0, lse + r0 + q0));
       }
     }
-    CUtensorMap mz_k, mz_mn, mh_mn, mo;
-    LS_TRY(gop::make_stack_map(&mz_k, dz, gop::MAP_BF16, rn, V, NP, p.Vp, p.R * p.Vp, 128));
-    LS_TRY(gop::make_stack_map(&mz_mn, dz, gop::MAP_BF16, rn, V, NP, p.Vp, p.R * p.Vp, 64));
+    CUtensorMap mz, mhz, mo;
+    LS_TRY(gop::make_operand_map(&mz, dz, gop::MAP_BF16, rn, V, NP, p.Vp, p.R * p.Vp));
     // dh = dz W
     T* dh = static_cast<T*>(a.dh) + rep * a.dh_stride + r0 * d;
     Params gh{};
@@ -446,31 +449,31 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     if (p.dh_fold) {
       float* part = reinterpret_cast<float*>(a.ws + p.o_dh);
       gh.c_zstep = p.splits;
-      LS_TRY(gop::make_stack_map(&mo, part, gop::MAP_F32, rn, d, p.splits, p.df, p.R * p.df, 32));
-      LS_TRY((gop::launch<NP, false, false, true, gop::EPI_F32>(mz_k, mw_mn, mo, mo, gh, V, st)));
+      LS_TRY(gop::make_output_map(&mo, part, gop::MAP_F32, rn, d, p.splits, p.df, p.R * p.df, kRow));
+      LS_TRY((gop::launch<NP, false, false, true, gop::EPI_F32>(p.nt_dh, mz, mw, mo, mo, gh, V, st)));
       LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(rn * ((d + 3) / 4))), dim3(256), 0, st, 1,
                         static_cast<const float*>(part), p.splits, p.R * p.df, p.df, rn, d, dh));
     } else {
-      LS_TRY(gop::make_stack_map(&mo, dh, F32 ? gop::MAP_F32 : gop::MAP_BF16, rn, d, 1, d, rn * d, 32));
-      LS_TRY((gop::launch<NP, false, false, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(mz_k, mw_mn, mo, mo, gh, V, st)));
+      LS_TRY(gop::make_output_map(&mo, dh, F32 ? gop::MAP_F32 : gop::MAP_BF16, rn, d, 1, d, rn * d, kRow));
+      LS_TRY((gop::launch<NP, false, false, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dh, mz, mw, mo, mo, gh, V, st)));
     }
     // dW (+)= dz^T h, with the rows that have no label cleared
     LS_TRY(pack<T>(hr, rn, d, hpack, p.dp, hplane, labels + r0, (int)V, st));
-    LS_TRY(gop::make_stack_map(&mh_mn, hpack, gop::MAP_BF16, rn, d, NP, p.dp, hplane, 64));
+    LS_TRY(gop::make_operand_map(&mhz, hpack, gop::MAP_BF16, rn, d, NP, p.dp, hplane));
     T* dW = static_cast<T*>(a.dW) + rep * a.dw_stride;
     Params gw{};
     gw.batch = 1; gw.splits = 1; gw.M = (int)V; gw.N = d; gw.alpha = a.scale; gw.alpha_dev = inv; gw.n_fast = 1;
     gw.reduce = piece > 0;
     if (p.dw_fold) {
       float* sum = reinterpret_cast<float*>(a.ws + p.o_dw);
-      LS_TRY(gop::make_stack_map(&mo, sum, gop::MAP_F32, V, d, 1, p.df, V * p.df, 32));
-      LS_TRY((gop::launch<NP, false, true, true, gop::EPI_F32>(mz_mn, mh_mn, mo, mo, gw, rn, st)));
+      LS_TRY(gop::make_output_map(&mo, sum, gop::MAP_F32, V, d, 1, p.df, V * p.df, kRow));
+      LS_TRY((gop::launch<NP, false, true, true, gop::EPI_F32>(p.nt_dw, mz, mhz, mo, mo, gw, rn, st)));
       if (r0 + p.R >= a.rows)
         LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(V * ((d + 3) / 4))), dim3(256), 0, st, 1,
                           static_cast<const float*>(sum), 1, (int64_t)0, p.df, V, d, dW));
     } else {
-      LS_TRY(gop::make_stack_map(&mo, dW, F32 ? gop::MAP_F32 : gop::MAP_BF16, V, d, 1, d, V * d, 32));
-      LS_TRY((gop::launch<NP, false, true, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(mz_mn, mh_mn, mo, mo, gw, rn, st)));
+      LS_TRY(gop::make_output_map(&mo, dW, F32 ? gop::MAP_F32 : gop::MAP_BF16, V, d, 1, d, V * d, kRow));
+      LS_TRY((gop::launch<NP, false, true, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dw, mz, mhz, mo, mo, gw, rn, st)));
     }
   }
   return LS_OK;
