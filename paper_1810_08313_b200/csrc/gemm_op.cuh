@@ -18,10 +18,9 @@
 //              accumulation truncates, which biases a sum of a thousand MMAs by about 2e-5 of its value: short
 //              chunks keep that below the last bits that matter (see kChunk*), and since a tile's last chunk is
 //              collected like any other, the epilogue of a tile runs under the products of the next one.
-// NT = 256 for one piece: 64 bytes of operands per clock and SM at the full MMA rate, 1540 of 1709 TFLOP/s (2047 x 50001 x
-// 1024).  With several pieces the chunks are so short that collecting 128 columns a thread, eight dependent
-// tcgen05.ld of 16 registers, took longer than the products (52 % of the MMA rate at 2048^3 x 8): NT = 128 collects a chunk
-// with one wait and has four accumulators.
+// NT = 256 where there are tiles for every pair (half the operand traffic per product of 128), else 128, whose chunks are
+// collected with one wait and have four accumulators.  Collecting a chunk costs about as much as two K blocks of 128-wide
+// tiles: a Newton-Schulz step of eight 2048 x 2048 matrices took 880 us at chunks of two, 780 us at eight.
 //
 // Outputs leave through boxes of shared memory per warp and TMA stores, which clip at the tensor's edge; ragged M, N
 // and K are the zero fill of the loads and that clip.  A symmetric result is computed on and above the diagonal tiles and
@@ -73,10 +72,12 @@ enum Epi {
 
 struct Params {
   int m_tiles, n_tiles, batch, splits;   // splits > 1: K is cut, split s writes plane c_z0 + z c_zstep + s
-  int num_kb, kb_per_split, chunk_kb;
+  int num_kb, kb_per_split;
+  int chunk_kb;                          // 0: chunk_of()
   int total;                             // tiles of the launch
   int tri;                               // 1: only tiles on or above the diagonal (symmetric C)
   int per, step;                         // tiles of one batch entry and split; 256 / NT
+  int dominant;                          // where one K block dominates a row's (1) or a column's (2) sum: see k_order()
   int n_fast;                            // 1: neighbouring pairs take neighbouring columns, else neighbouring rows
   int a_z0, a_zstep, b_z0, b_zstep;      // plane of batch entry z: z0 + z * zstep (+ piece)
   int c_z0, c_zstep;
@@ -119,6 +120,27 @@ __device__ __forceinline__ Tile tile_of(const Params& p, int t) {
     r.m = i - r.n * p.m_tiles;
   }
   return r;
+}
+
+// The order in which a tile takes its K blocks, and how they are cut into chunks: `first`, first + 1, ... round the end;
+// a chunk closes after every chunk_kb blocks, and each of the last `tail` blocks is a chunk of its own.
+//
+// When A is (nearly) diagonal, one product dominates an element's sum, the one with k = row (dominant = 1; 2: B is, and
+// k = column).  Every MMA that follows it in the accumulator truncates it again, a bias that the Newton-Schulz
+// iteration amplifies (error of five steps 2.9e-6 at chunks of 2 K blocks, 4.8e-6 at 4, 8.7e-6 at 8).  The blocks with
+// the tile's own k therefore come last, each in a chunk of its own, and the others, small sums of mixed signs, first.
+struct KOrder { int first, tail; };
+template <int NT>
+__device__ __forceinline__ KOrder k_order(const Params& p, const Tile& t) {
+  KOrder o{0, 0};
+  if (p.dominant != 0) {
+    const int width = (p.dominant == 1 ? kTileM : NT) / 64;
+    const int from = (p.dominant == 1 ? t.m * kTileM : t.n * NT) / 64;
+    const int end = min(from + width, p.num_kb);
+    o.tail = max(0, end - from);
+    o.first = end == p.num_kb ? 0 : end;
+  }
+  return o;
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -226,7 +248,8 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const int k1 = min(p.num_kb, k0 + p.kb_per_split);
       const int az = p.a_z0 + tl.z * p.a_zstep, bz = p.b_z0 + tl.z * p.b_zstep;
       const int ma = tl.m * kTileM + rank * 128, nb = tl.n * NT + rank * HALF;
-      for (int kb = k0; kb < k1 && !failed; ++kb) {
+      int kb = k0 + k_order<NT>(p, tl).first;
+      for (int left = k1 - k0; left > 0 && !failed; --left) {
 #pragma unroll
         for (int q = 0; q < NP; ++q) {
           if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[s], (round - 1) & 1))) { failed = true; break; }
@@ -251,6 +274,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           __syncwarp();
           if (++s == SLOTS) { s = 0; ++round; }
         }
+        if (++kb == k1) kb = k0;
       }
     }
     // the releases of the last slots arrive here from the leader's tensor core: wait for them before leaving
@@ -270,6 +294,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const Tile tl = tile_of(p, t);
         const int k0 = tl.split * p.kb_per_split;
         const int nk = min(p.num_kb, k0 + p.kb_per_split) - k0;
+        const int body = nk - k_order<NT>(p, tl).tail;
         int in_chunk = 0;
         for (int kb = 0; kb < nk; ++kb) {
           if (in_chunk == 0 && acc_round > 0 &&
@@ -286,7 +311,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
           if (!__all_sync(0xffffffffu, got)) { failed = true; break; }
           tc_fence_after_sync();
-          const bool last = in_chunk == p.chunk_kb - 1 || kb == nk - 1;
+          const bool last = in_chunk == p.chunk_kb - 1 || kb >= body - 1;
           if (lead) {
             const uint32_t d_tmem = tmem_base + (uint32_t)(acc * NT);
             // small products first
@@ -335,7 +360,8 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const Tile tl = tile_of(p, t);
       const int k0 = tl.split * p.kb_per_split;
       const int nk = min(p.num_kb, k0 + p.kb_per_split) - k0;
-      const int chunks = (nk + p.chunk_kb - 1) / p.chunk_kb;
+      const int tail = k_order<NT>(p, tl).tail;
+      const int chunks = (nk - tail + p.chunk_kb - 1) / p.chunk_kb + tail;
       uint32_t acc[G][32];
 #pragma unroll
       for (int j = 0; j < G; ++j)
@@ -568,10 +594,10 @@ int make_output_map(CUtensorMap* out, void* base, MapType type, int64_t rows, in
 // where a bounded wait that runs out is recorded (one word per device, read by ls_device_status); null on failure
 int* device_error_word();
 
-// K blocks per tensor-memory accumulator.  One MMA adds 16 products per element and truncates: 64 (24) MMAs per chunk
-// bias a sum of equal signs by about 2e-6 (0.8e-6) of its value, and sums of mixed signs by far less.  The row
-// statistics of bf16 operands, which leave in fp32, take 32.
-constexpr int kChunk1 = 16, kChunk2 = 2, kChunk3 = 1;
+// K blocks per tensor-memory accumulator.  One MMA adds 16 products per element and truncates: 64 MMAs bias a sum of equal
+// signs by about 2e-6 of its value, and sums of mixed signs by far less.  One piece: 64 MMAs for bf16 results, 32 for the row
+// statistics, which leave in fp32.  Two: 16 MMAs of the large product.  Three: 4 for fp32 results.
+constexpr int chunk_of(int np, bool stats) { return np == 1 ? (stats ? 8 : 16) : np == 2 ? 4 : 1; }
 constexpr int kPairs = 74;
 
 // Fills in the tile counts and launches.  p.splits, p.M, p.N, p.batch, p.tri, p.n_fast and the epilogue's fields are the
@@ -589,8 +615,9 @@ cudaError_t launch_nt(const CUtensorMap& a, const CUtensorMap& b, const CUtensor
   p.num_kb = (int)((K + 63) / 64);
   if (p.splits < 1) p.splits = 1;
   p.kb_per_split = (p.num_kb + p.splits - 1) / p.splits;
+  if (p.dominant != 0 && p.splits > 1) return cudaErrorInvalidValue;     // (the order goes round the whole K)
   p.splits = (p.num_kb + p.kb_per_split - 1) / p.kb_per_split;       // (callers ask split_count() first: no change here)
-  p.chunk_kb = NP == 1 ? (EPI == EPI_F32 || EPI == EPI_BF16 ? kChunk1 : kChunk1 / 2) : NP == 2 ? kChunk2 : kChunk3;
+  if (p.chunk_kb == 0) p.chunk_kb = chunk_of(NP, EPI != EPI_F32 && EPI != EPI_BF16);
   int64_t per = (int64_t)p.m_tiles * p.n_tiles;
   if (p.tri) {
     per = 0;

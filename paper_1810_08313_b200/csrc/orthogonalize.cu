@@ -293,6 +293,8 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
     else LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(nt_n, xk[cur], xk[cur], aco, act, g, p.k, st)));
     // P = a I + A C
     g.a_zstep = g.b_zstep = 4; g.b_z0 = 2; g.c_zstep = 2;
+    g.dominant = 1;             // A and C tend to multiples of I
+    g.chunk_kb = 8;
     g.n_out = 1;
     g.out_alpha[0] = kScaleP / (kScaleA * kScaleC);
     g.out_diag[0] = kNsA * kScaleP;
@@ -300,6 +302,8 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
     // X <- P X (wide) or X P (tall)
     g.a_zstep = g.b_zstep = g.c_zstep = 2; g.b_z0 = 0;
     g.tri = g.mirror = 0;
+    g.dominant = p.tall ? 2 : 1;
+    g.chunk_kb = 8;
     g.M = a.rows; g.N = a.cols;
     g.out_alpha[0] = 1.f / kScaleP;
     g.out_diag[0] = 0.f;
