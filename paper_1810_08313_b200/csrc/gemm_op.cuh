@@ -91,6 +91,7 @@ struct Params {
   int64_t stat_ld;
   const int32_t* labels;                 // [M]; a label inside the slice gets its logit written to label_logit[row]
   float* label_logit;
+  unsigned* clear;                       // a word that the launch sets to zero for the next one, or null
   // EPI_PIECES: output i (of n_out) is planes c + 2 i (first piece) and c + 2 i + 1 of the stack
   int n_out;
   float out_alpha[2], out_diag[2];       // out_alpha acc + out_diag on the diagonal
@@ -234,6 +235,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const uint32_t tmem_base = *tmem_slot;
   grid_dep_wait();
   grid_dep_launch();
+  if (blockIdx.x == 0 && threadIdx.x == 0 && p.clear != nullptr) *p.clear = 0u;
 
   // The loops of warps 0 and 1 run in all lanes (the waits too), so that addresses and descriptors are warp-uniform values;
   // one lane issues.  Slots and accumulators are counted with a place in the ring and the parity of the round.
@@ -596,8 +598,8 @@ int* device_error_word();
 
 // K blocks per tensor-memory accumulator.  One MMA adds 16 products per element and truncates: 64 MMAs bias a sum of equal
 // signs by about 2e-6 of its value, and sums of mixed signs by far less.  One piece: 64 MMAs for bf16 results, 32 for the row
-// statistics, which leave in fp32.  Two: 16 MMAs of the large product.  Three: 4 for fp32 results.
-constexpr int chunk_of(int np, bool stats) { return np == 1 ? (stats ? 8 : 16) : np == 2 ? 4 : 1; }
+// statistics, which leave in fp32.  Two: 16 MMAs of the large product.  Three: 8, for fp32 results.
+constexpr int chunk_of(int np, bool stats) { return np == 1 ? (stats ? 8 : 16) : np == 2 ? 4 : 2; }
 constexpr int kPairs = 74;
 
 // Fills in the tile counts and launches.  p.splits, p.M, p.N, p.batch, p.tri, p.n_fast and the epilogue's fields are the
@@ -645,15 +647,22 @@ cudaError_t launch(int nt, const CUtensorMap& a, const CUtensorMap& b, const CUt
                    : launch_nt<NP, 128, F16, A_MN, B_MN, EPI>(a, b, c, ct, p, K, st);
 }
 
-// Into how many parts the contraction is cut when `tiles` output tiles leave pairs idle: enough parts to give each pair
-// one, each of at least `least` K blocks.  Always a number that launch() keeps.
-inline int split_count(int64_t tiles, int64_t K, int least) {
+// Into how many parts the contraction of an M x N result is cut: the count with the least estimated time, rounds of tiles over
+// the pairs at 1.6 GHz and the full MMA rate, and for several parts 4 us for the launch that adds them up and their fp32
+// sums written and read once at 6 TB/s.  (8192 x 2048 over K = 65536: 256 tiles are four rounds, the last one with 34
+// tiles; two parts are seven half rounds.)  At least 8 K blocks a part.  Always a number that launch() keeps.
+inline int split_count(int64_t tiles, int64_t K, int np, int nt, int64_t results) {
   const int num_kb = (int)((K + 63) / 64);
-  int64_t s = tiles >= kPairs ? 1 : kPairs / tiles;
-  if (s > num_kb / least) s = num_kb / least;
-  if (s < 1) s = 1;
-  const int per = (int)((num_kb + s - 1) / s);
-  return (num_kb + per - 1) / per;
+  const double kb_us = (np == 1 ? 1 : np == 2 ? 3 : 6) * nt * 2 / 1600.0;
+  int best = 1;
+  double best_us = 0.0;
+  for (int s = 1; s <= 64 && (s == 1 || num_kb / s >= 8); ++s) {
+    const int per = (num_kb + s - 1) / s;
+    if ((num_kb + per - 1) / per != s) continue;
+    const double us = (double)((tiles * s + kPairs - 1) / kPairs) * per * kb_us + (s > 1 ? 4.0 + results * 8.0 * s / 6e6 : 0.0);
+    if (s == 1 || us < 0.97 * best_us) { best = s; best_us = us; }
+  }
+  return best;
 }
 
 }  // namespace gop

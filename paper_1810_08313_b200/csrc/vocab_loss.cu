@@ -20,7 +20,7 @@
 // in three pieces; sums over several pieces of rows are added into dW by the bulk-copy engine in fp32.
 //
 // The row sums, the loss and every accumulation are fp32 or wider and in a fixed order: results are
-// reproducible bit for bit.
+// reproducible bit for bit (the atomic counter only picks the CTA that finishes).
 #include "gemm_op.cuh"
 
 #include <math.h>
@@ -35,73 +35,48 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ bool has_label(int y, int V) { return y >= 0 && y < V; }
 
-// ---- number of rows with a label, per replica ----------------------------------------------------------------------
-__global__ void __launch_bounds__(1024) vocab_count_kernel(const int32_t* labels, int64_t rows, int V, float* inv_count) {
-  __shared__ long long red[32];
-  grid_dep_wait();
-  grid_dep_launch();
-  const int32_t* y = labels + (int64_t)blockIdx.x * rows;
-  long long n = 0;
-  for (int64_t i = threadIdx.x; i < rows; i += 1024) n += has_label(y[i], V) ? 1 : 0;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = n;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    long long t = 0;
-    for (int i = 0; i < 32; ++i) t += red[i];
-    inv_count[blockIdx.x] = t > 0 ? (float)(1.0 / (double)t) : 0.f;
-  }
-}
-
-// ---- mean loss of every replica: double sums, thread by thread and then in thread order -----------------------------
-__global__ void __launch_bounds__(1024) vocab_mean_kernel(const float* row_loss, const int32_t* labels, int64_t rows, int V,
-                                                          float* loss) {
+// ---- slices -> log-sum-exp and row loss: 32 rows per CTA, 32 warps take every 32nd slice ------------------------------
+// The last CTA to finish also counts the replica's labels (inv_count given: first piece of rows) and takes the mean of its
+// row losses (loss given: last piece), in double, thread by thread and then in thread order.  `done` counts the CTAs; the
+// product before this launch has cleared it.
+struct CombineArgs {
+  const float *stat_max, *stat_sum;
+  int64_t stat_ld;
+  int slices, rows, V;
+  const int32_t* labels;          // of the piece
+  const float* label_logit;
+  float *lse, *row_loss;
+  unsigned* done;
+  // of the whole replica
+  const int32_t* all_labels;
+  const float* all_row_loss;
+  int64_t all_rows;
+  float *inv_count, *loss;
+};
+__global__ void __launch_bounds__(1024) vocab_combine_kernel(const CombineArgs a) {
+  __shared__ float smax[32][33], ssum[32][33];
   __shared__ double sum[32];
   __shared__ long long cnt[32];
-  grid_dep_wait();
-  grid_dep_launch();
-  const float* l = row_loss + (int64_t)blockIdx.x * rows;
-  const int32_t* y = labels + (int64_t)blockIdx.x * rows;
-  double s = 0.0;
-  long long n = 0;
-  for (int64_t i = threadIdx.x; i < rows; i += 1024)
-    if (has_label(y[i], V)) { s += (double)l[i]; ++n; }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    s += __shfl_xor_sync(0xffffffffu, s, o);
-    n += __shfl_xor_sync(0xffffffffu, n, o);
-  }
-  if ((threadIdx.x & 31) == 0) { sum[threadIdx.x >> 5] = s; cnt[threadIdx.x >> 5] = n; }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    s = 0.0; n = 0;
-    for (int i = 0; i < 32; ++i) { s += sum[i]; n += cnt[i]; }
-    loss[blockIdx.x] = n > 0 ? (float)(s / (double)n) : 0.f;
-  }
-}
-
-// ---- slices -> log-sum-exp and row loss: 32 rows per CTA, 32 warps take every 32nd slice ------------------------------
-__global__ void __launch_bounds__(1024)
-vocab_combine_kernel(const float* stat_max, const float* stat_sum, int64_t stat_ld, int slices, int rows, int V,
-                     const int32_t* labels, const float* label_logit, float* lse, float* row_loss) {
-  __shared__ float smax[32][33], ssum[32][33];
+  __shared__ bool last;
   const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
   const int row = blockIdx.x * 32 + lane;
   grid_dep_wait();
   grid_dep_launch();
+  // the maximum first, so that neither loop has loads that wait for arithmetic
   float m = -INFINITY, s = 0.f;
-  if (row < rows) {
-    for (int t = wp; t < slices; t += 32) {
-      const float tm = __ldcg(stat_max + (int64_t)t * stat_ld + row), ts = __ldcg(stat_sum + (int64_t)t * stat_ld + row);
-      if (tm > m) { s = s * gop::ex2(m - tm) + ts; m = tm; }
-      else if (tm == -INFINITY) s += ts;             // only -inf (nothing to add), or NaN
-      else s += ts * gop::ex2(tm - m);
+  if (row < a.rows) {
+#pragma unroll 8
+    for (int t = wp; t < a.slices; t += 32) m = fmaxf(m, __ldcg(a.stat_max + (int64_t)t * a.stat_ld + row));
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 8
+    for (int t = wp; t < a.slices; t += 32) {
+      const float tm = __ldcg(a.stat_max + (int64_t)t * a.stat_ld + row), ts = __ldcg(a.stat_sum + (int64_t)t * a.stat_ld + row);
+      s += tm == -INFINITY ? ts : ts * gop::ex2(tm - ref);      // (only -inf: nothing to add, or NaN)
     }
   }
   smax[wp][lane] = m; ssum[wp][lane] = s;
   __syncthreads();
-  if (wp == 0 && row < rows) {
+  if (wp == 0 && row < a.rows) {
     float M = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 32; ++i) M = fmaxf(M, smax[i][lane]);
@@ -112,49 +87,89 @@ vocab_combine_kernel(const float* stat_max, const float* stat_sum, int64_t stat_
       S += tm == -INFINITY ? ssum[i][lane] : ssum[i][lane] * gop::ex2(tm - M);
     }
     const float l = (M == -INFINITY ? 0.f : M * kLn2) + logf(S);
-    lse[row] = l;
-    row_loss[row] = has_label(labels[row], V) ? l - label_logit[row] : 0.f;
+    a.lse[row] = l;
+    a.row_loss[row] = has_label(a.labels[row], a.V) ? l - a.label_logit[row] : 0.f;
+  }
+  if (a.inv_count == nullptr && a.loss == nullptr) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(a.done, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  double ls = 0.0;
+  long long n = 0;
+  for (int64_t i = threadIdx.x; i < a.all_rows; i += 1024)
+    if (has_label(a.all_labels[i], a.V)) {
+      ++n;
+      if (a.loss != nullptr) ls += (double)__ldcg(a.all_row_loss + i);
+    }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    ls += __shfl_xor_sync(0xffffffffu, ls, o);
+    n += __shfl_xor_sync(0xffffffffu, n, o);
+  }
+  if (lane == 0) { sum[wp] = ls; cnt[wp] = n; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    ls = 0.0; n = 0;
+    for (int i = 0; i < 32; ++i) { ls += sum[i]; n += cnt[i]; }
+    if (a.inv_count != nullptr) *a.inv_count = n > 0 ? (float)(1.0 / (double)n) : 0.f;
+    if (a.loss != nullptr) *a.loss = n > 0 ? (float)(ls / (double)n) : 0.f;
   }
 }
 
 // ---- exponentials -> dz, eight columns per thread ------------------------------------------------------------------------
 // bf16: in place over the fp16 numbers.
+// (Four groups of eight a thread: with one, a CTA per 2048 columns, the launch of the CTAs took as long as the bytes.)
+constexpr int kDzCols = 4 * 2048;        // columns of a CTA
 __global__ void __launch_bounds__(256)
 vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int V, const float* stat_max, int64_t stat_ld, int slice, const int32_t* labels,
                      const float* label_logit, const float* lse) {
   const int row = blockIdx.y;
-  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  const int c0 = blockIdx.x * kDzCols + threadIdx.x * 8;
   grid_dep_wait();
   grid_dep_launch();
-  if (c >= V) return;
-  uint16_t* at = e + (int64_t)row * ld + c;
+  uint16_t* at = e + (int64_t)row * ld;
   const int y = labels[row];
   if (!has_label(y, V)) {
-    *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c0 + k * 2048 < V) *reinterpret_cast<uint4*>(at + c0 + k * 2048) = make_uint4(0, 0, 0, 0);
     return;
   }
   const float l = lse[row];
-  const float f = gop::ex2(__ldg(stat_max + (int64_t)(c / slice) * stat_ld + row) - l * kLog2e);
-  uint4 u = *reinterpret_cast<const uint4*>(at);
-  uint32_t w[4] = {u.x, u.y, u.z, u.w};
-  float v[8];
+  uint4 u[4];
+  float f[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    v[2 * i] = t.x * f; v[2 * i + 1] = t.y * f;
-  }
-  const int d = y - c;
-  if (d >= 0 && d < 8) {
-    const float py = expm1f(label_logit[row] - l);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (i == d) v[i] = py;
+  for (int k = 0; k < 4; ++k) {
+    const int c = c0 + k * 2048;
+    if (c < V) {
+      u[k] = *reinterpret_cast<const uint4*>(at + c);
+      f[k] = gop::ex2(__ldg(stat_max + (int64_t)(c / slice) * stat_ld + row) - l * kLog2e);
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    w[i] = *reinterpret_cast<uint32_t*>(&t);
+  for (int k = 0; k < 4; ++k) {
+    const int c = c0 + k * 2048;
+    if (c >= V) break;
+    uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      v[2 * i] = t.x * f[k]; v[2 * i + 1] = t.y * f[k];
+    }
+    const int d = y - c;
+    if (d >= 0 && d < 8) {
+      const float py = expm1f(label_logit[row] - l);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (i == d) v[i] = py;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = gop::pack_bf16(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<uint4*>(at + c) = make_uint4(w[0], w[1], w[2], w[3]);
   }
-  *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // x = p0 + p1 + p2, each piece the bf16 rounding of what is left.  The first piece stays finite: the products pair every
@@ -283,7 +298,7 @@ struct Plan {
   int64_t stat_ld;
   int splits;           // of the contraction over V in dh
   bool dh_fold, dw_fold;   // dh, dW pass through an fp32 sum in the workspace (several parts, or rows of no whole 16 bytes)
-  size_t o_stat, o_logit, o_lse, o_rowloss, o_inv, o_e, o_dz, o_h, o_w, o_dh, o_dw, total;
+  size_t o_stat, o_logit, o_lse, o_rowloss, o_inv, o_done, o_e, o_dz, o_h, o_w, o_dh, o_dw, total;
 };
 
 int check_sizes(int m, int64_t rows, int64_t vocab, int d, int dtype) {
@@ -316,7 +331,7 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.nt_dw = gop::pick_nt(V, d, 1, false);
   p.slices = (int)(2 * ((V + p.nt - 1) / p.nt));
   const int64_t dh_tiles = (most_rows + 255) / 256 * ((d + p.nt_dh - 1) / p.nt_dh);
-  p.splits = grad && rows > 0 ? gop::split_count(dh_tiles, V, 8) : 1;
+  p.splits = grad && rows > 0 ? gop::split_count(dh_tiles, V, p.np, p.nt_dh, most_rows * (int64_t)d) : 1;
   const bool whole = d % (p.f32 ? 4 : 8) == 0;
   p.dh_fold = grad && (p.splits > 1 || !whole);
   p.dw_fold = grad && (!whole || (!p.f32 && p.pieces > 1));
@@ -327,6 +342,7 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.o_lse = take(m * rows * 4);
   p.o_rowloss = take(m * rows * 4);
   p.o_inv = take(m * 4);
+  p.o_done = take(4);
   // operands laid out anew: fp32 ones (as pieces), bf16 ones whose rows are no whole 16 bytes, and, for dW, h with the
   // rows that have no label cleared
   const bool lay = p.f32 || d % 8 != 0;
@@ -389,7 +405,8 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   float* logit = reinterpret_cast<float*>(a.ws + p.o_logit) + rep * a.rows;
   float* lse = (a.lse ? a.lse : reinterpret_cast<float*>(a.ws + p.o_lse)) + rep * a.rows;
   float* row_loss = (a.row_loss ? a.row_loss : reinterpret_cast<float*>(a.ws + p.o_rowloss)) + rep * a.rows;
-  const float* inv = reinterpret_cast<const float*>(a.ws + p.o_inv) + rep;
+  float* inv = reinterpret_cast<float*>(a.ws + p.o_inv) + rep;
+  unsigned* done = reinterpret_cast<unsigned*>(a.ws + p.o_done);
   bf* hpack = reinterpret_cast<bf*>(a.ws + p.o_h);
   bf* wpack = reinterpret_cast<bf*>(a.ws + p.o_w);
   const int64_t V = a.V;
@@ -413,7 +430,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     Params g{};
     g.batch = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
     g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld;
-    g.labels = labels + r0; g.label_logit = logit + r0;
+    g.labels = labels + r0; g.label_logit = logit + r0; g.clear = done;
     if (!p.grad) {
       LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(p.nt, mh, mw, mh, mh, g, d, st)));
     } else {
@@ -421,8 +438,13 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
       LS_TRY(gop::make_output_map(&me, a.ws + p.o_e, F32 ? gop::MAP_F32 : gop::MAP_F16, rn, V, 1, p.Vp, p.R * p.Vp, kRow));
       LS_TRY((gop::launch<NP, false, false, false, kEpi>(p.nt, mh, mw, me, me, g, d, st)));
     }
-    LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((rn + 31) / 32)), dim3(1024), 0, st, 1, stat_max, stat_sum,
-                      p.stat_ld, p.slices, (int)rn, (int)V, labels + r0, logit + r0, lse + r0, row_loss + r0));
+    CombineArgs cb{};
+    cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.slices = p.slices; cb.rows = (int)rn; cb.V = (int)V;
+    cb.labels = labels + r0; cb.label_logit = logit + r0; cb.lse = lse + r0; cb.row_loss = row_loss + r0;
+    cb.done = done; cb.all_labels = labels; cb.all_row_loss = row_loss; cb.all_rows = a.rows;
+    if (p.grad && piece == 0) cb.inv_count = inv;
+    if (r0 + p.R >= a.rows) cb.loss = a.loss + rep;
+    LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((rn + 31) / 32)), dim3(1024), 0, st, 1, cb));
     if (!p.grad) continue;
     // dz
     bf* dz = reinterpret_cast<bf*>(a.ws + p.o_dz);
@@ -435,7 +457,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
                           reinterpret_cast<const float*>(a.ws + p.o_e) + q0 * p.Vp, dz + q0 * p.Vp, p.Vp, p.R * p.Vp, (int)V,
                           ly, logit + r0 + q0, lse + r0 + q0));
       } else {
-        LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + 2047) / 2048), qn), dim3(256), 0, st, 1,
+        LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + kDzCols - 1) / kDzCols), qn), dim3(256), 0, st, 1,
                           reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)V, stat_max + q0, p.stat_ld, p.nt / 2, ly,
                           logit + r0 + q0, lse + r0 + q0));
       }
@@ -490,15 +512,10 @@ int run_vocab(const VocabArgs& a, bool grad, size_t ws_bytes, cudaStream_t st) {
         LS_TRY(cudaMemsetAsync(static_cast<char*>(a.dW) + i * a.dw_stride * eb, 0, (size_t)a.V * a.d * eb, st));
     return LS_OK;
   }
-  if (grad)
-    LS_TRY(launch_dep(vocab_count_kernel, dim3(a.m), dim3(1024), 0, st, 1, a.labels, a.rows, (int)a.V,
-                      reinterpret_cast<float*>(a.ws + p.o_inv)));
   for (int i = 0; i < a.m; ++i) {
     const int rc = p.f32 ? run_replica<float, 3>(a, p, i, st) : run_replica<__nv_bfloat16, 1>(a, p, i, st);
     if (rc != LS_OK) return rc;
   }
-  const float* row_loss = a.row_loss ? a.row_loss : reinterpret_cast<const float*>(a.ws + p.o_rowloss);
-  LS_TRY(launch_dep(vocab_mean_kernel, dim3(a.m), dim3(1024), 0, st, 1, row_loss, a.labels, a.rows, (int)a.V, a.loss));
   return LS_OK;
 }
 
