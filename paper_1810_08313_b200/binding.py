@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import math
 import os
 from typing import Optional, Sequence
 
@@ -401,6 +402,20 @@ class _Op:
             t.record_stream(self.stream)
         return t
 
+    def out(self, given, like, name: str, shape, dtype):
+        """An output [m][*tail]: the caller's tensor, or a new dense one.  Returns (tensor, pointer, stride)."""
+        if given is None:
+            t = self.new(like, shape, dtype)
+            return t, t.data_ptr(), math.prod(shape[1:])
+        ptr, _, step = self.stack(given, name, shape[1:], shape[0], dtype)
+        return given, ptr, step
+
+    def out_dense(self, given, like, name: str, shape, dtype):
+        if given is None:
+            t = self.new(like, shape, dtype)
+            return t, t.data_ptr()
+        return given, self.dense(given, name, shape, dtype)
+
     def workspace(self, like, given, nbytes: int):
         t = given
         if t is None:
@@ -461,14 +476,14 @@ def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None, mean=None, rst
         bp, _, bs = op.stack(bias, "bias", (d,), m, f32)
         if m > 1 and bs != ws:
             raise ValueError("weight and bias must have the same distance between replicas")
-    y = op.new(x, (m, rows, d), x.dtype) if out is None else out
-    mean_t = op.new(x, (m, rows), f32) if mean is None else mean
-    rstd_t = op.new(x, (m, rows), f32) if rstd is None else rstd
-    yp, _, ys = op.stack(y, "out", (rows, d), m, x.dtype)
-    mp, rp = op.dense(mean_t, "mean", (m, rows), f32), op.dense(rstd_t, "rstd", (m, rows), f32)
-    op.call("ls_layer_norm", xp, wp, bp, m, rows, d, xs, ws, dt, float(eps), yp, ys, mp, rp)
-    return (y if out is not None else _like(x, 3, y), mean_t if mean is not None else _like(x, 3, mean_t),
-            rstd_t if rstd is not None else _like(x, 3, rstd_t))
+    y, yp, ys = op.out(out, x, "out", (m, rows, d), x.dtype)
+    mean_t, mp = op.out_dense(mean, x, "mean", (m, rows), f32)
+    rstd_t, rp = op.out_dense(rstd, x, "rstd", (m, rows), f32)
+    op.call("ls_layer_norm", xp, wp, bp, m, rows, d, xs, ws, dt, eps, yp, ys, mp, rp)
+    if x.dim() == 3:
+        return y, mean_t, rstd_t
+    return (y if out is not None else y.squeeze(0), mean_t if mean is not None else mean_t.squeeze(0),
+            rstd_t if rstd is not None else rstd_t.squeeze(0))
 
 
 def layer_norm_grad_workspace(m: int, rows: int, d: int) -> int:
@@ -488,11 +503,11 @@ def layer_norm_grad(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None
     dyp, _, dys = op.stack(dy, "dy", (rows, d), m, x.dtype)
     wp, _, ws = op.stack(weight, "weight", (d,), m, f32)
     mp, rp = op.dense(mean, "mean", (m, rows), f32), op.dense(rstd, "rstd", (m, rows), f32)
-    dx_t = op.new(x, (m, rows, d), x.dtype) if dx is None else dx
-    dxp, _, dxs = op.stack(dx_t, "dx", (rows, d), m, x.dtype)
-    dw_t = op.new(x, (m, d), f32) if dweight is None else dweight
-    dwp, _, dps = op.stack(dw_t, "dweight", (d,), m, f32)
-    if dbias is None:
+    dx_t, dxp, dxs = op.out(dx, x, "dx", (m, rows, d), x.dtype)
+    dw_t, dwp, dps = op.out(dweight, x, "dweight", (m, d), f32)
+    if dbias is None and (m == 1 or dps == d):
+        db_t = op.new(x, (m, d), f32)
+    elif dbias is None:
         # beside dweight, with its distance between replicas
         db_t = op.torch.empty_strided((m, d), (dps, 1), dtype=f32, device=op.device)
         if op.stream is not None:
@@ -534,11 +549,10 @@ def vocab_loss(h, W, labels, loss=None, row_loss=None, lse=None, workspace=None,
     op = _Op(h, stream)
     dt, m, rows, d, vocab, hp, hs, wp, ws, lp = _vocab_args(op, h, W, labels)
     f32 = op.torch.float32
-    loss_t = op.new(h, (m,), f32) if loss is None else loss
-    rl_t = op.new(h, (m, rows), f32) if row_loss is None else row_loss
-    lse_t = op.new(h, (m, rows), f32) if lse is None else lse
-    outs = (op.dense(loss_t, "loss", (m,), f32), op.dense(rl_t, "row_loss", (m, rows), f32),
-            op.dense(lse_t, "lse", (m, rows), f32))
+    loss_t, loss_p = op.out_dense(loss, h, "loss", (m,), f32)
+    rl_t, rl_p = op.out_dense(row_loss, h, "row_loss", (m, rows), f32)
+    lse_t, lse_p = op.out_dense(lse, h, "lse", (m, rows), f32)
+    outs = (loss_p, rl_p, lse_p)
     base, nbytes, keep = op.workspace(h, workspace, _ws_bytes("ls_vocab_loss_ws_bytes", m, rows, vocab, d, dt, 0))
     op.call("ls_vocab_loss", hp, wp, lp, m, rows, vocab, d, hs, ws, dt, *outs, base, nbytes)
     return (loss_t, rl_t if row_loss is not None else _like(h, 3, rl_t), lse_t if lse is not None else _like(h, 3, lse_t))
@@ -551,15 +565,12 @@ def vocab_loss_grad(h, W, labels, scale: float = 1.0, dh=None, dW=None, loss=Non
     op = _Op(h, stream)
     dt, m, rows, d, vocab, hp, hs, wp, ws, lp = _vocab_args(op, h, W, labels)
     f32 = op.torch.float32
-    loss_t = op.new(h, (m,), f32) if loss is None else loss
-    rl_t = op.new(h, (m, rows), f32) if row_loss is None else row_loss
-    lse_t = op.new(h, (m, rows), f32) if lse is None else lse
-    outs = (op.dense(loss_t, "loss", (m,), f32), op.dense(rl_t, "row_loss", (m, rows), f32),
-            op.dense(lse_t, "lse", (m, rows), f32))
-    dh_t = op.new(h, (m, rows, d), h.dtype) if dh is None else dh
-    dW_t = op.new(h, (m, vocab, d), h.dtype) if dW is None else dW
-    dhp, _, dhs = op.stack(dh_t, "dh", (rows, d), m, h.dtype)
-    dwp, _, dws = op.stack(dW_t, "dW", (vocab, d), m, h.dtype)
+    loss_t, loss_p = op.out_dense(loss, h, "loss", (m,), f32)
+    rl_t, rl_p = op.out_dense(row_loss, h, "row_loss", (m, rows), f32)
+    lse_t, lse_p = op.out_dense(lse, h, "lse", (m, rows), f32)
+    outs = (loss_p, rl_p, lse_p)
+    dh_t, dhp, dhs = op.out(dh, h, "dh", (m, rows, d), h.dtype)
+    dW_t, dwp, dws = op.out(dW, h, "dW", (m, vocab, d), h.dtype)
     base, nbytes, keep = op.workspace(h, workspace, _ws_bytes("ls_vocab_loss_ws_bytes", m, rows, vocab, d, dt, 1))
     op.call("ls_vocab_loss_grad", hp, wp, lp, m, rows, vocab, d, hs, ws, dt, float(scale), *outs, dhp, dhs, dwp, dws, base,
             nbytes)
@@ -580,8 +591,7 @@ def orthogonalize(u, steps: int = 5, out=None, workspace=None, stream=None):
         raise ValueError("u must be [m][rows][cols] or [rows][cols]")
     rows, cols = u.shape[-2:]
     up, m, us = op.stack(u, "u", (rows, cols), None)
-    o = op.new(u, (m, rows, cols), u.dtype) if out is None else out
-    outp, _, outs = op.stack(o, "out", (rows, cols), m, u.dtype)
+    o, outp, outs = op.out(out, u, "out", (m, rows, cols), u.dtype)
     base, nbytes, keep = op.workspace(u, workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
     op.call("ls_orthogonalize", up, m, rows, cols, us, dt, int(steps), outp, outs, base, nbytes)
     return o if out is not None else _like(u, 3, o)

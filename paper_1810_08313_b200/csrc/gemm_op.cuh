@@ -18,9 +18,8 @@
 //              accumulation truncates, which biases a sum of a thousand MMAs by about 2e-5 of its value: short
 //              chunks keep that below the last bits that matter (see kChunk*), and since a tile's last chunk is
 //              collected like any other, the epilogue of a tile runs under the products of the next one.
-// NT = 256 where there are tiles for every pair (half the operand traffic per product of 128), else 128, whose chunks are
-// collected with one wait and have four accumulators.  Collecting a chunk costs about as much as two K blocks of 128-wide
-// tiles: a Newton-Schulz step of eight 2048 x 2048 matrices took 880 us at chunks of two, 780 us at eight.
+// NT is 256, or 128 where there are too few tiles for the pairs (pick_nt).  Collecting a chunk costs about as much as two K
+// blocks: a Newton-Schulz step of eight 2048 x 2048 matrices took 880 us at chunks of two, 780 us at eight.
 //
 // Outputs leave through boxes of shared memory per warp and TMA stores, which clip at the tensor's edge; ragged M, N
 // and K are the zero fill of the loads and that clip.  A symmetric result is computed on and above the diagonal tiles and
@@ -253,7 +252,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       int kb = k0 + k_order<NT>(p, tl).first;
       for (int left = k1 - k0; left > 0 && !failed; --left) {
 #pragma unroll
-        for (int q = 0; q < NP; ++q) {
+        for (int q = NP - 1; q >= 0; --q) {        // in the order in which the MMAs let go of them
           if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[s], (round - 1) & 1))) { failed = true; break; }
           if (lead) {
             if (rank == 0) mbar_expect_tx(&full[s], 2 * L::kSlot);      // both CTAs' bytes
@@ -302,10 +301,11 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           if (in_chunk == 0 && acc_round > 0 &&
               !__all_sync(0xffffffffu, mbar_wait(&acc_empty[acc], (acc_round - 1) & 1))) { failed = true; break; }
           uint32_t a_lo[NP], b_lo[NP];
-          int first_slot = s;
+          int slot[NP];
           bool got = true;
 #pragma unroll
-          for (int q = 0; q < NP; ++q) {
+          for (int q = NP - 1; q >= 0; --q) {
+            slot[q] = s;
             a_lo[q] = a_lo0 + (uint32_t)(s * (L::kSlot >> 4));
             b_lo[q] = b_lo0 + (uint32_t)(s * (L::kSlot >> 4));
             got = got && mbar_wait(&full[s], round & 1);
@@ -316,21 +316,25 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           const bool last = in_chunk == p.chunk_kb - 1 || kb >= body - 1;
           if (lead) {
             const uint32_t d_tmem = tmem_base + (uint32_t)(acc * NT);
-            // small products first
+            // small products first; a piece's slot is released after the last product that needs it
+            bool begin = in_chunk == 0;
 #pragma unroll
-            for (int i = NP - 1; i >= 0; --i)
+            for (int q = NP - 1; q >= 0; --q) {
 #pragma unroll
-              for (int j = NP - 1 - i; j >= 0; --j)
+              for (int o = q; o >= 0; --o) {
+                if (q + o >= NP) continue;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const bool begin = i == NP - 1 && j == 0 && k == 0;
-                  mma_f16_pair_lo(d_tmem, a_lo[i] + (A_MN ? k * 128 : k * 2), b_lo[j] + (B_MN ? k * 128 : k * 2), HI, IDESC,
-                                  begin && in_chunk == 0 ? 0u : 1u);
+                for (int turn = 0; turn < (q == o ? 1 : 2); ++turn) {
+                  const int i = turn == 0 ? q : o, j = turn == 0 ? o : q;
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) {
+                    mma_f16_pair_lo(d_tmem, a_lo[i] + (A_MN ? k * 128 : k * 2), b_lo[j] + (B_MN ? k * 128 : k * 2), HI, IDESC,
+                                    begin ? 0u : 1u);
+                    begin = false;
+                  }
                 }
-#pragma unroll
-            for (int q = 0; q < NP; ++q) {
-              mma_commit_pair(&empty[first_slot]);
-              if (++first_slot == SLOTS) first_slot = 0;
+              }
+              mma_commit_pair(&empty[slot[q]]);
             }
             if (last) mma_commit_pair(&acc_full[acc]);
           }
@@ -635,10 +639,17 @@ cudaError_t launch_nt(const CUtensorMap& a, const CUtensorMap& b, const CUtensor
   return launch_dep(kern, dim3(2 * pairs), dim3(kThreads), Smem<NP, NT>::kTotal, st, 2, a, b, c, ct, p);
 }
 
-// Columns of a tile: 256, or 128 where that leaves pairs without a tile.
+// Columns of a tile: 256, or 128 where that takes less time.  An MMA of 256 x 128 takes about 0.85 of one of 256 x 256, not
+// half (its operands come out of shared memory at 64 bytes a clock, 6 KB against 8 KB), so the halves pay only where they
+// keep idle pairs busy: compared by the rounds of tiles over the pairs.
 inline int pick_nt(int64_t M, int64_t N, int64_t batch, bool tri) {
-  const int64_t mt = (M + 255) / 256, nt = (N + 255) / 256;
-  return (tri ? mt * (mt + 1) / 2 : mt * nt) * batch < kPairs ? 128 : 256;
+  const int64_t mt = (M + 255) / 256;
+  auto tiles = [&](int64_t nt) {
+    const int64_t n = (N + nt - 1) / nt, step = 256 / nt;
+    return (tri ? mt * n - step * (mt * (mt - 1) / 2) : mt * n) * batch;
+  };
+  const int64_t wide = (tiles(256) + kPairs - 1) / kPairs, narrow = (tiles(128) + kPairs - 1) / kPairs;
+  return 0.85 * (double)narrow < (double)wide ? 128 : 256;
 }
 template <int NP, bool F16, bool A_MN, bool B_MN, int EPI>
 cudaError_t launch(int nt, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& ct,
@@ -653,7 +664,7 @@ cudaError_t launch(int nt, const CUtensorMap& a, const CUtensorMap& b, const CUt
 // tiles; two parts are seven half rounds.)  At least 8 K blocks a part.  Always a number that launch() keeps.
 inline int split_count(int64_t tiles, int64_t K, int np, int nt, int64_t results) {
   const int num_kb = (int)((K + 63) / 64);
-  const double kb_us = (np == 1 ? 1 : np == 2 ? 3 : 6) * nt * 2 / 1600.0;
+  const double kb_us = (np == 1 ? 1 : np == 2 ? 3 : 6) * (nt == 256 ? 512 : 435) / 1600.0;
   int best = 1;
   double best_us = 0.0;
   for (int s = 1; s <= 64 && (s == 1 || num_kb / s >= 8); ++s) {
