@@ -78,19 +78,22 @@ __device__ __forceinline__ void store4(T* p, int left, const float (&f)[4]) {
     for (int i = 0; i < 4; ++i) if (i < left) p[i] = (T)f[i];
   }
 }
-// f(offset in the matrix, row, column, elements left in the row) for every group of four of this warp's units
-template <typename F>
-__device__ __forceinline__ void for_groups(const MatArgs& a, F f) {
+// For each of this warp's units: load(k, offset, row, column, elements left in the row) for its four groups, then
+// use(k, ...) for them, so that the loads of a unit are in flight together.
+template <typename L, typename F>
+__device__ __forceinline__ void for_units(const MatArgs& a, L load, F use) {
   const int segs = (a.cols + kUnit - 1) / kUnit;
   const int64_t units = (int64_t)a.rows * segs;
   const int lane = threadIdx.x & 31;
   for (int64_t u = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * kWarps) {
-    const int r = (int)(u / segs), c0 = (int)(u - (int64_t)r * segs) * kUnit;
+    const int r = (int)(u / segs), c0 = (int)(u - (int64_t)r * segs) * kUnit + lane * 4;
+    const int64_t at = (int64_t)r * a.cols + c0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int c = c0 + k * 128 + lane * 4;
-      if (c < a.cols) f((int64_t)r * a.cols + c, r, c, a.cols - c);
-    }
+    for (int k = 0; k < 4; ++k)
+      if (c0 + k * 128 < a.cols) load(k, at + k * 128, r, c0 + k * 128, a.cols - c0 - k * 128);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c0 + k * 128 < a.cols) use(k, at + k * 128, r, c0 + k * 128, a.cols - c0 - k * 128);
   }
 }
 
@@ -101,23 +104,27 @@ __global__ void __launch_bounds__(32 * kWarps) ns_momentum_kernel(const MatArgs 
   grid_dep_wait();
   grid_dep_launch();
   const int64_t z = blockIdx.y;
+  const G* gz = static_cast<const G*>(a.g) + z * a.g_stride;
+  float* vz = MUON ? a.v + z * a.v_stride : nullptr;
   double s = 0.0;
-  for_groups(a, [&](int64_t at, int, int, int left) {
-    float g[4];
-    load4<G, VEC>(static_cast<const G*>(a.g) + z * a.g_stride + at, left, g);
-    if constexpr (MUON) {
-      float* vp = a.v + z * a.v_stride + at;
-      float v[4];
-      load4<float, VEC>(vp, left, v);
+  float g[4][4], v[4][4];
+  for_units(
+      a,
+      [&](int k, int64_t at, int, int, int left) {
+        load4<G, VEC>(gz + at, left, g[k]);
+        if constexpr (MUON) load4<float, VEC>(vz + at, left, v[k]);
+      },
+      [&](int k, int64_t at, int, int, int left) {
+        if constexpr (MUON) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = fmaf(a.mu, v[i], g[i]);
-      store4<float, VEC>(vp, left, v);
+          for (int i = 0; i < 4; ++i) v[k][i] = fmaf(a.mu, v[k][i], g[k][i]);
+          store4<float, VEC>(vz + at, left, v[k]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) g[i] = a.nesterov ? fmaf(a.mu, v[i], g[i]) : v[i];
-    }
+          for (int i = 0; i < 4; ++i) g[k][i] = a.nesterov ? fmaf(a.mu, v[k][i], g[k][i]) : v[k][i];
+        }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s += (double)g[i] * (double)g[i];
-  });
+        for (int i = 0; i < 4; ++i) s += (double)g[k][i] * (double)g[k][i];
+      });
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
@@ -146,31 +153,36 @@ __global__ void __launch_bounds__(32 * kWarps) ns_start_kernel(const MatArgs a, 
   __syncthreads();
   const float norm = norm_s;
   __half* hi = x + z * 2 * a.plane;
-  for_groups(a, [&](int64_t at, int r, int c, int left) {
-    float g[4];
-    load4<G, VEC>(static_cast<const G*>(a.g) + z * a.g_stride + at, left, g);
-    if constexpr (MUON) {
-      float v[4];
-      load4<float, VEC>(a.v + z * a.v_stride + at, left, v);
+  const G* gz = static_cast<const G*>(a.g) + z * a.g_stride;
+  const float* vz = MUON ? a.v + z * a.v_stride : nullptr;
+  float g[4][4], v[4][4];
+  for_units(
+      a,
+      [&](int k, int64_t at, int, int, int left) {
+        load4<G, VEC>(gz + at, left, g[k]);
+        if constexpr (MUON) load4<float, VEC>(vz + at, left, v[k]);
+      },
+      [&](int k, int64_t, int r, int c, int) {
+        if constexpr (MUON) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) g[i] = a.nesterov ? fmaf(a.mu, v[i], g[i]) : v[i];
-    }
-    float l[4];
-    uint32_t hw[2];
+          for (int i = 0; i < 4; ++i) g[k][i] = a.nesterov ? fmaf(a.mu, v[k][i], g[k][i]) : v[k][i];
+        }
+        float l[4];
+        uint32_t hw[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) g[i] = g[i] / norm * a.scale_x;
+        for (int i = 0; i < 4; ++i) g[k][i] = g[k][i] / norm * a.scale_x;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const __half2 h = __floats2half2_rn(g[2 * i], g[2 * i + 1]);
-      const float2 f = __half22float2(h);
-      l[2 * i] = g[2 * i] - f.x; l[2 * i + 1] = g[2 * i + 1] - f.y;
-      hw[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    // (rows of X are padded to whole 64 elements: the group past the last column is written as it is)
-    __half* o = hi + (int64_t)r * a.ld + c;
-    *reinterpret_cast<uint2*>(o) = make_uint2(hw[0], hw[1]);
-    *reinterpret_cast<uint2*>(o + a.plane) = make_uint2(gop::pack_f16(l[0], l[1]), gop::pack_f16(l[2], l[3]));
-  });
+        for (int i = 0; i < 2; ++i) {
+          const __half2 h = __floats2half2_rn(g[k][2 * i], g[k][2 * i + 1]);
+          const float2 f = __half22float2(h);
+          l[2 * i] = g[k][2 * i] - f.x; l[2 * i + 1] = g[k][2 * i + 1] - f.y;
+          hw[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        // (rows of X are padded to whole 64 elements: the group past the last column is written as it is)
+        __half* o = hi + (int64_t)r * a.ld + c;
+        *reinterpret_cast<uint2*>(o) = make_uint2(hw[0], hw[1]);
+        *reinterpret_cast<uint2*>(o + a.plane) = make_uint2(gop::pack_f16(l[0], l[1]), gop::pack_f16(l[2], l[3]));
+      });
 }
 
 // W <- W - step O, or out <- O, from the pieces of the last X
@@ -181,28 +193,35 @@ __global__ void __launch_bounds__(32 * kWarps) ns_finish_kernel(const MatArgs a,
   const int64_t z = blockIdx.y;
   const __half* hi = x + z * 2 * a.plane;
   const float inv = 1.f / a.scale_x;
-  for_groups(a, [&](int64_t at, int r, int c, int left) {
-    const __half* p = hi + (int64_t)r * a.ld + c;
-    const uint2 h = *reinterpret_cast<const uint2*>(p), l = *reinterpret_cast<const uint2*>(p + a.plane);
-    const uint32_t hw[2] = {h.x, h.y}, lw[2] = {l.x, l.y};
-    float o[4];
+  float* wz = MUON ? a.w + z * a.w_stride : nullptr;
+  G* oz = MUON ? nullptr : static_cast<G*>(a.out) + z * a.out_stride;
+  uint2 h[4], l[4];
+  float w[4][4];
+  for_units(
+      a,
+      [&](int k, int64_t at, int r, int c, int left) {
+        const __half* p = hi + (int64_t)r * a.ld + c;
+        h[k] = *reinterpret_cast<const uint2*>(p);
+        l[k] = *reinterpret_cast<const uint2*>(p + a.plane);
+        if constexpr (MUON) load4<float, VEC>(wz + at, left, w[k]);
+      },
+      [&](int k, int64_t at, int, int, int left) {
+        const uint32_t hw[2] = {h[k].x, h[k].y}, lw[2] = {l[k].x, l[k].y};
+        float o[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hw[i]));
-      const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&lw[i]));
-      o[2 * i] = (f.x + e.x) * inv; o[2 * i + 1] = (f.y + e.y) * inv;
-    }
-    if constexpr (MUON) {
-      float* wp = a.w + z * a.w_stride + at;
-      float w[4];
-      load4<float, VEC>(wp, left, w);
+        for (int i = 0; i < 2; ++i) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hw[i]));
+          const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&lw[i]));
+          o[2 * i] = (f.x + e.x) * inv; o[2 * i + 1] = (f.y + e.y) * inv;
+        }
+        if constexpr (MUON) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = fmaf(-step, o[i], w[i]);
-      store4<float, VEC>(wp, left, w);
-    } else {
-      store4<G, VEC>(static_cast<G*>(a.out) + z * a.out_stride + at, left, o);
-    }
-  });
+          for (int i = 0; i < 4; ++i) w[k][i] = fmaf(-step, o[i], w[k][i]);
+          store4<float, VEC>(wz + at, left, w[k]);
+        } else {
+          store4<G, VEC>(oz + at, left, o);
+        }
+      });
 }
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
