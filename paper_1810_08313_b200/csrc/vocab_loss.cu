@@ -121,17 +121,39 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(const CombineArgs a
 
 // ---- exponentials -> dz, eight columns per thread ------------------------------------------------------------------------
 // bf16: in place over the fp16 numbers.
+// What the launch that forms dz does to a row of h for dW: rows without a label are cleared, so that whatever they hold stays out
+// of dW.  h itself is the caller's: where the product read it in place (src given), the other rows are copied into the
+// workspace; where it was laid out there already, they stay.
+struct HRows {
+  const __nv_bfloat16* src;
+  __nv_bfloat16* dst;
+  int64_t ld, piece;
+  int d, np;
+};
+__device__ __forceinline__ void h_row(const HRows& h, int row, bool labelled) {
+  const int n = (h.d + 7) / 8;             // pieces of 16 bytes (rows of the workspace are padded to whole ones)
+  uint4* dst = reinterpret_cast<uint4*>(h.dst + (int64_t)row * h.ld);
+  if (!labelled) {
+    for (int q = 0; q < h.np; ++q)
+      for (int i = threadIdx.x; i < n; i += blockDim.x) dst[q * (h.piece / 8) + i] = make_uint4(0, 0, 0, 0);
+  } else if (h.src != nullptr) {
+    const uint4* src = reinterpret_cast<const uint4*>(h.src + (int64_t)row * h.d);
+    for (int i = threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
+  }
+}
+
 // (Four groups of eight a thread: with one, a CTA per 2048 columns, the launch of the CTAs took as long as the bytes.)
 constexpr int kDzCols = 4 * 2048;        // columns of a CTA
 __global__ void __launch_bounds__(256)
 vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int V, const float* stat_max, int64_t stat_ld, int slice, const int32_t* labels,
-                     const float* label_logit, const float* lse) {
+                     const float* label_logit, const float* lse, const HRows h) {
   const int row = blockIdx.y;
   const int c0 = blockIdx.x * kDzCols + threadIdx.x * 8;
   grid_dep_wait();
   grid_dep_launch();
   uint16_t* at = e + (int64_t)row * ld;
   const int y = labels[row];
+  if (blockIdx.x == 0) h_row(h, row, has_label(y, V));
   if (!has_label(y, V)) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -185,14 +207,15 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
 // fp32: logits z -> three pieces of dz.
 __global__ void __launch_bounds__(256)
 vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t piece, int V, const int32_t* labels,
-                     const float* label_logit, const float* lse) {
+                     const float* label_logit, const float* lse, const HRows h) {
   const int row = blockIdx.y;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   grid_dep_wait();
   grid_dep_launch();
+  const int y = labels[row];
+  if (blockIdx.x == 0) h_row(h, row, has_label(y, V));
   if (c >= V) return;
   const int64_t at = (int64_t)row * ld + c;
-  const int y = labels[row];
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   if (has_label(y, V)) {
       const float l = lse[row];
@@ -218,11 +241,9 @@ vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t pie
 }
 
 // ---- operands into the workspace: rows padded to whole 16 bytes, fp32 cut into three pieces ------------------------------
-// labels (optional): rows without a label are written as zeros, so that whatever they hold stays out of dW.
 template <typename T>
 __global__ void __launch_bounds__(256)
-vocab_pack_kernel(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t ld, int64_t piece, const int32_t* labels,
-                  int V, bool vec) {
+vocab_pack_kernel(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t ld, int64_t piece, bool vec) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int PER = F32 ? 4 : 8;
   const int per_row = (d + PER - 1) / PER;
@@ -233,10 +254,7 @@ vocab_pack_kernel(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t
     const int64_t row = i / per_row;
     const int c = (int)(i - row * per_row) * PER;
     T v[PER];
-    if (labels != nullptr && !has_label(labels[row], V)) {
-#pragma unroll
-      for (int k = 0; k < PER; ++k) v[k] = (T)0.f;
-    } else if (vec) {
+    if (vec) {
       *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(src + row * d + c);
     } else {
 #pragma unroll
@@ -364,12 +382,11 @@ unsigned stream_grid(int64_t items) {
 }
 
 template <typename T>
-cudaError_t pack(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t ld, int64_t piece, const int32_t* labels,
-                 int V, cudaStream_t st) {
+cudaError_t pack(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t ld, int64_t piece, cudaStream_t st) {
   const int per = 16 / sizeof(T);
   const bool vec = d % per == 0 && reinterpret_cast<uintptr_t>(src) % 16 == 0;
   return launch_dep(vocab_pack_kernel<T>, dim3(stream_grid(rows * ((d + per - 1) / per))), dim3(256), 0, st, 1, src, rows, d,
-                    dst, ld, piece, labels, V, vec);
+                    dst, ld, piece, vec);
 }
 
 struct VocabArgs {
@@ -412,7 +429,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   const int64_t V = a.V;
   const int d = a.d;
   const bool lay = F32 || d % 8 != 0;
-  if (lay) LS_TRY(pack<T>(W, V, d, wpack, p.dp, V * p.dp, nullptr, 0, st));
+  if (lay) LS_TRY(pack<T>(W, V, d, wpack, p.dp, V * p.dp, st));
   const bf* wop = lay ? wpack : reinterpret_cast<const bf*>(W);
   const int64_t wld = lay ? p.dp : d;
   CUtensorMap mw;
@@ -421,7 +438,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     const int64_t rn = a.rows - r0 < p.R ? a.rows - r0 : p.R;
     const T* hr = h + r0 * d;
     const int64_t hplane = p.R * p.dp;
-    if (lay) LS_TRY(pack<T>(hr, rn, d, hpack, p.dp, hplane, nullptr, 0, st));
+    if (lay) LS_TRY(pack<T>(hr, rn, d, hpack, p.dp, hplane, st));
     const bf* hop = lay ? hpack : reinterpret_cast<const bf*>(hr);
     const int64_t hld = lay ? p.dp : d;
     CUtensorMap mh, me;
@@ -448,18 +465,22 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     if (!p.grad) continue;
     // dz
     bf* dz = reinterpret_cast<bf*>(a.ws + p.o_dz);
+    const HRows hrows{lay ? nullptr : hop, hpack, p.dp, hplane, d, NP};
     // (grid.y is limited to 65535 rows a launch)
     for (int64_t q0 = 0; q0 < rn; q0 += 65280) {
       const unsigned qn = (unsigned)(rn - q0 < 65280 ? rn - q0 : 65280);
       const int32_t* ly = labels + r0 + q0;
+      HRows hr_q = hrows;
+      hr_q.dst += q0 * p.dp;
+      if (hr_q.src != nullptr) hr_q.src += q0 * d;
       if (F32) {
         LS_TRY(launch_dep(vocab_dz_fp32_kernel, dim3((unsigned)((V + 1023) / 1024), qn), dim3(256), 0, st, 1,
                           reinterpret_cast<const float*>(a.ws + p.o_e) + q0 * p.Vp, dz + q0 * p.Vp, p.Vp, p.R * p.Vp, (int)V,
-                          ly, logit + r0 + q0, lse + r0 + q0));
+                          ly, logit + r0 + q0, lse + r0 + q0, hr_q));
       } else {
         LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + kDzCols - 1) / kDzCols), qn), dim3(256), 0, st, 1,
                           reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)V, stat_max + q0, p.stat_ld, p.nt / 2, ly,
-                          logit + r0 + q0, lse + r0 + q0));
+                          logit + r0 + q0, lse + r0 + q0, hr_q));
       }
     }
     CUtensorMap mz, mhz, mo;
@@ -480,7 +501,6 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
       LS_TRY((gop::launch<NP, false, false, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dh, mz, mw, mo, mo, gh, V, st)));
     }
     // dW (+)= dz^T h, with the rows that have no label cleared
-    LS_TRY(pack<T>(hr, rn, d, hpack, p.dp, hplane, labels + r0, (int)V, st));
     LS_TRY(gop::make_operand_map(&mhz, hpack, gop::MAP_BF16, rn, d, NP, p.dp, hplane));
     T* dW = static_cast<T*>(a.dW) + rep * a.dw_stride;
     Params gw{};
