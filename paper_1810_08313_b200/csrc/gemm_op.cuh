@@ -93,7 +93,7 @@ struct Params {
   unsigned* clear;                       // a word that the launch sets to zero for the next one, or null
   // EPI_PIECES: output i (of n_out) is planes c + 2 i (first piece) and c + 2 i + 1 of the stack
   int n_out;
-  float out_alpha[2], out_diag[2];       // out_alpha acc + out_diag on the diagonal
+  float out_alpha[2], out_diag[2];       // out_alpha acc + out_diag on the diagonal (the last output only)
   int mirror;
   int* err;
 };
@@ -407,7 +407,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(empty_leader + (uint32_t)(buf * 8));
+        if (lane == 0) mbar_arrive_remote(empty_leader + (uint32_t)(buf * 8));
         __syncwarp();
         if (++buf == ACCS) { buf = 0; ++round; }
       }
@@ -527,8 +527,18 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         static_assert(EPI != EPI_PIECES || ROW == 64, "boxes of 32 x 32 16-bit numbers");
         const bool flip = p.mirror != 0 && tl.n >= (tl.m + 1) * p.step;          // strictly above the diagonal block
         for (int o = 0; o < p.n_out; ++o) {
-          const float alpha_o = p.out_alpha[o], diag_o = p.out_diag[o];
+          const float alpha_o = p.out_alpha[o];
           const int zp = zc + 2 * o;
+          if (p.out_diag[o] != 0.f && row >= col0 && row < col0 + HALF) {
+            // + diag I, on the accumulator (only the last output has one, so that it disturbs no other)
+            const float d = p.out_diag[o] / alpha_o;
+#pragma unroll
+            for (int j = 0; j < G; ++j)
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (row == col0 + j * 32 + i) acc[j][i] = __float_as_uint(__uint_as_float(acc[j][i]) + d);
+          }
+          __syncwarp();
 #pragma unroll
           for (int j = 0; j < G; ++j) {
             const int c0 = col0 + j * 32;
@@ -537,8 +547,8 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             uint32_t hi[16], lo[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float v0 = fmaf(alpha_o, __uint_as_float(acc[j][2 * e]), row == c0 + 2 * e ? diag_o : 0.f);
-              const float v1 = fmaf(alpha_o, __uint_as_float(acc[j][2 * e + 1]), row == c0 + 2 * e + 1 ? diag_o : 0.f);
+              const float v0 = alpha_o * __uint_as_float(acc[j][2 * e]);
+              const float v1 = alpha_o * __uint_as_float(acc[j][2 * e + 1]);
               const __half2 h = __floats2half2_rn(v0, v1);
               const float2 f = __half22float2(h);
               hi[e] = *reinterpret_cast<const uint32_t*>(&h);
@@ -622,7 +632,7 @@ cudaError_t launch_nt(const CUtensorMap& a, const CUtensorMap& b, const CUtensor
   if (p.splits < 1) p.splits = 1;
   p.kb_per_split = (p.num_kb + p.splits - 1) / p.splits;
   if (p.dominant != 0 && p.splits > 1) return cudaErrorInvalidValue;     // (the order goes round the whole K)
-  p.splits = (p.num_kb + p.kb_per_split - 1) / p.kb_per_split;       // (callers ask split_count() first: no change here)
+  p.splits = (p.num_kb + p.kb_per_split - 1) / p.kb_per_split;       // (callers ask pick_cut() first: no change here)
   if (p.chunk_kb == 0) p.chunk_kb = chunk_of(NP, EPI != EPI_F32 && EPI != EPI_BF16);
   int64_t per = (int64_t)p.m_tiles * p.n_tiles;
   if (p.tri) {
@@ -639,41 +649,42 @@ cudaError_t launch_nt(const CUtensorMap& a, const CUtensorMap& b, const CUtensor
   return launch_dep(kern, dim3(2 * pairs), dim3(kThreads), Smem<NP, NT>::kTotal, st, 2, a, b, c, ct, p);
 }
 
-// Columns of a tile: 256, or 128 where that takes less time.  An MMA of 256 x 128 takes about 0.85 of one of 256 x 256, not
-// half (its operands come out of shared memory at 64 bytes a clock, 6 KB against 8 KB), so the halves pay only where they
-// keep idle pairs busy: compared by the rounds of tiles over the pairs.
-inline int pick_nt(int64_t M, int64_t N, int64_t batch, bool tri) {
-  const int64_t mt = (M + 255) / 256;
-  auto tiles = [&](int64_t nt) {
-    const int64_t n = (N + nt - 1) / nt, step = 256 / nt;
-    return (tri ? mt * n - step * (mt * (mt - 1) / 2) : mt * n) * batch;
-  };
-  const int64_t wide = (tiles(256) + kPairs - 1) / kPairs, narrow = (tiles(128) + kPairs - 1) / kPairs;
-  return 0.85 * (double)narrow < (double)wide ? 128 : 256;
+// How a product is cut: columns of a tile (256 or 128) and parts of the contraction.
+struct Cut { int nt, splits; };
+inline int64_t tile_count(int64_t M, int64_t N, int64_t batch, bool tri, int64_t nt) {
+  const int64_t mt = (M + 255) / 256, n = (N + nt - 1) / nt, step = 256 / nt;
+  return (tri ? mt * n - step * (mt * (mt - 1) / 2) : mt * n) * batch;
 }
+// The cut with the least estimated time: rounds of tiles over the pairs at 1.6 GHz, and for several parts 5 us for the
+// launch that adds them up and their fp32 sums written and read once at 6 TB/s.  An MMA of 256 x 128 takes about 0.85 of one
+// of 256 x 256, not half (its operands come out of shared memory at 64 bytes a clock, 6 KB against 8 KB), so narrow
+// tiles pay only where they keep idle pairs busy.  (8192 x 2048 over K = 65536: 256 tiles are four rounds, the last one
+// with 34 tiles; two parts are seven half rounds.  The Gram matrices of two 1024 x 4096: 20 tiles; three parts of 22 K blocks.)  At
+// least 4 K blocks a part, and always a number of parts that launch() keeps.
+inline Cut pick_cut(int64_t M, int64_t N, int64_t batch, bool tri, int64_t K, int np, int most_splits) {
+  const int num_kb = (int)((K + 63) / 64);
+  const double kb_us = (np == 1 ? 1 : np == 2 ? 3 : 6) * 512 / 1600.0;
+  const double results = (double)M * (double)N * (double)batch * (tri ? 0.5 : 1.0);
+  Cut best{256, 1};
+  double best_us = 0.0;
+  for (int nt = 256; nt >= 128; nt /= 2) {
+    const int64_t tiles = tile_count(M, N, batch, tri, nt);
+    for (int s = 1; s <= most_splits && (s == 1 || num_kb / s >= 4); ++s) {
+      const int per = (num_kb + s - 1) / s;
+      if ((num_kb + per - 1) / per != s) continue;
+      const double us = (double)((tiles * s + kPairs - 1) / kPairs) * per * kb_us * (nt == 256 ? 1.0 : 0.85) +
+                        (s > 1 ? 5.0 + results * 8.0 * s / 6e6 : 0.0);
+      if ((nt == 256 && s == 1) || us < 0.97 * best_us) { best = Cut{nt, s}; best_us = us; }
+    }
+  }
+  return best;
+}
+inline int pick_nt(int64_t M, int64_t N, int64_t batch, bool tri) { return pick_cut(M, N, batch, tri, 64, 1, 1).nt; }
 template <int NP, bool F16, bool A_MN, bool B_MN, int EPI>
 cudaError_t launch(int nt, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& ct,
                    const Params& p, int64_t K, cudaStream_t st) {
   return nt == 256 ? launch_nt<NP, 256, F16, A_MN, B_MN, EPI>(a, b, c, ct, p, K, st)
                    : launch_nt<NP, 128, F16, A_MN, B_MN, EPI>(a, b, c, ct, p, K, st);
-}
-
-// Into how many parts the contraction of an M x N result is cut: the count with the least estimated time, rounds of tiles over
-// the pairs at 1.6 GHz and the full MMA rate, and for several parts 4 us for the launch that adds them up and their fp32
-// sums written and read once at 6 TB/s.  (8192 x 2048 over K = 65536: 256 tiles are four rounds, the last one with 34
-// tiles; two parts are seven half rounds.)  At least 8 K blocks a part.  Always a number that launch() keeps.
-inline int split_count(int64_t tiles, int64_t K, int np, int nt, int64_t results) {
-  const int num_kb = (int)((K + 63) / 64);
-  const double kb_us = (np == 1 ? 1 : np == 2 ? 3 : 6) * (nt == 256 ? 512 : 435) / 1600.0;
-  int best = 1;
-  double best_us = 0.0;
-  for (int s = 1; s <= 64 && (s == 1 || num_kb / s >= 8); ++s) {
-    const int per = (num_kb + s - 1) / s;
-    if ((num_kb + per - 1) / per != s) continue;
-    const double us = (double)((tiles * s + kPairs - 1) / kPairs) * per * kb_us + (s > 1 ? 4.0 + results * 8.0 * s / 6e6 : 0.0);
-    if (s == 1 || us < 0.97 * best_us) { best = s; best_us = us; }
-  }
-  return best;
 }
 
 }  // namespace gop

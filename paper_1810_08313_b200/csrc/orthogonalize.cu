@@ -224,6 +224,72 @@ __global__ void __launch_bounds__(32 * kWarps) ns_finish_kernel(const MatArgs a,
       });
 }
 
+// The Gram matrix from the parts of a cut contraction: A and C = b I + c A as pieces, on both sides of the diagonal.  A CTA takes a
+// block of 64 x 64 on or above it and adds the parts in index order, two columns a thread; the transposed block goes through
+// shared memory.
+struct FoldArgs {
+  const float* part;          // [m][splits] planes of n rows of ldf
+  __half* ac;                 // [m] of four planes
+  int n, splits;
+  int64_t ldf, planef, ldn, plane_n;
+  float alpha_a, alpha_c, diag_c;
+};
+__global__ void __launch_bounds__(256) ns_gram_fold_kernel(const FoldArgs a) {
+  __shared__ float tile[64][65];
+  grid_dep_wait();
+  grid_dep_launch();
+  // block of the upper triangle: column block bc, row block br <= bc
+  int bc = (int)((sqrtf(8.f * (float)blockIdx.x + 1.f) - 1.f) * 0.5f);
+  while ((bc + 1) * (bc + 2) / 2 <= (int)blockIdx.x) ++bc;
+  while (bc * (bc + 1) / 2 > (int)blockIdx.x) --bc;
+  const int br = (int)blockIdx.x - bc * (bc + 1) / 2;
+  const int64_t z = blockIdx.y;
+  const int x = (threadIdx.x & 31) * 2, y0 = threadIdx.x >> 5;
+  const float* src = a.part + z * a.splits * a.planef;
+  __half* out = a.ac + z * 4 * a.plane_n;
+  // columns col, col + 1 of row r (rows are padded to whole 64 columns)
+  auto put = [&](int r, int col, float v0, float v1) {
+    uint32_t* o = reinterpret_cast<uint32_t*>(out + (int64_t)r * a.ldn + col);
+    const int64_t plane = a.plane_n / 2;
+    auto pieces = [&](uint32_t* at, float u0, float u1) {
+      const __half2 h = __floats2half2_rn(u0, u1);
+      const float2 f = __half22float2(h);
+      at[0] = *reinterpret_cast<const uint32_t*>(&h);
+      at[plane] = gop::pack_f16(u0 - f.x, u1 - f.y);
+    };
+    pieces(o, a.alpha_a * v0, a.alpha_a * v1);
+    pieces(o + 2 * plane, fmaf(a.alpha_c, v0, r == col ? a.diag_c : 0.f), fmaf(a.alpha_c, v1, r == col + 1 ? a.diag_c : 0.f));
+  };
+  const int c = bc * 64 + x;
+  float2 v[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = make_float2(0.f, 0.f);
+  for (int s = 0; s < a.splits; ++s) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int r = br * 64 + y0 + k * 8;
+      if (r < a.n && c < a.n) {
+        const float2 u = __ldcg(reinterpret_cast<const float2*>(src + s * a.planef + (int64_t)r * a.ldf + c));
+        v[k].x += u.x; v[k].y += u.y;
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = br * 64 + y0 + k * 8;
+    if (r < a.n && c < a.n) put(r, c, v[k].x, v[k].y);
+    tile[y0 + k * 8][x] = v[k].x;
+    tile[y0 + k * 8][x + 1] = v[k].y;
+  }
+  if (br == bc) return;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = bc * 64 + y0 + k * 8, col = br * 64 + x;        // the transposed place
+    if (r < a.n && col < a.n) put(r, col, tile[x][y0 + k * 8], tile[x + 1][y0 + k * 8]);
+  }
+}
+
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 struct Plan {
@@ -231,7 +297,9 @@ struct Plan {
   bool tall;
   int64_t ld, plane;           // X
   int64_t ldn, plane_n;        // A, C, P
-  size_t o_partial, o_x[2], o_ac, o_p, total;
+  int64_t ldf, planef;         // parts of the Gram matrix
+  gop::Cut gram;
+  size_t o_partial, o_x[2], o_ac, o_p, o_gram, total;
 };
 
 Plan make_plan(int m, int rows, int cols) {
@@ -249,6 +317,10 @@ Plan make_plan(int m, int rows, int cols) {
   for (int i = 0; i < 2; ++i) p.o_x[i] = take((int64_t)m * 2 * p.plane * 2);
   p.o_ac = take((int64_t)m * 4 * p.plane_n * 2);
   p.o_p = take((int64_t)m * 2 * p.plane_n * 2);
+  p.gram = gop::pick_cut(p.n, p.n, m, true, p.k, 2, 32);
+  p.ldf = round_up(p.n, 4);
+  p.planef = p.ldf * p.n;
+  p.o_gram = take(p.gram.splits > 1 ? (int64_t)m * p.gram.splits * p.planef * 4 : 0);
   p.total = at;
   return p;
 }
@@ -283,7 +355,7 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
   LS_TRY(launch_dep(ns_start_kernel<G, MUON, VEC>, grid, dim3(32 * kWarps), 0, st, 1, a, x[0]));
   // maps: X as operand and as output; A, C and P as operands and as outputs, straight and transposed
   constexpr int kRow = gop::box_row(2);
-  CUtensorMap xk[2], xo[2], ack, aco, act, pk, po, pt;
+  CUtensorMap xk[2], xo[2], ack, aco, act, pk, po, pt, gf;
   const int64_t m = a.m;
   for (int i = 0; i < 2; ++i) {
     LS_TRY(gop::make_operand_map(&xk[i], x[i], gop::MAP_F16, a.rows, a.cols, 2 * m, p.ld, p.plane));
@@ -295,23 +367,39 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
   LS_TRY(gop::make_operand_map(&pk, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n));
   LS_TRY(gop::make_output_map(&po, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, kRow));
   LS_TRY(gop::make_output_map(&pt, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, kRow, true));
+  const bool cut = p.gram.splits > 1;
+  if (cut)
+    LS_TRY(gop::make_output_map(&gf, ws + p.o_gram, gop::MAP_F32, p.n, p.n, m * p.gram.splits, p.ldf, p.planef, kRow));
   const int nt_n = gop::pick_nt(p.n, p.n, m, true), nt_x = gop::pick_nt(a.rows, a.cols, m, false);
   int cur = 0;
   for (int s = 0; s < steps; ++s, cur ^= 1) {
     Params g{};
     g.batch = a.m;
     // A = X X^T (wide) or X^T X (tall), and C = b I + c A
-    g.M = g.N = p.n; g.tri = g.mirror = 1;
-    g.a_zstep = g.b_zstep = 2; g.c_zstep = 4;
-    g.n_out = 2;
+    g.M = g.N = p.n; g.tri = 1;
+    g.a_zstep = g.b_zstep = 2;
     const float unit = 1.f / (a.scale_x * a.scale_x);
-    g.out_alpha[0] = kScaleA * unit;
-    g.out_alpha[1] = kNsC * kScaleC * unit;
-    g.out_diag[1] = kNsB * kScaleC;
-    if (p.tall) LS_TRY((gop::launch<2, true, true, true, gop::EPI_PIECES>(nt_n, xk[cur], xk[cur], aco, act, g, p.k, st)));
-    else LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(nt_n, xk[cur], xk[cur], aco, act, g, p.k, st)));
+    if (cut) {
+      g.alpha = 1.f; g.splits = p.gram.splits; g.c_zstep = p.gram.splits;
+      if (p.tall) LS_TRY((gop::launch<2, true, true, true, gop::EPI_F32>(p.gram.nt, xk[cur], xk[cur], gf, gf, g, p.k, st)));
+      else LS_TRY((gop::launch<2, true, false, false, gop::EPI_F32>(p.gram.nt, xk[cur], xk[cur], gf, gf, g, p.k, st)));
+      const FoldArgs f{reinterpret_cast<const float*>(ws + p.o_gram), static_cast<__half*>(ac), p.n, p.gram.splits, p.ldf, p.planef,
+                       p.ldn, p.plane_n, kScaleA * unit, kNsC * kScaleC * unit, kNsB * kScaleC};
+      const unsigned nb = (unsigned)((p.n + 63) / 64);
+      LS_TRY(launch_dep(ns_gram_fold_kernel, dim3(nb * (nb + 1) / 2, (unsigned)a.m), dim3(256), 0, st, 1, f));
+      g.splits = 1;
+    } else {
+      g.mirror = 1; g.c_zstep = 4;
+      g.n_out = 2;
+      g.out_alpha[0] = kScaleA * unit;
+      g.out_alpha[1] = kNsC * kScaleC * unit;
+      g.out_diag[1] = kNsB * kScaleC;
+      if (p.tall) LS_TRY((gop::launch<2, true, true, true, gop::EPI_PIECES>(p.gram.nt, xk[cur], xk[cur], aco, act, g, p.k, st)));
+      else LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(p.gram.nt, xk[cur], xk[cur], aco, act, g, p.k, st)));
+    }
     // P = a I + A C
     g.a_zstep = g.b_zstep = 4; g.b_z0 = 2; g.c_zstep = 2;
+    g.mirror = 1;
     g.dominant = 1;             // A and C tend to multiples of I
     g.chunk_kb = 8;
     g.n_out = 1;

@@ -71,6 +71,12 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
+// The same without ordering this thread's other memory accesses beyond its CTA: enough where only tensor-memory reads that
+// have completed (tcgen05.wait::ld) are handed back.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
 // ---- thread-block clusters: rank, barrier, distributed shared memory ----------------
 __device__ __forceinline__ uint32_t cluster_ctarank() {
   uint32_t r;

@@ -345,11 +345,11 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   // tile widths of the three products (a slice of the statistics is half a tile)
   const int64_t most_rows = p.R < rows ? p.R : rows;
   p.nt = gop::pick_nt(most_rows, V, 1, false);
-  p.nt_dh = gop::pick_nt(most_rows, d, 1, false);
+  const gop::Cut cut = gop::pick_cut(most_rows, d, 1, false, V, p.np, grad ? 64 : 1);
+  p.nt_dh = cut.nt;
+  p.splits = cut.splits;
   p.nt_dw = gop::pick_nt(V, d, 1, false);
   p.slices = (int)(2 * ((V + p.nt - 1) / p.nt));
-  const int64_t dh_tiles = (most_rows + 255) / 256 * ((d + p.nt_dh - 1) / p.nt_dh);
-  p.splits = grad && rows > 0 ? gop::split_count(dh_tiles, V, p.np, p.nt_dh, most_rows * (int64_t)d) : 1;
   const bool whole = d % (p.f32 ? 4 : 8) == 0;
   p.dh_fold = grad && (p.splits > 1 || !whole);
   p.dw_fold = grad && (!whole || (!p.f32 && p.pieces > 1));
