@@ -405,7 +405,12 @@ class _Op:
     def out(self, given, like, name: str, shape, dtype):
         """An output [m][*tail]: the caller's tensor, or a new dense one.  Returns (tensor, pointer, stride)."""
         if given is None:
-            t = self.new(like, shape, dtype)
+            if like.shape == shape and like.dtype == dtype and like.is_contiguous():
+                t = self.torch.empty_like(like)
+            else:
+                t = like.new_empty(shape, dtype=dtype)
+            if self.stream is not None:
+                t.record_stream(self.stream)
             return t, t.data_ptr(), math.prod(shape[1:])
         ptr, _, step = self.stack(given, name, shape[1:], shape[0], dtype)
         return given, ptr, step

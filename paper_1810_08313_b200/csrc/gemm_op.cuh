@@ -87,10 +87,11 @@ struct Params {
   // row statistics: slice t = column / (NT / 2) of row r at [t * stat_ld + r]
   float* stat_max;                       // slice maximum * log2(e)
   float* stat_sum;                       // sum over the slice of exp(acc - slice maximum)
-  int64_t stat_ld;
-  const int32_t* labels;                 // [M]; a label inside the slice gets its logit written to label_logit[row]
-  float* label_logit;
-  unsigned* clear;                       // a word that the launch sets to zero for the next one, or null
+  int64_t stat_ld, stat_z;               // elements between slices, between batch entries
+  const int32_t* labels;                 // [M], label_z apart; a label inside the slice gets its logit written to
+  float* label_logit;                    // label_logit[row]
+  int64_t label_z;
+  unsigned* clear;                       // `batch` words that the launch sets to zero for the next one, or null
   // EPI_PIECES: output i (of n_out) is planes c + 2 i (first piece) and c + 2 i + 1 of the stack
   int n_out;
   float out_alpha[2], out_diag[2];       // out_alpha acc + out_diag on the diagonal (the last output only)
@@ -234,7 +235,8 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const uint32_t tmem_base = *tmem_slot;
   grid_dep_wait();
   grid_dep_launch();
-  if (blockIdx.x == 0 && threadIdx.x == 0 && p.clear != nullptr) *p.clear = 0u;
+  if (blockIdx.x == 0 && p.clear != nullptr)
+    for (int i = threadIdx.x; i < p.batch; i += kThreads) p.clear[i] = 0u;
 
   // The loops of warps 0 and 1 run in all lanes (the waits too), so that addresses and descriptors are warp-uniform values;
   // one lane issues.  Slots and accumulators are counted with a place in the ring and the parity of the round.
@@ -441,7 +443,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         // stays finite)
         const float ref = mx == -INFINITY ? 0.f : mx < 0.f ? fmaxf(mx * kLog2e, -3.4e38f) : mx * kLog2e;
         if (p.labels != nullptr) {
-          const int lab = row < p.M ? p.labels[row] - col0 : -1;
+          const int lab = row < p.M ? p.labels[tl.z * p.label_z + row] - col0 : -1;
           const bool mine = lab >= 0 && lab < HALF && lab + col0 < p.N;
           if (__any_sync(0xffffffffu, mine)) {
             float zl = 0.f;
@@ -450,7 +452,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
               for (int i = 0; i < 32; ++i)
                 if (lab == j * 32 + i) zl = __uint_as_float(acc[j][i]);
-            if (mine) p.label_logit[row] = zl;
+            if (mine) p.label_logit[tl.z * p.label_z + row] = zl;
           }
         }
         if constexpr (EPI == EPI_STATS_F32) {
@@ -479,7 +481,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             acc[j][i] = __float_as_uint(e);
           }
         if (row < p.M) {
-          const int64_t at = (int64_t)(tl.n * 2 + cs) * p.stat_ld + row;
+          const int64_t at = tl.z * p.stat_z + (int64_t)(tl.n * 2 + cs) * p.stat_ld + row;
           p.stat_max[at] = mx == -INFINITY ? -INFINITY : ref;
           p.stat_sum[at] = (part[0] + part[1]) + (part[2] + part[3]);
         }
@@ -611,9 +613,9 @@ int make_output_map(CUtensorMap* out, void* base, MapType type, int64_t rows, in
 int* device_error_word();
 
 // K blocks per tensor-memory accumulator.  One MMA adds 16 products per element and truncates: 64 MMAs bias a sum of equal
-// signs by about 2e-6 of its value, and sums of mixed signs by far less.  One piece: 64 MMAs for bf16 results, 32 for the row
-// statistics, which leave in fp32.  Two: 16 MMAs of the large product.  Three: 8, for fp32 results.
-constexpr int chunk_of(int np, bool stats) { return np == 1 ? (stats ? 8 : 16) : np == 2 ? 4 : 2; }
+// signs by about 2e-6 of its value, and sums of mixed signs by far less.  One piece: 256 MMAs for results that are rounded to bf16
+// (whose half step is 4e-3), 32 for the row statistics, which leave in fp32.  Two: 16 MMAs of the large product.  Three: 8.
+constexpr int chunk_of(int np, bool stats) { return np == 1 ? (stats ? 8 : 64) : np == 2 ? 4 : 2; }
 constexpr int kPairs = 74;
 
 // Fills in the tile counts and launches.  p.splits, p.M, p.N, p.batch, p.tri, p.n_fast and the epilogue's fields are the

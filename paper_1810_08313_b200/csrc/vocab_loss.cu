@@ -39,9 +39,10 @@ __device__ __forceinline__ bool has_label(int y, int V) { return y >= 0 && y < V
 // The last CTA to finish also counts the replica's labels (inv_count given: first piece of rows) and takes the mean of its
 // row losses (loss given: last piece), in double, thread by thread and then in thread order.  `done` counts the CTAs; the
 // product before this launch has cleared it.
+// (blockIdx.y: replicas taken together, stat_z and all_rows apart.)
 struct CombineArgs {
   const float *stat_max, *stat_sum;
-  int64_t stat_ld;
+  int64_t stat_ld, stat_z;
   int slices, rows, V;
   const int32_t* labels;          // of the piece
   const float* label_logit;
@@ -53,13 +54,19 @@ struct CombineArgs {
   int64_t all_rows;
   float *inv_count, *loss;
 };
-__global__ void __launch_bounds__(1024) vocab_combine_kernel(const CombineArgs a) {
+__global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
   __shared__ float smax[32][33], ssum[32][33];
   __shared__ double sum[32];
   __shared__ long long cnt[32];
   __shared__ bool last;
   const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
   const int row = blockIdx.x * 32 + lane;
+  const int64_t z = blockIdx.y;
+  a.stat_max += z * a.stat_z; a.stat_sum += z * a.stat_z;
+  a.labels += z * a.all_rows; a.label_logit += z * a.all_rows; a.lse += z * a.all_rows; a.row_loss += z * a.all_rows;
+  a.all_labels += z * a.all_rows; a.all_row_loss += z * a.all_rows;
+  a.done += z;
+  if (a.loss != nullptr) a.loss += z;
   grid_dep_wait();
   grid_dep_launch();
   // the maximum first, so that neither loop has loads that wait for arithmetic
@@ -307,6 +314,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 struct Plan {
   bool f32, grad;
   int np;
+  int batch;            // replicas taken together: all of them where that leaves one product and one combining launch
   int64_t R;            // rows of a piece
   int64_t pieces;
   int64_t Vp, dp;       // padded row lengths: probabilities, packed operands
@@ -342,9 +350,11 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.R = rows > 0 ? round_up((rows + p.pieces - 1) / p.pieces, 256) : 0;
   p.pieces = rows > 0 ? (rows + p.R - 1) / p.R : 0;
   p.stat_ld = p.R;
+  const bool lay = p.f32 || d % 8 != 0;
+  p.batch = !grad && !lay && p.pieces == 1 && p.R * (p.Vp / 64 + 2) * 8 * m <= (int64_t)1 << 28 ? m : 1;
   // tile widths of the three products (a slice of the statistics is half a tile)
   const int64_t most_rows = p.R < rows ? p.R : rows;
-  p.nt = gop::pick_nt(most_rows, V, 1, false);
+  p.nt = gop::pick_nt(most_rows, V, p.batch, false);
   const gop::Cut cut = gop::pick_cut(most_rows, d, 1, false, V, p.np, grad ? 64 : 1);
   p.nt_dh = cut.nt;
   p.splits = cut.splits;
@@ -355,15 +365,14 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.dw_fold = grad && (!whole || (!p.f32 && p.pieces > 1));
   size_t at = 0;
   auto take = [&at](int64_t bytes) { size_t o = at; at += (size_t)round_up(bytes, 256); return o; };
-  p.o_stat = take(2 * p.slices * p.stat_ld * 4);
+  p.o_stat = take(2 * (int64_t)p.batch * p.slices * p.stat_ld * 4);
   p.o_logit = take(m * rows * 4);
   p.o_lse = take(m * rows * 4);
   p.o_rowloss = take(m * rows * 4);
   p.o_inv = take(m * 4);
-  p.o_done = take(4);
+  p.o_done = take(4 * (int64_t)p.batch);
   // operands laid out anew: fp32 ones (as pieces), bf16 ones whose rows are no whole 16 bytes, and, for dW, h with the
   // rows that have no label cleared
-  const bool lay = p.f32 || d % 8 != 0;
   p.o_h = take(lay || grad ? p.np * p.R * p.dp * 2 : 0);
   p.o_w = take(lay ? p.np * V * p.dp * 2 : 0);
   if (grad) {
@@ -408,7 +417,7 @@ struct VocabArgs {
     if ((x) != cudaSuccess) return LS_ERR_CUDA;     \
   } while (0)
 
-// One replica.  T: element type of h, W, dh, dW.  NP: pieces an operand is given in.
+// One replica, or p.batch of them from `rep` on.  T: element type of h, W, dh, dW.  NP: pieces an operand is given in.
 template <typename T, int NP>
 int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   constexpr bool F32 = NP == 3;
@@ -418,7 +427,8 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   const T* W = static_cast<const T*>(a.W) + rep * a.w_stride;
   const int32_t* labels = a.labels + rep * a.rows;
   float* stat_max = reinterpret_cast<float*>(a.ws + p.o_stat);
-  float* stat_sum = stat_max + p.slices * p.stat_ld;
+  const int64_t stat_z = p.slices * p.stat_ld;
+  float* stat_sum = stat_max + p.batch * stat_z;
   float* logit = reinterpret_cast<float*>(a.ws + p.o_logit) + rep * a.rows;
   float* lse = (a.lse ? a.lse : reinterpret_cast<float*>(a.ws + p.o_lse)) + rep * a.rows;
   float* row_loss = (a.row_loss ? a.row_loss : reinterpret_cast<float*>(a.ws + p.o_rowloss)) + rep * a.rows;
@@ -433,7 +443,8 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   const bf* wop = lay ? wpack : reinterpret_cast<const bf*>(W);
   const int64_t wld = lay ? p.dp : d;
   CUtensorMap mw;
-  LS_TRY(gop::make_operand_map(&mw, wop, gop::MAP_BF16, V, d, NP, wld, V * wld));
+  const bool many = p.batch > 1;
+  LS_TRY(gop::make_operand_map(&mw, wop, gop::MAP_BF16, V, d, many ? p.batch : NP, wld, many ? a.w_stride : V * wld));
   for (int64_t r0 = 0, piece = 0; r0 < a.rows; r0 += p.R, ++piece) {
     const int64_t rn = a.rows - r0 < p.R ? a.rows - r0 : p.R;
     const T* hr = h + r0 * d;
@@ -442,11 +453,11 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     const bf* hop = lay ? hpack : reinterpret_cast<const bf*>(hr);
     const int64_t hld = lay ? p.dp : d;
     CUtensorMap mh, me;
-    LS_TRY(gop::make_operand_map(&mh, hop, gop::MAP_BF16, rn, d, NP, hld, hplane));
+    LS_TRY(gop::make_operand_map(&mh, hop, gop::MAP_BF16, rn, d, many ? p.batch : NP, hld, many ? a.h_stride : hplane));
     // logits
     Params g{};
-    g.batch = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
-    g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld;
+    g.batch = p.batch; g.a_zstep = g.b_zstep = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
+    g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld; g.stat_z = stat_z; g.label_z = a.rows;
     g.labels = labels + r0; g.label_logit = logit + r0; g.clear = done;
     if (!p.grad) {
       LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(p.nt, mh, mw, mh, mh, g, d, st)));
@@ -456,12 +467,12 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
       LS_TRY((gop::launch<NP, false, false, false, kEpi>(p.nt, mh, mw, me, me, g, d, st)));
     }
     CombineArgs cb{};
-    cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.slices = p.slices; cb.rows = (int)rn; cb.V = (int)V;
+    cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices; cb.rows = (int)rn; cb.V = (int)V;
     cb.labels = labels + r0; cb.label_logit = logit + r0; cb.lse = lse + r0; cb.row_loss = row_loss + r0;
     cb.done = done; cb.all_labels = labels; cb.all_row_loss = row_loss; cb.all_rows = a.rows;
     if (p.grad && piece == 0) cb.inv_count = inv;
     if (r0 + p.R >= a.rows) cb.loss = a.loss + rep;
-    LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((rn + 31) / 32)), dim3(1024), 0, st, 1, cb));
+    LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((rn + 31) / 32), (unsigned)p.batch), dim3(1024), 0, st, 1, cb));
     if (!p.grad) continue;
     // dz
     bf* dz = reinterpret_cast<bf*>(a.ws + p.o_dz);
@@ -532,7 +543,7 @@ int run_vocab(const VocabArgs& a, bool grad, size_t ws_bytes, cudaStream_t st) {
         LS_TRY(cudaMemsetAsync(static_cast<char*>(a.dW) + i * a.dw_stride * eb, 0, (size_t)a.V * a.d * eb, st));
     return LS_OK;
   }
-  for (int i = 0; i < a.m; ++i) {
+  for (int i = 0; i < a.m; i += p.batch) {
     const int rc = p.f32 ? run_replica<float, 3>(a, p, i, st) : run_replica<__nv_bfloat16, 1>(a, p, i, st);
     if (rc != LS_OK) return rc;
   }
