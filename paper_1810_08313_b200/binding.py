@@ -357,7 +357,7 @@ class _Op:
             if stream.device != self.device:
                 raise ValueError("the stream belongs to another device than the tensors")
             self.raw = int(stream.cuda_stream)
-            # tensors of the current stream that another one uses
+            # None where it is the current one
             self.stream = stream if stream != torch.cuda.current_stream(self.device) else None
 
     def stack(self, t, name: str, tail, m: Optional[int], dtype=None):
@@ -397,20 +397,26 @@ class _Op:
         return self.stack(t, name, shape[1:], shape[0], dtype)[0]
 
     def new(self, like, shape, dtype):
-        t = like.new_empty(shape, dtype=dtype)
-        if self.stream is not None:
-            t.record_stream(self.stream)
+        if self.stream is None:
+            return like.new_empty(shape, dtype=dtype)
+        return self.elsewhere(lambda: like.new_empty(shape, dtype=dtype))
+
+    def elsewhere(self, make):
+        """A new tensor for a call on a stream that is not the current one: out of that stream's memory (a block that the
+        current stream has given back may still be read by what is queued there), and kept from reuse until the current
+        stream, where the caller will read it, is through with it."""
+        with self.torch.cuda.stream(self.stream):
+            t = make()
+        t.record_stream(self.torch.cuda.current_stream(self.device))
         return t
 
     def out(self, given, like, name: str, shape, dtype):
         """An output [m][*tail]: the caller's tensor, or a new dense one.  Returns (tensor, pointer, stride)."""
         if given is None:
-            if like.shape == shape and like.dtype == dtype and like.is_contiguous():
+            if self.stream is None and like.shape == shape and like.dtype == dtype and like.is_contiguous():
                 t = self.torch.empty_like(like)
             else:
-                t = like.new_empty(shape, dtype=dtype)
-            if self.stream is not None:
-                t.record_stream(self.stream)
+                t = self.new(like, shape, dtype)
             return t, t.data_ptr(), math.prod(shape[1:])
         ptr, _, step = self.stack(given, name, shape[1:], shape[0], dtype)
         return given, ptr, step
@@ -514,9 +520,9 @@ def layer_norm_grad(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None
         db_t = op.new(x, (m, d), f32)
     elif dbias is None:
         # beside dweight, with its distance between replicas
-        db_t = op.torch.empty_strided((m, d), (dps, 1), dtype=f32, device=op.device)
-        if op.stream is not None:
-            db_t.record_stream(op.stream)
+        def beside():
+            return op.torch.empty_strided((m, d), (dps, 1), dtype=f32, device=op.device)
+        db_t = beside() if op.stream is None else op.elsewhere(beside)
     else:
         db_t = dbias
     dbp, _, dbs = op.stack(db_t, "dbias", (d,), m, f32)

@@ -694,6 +694,36 @@ def test_two_calls_at_once_on_two_streams():
     b.device_status()
 
 
+def test_new_tensors_on_another_stream_are_not_blocks_in_use():
+    """A block that the current stream has given back while a read of it is still queued there must not become an output
+    or a workspace of a call on another stream."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    s = _inputs(8, "fp32")
+    side = torch.cuda.Stream()
+    like = [(2, 150, 72), (2, 150), (2,), (2, 333, 72), (2, 72)]
+    nbytes = [b.orthogonalize_workspace(2, 150, 72), b.vocab_loss_workspace(2, 150, 333, 72, "fp32", True),
+              b.layer_norm_grad_workspace(2, 150, 72)]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    copies = []
+    for n in [4 * math.prod(t) for t in like] * 3 + nbytes:
+        block = torch.full((n,), 77, dtype=torch.uint8, device="cuda")
+        copies.append(torch.empty_like(block))
+        copies[-1].copy_(block)
+        del block
+    y, mean, rstd = b.layer_norm(s["x"], s["w"], s["bias"], stream=side)
+    b.layer_norm_grad(y, s["x"], s["w"], mean, rstd, stream=side)
+    b.vocab_loss(y, s["W"], s["labels"], stream=side)
+    b.vocab_loss_grad(y, s["W"], s["labels"], stream=side)
+    b.orthogonalize(s["x"], stream=side)
+    torch.cuda.synchronize()
+    for c in copies:
+        assert bool((c == 77).all())
+    assert torch.equal(y, b.layer_norm(s["x"], s["w"], s["bias"])[0])
+    b.device_status()
+
+
 def test_given_workspaces_and_outputs():
     import torch
     from paper_1810_08313_b200 import binding as b
