@@ -69,16 +69,26 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
   if (a.loss != nullptr) a.loss += z;
   grid_dep_wait();
   grid_dep_launch();
-  // the maximum first, so that neither loop has loads that wait for arithmetic
+  // eight slices at a time, their sixteen loads in flight together
   float m = -INFINITY, s = 0.f;
   if (row < a.rows) {
-#pragma unroll 8
-    for (int t = wp; t < a.slices; t += 32) m = fmaxf(m, __ldcg(a.stat_max + (int64_t)t * a.stat_ld + row));
-    const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll 8
-    for (int t = wp; t < a.slices; t += 32) {
-      const float tm = __ldcg(a.stat_max + (int64_t)t * a.stat_ld + row), ts = __ldcg(a.stat_sum + (int64_t)t * a.stat_ld + row);
-      s += tm == -INFINITY ? ts : ts * gop::ex2(tm - ref);      // (only -inf: nothing to add, or NaN)
+    for (int t0 = wp; t0 < a.slices; t0 += 8 * 32) {
+      float tm[8], ts[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t at = (int64_t)(t0 + i * 32) * a.stat_ld + row;
+        const bool in = t0 + i * 32 < a.slices;
+        tm[i] = in ? __ldcg(a.stat_max + at) : -INFINITY;
+        ts[i] = in ? __ldcg(a.stat_sum + at) : 0.f;
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, tm[i]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      if (m != -INFINITY) s *= gop::ex2(m - ref);               // (only -inf so far: nothing to add, or NaN)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += tm[i] == -INFINITY ? ts[i] : ts[i] * gop::ex2(tm[i] - ref);
+      m = top;
     }
   }
   smax[wp][lane] = m; ssum[wp][lane] = s;
@@ -149,55 +159,58 @@ __device__ __forceinline__ void h_row(const HRows& h, int row, bool labelled) {
   }
 }
 
-// (Four groups of eight a thread: with one, a CTA per 2048 columns, the launch of the CTAs took as long as the bytes.)
-constexpr int kDzCols = 4 * 2048;        // columns of a CTA
+// A CTA takes four rows of 2048 columns: a thread's four groups of eight columns lie below one another, in one slice, whose four
+// maxima are one load.  (Four groups of one row read as many sectors of the statistics as of a row; 8192 x 65536: 424 us.)
+constexpr int kDzCols = 2048, kDzRows = 4;
 __global__ void __launch_bounds__(256)
-vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int V, const float* stat_max, int64_t stat_ld, int slice, const int32_t* labels,
-                     const float* label_logit, const float* lse, const HRows h) {
-  const int row = blockIdx.y;
-  const int c0 = blockIdx.x * kDzCols + threadIdx.x * 8;
+vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int V, const float* stat_max, int64_t stat_ld, int slice,
+                     const int32_t* labels, const float* label_logit, const float* lse, const HRows h) {
+  const int row0 = blockIdx.y * kDzRows;
+  const int c = blockIdx.x * kDzCols + threadIdx.x * 8;
   grid_dep_wait();
   grid_dep_launch();
-  uint16_t* at = e + (int64_t)row * ld;
-  const int y = labels[row];
-  if (blockIdx.x == 0) h_row(h, row, has_label(y, V));
-  if (!has_label(y, V)) {
+  int y[kDzRows];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (c0 + k * 2048 < V) *reinterpret_cast<uint4*>(at + c0 + k * 2048) = make_uint4(0, 0, 0, 0);
-    return;
-  }
-  const float l = lse[row];
-  uint4 u[4];
-  float f[4];
+  for (int k = 0; k < kDzRows; ++k) y[k] = row0 + k < rows ? labels[row0 + k] : -1;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int c = c0 + k * 2048;
-    if (c < V) {
-      u[k] = *reinterpret_cast<const uint4*>(at + c);
-      f[k] = gop::ex2(__ldg(stat_max + (int64_t)(c / slice) * stat_ld + row) - l * kLog2e);
-    }
-  }
+  for (int k = 0; k < kDzRows; ++k)
+    if (k % gridDim.x == blockIdx.x && row0 + k < rows) h_row(h, row0 + k, has_label(y[k], V));
+  if (c >= V) return;
+  uint16_t* at = e + (int64_t)row0 * ld + c;
+  // (rows of the statistics beyond the last one exist, padded to whole 256)
+  const float4 top4 = __ldg(reinterpret_cast<const float4*>(stat_max + (int64_t)(c / slice) * stat_ld + row0));
+  const float top[kDzRows] = {top4.x, top4.y, top4.z, top4.w};
+  uint4 u[kDzRows];
+  float l[kDzRows];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int c = c0 + k * 2048;
-    if (c >= V) break;
-    uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      v[2 * i] = t.x * f[k]; v[2 * i + 1] = t.y * f[k];
-    }
-    const int d = y - c;
-    if (d >= 0 && d < 8) {
-      const float py = expm1f(label_logit[row] - l);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) if (i == d) v[i] = py;
+  for (int k = 0; k < kDzRows; ++k)
+    if (has_label(y[k], V)) {
+      u[k] = *reinterpret_cast<const uint4*>(at + k * ld);
+      l[k] = lse[row0 + k];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = gop::pack_bf16(v[2 * i], v[2 * i + 1]);
-    *reinterpret_cast<uint4*>(at + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  for (int k = 0; k < kDzRows; ++k) {
+    if (row0 + k >= rows) break;
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (has_label(y[k], V)) {
+      const uint32_t in[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+      const float f = gop::ex2(top[k] - l[k] * kLog2e);
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&in[i]));
+        v[2 * i] = t.x * f; v[2 * i + 1] = t.y * f;
+      }
+      const int d = y[k] - c;
+      if (d >= 0 && d < 8) {
+        const float py = expm1f(label_logit[row0 + k] - l[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i == d) v[i] = py;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = gop::pack_bf16(v[2 * i], v[2 * i + 1]);
+    }
+    *reinterpret_cast<uint4*>(at + k * ld) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -225,7 +238,7 @@ vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t pie
   const int64_t at = (int64_t)row * ld + c;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   if (has_label(y, V)) {
-      const float l = lse[row];
+    const float l = lse[row];
     const float4 u = *reinterpret_cast<const float4*>(z + at);
     v[0] = expf(u.x - l); v[1] = expf(u.y - l); v[2] = expf(u.z - l); v[3] = expf(u.w - l);
     const int d = y - c;
@@ -489,9 +502,9 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
                           reinterpret_cast<const float*>(a.ws + p.o_e) + q0 * p.Vp, dz + q0 * p.Vp, p.Vp, p.R * p.Vp, (int)V,
                           ly, logit + r0 + q0, lse + r0 + q0, hr_q));
       } else {
-        LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + kDzCols - 1) / kDzCols), qn), dim3(256), 0, st, 1,
-                          reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)V, stat_max + q0, p.stat_ld, p.nt / 2, ly,
-                          logit + r0 + q0, lse + r0 + q0, hr_q));
+        LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + kDzCols - 1) / kDzCols), (qn + kDzRows - 1) / kDzRows),
+                          dim3(256), 0, st, 1, reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)qn, (int)V,
+                          stat_max + q0, p.stat_ld, p.nt / 2, ly, logit + r0 + q0, lse + r0 + q0, hr_q));
       }
     }
     CUtensorMap mz, mhz, mo;
