@@ -442,9 +442,9 @@ int ls_layer_norm_grad(const void* dy_dev, const void* x_dev, const float* weigh
  * vocab <= 2^24, d <= 65536.  When a row is whole 16-byte pieces (d a multiple of 8 for bf16, 4 for fp32), h, W, dh, dW
  * and their strides must be 16-byte multiples (else LS_ERR_INVALID_ARG).
  * In fp32 an infinite element of h or W counts as 3.39e38 with its sign.
- * Workspace of the loss: a few numbers a row and 128 columns (and a copy of both operands for fp32 or d not a multiple
- * of 8).  Of the gradient: also the probabilities of a piece of rows, at most about 1 GiB, and the fp32 sum
- * of dW for bf16 when the rows take several pieces. */
+ * Workspace of the loss: two numbers a row and slice of 64 or 128 columns (and a copy of both operands for fp32 or d not
+ * a multiple of 8).  Of the gradient: also the probabilities of a piece of rows, at most about 1 GiB but at least 256
+ * rows, h of that piece, and the fp32 sum of dW for bf16 when the rows take several pieces. */
 int ls_vocab_loss_ws_bytes(int m, int64_t rows, int64_t vocab, int d, int dtype, int grad, size_t* bytes);
 int ls_vocab_loss(const void* h_dev, const void* W_dev, const int32_t* labels_dev, int m, int64_t rows, int64_t vocab,
                   int d, int64_t h_stride, int64_t w_stride, int dtype, float* loss_dev, float* row_loss_dev,
@@ -459,8 +459,11 @@ int ls_vocab_loss_grad(const void* h_dev, const void* W_dev, const int32_t* labe
 
 /* Orthogonalisation of the matrices u [m][rows][cols] by `steps` (1..64) Newton-Schulz steps:
  *   X = u / (|u|_F + 1e-7);  repeat: A = X X^T, X = 3.4445 X + (-4.7750 A + 2.0315 A A) X;  out = X
- * (for rows > cols the same of the transpose, transposed back).  Products are accurate to about 22 bits.  out has u's
- * dtype and shape.  rows, cols <= 32768.  The workspace also serves ls_muon_step. */
+ * (for rows > cols the same of the transpose, transposed back).  Products are accurate to about 22 bits; from bf16 numbers
+ * two or three steps of a large matrix longer than wide may be taken together (A of the first, A' = A P P after that),
+ * which is off by up to about 1e-5 of the result's norm before it is rounded.  |u|_F is added up in double; a matrix whose
+ * norm is not large against 1e-7 comes out smaller, as the formula has it.  out has u's dtype and shape.
+ * rows, cols <= 32768.  The workspace also serves ls_muon_step. */
 int ls_orthogonalize_ws_bytes(int m, int rows, int cols, size_t* bytes);
 int ls_orthogonalize(const void* u_dev, int m, int rows, int cols, int64_t u_stride, int dtype, int steps, void* out_dev,
                      int64_t out_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream);

@@ -652,7 +652,7 @@ cudaError_t launch_nt(const CUtensorMap& a, const CUtensorMap& b, const CUtensor
 }
 
 // How a product is cut: columns of a tile (256 or 128) and parts of the contraction.
-struct Cut { int nt, splits; };
+struct Cut { int nt, splits; double us; };       // (us: the estimate below)
 inline int64_t tile_count(int64_t M, int64_t N, int64_t batch, bool tri, int64_t nt) {
   const int64_t mt = (M + 255) / 256, n = (N + nt - 1) / nt, step = 256 / nt;
   return (tri ? mt * n - step * (mt * (mt - 1) / 2) : mt * n) * batch;
@@ -667,8 +667,7 @@ inline Cut pick_cut(int64_t M, int64_t N, int64_t batch, bool tri, int64_t K, in
   const int num_kb = (int)((K + 63) / 64);
   const double kb_us = (np == 1 ? 1 : np == 2 ? 3 : 6) * 512 / 1600.0;
   const double results = (double)M * (double)N * (double)batch * (tri ? 0.5 : 1.0);
-  Cut best{256, 1};
-  double best_us = 0.0;
+  Cut best{256, 1, 0.0};
   for (int nt = 256; nt >= 128; nt /= 2) {
     const int64_t tiles = tile_count(M, N, batch, tri, nt);
     for (int s = 1; s <= most_splits && (s == 1 || num_kb / s >= 4); ++s) {
@@ -676,7 +675,7 @@ inline Cut pick_cut(int64_t M, int64_t N, int64_t batch, bool tri, int64_t K, in
       if ((num_kb + per - 1) / per != s) continue;
       const double us = (double)((tiles * s + kPairs - 1) / kPairs) * per * kb_us * (nt == 256 ? 1.0 : 0.85) +
                         (s > 1 ? 5.0 + results * 8.0 * s / 6e6 : 0.0);
-      if ((nt == 256 && s == 1) || us < 0.97 * best_us) { best = Cut{nt, s}; best_us = us; }
+      if ((nt == 256 && s == 1) || us < 0.97 * best.us) best = Cut{nt, s, us};
     }
   }
   return best;

@@ -2,10 +2,9 @@
 // ls_muon_step; the update of the Muon optimiser).
 //
 //   X_0 = U / (|U|_F + 1e-7)
-//   X_{k+1} = a X_k + (b A + c A^2) X_k,   A = X_k X_k^T,   (a, b, c) = (3.4445, -4.7750, 2.0315)
+//   X_{k+1} = a X_k + (b A + c A^2) X_k = P_k X_k,   A = X_k X_k^T,   P = a I + A (b I + c A)
 //
-//             = P_k X_k,  P = a I + A (b I + c A)
-// which drives every singular value of U towards 1 (into about [0.7, 1.2]) and leaves the singular vectors alone.  With
+// with (a, b, c) = (3.4445, -4.7750, 2.0315), which drives every singular value of U towards 1 (into about [0.7, 1.2]) and leaves the singular vectors alone.  With
 // n the shorter and k the longer side the step is two symmetric products of n x n results and one full one.  The side of
 // the Gram matrix is the shorter one: A = X X^T and P X for a wide matrix, A = X^T X and X P for a tall one; both
 // read X as it lies (K- or MN-major operands), nothing is transposed.
@@ -16,6 +15,14 @@
 // symmetric products only the tiles on and above the diagonal are computed; the epilogue writes them to both places.
 // The multiples of I are added in the epilogues (one launch writes A and C from the same accumulator), so that no
 // epilogue reads a matrix.  Bound by the tensor cores: 3 (n^2 k + n^3 + 2 n^2 k) / 2 MMA multiply-adds a step.
+//
+// Steps taken together: A and P are polynomials of the first A, so they commute and A_{k+1} = A_k P_k P_k.  Two or three steps
+// need one A = X X^T and one X <- Q X with Q = P_2 P_1 P_0; each step after the first replaces that pair of products,
+// 3 n^2 k multiply-adds, by three symmetric ones more (B = A P, B P, P Q), 3 n^3 / 2.  That pays for matrices longer than wide whose
+// products fill the GPU (Plan::group compares both by pick_cut()'s estimates): 2 x 1024 x 4096 513 -> 417 us.  It costs
+// accuracy: what the tensor core truncates in A is multiplied by a^2 a step (11.9) before it acts, and every P and Q has
+// one large product a row.  Five steps of normal matrices are off by 4e-6 to 8e-6 of their norm, 2e-6 to 3e-6 one at a time (2e-6 to
+// 4e-6 in fp32 arithmetic), so only steps from bf16 numbers, which carry 2e-3, are taken together.
 #include "gemm_op.cuh"
 
 #include <math.h>
@@ -33,6 +40,9 @@ constexpr int kSumBlocks = 592;        // at most: partial sums of squares of a 
 // Scales of A, C and P in fp16.  Singular values stay below 1.25, so no entry of A exceeds 1.6, none of C |b| + 1.6 |c| < 8.1,
 // and P, whose eigenvalues lie between 0 and a, has none above 3.5.
 constexpr float kScaleA = 8192.f, kScaleC = 4096.f, kScaleP = 8192.f;
+// B = A P has no eigenvalue above 1.45; Q, a product of two or three P, none above a^2 = 11.9 or a^3 = 40.9.
+constexpr float kScaleB = 8192.f, kScaleQ[2] = {4096.f, 1024.f};
+constexpr double kLaunchUs = 6.0;      // what a product costs beside its tiles: first operands, last epilogue
 
 struct MatArgs {
   const void* g;                       // gradients (or the matrices to orthogonalise)
@@ -298,8 +308,9 @@ struct Plan {
   int64_t ld, plane;           // X
   int64_t ldn, plane_n;        // A, C, P
   int64_t ldf, planef;         // parts of the Gram matrix
-  gop::Cut gram;
-  size_t o_partial, o_x[2], o_ac, o_p, o_gram, total;
+  gop::Cut gram, full, square;   // X X^T, P X and a symmetric product of n x n matrices
+  bool group;                    // steps may be taken together
+  size_t o_partial, o_x[2], o_ac, o_s, o_gram, total;
 };
 
 Plan make_plan(int m, int rows, int cols) {
@@ -316,8 +327,12 @@ Plan make_plan(int m, int rows, int cols) {
   p.o_partial = take((int64_t)m * kSumBlocks * 8);
   for (int i = 0; i < 2; ++i) p.o_x[i] = take((int64_t)m * 2 * p.plane * 2);
   p.o_ac = take((int64_t)m * 4 * p.plane_n * 2);
-  p.o_p = take((int64_t)m * 2 * p.plane_n * 2);
   p.gram = gop::pick_cut(p.n, p.n, m, true, p.k, 2, 32);
+  p.full = gop::pick_cut(rows, cols, m, false, p.n, 2, 1);
+  p.square = gop::pick_cut(p.n, p.n, m, true, p.n, 2, 1);
+  // (by a tenth: the estimates are no better)
+  p.group = p.gram.us + p.full.us + 2 * kLaunchUs > 1.1 * 3 * (p.square.us + kLaunchUs);
+  p.o_s = take((int64_t)m * 2 * p.plane_n * 2 * (p.group ? 3 : 1));
   p.ldf = round_up(p.n, 4);
   p.planef = p.ldf * p.n;
   p.o_gram = take(p.gram.splits > 1 ? (int64_t)m * p.gram.splits * p.planef * 4 : 0);
@@ -348,14 +363,14 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
   if (blocks > kSumBlocks) blocks = kSumBlocks;
   a.blocks = (int)blocks;
   __half* x[2] = {reinterpret_cast<__half*>(ws + p.o_x[0]), reinterpret_cast<__half*>(ws + p.o_x[1])};
+  const bool cut = p.gram.splits > 1, together = p.group && sizeof(G) == 2;
   void* ac = ws + p.o_ac;      // [m][A first, second piece, C first, second piece]
-  void* pp = ws + p.o_p;
   const dim3 grid((unsigned)blocks, (unsigned)a.m);
   LS_TRY(launch_dep(ns_momentum_kernel<G, MUON, VEC>, grid, dim3(32 * kWarps), 0, st, 1, a));
   LS_TRY(launch_dep(ns_start_kernel<G, MUON, VEC>, grid, dim3(32 * kWarps), 0, st, 1, a, x[0]));
-  // maps: X as operand and as output; A, C and P as operands and as outputs, straight and transposed
+  // maps: X as operand and as output; A and C, and the matrices P, Q, B as operands and as outputs, straight and transposed
   constexpr int kRow = gop::box_row(2);
-  CUtensorMap xk[2], xo[2], ack, aco, act, pk, po, pt, gf;
+  CUtensorMap xk[2], xo[2], ack, aco, act, sk[3], so[3], sq[3], gf;
   const int64_t m = a.m;
   for (int i = 0; i < 2; ++i) {
     LS_TRY(gop::make_operand_map(&xk[i], x[i], gop::MAP_F16, a.rows, a.cols, 2 * m, p.ld, p.plane));
@@ -364,58 +379,86 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
   LS_TRY(gop::make_operand_map(&ack, ac, gop::MAP_F16, p.n, p.n, 4 * m, p.ldn, p.plane_n));
   LS_TRY(gop::make_output_map(&aco, ac, gop::MAP_F16, p.n, p.n, 4 * m, p.ldn, p.plane_n, kRow));
   LS_TRY(gop::make_output_map(&act, ac, gop::MAP_F16, p.n, p.n, 4 * m, p.ldn, p.plane_n, kRow, true));
-  LS_TRY(gop::make_operand_map(&pk, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n));
-  LS_TRY(gop::make_output_map(&po, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, kRow));
-  LS_TRY(gop::make_output_map(&pt, pp, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, kRow, true));
-  const bool cut = p.gram.splits > 1;
+  for (int i = 0; i < (together ? 3 : 1); ++i) {
+    void* s = ws + p.o_s + (size_t)i * m * 2 * p.plane_n * 2;
+    LS_TRY(gop::make_operand_map(&sk[i], s, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n));
+    LS_TRY(gop::make_output_map(&so[i], s, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, kRow));
+    LS_TRY(gop::make_output_map(&sq[i], s, gop::MAP_F16, p.n, p.n, 2 * m, p.ldn, p.plane_n, kRow, true));
+  }
   if (cut)
     LS_TRY(gop::make_output_map(&gf, ws + p.o_gram, gop::MAP_F32, p.n, p.n, m * p.gram.splits, p.ldf, p.planef, kRow));
-  const int nt_n = gop::pick_nt(p.n, p.n, m, true), nt_x = gop::pick_nt(a.rows, a.cols, m, false);
-  int cur = 0;
-  for (int s = 0; s < steps; ++s, cur ^= 1) {
+  // symmetric products of commuting n x n matrices, all of which tend to multiples of I
+  auto square = [&](const CUtensorMap& l, int lstep, const CUtensorMap& r, int rstep, int r0, const CUtensorMap& out,
+                    const CUtensorMap& out_t, int ostep, Params g) {
+    g.batch = a.m; g.M = g.N = p.n; g.tri = g.mirror = 1;
+    g.a_zstep = lstep; g.b_zstep = rstep; g.b_z0 = r0; g.c_zstep = ostep;
+    g.dominant = 1;
+    g.chunk_kb = together ? 2 : 8;          // (together: 2e-5 at chunks of 8 for singular values over six decades, 9e-6 at 2)
+    return gop::launch<2, true, false, false, gop::EPI_PIECES>(p.square.nt, l, r, out, out_t, g, p.n, st);
+  };
+  // A, and C = b I + c A, of a product whose operands were scaled
+  auto a_and_c = [](float operands) {
     Params g{};
-    g.batch = a.m;
+    g.n_out = 2;
+    g.out_alpha[0] = kScaleA / operands;
+    g.out_alpha[1] = kNsC * kScaleC / operands;
+    g.out_diag[1] = kNsB * kScaleC;
+    return g;
+  };
+  auto one = [](float alpha, float diag) {
+    Params g{};
+    g.n_out = 1;
+    g.out_alpha[0] = alpha;
+    g.out_diag[0] = diag;
+    return g;
+  };
+  int cur = 0;
+  for (int left = steps; left > 0; cur ^= 1) {
+    const int group = !together || left == 1 ? 1 : left % 2 == 1 ? 3 : 2;
+    left -= group;
     // A = X X^T (wide) or X^T X (tall), and C = b I + c A
-    g.M = g.N = p.n; g.tri = 1;
+    Params g{};
+    if (!cut) g = a_and_c(a.scale_x * a.scale_x);
+    g.batch = a.m; g.M = g.N = p.n; g.tri = 1;
     g.a_zstep = g.b_zstep = 2;
-    const float unit = 1.f / (a.scale_x * a.scale_x);
     if (cut) {
       g.alpha = 1.f; g.splits = p.gram.splits; g.c_zstep = p.gram.splits;
       if (p.tall) LS_TRY((gop::launch<2, true, true, true, gop::EPI_F32>(p.gram.nt, xk[cur], xk[cur], gf, gf, g, p.k, st)));
       else LS_TRY((gop::launch<2, true, false, false, gop::EPI_F32>(p.gram.nt, xk[cur], xk[cur], gf, gf, g, p.k, st)));
+      const float unit = 1.f / (a.scale_x * a.scale_x);
       const FoldArgs f{reinterpret_cast<const float*>(ws + p.o_gram), static_cast<__half*>(ac), p.n, p.gram.splits, p.ldf, p.planef,
                        p.ldn, p.plane_n, kScaleA * unit, kNsC * kScaleC * unit, kNsB * kScaleC};
       const unsigned nb = (unsigned)((p.n + 63) / 64);
       LS_TRY(launch_dep(ns_gram_fold_kernel, dim3(nb * (nb + 1) / 2, (unsigned)a.m), dim3(256), 0, st, 1, f));
-      g.splits = 1;
     } else {
       g.mirror = 1; g.c_zstep = 4;
-      g.n_out = 2;
-      g.out_alpha[0] = kScaleA * unit;
-      g.out_alpha[1] = kNsC * kScaleC * unit;
-      g.out_diag[1] = kNsB * kScaleC;
       if (p.tall) LS_TRY((gop::launch<2, true, true, true, gop::EPI_PIECES>(p.gram.nt, xk[cur], xk[cur], aco, act, g, p.k, st)));
       else LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(p.gram.nt, xk[cur], xk[cur], aco, act, g, p.k, st)));
     }
-    // P = a I + A C
-    g.a_zstep = g.b_zstep = 4; g.b_z0 = 2; g.c_zstep = 2;
-    g.mirror = 1;
-    g.dominant = 1;             // A and C tend to multiples of I
-    g.chunk_kb = 8;
-    g.n_out = 1;
-    g.out_alpha[0] = kScaleP / (kScaleA * kScaleC);
-    g.out_diag[0] = kNsA * kScaleP;
-    LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(nt_n, ack, ack, po, pt, g, p.n, st)));
-    // X <- P X (wide) or X P (tall)
-    g.a_zstep = g.b_zstep = g.c_zstep = 2; g.b_z0 = 0;
-    g.tri = g.mirror = 0;
+    // P = a I + A C, and Q = the product of the group's P
+    const Params make_p = one(kScaleP / (kScaleA * kScaleC), kNsA * kScaleP);
+    LS_TRY(square(ack, 4, ack, 4, 2, so[0], sq[0], 2, make_p));
+    int ip = 0, iq = 0;
+    float scale_q = kScaleP;
+    for (int s = 1; s < group; ++s) {
+      const int ib = ip == iq ? 1 : 3 - ip - iq;        // neither P nor Q
+      LS_TRY(square(ack, 4, sk[ip], 2, 0, so[ib], sq[ib], 2, one(kScaleB / (kScaleA * kScaleP), 0.f)));
+      LS_TRY(square(sk[ib], 2, sk[ip], 2, 0, aco, act, 4, a_and_c(kScaleB * kScaleP)));
+      ip = ib;
+      LS_TRY(square(ack, 4, ack, 4, 2, so[ip], sq[ip], 2, make_p));
+      const int in = 3 - ip - iq;
+      LS_TRY(square(sk[ip], 2, sk[iq], 2, 0, so[in], sq[in], 2, one(kScaleQ[s - 1] / (kScaleP * scale_q), 0.f)));
+      iq = in;
+      scale_q = kScaleQ[s - 1];
+    }
+    // X <- Q X (wide) or X Q (tall)
+    g = one(1.f / scale_q, 0.f);
+    g.batch = a.m; g.M = a.rows; g.N = a.cols;
+    g.a_zstep = g.b_zstep = g.c_zstep = 2;
     g.dominant = p.tall ? 2 : 1;
     g.chunk_kb = 8;
-    g.M = a.rows; g.N = a.cols;
-    g.out_alpha[0] = 1.f / kScaleP;
-    g.out_diag[0] = 0.f;
-    if (p.tall) LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(nt_x, xk[cur], pk, xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
-    else LS_TRY((gop::launch<2, true, false, true, gop::EPI_PIECES>(nt_x, pk, xk[cur], xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
+    if (p.tall) LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(p.full.nt, xk[cur], sk[iq], xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
+    else LS_TRY((gop::launch<2, true, false, true, gop::EPI_PIECES>(p.full.nt, sk[iq], xk[cur], xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
   }
   const float step = a.lr * sqrtf(fmaxf(1.f, (float)a.rows / (float)a.cols));
   LS_TRY(launch_dep(ns_finish_kernel<G, MUON, VEC>, grid, dim3(32 * kWarps), 0, st, 1, a, static_cast<const __half*>(x[cur]), step));

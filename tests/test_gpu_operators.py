@@ -531,6 +531,72 @@ def test_orthogonalize_step_by_step(rows, cols):
         assert float(sv.max()) < 1.25
 
 
+def _ns_group64(x, steps, start=None):
+    """`steps` Newton-Schulz steps of x [n][k] in 64 bits, and an elementwise bound of the error of a kernel that forms
+    their product Q from A = X X^T alone, A' = A P P, with the errors of _ns_step64.  start: the error of x."""
+    import torch
+    n, k = x.shape
+    K = lambda length: MMA * (28 + length / 128)      # noqa: E731
+    both = lambda t: torch.maximum(t, t.T)            # noqa: E731  (an element is computed on one side of the diagonal)
+
+    def prod(l, tl, r, tr, scale):
+        out = l @ r
+        return out, both(tl @ r.abs() + l.abs() @ tr + K(n) * (l.abs() @ r.abs())) + MMA * out.abs() + 2.0 ** -25 / scale
+
+    eye = torch.eye(n, device=x.device, dtype=torch.float64)
+    a = x @ x.T
+    ta = K(k) * (x.abs() @ x.abs().T) + MMA * a.abs() + 2.0 ** -25 / 8192
+    if start is not None:
+        ta = ta + start @ x.abs().T + x.abs() @ start.T
+    q = tq = None
+    for s in range(steps):
+        c = B * eye + CC * a
+        tc = CC * ta + MMA * c.abs() + 2.0 ** -25 / 4096
+        p, tp = prod(a, ta, c, tc, 8192)
+        p = p + A * eye
+        tp = tp + MMA * A * eye
+        if q is None:
+            q, tq = p, tp
+        else:
+            q, tq = prod(p, tp, q, tq, 4096 if s == 1 else 1024)
+        if s + 1 < steps:
+            bb, tb = prod(a, ta, p, tp, 8192)
+            a, ta = prod(bb, tb, p, tp, 8192)
+    out = q @ x
+    scale = min(16384.0, 2.0 ** math.floor(0.5 * math.log2(n * k)))
+    tol = tq @ x.abs() + K(n) * (q.abs() @ x.abs()) + MMA * out.abs() + 2.0 ** -25 / scale
+    if start is not None:
+        tol = tol + q.abs() @ start
+    return out, tol
+
+
+@pytest.mark.parametrize("m,rows,cols", [(30, 257, 1000), (40, 900, 257), (2, 1000, 2501)])
+def test_steps_from_bf16_taken_together(m, rows, cols):
+    """Sizes at which steps from bf16 gradients are taken in groups (three first when their number is odd, else two): each group
+    against 64 bits from the kernel's own result before it, elementwise.  W = 0, lr = 1 and no momentum give -O in fp32."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    u = (_randn(_gen(rows + cols), m, rows, cols) * 1e-3).to(torch.bfloat16)
+    flip = (lambda t: t.T) if rows > cols else (lambda t: t)
+    z = m - 1
+    u64 = flip(u[z].double())
+    factor = math.sqrt(max(1.0, rows / cols))
+    got = {0: u64 / (torch.linalg.norm(u64) + 1e-7)}
+    for before, steps in ((0, 1), (0, 2), (0, 3), (2, 4), (3, 5), (5, 7)):
+        w, v = torch.zeros(m, rows, cols, device="cuda"), torch.zeros(m, rows, cols, device="cuda")
+        b.muon_step(w, v, u, 1.0, momentum=0.0, nesterov=False, steps=steps)
+        x = got[before]
+        want, tol = _ns_group64(x, steps - before, 2 * MMA * x.abs() if before == 0 else None)
+        # (the factor and its product with O are rounded, and the earlier result carries the same: three roundings more)
+        got[steps] = flip(-w[z].double()) / factor
+        _within(got[steps], want, tol * 1.05 + 8 * U * want.abs() + 1e-30, f"{before} to {steps} steps")
+    # in bf16 the same result, rounded
+    out = b.orthogonalize(u, steps=5)
+    assert torch.equal(out, b.orthogonalize(u, steps=5))
+    _within(flip(out[z].double()), got[5], 2.0 ** -8 * got[5].abs() + 1e-30, "bf16")
+    b.device_status()
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("m,rows,cols", [(3, 96, 160), (2, 513, 300), (1, 64, 1000)])
 def test_orthogonalize_replicas_and_types(m, rows, cols, dtype):
