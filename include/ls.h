@@ -461,7 +461,7 @@ int ls_vocab_loss_grad(const void* h_dev, const void* W_dev, const int32_t* labe
  *   X = u / (|u|_F + 1e-7);  repeat: A = X X^T, X = 3.4445 X + (-4.7750 A + 2.0315 A A) X;  out = X
  * (for rows > cols the same of the transpose, transposed back).  Products are accurate to about 22 bits; from bf16 numbers
  * two or three steps of a large matrix longer than wide may be taken together (A of the first, A' = A P P after that),
- * which is off by up to about 1e-5 of the result's norm before it is rounded.  |u|_F is added up in double; a matrix whose
+ * which is off by some 1e-6 of the result's norm, 2e-5 where singular values span decades.  |u|_F is added up in double; a matrix whose
  * norm is not large against 1e-7 comes out smaller, as the formula has it.  out has u's dtype and shape.
  * rows, cols <= 32768.  The workspace also serves ls_muon_step. */
 int ls_orthogonalize_ws_bytes(int m, int rows, int cols, size_t* bytes);
