@@ -17,7 +17,8 @@
 // of 1 / count, where -1 is exact.
 //
 // fp32 tensors: operands as three bf16 pieces (24 bits) and six products (gemm_op.cuh), logits kept in fp32 for a piece of rows, dz
-// in three pieces; sums over several pieces of rows are added into dW by the bulk-copy engine in fp32.
+// in three pieces; sums over several pieces of rows are added into dW by the bulk-copy engine in fp32.  A few rows take the
+// CUDA cores instead (vocab_few_*).
 //
 // The row sums, the loss and every accumulation are fp32 or wider and in a fixed order: results are
 // reproducible bit for bit (the atomic counter only picks the CTA that finishes).
@@ -47,6 +48,7 @@ struct CombineArgs {
   const int32_t* labels;          // of the piece
   const float* label_logit;
   float *lse, *row_loss;
+  float2* norm;                   // fp32 gradient: (reference of the exponentials, their sum) of the piece's rows, or null
   unsigned* done;
   // of the whole replica
   const int32_t* all_labels;
@@ -66,6 +68,8 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
   a.labels += z * a.all_rows; a.label_logit += z * a.all_rows; a.lse += z * a.all_rows; a.row_loss += z * a.all_rows;
   a.all_labels += z * a.all_rows; a.all_row_loss += z * a.all_rows;
   a.done += z;
+  if (a.norm != nullptr) a.norm += z * a.all_rows;
+  if (a.inv_count != nullptr) a.inv_count += z;
   if (a.loss != nullptr) a.loss += z;
   grid_dep_wait();
   grid_dep_launch();
@@ -105,6 +109,7 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
     }
     const float l = (M == -INFINITY ? 0.f : M * kLn2) + logf(S);
     a.lse[row] = l;
+    if (a.norm != nullptr) a.norm[row] = make_float2(M == -INFINITY ? 0.f : M, S);
     a.row_loss[row] = has_label(a.labels[row], a.V) ? l - a.label_logit[row] : 0.f;
   }
   if (a.inv_count == nullptr && a.loss == nullptr) return;
@@ -224,10 +229,19 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
   p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
 }
 
+// dz of an fp32 logit: exp(z - lse) as 2^(z log2(e) - M) / S with the reference M that the sum S was formed with.  lse itself, rounded
+// at its size, would put an error of 1e-6 at a log-sum-exp of 20 into every number of the row.
+struct Norm {
+  float ref, inv, log_sum;
+  __device__ __forceinline__ explicit Norm(float2 n) : ref(n.x), inv(1.f / n.y), log_sum(logf(n.y)) {}
+  __device__ __forceinline__ float p(float z) const { return exp2f(fmaf(z, kLog2e, -ref)) * inv; }
+  __device__ __forceinline__ float p_minus_1(float z) const { return expm1f(fmaf(fmaf(z, kLog2e, -ref), kLn2, -log_sum)); }
+};
+
 // fp32: logits z -> three pieces of dz.
 __global__ void __launch_bounds__(256)
 vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t piece, int V, const int32_t* labels,
-                     const float* label_logit, const float* lse, const HRows h) {
+                     const float* label_logit, const float2* norm, const HRows h) {
   const int row = blockIdx.y;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   grid_dep_wait();
@@ -238,12 +252,12 @@ vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t pie
   const int64_t at = (int64_t)row * ld + c;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   if (has_label(y, V)) {
-    const float l = lse[row];
+    const Norm n(norm[row]);
     const float4 u = *reinterpret_cast<const float4*>(z + at);
-    v[0] = expf(u.x - l); v[1] = expf(u.y - l); v[2] = expf(u.z - l); v[3] = expf(u.w - l);
+    v[0] = n.p(u.x); v[1] = n.p(u.y); v[2] = n.p(u.z); v[3] = n.p(u.w);
     const int d = y - c;
     if (d >= 0 && d < 4) {
-      const float py = expm1f(label_logit[row] - l);
+      const float py = n.p_minus_1(label_logit[row]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) if (i == d) v[i] = py;
     }
@@ -299,10 +313,12 @@ vocab_pack_kernel(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t
 // ---- sum of fp32 planes in index order, rounded to the output type --------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256)
-vocab_fold_kernel(const float* part, int planes, int64_t plane, int64_t ld, int64_t rows, int d, T* out) {
+vocab_fold_kernel(const float* part, int planes, int64_t plane, int64_t ld, int64_t rows, int d, T* out, int64_t out_stride) {
   const int per_row = (d + 3) / 4;
   grid_dep_wait();
   grid_dep_launch();
+  part += blockIdx.y * planes * plane;         // replica
+  out += blockIdx.y * out_stride;
   const int64_t total = rows * per_row;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / per_row;
@@ -319,13 +335,336 @@ vocab_fold_kernel(const float* part, int planes, int64_t plane, int64_t ld, int6
   }
 }
 
+// ---- fp32, few rows: CUDA cores ----------------------------------------------------------------------------------------
+// With a handful of rows W is all there is to read, and six tensor-core products of rows padded to 256 take longer than the
+// FMAs; laying W out as pieces alone moves 2.5 times its bytes.  Here W is read once for the logits and once more for the
+// gradient, whose pass also writes dW (kFewRows says up to where).  The logits' kernel is bound by the latency of its steps, at 3 to 4
+// TB/s of W for 8 rows; the gradient's by HBM, 5 TB/s for 8 rows.
+
+// An infinity counts as the largest bf16 number, as it does in split3(); NaN stays.
+__device__ __forceinline__ float finite(float x) {
+  const float kMax = 3.3895313892515355e38f;
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(-kMax));
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(y), "f"(kMax));
+  return y;
+}
+__device__ __forceinline__ float4 finite(float4 v) { return make_float4(finite(v.x), finite(v.y), finite(v.z), finite(v.w)); }
+
+struct FewArgs {
+  const float *h, *W;
+  int64_t h_stride, w_stride;
+  int rows, V, d;
+  float* z;                       // [replica][rows][ldz] logits, or null
+  int64_t ldz;
+  float *stat_max, *stat_sum;
+  int64_t stat_ld, stat_z;
+  const int32_t* labels;
+  float* label_logit;
+  unsigned* done;                 // cleared for the combining launch
+};
+// Logits of RT rows and 128 columns per CTA: 32-wide steps of d through a ring of cp.async, a thread has four columns and RT / 4
+// rows.  A warp's eight columns and four rows at a time are one shared-memory wavefront each (rows 144 bytes apart).  The
+// products of a step are added up by themselves first.
+constexpr int kFewCols = 128, kFewStep = 32, kFewPitch = 36, kFewStages = 3;
+template <int RT>
+constexpr int kFewSmem = kFewStages * (kFewCols + RT) * kFewPitch * 4;
+
+template <bool VEC>
+__device__ __forceinline__ void few_copy(float* dst, const float* src, int64_t row, int rows, int d, int k, int piece) {
+  // piece: four floats of the step; floats past the row's end, and rows past the last, become zeros
+  const bool in = row < rows;
+  const float* from = src + (in ? row : 0) * d;
+  if constexpr (VEC) {
+    const int c = k + piece * 4;
+    const int left = in && c < d ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst + piece * 4)),
+                 "l"(from + (left ? c : 0)), "r"(left) : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = k + piece * 4 + i;
+      const int left = in && c < d ? 4 : 0;
+      asm volatile("cp.async.ca.shared.global.L2::256B [%0], [%1], 4, %2;" ::"r"(ptx::smem_u32(dst + piece * 4 + i)),
+                   "l"(from + (left ? c : 0)), "r"(left) : "memory");
+    }
+  }
+}
+
+template <int RT, bool VEC>
+__global__ void __launch_bounds__(128) vocab_few_logits_kernel(const FewArgs a) {
+  constexpr int RPT = RT / 4;
+  extern __shared__ __align__(16) float few[];
+  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
+  const int tiles = (a.rows + RT - 1) / RT;                     // of rows: neighbouring CTAs read the same columns' rows of W
+  const int slice = blockIdx.x / tiles;
+  const int row0 = (int)(blockIdx.x - slice * tiles) * RT;
+  const int64_t v0 = (int64_t)slice * kFewCols, z = blockIdx.z;
+  grid_dep_wait();
+  grid_dep_launch();
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.done[z] = 0u;
+  const float* W = a.W + z * a.w_stride;
+  const float* h = a.h + z * a.h_stride;
+  const int steps = (a.d + kFewStep - 1) / kFewStep;
+  auto load = [&](int s) {
+    if (s < steps) {
+      float* w = few + (s % kFewStages) * (kFewCols + RT) * kFewPitch;
+      float* hs = w + kFewCols * kFewPitch;
+#pragma unroll
+      for (int i = 0; i < kFewCols / 16; ++i) {
+        const int r = i * 16 + (threadIdx.x >> 3);
+        few_copy<VEC>(w + r * kFewPitch, W, v0 + r, a.V, a.d, s * kFewStep, threadIdx.x & 7);
+      }
+#pragma unroll
+      for (int i = 0; i < (RT + 15) / 16; ++i) {
+        const int r = i * 16 + (threadIdx.x >> 3);
+        if (r < RT) few_copy<VEC>(hs + r * kFewPitch, h, row0 + r, a.rows, a.d, s * kFewStep, threadIdx.x & 7);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  const int vl = wp * 32 + (lane & 7), rl = lane >> 3;          // columns vl + 8 i, rows rl + 4 j
+  float acc[4][RPT];
+  auto pass = [&](auto clamp) {
+    for (int s = 0; s < kFewStages - 1; ++s) load(s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < RPT; ++j) acc[i][j] = 0.f;
+    for (int s = 0; s < steps; ++s) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 2) : "memory");
+      __syncthreads();                                          // step s is there, and step s - 1 has been read
+      load(s + kFewStages - 1);
+      const float* w = few + (s % kFewStages) * (kFewCols + RT) * kFewPitch;
+      const float* hs = w + kFewCols * kFewPitch;
+      float part[4][RPT];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < RPT; ++j) part[i][j] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kFewStep; k += 4) {
+        float4 wv[4], hv[RPT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wv[i] = clamp(*reinterpret_cast<const float4*>(w + (vl + 8 * i) * kFewPitch + k));
+#pragma unroll
+        for (int j = 0; j < RPT; ++j) hv[j] = clamp(*reinterpret_cast<const float4*>(hs + (rl + 4 * j) * kFewPitch + k));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < RPT; ++j) {
+            float t = part[i][j];
+            t = fmaf(wv[i].x, hv[j].x, t);
+            t = fmaf(wv[i].y, hv[j].y, t);
+            t = fmaf(wv[i].z, hv[j].z, t);
+            part[i][j] = fmaf(wv[i].w, hv[j].w, t);
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < RPT; ++j) acc[i][j] += part[i][j];
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+  };
+  pass([](float4 v) { return v; });
+  // an infinite operand leaves an infinity or a NaN in every sum it enters: only then once more, with operands made finite
+  float odd = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < RPT; ++j) odd = isfinite(acc[i][j]) ? odd : 1.f;
+  if (__syncthreads_or(odd != 0.f)) pass([](float4 v) { return finite(v); });
+  // the tile through shared memory: a warp takes a row's 128 logits, one slice of the statistics
+  constexpr int kPitch = kFewCols + 4;
+  static_assert(RT * kPitch * 4 <= kFewSmem<RT>, "tile of logits");
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < RPT; ++j) few[(rl + 4 * j) * kPitch + vl + 8 * i] = acc[i][j];
+  __syncthreads();
+  for (int r = wp; r < RT; r += 4) {
+    const int row = row0 + r;
+    if (row >= a.rows) break;
+    const int64_t c = v0 + lane * 4;
+    const float4 t = *reinterpret_cast<const float4*>(few + r * kPitch + lane * 4);
+    float v[4] = {t.x, t.y, t.z, t.w};
+    const int64_t lab = a.labels[z * a.rows + row] - c;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (c + i >= a.V) v[i] = -INFINITY;
+      else if (lab == i) a.label_logit[z * a.rows + row] = v[i];
+      mx = fmaxf(mx, v[i]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    // (the reference stays finite for a finite maximum, and where there is nothing but -inf: EPI_STATS)
+    const float ref = mx == -INFINITY ? 0.f : mx < 0.f ? fmaxf(mx * kLog2e, -3.4e38f) : mx * kLog2e;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += gop::ex2(fmaf(v[i], kLog2e, -ref));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) {
+      const int64_t at = z * a.stat_z + (int64_t)slice * a.stat_ld + row;
+      a.stat_max[at] = mx == -INFINITY ? -INFINITY : ref;
+      a.stat_sum[at] = sum;
+    }
+    if (a.z != nullptr && c < a.V)
+      *reinterpret_cast<float4*>(a.z + (z * a.rows + row) * a.ldz + c) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+// z -> dz in place, four columns a thread
+__global__ void __launch_bounds__(256)
+vocab_few_dz_kernel(float* zz, int64_t ld, int rows, int V, const int32_t* labels, const float* label_logit, const float2* norm) {
+  const int64_t at_row = (int64_t)blockIdx.z * rows + blockIdx.y;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  grid_dep_wait();
+  grid_dep_launch();
+  if (c >= V) return;
+  const int y = labels[at_row];
+  float4* at = reinterpret_cast<float4*>(zz + at_row * ld + c);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (has_label(y, V)) {
+    const Norm n(norm[at_row]);
+    const float4 u = *at;
+    o = make_float4(n.p(u.x), n.p(u.y), n.p(u.z), n.p(u.w));
+    const int d = y - c;
+    if (d >= 0 && d < 4) {
+      const float py = n.p_minus_1(label_logit[at_row]);
+      if (d == 0) o.x = py;
+      else if (d == 1) o.y = py;
+      else if (d == 2) o.z = py;
+      else o.w = py;
+    }
+  }
+  *at = o;
+}
+
+// dW = dz^T h and, per block of `block` columns of dz, its part of dh = dz W.  A CTA has 128 elements of d, a warp every fourth row
+// of W of the block: a lane reads its four elements, adds them times dz to RT rows of dh in registers, and writes the four of
+// dW from RT rows of h in registers.  The warps' sums of dh are added in order.
+struct FewGradArgs {
+  const float *h, *W, *dz;
+  int64_t h_stride, w_stride, dw_stride, ldz;
+  int rows, V, d, block;
+  const int32_t* labels;
+  const float* inv;
+  float scale;
+  float *dW, *part;               // part: [replica][block][rows][ldp]
+  int64_t ldp;
+};
+template <int RT, bool VEC>
+__global__ void __launch_bounds__(128) vocab_few_grad_kernel(const FewGradArgs a) {
+  constexpr int kChunk = 128, kRows = 4;      // columns of dz in shared memory at a time; rows of W that a warp reads at a time
+  __shared__ __align__(16) float dz[kChunk][RT];
+  __shared__ float sum[4][RT][128];
+  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
+  const int64_t z = blockIdx.z;
+  const int k0 = blockIdx.x * 128;
+  grid_dep_wait();
+  grid_dep_launch();
+  const float* W = a.W + z * a.w_stride;
+  float* dW = a.dW + z * a.dw_stride;
+  const float* zz = a.dz + z * a.rows * a.ldz;
+  const float alpha = a.scale * a.inv[z];
+  auto col = [&](int i) { return VEC ? k0 + lane * 4 + i : k0 + i * 32 + lane; };
+  float h[RT][4], acc[RT][4];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const bool in = r < a.rows && has_label(a.labels[z * a.rows + (r < a.rows ? r : 0)], a.V);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[r][i] = in && col(i) < a.d ? finite(a.h[z * a.h_stride + (int64_t)r * a.d + col(i)]) : 0.f;
+      acc[r][i] = 0.f;
+    }
+  }
+  const int from = blockIdx.y * a.block, to = min(from + a.block, a.V);
+  float w[kRows][4];
+  auto read = [&](int v0) {                   // rows v0, v0 + 4, ...
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      const int64_t at = (int64_t)(v0 + q * 4) * a.d;
+      const bool in = v0 + q * 4 < to;
+      if constexpr (VEC) {
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (in && col(0) < a.d) t = __ldg(reinterpret_cast<const float4*>(W + at + col(0)));
+        w[q][0] = t.x; w[q][1] = t.y; w[q][2] = t.z; w[q][3] = t.w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[q][i] = in && col(i) < a.d ? __ldg(W + at + col(i)) : 0.f;
+      }
+    }
+  };
+  read(from + wp);
+  for (int c0 = from; c0 < to; c0 += kChunk) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kChunk * RT; i += 128) {
+      const int r = i / kChunk, c = i - r * kChunk;
+      dz[c][r] = r < a.rows && c0 + c < to ? zz[r * a.ldz + c0 + c] : 0.f;
+    }
+    __syncthreads();
+    for (int c = wp; c < kChunk && c0 + c < to; c += 4 * kRows) {
+      float x[kRows][4];
+#pragma unroll
+      for (int q = 0; q < kRows; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[q][i] = finite(w[q][i]);
+      read(c0 + c + 4 * kRows);               // the next ones, also across chunks
+#pragma unroll
+      for (int q = 0; q < kRows; ++q) {
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const float g = dz[c + q * 4][r];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            acc[r][i] = fmaf(g, x[q][i], acc[r][i]);
+            o[i] = fmaf(g, h[r][i], o[i]);
+          }
+        }
+        const int v = c0 + c + q * 4;
+        if (v < to) {
+          const int64_t at = (int64_t)v * a.d;
+          if constexpr (VEC) {
+            if (col(0) < a.d)
+              *reinterpret_cast<float4*>(dW + at + col(0)) = make_float4(alpha * o[0], alpha * o[1], alpha * o[2], alpha * o[3]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (col(i) < a.d) dW[at + col(i)] = alpha * o[i];
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[wp][r][VEC ? lane * 4 + i : i * 32 + lane] = acc[r][i];
+  __syncthreads();
+  float* part = a.part + (z * gridDim.y + blockIdx.y) * a.rows * a.ldp;
+  const int k = k0 + threadIdx.x;
+  if (k < a.d)
+    for (int r = 0; r < a.rows; ++r) {
+      const int t = threadIdx.x;
+      part[r * a.ldp + k] = alpha * (((sum[0][r][t] + sum[1][r][t]) + sum[2][r][t]) + sum[3][r][t]);
+    }
+}
+
 // ---- plan: what a call keeps in its workspace ---------------------------------------------------------------------------------
 constexpr int64_t kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
+// fp32: at most so many rows go to the CUDA cores.  (118995 x 1608, loss: 8 rows 229 us, 32 rows 435, 64 rows 810, on the tensor
+// cores 790 for any of them; gradient: 8 rows 530 us, 16 rows 826, tensor cores 1270.  32000 x 2048: 138 us for a loss of 32 rows, 257.)
+constexpr int64_t kFewRows = 32, kFewRowsGrad = 16;
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 struct Plan {
   bool f32, grad;
+  bool few;             // the CUDA-core path of few fp32 rows, all replicas at once
   int np;
   int batch;            // replicas taken together: all of them where that leaves one product and one combining launch
   int64_t R;            // rows of a piece
@@ -336,8 +675,9 @@ struct Plan {
   int slices;
   int64_t stat_ld;
   int splits;           // of the contraction over V in dh
+  int block;            // few rows: columns of a part
   bool dh_fold, dw_fold;   // dh, dW pass through an fp32 sum in the workspace (several parts, or rows of no whole 16 bytes)
-  size_t o_stat, o_logit, o_lse, o_rowloss, o_inv, o_done, o_e, o_dz, o_h, o_w, o_dh, o_dw, total;
+  size_t o_stat, o_logit, o_lse, o_rowloss, o_norm, o_inv, o_done, o_e, o_dz, o_h, o_w, o_dh, o_dw, total;
 };
 
 int check_sizes(int m, int64_t rows, int64_t vocab, int d, int dtype) {
@@ -345,6 +685,31 @@ int check_sizes(int m, int64_t rows, int64_t vocab, int d, int dtype) {
   if (dtype != LS_DTYPE_FP32 && dtype != LS_DTYPE_BF16) return LS_ERR_INVALID_ARG;
   if (m > 65535 || rows > 2147483647ll || vocab > kMaxVocab || d > kMaxWidth) return LS_ERR_TOO_LARGE;
   return LS_OK;
+}
+
+// The parts of dh: about four CTAs an SM, in blocks of whole 64 columns.
+Plan few_plan(Plan p, int m, int64_t rows, int64_t V, int d) {
+  p.batch = m;
+  p.slices = (int)((V + kFewCols - 1) / kFewCols);
+  p.stat_ld = round_up(rows, 32);
+  const int64_t kb = (d + 127) / 128, want = (148 * 4 + kb * m - 1) / (kb * m);
+  p.block = (int)round_up((V + want - 1) / want, 64);
+  p.splits = (int)((V + p.block - 1) / p.block);
+  size_t at = 0;
+  auto take = [&at](int64_t bytes) { size_t o = at; at += (size_t)round_up(bytes, 256); return o; };
+  p.o_stat = take(2 * (int64_t)m * p.slices * p.stat_ld * 4);
+  p.o_logit = take(m * rows * 4);
+  p.o_lse = take(m * rows * 4);
+  p.o_rowloss = take(m * rows * 4);
+  p.o_norm = take(m * rows * 8);
+  p.o_inv = take(m * 4);
+  p.o_done = take(m * 4);
+  if (p.grad) {
+    p.o_e = take(m * rows * p.Vp * 4);
+    p.o_dh = take(m * p.splits * rows * p.df * 4);
+  }
+  p.total = at;
+  return p;
 }
 
 Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
@@ -363,6 +728,8 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.R = rows > 0 ? round_up((rows + p.pieces - 1) / p.pieces, 256) : 0;
   p.pieces = rows > 0 ? (rows + p.R - 1) / p.R : 0;
   p.stat_ld = p.R;
+  p.few = p.f32 && rows > 0 && rows <= (grad ? kFewRowsGrad : kFewRows);
+  if (p.few) return few_plan(p, m, rows, V, d);
   const bool lay = p.f32 || d % 8 != 0;
   p.batch = !grad && !lay && p.pieces == 1 && p.R * (p.Vp / 64 + 2) * 8 * m <= (int64_t)1 << 28 ? m : 1;
   // tile widths of the three products (a slice of the statistics is half a tile)
@@ -382,6 +749,7 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.o_logit = take(m * rows * 4);
   p.o_lse = take(m * rows * 4);
   p.o_rowloss = take(m * rows * 4);
+  p.o_norm = take(p.f32 && grad ? p.R * 8 : 0);
   p.o_inv = take(m * 4);
   p.o_done = take(4 * (int64_t)p.batch);
   // operands laid out anew: fp32 ones (as pieces), bf16 ones whose rows are no whole 16 bytes, and, for dW, h with the
@@ -446,6 +814,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   float* lse = (a.lse ? a.lse : reinterpret_cast<float*>(a.ws + p.o_lse)) + rep * a.rows;
   float* row_loss = (a.row_loss ? a.row_loss : reinterpret_cast<float*>(a.ws + p.o_rowloss)) + rep * a.rows;
   float* inv = reinterpret_cast<float*>(a.ws + p.o_inv) + rep;
+  float2* norm = reinterpret_cast<float2*>(a.ws + p.o_norm);
   unsigned* done = reinterpret_cast<unsigned*>(a.ws + p.o_done);
   bf* hpack = reinterpret_cast<bf*>(a.ws + p.o_h);
   bf* wpack = reinterpret_cast<bf*>(a.ws + p.o_w);
@@ -483,6 +852,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices; cb.rows = (int)rn; cb.V = (int)V;
     cb.labels = labels + r0; cb.label_logit = logit + r0; cb.lse = lse + r0; cb.row_loss = row_loss + r0;
     cb.done = done; cb.all_labels = labels; cb.all_row_loss = row_loss; cb.all_rows = a.rows;
+    cb.norm = F32 && p.grad ? norm : nullptr;
     if (p.grad && piece == 0) cb.inv_count = inv;
     if (r0 + p.R >= a.rows) cb.loss = a.loss + rep;
     LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((rn + 31) / 32), (unsigned)p.batch), dim3(1024), 0, st, 1, cb));
@@ -500,7 +870,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
       if (F32) {
         LS_TRY(launch_dep(vocab_dz_fp32_kernel, dim3((unsigned)((V + 1023) / 1024), qn), dim3(256), 0, st, 1,
                           reinterpret_cast<const float*>(a.ws + p.o_e) + q0 * p.Vp, dz + q0 * p.Vp, p.Vp, p.R * p.Vp, (int)V,
-                          ly, logit + r0 + q0, lse + r0 + q0, hr_q));
+                          ly, logit + r0 + q0, norm + q0, hr_q));
       } else {
         LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + kDzCols - 1) / kDzCols), (qn + kDzRows - 1) / kDzRows),
                           dim3(256), 0, st, 1, reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)qn, (int)V,
@@ -519,7 +889,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
       LS_TRY(gop::make_output_map(&mo, part, gop::MAP_F32, rn, d, p.splits, p.df, p.R * p.df, kRow));
       LS_TRY((gop::launch<NP, false, false, true, gop::EPI_F32>(p.nt_dh, mz, mw, mo, mo, gh, V, st)));
       LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(rn * ((d + 3) / 4))), dim3(256), 0, st, 1,
-                        static_cast<const float*>(part), p.splits, p.R * p.df, p.df, rn, d, dh));
+                        static_cast<const float*>(part), p.splits, p.R * p.df, p.df, rn, d, dh, (int64_t)0));
     } else {
       LS_TRY(gop::make_output_map(&mo, dh, F32 ? gop::MAP_F32 : gop::MAP_BF16, rn, d, 1, d, rn * d, kRow));
       LS_TRY((gop::launch<NP, false, false, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dh, mz, mw, mo, mo, gh, V, st)));
@@ -536,12 +906,63 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
       LS_TRY((gop::launch<NP, false, true, true, gop::EPI_F32>(p.nt_dw, mz, mhz, mo, mo, gw, rn, st)));
       if (r0 + p.R >= a.rows)
         LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(V * ((d + 3) / 4))), dim3(256), 0, st, 1,
-                          static_cast<const float*>(sum), 1, (int64_t)0, p.df, V, d, dW));
+                          static_cast<const float*>(sum), 1, (int64_t)0, p.df, V, d, dW, (int64_t)0));
     } else {
       LS_TRY(gop::make_output_map(&mo, dW, F32 ? gop::MAP_F32 : gop::MAP_BF16, V, d, 1, d, V * d, kRow));
       LS_TRY((gop::launch<NP, false, true, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dw, mz, mhz, mo, mo, gw, rn, st)));
     }
   }
+  return LS_OK;
+}
+
+template <int RT, bool VEC>
+cudaError_t launch_few_logits(const FewArgs& f, unsigned m, cudaStream_t st) {
+  static uint64_t configured = 0;        // one bit per device
+  auto kern = vocab_few_logits_kernel<RT, VEC>;
+  const cudaError_t e = allow_dynamic_smem(kern, kFewSmem<RT>, &configured);
+  if (e != cudaSuccess) return e;
+  const dim3 grid((unsigned)((f.rows + RT - 1) / RT) * (unsigned)((f.V + kFewCols - 1) / kFewCols), 1, m);
+  return launch_dep(kern, grid, dim3(128), kFewSmem<RT>, st, 1, f);
+}
+template <bool VEC>
+int run_few(const VocabArgs& a, const Plan& p, cudaStream_t st) {
+  const unsigned m = (unsigned)a.m;
+  FewArgs f{};
+  f.h = static_cast<const float*>(a.h); f.W = static_cast<const float*>(a.W);
+  f.h_stride = a.h_stride; f.w_stride = a.w_stride; f.rows = (int)a.rows; f.V = (int)a.V; f.d = a.d;
+  f.z = p.grad ? reinterpret_cast<float*>(a.ws + p.o_e) : nullptr;
+  f.ldz = p.Vp;
+  f.stat_max = reinterpret_cast<float*>(a.ws + p.o_stat);
+  f.stat_ld = p.stat_ld; f.stat_z = p.slices * p.stat_ld;
+  f.stat_sum = f.stat_max + m * f.stat_z;
+  f.labels = a.labels;
+  f.label_logit = reinterpret_cast<float*>(a.ws + p.o_logit);
+  f.done = reinterpret_cast<unsigned*>(a.ws + p.o_done);
+  if (a.rows <= 8) LS_TRY((launch_few_logits<8, VEC>(f, m, st)));
+  else if (a.rows <= 16) LS_TRY((launch_few_logits<16, VEC>(f, m, st)));
+  else LS_TRY((launch_few_logits<32, VEC>(f, m, st)));
+  CombineArgs cb{};
+  cb.stat_max = f.stat_max; cb.stat_sum = f.stat_sum; cb.stat_ld = f.stat_ld; cb.stat_z = f.stat_z; cb.slices = p.slices;
+  cb.rows = f.rows; cb.V = f.V; cb.labels = cb.all_labels = a.labels; cb.label_logit = f.label_logit;
+  cb.lse = a.lse ? a.lse : reinterpret_cast<float*>(a.ws + p.o_lse);
+  cb.row_loss = a.row_loss ? a.row_loss : reinterpret_cast<float*>(a.ws + p.o_rowloss);
+  cb.all_row_loss = cb.row_loss; cb.all_rows = a.rows; cb.done = f.done; cb.loss = a.loss;
+  float2* norm = reinterpret_cast<float2*>(a.ws + p.o_norm);
+  float* inv = reinterpret_cast<float*>(a.ws + p.o_inv);
+  if (p.grad) { cb.norm = norm; cb.inv_count = inv; }
+  LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((a.rows + 31) / 32), m), dim3(1024), 0, st, 1, cb));
+  if (!p.grad) return LS_OK;
+  LS_TRY(launch_dep(vocab_few_dz_kernel, dim3((unsigned)((a.V + 1023) / 1024), (unsigned)a.rows, m), dim3(256), 0, st, 1, f.z, f.ldz,
+                    f.rows, f.V, a.labels, static_cast<const float*>(f.label_logit), static_cast<const float2*>(norm)));
+  FewGradArgs g{};
+  g.h = f.h; g.W = f.W; g.dz = f.z; g.h_stride = a.h_stride; g.w_stride = a.w_stride; g.dw_stride = a.dw_stride; g.ldz = f.ldz;
+  g.rows = f.rows; g.V = f.V; g.d = a.d; g.block = p.block; g.labels = a.labels; g.inv = inv; g.scale = a.scale;
+  g.dW = static_cast<float*>(a.dW); g.part = reinterpret_cast<float*>(a.ws + p.o_dh); g.ldp = p.df;
+  const dim3 grid((unsigned)((a.d + 127) / 128), (unsigned)p.splits, m);
+  if (a.rows <= 8) LS_TRY(launch_dep(vocab_few_grad_kernel<8, VEC>, grid, dim3(128), 0, st, 1, g));
+  else LS_TRY(launch_dep(vocab_few_grad_kernel<16, VEC>, grid, dim3(128), 0, st, 1, g));
+  LS_TRY(launch_dep(vocab_fold_kernel<float>, dim3(stream_grid(a.rows * ((a.d + 3) / 4)), m), dim3(256), 0, st, 1,
+                    static_cast<const float*>(g.part), p.splits, a.rows * p.df, p.df, a.rows, a.d, static_cast<float*>(a.dh), a.dh_stride));
   return LS_OK;
 }
 
@@ -556,6 +977,7 @@ int run_vocab(const VocabArgs& a, bool grad, size_t ws_bytes, cudaStream_t st) {
         LS_TRY(cudaMemsetAsync(static_cast<char*>(a.dW) + i * a.dw_stride * eb, 0, (size_t)a.V * a.d * eb, st));
     return LS_OK;
   }
+  if (p.few) return a.d % 4 == 0 ? run_few<true>(a, p, st) : run_few<false>(a, p, st);
   for (int i = 0; i < a.m; i += p.batch) {
     const int rc = p.f32 ? run_replica<float, 3>(a, p, i, st) : run_replica<__nv_bfloat16, 1>(a, p, i, st);
     if (rc != LS_OK) return rc;

@@ -369,6 +369,30 @@ def test_vocab_loss_extreme_logits(dtype):
     assert abs(float(lse) - math.log(128.0)) < 1e-5 and abs(float(loss) - math.log(128.0)) < 1e-5
 
 
+@pytest.mark.parametrize("rows", [8, 200])
+def test_vocab_loss_fp32_probabilities_of_large_logits(rows):
+    """Exact logits around a log-sum-exp of 100: the probabilities must not carry the rounding of that number (2^-18), only
+    that of differences.  p = 2^t / S, t = (z - max) log2(e): t is off by 2^-24 |t| and by the constant's 2^-26 |t|, which
+    p turns into ln 2 of that; exp2 of p and of the terms of S, the division, the sums and the products with h = 1 are below
+    2^-20 together."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    d, V = 256, 700
+    g = _gen(rows)
+    h = torch.zeros(1, rows, d, device="cuda")
+    h[0, torch.arange(rows), torch.arange(rows)] = 1.0
+    W = (torch.randint(60 * 64, 100 * 64, (1, V, d), generator=g, device="cuda") / 64).float()
+    labels = torch.randint(0, V, (1, rows), generator=g, device="cuda", dtype=torch.int32)
+    _, _, _, dh, dW = b.vocab_loss_grad(h, W, labels, scale=float(rows))
+    z = W[0, :, :rows].double().T
+    p = torch.softmax(z, -1)
+    t = z.max(-1, keepdim=True)[0] - z
+    want = p - torch.nn.functional.one_hot(labels[0].long(), V).double()
+    # 1 / rows is rounded, too, and its product with the scale
+    _within(dW[0, :, :rows].T, want, (2.0 ** -20 + 2.0 ** -23 * t) * p + 4 * U * want.abs() + 1e-37, "dW")
+    assert float(dW[0, :, rows:].abs().max()) == 0.0
+
+
 def test_vocab_loss_gradient_against_differences():
     """Central differences of the 64-bit mean loss.  h = 1e-4 along directions of unit entries: truncation below
     h^2 (sum|dir W|)^3-scaled third derivatives of a softmax, under 1e-6 of the loss scale here; the kernel's fp32 gradient is
