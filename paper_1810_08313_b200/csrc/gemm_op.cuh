@@ -16,7 +16,7 @@
 //   warps 2-9  epilogue: warp w owns TMEM lanes 32 (w % 4) .. + 31 (rows) and one half of the columns; a thread adds the
 //              chunks of its row's NT / 2 columns in registers, rounding to nearest.  The tensor core's own fp32
 //              accumulation truncates, which biases a sum of a thousand MMAs by about 2e-5 of its value: short
-//              chunks keep that below the last bits that matter (see kChunk*), and since a tile's last chunk is
+//              chunks keep that below the last bits that matter (see chunk_of()), and since a tile's last chunk is
 //              collected like any other, the epilogue of a tile runs under the products of the next one.
 // NT is 256, or 128 where there are too few tiles for the pairs (pick_nt).  Collecting a chunk costs about as much as two K
 // blocks: a Newton-Schulz step of eight 2048 x 2048 matrices took 880 us at chunks of two, 780 us at eight.
@@ -614,9 +614,13 @@ int* device_error_word();
 
 // K blocks per tensor-memory accumulator.  One MMA adds 16 products per element and truncates: 64 MMAs bias a sum of equal
 // signs by about 2e-6 of its value, and sums of mixed signs by far less.  One piece: 256 MMAs for results that are rounded to
-// bf16 (whose half step is 4e-3), 32 for the row statistics, which leave in fp32.  Two: 16 MMAs of the large product.  Three:
-// 4, for 2 % more time than 8, which leave the gradient of a cross entropy over 10007 columns off by 6.9e-7, not 2.6e-7.
-constexpr int chunk_of(int np, bool stats) { return np == 1 ? (stats ? 8 : 64) : np == 2 ? 4 : 1; }
+// bf16 (whose half step is 4e-3), 32 for the row statistics, which leave in fp32, or 16 for a single tile of rows, where the
+// bytes of B bound the product and few rows average the losses' errors (2 x 2047 x 50001: 332 us at 32, 369 at 16, loss off by
+// 4e-7 and 2e-7; 64 x 32000: 26.5 and 27.1 us).  Two: 16 MMAs of the large product.  Three: 4, for 2 % more time than 8, which
+// leave the gradient of a cross entropy over 10007 columns off by 6.9e-7, not 2.6e-7.
+constexpr int chunk_of(int np, bool stats, int m_tiles) {
+  return np == 1 ? (!stats ? 64 : m_tiles > 1 ? 8 : 4) : np == 2 ? 4 : 1;
+}
 constexpr int kPairs = 74;
 
 // Fills in the tile counts and launches.  p.splits, p.M, p.N, p.batch, p.tri, p.n_fast and the epilogue's fields are the
@@ -636,7 +640,7 @@ cudaError_t launch_nt(const CUtensorMap& a, const CUtensorMap& b, const CUtensor
   p.kb_per_split = (p.num_kb + p.splits - 1) / p.splits;
   if (p.dominant != 0 && p.splits > 1) return cudaErrorInvalidValue;     // (the order goes round the whole K)
   p.splits = (p.num_kb + p.kb_per_split - 1) / p.kb_per_split;       // (callers ask pick_cut() first: no change here)
-  if (p.chunk_kb == 0) p.chunk_kb = chunk_of(NP, EPI != EPI_F32 && EPI != EPI_BF16);
+  if (p.chunk_kb == 0) p.chunk_kb = chunk_of(NP, EPI != EPI_F32 && EPI != EPI_BF16, p.m_tiles);
   int64_t per = (int64_t)p.m_tiles * p.n_tiles;
   if (p.tri) {
     per = 0;

@@ -107,10 +107,15 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
       const float tm = smax[i][lane];
       S += tm == -INFINITY ? ssum[i][lane] : ssum[i][lane] * gop::ex2(tm - M);
     }
-    const float l = (M == -INFINITY ? 0.f : M * kLn2) + logf(S);
-    a.lse[row] = l;
-    if (a.norm != nullptr) a.norm[row] = make_float2(M == -INFINITY ? 0.f : M, S);
-    a.row_loss[row] = has_label(a.labels[row], a.V) ? l - a.label_logit[row] : 0.f;
+    // S is a sum of 2^(z kLog2e - M), so that log-sum-exp and row loss are differences in that base, formed in double: rounded,
+    // a log-sum-exp of 20 is off by 1e-6, and so would be the loss, however small it is
+    const float ref = M == -INFINITY ? 0.f : M;
+    const double log_sum = (double)logf(S) * (1.0 / (double)kLn2);
+    a.lse[row] = (float)(((double)ref + log_sum) / (double)kLog2e);
+    if (a.norm != nullptr) a.norm[row] = make_float2(ref, S);
+    const bool labelled = has_label(a.labels[row], a.V);
+    a.row_loss[row] =
+        labelled ? (float)((fma(-(double)a.label_logit[row], (double)kLog2e, (double)ref) + log_sum) / (double)kLog2e) : 0.f;
   }
   if (a.inv_count == nullptr && a.loss == nullptr) return;
   __threadfence();
