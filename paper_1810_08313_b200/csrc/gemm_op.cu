@@ -57,8 +57,8 @@ static int make_map(CUtensorMap* out, const void* base, MapType type, int64_t ro
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 int make_operand_map(CUtensorMap* out, const void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
-                     int64_t plane) {
-  return make_map(out, base, type, rows, cols, planes, ld, plane, 128, 64, true);
+                     int64_t plane, int box_rows) {
+  return make_map(out, base, type, rows, cols, planes, ld, plane, 128, box_rows, true);
 }
 int make_output_map(CUtensorMap* out, void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
                     int64_t plane, int row_bytes, bool transposed) {

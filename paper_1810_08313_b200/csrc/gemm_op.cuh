@@ -77,6 +77,7 @@ struct Params {
   int tri;                               // 1: only tiles on or above the diagonal (symmetric C)
   int per, step;                         // tiles of one batch entry and split; 256 / NT
   int dominant;                          // where one K block dominates a row's (1) or a column's (2) sum: see k_order()
+  int a_box;                             // rows of a box of A's map if not 64 (K-major A with M <= a_box only)
   int n_fast;                            // 1: neighbouring pairs take neighbouring columns, else neighbouring rows
   int a_z0, a_zstep, b_z0, b_zstep;      // plane of batch entry z: z0 + z * zstep (+ piece)
   int c_z0, c_zstep;
@@ -251,27 +252,39 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const int k1 = min(p.num_kb, k0 + p.kb_per_split);
       const int az = p.a_z0 + tl.z * p.a_zstep, bz = p.b_z0 + tl.z * p.b_zstep;
       const int ma = tl.m * kTileM + rank * 128, nb = tl.n * NT + rank * HALF;
+      // Boxes wholly outside are left out: zero-filled rows are requests too, all to one place of the L2 (8 rows of 2048 times
+      // 32000 took 147 us instead of 36).  What their place holds ends in rows and columns that are not stored.
+      auto inside = [](int extent, int from, int most) { return min(max((extent - from + 63) / 64, 0), most); };
+      const int a_boxes = inside(p.M, ma, 2), b_boxes = inside(p.N, nb, HALF / 64);
+      const uint32_t bytes = (uint32_t)((inside(p.M, tl.m * kTileM, 2) + inside(p.M, tl.m * kTileM + 128, 2)) * p.a_box * 128 +
+                                        (inside(p.N, tl.n * NT, HALF / 64) + inside(p.N, tl.n * NT + HALF, HALF / 64)) * 8192);
+      const bool whole = a_boxes == 2 && b_boxes == HALF / 64;
       int kb = k0 + k_order<NT>(p, tl).first;
       for (int left = k1 - k0; left > 0 && !failed; --left) {
 #pragma unroll
         for (int q = NP - 1; q >= 0; --q) {        // in the order in which the MMAs let go of them
           if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[s], (round - 1) & 1))) { failed = true; break; }
           if (lead) {
-            if (rank == 0) mbar_expect_tx(&full[s], 2 * L::kSlot);      // both CTAs' bytes
+            if (rank == 0) mbar_expect_tx(&full[s], bytes);             // both CTAs'
             const uint32_t bar = full_leader + (uint32_t)(s * 8);
             uint8_t* sa = smem + s * L::kSlot;
             uint8_t* sb = sa + L::kA;
-            if (A_MN) {
-              tma_load_3d_pair(sa, &tmA, bar, ma, kb * 64, az + q, pol);
-              tma_load_3d_pair(sa + 8192, &tmA, bar, ma + 64, kb * 64, az + q, pol);
-            } else {
-              tma_load_3d_pair(sa, &tmA, bar, kb * 64, ma, az + q, pol);
-              tma_load_3d_pair(sa + 8192, &tmA, bar, kb * 64, ma + 64, az + q, pol);
-            }
-#pragma unroll
-            for (int c = 0; c < HALF / 64; ++c) {
+            auto load_a = [&](int c) {
+              if (A_MN) tma_load_3d_pair(sa + c * 8192, &tmA, bar, ma + c * 64, kb * 64, az + q, pol);
+              else tma_load_3d_pair(sa + c * 8192, &tmA, bar, kb * 64, ma + c * 64, az + q, pol);
+            };
+            auto load_b = [&](int c) {
               if (B_MN) tma_load_3d_pair(sb + c * 8192, &tmB, bar, nb + c * 64, kb * 64, bz + q, pol);
               else tma_load_3d_pair(sb + c * 8192, &tmB, bar, kb * 64, nb + c * 64, bz + q, pol);
+            };
+            if (whole) {                               // (unrolled: tests between the loads cost 3 % of a large product)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) load_a(c);
+#pragma unroll
+              for (int c = 0; c < HALF / 64; ++c) load_b(c);
+            } else {
+              for (int c = 0; c < a_boxes; ++c) load_a(c);
+              for (int c = 0; c < b_boxes; ++c) load_b(c);
             }
           }
           __syncwarp();
@@ -602,11 +615,11 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 // ---- host side ---------------------------------------------------------------------------------------------------
 
 // A stack of `planes` row-major matrices [rows][cols] of 16-bit or fp32 numbers (row pitch ld, plane pitch `plane`, in
-// elements, both 16-byte multiples).  An operand is read in boxes of 64 rows x 128 bytes with the 128-byte swizzle; an output
+// elements, both 16-byte multiples).  An operand is read in boxes of 64 rows (or box_rows, whole 8s) x 128 bytes with the 128-byte swizzle; an output
 // is written in boxes of 32 rows x `row_bytes` (Smem::kBoxRow) with the swizzle of that width, or, transposed, none.
 enum MapType { MAP_BF16, MAP_F16, MAP_F32 };
 int make_operand_map(CUtensorMap* out, const void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
-                     int64_t plane);
+                     int64_t plane, int box_rows = 64);
 int make_output_map(CUtensorMap* out, void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
                     int64_t plane, int row_bytes, bool transposed = false);
 // where a bounded wait that runs out is recorded (one word per device, read by ls_device_status); null on failure
@@ -648,6 +661,8 @@ cudaError_t launch_nt(const CUtensorMap& a, const CUtensorMap& b, const CUtensor
   }
   const int64_t total = per * p.splits * p.batch;
   if (total > 2000000000ll) return cudaErrorInvalidValue;
+  if (p.a_box == 0) p.a_box = 64;
+  if (p.a_box != 64 && (A_MN || p.M > p.a_box)) return cudaErrorInvalidValue;
   p.per = (int)per;
   p.total = (int)total;
   p.err = device_error_word();

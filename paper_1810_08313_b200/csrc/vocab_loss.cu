@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
 }
 
 // ---- exponentials -> dz, eight columns per thread ------------------------------------------------------------------------
-// bf16: in place over the fp16 numbers.
+// bf16: in place over the fp16 numbers.  Rows from `rows` to `pad`, which fill the last K block of dW, become zeros.
 // What the launch that forms dz does to a row of h for dW: rows without a label are cleared, so that whatever they hold stays out
 // of dW.  h itself is the caller's: where the product read it in place (src given), the other rows are copied into the
 // workspace; where it was laid out there already, they stay.
@@ -173,7 +173,7 @@ __device__ __forceinline__ void h_row(const HRows& h, int row, bool labelled) {
 // maxima are one load.  (Four groups of one row read as many sectors of the statistics as of a row; 8192 x 65536: 424 us.)
 constexpr int kDzCols = 2048, kDzRows = 4;
 __global__ void __launch_bounds__(256)
-vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int V, const float* stat_max, int64_t stat_ld, int slice,
+vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int pad, int V, const float* stat_max, int64_t stat_ld, int slice,
                      const int32_t* labels, const float* label_logit, const float* lse, const HRows h) {
   const int row0 = blockIdx.y * kDzRows;
   const int c = blockIdx.x * kDzCols + threadIdx.x * 8;
@@ -184,7 +184,7 @@ vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int V, const float* stat
   for (int k = 0; k < kDzRows; ++k) y[k] = row0 + k < rows ? labels[row0 + k] : -1;
 #pragma unroll
   for (int k = 0; k < kDzRows; ++k)
-    if (k % gridDim.x == blockIdx.x && row0 + k < rows) h_row(h, row0 + k, has_label(y[k], V));
+    if (k % gridDim.x == blockIdx.x && row0 + k < pad) h_row(h, row0 + k, has_label(y[k], V));
   if (c >= V) return;
   uint16_t* at = e + (int64_t)row0 * ld + c;
   // (rows of the statistics beyond the last one exist, padded to whole 256)
@@ -200,7 +200,7 @@ vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int V, const float* stat
     }
 #pragma unroll
   for (int k = 0; k < kDzRows; ++k) {
-    if (row0 + k >= rows) break;
+    if (row0 + k >= pad) break;
     uint32_t w[4] = {0, 0, 0, 0};
     if (has_label(y[k], V)) {
       const uint32_t in[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
@@ -245,13 +245,13 @@ struct Norm {
 
 // fp32: logits z -> three pieces of dz.
 __global__ void __launch_bounds__(256)
-vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t piece, int V, const int32_t* labels,
+vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t piece, int rows, int V, const int32_t* labels,
                      const float* label_logit, const float2* norm, const HRows h) {
   const int row = blockIdx.y;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   grid_dep_wait();
   grid_dep_launch();
-  const int y = labels[row];
+  const int y = row < rows ? labels[row] : -1;
   if (blockIdx.x == 0) h_row(h, row, has_label(y, V));
   if (c >= V) return;
   const int64_t at = (int64_t)row * ld + c;
@@ -771,6 +771,9 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   return p;
 }
 
+// Rows of a box of an operand with so many rows in all.
+int box_rows(int64_t rows) { return rows < 64 ? (int)round_up(rows, 8) : 64; }
+
 unsigned stream_grid(int64_t items) {
   const int64_t g = (items + 255) / 256;
   return (unsigned)(g < 148 * 8 ? (g < 1 ? 1 : g) : 148 * 8);
@@ -840,12 +843,13 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     const bf* hop = lay ? hpack : reinterpret_cast<const bf*>(hr);
     const int64_t hld = lay ? p.dp : d;
     CUtensorMap mh, me;
-    LS_TRY(gop::make_operand_map(&mh, hop, gop::MAP_BF16, rn, d, many ? p.batch : NP, hld, many ? a.h_stride : hplane));
+    const int a_box = box_rows(rn);
+    LS_TRY(gop::make_operand_map(&mh, hop, gop::MAP_BF16, rn, d, many ? p.batch : NP, hld, many ? a.h_stride : hplane, a_box));
     // logits
     Params g{};
     g.batch = p.batch; g.a_zstep = g.b_zstep = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
     g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld; g.stat_z = stat_z; g.label_z = a.rows;
-    g.labels = labels + r0; g.label_logit = logit + r0; g.clear = done;
+    g.labels = labels + r0; g.label_logit = logit + r0; g.clear = done; g.a_box = a_box;
     if (!p.grad) {
       LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(p.nt, mh, mw, mh, mh, g, d, st)));
     } else {
@@ -865,42 +869,44 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     // dz
     bf* dz = reinterpret_cast<bf*>(a.ws + p.o_dz);
     const HRows hrows{lay ? nullptr : hop, hpack, p.dp, hplane, d, NP};
-    // (grid.y is limited to 65535 rows a launch)
-    for (int64_t q0 = 0; q0 < rn; q0 += 65280) {
-      const unsigned qn = (unsigned)(rn - q0 < 65280 ? rn - q0 : 65280);
+    // (grid.y is limited to 65535 rows a launch; p.R rows are there, so that the padding is, too)
+    const int64_t rp = round_up(rn, 64);
+    for (int64_t q0 = 0; q0 < rp; q0 += 65280) {
+      const int qn = (int)(rp - q0 < 65280 ? rp - q0 : 65280), ql = (int)(rn - q0 < qn ? rn - q0 : qn);
       const int32_t* ly = labels + r0 + q0;
       HRows hr_q = hrows;
       hr_q.dst += q0 * p.dp;
       if (hr_q.src != nullptr) hr_q.src += q0 * d;
       if (F32) {
-        LS_TRY(launch_dep(vocab_dz_fp32_kernel, dim3((unsigned)((V + 1023) / 1024), qn), dim3(256), 0, st, 1,
-                          reinterpret_cast<const float*>(a.ws + p.o_e) + q0 * p.Vp, dz + q0 * p.Vp, p.Vp, p.R * p.Vp, (int)V,
+        LS_TRY(launch_dep(vocab_dz_fp32_kernel, dim3((unsigned)((V + 1023) / 1024), (unsigned)qn), dim3(256), 0, st, 1,
+                          reinterpret_cast<const float*>(a.ws + p.o_e) + q0 * p.Vp, dz + q0 * p.Vp, p.Vp, p.R * p.Vp, ql, (int)V,
                           ly, logit + r0 + q0, norm + q0, hr_q));
       } else {
-        LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + kDzCols - 1) / kDzCols), (qn + kDzRows - 1) / kDzRows),
-                          dim3(256), 0, st, 1, reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, (int)qn, (int)V,
+        LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + kDzCols - 1) / kDzCols), (unsigned)(qn + kDzRows - 1) / kDzRows),
+                          dim3(256), 0, st, 1, reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, ql, qn, (int)V,
                           stat_max + q0, p.stat_ld, p.nt / 2, ly, logit + r0 + q0, lse + r0 + q0, hr_q));
       }
     }
-    CUtensorMap mz, mhz, mo;
-    LS_TRY(gop::make_operand_map(&mz, dz, gop::MAP_BF16, rn, V, NP, p.Vp, p.R * p.Vp));
+    CUtensorMap mz, mzk, mhz, mo;
+    LS_TRY(gop::make_operand_map(&mz, dz, gop::MAP_BF16, rp, V, NP, p.Vp, p.R * p.Vp));
+    LS_TRY(gop::make_operand_map(&mzk, dz, gop::MAP_BF16, rn, V, NP, p.Vp, p.R * p.Vp, a_box));
     // dh = dz W
     T* dh = static_cast<T*>(a.dh) + rep * a.dh_stride + r0 * d;
     Params gh{};
-    gh.batch = 1; gh.splits = p.splits; gh.M = (int)rn; gh.N = d; gh.alpha = a.scale; gh.alpha_dev = inv; gh.n_fast = 1;
+    gh.batch = 1; gh.splits = p.splits; gh.M = (int)rn; gh.N = d; gh.alpha = a.scale; gh.alpha_dev = inv; gh.n_fast = 1; gh.a_box = a_box;
     if (p.dh_fold) {
       float* part = reinterpret_cast<float*>(a.ws + p.o_dh);
       gh.c_zstep = p.splits;
       LS_TRY(gop::make_output_map(&mo, part, gop::MAP_F32, rn, d, p.splits, p.df, p.R * p.df, kRow));
-      LS_TRY((gop::launch<NP, false, false, true, gop::EPI_F32>(p.nt_dh, mz, mw, mo, mo, gh, V, st)));
+      LS_TRY((gop::launch<NP, false, false, true, gop::EPI_F32>(p.nt_dh, mzk, mw, mo, mo, gh, V, st)));
       LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(rn * ((d + 3) / 4))), dim3(256), 0, st, 1,
                         static_cast<const float*>(part), p.splits, p.R * p.df, p.df, rn, d, dh, (int64_t)0));
     } else {
       LS_TRY(gop::make_output_map(&mo, dh, F32 ? gop::MAP_F32 : gop::MAP_BF16, rn, d, 1, d, rn * d, kRow));
-      LS_TRY((gop::launch<NP, false, false, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dh, mz, mw, mo, mo, gh, V, st)));
+      LS_TRY((gop::launch<NP, false, false, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dh, mzk, mw, mo, mo, gh, V, st)));
     }
     // dW (+)= dz^T h, with the rows that have no label cleared
-    LS_TRY(gop::make_operand_map(&mhz, hpack, gop::MAP_BF16, rn, d, NP, p.dp, hplane));
+    LS_TRY(gop::make_operand_map(&mhz, hpack, gop::MAP_BF16, rp, d, NP, p.dp, hplane));
     T* dW = static_cast<T*>(a.dW) + rep * a.dw_stride;
     Params gw{};
     gw.batch = 1; gw.splits = 1; gw.M = (int)V; gw.N = d; gw.alpha = a.scale; gw.alpha_dev = inv; gw.n_fast = 1;

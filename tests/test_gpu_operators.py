@@ -305,6 +305,17 @@ def test_vocab_loss_and_gradient(m, rows, d, V, dtype):
     _ce_check(h, W, y, b.vocab_loss_grad(h, W, y, scale=1.7), dtype, scale=1.7)
 
 
+@pytest.mark.parametrize("rows", [7, 16, 17, 31, 33, 64, 65, 127, 129, 191, 193, 255])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_vocab_loss_every_count_of_boxes(rows, dtype):
+    """Row counts whose tiles are filled by one to four boxes, whole and partial, and label-less rows at the end of each."""
+    from paper_1810_08313_b200 import binding as b
+    h, W, y = _ce_case(1, rows, 72, 300, dtype, seed=rows)
+    y[:, -1] = -1
+    _ce_check(h, W, y, b.vocab_loss(h, W, y), dtype, grad=False)
+    _ce_check(h, W, y, b.vocab_loss_grad(h, W, y), dtype)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_vocab_loss_labels_that_do_not_count(dtype):
     """Rows without a label (negative or beyond the vocabulary) have no loss and no gradient, and whatever their h holds
