@@ -340,11 +340,11 @@ vocab_fold_kernel(const float* part, int planes, int64_t plane, int64_t ld, int6
   }
 }
 
-// ---- fp32, few rows: CUDA cores ----------------------------------------------------------------------------------------
-// With a handful of rows W is all there is to read, and six tensor-core products of rows padded to 256 take longer than the
-// FMAs; laying W out as pieces alone moves 2.5 times its bytes.  Here W is read once for the logits and once more for the
-// gradient, whose pass also writes dW (kFewRows says up to where).  The logits' kernel is bound by the latency of its steps, at 3 to 4
-// TB/s of W for 8 rows; the gradient's by HBM, 5 TB/s for 8 rows.
+// ---- few rows: CUDA cores (bf16: of the gradient, after the product that gives the logits) ------------------------------
+// With a handful of rows W is all there is to read, and products of rows padded to 256 take longer than the FMAs; laying
+// an fp32 W out as pieces alone moves 2.5 times its bytes.  Here W is read once for the logits and once more for the
+// gradient, whose pass also writes dW (kFewRows says up to where).  The logits' kernel is bound by the latency of its steps, at 3
+// to 4 TB/s of W for 8 rows; the gradient's by HBM, 5 TB/s for 8 rows.
 
 // An infinity counts as the largest bf16 number, as it does in split3(); NaN stays.
 __device__ __forceinline__ float finite(float x) {
@@ -355,6 +355,9 @@ __device__ __forceinline__ float finite(float x) {
   return y;
 }
 __device__ __forceinline__ float4 finite(float4 v) { return make_float4(finite(v.x), finite(v.y), finite(v.z), finite(v.w)); }
+
+template <typename T>
+__device__ __forceinline__ float few_operand(float x) { return sizeof(T) == 4 ? finite(x) : x; }
 
 struct FewArgs {
   const float *h, *W;
@@ -549,58 +552,65 @@ vocab_few_dz_kernel(float* zz, int64_t ld, int rows, int V, const int32_t* label
   *at = o;
 }
 
-// dW = dz^T h and, per block of `block` columns of dz, its part of dh = dz W.  A CTA has 128 elements of d, a warp every fourth row
-// of W of the block: a lane reads its four elements, adds them times dz to RT rows of dh in registers, and writes the four of
-// dW from RT rows of h in registers.  The warps' sums of dh are added in order.
+// dW = dz^T h and, per block of `block` columns of dz, its part of dh = dz W.  A CTA has 128 (bf16: 256) elements of d, a warp every
+// fourth row of W of the block: a lane reads its 16 bytes, adds them times dz to RT rows of dh in registers, and writes the 16
+// bytes of dW from RT rows of h in registers.  The warps' sums of dh are added in order.
+template <typename T>
 struct FewGradArgs {
-  const float *h, *W, *dz;
+  const T *h, *W;
+  const float* dz;
   int64_t h_stride, w_stride, dw_stride, ldz;
   int rows, V, d, block;
   const int32_t* labels;
   const float* inv;
   float scale;
-  float *dW, *part;               // part: [replica][block][rows][ldp]
+  T* dW;
+  float* part;                    // [replica][block][rows][ldp]
   int64_t ldp;
 };
-template <int RT, bool VEC>
-__global__ void __launch_bounds__(128) vocab_few_grad_kernel(const FewGradArgs a) {
-  constexpr int kChunk = 128, kRows = 4;      // columns of dz in shared memory at a time; rows of W that a warp reads at a time
+template <typename T, int RT, bool VEC>
+__global__ void __launch_bounds__(128) vocab_few_grad_kernel(const FewGradArgs<T> a) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int C = F32 ? 4 : 8, kWide = 32 * C;   // elements of a lane, of a CTA
+  constexpr int kChunk = 128, kRows = 4;           // columns of dz in shared memory at a time; rows of W that a warp reads at a time
+  static_assert(F32 || VEC, "bf16 rows of whole 16 bytes");
   __shared__ __align__(16) float dz[kChunk][RT];
-  __shared__ float sum[4][RT][128];
+  __shared__ float sum[4][RT][kWide];
   const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
   const int64_t z = blockIdx.z;
-  const int k0 = blockIdx.x * 128;
+  const int k0 = blockIdx.x * kWide;
   grid_dep_wait();
   grid_dep_launch();
-  const float* W = a.W + z * a.w_stride;
-  float* dW = a.dW + z * a.dw_stride;
+  const T* W = a.W + z * a.w_stride;
+  T* dW = a.dW + z * a.dw_stride;
   const float* zz = a.dz + z * a.rows * a.ldz;
   const float alpha = a.scale * a.inv[z];
-  auto col = [&](int i) { return VEC ? k0 + lane * 4 + i : k0 + i * 32 + lane; };
-  float h[RT][4], acc[RT][4];
+  auto col = [&](int i) { return VEC ? k0 + lane * C + i : k0 + i * 32 + lane; };
+  float h[RT][C], acc[RT][C];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const bool in = r < a.rows && has_label(a.labels[z * a.rows + (r < a.rows ? r : 0)], a.V);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      h[r][i] = in && col(i) < a.d ? finite(a.h[z * a.h_stride + (int64_t)r * a.d + col(i)]) : 0.f;
+    for (int i = 0; i < C; ++i) {
+      h[r][i] = in && col(i) < a.d ? few_operand<T>((float)a.h[z * a.h_stride + (int64_t)r * a.d + col(i)]) : 0.f;
       acc[r][i] = 0.f;
     }
   }
   const int from = blockIdx.y * a.block, to = min(from + a.block, a.V);
-  float w[kRows][4];
-  auto read = [&](int v0) {                   // rows v0, v0 + 4, ...
+  uint4 w[kRows];                                  // as they lie in memory
+  auto read = [&](int v0) {                        // rows v0, v0 + 4, ...
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
       const int64_t at = (int64_t)(v0 + q * 4) * a.d;
       const bool in = v0 + q * 4 < to;
+      w[q] = make_uint4(0, 0, 0, 0);
       if constexpr (VEC) {
-        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (in && col(0) < a.d) t = __ldg(reinterpret_cast<const float4*>(W + at + col(0)));
-        w[q][0] = t.x; w[q][1] = t.y; w[q][2] = t.z; w[q][3] = t.w;
+        if (in && col(0) < a.d) w[q] = __ldg(reinterpret_cast<const uint4*>(W + at + col(0)));
       } else {
+        uint32_t* e = reinterpret_cast<uint32_t*>(&w[q]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[q][i] = in && col(i) < a.d ? __ldg(W + at + col(i)) : 0.f;
+        for (int i = 0; i < 4; ++i)
+          if (in && col(i) < a.d) e[i] = __float_as_uint(__ldg(W + at + col(i)));
       }
     }
   };
@@ -613,21 +623,31 @@ __global__ void __launch_bounds__(128) vocab_few_grad_kernel(const FewGradArgs a
     }
     __syncthreads();
     for (int c = wp; c < kChunk && c0 + c < to; c += 4 * kRows) {
-      float x[kRows][4];
+      uint4 x[kRows];
 #pragma unroll
-      for (int q = 0; q < kRows; ++q)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[q][i] = finite(w[q][i]);
-      read(c0 + c + 4 * kRows);               // the next ones, also across chunks
+      for (int q = 0; q < kRows; ++q) x[q] = w[q];
+      read(c0 + c + 4 * kRows);                    // the next ones, also across chunks
 #pragma unroll
       for (int q = 0; q < kRows; ++q) {
-        float o[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint32_t u[4] = {x[q].x, x[q].y, x[q].z, x[q].w};
+        float f[C], o[C];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (F32) {
+            f[i] = few_operand<T>(__uint_as_float(u[i]));
+          } else {
+            f[2 * i] = __uint_as_float(u[i] << 16);
+            f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) o[i] = 0.f;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
           const float g = dz[c + q * 4][r];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            acc[r][i] = fmaf(g, x[q][i], acc[r][i]);
+          for (int i = 0; i < C; ++i) {
+            acc[r][i] = fmaf(g, f[i], acc[r][i]);
             o[i] = fmaf(g, h[r][i], o[i]);
           }
         }
@@ -635,8 +655,13 @@ __global__ void __launch_bounds__(128) vocab_few_grad_kernel(const FewGradArgs a
         if (v < to) {
           const int64_t at = (int64_t)v * a.d;
           if constexpr (VEC) {
-            if (col(0) < a.d)
-              *reinterpret_cast<float4*>(dW + at + col(0)) = make_float4(alpha * o[0], alpha * o[1], alpha * o[2], alpha * o[3]);
+            uint32_t p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if constexpr (F32) p[i] = __float_as_uint(alpha * o[i]);
+              else p[i] = gop::pack_bf16(alpha * o[2 * i], alpha * o[2 * i + 1]);
+            }
+            if (col(0) < a.d) *reinterpret_cast<uint4*>(dW + at + col(0)) = make_uint4(p[0], p[1], p[2], p[3]);
           } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) if (col(i) < a.d) dW[at + col(i)] = alpha * o[i];
@@ -648,28 +673,27 @@ __global__ void __launch_bounds__(128) vocab_few_grad_kernel(const FewGradArgs a
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[wp][r][VEC ? lane * 4 + i : i * 32 + lane] = acc[r][i];
+    for (int i = 0; i < C; ++i) sum[wp][r][VEC ? lane * C + i : i * 32 + lane] = acc[r][i];
   __syncthreads();
   float* part = a.part + (z * gridDim.y + blockIdx.y) * a.rows * a.ldp;
-  const int k = k0 + threadIdx.x;
-  if (k < a.d)
-    for (int r = 0; r < a.rows; ++r) {
-      const int t = threadIdx.x;
-      part[r * a.ldp + k] = alpha * (((sum[0][r][t] + sum[1][r][t]) + sum[2][r][t]) + sum[3][r][t]);
-    }
+  for (int t = threadIdx.x; t < kWide && k0 + t < a.d; t += 128)
+    for (int r = 0; r < a.rows; ++r)
+      part[r * a.ldp + k0 + t] = alpha * (((sum[0][r][t] + sum[1][r][t]) + sum[2][r][t]) + sum[3][r][t]);
 }
 
 // ---- plan: what a call keeps in its workspace ---------------------------------------------------------------------------------
 constexpr int64_t kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
-// fp32: at most so many rows go to the CUDA cores.  (118995 x 1608, loss: 8 rows 229 us, 32 rows 435, 64 rows 810, on the tensor
-// cores 790 for any of them; gradient: 8 rows 530 us, 16 rows 826, tensor cores 1270.  32000 x 2048: 138 us for a loss of 32 rows, 257.)
-constexpr int64_t kFewRows = 32, kFewRowsGrad = 16;
+// At most so many rows go to the CUDA cores.  fp32 loss of 118995 x 1608: 8 rows 229 us, 32 rows 435, 64 rows 810, on the tensor
+// cores 790 for any of them (32000 x 2048: 138 us for 32 rows, 257).  fp32 gradient: 8 rows 530 us, 16 rows 830, tensor cores
+// 1270.  bf16 gradient of 118992 x 1608: 4 rows 280 us, 8 rows 379, tensor cores 288; dz stays in fp32 here, whose
+// rounding to bf16 no other row would average.
+constexpr int64_t kFewRows = 32, kFewRowsGrad = 16, kFewRowsGrad16 = 4;
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 struct Plan {
   bool f32, grad;
-  bool few;             // the CUDA-core path of few fp32 rows, all replicas at once
+  bool few;             // few rows on the CUDA cores, all replicas at once
   int np;
   int batch;            // replicas taken together: all of them where that leaves one product and one combining launch
   int64_t R;            // rows of a piece
@@ -695,9 +719,10 @@ int check_sizes(int m, int64_t rows, int64_t vocab, int d, int dtype) {
 // The parts of dh: about four CTAs an SM, in blocks of whole 64 columns.
 Plan few_plan(Plan p, int m, int64_t rows, int64_t V, int d) {
   p.batch = m;
-  p.slices = (int)((V + kFewCols - 1) / kFewCols);
+  p.nt = gop::pick_nt(rows, V, m, false);                  // (bf16: the logits are a product of all replicas)
+  p.slices = (int)(p.f32 ? (V + kFewCols - 1) / kFewCols : 2 * ((V + p.nt - 1) / p.nt));
   p.stat_ld = round_up(rows, 32);
-  const int64_t kb = (d + 127) / 128, want = (148 * 4 + kb * m - 1) / (kb * m);
+  const int64_t wide = p.f32 ? 128 : 256, kb = (d + wide - 1) / wide, want = (148 * 4 + kb * m - 1) / (kb * m);
   p.block = (int)round_up((V + want - 1) / want, 64);
   p.splits = (int)((V + p.block - 1) / p.block);
   size_t at = 0;
@@ -733,7 +758,7 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.R = rows > 0 ? round_up((rows + p.pieces - 1) / p.pieces, 256) : 0;
   p.pieces = rows > 0 ? (rows + p.R - 1) / p.R : 0;
   p.stat_ld = p.R;
-  p.few = p.f32 && rows > 0 && rows <= (grad ? kFewRowsGrad : kFewRows);
+  p.few = rows > 0 && (p.f32 ? rows <= (grad ? kFewRowsGrad : kFewRows) : grad && d % 8 == 0 && rows <= kFewRowsGrad16);
   if (p.few) return few_plan(p, m, rows, V, d);
   const bool lay = p.f32 || d % 8 != 0;
   p.batch = !grad && !lay && p.pieces == 1 && p.R * (p.Vp / 64 + 2) * 8 * m <= (int64_t)1 << 28 ? m : 1;
@@ -858,7 +883,8 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
       LS_TRY((gop::launch<NP, false, false, false, kEpi>(p.nt, mh, mw, me, me, g, d, st)));
     }
     CombineArgs cb{};
-    cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices; cb.rows = (int)rn; cb.V = (int)V;
+    cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices;
+    cb.rows = (int)rn; cb.V = (int)V;
     cb.labels = labels + r0; cb.label_logit = logit + r0; cb.lse = lse + r0; cb.row_loss = row_loss + r0;
     cb.done = done; cb.all_labels = labels; cb.all_row_loss = row_loss; cb.all_rows = a.rows;
     cb.norm = F32 && p.grad ? norm : nullptr;
@@ -935,45 +961,65 @@ cudaError_t launch_few_logits(const FewArgs& f, unsigned m, cudaStream_t st) {
   const dim3 grid((unsigned)((f.rows + RT - 1) / RT) * (unsigned)((f.V + kFewCols - 1) / kFewCols), 1, m);
   return launch_dep(kern, grid, dim3(128), kFewSmem<RT>, st, 1, f);
 }
-template <bool VEC>
+template <typename T, bool VEC>
 int run_few(const VocabArgs& a, const Plan& p, cudaStream_t st) {
   const unsigned m = (unsigned)a.m;
-  FewArgs f{};
-  f.h = static_cast<const float*>(a.h); f.W = static_cast<const float*>(a.W);
-  f.h_stride = a.h_stride; f.w_stride = a.w_stride; f.rows = (int)a.rows; f.V = (int)a.V; f.d = a.d;
-  f.z = p.grad ? reinterpret_cast<float*>(a.ws + p.o_e) : nullptr;
-  f.ldz = p.Vp;
-  f.stat_max = reinterpret_cast<float*>(a.ws + p.o_stat);
-  f.stat_ld = p.stat_ld; f.stat_z = p.slices * p.stat_ld;
-  f.stat_sum = f.stat_max + m * f.stat_z;
-  f.labels = a.labels;
-  f.label_logit = reinterpret_cast<float*>(a.ws + p.o_logit);
-  f.done = reinterpret_cast<unsigned*>(a.ws + p.o_done);
-  if (a.rows <= 8) LS_TRY((launch_few_logits<8, VEC>(f, m, st)));
-  else if (a.rows <= 16) LS_TRY((launch_few_logits<16, VEC>(f, m, st)));
-  else LS_TRY((launch_few_logits<32, VEC>(f, m, st)));
+  const int rows = (int)a.rows, V = (int)a.V;
+  float* z = p.grad ? reinterpret_cast<float*>(a.ws + p.o_e) : nullptr;
+  float* stat_max = reinterpret_cast<float*>(a.ws + p.o_stat);
+  const int64_t stat_z = p.slices * p.stat_ld;
+  float* stat_sum = stat_max + m * stat_z;
+  float* logit = reinterpret_cast<float*>(a.ws + p.o_logit);
+  unsigned* done = reinterpret_cast<unsigned*>(a.ws + p.o_done);
+  if constexpr (sizeof(T) == 4) {
+    FewArgs f{};
+    f.h = static_cast<const float*>(a.h); f.W = static_cast<const float*>(a.W);
+    f.h_stride = a.h_stride; f.w_stride = a.w_stride; f.rows = rows; f.V = V; f.d = a.d;
+    f.z = z; f.ldz = p.Vp;
+    f.stat_max = stat_max; f.stat_sum = stat_sum; f.stat_ld = p.stat_ld; f.stat_z = stat_z;
+    f.labels = a.labels; f.label_logit = logit; f.done = done;
+    if (rows <= 8) LS_TRY((launch_few_logits<8, VEC>(f, m, st)));
+    else if (rows <= 16) LS_TRY((launch_few_logits<16, VEC>(f, m, st)));
+    else LS_TRY((launch_few_logits<32, VEC>(f, m, st)));
+  } else {
+    CUtensorMap mh, mw, mz;
+    const int a_box = box_rows(rows);
+    LS_TRY(gop::make_operand_map(&mh, a.h, gop::MAP_BF16, rows, a.d, m, a.d, m > 1 ? a.h_stride : (int64_t)rows * a.d, a_box));
+    LS_TRY(gop::make_operand_map(&mw, a.W, gop::MAP_BF16, V, a.d, m, a.d, m > 1 ? a.w_stride : a.V * a.d));
+    LS_TRY(gop::make_output_map(&mz, z, gop::MAP_F32, rows, V, m, p.Vp, rows * p.Vp, gop::box_row(1)));
+    Params g{};
+    g.batch = a.m; g.a_zstep = g.b_zstep = g.c_zstep = 1; g.splits = 1; g.M = rows; g.N = V; g.alpha = 1.f;
+    g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld; g.stat_z = stat_z; g.label_z = rows;
+    g.labels = a.labels; g.label_logit = logit; g.clear = done; g.a_box = a_box;
+    LS_TRY((gop::launch<1, false, false, false, gop::EPI_STATS_F32>(p.nt, mh, mw, mz, mz, g, a.d, st)));
+  }
   CombineArgs cb{};
-  cb.stat_max = f.stat_max; cb.stat_sum = f.stat_sum; cb.stat_ld = f.stat_ld; cb.stat_z = f.stat_z; cb.slices = p.slices;
-  cb.rows = f.rows; cb.V = f.V; cb.labels = cb.all_labels = a.labels; cb.label_logit = f.label_logit;
+  cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices;
+  cb.rows = rows; cb.V = V; cb.labels = cb.all_labels = a.labels; cb.label_logit = logit;
   cb.lse = a.lse ? a.lse : reinterpret_cast<float*>(a.ws + p.o_lse);
   cb.row_loss = a.row_loss ? a.row_loss : reinterpret_cast<float*>(a.ws + p.o_rowloss);
-  cb.all_row_loss = cb.row_loss; cb.all_rows = a.rows; cb.done = f.done; cb.loss = a.loss;
+  cb.all_row_loss = cb.row_loss; cb.all_rows = a.rows; cb.done = done; cb.loss = a.loss;
   float2* norm = reinterpret_cast<float2*>(a.ws + p.o_norm);
   float* inv = reinterpret_cast<float*>(a.ws + p.o_inv);
   if (p.grad) { cb.norm = norm; cb.inv_count = inv; }
-  LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((a.rows + 31) / 32), m), dim3(1024), 0, st, 1, cb));
+  LS_TRY(launch_dep(vocab_combine_kernel, dim3((unsigned)((rows + 31) / 32), m), dim3(1024), 0, st, 1, cb));
   if (!p.grad) return LS_OK;
-  LS_TRY(launch_dep(vocab_few_dz_kernel, dim3((unsigned)((a.V + 1023) / 1024), (unsigned)a.rows, m), dim3(256), 0, st, 1, f.z, f.ldz,
-                    f.rows, f.V, a.labels, static_cast<const float*>(f.label_logit), static_cast<const float2*>(norm)));
-  FewGradArgs g{};
-  g.h = f.h; g.W = f.W; g.dz = f.z; g.h_stride = a.h_stride; g.w_stride = a.w_stride; g.dw_stride = a.dw_stride; g.ldz = f.ldz;
-  g.rows = f.rows; g.V = f.V; g.d = a.d; g.block = p.block; g.labels = a.labels; g.inv = inv; g.scale = a.scale;
-  g.dW = static_cast<float*>(a.dW); g.part = reinterpret_cast<float*>(a.ws + p.o_dh); g.ldp = p.df;
-  const dim3 grid((unsigned)((a.d + 127) / 128), (unsigned)p.splits, m);
-  if (a.rows <= 8) LS_TRY(launch_dep(vocab_few_grad_kernel<8, VEC>, grid, dim3(128), 0, st, 1, g));
-  else LS_TRY(launch_dep(vocab_few_grad_kernel<16, VEC>, grid, dim3(128), 0, st, 1, g));
-  LS_TRY(launch_dep(vocab_fold_kernel<float>, dim3(stream_grid(a.rows * ((a.d + 3) / 4)), m), dim3(256), 0, st, 1,
-                    static_cast<const float*>(g.part), p.splits, a.rows * p.df, p.df, a.rows, a.d, static_cast<float*>(a.dh), a.dh_stride));
+  LS_TRY(launch_dep(vocab_few_dz_kernel, dim3((unsigned)((V + 1023) / 1024), (unsigned)rows, m), dim3(256), 0, st, 1, z, p.Vp, rows, V,
+                    a.labels, static_cast<const float*>(logit), static_cast<const float2*>(norm)));
+  FewGradArgs<T> g{};
+  g.h = static_cast<const T*>(a.h); g.W = static_cast<const T*>(a.W); g.dz = z;
+  g.h_stride = a.h_stride; g.w_stride = a.w_stride; g.dw_stride = a.dw_stride; g.ldz = p.Vp;
+  g.rows = rows; g.V = V; g.d = a.d; g.block = p.block; g.labels = a.labels; g.inv = inv; g.scale = a.scale;
+  g.dW = static_cast<T*>(a.dW); g.part = reinterpret_cast<float*>(a.ws + p.o_dh); g.ldp = p.df;
+  constexpr int kWide = sizeof(T) == 4 ? 128 : 256;
+  const dim3 grid((unsigned)((a.d + kWide - 1) / kWide), (unsigned)p.splits, m);
+  if (rows <= 4) LS_TRY(launch_dep(vocab_few_grad_kernel<T, 4, VEC>, grid, dim3(128), 0, st, 1, g));
+  if constexpr (sizeof(T) == 4) {
+    if (rows > 4 && rows <= 8) LS_TRY(launch_dep(vocab_few_grad_kernel<T, 8, VEC>, grid, dim3(128), 0, st, 1, g));
+    if (rows > 8) LS_TRY(launch_dep(vocab_few_grad_kernel<T, 16, VEC>, grid, dim3(128), 0, st, 1, g));
+  }
+  LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(a.rows * ((a.d + 3) / 4)), m), dim3(256), 0, st, 1,
+                    static_cast<const float*>(g.part), p.splits, rows * p.df, p.df, a.rows, a.d, static_cast<T*>(a.dh), a.dh_stride));
   return LS_OK;
 }
 
@@ -988,7 +1034,8 @@ int run_vocab(const VocabArgs& a, bool grad, size_t ws_bytes, cudaStream_t st) {
         LS_TRY(cudaMemsetAsync(static_cast<char*>(a.dW) + i * a.dw_stride * eb, 0, (size_t)a.V * a.d * eb, st));
     return LS_OK;
   }
-  if (p.few) return a.d % 4 == 0 ? run_few<true>(a, p, st) : run_few<false>(a, p, st);
+  if (p.few && !p.f32) return run_few<__nv_bfloat16, true>(a, p, st);
+  if (p.few) return a.d % 4 == 0 ? run_few<float, true>(a, p, st) : run_few<float, false>(a, p, st);
   for (int i = 0; i < a.m; i += p.batch) {
     const int rc = p.f32 ? run_replica<float, 3>(a, p, i, st) : run_replica<__nv_bfloat16, 1>(a, p, i, st);
     if (rc != LS_OK) return rc;
