@@ -83,7 +83,7 @@ struct Params {
   int c_z0, c_zstep;
   int M, N;
   float alpha;
-  const float* alpha_dev;                // EPI_F32, EPI_BF16: a further factor of alpha in device memory, or null
+  const float* alpha_dev;                // EPI_F32, EPI_BF16: further factors of alpha in device memory, one per batch entry, or null
   int reduce;                            // EPI_F32: C += instead of C =
   // row statistics: slice t = column / (NT / 2) of row r at [t * stat_ld + r]
   float* stat_max;                       // slice maximum * log2(e)
@@ -500,7 +500,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
       }
       if constexpr (EPI == EPI_STATS_F16 || EPI == EPI_BF16) {
-        const float alpha = EPI == EPI_BF16 && p.alpha_dev != nullptr ? p.alpha * __ldg(p.alpha_dev) : p.alpha;
+        const float alpha = EPI == EPI_BF16 && p.alpha_dev != nullptr ? p.alpha * __ldg(p.alpha_dev + tl.z) : p.alpha;
         constexpr int W = ROW / 2;
 #pragma unroll
         for (int j = 0; j < HALF / W; ++j) {
@@ -521,7 +521,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
       }
       if constexpr (EPI == EPI_F32) {
-        const float alpha = p.alpha_dev != nullptr ? p.alpha * __ldg(p.alpha_dev) : p.alpha;
+        const float alpha = p.alpha_dev != nullptr ? p.alpha * __ldg(p.alpha_dev + tl.z) : p.alpha;
         constexpr int W = ROW / 4;
 #pragma unroll
         for (int j = 0; j < HALF / W; ++j) {

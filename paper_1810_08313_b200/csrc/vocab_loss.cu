@@ -155,16 +155,17 @@ struct HRows {
   const __nv_bfloat16* src;
   __nv_bfloat16* dst;
   int64_t ld, piece;
+  int64_t src_z, dst_z;                    // between replicas
   int d, np;
 };
-__device__ __forceinline__ void h_row(const HRows& h, int row, bool labelled) {
+__device__ __forceinline__ void h_row(const HRows& h, int64_t z, int row, bool labelled) {
   const int n = (h.d + 7) / 8;             // pieces of 16 bytes (rows of the workspace are padded to whole ones)
-  uint4* dst = reinterpret_cast<uint4*>(h.dst + (int64_t)row * h.ld);
+  uint4* dst = reinterpret_cast<uint4*>(h.dst + z * h.dst_z + (int64_t)row * h.ld);
   if (!labelled) {
     for (int q = 0; q < h.np; ++q)
       for (int i = threadIdx.x; i < n; i += blockDim.x) dst[q * (h.piece / 8) + i] = make_uint4(0, 0, 0, 0);
   } else if (h.src != nullptr) {
-    const uint4* src = reinterpret_cast<const uint4*>(h.src + (int64_t)row * h.d);
+    const uint4* src = reinterpret_cast<const uint4*>(h.src + z * h.src_z + (int64_t)row * h.d);
     for (int i = threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
   }
 }
@@ -172,11 +173,14 @@ __device__ __forceinline__ void h_row(const HRows& h, int row, bool labelled) {
 // A CTA takes four rows of 2048 columns: a thread's four groups of eight columns lie below one another, in one slice, whose four
 // maxima are one load.  (Four groups of one row read as many sectors of the statistics as of a row; 8192 x 65536: 424 us.)
 constexpr int kDzCols = 2048, kDzRows = 4;
+struct DzStep { int64_t e, out, stat, rows; };          // elements between replicas (blockIdx.z)
 __global__ void __launch_bounds__(256)
 vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int pad, int V, const float* stat_max, int64_t stat_ld, int slice,
-                     const int32_t* labels, const float* label_logit, const float* lse, const HRows h) {
+                     const int32_t* labels, const float* label_logit, const float* lse, const HRows h, const DzStep by) {
   const int row0 = blockIdx.y * kDzRows;
   const int c = blockIdx.x * kDzCols + threadIdx.x * 8;
+  const int64_t z = blockIdx.z;
+  e += z * by.e; stat_max += z * by.stat; labels += z * by.rows; label_logit += z * by.rows; lse += z * by.rows;
   grid_dep_wait();
   grid_dep_launch();
   int y[kDzRows];
@@ -184,7 +188,7 @@ vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int pad, int V, const fl
   for (int k = 0; k < kDzRows; ++k) y[k] = row0 + k < rows ? labels[row0 + k] : -1;
 #pragma unroll
   for (int k = 0; k < kDzRows; ++k)
-    if (k % gridDim.x == blockIdx.x && row0 + k < pad) h_row(h, row0 + k, has_label(y[k], V));
+    if (k % gridDim.x == blockIdx.x && row0 + k < pad) h_row(h, z, row0 + k, has_label(y[k], V));
   if (c >= V) return;
   uint16_t* at = e + (int64_t)row0 * ld + c;
   // (rows of the statistics beyond the last one exist, padded to whole 256)
@@ -246,13 +250,15 @@ struct Norm {
 // fp32: logits z -> three pieces of dz.
 __global__ void __launch_bounds__(256)
 vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t piece, int rows, int V, const int32_t* labels,
-                     const float* label_logit, const float2* norm, const HRows h) {
+                     const float* label_logit, const float2* norm, const HRows h, const DzStep by) {
   const int row = blockIdx.y;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  const int64_t rep = blockIdx.z;
+  z += rep * by.e; out += rep * by.out; labels += rep * by.rows; label_logit += rep * by.rows; norm += rep * by.rows;
   grid_dep_wait();
   grid_dep_launch();
   const int y = row < rows ? labels[row] : -1;
-  if (blockIdx.x == 0) h_row(h, row, has_label(y, V));
+  if (blockIdx.x == 0) h_row(h, rep, row, has_label(y, V));
   if (c >= V) return;
   const int64_t at = (int64_t)row * ld + c;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -282,7 +288,10 @@ vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t pie
 // ---- operands into the workspace: rows padded to whole 16 bytes, fp32 cut into three pieces ------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256)
-vocab_pack_kernel(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t ld, int64_t piece, bool vec) {
+vocab_pack_kernel(const T* src, int64_t src_z, int64_t rows, int d, __nv_bfloat16* dst, int64_t dst_z, int64_t ld, int64_t piece,
+                  bool vec) {
+  src += blockIdx.y * src_z;                   // replica
+  dst += blockIdx.y * dst_z;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int PER = F32 ? 4 : 8;
   const int per_row = (d + PER - 1) / PER;
@@ -695,7 +704,7 @@ struct Plan {
   bool f32, grad;
   bool few;             // few rows on the CUDA cores, all replicas at once
   int np;
-  int batch;            // replicas taken together: all of them where that leaves one product and one combining launch
+  int batch;            // replicas taken together: all of them where the rows are one piece and the workspace stays small
   int64_t R;            // rows of a piece
   int64_t pieces;
   int64_t Vp, dp;       // padded row lengths: probabilities, packed operands
@@ -714,6 +723,45 @@ int check_sizes(int m, int64_t rows, int64_t vocab, int d, int dtype) {
   if (dtype != LS_DTYPE_FP32 && dtype != LS_DTYPE_BF16) return LS_ERR_INVALID_ARG;
   if (m > 65535 || rows > 2147483647ll || vocab > kMaxVocab || d > kMaxWidth) return LS_ERR_TOO_LARGE;
   return LS_OK;
+}
+
+// What m replicas need that are taken `batch` at a time.
+Plan replica_plan(Plan p, int m, int batch, int64_t rows, int64_t V, int d) {
+  const bool grad = p.grad, lay = p.f32 || d % 8 != 0;
+  p.batch = batch;
+  p.stat_ld = p.R;
+  // tile widths of the three products (a slice of the statistics is half a tile)
+  const int64_t most_rows = p.R < rows ? p.R : rows;
+  p.nt = gop::pick_nt(most_rows, V, p.batch, false);
+  const gop::Cut cut = gop::pick_cut(most_rows, d, batch, false, V, p.np, grad ? 64 : 1);
+  p.nt_dh = cut.nt;
+  p.splits = cut.splits;
+  p.nt_dw = gop::pick_nt(V, d, batch, false);
+  p.slices = (int)(2 * ((V + p.nt - 1) / p.nt));
+  const bool whole = d % (p.f32 ? 4 : 8) == 0;
+  p.dh_fold = grad && (p.splits > 1 || !whole);
+  p.dw_fold = grad && (!whole || (!p.f32 && p.pieces > 1));
+  size_t at = 0;
+  auto take = [&at](int64_t bytes) { size_t o = at; at += (size_t)round_up(bytes, 256); return o; };
+  p.o_stat = take(2 * (int64_t)p.batch * p.slices * p.stat_ld * 4);
+  p.o_logit = take(m * rows * 4);
+  p.o_lse = take(m * rows * 4);
+  p.o_rowloss = take(m * rows * 4);
+  p.o_norm = take(p.f32 && grad ? batch * p.R * 8 : 0);
+  p.o_inv = take(m * 4);
+  p.o_done = take(4 * (int64_t)p.batch);
+  // operands laid out anew: fp32 ones (as pieces), bf16 ones whose rows are no whole 16 bytes, and, for dW, h with the
+  // rows that have no label cleared
+  p.o_h = take(lay || grad ? batch * p.np * p.R * p.dp * 2 : 0);
+  p.o_w = take(lay ? batch * p.np * V * p.dp * 2 : 0);
+  if (grad) {
+    p.o_e = take(batch * p.R * p.Vp * (p.f32 ? 4 : 2));
+    p.o_dz = p.f32 ? take(batch * 3 * p.R * p.Vp * 2) : p.o_e;
+    p.o_dh = take(p.dh_fold ? (int64_t)batch * p.splits * p.R * p.df * 4 : 0);
+    p.o_dw = take(p.dw_fold ? batch * V * p.df * 4 : 0);
+  }
+  p.total = at;
+  return p;
 }
 
 // The parts of dh: about four CTAs an SM, in blocks of whole 64 columns.
@@ -757,43 +805,13 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.pieces = rows > 0 ? (rows + R - 1) / R : 0;
   p.R = rows > 0 ? round_up((rows + p.pieces - 1) / p.pieces, 256) : 0;
   p.pieces = rows > 0 ? (rows + p.R - 1) / p.R : 0;
-  p.stat_ld = p.R;
   p.few = rows > 0 && (p.f32 ? rows <= (grad ? kFewRowsGrad : kFewRows) : grad && d % 8 == 0 && rows <= kFewRowsGrad16);
   if (p.few) return few_plan(p, m, rows, V, d);
-  const bool lay = p.f32 || d % 8 != 0;
-  p.batch = !grad && !lay && p.pieces == 1 && p.R * (p.Vp / 64 + 2) * 8 * m <= (int64_t)1 << 28 ? m : 1;
-  // tile widths of the three products (a slice of the statistics is half a tile)
-  const int64_t most_rows = p.R < rows ? p.R : rows;
-  p.nt = gop::pick_nt(most_rows, V, p.batch, false);
-  const gop::Cut cut = gop::pick_cut(most_rows, d, 1, false, V, p.np, grad ? 64 : 1);
-  p.nt_dh = cut.nt;
-  p.splits = cut.splits;
-  p.nt_dw = gop::pick_nt(V, d, 1, false);
-  p.slices = (int)(2 * ((V + p.nt - 1) / p.nt));
-  const bool whole = d % (p.f32 ? 4 : 8) == 0;
-  p.dh_fold = grad && (p.splits > 1 || !whole);
-  p.dw_fold = grad && (!whole || (!p.f32 && p.pieces > 1));
-  size_t at = 0;
-  auto take = [&at](int64_t bytes) { size_t o = at; at += (size_t)round_up(bytes, 256); return o; };
-  p.o_stat = take(2 * (int64_t)p.batch * p.slices * p.stat_ld * 4);
-  p.o_logit = take(m * rows * 4);
-  p.o_lse = take(m * rows * 4);
-  p.o_rowloss = take(m * rows * 4);
-  p.o_norm = take(p.f32 && grad ? p.R * 8 : 0);
-  p.o_inv = take(m * 4);
-  p.o_done = take(4 * (int64_t)p.batch);
-  // operands laid out anew: fp32 ones (as pieces), bf16 ones whose rows are no whole 16 bytes, and, for dW, h with the
-  // rows that have no label cleared
-  p.o_h = take(lay || grad ? p.np * p.R * p.dp * 2 : 0);
-  p.o_w = take(lay ? p.np * V * p.dp * 2 : 0);
-  if (grad) {
-    p.o_e = take(p.R * p.Vp * (p.f32 ? 4 : 2));
-    p.o_dz = p.f32 ? take(3 * p.R * p.Vp * 2) : p.o_e;
-    p.o_dh = take(p.dh_fold ? (int64_t)p.splits * p.R * p.df * 4 : 0);
-    p.o_dw = take(p.dw_fold ? V * p.df * 4 : 0);
+  if (m > 1 && p.pieces == 1) {
+    const Plan all = replica_plan(p, m, m, rows, V, d);
+    if (all.total <= (size_t)1 << 28) return all;
   }
-  p.total = at;
-  return p;
+  return replica_plan(p, m, 1, rows, V, d);
 }
 
 // Rows of a box of an operand with so many rows in all.
@@ -805,11 +823,12 @@ unsigned stream_grid(int64_t items) {
 }
 
 template <typename T>
-cudaError_t pack(const T* src, int64_t rows, int d, __nv_bfloat16* dst, int64_t ld, int64_t piece, cudaStream_t st) {
+cudaError_t pack(const T* src, int64_t src_z, int m, int64_t rows, int d, __nv_bfloat16* dst, int64_t dst_z, int64_t ld,
+                 int64_t piece, cudaStream_t st) {
   const int per = 16 / sizeof(T);
-  const bool vec = d % per == 0 && reinterpret_cast<uintptr_t>(src) % 16 == 0;
-  return launch_dep(vocab_pack_kernel<T>, dim3(stream_grid(rows * ((d + per - 1) / per))), dim3(256), 0, st, 1, src, rows, d,
-                    dst, ld, piece, vec);
+  const bool vec = d % per == 0 && reinterpret_cast<uintptr_t>(src) % 16 == 0 && (m == 1 || src_z % per == 0);
+  return launch_dep(vocab_pack_kernel<T>, dim3(stream_grid(rows * ((d + per - 1) / per)), (unsigned)m), dim3(256), 0, st, 1, src,
+                    src_z, rows, d, dst, dst_z, ld, piece, vec);
 }
 
 struct VocabArgs {
@@ -854,32 +873,33 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
   const int64_t V = a.V;
   const int d = a.d;
   const bool lay = F32 || d % 8 != 0;
-  if (lay) LS_TRY(pack<T>(W, V, d, wpack, p.dp, V * p.dp, st));
+  const int nb = p.batch;
+  const bool many = nb > 1;
+  if (lay) LS_TRY(pack<T>(W, a.w_stride, nb, V, d, wpack, NP * V * p.dp, p.dp, V * p.dp, st));
   const bf* wop = lay ? wpack : reinterpret_cast<const bf*>(W);
   const int64_t wld = lay ? p.dp : d;
   CUtensorMap mw;
-  const bool many = p.batch > 1;
-  LS_TRY(gop::make_operand_map(&mw, wop, gop::MAP_BF16, V, d, many ? p.batch : NP, wld, many ? a.w_stride : V * wld));
+  LS_TRY(gop::make_operand_map(&mw, wop, gop::MAP_BF16, V, d, nb * NP, wld, many && !lay ? a.w_stride : V * wld));
   for (int64_t r0 = 0, piece = 0; r0 < a.rows; r0 += p.R, ++piece) {
     const int64_t rn = a.rows - r0 < p.R ? a.rows - r0 : p.R;
     const T* hr = h + r0 * d;
     const int64_t hplane = p.R * p.dp;
-    if (lay) LS_TRY(pack<T>(hr, rn, d, hpack, p.dp, hplane, st));
+    if (lay) LS_TRY(pack<T>(hr, a.h_stride, nb, rn, d, hpack, NP * hplane, p.dp, hplane, st));
     const bf* hop = lay ? hpack : reinterpret_cast<const bf*>(hr);
     const int64_t hld = lay ? p.dp : d;
     CUtensorMap mh, me;
     const int a_box = box_rows(rn);
-    LS_TRY(gop::make_operand_map(&mh, hop, gop::MAP_BF16, rn, d, many ? p.batch : NP, hld, many ? a.h_stride : hplane, a_box));
+    LS_TRY(gop::make_operand_map(&mh, hop, gop::MAP_BF16, rn, d, nb * NP, hld, many && !lay ? a.h_stride : hplane, a_box));
     // logits
     Params g{};
-    g.batch = p.batch; g.a_zstep = g.b_zstep = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
+    g.batch = nb; g.a_zstep = g.b_zstep = NP; g.c_zstep = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
     g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld; g.stat_z = stat_z; g.label_z = a.rows;
     g.labels = labels + r0; g.label_logit = logit + r0; g.clear = done; g.a_box = a_box;
     if (!p.grad) {
       LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(p.nt, mh, mw, mh, mh, g, d, st)));
     } else {
       constexpr gop::Epi kEpi = F32 ? gop::EPI_STATS_F32 : gop::EPI_STATS_F16;
-      LS_TRY(gop::make_output_map(&me, a.ws + p.o_e, F32 ? gop::MAP_F32 : gop::MAP_F16, rn, V, 1, p.Vp, p.R * p.Vp, kRow));
+      LS_TRY(gop::make_output_map(&me, a.ws + p.o_e, F32 ? gop::MAP_F32 : gop::MAP_F16, rn, V, nb, p.Vp, p.R * p.Vp, kRow));
       LS_TRY((gop::launch<NP, false, false, false, kEpi>(p.nt, mh, mw, me, me, g, d, st)));
     }
     CombineArgs cb{};
@@ -894,7 +914,8 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     if (!p.grad) continue;
     // dz
     bf* dz = reinterpret_cast<bf*>(a.ws + p.o_dz);
-    const HRows hrows{lay ? nullptr : hop, hpack, p.dp, hplane, d, NP};
+    const HRows hrows{lay ? nullptr : hop, hpack, p.dp, hplane, a.h_stride, NP * hplane, d, NP};
+    const DzStep by{p.R * p.Vp, NP * p.R * p.Vp, stat_z, a.rows};
     // (grid.y is limited to 65535 rows a launch; p.R rows are there, so that the padding is, too)
     const int64_t rp = round_up(rn, 64);
     for (int64_t q0 = 0; q0 < rp; q0 += 65280) {
@@ -904,48 +925,48 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
       hr_q.dst += q0 * p.dp;
       if (hr_q.src != nullptr) hr_q.src += q0 * d;
       if (F32) {
-        LS_TRY(launch_dep(vocab_dz_fp32_kernel, dim3((unsigned)((V + 1023) / 1024), (unsigned)qn), dim3(256), 0, st, 1,
+        LS_TRY(launch_dep(vocab_dz_fp32_kernel, dim3((unsigned)((V + 1023) / 1024), (unsigned)qn, (unsigned)nb), dim3(256), 0, st, 1,
                           reinterpret_cast<const float*>(a.ws + p.o_e) + q0 * p.Vp, dz + q0 * p.Vp, p.Vp, p.R * p.Vp, ql, (int)V,
-                          ly, logit + r0 + q0, norm + q0, hr_q));
+                          ly, logit + r0 + q0, norm + q0, hr_q, by));
       } else {
-        LS_TRY(launch_dep(vocab_dz_bf16_kernel, dim3((unsigned)((V + kDzCols - 1) / kDzCols), (unsigned)(qn + kDzRows - 1) / kDzRows),
-                          dim3(256), 0, st, 1, reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, ql, qn, (int)V,
-                          stat_max + q0, p.stat_ld, p.nt / 2, ly, logit + r0 + q0, lse + r0 + q0, hr_q));
+        LS_TRY(launch_dep(vocab_dz_bf16_kernel,
+                          dim3((unsigned)((V + kDzCols - 1) / kDzCols), (unsigned)(qn + kDzRows - 1) / kDzRows, (unsigned)nb), dim3(256), 0, st, 1, reinterpret_cast<uint16_t*>(dz) + q0 * p.Vp, p.Vp, ql, qn, (int)V,
+                          stat_max + q0, p.stat_ld, p.nt / 2, ly, logit + r0 + q0, lse + r0 + q0, hr_q, by));
       }
     }
     CUtensorMap mz, mzk, mhz, mo;
-    LS_TRY(gop::make_operand_map(&mz, dz, gop::MAP_BF16, rp, V, NP, p.Vp, p.R * p.Vp));
-    LS_TRY(gop::make_operand_map(&mzk, dz, gop::MAP_BF16, rn, V, NP, p.Vp, p.R * p.Vp, a_box));
+    LS_TRY(gop::make_operand_map(&mz, dz, gop::MAP_BF16, rp, V, nb * NP, p.Vp, p.R * p.Vp));
+    LS_TRY(gop::make_operand_map(&mzk, dz, gop::MAP_BF16, rn, V, nb * NP, p.Vp, p.R * p.Vp, a_box));
     // dh = dz W
     T* dh = static_cast<T*>(a.dh) + rep * a.dh_stride + r0 * d;
     Params gh{};
-    gh.batch = 1; gh.splits = p.splits; gh.M = (int)rn; gh.N = d; gh.alpha = a.scale; gh.alpha_dev = inv; gh.n_fast = 1; gh.a_box = a_box;
+    gh.batch = nb; gh.a_zstep = gh.b_zstep = NP; gh.c_zstep = 1; gh.splits = p.splits; gh.M = (int)rn; gh.N = d; gh.alpha = a.scale; gh.alpha_dev = inv; gh.n_fast = 1; gh.a_box = a_box;
     if (p.dh_fold) {
       float* part = reinterpret_cast<float*>(a.ws + p.o_dh);
       gh.c_zstep = p.splits;
-      LS_TRY(gop::make_output_map(&mo, part, gop::MAP_F32, rn, d, p.splits, p.df, p.R * p.df, kRow));
+      LS_TRY(gop::make_output_map(&mo, part, gop::MAP_F32, rn, d, (int64_t)nb * p.splits, p.df, p.R * p.df, kRow));
       LS_TRY((gop::launch<NP, false, false, true, gop::EPI_F32>(p.nt_dh, mzk, mw, mo, mo, gh, V, st)));
-      LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(rn * ((d + 3) / 4))), dim3(256), 0, st, 1,
-                        static_cast<const float*>(part), p.splits, p.R * p.df, p.df, rn, d, dh, (int64_t)0));
+      LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(rn * ((d + 3) / 4)), (unsigned)nb), dim3(256), 0, st, 1,
+                        static_cast<const float*>(part), p.splits, p.R * p.df, p.df, rn, d, dh, a.dh_stride));
     } else {
-      LS_TRY(gop::make_output_map(&mo, dh, F32 ? gop::MAP_F32 : gop::MAP_BF16, rn, d, 1, d, rn * d, kRow));
+      LS_TRY(gop::make_output_map(&mo, dh, F32 ? gop::MAP_F32 : gop::MAP_BF16, rn, d, nb, d, many ? a.dh_stride : rn * d, kRow));
       LS_TRY((gop::launch<NP, false, false, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dh, mzk, mw, mo, mo, gh, V, st)));
     }
     // dW (+)= dz^T h, with the rows that have no label cleared
-    LS_TRY(gop::make_operand_map(&mhz, hpack, gop::MAP_BF16, rp, d, NP, p.dp, hplane));
+    LS_TRY(gop::make_operand_map(&mhz, hpack, gop::MAP_BF16, rp, d, nb * NP, p.dp, hplane));
     T* dW = static_cast<T*>(a.dW) + rep * a.dw_stride;
     Params gw{};
-    gw.batch = 1; gw.splits = 1; gw.M = (int)V; gw.N = d; gw.alpha = a.scale; gw.alpha_dev = inv; gw.n_fast = 1;
+    gw.batch = nb; gw.a_zstep = gw.b_zstep = NP; gw.c_zstep = 1; gw.splits = 1; gw.M = (int)V; gw.N = d; gw.alpha = a.scale; gw.alpha_dev = inv; gw.n_fast = 1;
     gw.reduce = piece > 0;
     if (p.dw_fold) {
       float* sum = reinterpret_cast<float*>(a.ws + p.o_dw);
-      LS_TRY(gop::make_output_map(&mo, sum, gop::MAP_F32, V, d, 1, p.df, V * p.df, kRow));
+      LS_TRY(gop::make_output_map(&mo, sum, gop::MAP_F32, V, d, nb, p.df, V * p.df, kRow));
       LS_TRY((gop::launch<NP, false, true, true, gop::EPI_F32>(p.nt_dw, mz, mhz, mo, mo, gw, rn, st)));
       if (r0 + p.R >= a.rows)
-        LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(V * ((d + 3) / 4))), dim3(256), 0, st, 1,
-                          static_cast<const float*>(sum), 1, (int64_t)0, p.df, V, d, dW, (int64_t)0));
+        LS_TRY(launch_dep(vocab_fold_kernel<T>, dim3(stream_grid(V * ((d + 3) / 4)), (unsigned)nb), dim3(256), 0, st, 1,
+                          static_cast<const float*>(sum), 1, V * p.df, p.df, V, d, dW, a.dw_stride));
     } else {
-      LS_TRY(gop::make_output_map(&mo, dW, F32 ? gop::MAP_F32 : gop::MAP_BF16, V, d, 1, d, V * d, kRow));
+      LS_TRY(gop::make_output_map(&mo, dW, F32 ? gop::MAP_F32 : gop::MAP_BF16, V, d, nb, d, many ? a.dw_stride : V * d, kRow));
       LS_TRY((gop::launch<NP, false, true, true, F32 ? gop::EPI_F32 : gop::EPI_BF16>(p.nt_dw, mz, mhz, mo, mo, gw, rn, st)));
     }
   }
