@@ -615,8 +615,8 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 // ---- host side ---------------------------------------------------------------------------------------------------
 
 // A stack of `planes` row-major matrices [rows][cols] of 16-bit or fp32 numbers (row pitch ld, plane pitch `plane`, in
-// elements, both 16-byte multiples).  An operand is read in boxes of 64 rows (or box_rows, whole 8s) x 128 bytes with the 128-byte swizzle; an output
-// is written in boxes of 32 rows x `row_bytes` (Smem::kBoxRow) with the swizzle of that width, or, transposed, none.
+// elements, both 16-byte multiples).  An operand is read in boxes of 64 rows (or box_rows, whole 8s) x 128 bytes with
+// the 128-byte swizzle; an output is written in boxes of 32 rows x `row_bytes` (Smem::kBoxRow) with the swizzle of that width, or, transposed, none.
 enum MapType { MAP_BF16, MAP_F16, MAP_F32 };
 int make_operand_map(CUtensorMap* out, const void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
                      int64_t plane, int box_rows = 64);

@@ -4,8 +4,8 @@
 //   X_0 = U / (|U|_F + 1e-7)
 //   X_{k+1} = a X_k + (b A + c A^2) X_k = P_k X_k,   A = X_k X_k^T,   P = a I + A (b I + c A)
 //
-// with (a, b, c) = (3.4445, -4.7750, 2.0315), which drives every singular value of U towards 1 (into about [0.7, 1.2]) and leaves the singular vectors alone.  With
-// n the shorter and k the longer side the step is two symmetric products of n x n results and one full one.  The side of
+// with (a, b, c) = (3.4445, -4.7750, 2.0315), which drives every singular value of U towards 1 (into about [0.7, 1.2]) and
+// leaves the singular vectors alone.  With n the shorter and k the longer side the step is two symmetric products of n x n results and one full one.  The side of
 // the Gram matrix is the shorter one: A = X X^T and P X for a wide matrix, A = X^T X and X P for a tall one; both
 // read X as it lies (K- or MN-major operands), nothing is transposed.
 //
