@@ -317,6 +317,29 @@ def test_vocab_loss_every_count_of_boxes(rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("m,rows,d,V", [(1, 1, 8, 130), (2, 4, 136, 1000), (3, 4, 264, 257), (2, 5, 520, 700), (2, 9, 132, 385),
+                                        (1, 16, 1000, 129), (2, 17, 260, 500), (1, 32, 77, 1025)])
+def test_vocab_loss_few_rows(m, rows, d, V, dtype):
+    """Row counts on both sides of every limit for few rows, several replicas; a row without a label may hold anything."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    h, W, y = _ce_case(m, rows, d, V, dtype, seed=rows + d)
+    _ce_check(h, W, y, b.vocab_loss(h, W, y), dtype, grad=False)
+    _ce_check(h, W, y, b.vocab_loss_grad(h, W, y, scale=0.7), dtype, scale=0.7)
+    y2 = y.clone()
+    y2[:, -1] = V
+    clean = b.vocab_loss_grad(h, W, y2)
+    h2 = h.clone()
+    h2[:, -1] = float("nan")
+    for i, (got, want) in enumerate(zip(b.vocab_loss_grad(h2, W, y2), clean)):
+        if i == 2:
+            got, want = got[:, :-1], want[:, :-1]          # lse of the row itself is NaN
+        assert torch.equal(got, want)
+    assert float(clean[3][:, -1].abs().max()) == 0.0
+    b.device_status()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_vocab_loss_labels_that_do_not_count(dtype):
     """Rows without a label (negative or beyond the vocabulary) have no loss and no gradient, and whatever their h holds
     stays out of dW; a call without any label has loss 0 and zero gradients."""
