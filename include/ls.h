@@ -143,7 +143,12 @@ int ls_set_params(ls_handle* h, const float* x1_host);
 int ls_set_state(ls_handle* h, int replica, const float* params_host, const float* momentum_host);
 int ls_get_state(ls_handle* h, int replica, float* params_host, float* momentum_host);
 /* Device views of the packed replicas: base pointers and the stride between
- * replicas in floats.  The memory belongs to the state block. */
+ * replicas in floats.  The memory belongs to the state block.  Views are for
+ * reading: the handle does not see a write through them (the bf16 copies that the
+ * products of a bf16 model read, and the copy of the synchronized model that the
+ * first local step after ls_set_params or an averaging step reads, keep the old
+ * values).  Inside a replica, tensors start at multiples of 64 floats, and a bf16
+ * model keeps the matrices of its wide layers in 32 x 32 blocks, not row-major. */
 int ls_state_view(ls_handle* h, float** params_dev, float** momentum_dev, int64_t* stride_floats);
 
 /* ---- data -------------------------------------------------------------- */
@@ -470,12 +475,20 @@ int ls_orthogonalize(const void* u_dev, int m, int rows, int cols, int64_t u_str
                      int64_t out_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream);
 
 /* One orthogonalised momentum step (the Muon update) of the matrices w [m][rows][cols] with momentum buffers v, both
- * fp32 (ls_state_view() of a handle gives such stacks), from gradients g of g_dtype:
+ * fp32, in the caller's memory (for the weights of a handle: ls_muon_step_layer()), from gradients g of g_dtype:
  *   v <- momentum * v + g;   u = nesterov ? g + momentum * v : v;   w <- w - lr * sqrt(max(1, rows / cols)) * O(u)
  * with O the orthogonalisation above.  0 <= momentum < 1. */
 int ls_muon_step(float* w_dev, float* v_dev, const void* g_dev, int m, int rows, int cols, int64_t w_stride,
                  int64_t v_stride, int64_t g_stride, int g_dtype, float lr, float momentum, int nesterov, int steps, void* ws_dev,
                  size_t ws_bytes, void* cuda_stream);
+
+/* The same step of the matrix W_l of layer `layer` (0-based) of all m replicas of a handle, with the handle's momentum
+ * buffers as v, from gradients g [m][dims[layer + 1]][dims[layer]], row-major, g_stride elements apart.  Whatever the
+ * handle keeps beside the weights follows: local steps, averages and losses after the call see the new weights.  Biases stay as
+ * they are; lr and momentum are this call's own, not the handle's.  Enqueued on the handle's stream; workspace as
+ * ls_orthogonalize_ws_bytes(m, dims[layer + 1], dims[layer]) has it. */
+int ls_muon_step_layer(ls_handle* h, int layer, const void* g_dev, int64_t g_stride, int g_dtype, float lr, float momentum,
+                       int nesterov, int steps, void* ws_dev, size_t ws_bytes);
 
 /* Per-kernel device timing.  Between ls_profile_begin() and ls_profile_end()
  * every launch of a kernel class selected by class_mask (bit c = class c; for

@@ -132,6 +132,7 @@ def _lib():
         "ls_orthogonalize": (C.c_int, [vp, C.c_int, C.c_int, C.c_int, i64, C.c_int, C.c_int, vp, i64, vp, C.c_size_t, vp]),
         "ls_muon_step": (C.c_int, [vp, vp, vp, C.c_int, C.c_int, C.c_int, i64, i64, i64, C.c_int, f32, f32, C.c_int, C.c_int,
                                    vp, C.c_size_t, vp]),
+        "ls_muon_step_layer": (C.c_int, [vp, C.c_int, vp, i64, C.c_int, f32, f32, C.c_int, C.c_int, vp, C.c_size_t]),
         "ls_shard_buffer_floats": (C.c_int, [vp, P(i64)]),
         "ls_set_shard": (C.c_int, [vp, C.c_int, C.c_int, vp, vp, EXCHANGE_FN, vp]),
         "ls_shard_partial_sum": (C.c_int, [vp, vp]),
@@ -611,8 +612,8 @@ def orthogonalize(u, steps: int = 5, out=None, workspace=None, stream=None):
 def muon_step(w, v, g, lr: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5, workspace=None,
               stream=None) -> None:
     """One orthogonalised momentum step of the float32 matrices w [m][rows][cols] with momentum buffers v, in place,
-    from gradients g (float32 or bfloat16) (ls_muon_step).  w and v may be views into packed replica vectors
-    (LocalSGD.state_view)."""
+    from gradients g (float32 or bfloat16) (ls_muon_step).  w and v may be views into packed replica vectors of the
+    caller's; the weights of a LocalSGD take LocalSGD.muon_step."""
     op = _Op(w, stream)
     dt = _op_dtype(g, "g")
     if w.dim() not in (2, 3):
@@ -720,7 +721,8 @@ class LocalSGD:
         return np.stack(ps), np.stack(vs)
 
     def state_view(self):
-        """(params, momentum) as float32 CUDA tensors [m][stride] aliasing the state block."""
+        """(params, momentum) as float32 CUDA tensors [m][stride] aliasing the state block, to be read: the handle does
+        not see what is written through them (ls_state_view)."""
         torch = self._torch
         pp, vp, st = C.c_void_p(), C.c_void_p(), C.c_int64()
         _check(self.lib.ls_state_view(self.h, C.byref(pp), C.byref(vp), C.byref(st)), "ls_state_view")
@@ -730,6 +732,21 @@ class LocalSGD:
             off = ptr - base
             out.append(self.state[off:off + self.m * st.value * 4].view(torch.float32).view(self.m, st.value))
         return out[0], out[1]
+
+    def muon_step(self, layer: int, g, lr: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
+                  workspace=None) -> None:
+        """One orthogonalised momentum step of layer `layer`'s matrix (0-based) of all replicas, from gradients g
+        [m][dims[layer + 1]][dims[layer]] (float32 or bfloat16), on the handle's stream (ls_muon_step_layer)."""
+        if not 0 <= layer < len(self.dims) - 1:
+            raise ValueError("no such layer")
+        op = _Op(g, self.stream)
+        dt = _op_dtype(g, "g")
+        rows, cols = self.dims[layer + 1], self.dims[layer]
+        gp, _, gs = op.stack(g, "g", (rows, cols), self.m)
+        base, nbytes, keep = op.workspace(g, workspace, _ws_bytes("ls_orthogonalize_ws_bytes", self.m, rows, cols))
+        with self._torch.cuda.device(self.device):
+            _check(self.lib.ls_muon_step_layer(self.h, int(layer), gp, gs, dt, float(lr), float(momentum),
+                                               int(bool(nesterov)), int(steps), base, nbytes), "ls_muon_step_layer")
 
     # -- data ---------------------------------------------------------------
     def bind_dataset(self, x, y):

@@ -917,6 +917,21 @@ int ls_state_view(ls_handle* h, float** params_dev, float** momentum_dev, int64_
   return LS_OK;
 }
 
+int ls_muon_step_layer(ls_handle* h, int layer, const void* g_dev, int64_t g_stride, int g_dtype, float lr, float momentum,
+                       int nesterov, int steps, void* ws_dev, size_t ws_bytes) {
+  if (!ok_handle(h)) return LS_ERR_BAD_HANDLE;
+  const Layout& lay = h->lay;
+  if (layer < 0 || layer >= lay.L) return LS_ERR_INVALID_ARG;
+  const int rc = muon_step(params_of(h) + lay.w_off[layer], mom_of(h) + lay.w_off[layer], g_dev, lay.m, lay.dims[layer + 1],
+                           lay.dims[layer], lay.stride, lay.stride, g_stride, g_dtype, lr, momentum, nesterov, steps,
+                           lay.tiled[layer] != 0, ws_dev, ws_bytes, h->stream);
+  // (a refused call has changed nothing; after a failed launch something may have run)
+  if (rc != LS_OK && rc != LS_ERR_CUDA) return rc;
+  h->sync_valid = false;           // the replicas have left the synchronized copy
+  if (rc != LS_OK) return rc;
+  return refresh_shadow(h);
+}
+
 int ls_bind_dataset(ls_handle* h, const void* x_dev, const void* y_dev, int64_t n_rows) {
   if (!ok_handle(h)) return LS_ERR_BAD_HANDLE;
   if (x_dev == nullptr || y_dev == nullptr || n_rows < h->lay.batch) return LS_ERR_INVALID_ARG;

@@ -52,6 +52,7 @@ struct MatArgs {
   int64_t w_stride, v_stride, g_stride, out_stride;
   float lr, mu;
   int nesterov;
+  int blocked;                         // w and v lie in 32 x 32 blocks (TileMap), rows and cols multiples of 32
   int64_t ld, plane;                   // pieces of X: row pitch, elements of one piece
   double* partial;                     // [m][kSumBlocks]
   int blocks;                          // partial sums per matrix
@@ -88,6 +89,10 @@ __device__ __forceinline__ void store4(T* p, int left, const float (&f)[4]) {
     for (int i = 0; i < 4; ++i) if (i < left) p[i] = (T)f[i];
   }
 }
+// Where four consecutive elements of w and v from (r, c) on start, `at` their place in row-major order.
+__device__ __forceinline__ int64_t state_at(const MatArgs& a, int64_t at, int r, int c) {
+  return a.blocked ? ((int64_t)(r >> 5) * (a.cols >> 5) + (c >> 5)) * 1024 + (r & 31) * 32 + (c & 31) : at;
+}
 // For each of this warp's units: load(k, offset, row, column, elements left in the row) for its four groups, then
 // use(k, ...) for them, so that the loads of a unit are in flight together.
 template <typename L, typename F>
@@ -120,15 +125,15 @@ __global__ void __launch_bounds__(32 * kWarps) ns_momentum_kernel(const MatArgs 
   float g[4][4], v[4][4];
   for_units(
       a,
-      [&](int k, int64_t at, int, int, int left) {
+      [&](int k, int64_t at, int r, int c, int left) {
         load4<G, VEC>(gz + at, left, g[k]);
-        if constexpr (MUON) load4<float, VEC>(vz + at, left, v[k]);
+        if constexpr (MUON) load4<float, VEC>(vz + state_at(a, at, r, c), left, v[k]);
       },
-      [&](int k, int64_t at, int, int, int left) {
+      [&](int k, int64_t at, int r, int c, int left) {
         if constexpr (MUON) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[k][i] = fmaf(a.mu, v[k][i], g[k][i]);
-          store4<float, VEC>(vz + at, left, v[k]);
+          store4<float, VEC>(vz + state_at(a, at, r, c), left, v[k]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) g[k][i] = a.nesterov ? fmaf(a.mu, v[k][i], g[k][i]) : v[k][i];
         }
@@ -168,9 +173,9 @@ __global__ void __launch_bounds__(32 * kWarps) ns_start_kernel(const MatArgs a, 
   float g[4][4], v[4][4];
   for_units(
       a,
-      [&](int k, int64_t at, int, int, int left) {
+      [&](int k, int64_t at, int r, int c, int left) {
         load4<G, VEC>(gz + at, left, g[k]);
-        if constexpr (MUON) load4<float, VEC>(vz + at, left, v[k]);
+        if constexpr (MUON) load4<float, VEC>(vz + state_at(a, at, r, c), left, v[k]);
       },
       [&](int k, int64_t, int r, int c, int) {
         if constexpr (MUON) {
@@ -213,9 +218,9 @@ __global__ void __launch_bounds__(32 * kWarps) ns_finish_kernel(const MatArgs a,
         const __half* p = hi + (int64_t)r * a.ld + c;
         h[k] = *reinterpret_cast<const uint2*>(p);
         l[k] = *reinterpret_cast<const uint2*>(p + a.plane);
-        if constexpr (MUON) load4<float, VEC>(wz + at, left, w[k]);
+        if constexpr (MUON) load4<float, VEC>(wz + state_at(a, at, r, c), left, w[k]);
       },
-      [&](int k, int64_t at, int, int, int left) {
+      [&](int k, int64_t at, int r, int c, int left) {
         const uint32_t hw[2] = {h[k].x, h[k].y}, lw[2] = {l[k].x, l[k].y};
         float o[4];
 #pragma unroll
@@ -227,7 +232,7 @@ __global__ void __launch_bounds__(32 * kWarps) ns_finish_kernel(const MatArgs a,
         if constexpr (MUON) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[k][i] = fmaf(-step, o[i], w[k][i]);
-          store4<float, VEC>(wz + at, left, w[k]);
+          store4<float, VEC>(wz + state_at(a, at, r, c), left, w[k]);
         } else {
           store4<G, VEC>(oz + at, left, o);
         }
@@ -487,6 +492,27 @@ int check_ws(int m, int rows, int cols, const void* ws, size_t ws_bytes) {
 }
 
 }  // namespace
+
+int muon_step(float* w_dev, float* v_dev, const void* g_dev, int m, int rows, int cols, int64_t w_stride, int64_t v_stride,
+              int64_t g_stride, int g_dtype, float lr, float momentum, int nesterov, int steps, bool blocked, void* ws_dev,
+              size_t ws_bytes, cudaStream_t st) {
+  int rc = check_sizes(m, rows, cols);
+  if (rc != LS_OK) return rc;
+  if (w_dev == nullptr || v_dev == nullptr || g_dev == nullptr || steps < 1 || steps > kMaxSteps) return LS_ERR_INVALID_ARG;
+  if (g_dtype != LS_DTYPE_FP32 && g_dtype != LS_DTYPE_BF16) return LS_ERR_INVALID_ARG;
+  if (!isfinite(lr) || !(momentum >= 0.f) || !(momentum < 1.f) || (nesterov != 0 && nesterov != 1)) return LS_ERR_INVALID_ARG;
+  if (off(w_dev, 4) || off(v_dev, 4) || off(g_dev, g_dtype == LS_DTYPE_BF16 ? 2 : 4)) return LS_ERR_INVALID_ARG;
+  const int64_t n = (int64_t)rows * cols;
+  if (m > 1 && (w_stride < n || v_stride < n || g_stride < n)) return LS_ERR_INVALID_ARG;
+  rc = check_ws(m, rows, cols, ws_dev, ws_bytes);
+  if (rc != LS_OK) return rc;
+  MatArgs a{};
+  a.g = g_dev; a.g_stride = g_stride; a.w = w_dev; a.v = v_dev; a.w_stride = w_stride; a.v_stride = v_stride;
+  a.m = m; a.rows = rows; a.cols = cols; a.lr = lr; a.mu = momentum; a.nesterov = nesterov; a.blocked = blocked ? 1 : 0;
+  return g_dtype == LS_DTYPE_BF16 ? pick_ns<__nv_bfloat16, true>(a, steps, static_cast<char*>(ws_dev), st)
+                                  : pick_ns<float, true>(a, steps, static_cast<char*>(ws_dev), st);
+}
+
 }  // namespace ls
 
 extern "C" int ls_orthogonalize_ws_bytes(int m, int rows, int cols, size_t* bytes) {
@@ -521,21 +547,6 @@ extern "C" int ls_orthogonalize(const void* u_dev, int m, int rows, int cols, in
 extern "C" int ls_muon_step(float* w_dev, float* v_dev, const void* g_dev, int m, int rows, int cols, int64_t w_stride,
                             int64_t v_stride, int64_t g_stride, int g_dtype, float lr, float momentum, int nesterov, int steps, void* ws_dev,
                             size_t ws_bytes, void* cuda_stream) {
-  using namespace ls;
-  int rc = check_sizes(m, rows, cols);
-  if (rc != LS_OK) return rc;
-  if (w_dev == nullptr || v_dev == nullptr || g_dev == nullptr || steps < 1 || steps > kMaxSteps) return LS_ERR_INVALID_ARG;
-  if (g_dtype != LS_DTYPE_FP32 && g_dtype != LS_DTYPE_BF16) return LS_ERR_INVALID_ARG;
-  if (!isfinite(lr) || !(momentum >= 0.f) || !(momentum < 1.f) || (nesterov != 0 && nesterov != 1)) return LS_ERR_INVALID_ARG;
-  if (off(w_dev, 4) || off(v_dev, 4) || off(g_dev, g_dtype == LS_DTYPE_BF16 ? 2 : 4)) return LS_ERR_INVALID_ARG;
-  const int64_t n = (int64_t)rows * cols;
-  if (m > 1 && (w_stride < n || v_stride < n || g_stride < n)) return LS_ERR_INVALID_ARG;
-  rc = check_ws(m, rows, cols, ws_dev, ws_bytes);
-  if (rc != LS_OK) return rc;
-  MatArgs a{};
-  a.g = g_dev; a.g_stride = g_stride; a.w = w_dev; a.v = v_dev; a.w_stride = w_stride; a.v_stride = v_stride;
-  a.m = m; a.rows = rows; a.cols = cols; a.lr = lr; a.mu = momentum; a.nesterov = nesterov;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return g_dtype == LS_DTYPE_BF16 ? pick_ns<__nv_bfloat16, true>(a, steps, static_cast<char*>(ws_dev), st)
-                                  : pick_ns<float, true>(a, steps, static_cast<char*>(ws_dev), st);
+  return ls::muon_step(w_dev, v_dev, g_dev, m, rows, cols, w_stride, v_stride, g_stride, g_dtype, lr, momentum, nesterov, steps,
+                       false, ws_dev, ws_bytes, static_cast<cudaStream_t>(cuda_stream));
 }

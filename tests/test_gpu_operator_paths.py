@@ -1,0 +1,101 @@
+"""Paths of the operators beside the plain call: on a handle's weights, replica by replica, in pieces, with failures."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import localsgd_oracle as orc
+from paper_1810_08313_b200 import workloads as wl
+from tests.helpers import f32, max_rel_err_per_tensor, small_problem, tensor_slices, to_device
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- the momentum step on a handle's weights -----------------------------------------------------------------------
+
+def _newton(u):
+    import torch
+    x = u / (torch.linalg.norm(u) + 1e-7)
+    x = x.T if u.shape[0] > u.shape[1] else x
+    for _ in range(5):
+        a = x @ x.T
+        x = 3.4445 * x + (-4.7750 * a + 2.0315 * a @ a) @ x
+    return x.T if u.shape[0] > u.shape[1] else x
+
+
+@pytest.mark.parametrize("gdtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dims,dtype,B,layer", [
+    ((24, 40, 10), "fp32", 8, 1),                # CUDA-core layers
+    ((256, 384, 128, 10), "fp32", 128, 0),       # tensor-core layers of an fp32 model: row-major, read from the synchronized copy
+    ((256, 384, 128, 10), "fp32", 128, 1),
+    ((384, 512, 256, 10), "bf16", 256, 0),       # blocked matrices with their operand copies, tall and wide
+    ((384, 512, 256, 10), "bf16", 256, 1),
+    ((384, 512, 256, 10), "bf16", 256, 2),       # the narrow output layer
+    ((200, 136, 72, 10), "bf16", 48, 1),         # row-major matrices with operand copies
+])
+def test_muon_step_of_a_handles_layer(dims, dtype, B, layer, gdtype):
+    """After set_params and after an averaging step, when the handle knows its replicas to be equal: the step's weights and
+    momentum against 64 bits, every other tensor untouched, and local steps that go on from them as a handle does that was
+    given the same state from the host."""
+    import torch
+    from paper_1810_08313_b200.binding import LocalSGD
+    m, bf = 3, dtype == "bf16"
+    spec, X, y, x1 = small_problem(dims, "softmax_ce", True, 1024, 31, bf16=bf)
+    xd, yd = to_device(X, y, bf16=bf)
+    offs = wl.batch_row_offsets(3, 4, m, 1024, B)
+    eng, other = [LocalSGD(m, dims, gemm_dtype=dtype, lr=0.05, momentum=0.9, batch=B) for _ in range(2)]
+    for e in (eng, other):
+        e.bind_dataset(xd, yd)
+    eng.set_params(x1)
+    rows, cols = dims[layer + 1], dims[layer]
+    mine = dict(tensor_slices(dims, True))[f"W{layer + 1}"]
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    lr, mu = 0.3, 0.95
+    for turn in range(2):
+        g = torch.randn(m, rows, cols, generator=gen, device="cuda").to(torch.bfloat16 if gdtype == "bf16" else torch.float32)
+        p0, v0 = eng.get_all()
+        assert np.array_equal(p0[0], p0[1])
+        eng.muon_step(layer, g, lr=lr, momentum=mu)
+        p1, v1 = eng.get_all()
+        for i in range(m):
+            g64 = g[i].double()
+            v64 = f32(mu) * torch.from_numpy(v0[i][mine]).cuda().double().view(rows, cols) + g64
+            w64 = torch.from_numpy(p0[i][mine]).cuda().double().view(rows, cols) - \
+                f32(lr) * math.sqrt(max(1.0, rows / cols)) * _newton(g64 + f32(mu) * v64)
+            # v: two roundings.  w: five steps turn the products' 2^-22 into at most 4^5 of it, relative to the norm of O
+            assert float((torch.from_numpy(v1[i][mine]).cuda().double().view(rows, cols) - v64).abs().max()) \
+                <= 2.0 ** -22 * float(v64.abs().max())
+            err = torch.linalg.norm(torch.from_numpy(p1[i][mine]).cuda().double().view(rows, cols) - w64)
+            assert float(err) <= lr * math.sqrt(max(1.0, rows / cols) * min(rows, cols)) * 2.0 ** -12 + 2.0 ** -23 * float(w64.norm())
+            keep = np.ones(p0.shape[1], dtype=bool)
+            keep[mine] = False
+            assert np.array_equal(p1[i][keep], p0[i][keep]) and np.array_equal(v1[i][keep], v0[i][keep])
+        losses = []
+        for e in (eng, other):
+            if e is other:
+                for i in range(m):
+                    e.set_state(i, p1[i], v1[i])
+            out = torch.zeros(2, m, device="cuda")
+            e.local_steps(2, offs[2 * turn:2 * turn + 2], out)
+            e.sync()
+            losses.append(out.cpu().numpy())
+        assert np.array_equal(losses[0], losses[1])
+        for a, c in zip(eng.get_all(), other.get_all()):
+            assert np.array_equal(a, c)
+        for i in range(m):
+            r0 = int(offs[2 * turn, i])
+            want, grad = orc.loss_and_grad(spec, p1[i], X[r0:r0 + B], y[r0:r0 + B])
+            assert abs(losses[0][0, i] - want) <= (2e-2 if bf else 1e-5) * want
+            if not bf:
+                step = p1[i] - f32(0.05) * (f32(0.9) * v1[i].astype(np.float64) + grad)
+                r1 = int(offs[2 * turn + 1, i])
+                want = orc.batch_loss(spec, step.astype(np.float32), X[r1:r1 + B], y[r1:r1 + B])
+                assert abs(losses[0][1, i] - want) <= 1e-4 * want
+        eng.average()
+    eng.sync()
+    with pytest.raises(ValueError):
+        eng.muon_step(len(dims) - 1, g, lr=lr)
+    with pytest.raises(ValueError):
+        eng.muon_step(layer, g[:, :-1], lr=lr)
+    eng.close()
+    other.close()

@@ -130,3 +130,8 @@ def test_binding_refuses_tensors_that_are_not_on_a_gpu():
                  lambda: b.orthogonalize(x), lambda: b.muon_step(x, x, x, 0.1)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_muon_step_of_a_layer_needs_a_handle():
+    lib = b._lib()
+    assert lib.ls_muon_step_layer(None, 0, P, 64, 0, 0.1, 0.9, 1, 5, P, 1 << 40) == b.LS_ERR_BAD_HANDLE
