@@ -438,7 +438,8 @@ class _Op:
             t.record_stream(self.stream)
         start = t.data_ptr()
         base = (start + 255) & -256
-        return base, start + t.numel() - base, t
+        # (a view that ends before the first 256-byte boundary holds nothing)
+        return base, max(0, start + t.numel() - base), t
 
     def call(self, name: str, *args):
         fn = getattr(_LIB or _lib(), name)

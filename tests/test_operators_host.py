@@ -135,3 +135,33 @@ def test_binding_refuses_tensors_that_are_not_on_a_gpu():
 def test_muon_step_of_a_layer_needs_a_handle():
     lib = b._lib()
     assert lib.ls_muon_step_layer(None, 0, P, 64, 0, 0.1, 0.9, 1, 5, P, 1 << 40) == b.LS_ERR_BAD_HANDLE
+
+
+class _FakeDeviceBytes:
+    """What the wrapper looks at of a uint8 tensor on a GPU."""
+    is_cuda = True
+
+    def __init__(self, torch, device, start, numel):
+        self.dtype, self.device, self._start, self._numel = torch.uint8, device, start, numel
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self._start
+
+    def numel(self):
+        return self._numel
+
+
+@pytest.mark.parametrize("start,numel,want", [(P, 4096, (P, 4096)), (P + 1, 4096, (P + 256, 4096 - 255)), (P + 255, 1, (P + 256, 0)),
+                                              (P + 1, 255, (P + 256, 0)), (P + 1, 254, None), (P + 1, 100, None), (P + 200, 3, None)])
+def test_workspace_that_ends_before_its_first_aligned_byte(start, numel, want):
+    """A view that holds no 256-byte boundary has no usable byte; its size must not wrap round to a huge one."""
+    import torch
+    op = object.__new__(b._Op)
+    op.torch, op.device, op.stream, op.raw = torch, torch.device("cpu"), None, 0
+    base, nbytes, _ = op.workspace(None, _FakeDeviceBytes(torch, op.device, start, numel), 64)
+    assert base % 256 == 0
+    assert (base, nbytes) == (want if want is not None else (P + 256, 0))
+    assert b._lib().ls_orthogonalize(P, 1, 8, 8, 64, 0, 5, P, 64, base, nbytes, None) == WS      # needs more than 4096
