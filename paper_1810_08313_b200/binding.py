@@ -457,8 +457,17 @@ def _like(t, lead, out):
     return out if t.dim() == lead else out.squeeze(0)
 
 
+def _int32(v: int, code: int, name: str) -> int:
+    """v as the C int that the library takes; ctypes would keep its low 32 bits."""
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise LsError(code, name)
+    return v
+
+
 @functools.lru_cache(maxsize=256)
 def _ws_bytes(name: str, *args) -> int:
+    for v in args:                       # (no operator takes a size beyond 2^31 - 1, whatever the type of its argument)
+        _int32(v, LS_ERR_TOO_LARGE, name)
     n = C.c_size_t()
     _check(getattr(_lib(), name)(*args, C.byref(n)), name)
     return n.value
@@ -482,6 +491,8 @@ def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None, mean=None, rst
         raise ValueError("x must be [m][rows][d] or [rows][d]")
     rows, d = x.shape[-2:]
     xp, m, xs = op.stack(x, "x", (rows, d), None)
+    if d >= 2 ** 31 or m >= 2 ** 31:
+        raise LsError(LS_ERR_TOO_LARGE, "ls_layer_norm")
     f32 = op.torch.float32
     wp, _, ws = op.stack(weight, "weight", (d,), m, f32)
     bp = None
@@ -606,7 +617,7 @@ def orthogonalize(u, steps: int = 5, out=None, workspace=None, stream=None):
     up, m, us = op.stack(u, "u", (rows, cols), None)
     o, outp, outs = op.out(out, u, "out", (m, rows, cols), u.dtype)
     base, nbytes, keep = op.workspace(u, workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
-    op.call("ls_orthogonalize", up, m, rows, cols, us, dt, int(steps), outp, outs, base, nbytes)
+    op.call("ls_orthogonalize", up, m, rows, cols, us, dt, _int32(int(steps), LS_ERR_INVALID_ARG, "steps"), outp, outs, base, nbytes)
     return o if out is not None else _like(u, 3, o)
 
 
@@ -626,7 +637,7 @@ def muon_step(w, v, g, lr: float, momentum: float = 0.95, nesterov: bool = True,
     gp, _, gs = op.stack(g, "g", (rows, cols), m)
     base, nbytes, keep = op.workspace(w, workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
     op.call("ls_muon_step", wp, vp, gp, m, rows, cols, ws, vs, gs, dt, float(lr), float(momentum), int(bool(nesterov)),
-            int(steps), base, nbytes)
+            _int32(int(steps), LS_ERR_INVALID_ARG, "steps"), base, nbytes)
 
 
 class LocalSGD:
@@ -747,7 +758,8 @@ class LocalSGD:
         base, nbytes, keep = op.workspace(g, workspace, _ws_bytes("ls_orthogonalize_ws_bytes", self.m, rows, cols))
         with self._torch.cuda.device(self.device):
             _check(self.lib.ls_muon_step_layer(self.h, int(layer), gp, gs, dt, float(lr), float(momentum),
-                                               int(bool(nesterov)), int(steps), base, nbytes), "ls_muon_step_layer")
+                                               int(bool(nesterov)), _int32(int(steps), LS_ERR_INVALID_ARG, "steps"), base,
+                                               nbytes), "ls_muon_step_layer")
 
     # -- data ---------------------------------------------------------------
     def bind_dataset(self, x, y):

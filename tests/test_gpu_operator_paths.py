@@ -99,3 +99,27 @@ def test_muon_step_of_a_handles_layer(dims, dtype, B, layer, gdtype):
         eng.muon_step(layer, g[:, :-1], lr=lr)
     eng.close()
     other.close()
+
+
+# ---- sizes beyond a C int ------------------------------------------------------------------------------------------
+
+def test_sizes_beyond_32_bits_are_refused():
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    big = 2 ** 32 + 8
+    wide = torch.empty(big, device="cuda", dtype=torch.bfloat16)
+    w = torch.ones(8, device="cuda")
+    for call in (lambda: b.layer_norm(wide.view(1, big), w), lambda: b.layer_norm(wide.view(big, 1, 1), w),
+                 lambda: b.orthogonalize(wide.view(big, 1), out=wide.view(big, 1)),
+                 lambda: b.orthogonalize(wide.view(1, big), out=wide.view(1, big))):
+        with pytest.raises(b.LsError) as e:
+            call()
+        assert e.value.code == b.LS_ERR_TOO_LARGE
+    with pytest.raises(b.LsError) as e:
+        b.orthogonalize(torch.randn(8, 8, device="cuda"), steps=2 ** 32 + 5)
+    assert e.value.code == b.LS_ERR_INVALID_ARG
+    buf = torch.empty(4096, device="cuda", dtype=torch.uint8)
+    with pytest.raises(b.LsError) as e:
+        b.orthogonalize(torch.randn(8, 8, device="cuda"), workspace=buf[1:100])
+    assert e.value.code == b.LS_ERR_STATE_SIZE
+    torch.cuda.empty_cache()

@@ -165,3 +165,19 @@ def test_workspace_that_ends_before_its_first_aligned_byte(start, numel, want):
     assert base % 256 == 0
     assert (base, nbytes) == (want if want is not None else (P + 256, 0))
     assert b._lib().ls_orthogonalize(P, 1, 8, 8, 64, 0, 5, P, 64, base, nbytes, None) == WS      # needs more than 4096
+
+
+def test_sizes_that_do_not_fit_a_c_int():
+    """Their low 32 bits name another, smaller call."""
+    big = 2 ** 32 + 8
+    for call in (lambda: b.orthogonalize_workspace(1, big, 8), lambda: b.orthogonalize_workspace(1, 8, big),
+                 lambda: b.orthogonalize_workspace(big, 8, 8), lambda: b.layer_norm_grad_workspace(1, 8, big),
+                 lambda: b.layer_norm_grad_workspace(big, 8, 8), lambda: b.vocab_loss_workspace(big, 8, 8, 8),
+                 lambda: b.vocab_loss_workspace(1, 8, 8, big), lambda: b.orthogonalize_workspace(1, 8 - 2 ** 32, 8)):
+        with pytest.raises(b.LsError) as e:
+            call()
+        assert e.value.code == BIG
+    for steps in (2 ** 32 + 5, 5 - 2 ** 32):
+        with pytest.raises(b.LsError) as e:
+            b._int32(steps, INV, "steps")
+        assert e.value.code == INV
