@@ -64,7 +64,7 @@ enum Epi {
   EPI_F32,        // fp32 C = alpha acc (reduce: C += alpha acc)
   EPI_BF16,       // bf16 C = alpha acc
   EPI_STATS,      // row statistics of exp only
-  EPI_STATS_F16,  // statistics, and C = fp16 exp(acc - slice maximum)
+  EPI_STATS_E16,  // statistics, and C = exp(acc - slice maximum) as 16-bit numbers (pack_e16)
   EPI_STATS_F32,  // statistics, and C = fp32 acc
   EPI_PIECES,     // two fp16 pieces of alpha acc + diag I (once or twice, with other factors), optionally mirrored
 };
@@ -191,6 +191,23 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<uint32_t*>(&h);
+}
+
+// Exponentials, numbers in [0, 1], in 16 bits: they need no sign and no exponent above 0, so there are six bits of exponent and
+// ten of mantissa, the precision of fp16 (half a step is 2^-11) down to 2^-62; below, the steps stay 2^-72 (the value is off by
+// 2^-63 at most), and zero is zero.  In the bits of an fp32 number that is a subtraction from the exponent and a rounding at
+// bit 13; one saturating instruction does both and keeps any other bits (the largest exponential of logits beyond 10^7, NaN)
+// inside the 16.  (fp16 itself has 11 bits down to 2^-14 only, 9.7 nats, and nothing below 2^-25.)
+constexpr int kE16Bias = 64 << 23;       // subtracted from the bits of an exponential
+constexpr float kE16Scale = 18446744073709551616.f;       // 2^64: what unpack_e16() leaves to be multiplied by
+__device__ __forceinline__ uint32_t pack_e16(float a, float b) {
+  const int x = __viaddmin_s32_relu(__float_as_int(a), 0x1000 - kE16Bias, 0x1FFFFFFF);
+  const int y = __viaddmin_s32_relu(__float_as_int(b), 0x1000 - kE16Bias, 0x1FFFFFFF);
+  return __byte_perm((uint32_t)x << 3, (uint32_t)y << 3, 0x7632);
+}
+// the two numbers of a word, divided by kE16Scale (a field of zeros then reads as a number without the implicit bit)
+__device__ __forceinline__ float2 unpack_e16(uint32_t w) {
+  return make_float2(__uint_as_float((w << 13) & 0x1FFFE000u), __uint_as_float((w >> 3) & 0x1FFFE000u));
 }
 
 template <int NP, int NT, bool F16, bool A_MN, bool B_MN, int EPI>
@@ -438,7 +455,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         box_free<NBOX>(lane);
         return b;
       };
-      if constexpr (EPI == EPI_STATS || EPI == EPI_STATS_F16 || EPI == EPI_STATS_F32) {
+      if constexpr (EPI == EPI_STATS || EPI == EPI_STATS_E16 || EPI == EPI_STATS_F32) {
         if (col0 + HALF > p.N) {                                   // the ragged end (or all) of the last slices
 #pragma unroll
           for (int j = 0; j < G; ++j)
@@ -499,7 +516,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           p.stat_sum[at] = (part[0] + part[1]) + (part[2] + part[3]);
         }
       }
-      if constexpr (EPI == EPI_STATS_F16 || EPI == EPI_BF16) {
+      if constexpr (EPI == EPI_STATS_E16 || EPI == EPI_BF16) {
         const float alpha = EPI == EPI_BF16 && p.alpha_dev != nullptr ? p.alpha * __ldg(p.alpha_dev + tl.z) : p.alpha;
         constexpr int W = ROW / 2;
 #pragma unroll
@@ -513,7 +530,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             for (int e = 0; e < 4; ++e) {
               const int i = j * W + u * 8 + e * 2;
               const float a = __uint_as_float(acc[i >> 5][i & 31]), b = __uint_as_float(acc[i >> 5][(i + 1) & 31]);
-              w[e] = EPI == EPI_BF16 ? pack_bf16(alpha * a, alpha * b) : pack_f16(a, b);
+              w[e] = EPI == EPI_BF16 ? pack_bf16(alpha * a, alpha * b) : pack_e16(a, b);
             }
             *box_piece<ROW>(box, lane, u) = make_uint4(w[0], w[1], w[2], w[3]);
           }

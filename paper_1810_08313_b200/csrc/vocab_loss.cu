@@ -8,11 +8,12 @@
 // (maximum, sum of exponentials) per slice of half a tile's columns, and a small kernel combines those.  The gradient needs the
 // normalised probabilities twice, as an operand of dh (contracted over V) and of dW (contracted over rows), and their
 // normaliser only when the last column is known.  Recomputing the logits would cost a third more flops; instead a piece
-// of rows (at most 2^29 elements of the piece's probabilities, 1 GiB) keeps exp(z - slice maximum) as fp16 numbers in
-// [0, 1], a streaming pass scales them to dz in bf16 in place (4 bytes a logit against 6 d flops), and both products
-// read them.  fp16 and not bf16 there because the number is rounded once more: 11 bits against 8, its error
-// disappears under the bf16 rounding of dz, which the tensor cores need and which is of the same size as the rounding
-// of the bf16 results.  At the label, exp(z_y - lse) - 1 is formed from the fp32 logit with expm1.  The factor
+// of rows (at most 2^29 elements of the piece's probabilities, 1 GiB) keeps exp(z - slice maximum) as 16-bit numbers,
+// a streaming pass scales them to dz in bf16 in place (4 bytes a logit against 6 d flops), and both products
+// read them.  The number is rounded once more, so it has 11 bits and not bf16's 8: its error (2^-11) disappears under the bf16
+// rounding of dz (2^-8), which the tensor cores need and which is of the same size as the rounding of the bf16 results.
+// It keeps them down to 2^-62 of the slice's maximum, 43 nats, so that an unlikely column's dz is as accurate as a likely
+// one's (pack_e16 in gemm_op.cuh).  At the label, exp(z_y - lse) - 1 is formed from the fp32 logit with expm1.  The factor
 // scale / count is applied to the fp32 accumulators: in dz it would give every uncertain row the same rounding error
 // of 1 / count, where -1 is exact.
 //
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
 }
 
 // ---- exponentials -> dz, eight columns per thread ------------------------------------------------------------------------
-// bf16: in place over the fp16 numbers.  Rows from `rows` to `pad`, which fill the last K block of dW, become zeros.
+// bf16: in place over the 16-bit exponentials.  Rows from `rows` to `pad`, which fill the last K block of dW, become zeros.
 // What the launch that forms dz does to a row of h for dW: rows without a label are cleared, so that whatever they hold stays out
 // of dW.  h itself is the caller's: where the product read it in place (src given), the other rows are copied into the
 // workspace; where it was laid out there already, they stay.
@@ -208,11 +209,11 @@ vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int pad, int V, const fl
     uint32_t w[4] = {0, 0, 0, 0};
     if (has_label(y[k], V)) {
       const uint32_t in[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-      const float f = gop::ex2(top[k] - l[k] * kLog2e);
+      const float f = gop::ex2(top[k] - l[k] * kLog2e) * gop::kE16Scale;
       float v[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&in[i]));
+        const float2 t = gop::unpack_e16(in[i]);
         v[2 * i] = t.x * f; v[2 * i + 1] = t.y * f;
       }
       const int d = y[k] - c;
@@ -900,7 +901,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     if (!p.grad) {
       LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(p.nt, mh, mw, mh, mh, g, d, st)));
     } else {
-      constexpr gop::Epi kEpi = F32 ? gop::EPI_STATS_F32 : gop::EPI_STATS_F16;
+      constexpr gop::Epi kEpi = F32 ? gop::EPI_STATS_F32 : gop::EPI_STATS_E16;
       LS_TRY(gop::make_output_map(&me, a.ws + p.o_e, F32 ? gop::MAP_F32 : gop::MAP_F16, rn, V, nb, p.Vp, p.R * p.Vp, kRow));
       LS_TRY((gop::launch<NP, false, false, false, kEpi>(p.nt, mh, mw, me, me, g, d, st)));
     }
