@@ -89,8 +89,8 @@ struct Params {
   float* stat_max;                       // slice maximum * log2(e)
   float* stat_sum;                       // sum over the slice of exp(acc - slice maximum)
   int64_t stat_ld, stat_z;               // elements between slices, between batch entries
-  const int32_t* labels;                 // [M], label_z apart; a label inside the slice gets its logit written to
-  float* label_logit;                    // label_logit[row]
+  const int32_t* labels;                 // [M], label_z apart; the label's logit is written to label_logit[row], and the slice's
+  float* label_logit;                    // numbers are those of the other columns
   int64_t label_z;
   unsigned* clear;                       // `batch` words that the launch sets to zero for the next one, or null
   // EPI_PIECES: output i (of n_out) is planes c + 2 i (first piece) and c + 2 i + 1 of the stack
@@ -463,6 +463,24 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             for (int i = 0; i < 32; ++i)
               if (col0 + j * 32 + i >= p.N) acc[j][i] = 0xff800000u;
         }
+        // A row's label stays out of its statistics: its logit leaves on its own and the combining kernel adds its term, so that
+        // 1 - p of a certain row is a sum of small numbers and not what is left of 1.
+        if (p.labels != nullptr) {
+          const int lab = row < p.M ? p.labels[tl.z * p.label_z + row] - col0 : -1;
+          const bool mine = lab >= 0 && lab < HALF && lab + col0 < p.N;
+          float zl = 0.f;
+#pragma unroll
+          for (int j = 0; j < G; ++j) {
+            if (!__any_sync(0xffffffffu, mine && lab >> 5 == j)) continue;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (lab == j * 32 + i) {
+                zl = __uint_as_float(acc[j][i]);
+                acc[j][i] = 0xff800000u;
+              }
+          }
+          if (mine) p.label_logit[tl.z * p.label_z + row] = zl;
+        }
         float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < G; ++j)
@@ -472,21 +490,8 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         // (a slice of nothing but -inf: any finite reference gives the zero terms that it has; a finite maximum's reference
         // stays finite)
         const float ref = mx == -INFINITY ? 0.f : mx < 0.f ? fmaxf(mx * kLog2e, -3.4e38f) : mx * kLog2e;
-        if (p.labels != nullptr) {
-          const int lab = row < p.M ? p.labels[tl.z * p.label_z + row] - col0 : -1;
-          const bool mine = lab >= 0 && lab < HALF && lab + col0 < p.N;
-          if (__any_sync(0xffffffffu, mine)) {
-            float zl = 0.f;
-#pragma unroll
-            for (int j = 0; j < G; ++j)
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (lab == j * 32 + i) zl = __uint_as_float(acc[j][i]);
-            if (mine) p.label_logit[tl.z * p.label_z + row] = zl;
-          }
-        }
         if constexpr (EPI == EPI_STATS_F32) {
-          // the logits themselves leave; the exponentials are only summed
+          // the logits themselves (-inf at the label) leave; the exponentials are only summed
           constexpr int W = ROW / 4;                               // columns of a box
 #pragma unroll
           for (int j = 0; j < HALF / W; ++j) {

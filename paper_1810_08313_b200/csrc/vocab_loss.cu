@@ -13,7 +13,9 @@
 // read them.  The number is rounded once more, so it has 11 bits and not bf16's 8: its error (2^-11) disappears under the bf16
 // rounding of dz (2^-8), which the tensor cores need and which is of the same size as the rounding of the bf16 results.
 // It keeps them down to 2^-62 of the slice's maximum, 43 nats, so that an unlikely column's dz is as accurate as a likely
-// one's (pack_e16 in gemm_op.cuh).  At the label, exp(z_y - lse) - 1 is formed from the fp32 logit with expm1.  The factor
+// one's (pack_e16 in gemm_op.cuh).  The label's logit is no part of any slice: with S the sum of the other columns and e_y the label's
+// term, the loss of a row with S < e_y is log1p(S / e_y) and dz at the label -S / (S + e_y), which lose nothing
+// however certain the row is (of a rounded log-sum-exp, 1 - p is right to 1e-6 only).  The factor
 // scale / count is applied to the fp32 accumulators: in dz it would give every uncertain row the same rounding error
 // of 1 / count, where -1 is exact.
 //
@@ -47,7 +49,7 @@ struct CombineArgs {
   int64_t stat_ld, stat_z;
   int slices, rows, V;
   const int32_t* labels;          // of the piece
-  const float* label_logit;
+  float* label;                   // the label's logit; replaced by dz at the label
   float *lse, *row_loss;
   float2* norm;                   // fp32 gradient: (reference of the exponentials, their sum) of the piece's rows, or null
   unsigned* done;
@@ -66,7 +68,7 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
   const int row = blockIdx.x * 32 + lane;
   const int64_t z = blockIdx.y;
   a.stat_max += z * a.stat_z; a.stat_sum += z * a.stat_z;
-  a.labels += z * a.all_rows; a.label_logit += z * a.all_rows; a.lse += z * a.all_rows; a.row_loss += z * a.all_rows;
+  a.labels += z * a.all_rows; a.label += z * a.all_rows; a.lse += z * a.all_rows; a.row_loss += z * a.all_rows;
   a.all_labels += z * a.all_rows; a.all_row_loss += z * a.all_rows;
   a.done += z;
   if (a.norm != nullptr) a.norm += z * a.all_rows;
@@ -74,6 +76,9 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
   if (a.loss != nullptr) a.loss += z;
   grid_dep_wait();
   grid_dep_launch();
+  int y = -1;
+  float zy = 0.f;
+  if (wp == 0 && row < a.rows) { y = a.labels[row]; zy = __ldcg(a.label + row); }       // (zy: whatever is there without a label)
   // eight slices at a time, their sixteen loads in flight together
   float m = -INFINITY, s = 0.f;
   if (row < a.rows) {
@@ -108,15 +113,25 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
       const float tm = smax[i][lane];
       S += tm == -INFINITY ? ssum[i][lane] : ssum[i][lane] * gop::ex2(tm - M);
     }
-    // S is a sum of 2^(z kLog2e - M), so that log-sum-exp and row loss are differences in that base, formed in double: rounded,
-    // a log-sum-exp of 20 is off by 1e-6, and so would be the loss, however small it is
-    const float ref = M == -INFINITY ? 0.f : M;
-    const double log_sum = (double)logf(S) * (1.0 / (double)kLn2);
+    // the label's term, with the larger reference of the two (a NaN stays out of the reference and enters the sum)
+    const bool labelled = has_label(y, a.V);
+    const float ry = !labelled ? -INFINITY : zy < 0.f && zy != -INFINITY ? fmaxf(zy * kLog2e, -3.4e38f) : zy * kLog2e;
+    const float top = fmaxf(M, ry);
+    const float ref = top == -INFINITY ? 0.f : top;
+    if (M != -INFINITY) S *= gop::ex2(M - ref);
+    const float ey = labelled ? gop::ex2(fmaf(zy, kLog2e, -ref)) : 0.f;
+    const float T = S + ey;
+    // T is a sum of 2^(z kLog2e - ref), so that log-sum-exp and row loss are differences in that base, formed in double: rounded,
+    // a log-sum-exp of 20 is off by 1e-6, and so would be the loss
+    const double log_sum = (double)logf(T) * (1.0 / (double)kLn2);
     a.lse[row] = (float)(((double)ref + log_sum) / (double)kLog2e);
-    if (a.norm != nullptr) a.norm[row] = make_float2(ref, S);
-    const bool labelled = has_label(a.labels[row], a.V);
-    a.row_loss[row] =
-        labelled ? (float)((fma(-(double)a.label_logit[row], (double)kLog2e, (double)ref) + log_sum) / (double)kLog2e) : 0.f;
+    if (a.norm != nullptr) a.norm[row] = make_float2(ref, T);
+    float loss = 0.f;
+    if (labelled) {
+      loss = S < ey ? log1pf(S / ey) : (float)((fma(-(double)zy, (double)kLog2e, (double)ref) + log_sum) / (double)kLog2e);
+      a.label[row] = -(S / T);
+    }
+    a.row_loss[row] = loss;
   }
   if (a.inv_count == nullptr && a.loss == nullptr) return;
   __threadfence();
@@ -177,11 +192,11 @@ constexpr int kDzCols = 2048, kDzRows = 4;
 struct DzStep { int64_t e, out, stat, rows; };          // elements between replicas (blockIdx.z)
 __global__ void __launch_bounds__(256)
 vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int pad, int V, const float* stat_max, int64_t stat_ld, int slice,
-                     const int32_t* labels, const float* label_logit, const float* lse, const HRows h, const DzStep by) {
+                     const int32_t* labels, const float* label_dz, const float* lse, const HRows h, const DzStep by) {
   const int row0 = blockIdx.y * kDzRows;
   const int c = blockIdx.x * kDzCols + threadIdx.x * 8;
   const int64_t z = blockIdx.z;
-  e += z * by.e; stat_max += z * by.stat; labels += z * by.rows; label_logit += z * by.rows; lse += z * by.rows;
+  e += z * by.e; stat_max += z * by.stat; labels += z * by.rows; label_dz += z * by.rows; lse += z * by.rows;
   grid_dep_wait();
   grid_dep_launch();
   int y[kDzRows];
@@ -218,7 +233,7 @@ vocab_dz_bf16_kernel(uint16_t* e, int64_t ld, int rows, int pad, int V, const fl
       }
       const int d = y[k] - c;
       if (d >= 0 && d < 8) {
-        const float py = expm1f(label_logit[row0 + k] - l[k]);
+        const float py = label_dz[row0 + k];
 #pragma unroll
         for (int i = 0; i < 8; ++i) if (i == d) v[i] = py;
       }
@@ -242,20 +257,19 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
 // dz of an fp32 logit: exp(z - lse) as 2^(z log2(e) - M) / S with the reference M that the sum S was formed with.  lse itself, rounded
 // at its size, would put an error of 1e-6 at a log-sum-exp of 20 into every number of the row.
 struct Norm {
-  float ref, inv, log_sum;
-  __device__ __forceinline__ explicit Norm(float2 n) : ref(n.x), inv(1.f / n.y), log_sum(logf(n.y)) {}
+  float ref, inv;
+  __device__ __forceinline__ explicit Norm(float2 n) : ref(n.x), inv(1.f / n.y) {}
   __device__ __forceinline__ float p(float z) const { return exp2f(fmaf(z, kLog2e, -ref)) * inv; }
-  __device__ __forceinline__ float p_minus_1(float z) const { return expm1f(fmaf(fmaf(z, kLog2e, -ref), kLn2, -log_sum)); }
 };
 
 // fp32: logits z -> three pieces of dz.
 __global__ void __launch_bounds__(256)
 vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t piece, int rows, int V, const int32_t* labels,
-                     const float* label_logit, const float2* norm, const HRows h, const DzStep by) {
+                     const float* label_dz, const float2* norm, const HRows h, const DzStep by) {
   const int row = blockIdx.y;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   const int64_t rep = blockIdx.z;
-  z += rep * by.e; out += rep * by.out; labels += rep * by.rows; label_logit += rep * by.rows; norm += rep * by.rows;
+  z += rep * by.e; out += rep * by.out; labels += rep * by.rows; label_dz += rep * by.rows; norm += rep * by.rows;
   grid_dep_wait();
   grid_dep_launch();
   const int y = row < rows ? labels[row] : -1;
@@ -269,7 +283,7 @@ vocab_dz_fp32_kernel(const float* z, __nv_bfloat16* out, int64_t ld, int64_t pie
     v[0] = n.p(u.x); v[1] = n.p(u.y); v[2] = n.p(u.z); v[3] = n.p(u.w);
     const int d = y - c;
     if (d >= 0 && d < 4) {
-      const float py = n.p_minus_1(label_logit[row]);
+      const float py = label_dz[row];
 #pragma unroll
       for (int i = 0; i < 4; ++i) if (i == d) v[i] = py;
     }
@@ -513,7 +527,10 @@ __global__ void __launch_bounds__(128) vocab_few_logits_kernel(const FewArgs a) 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (c + i >= a.V) v[i] = -INFINITY;
-      else if (lab == i) a.label_logit[z * a.rows + row] = v[i];
+      else if (lab == i) {                                        // no part of the statistics: EPI_STATS
+        a.label_logit[z * a.rows + row] = v[i];
+        v[i] = -INFINITY;
+      }
       mx = fmaxf(mx, v[i]);
     }
 #pragma unroll
@@ -537,7 +554,7 @@ __global__ void __launch_bounds__(128) vocab_few_logits_kernel(const FewArgs a) 
 
 // z -> dz in place, four columns a thread
 __global__ void __launch_bounds__(256)
-vocab_few_dz_kernel(float* zz, int64_t ld, int rows, int V, const int32_t* labels, const float* label_logit, const float2* norm) {
+vocab_few_dz_kernel(float* zz, int64_t ld, int rows, int V, const int32_t* labels, const float* label_dz, const float2* norm) {
   const int64_t at_row = (int64_t)blockIdx.z * rows + blockIdx.y;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   grid_dep_wait();
@@ -552,7 +569,7 @@ vocab_few_dz_kernel(float* zz, int64_t ld, int rows, int V, const int32_t* label
     o = make_float4(n.p(u.x), n.p(u.y), n.p(u.z), n.p(u.w));
     const int d = y - c;
     if (d >= 0 && d < 4) {
-      const float py = n.p_minus_1(label_logit[at_row]);
+      const float py = label_dz[at_row];
       if (d == 0) o.x = py;
       else if (d == 1) o.y = py;
       else if (d == 2) o.z = py;
@@ -908,7 +925,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     CombineArgs cb{};
     cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices;
     cb.rows = (int)rn; cb.V = (int)V;
-    cb.labels = labels + r0; cb.label_logit = logit + r0; cb.lse = lse + r0; cb.row_loss = row_loss + r0;
+    cb.labels = labels + r0; cb.label = logit + r0; cb.lse = lse + r0; cb.row_loss = row_loss + r0;
     cb.done = done; cb.all_labels = labels; cb.all_row_loss = row_loss; cb.all_rows = a.rows;
     cb.norm = F32 && p.grad ? norm : nullptr;
     if (p.grad && piece == 0) cb.inv_count = inv;
@@ -1019,7 +1036,7 @@ int run_few(const VocabArgs& a, const Plan& p, cudaStream_t st) {
   }
   CombineArgs cb{};
   cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices;
-  cb.rows = rows; cb.V = V; cb.labels = cb.all_labels = a.labels; cb.label_logit = logit;
+  cb.rows = rows; cb.V = V; cb.labels = cb.all_labels = a.labels; cb.label = logit;
   cb.lse = a.lse ? a.lse : reinterpret_cast<float*>(a.ws + p.o_lse);
   cb.row_loss = a.row_loss ? a.row_loss : reinterpret_cast<float*>(a.ws + p.o_rowloss);
   cb.all_row_loss = cb.row_loss; cb.all_rows = a.rows; cb.done = done; cb.loss = a.loss;

@@ -51,3 +51,57 @@ def test_gradient_of_unlikely_columns(rows, V, d, dtype):
     err = (got - dz).abs()
     assert bool((err <= tol).all()), float((err / tol).max())
     assert float(got[:, V - 1].abs().min()) > 0.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,V,d", [(1, 100, 64), (4, 700, 64), (8, 100, 64), (12, 700, 72), (40, 128, 65), (60, 3001, 64)])
+def test_certain_rows(rows, V, d, dtype):
+    """Labels 8 to 25 above every other logit, which are within 3 of one another: loss, dz at the label and dh are sums of the other
+    columns' small terms and keep their relative accuracy.  Terms and their sums: below 2^-16 (the argument, up to 41, is rounded
+    once, the constant is off by 2^-25 of it, the exponential by 2^-22).  bf16: roundings as in
+    test_gradient_of_unlikely_columns; dh adds them up."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    g = torch.Generator(device="cuda").manual_seed(rows + V + 1)
+    margin = (32 + (torch.arange(rows, device="cuda") * 68) // max(1, rows - 1)).double()[:, None] / 4
+    z = -margin - _quarters(g, 0, 3, rows, V)
+    labels = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    z.scatter_(1, labels[:, None], 0.0)
+    z += _quarters(g, 0, 16, rows, 1)                              # log-sum-exps away from zero
+    h, W, y, dz, others, total = _case(z, labels, dtype, d)
+    want = torch.log1p(others / (total - others))
+    for out in (b.vocab_loss(h, W, y), b.vocab_loss_grad(h, W, y, scale=float(rows))):
+        assert bool(((out[1][0].double() - want).abs() <= 2.0 ** -16 * want).all()), (out[1][0], want)
+        assert abs(float(out[0]) - float(want.mean())) <= 2.0 ** -15 * float(want.mean())
+    one = 2.0 ** -11 + 2.0 ** -8 + 2.0 ** -14 if dtype == "bf16" else 2.0 ** -15
+    end = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -22
+    got = out[4][0, :, :rows].T.double()
+    assert bool(((got - dz).abs() <= (one * 1.01 + end) * dz.abs()).all()), float(((got - dz) / dz).abs().max())
+    w64 = W[0].double()
+    ref, size = dz @ w64, dz.abs() @ w64.abs()
+    assert bool(((out[3][0].double() - ref).abs() <= (one + 2.0 ** -14) * size + end * ref.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [3, 20])
+def test_labels_of_infinite_logits(rows, dtype):
+    """A label with a logit of -inf has an infinite loss and dz -1; beside columns of -inf a label alone has loss 0.  (fp32 counts
+    infinities as 3.39e38.)"""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    dt = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    h = torch.ones(1, rows, 64, device="cuda", dtype=dt)
+    h[..., 1:] = 0.0
+    W = torch.zeros(1, 300, 64, device="cuda", dtype=dt)
+    W[0, 7, 0] = float("-inf")
+    y = torch.full((1, rows), 7, device="cuda", dtype=torch.int32)
+    y[0, 0] = 9
+    loss, rl, lse, _, _ = b.vocab_loss_grad(h, W, y)
+    assert bool((rl[0, 1:] > 3e38).all()) and abs(float(rl[0, 0]) - 5.7004436) < 1e-5       # log 299
+    assert bool(((lse - 5.7004436).abs() < 1e-5).all())
+    W[0, :, 0] = float("-inf")
+    W[0, 9, 0] = 2.0
+    y.fill_(9)
+    loss, rl, lse, _, dW = b.vocab_loss_grad(h, W, y)
+    assert float(loss) == 0.0 and float(rl.abs().max()) == 0.0 and bool((lse == 2.0).all())
+    assert float(dW[0, 9].abs().max()) == 0.0
