@@ -421,6 +421,9 @@ int ls_linear_loss_static(const float* W_dev, const float* bias_dev, const float
 /* Waits for cuda_stream, then returns LS_ERR_DEVICE_TIMEOUT once (and clears the record) if a wait of one of these operators ran
  * out on the current device since the last call, else LS_OK. */
 int ls_device_status(void* cuda_stream);
+/* Housekeeping: ls_selftest_wait_timeout() for this report path.  The kernel records its failure like an operator on the
+ * current device would: the next ls_device_status() returns LS_ERR_DEVICE_TIMEOUT, the one after it LS_OK. */
+int ls_selftest_device_timeout(int64_t limit_cycles, void* cuda_stream);
 
 /* Layer norm of every row of x [m][rows][d]:  y = (x - mean) * rstd * weight + bias,  rstd = 1 / sqrt(var + eps), var the
  * mean square of x - mean.  weight, bias (may be NULL): float [m][d], param_stride apart.  y like x.  mean, rstd

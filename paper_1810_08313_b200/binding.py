@@ -119,6 +119,7 @@ def _lib():
         "ls_get_lr": (C.c_int, [vp, P(f32)]),
         "ls_linear_loss_static": (C.c_int, [vp, vp, vp, vp, i64, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp]),
         "ls_device_status": (C.c_int, [vp]),
+        "ls_selftest_device_timeout": (C.c_int, [i64, vp]),
         "ls_layer_norm": (C.c_int, [vp, vp, vp, C.c_int, i64, C.c_int, i64, i64, C.c_int, f32, vp, i64, vp, vp, vp]),
         "ls_layer_norm_grad_ws_bytes": (C.c_int, [C.c_int, i64, C.c_int, P(C.c_size_t)]),
         "ls_layer_norm_grad": (C.c_int, [vp, vp, vp, vp, vp, C.c_int, i64, C.c_int, i64, i64, i64, C.c_int, vp, i64, vp, vp,
@@ -480,6 +481,15 @@ def device_status(stream=None) -> None:
     s = stream if stream is not None else torch.cuda.current_stream()
     with torch.cuda.device(s.device):
         _check(_lib().ls_device_status(int(s.cuda_stream)), "ls_device_status")
+
+
+def selftest_device_timeout(limit_cycles: int = 2_000_000, stream=None) -> None:
+    """Enqueue the kernel whose bounded wait runs out (ls_selftest_device_timeout); the next device_status() of that device
+    raises LsError(LS_ERR_DEVICE_TIMEOUT)."""
+    import torch
+    s = stream if stream is not None else torch.cuda.current_stream()
+    with torch.cuda.device(s.device):
+        _check(_lib().ls_selftest_device_timeout(int(limit_cycles), int(s.cuda_stream)), "ls_selftest_device_timeout")
 
 
 def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None, mean=None, rstd=None, stream=None):

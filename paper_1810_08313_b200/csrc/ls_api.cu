@@ -1212,6 +1212,14 @@ int ls_selftest_wait_timeout(ls_handle* h, int64_t limit_cycles) {
   return LS_OK;
 }
 
+int ls_selftest_device_timeout(int64_t limit_cycles, void* cuda_stream) {
+  if (limit_cycles < 1 || limit_cycles > 2000000000ll) return LS_ERR_INVALID_ARG;
+  int* word = gop::device_error_word();
+  if (word == nullptr) return LS_ERR_CUDA;
+  wait_timeout_selftest_kernel<<<1, 32, 0, static_cast<cudaStream_t>(cuda_stream)>>>(word, (long long)limit_cycles);
+  return cudaGetLastError() == cudaSuccess ? LS_OK : LS_ERR_CUDA;
+}
+
 int ls_get_lr(const ls_handle* h, float* lr) {
   if (!ok_handle(h)) return LS_ERR_BAD_HANDLE;
   if (lr == nullptr) return LS_ERR_INVALID_ARG;

@@ -387,6 +387,7 @@ int launch_to_bf16(const float* src, __nv_bfloat16* dst, int m, int64_t stride, 
                    int64_t* launches);
 // one matrix between row-major and blocked order (to_blocked: dst blocked <- src row-major, else the reverse)
 int launch_retile(float* dst, const float* src, int rows, int cols, bool to_blocked, cudaStream_t st, int64_t* launches);
+namespace gop { int* device_error_word(); }       // see gemm_op.cuh
 // ls_muon_step with w and v row-major or (blocked) in 32 x 32 blocks, see TileMap (orthogonalize.cu)
 int muon_step(float* w_dev, float* v_dev, const void* g_dev, int m, int rows, int cols, int64_t w_stride, int64_t v_stride,
               int64_t g_stride, int g_dtype, float lr, float momentum, int nesterov, int steps, bool blocked, void* ws_dev,

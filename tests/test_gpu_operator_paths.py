@@ -123,3 +123,51 @@ def test_sizes_beyond_32_bits_are_refused():
         b.orthogonalize(torch.randn(8, 8, device="cuda"), workspace=buf[1:100])
     assert e.value.code == b.LS_ERR_STATE_SIZE
     torch.cuda.empty_cache()
+
+
+# ---- a wait that runs out ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("side", [False, True])
+def test_wait_that_runs_out_is_reported_once_and_operators_go_on(side):
+    """A kernel of one thread waits about a millisecond on a barrier on which nothing arrives and records it, as an operator
+    would.  device_status() raises once; results before and after are the same bits, and a handle's own record stays clear."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(2, 90, 72, generator=g, device="cuda")
+    w = torch.ones(2, 72, device="cuda")
+    W = torch.randn(2, 200, 72, generator=g, device="cuda") / 8
+    y = torch.randint(0, 200, (2, 90), generator=g, device="cuda").int()
+
+    def run():
+        n, mean, rstd = b.layer_norm(x, w)
+        out = b.vocab_loss_grad(n, W, y)
+        return (n, mean, rstd) + out + b.layer_norm_grad(out[3], x, w, mean, rstd) + (b.orthogonalize(out[4]),)
+
+    ref = [t.clone() for t in run()]
+    stream = torch.cuda.Stream() if side else None
+    b.device_status(stream)
+    eng = b.LocalSGD(2, (24, 16, 10), lr=0.1, momentum=0.9, batch=8)
+    b.selftest_device_timeout(2_000_000, stream)
+    with pytest.raises(b.LsError) as e:
+        b.device_status(stream)
+    assert e.value.code == b.LS_ERR_DEVICE_TIMEOUT
+    b.device_status(stream)
+    b.device_status()
+    eng.sync()
+    # not asked for: calls go on, the record waits
+    b.selftest_device_timeout(2_000_000, stream)
+    got = run()
+    torch.cuda.synchronize()
+    with pytest.raises(b.LsError):
+        b.device_status()
+    b.device_status()
+    for t, r in zip(got, ref):
+        assert torch.equal(t, r)
+    # the handle's record is another one
+    eng.selftest_wait_timeout(2_000_000)
+    torch.cuda.synchronize()
+    b.device_status()
+    with pytest.raises(b.LsError):
+        eng.sync()
+    eng.close()

@@ -181,3 +181,8 @@ def test_sizes_that_do_not_fit_a_c_int():
         with pytest.raises(b.LsError) as e:
             b._int32(steps, INV, "steps")
         assert e.value.code == INV
+
+
+def test_selftest_of_the_report_path_refuses_limits():
+    for limit in (0, -1, 2 * 10 ** 9 + 1):
+        assert b._lib().ls_selftest_device_timeout(limit, None) == INV
