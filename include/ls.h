@@ -453,7 +453,7 @@ int ls_layer_norm_grad(const void* dy_dev, const void* x_dev, const float* weigh
  * Workspace of the loss: two numbers a row and slice of 64 or 128 columns (and a copy of both operands for fp32 or d not
  * a multiple of 8).  Of the gradient: also the probabilities of a piece of rows, at most about 1 GiB but at least 256
  * rows, h of that piece, and the fp32 sum of dW for bf16 when the rows take several pieces.  Where all of that stays below
- * 512 MB for all replicas, they are taken together. */
+ * 512 MB for all replicas, they are taken together.  A workspace of the gradient's size serves the loss of the same sizes, too. */
 int ls_vocab_loss_ws_bytes(int m, int64_t rows, int64_t vocab, int d, int dtype, int grad, size_t* bytes);
 int ls_vocab_loss(const void* h_dev, const void* W_dev, const int32_t* labels_dev, int m, int64_t rows, int64_t vocab,
                   int d, int64_t h_stride, int64_t w_stride, int dtype, float* loss_dev, float* row_loss_dev,

@@ -1118,7 +1118,9 @@ extern "C" int ls_vocab_loss_ws_bytes(int m, int64_t rows, int64_t vocab, int d,
   int rc = check_sizes(m, rows, vocab, d, dtype);
   if (rc != LS_OK) return rc;
   if (bytes == nullptr) return LS_ERR_INVALID_ARG;
-  *bytes = make_plan(m, rows, vocab, d, dtype, grad != 0).total;
+  // (few rows take less for a gradient than for a loss, which then runs on other kernels: the gradient's size serves both)
+  const size_t loss = make_plan(m, rows, vocab, d, dtype, false).total, both = grad != 0 ? make_plan(m, rows, vocab, d, dtype, true).total : 0;
+  *bytes = loss > both ? loss : both;
   return LS_OK;
 }
 

@@ -171,3 +171,55 @@ def test_wait_that_runs_out_is_reported_once_and_operators_go_on(side):
     with pytest.raises(b.LsError):
         eng.sync()
     eng.close()
+
+
+# ---- cross entropy: replicas one after another, pieces of rows, strides, outputs left out ---------------------------
+
+def _vocab(m, rows, d, V, dtype, seed):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    h = torch.randn(m, rows, d, generator=g, device="cuda").to(dt)
+    W = (torch.randn(m, V, d, generator=g, device="cuda") / math.sqrt(d)).to(dt)
+    y = torch.randint(0, V, (m, rows), generator=g, device="cuda")
+    y[torch.rand((m, rows), generator=g, device="cuda") < 0.1] = -1
+    return h, W, y.int()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [3, 12, 70])
+def test_row_outputs_left_out(rows, dtype):
+    """row_loss, lse, mean, rstd and dbias may be null at the C entry: the rest keeps its bits."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    lib = b._lib()
+    m, d, V = 2, 72, 301
+    code = {"fp32": 0, "bf16": 1}[dtype]
+    h, W, y = _vocab(m, rows, d, V, dtype, seed=rows)
+    ref, plain = b.vocab_loss_grad(h, W, y), b.vocab_loss(h, W, y)
+    st = torch.cuda.current_stream().cuda_stream
+    ws = torch.empty(b.vocab_loss_workspace(m, rows, V, d, dtype, True), device="cuda", dtype=torch.uint8)
+    base = (ws.data_ptr() + 255) // 256 * 256
+    nb = ws.numel() - 256
+    loss, dh, dW = torch.full((m,), 9.0, device="cuda"), torch.empty_like(h), torch.empty_like(W)
+    assert lib.ls_vocab_loss_grad(h.data_ptr(), W.data_ptr(), y.data_ptr(), m, rows, V, d, rows * d, V * d, code, 1.0,
+                                  loss.data_ptr(), None, None, dh.data_ptr(), rows * d, dW.data_ptr(), V * d, base, nb, st) == b.LS_OK
+    assert torch.equal(loss, ref[0]) and torch.equal(dh, ref[3]) and torch.equal(dW, ref[4])
+    loss.fill_(9.0)
+    assert lib.ls_vocab_loss(h.data_ptr(), W.data_ptr(), y.data_ptr(), m, rows, V, d, rows * d, V * d, code, loss.data_ptr(), None,
+                             None, base, nb, st) == b.LS_OK
+    assert torch.equal(loss, plain[0])
+    w = torch.ones(m, d, device="cuda")
+    yy, mean, rstd = b.layer_norm(h, w)
+    out = torch.empty_like(h)
+    assert lib.ls_layer_norm(h.data_ptr(), w.data_ptr(), None, m, rows, d, rows * d, d, code, 1e-5, out.data_ptr(), rows * d, None,
+                             None, st) == b.LS_OK
+    assert torch.equal(out, yy)
+    dx, dw, _ = b.layer_norm_grad(yy, h, w, mean, rstd)
+    dx2, dw2 = torch.empty_like(h), torch.empty_like(w)
+    ws = torch.empty(b.layer_norm_grad_workspace(m, rows, d), device="cuda", dtype=torch.uint8)
+    base = (ws.data_ptr() + 255) // 256 * 256
+    assert lib.ls_layer_norm_grad(yy.data_ptr(), h.data_ptr(), w.data_ptr(), mean.data_ptr(), rstd.data_ptr(), m, rows, d, rows * d,
+                                  rows * d, d, code, dx2.data_ptr(), rows * d, dw2.data_ptr(), None, d, base, ws.numel() - 256,
+                                  st) == b.LS_OK
+    assert torch.equal(dx2, dx) and torch.equal(dw2, dw)

@@ -186,3 +186,13 @@ def test_sizes_that_do_not_fit_a_c_int():
 def test_selftest_of_the_report_path_refuses_limits():
     for limit in (0, -1, 2 * 10 ** 9 + 1):
         assert b._lib().ls_selftest_device_timeout(limit, None) == INV
+
+
+def test_workspace_of_a_gradient_serves_the_loss():
+    for m in (1, 2, 7):
+        for rows in (0, 1, 3, 4, 5, 16, 17, 32, 33, 64, 300, 5000, 70000):
+            for V in (1, 100, 301, 32000, 131072, 1 << 23):
+                for d in (1, 8, 72, 77, 4096):
+                    for dt in (0, 1):
+                        loss, grad = (_bytes("ls_vocab_loss_ws_bytes", m, rows, V, d, dt, g) for g in (0, 1))
+                        assert loss[0] == grad[0] == OK and grad[1] >= loss[1], (m, rows, V, d, dt)
