@@ -186,6 +186,125 @@ def _vocab(m, rows, d, V, dtype, seed):
     return h, W, y.int()
 
 
+@pytest.mark.parametrize("dtype,m,rows,d,V", [
+    ("bf16", 2, 2300, 64, 65536),          # one piece a replica, together beyond 512 MB: one replica after another
+    ("bf16", 3, 1500, 65, 65536),          # ... with operands laid out anew
+    ("fp32", 2, 600, 24, 65536),
+    ("bf16", 2, 4400, 32, 131072),         # two pieces a replica
+    ("fp32", 2, 1100, 13, 131072),
+])
+def test_replicas_one_after_another(dtype, m, rows, d, V):
+    """Each replica is the bits of a call of its own: the statistics, counters and operand copies of one are not seen by the next.
+    The losses also without a gradient."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    h, W, y = _vocab(m, rows, d, V, dtype, seed=rows)
+    y[1, -7:] = -1
+    out = b.vocab_loss_grad(h, W, y, scale=1.5)
+    for i in range(m):
+        one = b.vocab_loss_grad(h[i], W[i], y[i], scale=1.5)
+        for got, want in zip(out, one):
+            assert torch.equal(got[i], want.view_as(got[i]))
+    plain = b.vocab_loss(h, W, y)
+    for i in range(m):
+        for got, want in zip(plain, b.vocab_loss(h[i], W[i], y[i])):
+            assert torch.equal(got[i], want.view_as(got[i]))
+        keep = y[i] >= 0
+        want = out[1][i].double().sum() / int(keep.sum())
+        assert abs(float(out[0][i]) - float(want)) <= 2.0 ** -23 * abs(float(want))
+        assert bool((out[1][i][~keep] == 0).all()) and float(out[3][i][~keep].abs().max()) == 0.0
+    b.device_status()
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,d,V", [("bf16", 64, 131072), ("fp32", 16, 131072), ("bf16", 65, 131072)])
+def test_dh_of_every_piece_of_rows(dtype, d, V):
+    """dh of the rows of the last piece, and of the first, as calls of those rows alone give it: apart from 1 / count, whose
+    rounding and product are 2^-23, and the output's rounding on both sides (an fp32 sum over V cut another way: 2^-18 of the
+    absolute sum, checked against the largest entry of the row)."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    rows = (2 ** 29 if dtype == "bf16" else 2 ** 27) // V + 300
+    h, W, y = _vocab(1, rows, d, V, dtype, seed=5)
+    _, _, _, dh, _ = b.vocab_loss_grad(h, W, y, scale=float((y >= 0).sum()))
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    for part in (slice(0, 256), slice(rows - 256, rows)):
+        hp, yp = h[:, part].contiguous(), y[:, part].contiguous()
+        want = b.vocab_loss_grad(hp, W, yp, scale=float((yp >= 0).sum()))[3].double()
+        err = (dh[:, part].double() - want).abs()
+        tol = (2 * half + 2.0 ** -22) * want.abs() * 1.01 + 2.0 ** -16 * want.abs().amax(-1, keepdim=True)
+        assert bool((err <= tol).all()), float((err / tol.clamp(min=1e-30)).max())
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_more_rows_than_one_launch_of_dz_takes(dtype):
+    """A piece of more than 65280 rows: dz is formed by two launches.  Rows on both sides of the border and the last ones against
+    64 bits, and dW of the whole (the sum over 65700 rows: u-relative bounds as in the tests of the gradient)."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    rows, d, V = 65700, 40, 130
+    h, W, y = _vocab(1, rows, d, V, dtype, seed=8)
+    y[0, 65270:65275] = -1
+    n = int((y >= 0).sum())
+    loss, rl, lse, dh, dW = b.vocab_loss_grad(h, W, y, scale=float(n))
+    z = h[0].double() @ W[0].double().T
+    l64 = torch.logsumexp(z, 1)
+    keep = y[0] >= 0
+    at = y[0].long().clamp(min=0)[:, None]
+    assert bool(((lse[0].double() - l64).abs() <= 2.0 ** -18 * (1 + l64.abs())).all())
+    want = torch.where(keep, l64 - z.gather(1, at)[:, 0], 0.0)
+    assert bool(((rl[0].double() - want).abs() <= 2.0 ** -16 * (1 + want)).all())
+    assert abs(float(loss[0]) - float(want.sum()) / n) <= 2.0 ** -18 * float(want.sum()) / n
+    dz = torch.softmax(z, 1).scatter_add_(1, at, torch.full_like(l64, -1.0)[:, None]) * keep[:, None]
+    # dz: 2^-11 and 2^-8 (bf16) or the logits' 2^-16; then one rounding of the sum
+    one = 2.0 ** -11 + 2.0 ** -8 + 2.0 ** -15 if dtype == "bf16" else 2.0 ** -15
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -22
+    for got, a, o in ((dh[0], dz, W[0].double()), (dW[0], dz.T, h[0].double())):
+        want = a @ o
+        tol = (one + 2.0 ** -15) * (a.abs() @ o.abs()) + half * want.abs()
+        assert bool(((got.double() - want).abs() <= tol).all())
+
+
+def test_loss_of_a_vocabulary_whose_rows_come_in_pieces():
+    """Without a gradient a piece is 2^31 logits or 256 rows: two pieces of 300 rows over more than 2^23 columns, each row with the
+    bits of a call of its piece alone."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    h, W, y = _vocab(1, 300, 8, 2 ** 23 + 77, "bf16", seed=1)
+    loss, rl, lse = b.vocab_loss(h, W, y)
+    for part in (slice(0, 256), slice(256, 300)):
+        _, r, l = b.vocab_loss(h[:, part].contiguous(), W, y[:, part].contiguous())
+        assert torch.equal(r, rl[:, part]) and torch.equal(l, lse[:, part])
+    want = rl.double().sum() / int((y >= 0).sum())
+    assert abs(float(loss) - float(want)) <= 2.0 ** -23 * float(want)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 96), ("bf16", 97), ("fp32", 96), ("fp32", 33)])
+@pytest.mark.parametrize("rows", [3, 12, 30])
+def test_few_rows_of_replicas_apart(rows, dtype, d):
+    """Replicas with gaps between them give the bits of dense ones, and the gaps stay as they were."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    m, V = 2, 301
+    h, W, y = _vocab(m, rows, d, V, dtype, seed=rows)
+    ref, plain = b.vocab_loss_grad(h, W, y), b.vocab_loss(h, W, y)
+    gaps = [rows * d + (64 if d % 8 == 0 else 67), V * d + (128 if d % 8 == 0 else 133)]
+    bufs = [torch.full((m * g,), 5.0, device="cuda", dtype=h.dtype) for g in gaps * 2]
+    views = [torch.as_strided(t, (m, n, d), (g, d, 1)) for t, g, n in zip(bufs, gaps * 2, (rows, V) * 2)]
+    views[0].copy_(h)
+    views[1].copy_(W)
+    got = b.vocab_loss_grad(views[0], views[1], y, dh=views[2], dW=views[3])
+    for t, r in zip(got, ref):
+        assert torch.equal(t, r)
+    for t, r in zip(b.vocab_loss(views[0], views[1], y), plain):
+        assert torch.equal(t, r)
+    for t, g, n in zip(bufs, gaps * 2, (rows, V) * 2):
+        flat = torch.ones_like(t, dtype=torch.bool)
+        torch.as_strided(flat, (m, n, d), (g, d, 1)).fill_(False)
+        assert bool((t[flat] == 5.0).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows", [3, 12, 70])
 def test_row_outputs_left_out(rows, dtype):
