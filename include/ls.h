@@ -488,8 +488,9 @@ int ls_muon_step(float* w_dev, float* v_dev, const void* g_dev, int m, int rows,
 /* The same step of the matrix W_l of layer `layer` (0-based) of all m replicas of a handle, with the handle's momentum
  * buffers as v, from gradients g [m][dims[layer + 1]][dims[layer]], row-major, g_stride elements apart.  Whatever the
  * handle keeps beside the weights follows: local steps, averages and losses after the call see the new weights.  Biases stay as
- * they are; lr and momentum are this call's own, not the handle's.  Enqueued on the handle's stream; workspace as
- * ls_orthogonalize_ws_bytes(m, dims[layer + 1], dims[layer]) has it. */
+ * they are; lr and momentum are this call's own, not the handle's.  Enqueued on the handle's stream, and not to
+ * be captured into a graph (LS_ERR_UNSUPPORTED); workspace as ls_orthogonalize_ws_bytes(m, dims[layer + 1], dims[layer]) has it.
+ * A wait that runs out is reported by ls_device_status(), not by ls_sync(). */
 int ls_muon_step_layer(ls_handle* h, int layer, const void* g_dev, int64_t g_stride, int g_dtype, float lr, float momentum,
                        int nesterov, int steps, void* ws_dev, size_t ws_bytes);
 

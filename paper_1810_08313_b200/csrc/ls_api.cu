@@ -922,6 +922,10 @@ int ls_muon_step_layer(ls_handle* h, int layer, const void* g_dev, int64_t g_str
   if (!ok_handle(h)) return LS_ERR_BAD_HANDLE;
   const Layout& lay = h->lay;
   if (layer < 0 || layer >= lay.L) return LS_ERR_INVALID_ARG;
+  // what the call does to the handle itself (the synchronized copy is no longer valid) would be missing in a replay
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  LS_CUDA(h, cudaStreamIsCapturing(h->stream, &capture));
+  if (capture != cudaStreamCaptureStatusNone) return LS_ERR_UNSUPPORTED;
   const int rc = muon_step(params_of(h) + lay.w_off[layer], mom_of(h) + lay.w_off[layer], g_dev, lay.m, lay.dims[layer + 1],
                            lay.dims[layer], lay.stride, lay.stride, g_stride, g_dtype, lr, momentum, nesterov, steps,
                            lay.tiled[layer] != 0, ws_dev, ws_bytes, h->stream);

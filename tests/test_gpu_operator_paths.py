@@ -101,6 +101,36 @@ def test_muon_step_of_a_handles_layer(dims, dtype, B, layer, gdtype):
     other.close()
 
 
+def test_muon_step_of_a_handles_layer_in_a_capture_is_refused():
+    """A replay would change the weights behind the handle's back, after an averaging step for instance.  Nothing is captured, and the
+    handle goes on."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        eng = b.LocalSGD(2, (24, 40, 10), lr=0.1, momentum=0.9, batch=8, stream=stream)
+        gr = torch.randn(2, 40, 24, device="cuda")
+        ws = torch.empty(b.orthogonalize_workspace(2, 40, 24), device="cuda", dtype=torch.uint8)
+        eng.set_params(np.linspace(-1, 1, eng.P, dtype=np.float32))
+        eng.muon_step(0, gr, lr=0.1, workspace=ws)
+        before = eng.get_all()
+    g = torch.cuda.CUDAGraph()
+    out = torch.zeros(4, device="cuda")
+    with torch.cuda.graph(g, stream=stream):
+        out += 1.0
+        with pytest.raises(b.LsError) as e:
+            eng.muon_step(0, gr, lr=0.1, workspace=ws)
+        assert e.value.code == b.LS_ERR_UNSUPPORTED
+    g.replay()
+    torch.cuda.synchronize()
+    assert float(out.min()) == 1.0
+    for a, c in zip(before, eng.get_all()):
+        assert np.array_equal(a, c)
+    eng.muon_step(0, gr, lr=0.1, workspace=ws)
+    assert not np.array_equal(eng.get_all()[0], before[0])
+    eng.close()
+
+
 # ---- sizes beyond a C int ------------------------------------------------------------------------------------------
 
 def test_sizes_beyond_32_bits_are_refused():
