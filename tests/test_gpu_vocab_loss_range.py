@@ -105,3 +105,25 @@ def test_labels_of_infinite_logits(rows, dtype):
     loss, rl, lse, _, dW = b.vocab_loss_grad(h, W, y)
     assert float(loss) == 0.0 and float(rl.abs().max()) == 0.0 and bool((lse == 2.0).all())
     assert float(dW[0, 9].abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [3, 12, 70])
+def test_rows_of_nan_keep_to_themselves(rows, dtype):
+    """A labelled row that is NaN makes its own losses, dh and the mean NaN; the other rows keep their bits.  dW, a sum over the
+    rows, is NaN where that row enters."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    dt = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    h = torch.randn(1, rows, 64, generator=g, device="cuda").to(dt)
+    W = (torch.randn(1, 400, 64, generator=g, device="cuda") / 8).to(dt)
+    y = torch.randint(0, 400, (1, rows), generator=g, device="cuda").int()
+    ref = b.vocab_loss_grad(h, W, y)
+    bad = h.clone()
+    bad[0, 1, 5] = float("nan")
+    got = b.vocab_loss_grad(bad, W, y)
+    keep = [i for i in range(rows) if i != 1]
+    for k in (1, 2, 3):
+        assert torch.equal(got[k][0, keep], ref[k][0, keep]) and bool(got[k][0, 1].isnan().all())
+    assert bool(got[0].isnan().all()) and bool(got[4].isnan().all())
