@@ -76,6 +76,7 @@ struct Params {
   int total;                             // tiles of the launch
   int tri;                               // 1: only tiles on or above the diagonal (symmetric C)
   int per, step;                         // tiles of one batch entry and split; 256 / NT
+  int fine;                              // EPI_PIECES: 1 cuts the tail's chunks further, see k_order()
   int dominant;                          // where one K block dominates a row's (1) or a column's (2) sum: see k_order()
   int a_box;                             // rows of a box of A's map if not 64 (K-major A with M <= a_box only)
   int n_fast;                            // 1: neighbouring pairs take neighbouring columns, else neighbouring rows
@@ -131,6 +132,8 @@ __device__ __forceinline__ Tile tile_of(const Params& p, int t) {
 // k = column).  Every MMA that follows it in the accumulator truncates it again, a bias that the Newton-Schulz
 // iteration amplifies (error of five steps 2.9e-6 at chunks of 2 K blocks, 4.8e-6 at 4, 8.7e-6 at 8).  The blocks with
 // the tile's own k therefore come last, each in a chunk of its own, and the others, small sums of mixed signs, first.
+// Params::fine: each of the four MMAs of such a block's first pieces has a chunk of its own, because within the block, too, up to three
+// MMAs follow the dominant product.
 struct KOrder { int first, tail; };
 template <int NT>
 __device__ __forceinline__ KOrder k_order(const Params& p, const Tile& t) {
@@ -345,7 +348,8 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
           if (!__all_sync(0xffffffffu, got)) { failed = true; break; }
           tc_fence_after_sync();
-          const bool last = in_chunk == p.chunk_kb - 1 || kb >= body - 1;
+          const bool fine = EPI == EPI_PIECES && p.fine != 0 && kb >= body;
+          const bool last = fine || in_chunk == p.chunk_kb - 1 || kb >= body - 1;
           if (lead) {
             const uint32_t d_tmem = tmem_base + (uint32_t)(acc * NT);
             // small products first; a piece's slot is released after the last product that needs it
@@ -360,13 +364,14 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                   const int i = turn == 0 ? q : o, j = turn == 0 ? o : q;
 #pragma unroll
                   for (int k = 0; k < 4; ++k) {
+                    if (q == 0 && k > 0 && fine) continue;
                     mma_f16_pair_lo(d_tmem, a_lo[i] + (A_MN ? k * 128 : k * 2), b_lo[j] + (B_MN ? k * 128 : k * 2), HI, IDESC,
                                     begin ? 0u : 1u);
                     begin = false;
                   }
                 }
               }
-              mma_commit_pair(&empty[slot[q]]);
+              if (q > 0 || !fine) mma_commit_pair(&empty[slot[q]]);
             }
             if (last) mma_commit_pair(&acc_full[acc]);
           }
@@ -375,6 +380,21 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           if (last) {
             in_chunk = 0;
             if (++acc == ACCS) { acc = 0; ++acc_round; }
+          }
+          if (fine) {                        // the other three MMAs of the first pieces
+            for (int k = 1; k < 4; ++k) {
+              if (acc_round > 0 && !__all_sync(0xffffffffu, mbar_wait(&acc_empty[acc], (acc_round - 1) & 1))) { failed = true; break; }
+              tc_fence_after_sync();
+              if (lead) {
+                mma_f16_pair_lo(tmem_base + (uint32_t)(acc * NT), a_lo[0] + (A_MN ? k * 128 : k * 2), b_lo[0] + (B_MN ? k * 128 : k * 2),
+                                HI, IDESC, 0u);
+                if (k == 3) mma_commit_pair(&empty[slot[0]]);
+                mma_commit_pair(&acc_full[acc]);
+              }
+              __syncwarp();
+              if (++acc == ACCS) { acc = 0; ++acc_round; }
+            }
+            if (failed) break;
           }
         }
       }
@@ -399,7 +419,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const int k0 = tl.split * p.kb_per_split;
       const int nk = min(p.num_kb, k0 + p.kb_per_split) - k0;
       const int tail = k_order<NT>(p, tl).tail;
-      const int chunks = (nk - tail + p.chunk_kb - 1) / p.chunk_kb + tail;
+      const int chunks = (nk - tail + p.chunk_kb - 1) / p.chunk_kb + tail * (EPI == EPI_PIECES && p.fine != 0 ? 4 : 1);
       uint32_t acc[G][32];
 #pragma unroll
       for (int j = 0; j < G; ++j)
@@ -651,7 +671,8 @@ int* device_error_word();
 // signs by about 2e-6 of its value, and sums of mixed signs by far less.  One piece: 256 MMAs for results that are rounded to
 // bf16 (whose half step is 4e-3), 32 for the row statistics, which leave in fp32, or 16 for a single tile of rows, where the
 // bytes of B bound the product and few rows average the losses' errors (2 x 2047 x 50001: 332 us at 32, 369 at 16, loss off by
-// 4e-7 and 2e-7; 64 x 32000: 26.5 and 27.1 us).  Two: 16 MMAs of the large product.  Three: 4, for 2 % more time than 8, which
+// 4e-7 and 2e-7; 64 x 32000: 26.5 and 27.1 us).  Two: 16 MMAs of the large product, unless the caller asks for fewer.  Three: 4, for
+// 2 % more time than 8, which
 // leave the gradient of a cross entropy over 10007 columns off by 6.9e-7, not 2.6e-7.
 constexpr int chunk_of(int np, bool stats, int m_tiles) {
   return np == 1 ? (!stats ? 64 : m_tiles > 1 ? 8 : 4) : np == 2 ? 4 : 1;

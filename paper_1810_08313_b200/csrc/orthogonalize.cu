@@ -398,7 +398,11 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
     g.batch = a.m; g.M = g.N = p.n; g.tri = g.mirror = 1;
     g.a_zstep = lstep; g.b_zstep = rstep; g.b_z0 = r0; g.c_zstep = ostep;
     g.dominant = 1;
-    g.chunk_kb = together ? 2 : 8;          // (together: 2e-5 at chunks of 8 for singular values over six decades, 9e-6 at 2)
+    g.chunk_kb = together ? 2 : 4;          // (together: 2e-5 at chunks of 8 for singular values over six decades, 9e-6 at 2)
+    // P of a small matrix (up to three K blocks): few elements average what the MMAs after a row's dominant product truncate, and
+    // near singular values of 1 P is what is left of a - 2.7.  1524 x 65 is off by 1.7e-6 without, 1.1e-6 with it, 763 x 189 by 1.5
+    // and 0.7 times fp32 arithmetic's error; at 256 x 256 (129 and 142 us) the two errors are alike already.
+    g.fine = !together && p.n <= 192;
     return gop::launch<2, true, false, false, gop::EPI_PIECES>(p.square.nt, l, r, out, out_t, g, p.n, st);
   };
   // A, and C = b I + c A, of a product whose operands were scaled
@@ -426,6 +430,9 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
     if (!cut) g = a_and_c(a.scale_x * a.scale_x);
     g.batch = a.m; g.M = g.N = p.n; g.tri = 1;
     g.a_zstep = g.b_zstep = 2;
+    // The diagonal is a sum of equal signs, and what it loses moves all singular values the same way: 1524 x 65 is off by 2.5e-6 at
+    // chunks of 4 and 1.7e-6 at 1 for the same time.  It no longer shows with many rows, where it costs time (8 x 2048 x 2048: about 1 %).
+    g.chunk_kb = p.n <= 512 ? 1 : 4;
     if (cut) {
       g.alpha = 1.f; g.splits = p.gram.splits; g.c_zstep = p.gram.splits;
       if (p.tall) LS_TRY((gop::launch<2, true, true, true, gop::EPI_F32>(p.gram.nt, xk[cur], xk[cur], gf, gf, g, p.k, st)));
@@ -461,7 +468,9 @@ int run_ns(MatArgs a, int steps, char* ws, cudaStream_t st) {
     g.batch = a.m; g.M = a.rows; g.N = a.cols;
     g.a_zstep = g.b_zstep = g.c_zstep = 2;
     g.dominant = p.tall ? 2 : 1;
-    g.chunk_kb = 8;
+    // (directions of large singular values are sums over the whole K: 722 x 805 of rank 45 and noise is 1.95 times as far off as fp32
+    // arithmetic at chunks of 8 here and in P, 1.2 times at 4; 2 x 2501 x 1000: 464 and 474 us)
+    g.chunk_kb = 4;
     if (p.tall) LS_TRY((gop::launch<2, true, false, false, gop::EPI_PIECES>(p.full.nt, xk[cur], sk[iq], xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
     else LS_TRY((gop::launch<2, true, false, true, gop::EPI_PIECES>(p.full.nt, sk[iq], xk[cur], xo[cur ^ 1], xo[cur ^ 1], g, p.n, st)));
   }
