@@ -93,6 +93,12 @@ struct Params {
   const int32_t* labels;                 // [M], label_z apart; the label's logit is written to label_logit[row], and the slice's
   float* label_logit;                    // numbers are those of the other columns
   int64_t label_z;
+  // few rows (or null): row-major h [M][dot_d] and W [N][dot_d], dot_hz and dot_wz apart, from which the labels' logits are formed
+  // beside the product, see label_dots(); label_lo[row] receives what label_logit[row] leaves over
+  const __nv_bfloat16 *dot_h, *dot_w;
+  int64_t dot_hz, dot_wz;
+  int dot_d;
+  float* label_lo;
   unsigned* clear;                       // `batch` words that the launch sets to zero for the next one, or null
   // EPI_PIECES: output i (of n_out) is planes c + 2 i (first piece) and c + 2 i + 1 of the stack
   int n_out;
@@ -211,6 +217,42 @@ __device__ __forceinline__ uint32_t pack_e16(float a, float b) {
 // the two numbers of a word, divided by kE16Scale (a field of zeros then reads as a number without the implicit bit)
 __device__ __forceinline__ float2 unpack_e16(uint32_t w) {
   return make_float2(__uint_as_float((w << 13) & 0x1FFFE000u), __uint_as_float((w >> 3) & 0x1FFFE000u));
+}
+
+// The logit of a label is a sum of equal signs where a row is sure of it, which the tensor core's truncation leaves off by 1e-6,
+// and with a handful of rows nothing averages the losses.  One warp of a CTA forms it in double while the first tile's products run.
+// (Chunks of one K block for all columns instead: a quarter to a third more time.)
+__device__ __forceinline__ void label_dots(const Params& p, int lane) {
+  for (int i = blockIdx.x; i < p.M * p.batch; i += gridDim.x) {
+    const int z = i / p.M, row = i - z * p.M;
+    const int y = p.labels[z * p.label_z + row];
+    if (y < 0 || y >= p.N) continue;
+    const __nv_bfloat16* h = p.dot_h + z * p.dot_hz + (int64_t)row * p.dot_d;
+    const __nv_bfloat16* w = p.dot_w + z * p.dot_wz + (int64_t)y * p.dot_d;
+    double sum = 0.0;
+    if (p.dot_d % 8 == 0) {                  // (rows start on 16-byte boundaries then)
+#pragma unroll 4
+      for (int k = lane * 8; k < p.dot_d; k += 256) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(h + k)), b = __ldg(reinterpret_cast<const uint4*>(w + k));
+        const uint32_t u[4] = {a.x, a.y, a.z, a.w}, v[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {        // (products of bf16 numbers are exact in fp32)
+          sum += (double)(__uint_as_float(u[e] << 16) * __uint_as_float(v[e] << 16));
+          sum += (double)(__uint_as_float(u[e] & 0xFFFF0000u) * __uint_as_float(v[e] & 0xFFFF0000u));
+        }
+      }
+    } else {
+#pragma unroll 8
+      for (int k = lane; k < p.dot_d; k += 32) sum += (double)(__bfloat162float(h[k]) * __bfloat162float(w[k]));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) {
+      const float hi = (float)sum;
+      p.label_logit[z * p.label_z + row] = hi;
+      p.label_lo[z * p.label_z + row] = isfinite(hi) ? (float)(sum - (double)hi) : 0.f;
+    }
+  }
 }
 
 template <int NP, int NT, bool F16, bool A_MN, bool B_MN, int EPI>
@@ -414,6 +456,9 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     int turn = 0;                            // which box is next
     const uint32_t empty_leader = map_to_rank(smem_u32(&acc_empty[0]), 0);
     int buf = 0, round = 0;
+    if constexpr (NP == 1 && (EPI == EPI_STATS || EPI == EPI_STATS_E16 || EPI == EPI_STATS_F32)) {
+      if (p.dot_h != nullptr && warp == 2) label_dots(p, lane);
+    }
     for (int t = pair; t < p.total && !failed; t += pairs) {
       const Tile tl = tile_of(p, t);
       const int k0 = tl.split * p.kb_per_split;
@@ -499,7 +544,7 @@ gemm_op_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 acc[j][i] = 0xff800000u;
               }
           }
-          if (mine) p.label_logit[tl.z * p.label_z + row] = zl;
+          if (mine && p.dot_h == nullptr) p.label_logit[tl.z * p.label_z + row] = zl;
         }
         float mx = -INFINITY;
 #pragma unroll

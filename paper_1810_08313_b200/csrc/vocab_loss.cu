@@ -50,6 +50,7 @@ struct CombineArgs {
   int slices, rows, V;
   const int32_t* labels;          // of the piece
   float* label;                   // the label's logit; replaced by dz at the label
+  const float* label_lo;          // what it leaves over, or null
   float *lse, *row_loss;
   float2* norm;                   // fp32 gradient: (reference of the exponentials, their sum) of the piece's rows, or null
   unsigned* done;
@@ -72,13 +73,18 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
   a.all_labels += z * a.all_rows; a.all_row_loss += z * a.all_rows;
   a.done += z;
   if (a.norm != nullptr) a.norm += z * a.all_rows;
+  if (a.label_lo != nullptr) a.label_lo += z * a.all_rows;
   if (a.inv_count != nullptr) a.inv_count += z;
   if (a.loss != nullptr) a.loss += z;
   grid_dep_wait();
   grid_dep_launch();
   int y = -1;
-  float zy = 0.f;
-  if (wp == 0 && row < a.rows) { y = a.labels[row]; zy = __ldcg(a.label + row); }       // (zy: whatever is there without a label)
+  float zy = 0.f, zy_lo = 0.f;                              // (whatever is there without a label)
+  if (wp == 0 && row < a.rows) {
+    y = a.labels[row];
+    zy = __ldcg(a.label + row);
+    if (a.label_lo != nullptr) zy_lo = __ldcg(a.label_lo + row);
+  }
   // eight slices at a time, their sixteen loads in flight together
   float m = -INFINITY, s = 0.f;
   if (row < a.rows) {
@@ -119,7 +125,8 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
     const float top = fmaxf(M, ry);
     const float ref = top == -INFINITY ? 0.f : top;
     if (M != -INFINITY) S *= gop::ex2(M - ref);
-    const float ey = labelled ? gop::ex2(fmaf(zy, kLog2e, -ref)) : 0.f;
+    const double dy = fma((double)zy + (double)zy_lo, (double)kLog2e, -(double)ref);
+    const float ey = labelled ? gop::ex2((float)dy) : 0.f;
     const float T = S + ey;
     // T is a sum of 2^(z kLog2e - ref), so that log-sum-exp and row loss are differences in that base, formed in double: rounded,
     // a log-sum-exp of 20 is off by 1e-6, and so would be the loss
@@ -128,7 +135,7 @@ __global__ void __launch_bounds__(1024) vocab_combine_kernel(CombineArgs a) {
     if (a.norm != nullptr) a.norm[row] = make_float2(ref, T);
     float loss = 0.f;
     if (labelled) {
-      loss = S < ey ? log1pf(S / ey) : (float)((fma(-(double)zy, (double)kLog2e, (double)ref) + log_sum) / (double)kLog2e);
+      loss = S < ey ? log1pf(S / ey) : (float)((log_sum - dy) / (double)kLog2e);
       a.label[row] = -(S / T);
     }
     a.row_loss[row] = loss;
@@ -715,6 +722,8 @@ constexpr int64_t kMaxVocab = 1 << 24, kMaxWidth = 1 << 16;
 // 1270.  bf16 gradient of 118992 x 1608: 4 rows 280 us, 8 rows 379, tensor cores 288; dz stays in fp32 here, whose
 // rounding to bf16 no other row would average.
 constexpr int64_t kFewRows = 32, kFewRowsGrad = 16, kFewRowsGrad16 = 4;
+// bf16: up to so many rows the labels' logits are formed on their own (gop::label_dots()).
+constexpr int64_t kDotRows = 4;
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
@@ -762,7 +771,7 @@ Plan replica_plan(Plan p, int m, int batch, int64_t rows, int64_t V, int d) {
   size_t at = 0;
   auto take = [&at](int64_t bytes) { size_t o = at; at += (size_t)round_up(bytes, 256); return o; };
   p.o_stat = take(2 * (int64_t)p.batch * p.slices * p.stat_ld * 4);
-  p.o_logit = take(m * rows * 4);
+  p.o_logit = take(m * rows * 8);          // (and what it leaves over)
   p.o_lse = take(m * rows * 4);
   p.o_rowloss = take(m * rows * 4);
   p.o_norm = take(p.f32 && grad ? batch * p.R * 8 : 0);
@@ -794,7 +803,7 @@ Plan few_plan(Plan p, int m, int64_t rows, int64_t V, int d) {
   size_t at = 0;
   auto take = [&at](int64_t bytes) { size_t o = at; at += (size_t)round_up(bytes, 256); return o; };
   p.o_stat = take(2 * (int64_t)m * p.slices * p.stat_ld * 4);
-  p.o_logit = take(m * rows * 4);
+  p.o_logit = take(m * rows * 8);          // (and what it leaves over)
   p.o_lse = take(m * rows * 4);
   p.o_rowloss = take(m * rows * 4);
   p.o_norm = take(m * rows * 8);
@@ -915,6 +924,12 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     g.batch = nb; g.a_zstep = g.b_zstep = NP; g.c_zstep = 1; g.splits = 1; g.M = (int)rn; g.N = (int)V; g.alpha = 1.f;
     g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld; g.stat_z = stat_z; g.label_z = a.rows;
     g.labels = labels + r0; g.label_logit = logit + r0; g.clear = done; g.a_box = a_box;
+    float* label_lo = nullptr;
+    if (!F32 && a.rows <= kDotRows) {
+      label_lo = logit + a.m * a.rows;
+      g.dot_h = reinterpret_cast<const bf*>(h); g.dot_w = reinterpret_cast<const bf*>(W);
+      g.dot_hz = a.h_stride; g.dot_wz = a.w_stride; g.dot_d = d; g.label_lo = label_lo;
+    }
     if (!p.grad) {
       LS_TRY((gop::launch<NP, false, false, false, gop::EPI_STATS>(p.nt, mh, mw, mh, mh, g, d, st)));
     } else {
@@ -925,7 +940,7 @@ int run_replica(const VocabArgs& a, const Plan& p, int rep, cudaStream_t st) {
     CombineArgs cb{};
     cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices;
     cb.rows = (int)rn; cb.V = (int)V;
-    cb.labels = labels + r0; cb.label = logit + r0; cb.lse = lse + r0; cb.row_loss = row_loss + r0;
+    cb.labels = labels + r0; cb.label = logit + r0; cb.label_lo = label_lo; cb.lse = lse + r0; cb.row_loss = row_loss + r0;
     cb.done = done; cb.all_labels = labels; cb.all_row_loss = row_loss; cb.all_rows = a.rows;
     cb.norm = F32 && p.grad ? norm : nullptr;
     if (p.grad && piece == 0) cb.inv_count = inv;
@@ -1012,6 +1027,7 @@ int run_few(const VocabArgs& a, const Plan& p, cudaStream_t st) {
   float* stat_sum = stat_max + m * stat_z;
   float* logit = reinterpret_cast<float*>(a.ws + p.o_logit);
   unsigned* done = reinterpret_cast<unsigned*>(a.ws + p.o_done);
+  float* label_lo = nullptr;
   if constexpr (sizeof(T) == 4) {
     FewArgs f{};
     f.h = static_cast<const float*>(a.h); f.W = static_cast<const float*>(a.W);
@@ -1032,11 +1048,14 @@ int run_few(const VocabArgs& a, const Plan& p, cudaStream_t st) {
     g.batch = a.m; g.a_zstep = g.b_zstep = g.c_zstep = 1; g.splits = 1; g.M = rows; g.N = V; g.alpha = 1.f;
     g.stat_max = stat_max; g.stat_sum = stat_sum; g.stat_ld = p.stat_ld; g.stat_z = stat_z; g.label_z = rows;
     g.labels = a.labels; g.label_logit = logit; g.clear = done; g.a_box = a_box;
+    label_lo = logit + m * a.rows;
+    g.dot_h = reinterpret_cast<const __nv_bfloat16*>(a.h); g.dot_w = reinterpret_cast<const __nv_bfloat16*>(a.W);
+    g.dot_hz = a.h_stride; g.dot_wz = a.w_stride; g.dot_d = a.d; g.label_lo = label_lo;
     LS_TRY((gop::launch<1, false, false, false, gop::EPI_STATS_F32>(p.nt, mh, mw, mz, mz, g, a.d, st)));
   }
   CombineArgs cb{};
   cb.stat_max = stat_max; cb.stat_sum = stat_sum; cb.stat_ld = p.stat_ld; cb.stat_z = stat_z; cb.slices = p.slices;
-  cb.rows = rows; cb.V = V; cb.labels = cb.all_labels = a.labels; cb.label = logit;
+  cb.rows = rows; cb.V = V; cb.labels = cb.all_labels = a.labels; cb.label = logit; cb.label_lo = label_lo;
   cb.lse = a.lse ? a.lse : reinterpret_cast<float*>(a.ws + p.o_lse);
   cb.row_loss = a.row_loss ? a.row_loss : reinterpret_cast<float*>(a.ws + p.o_rowloss);
   cb.all_row_loss = cb.row_loss; cb.all_rows = a.rows; cb.done = done; cb.loss = a.loss;

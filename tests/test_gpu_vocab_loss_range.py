@@ -127,3 +127,36 @@ def test_rows_of_nan_keep_to_themselves(rows, dtype):
     for k in (1, 2, 3):
         assert torch.equal(got[k][0, keep], ref[k][0, keep]) and bool(got[k][0, 1].isnan().all())
     assert bool(got[0].isnan().all()) and bool(got[4].isnan().all())
+
+
+@pytest.mark.parametrize("rows", [1, 2, 4])
+@pytest.mark.parametrize("d", [4096, 2000, 385])
+def test_label_logits_of_few_rows(rows, d):
+    """Long sums of equal signs at the label, zeros elsewhere: with a handful of bf16 rows nothing averages the losses, so the
+    label's logit must not carry the truncation of the tensor core.  The other columns' sum is exact but for one exponential
+    (2^-22); the label's argument is rounded near zero; a logarithm and the result: 2^-20 of the loss in all."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    V, m = 20001, 2
+    g = torch.Generator(device="cuda").manual_seed(rows + d)
+    h = torch.randn(m, rows, d, generator=g, device="cuda").abs().bfloat16()
+    W = torch.zeros(m, V, d, device="cuda", dtype=torch.bfloat16)
+    y = torch.stack([torch.randperm(V, generator=g, device="cuda")[:rows] for _ in range(m)])
+    own = torch.rand(m, rows, d, generator=g, device="cuda") + 0.2
+    own = (own / (own * h.float()).sum(-1, keepdim=True) * (9.5 + torch.rand(m, rows, 1, generator=g, device="cuda"))).bfloat16()
+    for i in range(m):
+        W[i, y[i]] = own[i]
+    z = torch.einsum("mrd,mvd->mrv", h.double(), own.double())      # the rows' labels among one another
+    zy = z.diagonal(dim1=1, dim2=2)
+    top = z.max(-1).values
+    # (a row's other columns: zeros, and the logits of the other rows' labels)
+    others = (z - zy[..., None]).exp().sum(-1) - 1.0 + (V - rows) * torch.exp(-zy)
+    want = torch.log1p(others)
+    for out in (b.vocab_loss(h, W, y.int()), b.vocab_loss_grad(h, W, y.int())):
+        if rows == 1:
+            assert bool(((out[1].double() - want).abs() <= 2.0 ** -20 * want).all()), (out[1].double() - want) / want
+        else:
+            # (those logits are products of the tensor core: 2^-22 of them for each of its chunks' 16 MMAs, in their share)
+            share = 1.0 - (V - rows) * torch.exp(-zy) / others
+            tol = 2.0 ** -20 * want + 2.0 ** -18 * top * share
+            assert bool(((out[1].double() - want).abs() <= tol).all()), (out[1].double() - want) / want
