@@ -459,8 +459,10 @@ int ls_vocab_loss(const void* h_dev, const void* W_dev, const int32_t* labels_de
                   int d, int64_t h_stride, int64_t w_stride, int dtype, float* loss_dev, float* row_loss_dev,
                   float* lse_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream);
 
-/* The same losses, and the gradients of scale * loss: dh [m][rows][d] (zero in rows without a label), dW [m][vocab][d],
- * both of dtype, overwritten.  h of rows without a label does not enter dW, whatever it holds. */
+/* The same losses, and the gradients of scale * loss: dh [m][rows][d] (zero in rows without a label, if W is finite),
+ * dW [m][vocab][d], both of dtype, overwritten.  h of rows without a label does not enter dW, whatever it holds.
+ * bf16: the gradient of the logits, an operand of both products, is rounded to bf16 (2^-8 of each of its numbers, down to 43 nats
+ * below the largest of its 64 or 128 neighbours), except for up to 4 rows with d a multiple of 8. */
 int ls_vocab_loss_grad(const void* h_dev, const void* W_dev, const int32_t* labels_dev, int m, int64_t rows, int64_t vocab,
                        int d, int64_t h_stride, int64_t w_stride, int dtype, float scale, float* loss_dev,
                        float* row_loss_dev, float* lse_dev, void* dh_dev, int64_t dh_stride, void* dW_dev,

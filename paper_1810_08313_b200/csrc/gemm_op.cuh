@@ -19,7 +19,7 @@
 //              chunks keep that below the last bits that matter (see chunk_of()), and since a tile's last chunk is
 //              collected like any other, the epilogue of a tile runs under the products of the next one.
 // NT is 256, or 128 where there are too few tiles for the pairs (pick_nt).  Collecting a chunk costs about as much as two K
-// blocks: a Newton-Schulz step of eight 2048 x 2048 matrices took 880 us at chunks of two, 780 us at eight.
+// blocks: a Newton-Schulz step of eight 2048 x 2048 matrices took 880 us at chunks of two, 780 us at eight, 800 us as they are now.
 //
 // Outputs leave through boxes of shared memory per warp and TMA stores, which clip at the tensor's edge; ragged M, N
 // and K are the zero fill of the loads and that clip.  A symmetric result is computed on and above the diagonal tiles and

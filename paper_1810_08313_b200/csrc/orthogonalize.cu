@@ -19,10 +19,10 @@
 // Steps taken together: A and P are polynomials of the first A, so they commute and A_{k+1} = A_k P_k P_k.  Two or three steps
 // need one A = X X^T and one X <- Q X with Q = P_2 P_1 P_0; each step after the first replaces that pair of products,
 // 3 n^2 k multiply-adds, by three symmetric ones more (B = A P, B P, P Q), 3 n^3 / 2.  That pays for matrices longer than wide whose
-// products fill the GPU (Plan::group compares both by pick_cut()'s estimates): 2 x 1024 x 4096 513 -> 417 us.  It costs
+// products fill the GPU (Plan::group compares both by pick_cut()'s estimates): 2 x 1024 x 4096 513 -> 436 us.  It costs
 // accuracy: what the tensor core truncates in A is multiplied by a^2 a step (11.9) before it acts, and every P and Q has
-// one large product a row.  Five steps of normal matrices are off by 4e-6 to 8e-6 of their norm, 2e-6 to 3e-6 one at a time (2e-6 to
-// 4e-6 in fp32 arithmetic), so only steps from bf16 numbers, which carry 2e-3, are taken together.
+// one large product a row.  Five steps of normal matrices are off by 4e-6 to 8e-6 of their norm, 1e-6 to 3e-6 one at a time, as in
+// fp32 arithmetic, so only steps from bf16 numbers, which carry 2e-3, are taken together.
 #include "gemm_op.cuh"
 
 #include <math.h>

@@ -835,7 +835,7 @@ Plan make_plan(int m, int64_t rows, int64_t V, int d, int dtype, bool grad) {
   p.few = rows > 0 && (p.f32 ? rows <= (grad ? kFewRowsGrad : kFewRows) : grad && d % 8 == 0 && rows <= kFewRowsGrad16);
   if (p.few) return few_plan(p, m, rows, V, d);
   // All replicas in one set of launches while the workspace of that stays below 512 MB; larger ones fill the GPU by
-  // themselves (fp32 gradients of 2 x 513 x 10007 x 760: 381 -> 339 us, 4 x 178 x 21522 x 512: 605 -> 397 us).
+  // themselves (fp32 gradients, time on the GPU: 2 x 513 x 10007 x 760 381 -> 339 us, 4 x 178 x 21522 x 512 605 -> 397 us).
   if (m > 1 && p.pieces == 1) {
     const Plan all = replica_plan(p, m, m, rows, V, d);
     if (all.total <= (size_t)1 << 29) return all;
