@@ -101,6 +101,31 @@ def test_muon_step_of_a_handles_layer(dims, dtype, B, layer, gdtype):
     other.close()
 
 
+@pytest.mark.parametrize("gdtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dims,dtype,B", [((384, 512, 256, 10), "bf16", 256), ((24, 40, 10), "fp32", 8)])
+def test_muon_step_of_a_handles_layer_from_strided_gradients(dims, dtype, B, gdtype):
+    """Gradients with gaps between the replicas and an odd start take the element-wise reads: the bits of a dense call."""
+    import torch
+    from paper_1810_08313_b200.binding import LocalSGD
+    m, rows, cols = 2, dims[1], dims[0]
+    x1 = wl.random_mlp_point(3, dims, True)
+    g = torch.randn(m, rows, cols, device="cuda").to(torch.bfloat16 if gdtype == "bf16" else torch.float32)
+    gap = rows * cols + 7
+    buf = torch.zeros(m * gap + 1, device="cuda", dtype=g.dtype)
+    apart = torch.as_strided(buf, (m, rows, cols), (gap, cols, 1), 1)
+    apart.copy_(g)
+    got = []
+    for grad in (g, apart):
+        eng = LocalSGD(m, dims, gemm_dtype=dtype, lr=0.05, momentum=0.9, batch=B)
+        eng.set_params(x1)
+        for _ in range(2):
+            eng.muon_step(0, grad, lr=0.1, nesterov=False)
+        got.append(eng.get_all())
+        eng.close()
+    for a, c in zip(*got):
+        assert np.array_equal(a, c)
+
+
 def test_muon_step_of_a_handles_layer_in_a_capture_is_refused():
     """A replay would change the weights behind the handle's back, after an averaging step for instance.  Nothing is captured, and the
     handle goes on."""
