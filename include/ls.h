@@ -402,7 +402,7 @@ int ls_linear_loss_static(const float* W_dev, const float* bias_dev, const float
                           int64_t n_rows, int d_in, int d_out, int loss, int chunk_rows, float* chunk_loss_dev,
                           void* cuda_stream);
 
-/* ---- operators of a language model's last layers and its weight update, on raw buffers ------------------------
+/* ---- operators of a language model's blocks, last layers and weight update, on raw buffers ---------------------
  * Not passages of the paper: what a local-SGD job of a language model needs beside the averaging step.  Conventions:
  *  - m replicas in one call; *_stride is the distance in elements between replicas of that tensor (ignored for m == 1),
  *    inside a replica every tensor is dense and row-major.  Any size is allowed up to the limits stated; rows and
@@ -496,6 +496,73 @@ int ls_muon_step(float* w_dev, float* v_dev, const void* g_dev, int m, int rows,
  * A wait that runs out is reported by ls_device_status(), not by ls_sync(). */
 int ls_muon_step_layer(ls_handle* h, int layer, const void* g_dev, int64_t g_stride, int g_dtype, float lr, float momentum,
                        int nesterov, int steps, void* ws_dev, size_t ws_bytes);
+
+/* RMS norm of every head of q and k and rotation by position, in one pass:
+ *   z = x / sqrt(mean of x^2 over the head + eps) * weight,  then the pairs of the first rot_dim elements of z are turned:
+ *   (a, b) -> (a cos - b sin, a sin + b cos),  angle = positions[token] * inv_freq[pair]
+ * Pair p is the elements (p, p + rot_dim / 2), or (2 p, 2 p + 1) when interleaved; the other elements stay as they are.
+ * q [m][tokens][heads][head_dim], k [m][tokens][kv_heads][head_dim], and their outputs, of dtype: *_row is the distance in
+ * elements between tokens of a tensor, *_stride that between replicas (ignored for one token, one replica), the heads of a
+ * token are dense, so that q and k may be parts of one projection.  weights: float [m][head_dim], weight_stride apart.
+ * inv_freq: double [rot_dim / 2], positions: int32 [m][tokens], dense (either may be NULL if rot_dim == 0).  Angles
+ * are formed in double.  rot_dim is even.  head_dim <= 256, tokens <= 2^30, heads <= 65536. */
+int ls_qk_norm_rope(const void* q_dev, const void* k_dev, const float* q_weight_dev, const float* k_weight_dev,
+                    const int32_t* positions_dev, const double* inv_freq_dev, int m, int64_t tokens, int heads, int kv_heads,
+                    int head_dim, int rot_dim, int interleaved, int64_t q_row, int64_t k_row, int64_t q_stride, int64_t k_stride,
+                    int64_t weight_stride, int dtype, float eps, void* q_out_dev, void* k_out_dev, int64_t q_out_row,
+                    int64_t k_out_row, int64_t q_out_stride, int64_t k_out_stride, void* cuda_stream);
+
+/* Its gradient, from the gradients of both outputs and the call's inputs: dq, dk like q and k (in rows of their own distances), and
+ * dq_weight, dk_weight: float [m][head_dim], dweight_stride apart, sums over tokens and heads, overwritten (zeros for no tokens). */
+int ls_qk_norm_rope_grad_ws_bytes(int m, int64_t tokens, int head_dim, size_t* bytes);
+int ls_qk_norm_rope_grad(const void* dq_out_dev, const void* dk_out_dev, const void* q_dev, const void* k_dev,
+                         const float* q_weight_dev, const float* k_weight_dev, const int32_t* positions_dev,
+                         const double* inv_freq_dev, int m, int64_t tokens, int heads, int kv_heads, int head_dim, int rot_dim,
+                         int interleaved, int64_t dq_out_row, int64_t dk_out_row, int64_t q_row, int64_t k_row,
+                         int64_t dq_out_stride, int64_t dk_out_stride, int64_t q_stride, int64_t k_stride, int64_t weight_stride,
+                         int dtype, float eps, void* dq_dev, void* dk_dev, int64_t dq_row, int64_t dk_row, int64_t dq_stride,
+                         int64_t dk_stride, float* dq_weight_dev, float* dk_weight_dev, int64_t dweight_stride, void* ws_dev,
+                         size_t ws_bytes, void* cuda_stream);
+
+/* Causal attention over packed sequences, without stored scores:
+ *   s_ij = scale q_i . k_j  over the keys j <= i of i's own sequence,  out_i = sum_j softmax(s_i)_j v_j,  lse_i = log sum_j exp s_ij
+ * q, out [m][tokens][heads][head_dim], k, v [m][tokens][kv_heads][head_dim] of dtype, rows and replicas apart as for
+ * ls_qk_norm_rope; heads is a multiple of kv_heads, and head h reads key head h / (heads / kv_heads).
+ * seq_start: int32 [m][n_seqs + 1], dense, ascending: sequence s of a replica is the rows [seq_start[s], seq_start[s + 1]), of any
+ * length, none included.  NULL with n_seqs == 1: one sequence of all rows.  Rows in no sequence (before the first, behind the
+ * last) get out = 0 and lse = 0, and whatever they hold reaches no other row; nor does a NaN reach another sequence or an
+ * earlier row of its own.  (Boundaries that do not ascend or leave [0, tokens] give wrong results, but no access outside.)
+ * lse: float [m][heads][tokens], dense.  A row whose scores are all -inf, or one +inf, has no softmax: its out is NaN.
+ * head_dim <= 256, tokens <= 2^30. */
+int ls_attention(const void* q_dev, const void* k_dev, const void* v_dev, const int32_t* seq_start_dev, int m, int64_t tokens,
+                 int n_seqs, int heads, int kv_heads, int head_dim, int64_t q_row, int64_t k_row, int64_t v_row, int64_t q_stride,
+                 int64_t k_stride, int64_t v_stride, int dtype, float scale, void* out_dev, int64_t out_row, int64_t out_stride,
+                 float* lse_dev, void* cuda_stream);
+
+/* Its gradient, from dout, the inputs, and the out and lse that the forward call wrote:
+ *   P_ij = exp(s_ij - lse_i),  dS_ij = P_ij (dout_i . v_j - dout_i . out_i),
+ *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
+ * dk and dv sum over the query heads of their group.  Zero for rows in no sequence, whose dout may hold anything. */
+int ls_attention_grad_ws_bytes(int m, int64_t tokens, int heads, int kv_heads, int head_dim, size_t* bytes);
+int ls_attention_grad(const void* dout_dev, const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
+                      const float* lse_dev, const int32_t* seq_start_dev, int m, int64_t tokens, int n_seqs, int heads, int kv_heads,
+                      int head_dim, int64_t dout_row, int64_t q_row, int64_t k_row, int64_t v_row, int64_t out_row,
+                      int64_t dout_stride, int64_t q_stride, int64_t k_stride, int64_t v_stride, int64_t out_stride, int dtype,
+                      float scale, void* dq_dev, void* dk_dev, void* dv_dev, int64_t dq_row, int64_t dk_row, int64_t dv_row,
+                      int64_t dq_stride, int64_t dk_stride, int64_t dv_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
+/* The global norm of every replica's gradients, and clipping to it:
+ *   norm[r] = sqrt(sum over all tensors of replica r of g^2),  g <- g if norm[r] <= max_norm, else g * (max_norm / norm[r])
+ * Host arrays of n_tensors entries: tensor i has sizes[i] elements a replica, of dtypes[i], strides[i] apart (dense within a
+ * replica; strides may be NULL for m == 1).  outs NULL: in place; else the results go to outs[i] (of out_dtypes[i], rounded once,
+ * out_strides[i] apart; grads[i] itself, with its type and stride, is allowed) and gradients that are not their own outputs stay.
+ * norm: float [m].  max_norm > 0; INFINITY: the norm, and nothing is scaled.  A norm of NaN makes the replica's results NaN;
+ * an infinite one makes them 0, and NaN where a gradient is infinite.  Sums are formed in double over fp32 sums of 32 squares; no square
+ * overflows or underflows.  The arrays are read before the call returns.  n_tensors <= 65536. */
+int ls_clip_grads_ws_bytes(const int64_t* sizes, int n_tensors, int m, size_t* bytes);
+int ls_clip_grads(const void* const* grads_dev, const int64_t* sizes, const int64_t* strides, const int32_t* dtypes, int n_tensors,
+                  int m, float max_norm, void* const* outs_dev, const int64_t* out_strides, const int32_t* out_dtypes,
+                  float* norm_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream);
 
 /* Per-kernel device timing.  Between ls_profile_begin() and ls_profile_end()
  * every launch of a kernel class selected by class_mask (bit c = class c; for

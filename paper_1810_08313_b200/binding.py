@@ -134,6 +134,16 @@ def _lib():
         "ls_muon_step": (C.c_int, [vp, vp, vp, C.c_int, C.c_int, C.c_int, i64, i64, i64, C.c_int, f32, f32, C.c_int, C.c_int,
                                    vp, C.c_size_t, vp]),
         "ls_muon_step_layer": (C.c_int, [vp, C.c_int, vp, i64, C.c_int, f32, f32, C.c_int, C.c_int, vp, C.c_size_t]),
+        "ls_qk_norm_rope": (C.c_int, [vp] * 6 + [C.c_int, i64] + [C.c_int] * 5 + [i64] * 5 + [C.c_int, f32, vp, vp] + [i64] * 4 + [vp]),
+        "ls_qk_norm_rope_grad_ws_bytes": (C.c_int, [C.c_int, i64, C.c_int, P(C.c_size_t)]),
+        "ls_qk_norm_rope_grad": (C.c_int, [vp] * 8 + [C.c_int, i64] + [C.c_int] * 5 + [i64] * 9 + [C.c_int, f32, vp, vp] + [i64] * 4 +
+                                 [vp, vp, i64, vp, C.c_size_t, vp]),
+        "ls_attention": (C.c_int, [vp] * 4 + [C.c_int, i64] + [C.c_int] * 4 + [i64] * 6 + [C.c_int, f32, vp, i64, i64, vp, vp]),
+        "ls_attention_grad_ws_bytes": (C.c_int, [C.c_int, i64, C.c_int, C.c_int, C.c_int, P(C.c_size_t)]),
+        "ls_attention_grad": (C.c_int, [vp] * 7 + [C.c_int, i64] + [C.c_int] * 4 + [i64] * 10 + [C.c_int, f32, vp, vp, vp] + [i64] * 6 +
+                              [vp, C.c_size_t, vp]),
+        "ls_clip_grads_ws_bytes": (C.c_int, [vp, C.c_int, C.c_int, P(C.c_size_t)]),
+        "ls_clip_grads": (C.c_int, [vp, vp, vp, vp, C.c_int, C.c_int, f32, vp, vp, vp, vp, vp, C.c_size_t, vp]),
         "ls_shard_buffer_floats": (C.c_int, [vp, P(i64)]),
         "ls_set_shard": (C.c_int, [vp, C.c_int, C.c_int, vp, vp, EXCHANGE_FN, vp]),
         "ls_shard_partial_sum": (C.c_int, [vp, vp]),
@@ -398,6 +408,33 @@ class _Op:
             raise ValueError(f"{name} must be contiguous")
         return self.stack(t, name, shape[1:], shape[0], dtype)[0]
 
+    def heads(self, t, name: str, m: Optional[int], tokens: Optional[int], heads: Optional[int], hd: Optional[int], dtype):
+        """t as [m][tokens][heads][head_dim] with the heads of a token dense (None: from t); returns (pointer, distance between
+        tokens, distance between replicas)."""
+        torch = self.torch
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            raise ValueError(f"{name} must be a tensor on {self.device}")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+        shape, step = t.shape, t.stride()
+        if len(shape) == 3:
+            shape, step = (1, *shape), (0, *step)
+        if len(shape) != 4 or (m is not None and shape[0] != m) or (tokens is not None and shape[1] != tokens) or \
+                (heads is not None and shape[2] != heads) or (hd is not None and shape[3] != hd):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [m = {m}][tokens = {tokens}][heads = {heads}][head_dim = {hd}]")
+        if (step[3] != 1 and shape[3] > 1) or (step[2] != shape[3] and shape[2] > 1):
+            raise ValueError(f"{name}: the heads of a token must be dense")
+        if self.stream is not None:
+            t.record_stream(self.stream)
+        return t.data_ptr(), step[1], step[0]
+
+    def heads_out(self, given, like, name: str, m, tokens, heads, hd, dtype):
+        """An output [m][tokens][heads][head_dim]: the caller's tensor, or a new dense one.  (tensor, pointer, row, stride)"""
+        if given is None:
+            t = self.new(like, (m, tokens, heads, hd), dtype)
+            return t, t.data_ptr(), heads * hd, tokens * heads * hd
+        return (given, *self.heads(given, name, m, tokens, heads, hd, dtype))
+
     def new(self, like, shape, dtype):
         if self.stream is None:
             return like.new_empty(shape, dtype=dtype)
@@ -648,6 +685,211 @@ def muon_step(w, v, g, lr: float, momentum: float = 0.95, nesterov: bool = True,
     base, nbytes, keep = op.workspace(w, workspace, _ws_bytes("ls_orthogonalize_ws_bytes", m, rows, cols))
     op.call("ls_muon_step", wp, vp, gp, m, rows, cols, ws, vs, gs, dt, float(lr), float(momentum), int(bool(nesterov)),
             _int32(int(steps), LS_ERR_INVALID_ARG, "steps"), base, nbytes)
+
+
+def _head_shapes(q, k, what: str):
+    """(m, tokens, heads, kv_heads, head_dim) of q [m][tokens][heads][head_dim] and k (either without m)."""
+    if q.dim() not in (3, 4) or k.dim() != q.dim():
+        raise ValueError(f"{what}: q and k must be [m][tokens][heads][head_dim] or [tokens][heads][head_dim]")
+    m = q.shape[0] if q.dim() == 4 else 1
+    tokens, heads, hd = q.shape[-3:]
+    kv = k.shape[-2]
+    for v in (m, tokens, heads, kv, hd):
+        _int32(v, LS_ERR_TOO_LARGE, what)
+    return m, tokens, heads, kv, hd
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, device="cuda"):
+    """The frequencies base^(-2 p / rot_dim) of the rot_dim / 2 pairs, float64: what qk_norm_rope takes as inv_freq.  Made once by
+    a program; scaled variants are arithmetic on this tensor."""
+    torch = _op_torch()
+    if rot_dim < 0 or rot_dim % 2:
+        raise ValueError("rot_dim must be even")
+    p = torch.arange(0, rot_dim, 2, dtype=torch.float64)
+    return (float(base) ** (-p / max(1, rot_dim))).to(device)
+
+
+def _rope_args(op, q, k, q_weight, k_weight, positions, inv_freq, what):
+    torch = op.torch
+    dt = _op_dtype(q, "q")
+    m, tokens, heads, kv, hd = _head_shapes(q, k, what)
+    if not (isinstance(inv_freq, torch.Tensor) and inv_freq.dim() == 1):
+        raise ValueError("inv_freq must be a float64 tensor [rot_dim / 2]")
+    fp = op.stack(inv_freq, "inv_freq", (inv_freq.shape[0],), 1, torch.float64)[0]
+    pp = op.dense(positions, "positions", (m, tokens), torch.int32)
+    f32 = torch.float32
+    qw, _, ws = op.stack(q_weight, "q_weight", (hd,), m, f32)
+    kw, _, kws = op.stack(k_weight, "k_weight", (hd,), m, f32)
+    if m > 1 and ws != kws:
+        raise ValueError("q_weight and k_weight must have the same distance between replicas")
+    return dt, m, tokens, heads, kv, hd, 2 * inv_freq.shape[0], qw, kw, ws, pp, fp
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, eps: float = 1e-6, interleaved: bool = False, q_out=None, k_out=None,
+                 stream=None):
+    """RMS norm of every head of q [m][tokens][heads][head_dim] and k [m][tokens][kv_heads][head_dim] (float32 or bfloat16; the
+    heads of a token dense, tokens and replicas any distance apart) with float32 weights [m][head_dim], and rotation of the
+    first 2 len(inv_freq) elements by positions (int32 [m][tokens]) times inv_freq (float64, rope_frequencies()), in one
+    pass (ls_qk_norm_rope).  Returns the two results."""
+    op = _Op(q, stream)
+    dt, m, tokens, heads, kv, hd, rot, qw, kw, ws, pp, fp = _rope_args(op, q, k, q_weight, k_weight, positions, inv_freq,
+                                                                      "ls_qk_norm_rope")
+    qp, qr, qs = op.heads(q, "q", m, tokens, heads, hd, q.dtype)
+    kp, kr, ks = op.heads(k, "k", m, tokens, kv, hd, q.dtype)
+    qo, qop, qor, qos = op.heads_out(q_out, q, "q_out", m, tokens, heads, hd, q.dtype)
+    ko, kop, kor, kos = op.heads_out(k_out, q, "k_out", m, tokens, kv, hd, q.dtype)
+    op.call("ls_qk_norm_rope", qp, kp, qw, kw, pp, fp, m, tokens, heads, kv, hd, rot, int(bool(interleaved)), qr, kr, qs, ks, ws, dt, eps,
+            qop, kop, qor, kor, qos, kos)
+    return qo if q_out is not None else _like(q, 4, qo), ko if k_out is not None else _like(q, 4, ko)
+
+
+def qk_norm_rope_grad_workspace(m: int, tokens: int, head_dim: int) -> int:
+    return _ws_bytes("ls_qk_norm_rope_grad_ws_bytes", int(m), int(tokens), int(head_dim)) + 256
+
+
+def qk_norm_rope_grad(dq_out, dk_out, q, k, q_weight, k_weight, positions, inv_freq, eps: float = 1e-6, interleaved: bool = False,
+                      dq=None, dk=None, dq_weight=None, dk_weight=None, workspace=None, stream=None):
+    """Gradient of qk_norm_rope from the gradients of its results and its inputs (ls_qk_norm_rope_grad).  Returns (dq like q,
+    dk like k, dq_weight, dk_weight float32 [m][head_dim])."""
+    op = _Op(q, stream)
+    dt, m, tokens, heads, kv, hd, rot, qw, kw, ws, pp, fp = _rope_args(op, q, k, q_weight, k_weight, positions, inv_freq,
+                                                                      "ls_qk_norm_rope_grad")
+    gq, gqr, gqs = op.heads(dq_out, "dq_out", m, tokens, heads, hd, q.dtype)
+    gk, gkr, gks = op.heads(dk_out, "dk_out", m, tokens, kv, hd, q.dtype)
+    qp, qr, qs = op.heads(q, "q", m, tokens, heads, hd, q.dtype)
+    kp, kr, ks = op.heads(k, "k", m, tokens, kv, hd, q.dtype)
+    dq_t, dqp, dqr, dqs = op.heads_out(dq, q, "dq", m, tokens, heads, hd, q.dtype)
+    dk_t, dkp, dkr, dks = op.heads_out(dk, q, "dk", m, tokens, kv, hd, q.dtype)
+    f32 = op.torch.float32
+    dqw_t, dqw, dws = op.out(dq_weight, q, "dq_weight", (m, hd), f32)
+    dkw_t, dkw, dkws = op.out(dk_weight, q, "dk_weight", (m, hd), f32)
+    if m > 1 and dws != dkws:
+        raise ValueError("dq_weight and dk_weight must have the same distance between replicas")
+    base, nbytes, keep = op.workspace(q, workspace, _ws_bytes("ls_qk_norm_rope_grad_ws_bytes", m, tokens, hd))
+    op.call("ls_qk_norm_rope_grad", gq, gk, qp, kp, qw, kw, pp, fp, m, tokens, heads, kv, hd, rot, int(bool(interleaved)), gqr, gkr, qr,
+            kr, gqs, gks, qs, ks, ws, dt, eps, dqp, dkp, dqr, dkr, dqs, dks, dqw, dkw, dws, base, nbytes)
+    return (dq_t if dq is not None else _like(q, 4, dq_t), dk_t if dk is not None else _like(q, 4, dk_t),
+            dqw_t if dq_weight is not None else _like(q, 4, dqw_t), dkw_t if dk_weight is not None else _like(q, 4, dkw_t))
+
+
+def _sequences(op, seq_start, m):
+    if seq_start is None:
+        return None, 1
+    n = seq_start.shape[-1] - 1 if isinstance(seq_start, op.torch.Tensor) and seq_start.dim() else 0
+    if n < 0:
+        raise ValueError("seq_start must be an int32 tensor [m][sequences + 1]")
+    return op.dense(seq_start, "seq_start", (m, n + 1), op.torch.int32), n
+
+
+def attention(q, k, v, seq_start=None, scale: Optional[float] = None, out=None, lse=None, stream=None):
+    """Causal attention with grouped heads over packed sequences: q [m][tokens][heads][head_dim], k and v
+    [m][tokens][kv_heads][head_dim] (float32 or bfloat16; the heads of a token dense, tokens and replicas any distance apart),
+    seq_start int32 [m][sequences + 1] (None: one sequence of all tokens), scale 1 / sqrt(head_dim) if None (ls_attention).
+    Returns (out like q, log-sum-exp float32 [m][heads][tokens]); rows in no sequence are zero in both."""
+    op = _Op(q, stream)
+    dt = _op_dtype(q, "q")
+    m, tokens, heads, kv, hd = _head_shapes(q, k, "ls_attention")
+    qp, qr, qs = op.heads(q, "q", m, tokens, heads, hd, q.dtype)
+    kp, kr, ks = op.heads(k, "k", m, tokens, kv, hd, q.dtype)
+    vp, vr, vs = op.heads(v, "v", m, tokens, kv, hd, q.dtype)
+    sp, n = _sequences(op, seq_start, m)
+    o, outp, outr, outs = op.heads_out(out, q, "out", m, tokens, heads, hd, q.dtype)
+    lse_t, lp = op.out_dense(lse, q, "lse", (m, heads, tokens), op.torch.float32)
+    op.call("ls_attention", qp, kp, vp, sp, m, tokens, n, heads, kv, hd, qr, kr, vr, qs, ks, vs, dt,
+            1.0 / math.sqrt(hd) if scale is None else scale, outp, outr, outs, lp)
+    return o if out is not None else _like(q, 4, o), lse_t if lse is not None else _like(q, 4, lse_t)
+
+
+def attention_grad_workspace(m: int, tokens: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return _ws_bytes("ls_attention_grad_ws_bytes", int(m), int(tokens), int(heads), int(kv_heads), int(head_dim)) + 256
+
+
+def attention_grad(dout, q, k, v, out, lse, seq_start=None, scale: Optional[float] = None, dq=None, dk=None, dv=None, workspace=None,
+                   stream=None):
+    """Gradient of attention from dout, its inputs and its results (ls_attention_grad).  Returns (dq, dk, dv) like q, k, v; zero for
+    rows in no sequence."""
+    op = _Op(q, stream)
+    dt = _op_dtype(q, "q")
+    m, tokens, heads, kv, hd = _head_shapes(q, k, "ls_attention_grad")
+    gp, gr, gs = op.heads(dout, "dout", m, tokens, heads, hd, q.dtype)
+    qp, qr, qs = op.heads(q, "q", m, tokens, heads, hd, q.dtype)
+    kp, kr, ks = op.heads(k, "k", m, tokens, kv, hd, q.dtype)
+    vp, vr, vs = op.heads(v, "v", m, tokens, kv, hd, q.dtype)
+    outp, outr, outs = op.heads(out, "out", m, tokens, heads, hd, q.dtype)
+    lp = op.dense(lse, "lse", (m, heads, tokens), op.torch.float32)
+    sp, n = _sequences(op, seq_start, m)
+    dq_t, dqp, dqr, dqs = op.heads_out(dq, q, "dq", m, tokens, heads, hd, q.dtype)
+    dk_t, dkp, dkr, dks = op.heads_out(dk, q, "dk", m, tokens, kv, hd, q.dtype)
+    dv_t, dvp, dvr, dvs = op.heads_out(dv, q, "dv", m, tokens, kv, hd, q.dtype)
+    base, nbytes, keep = op.workspace(q, workspace, _ws_bytes("ls_attention_grad_ws_bytes", m, tokens, heads, kv, hd))
+    op.call("ls_attention_grad", gp, qp, kp, vp, outp, lp, sp, m, tokens, n, heads, kv, hd, gr, qr, kr, vr, outr, gs, qs, ks, vs, outs,
+            dt, 1.0 / math.sqrt(hd) if scale is None else scale, dqp, dkp, dvp, dqr, dkr, dvr, dqs, dks, dvs, base, nbytes)
+    return (dq_t if dq is not None else _like(q, 4, dq_t), dk_t if dk is not None else _like(q, 4, dk_t),
+            dv_t if dv is not None else _like(q, 4, dv_t))
+
+
+def clip_grads_workspace(sizes: Sequence[int], m: int) -> int:
+    """Workspace of clip_grads for tensors of so many elements a replica."""
+    n = C.c_size_t()
+    a = (C.c_int64 * max(1, len(sizes)))(*sizes)
+    _check(_lib().ls_clip_grads_ws_bytes(a, _int32(len(sizes), LS_ERR_TOO_LARGE, "ls_clip_grads_ws_bytes"),
+                                         _int32(int(m), LS_ERR_TOO_LARGE, "ls_clip_grads_ws_bytes"), C.byref(n)),
+           "ls_clip_grads_ws_bytes")
+    return n.value + 256
+
+
+def clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, stream=None):
+    """The global norm [m] (float32) of every replica's gradients, a sequence of tensors [m][...] (float32 or bfloat16, a replica
+    dense), which are scaled in place so that no replica's norm exceeds max_norm (ls_clip_grads).  out: a sequence of tensors of
+    the same shapes (of either type) that take the results instead.  max_norm = inf: the norm only."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("no gradients")
+    first = grads[0]
+    op = _Op(first, stream)
+    torch = op.torch
+    if first.dim() < 1:
+        raise ValueError("gradients must be [m][...]")
+    m, count, what = first.shape[0], len(grads), "ls_clip_grads"
+    _int32(m, LS_ERR_TOO_LARGE, what)
+    outs = None if out is None else list(out)
+    if outs is not None and len(outs) != count:
+        raise ValueError("out must have as many tensors as grads")
+
+    def table(tensors, name, like):
+        ptrs, sizes, steps, types = [], [], [], []
+        for i, t in enumerate(tensors):
+            if not isinstance(t, torch.Tensor) or t.device != op.device:
+                raise ValueError(f"{name}[{i}] must be a tensor on {op.device}")
+            dt = _OP_DTYPE.get(t.dtype)
+            if dt is None:
+                raise ValueError(f"{name}[{i}] must be float32 or bfloat16, not {t.dtype}")
+            shape = t.shape
+            if len(shape) < 1 or shape[0] != m or (like is not None and shape != like[i].shape):
+                raise ValueError(f"{name}[{i}] has shape {tuple(shape)}" + (f", expected [{m}][...]" if like is None else
+                                                                           f", expected {tuple(like[i].shape)}"))
+            n = t.numel() // m if m else 0
+            step = n
+            if not t.is_contiguous():
+                _, _, step = op.stack(t, f"{name}[{i}]", tuple(shape[1:]), m)
+            elif op.stream is not None:
+                t.record_stream(op.stream)
+            ptrs.append(t.data_ptr())
+            sizes.append(n)
+            steps.append(step)
+            types.append(dt)
+        return (C.c_void_p * count)(*ptrs), (C.c_int64 * count)(*sizes), (C.c_int64 * count)(*steps), (C.c_int32 * count)(*types)
+
+    gp, sizes, gs, gt = table(grads, "grads", None)
+    op_, os_, ot = None, None, None
+    if outs is not None:
+        op_, _, os_, ot = table(outs, "out", grads)
+    norm_t, np_ = op.out_dense(norm, first, "norm", (m,), torch.float32)
+    need = C.c_size_t()
+    _check(_lib().ls_clip_grads_ws_bytes(sizes, count, m, C.byref(need)), what)
+    base, nbytes, keep = op.workspace(first, workspace, need.value)
+    op.call(what, gp, sizes, gs, gt, count, m, float(max_norm), op_, os_, ot, np_, base, nbytes)
+    return norm_t
 
 
 class LocalSGD:

@@ -1,0 +1,516 @@
+// Attention over packed sequences and its gradient on the CUDA cores (see attention.cuh for the formulas), and the entry points.
+//
+// One CTA of 256 threads per tile of 64 rows (32 for heads of more than 128) of one head; tiles of 64 keys pass through shared
+// memory once each, and scores never leave the SM.  Thread (ty, tx) of 16 x 16 has the rows ty R .. + R - 1 and the keys
+// tx + 16 c of a tile of scores; operands are read four elements of a head at a time, rows padded by four floats, so that
+// the reads of a quarter warp fall into distinct banks and R x R x 4 multiply-adds need 2 R reads of 16 bytes.  The
+// second products read the scores back from shared memory the same way.  Forward: a running maximum and sum a row; the backward
+// pass has one kernel for dq (and D), tiles of queries, and one for dk and dv, tiles of keys which take all the queries of
+// their group's heads: the scores are formed twice, and no sum depends on an order of arrival.
+#include "attention.cuh"
+
+namespace ls {
+namespace attn {
+namespace {
+
+constexpr int kNT = 256;
+
+template <int HD>
+struct Way {
+  static constexpr int R = HD > 128 ? 2 : 4;      // rows and keys of a thread
+  static constexpr int B = 16 * R;                // of a tile
+  static constexpr int P = HD + 4;                // floats between rows of an operand
+  static constexpr int PS = B + 4;                // of the scores
+  static constexpr int C = HD / 16;               // result columns of a thread: 4 tx + 64 c .. + 3, or tx + 16 c below 64
+  static constexpr int tile = B * P, scores = B * PS;
+};
+
+// rows [r0, r0 + B) of a head into shared memory as floats; zeros outside the tensor and the head
+template <typename T, int HD>
+__device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t row, int64_t r0, int64_t rows, int hd) {
+  using W = Way<HD>;
+  for (int i = threadIdx.x; i < W::B * HD; i += kNT) {
+    const int r = i / HD, c = i - r * HD;
+    dst[r * W::P + c] = r0 + r < rows && c < hd ? to_f32(src[(r0 + r) * row + c]) : 0.f;
+  }
+}
+
+// s[r][c] = x row (ty R + r) . y row (tx + 16 c)
+template <int HD>
+__device__ __forceinline__ void dots(const float* x, const float* y, int ty, int tx, float (&s)[Way<HD>::R][Way<HD>::R]) {
+  using W = Way<HD>;
+#pragma unroll
+  for (int r = 0; r < W::R; ++r)
+#pragma unroll
+    for (int c = 0; c < W::R; ++c) s[r][c] = 0.f;
+#pragma unroll 4
+  for (int d = 0; d < HD; d += 4) {
+    float4 a[W::R], b[W::R];
+#pragma unroll
+    for (int r = 0; r < W::R; ++r) a[r] = *reinterpret_cast<const float4*>(x + (ty * W::R + r) * W::P + d);
+#pragma unroll
+    for (int c = 0; c < W::R; ++c) b[c] = *reinterpret_cast<const float4*>(y + (tx + 16 * c) * W::P + d);
+#pragma unroll
+    for (int r = 0; r < W::R; ++r)
+#pragma unroll
+      for (int c = 0; c < W::R; ++c)
+        s[r][c] = fmaf(a[r].w, b[c].w, fmaf(a[r].z, b[c].z, fmaf(a[r].y, b[c].y, fmaf(a[r].x, b[c].x, s[r][c]))));
+  }
+}
+
+// the column of a head that is c-th of thread tx
+template <int HD>
+__device__ __forceinline__ int column(int tx, int c) {
+  return HD >= 64 ? (c & ~3) * 16 + tx * 4 + (c & 3) : tx + 16 * c;
+}
+// acc[r][c] += sum over j of s[ty R + r][j] y[j][column c]
+template <int HD>
+__device__ __forceinline__ void accumulate(const float* s, const float* y, int ty, int tx, float (&acc)[Way<HD>::R][Way<HD>::C]) {
+  using W = Way<HD>;
+#pragma unroll 2
+  for (int j = 0; j < W::B; j += 4) {
+    float4 a[W::R];
+#pragma unroll
+    for (int r = 0; r < W::R; ++r) a[r] = *reinterpret_cast<const float4*>(s + (ty * W::R + r) * W::PS + j);
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) {
+      float b[W::C];
+      const float* row = y + (j + jj) * W::P;
+      if constexpr (HD >= 64) {
+#pragma unroll
+        for (int c = 0; c < W::C; c += 4) {
+          const float4 t = *reinterpret_cast<const float4*>(row + column<HD>(tx, c));
+          b[c] = t.x; b[c + 1] = t.y; b[c + 2] = t.z; b[c + 3] = t.w;
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < W::C; ++c) b[c] = row[column<HD>(tx, c)];
+      }
+#pragma unroll
+      for (int r = 0; r < W::R; ++r) {
+        const float f = jj == 0 ? a[r].x : jj == 1 ? a[r].y : jj == 2 ? a[r].z : a[r].w;
+#pragma unroll
+        for (int c = 0; c < W::C; ++c) acc[r][c] = fmaf(f, b[c], acc[r][c]);
+      }
+    }
+  }
+}
+
+// Writes acc[r][c] * by[r] to the rows r0 + ty R + r of the tensor; returns whether all of the thread's numbers are finite.
+template <typename T, int HD>
+__device__ __forceinline__ bool write_rows(T* dst, int64_t row, int64_t r0, int64_t rows, int hd, int ty, int tx,
+                                           const float (&acc)[Way<HD>::R][Way<HD>::C], const float (&by)[Way<HD>::R],
+                                           uint32_t* bad) {
+  using W = Way<HD>;
+  bool good = true;
+#pragma unroll
+  for (int r = 0; r < W::R; ++r) {
+    const int64_t i = r0 + ty * W::R + r;
+    if (i >= rows) continue;
+    bool fine = true;
+#pragma unroll
+    for (int c = 0; c < W::C; ++c) {
+      const int d = column<HD>(tx, c);
+      const float x = acc[r][c] * by[r];
+      fine = fine && fabsf(x) < INFINITY;
+      if (d < hd) dst[i * row + d] = from_f32<T>(x);
+    }
+    if (!fine) bad[ty * W::R + r] = 1u;
+    good = good && fine;
+  }
+  return good;
+}
+
+// sum or maximum over the 16 threads of a row
+__device__ __forceinline__ float row_total(float x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+__device__ __forceinline__ float row_max(float x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kNT)
+attention_kernel(const __grid_constant__ Args a) {
+  using W = Way<HD>;
+  extern __shared__ __align__(16) float sm[];
+  float* sq = sm;
+  float* sk = sq + W::tile;
+  float* sv = sk + W::tile;
+  float* sp = sv + W::tile;
+  __shared__ uint32_t bad[W::B];
+  __shared__ int start[W::B];
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, hd = a.head_dim;
+  grid_dep_wait();
+  grid_dep_launch();
+  // the rows with the most keys first
+  const int tiles = (int)((a.tokens + W::B - 1) / W::B);
+  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
+  const int64_t r0 = (int64_t)(tiles - 1 - rest / a.m) * W::B;
+  const int kvh = head / (a.heads / a.kv_heads);
+  load_tile<T, HD>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd);
+  if (tid < W::B) {
+    bad[tid] = 0u;
+    start[tid] = row_start(a, rep, (int)r0 + tid);
+  }
+  __syncthreads();
+  const float scale2 = a.scale * kLog2e;
+  float acc[W::R][W::C] = {}, top[W::R], sum[W::R];
+#pragma unroll
+  for (int r = 0; r < W::R; ++r) { top[r] = -INFINITY; sum[r] = 0.f; }
+  const int64_t end = min(r0 + W::B, a.tokens);
+  for (int64_t j0 = first_key(a, rep, (int)r0) / W::B * W::B; j0 < end; j0 += W::B) {
+    load_tile<T, HD>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd);
+    load_tile<T, HD>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd);
+    __syncthreads();
+    float s[W::R][W::R];
+    dots<HD>(sq, sk, ty, tx, s);
+#pragma unroll
+    for (int r = 0; r < W::R; ++r) {
+      const int row = ty * W::R + r;
+      float most = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < W::R; ++c) {
+        const int64_t j = j0 + tx + 16 * c;
+        s[r][c] = j >= start[row] && j <= r0 + row ? s[r][c] * scale2 : -INFINITY;
+        most = fmaxf(most, s[r][c]);
+      }
+      most = fmaxf(row_max(most), top[r]);
+      const float ref = most == -INFINITY ? 0.f : most;
+      const float keep = exp2f(top[r] - ref);
+      top[r] = most;
+      float part = 0.f;
+#pragma unroll
+      for (int c = 0; c < W::R; ++c) {
+        const float p = exp2f(s[r][c] - ref);
+        part += p;
+        sp[row * W::PS + tx + 16 * c] = p;
+      }
+      sum[r] = fmaf(sum[r], keep, part);
+#pragma unroll
+      for (int c = 0; c < W::C; ++c) acc[r][c] *= keep;
+    }
+    __syncthreads();
+    accumulate<HD>(sp, sv, ty, tx, acc);
+    __syncthreads();
+  }
+  float by[W::R];
+#pragma unroll
+  for (int r = 0; r < W::R; ++r) {
+    const int64_t i = r0 + ty * W::R + r;
+    sum[r] = row_total(sum[r]);
+    const bool none = start[ty * W::R + r] > i;
+    if (none) {
+#pragma unroll
+      for (int c = 0; c < W::C; ++c) acc[r][c] = 0.f;
+    }
+    by[r] = none ? 0.f : 1.f / sum[r];
+    if (tx == 0 && i < a.tokens)
+      a.lse[((int64_t)rep * a.heads + head) * a.tokens + i] = none ? 0.f : fmaf(top[r], kLn2, logf(sum[r]));
+  }
+  const bool good = write_rows<T, HD>(head_ptr<T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
+  if (__syncthreads_and(good)) return;
+  for (int r = tid >> 5; r < W::B; r += kNT / 32)
+    if (bad[r] != 0u) forward_row<T>(a, rep, head, (int)r0 + r);
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kNT)
+attention_dq_kernel(const __grid_constant__ Args a) {
+  using W = Way<HD>;
+  extern __shared__ __align__(16) float sm[];
+  float* sq = sm;
+  float* sg = sq + W::tile;
+  float* sk = sg + W::tile;
+  float* sv = sk + W::tile;
+  float* sp = sv + W::tile;
+  __shared__ uint32_t bad[W::B];
+  __shared__ int start[W::B];
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, hd = a.head_dim;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int tiles = (int)((a.tokens + W::B - 1) / W::B);
+  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
+  const int64_t r0 = (int64_t)(tiles - 1 - rest / a.m) * W::B;
+  const int kvh = head / (a.heads / a.kv_heads);
+  const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens;
+  load_tile<T, HD>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd);
+  load_tile<T, HD>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, r0, a.tokens, hd);
+  load_tile<T, HD>(sk, head_ptr<const T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd);
+  if (tid < W::B) {
+    bad[tid] = 0u;
+    start[tid] = row_start(a, rep, (int)r0 + tid);
+  }
+  __syncthreads();
+  float lse2[W::R], dot[W::R];
+#pragma unroll
+  for (int r = 0; r < W::R; ++r) {
+    const int row = ty * W::R + r;
+    float d = 0.f;
+    for (int e = tx; e < HD; e += 16) d = fmaf(sg[row * W::P + e], sk[row * W::P + e], d);
+    dot[r] = row_total(d);
+    lse2[r] = r0 + row < a.tokens ? a.lse[stat + r0 + row] * kLog2e : 0.f;
+    if (tx == 0 && r0 + row < a.tokens) a.dot[stat + r0 + row] = dot[r];
+  }
+  __syncthreads();
+  const float scale2 = a.scale * kLog2e;
+  float acc[W::R][W::C] = {};
+  const int64_t end = min(r0 + W::B, a.tokens);
+  for (int64_t j0 = first_key(a, rep, (int)r0) / W::B * W::B; j0 < end; j0 += W::B) {
+    load_tile<T, HD>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd);
+    load_tile<T, HD>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd);
+    __syncthreads();
+    float s[W::R][W::R], g[W::R][W::R];
+    dots<HD>(sq, sk, ty, tx, s);
+    dots<HD>(sg, sv, ty, tx, g);
+#pragma unroll
+    for (int r = 0; r < W::R; ++r) {
+      const int row = ty * W::R + r;
+#pragma unroll
+      for (int c = 0; c < W::R; ++c) {
+        const int64_t j = j0 + tx + 16 * c;
+        const bool seen = j >= start[row] && j <= r0 + row;
+        sp[row * W::PS + tx + 16 * c] = seen ? exp2f(fmaf(s[r][c], scale2, -lse2[r])) * (g[r][c] - dot[r]) : 0.f;
+      }
+    }
+    __syncthreads();
+    accumulate<HD>(sp, sk, ty, tx, acc);
+    __syncthreads();
+  }
+  float by[W::R];
+#pragma unroll
+  for (int r = 0; r < W::R; ++r) {
+    by[r] = a.scale;
+    if (start[ty * W::R + r] > r0 + ty * W::R + r) {
+#pragma unroll
+      for (int c = 0; c < W::C; ++c) acc[r][c] = 0.f;
+    }
+  }
+  const bool good = write_rows<T, HD>(head_ptr<T>(a.dq, rep, head, hd), a.dq.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
+  if (__syncthreads_and(good)) return;
+  for (int r = tid >> 5; r < W::B; r += kNT / 32)
+    if (bad[r] != 0u) dq_row<T>(a, rep, head, (int)r0 + r);
+}
+
+// Tiles of keys: scores with the keys as rows and the queries as columns.
+template <typename T, int HD>
+__global__ void __launch_bounds__(kNT)
+attention_dkv_kernel(const __grid_constant__ Args a) {
+  using W = Way<HD>;
+  extern __shared__ __align__(16) float sm[];
+  float* sk = sm;
+  float* sv = sk + W::tile;
+  float* sq = sv + W::tile;
+  float* sg = sq + W::tile;
+  float* sp = sg + W::tile;
+  __shared__ uint32_t bad[W::B];
+  __shared__ float lse2[W::B], dot[W::B];
+  __shared__ int start[W::B];
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, hd = a.head_dim;
+  grid_dep_wait();
+  grid_dep_launch();
+  // the keys with the most queries first
+  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, rep = rest % a.m;
+  const int64_t k0 = (int64_t)(rest / a.m) * W::B;
+  const int group = a.heads / a.kv_heads;
+  load_tile<T, HD>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, k0, a.tokens, hd);
+  load_tile<T, HD>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, k0, a.tokens, hd);
+  if (tid < W::B) bad[tid] = 0u;
+  const float scale2 = a.scale * kLog2e;
+  float dk[W::R][W::C] = {}, dv[W::R][W::C] = {};
+  const int64_t end = last_query(a, rep, (int)min(k0 + W::B, a.tokens) - 1);
+  for (int head = kvh * group; head < (kvh + 1) * group; ++head) {
+    const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens;
+    for (int64_t i0 = k0; i0 < end; i0 += W::B) {
+      __syncthreads();
+      load_tile<T, HD>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, i0, a.tokens, hd);
+      load_tile<T, HD>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, i0, a.tokens, hd);
+      if (tid < W::B) {
+        const bool in = i0 + tid < a.tokens;
+        lse2[tid] = in ? a.lse[stat + i0 + tid] * kLog2e : 0.f;
+        dot[tid] = in ? a.dot[stat + i0 + tid] : 0.f;
+        start[tid] = row_start(a, rep, (int)i0 + tid);
+      }
+      __syncthreads();
+      float s[W::R][W::R], g[W::R][W::R];
+      dots<HD>(sk, sq, ty, tx, s);
+      dots<HD>(sv, sg, ty, tx, g);
+#pragma unroll
+      for (int r = 0; r < W::R; ++r) {
+        const int64_t j = k0 + ty * W::R + r;
+#pragma unroll
+        for (int c = 0; c < W::R; ++c) {
+          const int col = tx + 16 * c;
+          const bool seen = j >= start[col] && j <= i0 + col;
+          const float p = seen ? exp2f(fmaf(s[r][c], scale2, -lse2[col])) : 0.f;
+          sp[(ty * W::R + r) * W::PS + col] = p;
+          s[r][c] = seen ? p * (g[r][c] - dot[col]) : 0.f;
+        }
+      }
+      __syncwarp();                        // (a row of scores is one half warp's)
+      accumulate<HD>(sp, sg, ty, tx, dv);
+      __syncwarp();
+#pragma unroll
+      for (int r = 0; r < W::R; ++r)
+#pragma unroll
+        for (int c = 0; c < W::R; ++c) sp[(ty * W::R + r) * W::PS + tx + 16 * c] = s[r][c];
+      __syncwarp();
+      accumulate<HD>(sp, sq, ty, tx, dk);
+    }
+  }
+  float one[W::R], scale[W::R];
+#pragma unroll
+  for (int r = 0; r < W::R; ++r) { one[r] = 1.f; scale[r] = a.scale; }
+  bool good = write_rows<T, HD>(head_ptr<T>(a.dk, rep, kvh, hd), a.dk.row, k0, a.tokens, hd, ty, tx, dk, scale, bad);
+  good = write_rows<T, HD>(head_ptr<T>(a.dv, rep, kvh, hd), a.dv.row, k0, a.tokens, hd, ty, tx, dv, one, bad) && good;
+  if (__syncthreads_and(good)) return;
+  for (int r = tid >> 5; r < W::B; r += kNT / 32)
+    if (bad[r] != 0u) dkv_row<T>(a, rep, kvh, (int)k0 + r);
+}
+
+template <typename T, int HD>
+cudaError_t launch(const Args& a, bool grad, cudaStream_t st) {
+  using W = Way<HD>;
+  const int fwd = (3 * W::tile + W::scores) * 4, bwd = (4 * W::tile + W::scores) * 4;
+  static_assert((4 * W::tile + W::scores) * 4 <= 220 * 1024, "shared memory budget");
+  static uint64_t done[3] = {0, 0, 0};   // one bit per device
+  const int64_t tiles = (a.tokens + W::B - 1) / W::B;
+  if (!grad) {
+    const cudaError_t e = allow_dynamic_smem(attention_kernel<T, HD>, fwd, &done[0]);
+    if (e != cudaSuccess) return e;
+    return launch_dep(attention_kernel<T, HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kNT), fwd, st, 1, a);
+  }
+  cudaError_t e = allow_dynamic_smem(attention_dq_kernel<T, HD>, bwd, &done[1]);
+  if (e == cudaSuccess) e = allow_dynamic_smem(attention_dkv_kernel<T, HD>, bwd, &done[2]);
+  if (e == cudaSuccess) e = launch_dep(attention_dq_kernel<T, HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kNT), bwd, st, 1, a);
+  if (e == cudaSuccess)
+    e = launch_dep(attention_dkv_kernel<T, HD>, dim3((unsigned)(tiles * a.kv_heads * a.m)), dim3(kNT), bwd, st, 1, a);
+  return e;
+}
+template <typename T>
+cudaError_t pick(const Args& a, bool grad, cudaStream_t st) {
+  if (a.head_dim <= 32) return launch<T, 32>(a, grad, st);
+  if (a.head_dim <= 64) return launch<T, 64>(a, grad, st);
+  if (a.head_dim <= 128) return launch<T, 128>(a, grad, st);
+  return launch<T, 256>(a, grad, st);
+}
+cudaError_t run(const Args& a, int dtype, bool grad, cudaStream_t st) {
+  return dtype == LS_DTYPE_BF16 ? pick<__nv_bfloat16>(a, grad, st) : pick<float>(a, grad, st);
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------
+
+int check_sizes(int m, int64_t tokens, int heads, int kv_heads, int head_dim, int dtype) {
+  if (m < 1 || tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || head_dim < 1) return LS_ERR_INVALID_ARG;
+  if (dtype != LS_DTYPE_FP32 && dtype != LS_DTYPE_BF16) return LS_ERR_INVALID_ARG;
+  if (m > 65535 || tokens > (1ll << 30) || heads > 65536 || head_dim > 256) return LS_ERR_TOO_LARGE;
+  // (tiles of 32 rows, all heads, all replicas: blocks of one launch)
+  if ((tokens + 31) / 32 * heads > 2147483647ll / m) return LS_ERR_TOO_LARGE;
+  return LS_OK;
+}
+// distances that no element uses, as the kernels' tensor maps take them
+void settle(const Args& a, Tensor* t, int heads) {
+  if (a.tokens <= 1) t->row = (int64_t)heads * a.head_dim;
+  if (a.m == 1) t->replica = a.tokens * t->row;
+}
+// a tensor [m][tokens][heads][head_dim] whose rows are dense
+bool bad_tensor(const Args& a, const Tensor& t, int heads, int dtype) {
+  const int64_t width = (int64_t)heads * a.head_dim;
+  if (reinterpret_cast<uintptr_t>(t.p) % (dtype == LS_DTYPE_BF16 ? 2 : 4) != 0) return true;
+  if (a.tokens == 0) return false;
+  if (t.p == nullptr || (a.tokens > 1 && t.row < width)) return true;
+  if (t.row > (1ll << 40) / a.tokens) return true;
+  return a.m > 1 && t.replica < (a.tokens - 1) * (a.tokens > 1 ? t.row : 0) + width;
+}
+bool misaligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0; }
+
+}  // namespace
+}  // namespace attn
+}  // namespace ls
+
+extern "C" int ls_attention(const void* q_dev, const void* k_dev, const void* v_dev, const int32_t* seq_start_dev, int m,
+                            int64_t tokens, int n_seqs, int heads, int kv_heads, int head_dim, int64_t q_row, int64_t k_row,
+                            int64_t v_row, int64_t q_stride, int64_t k_stride, int64_t v_stride, int dtype, float scale,
+                            void* out_dev, int64_t out_row, int64_t out_stride, float* lse_dev, void* cuda_stream) {
+  using namespace ls;
+  using namespace ls::attn;
+  int rc = check_sizes(m, tokens, heads, kv_heads, head_dim, dtype);
+  if (rc != LS_OK) return rc;
+  Args a{};
+  a.m = m; a.tokens = tokens; a.heads = heads; a.kv_heads = kv_heads; a.head_dim = head_dim; a.n_seqs = n_seqs; a.scale = scale;
+  a.q = Tensor{const_cast<void*>(q_dev), q_row, q_stride};
+  a.k = Tensor{const_cast<void*>(k_dev), k_row, k_stride};
+  a.v = Tensor{const_cast<void*>(v_dev), v_row, v_stride};
+  a.out = Tensor{out_dev, out_row, out_stride};
+  a.lse = lse_dev;
+  a.seq_start = seq_start_dev;
+  if (n_seqs < 0 || n_seqs > (1 << 30) || (seq_start_dev == nullptr && n_seqs != 1) || !isfinite(scale)) return LS_ERR_INVALID_ARG;
+  if (bad_tensor(a, a.q, heads, dtype) || bad_tensor(a, a.k, kv_heads, dtype) || bad_tensor(a, a.v, kv_heads, dtype) ||
+      bad_tensor(a, a.out, heads, dtype) || misaligned4(lse_dev) || misaligned4(seq_start_dev) ||
+      (tokens > 0 && lse_dev == nullptr))
+    return LS_ERR_INVALID_ARG;
+  if (tokens == 0) return LS_OK;
+  settle(a, &a.q, heads);
+  settle(a, &a.out, heads);
+  settle(a, &a.k, kv_heads);
+  settle(a, &a.v, kv_heads);
+  a.err = gop::device_error_word();
+  if (a.err == nullptr) return LS_ERR_CUDA;
+  return run(a, dtype, false, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LS_OK : LS_ERR_CUDA;
+}
+
+extern "C" int ls_attention_grad_ws_bytes(int m, int64_t tokens, int heads, int kv_heads, int head_dim, size_t* bytes) {
+  using namespace ls::attn;
+  const int rc = check_sizes(m, tokens, heads, kv_heads, head_dim, LS_DTYPE_FP32);
+  if (rc != LS_OK) return rc;
+  if (bytes == nullptr) return LS_ERR_INVALID_ARG;
+  *bytes = (size_t)m * (size_t)heads * (size_t)tokens * sizeof(float);
+  return LS_OK;
+}
+
+extern "C" int ls_attention_grad(const void* dout_dev, const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
+                                 const float* lse_dev, const int32_t* seq_start_dev, int m, int64_t tokens, int n_seqs, int heads,
+                                 int kv_heads, int head_dim, int64_t dout_row, int64_t q_row, int64_t k_row, int64_t v_row,
+                                 int64_t out_row, int64_t dout_stride, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                 int64_t out_stride, int dtype, float scale, void* dq_dev, void* dk_dev, void* dv_dev, int64_t dq_row,
+                                 int64_t dk_row, int64_t dv_row, int64_t dq_stride, int64_t dk_stride, int64_t dv_stride,
+                                 void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  using namespace ls;
+  using namespace ls::attn;
+  int rc = check_sizes(m, tokens, heads, kv_heads, head_dim, dtype);
+  if (rc != LS_OK) return rc;
+  Args a{};
+  a.m = m; a.tokens = tokens; a.heads = heads; a.kv_heads = kv_heads; a.head_dim = head_dim; a.n_seqs = n_seqs; a.scale = scale;
+  a.dout = Tensor{const_cast<void*>(dout_dev), dout_row, dout_stride};
+  a.q = Tensor{const_cast<void*>(q_dev), q_row, q_stride};
+  a.k = Tensor{const_cast<void*>(k_dev), k_row, k_stride};
+  a.v = Tensor{const_cast<void*>(v_dev), v_row, v_stride};
+  a.out = Tensor{const_cast<void*>(out_dev), out_row, out_stride};
+  a.dq = Tensor{dq_dev, dq_row, dq_stride};
+  a.dk = Tensor{dk_dev, dk_row, dk_stride};
+  a.dv = Tensor{dv_dev, dv_row, dv_stride};
+  a.lse = const_cast<float*>(lse_dev);
+  a.seq_start = seq_start_dev;
+  if (n_seqs < 0 || n_seqs > (1 << 30) || (seq_start_dev == nullptr && n_seqs != 1) || !isfinite(scale)) return LS_ERR_INVALID_ARG;
+  for (const Tensor* t : {&a.dout, &a.q, &a.out, &a.dq})
+    if (bad_tensor(a, *t, heads, dtype)) return LS_ERR_INVALID_ARG;
+  for (const Tensor* t : {&a.k, &a.v, &a.dk, &a.dv})
+    if (bad_tensor(a, *t, kv_heads, dtype)) return LS_ERR_INVALID_ARG;
+  if (misaligned4(lse_dev) || misaligned4(seq_start_dev) || (tokens > 0 && lse_dev == nullptr)) return LS_ERR_INVALID_ARG;
+  if (ws_dev == nullptr && tokens > 0) return LS_ERR_INVALID_ARG;
+  size_t need = 0;
+  rc = ls_attention_grad_ws_bytes(m, tokens, heads, kv_heads, head_dim, &need);
+  if (rc != LS_OK) return rc;
+  if (ws_bytes < need || reinterpret_cast<uintptr_t>(ws_dev) % 256 != 0) return LS_ERR_STATE_SIZE;
+  if (tokens == 0) return LS_OK;
+  for (Tensor* t : {&a.dout, &a.q, &a.out, &a.dq}) settle(a, t, heads);
+  for (Tensor* t : {&a.k, &a.v, &a.dk, &a.dv}) settle(a, t, kv_heads);
+  a.dot = static_cast<float*>(ws_dev);
+  a.err = gop::device_error_word();
+  if (a.err == nullptr) return LS_ERR_CUDA;
+  return run(a, dtype, true, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LS_OK : LS_ERR_CUDA;
+}

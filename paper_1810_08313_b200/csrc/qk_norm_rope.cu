@@ -1,0 +1,453 @@
+// RMS norm of every head of q and k with the rotation by position in the same pass, and its gradient (ls_qk_norm_rope,
+// ls_qk_norm_rope_grad).
+//
+//   xhat = x * rstd,  rstd = 1 / sqrt(mean of x^2 over the head + eps),  z = xhat * w
+//   y: the pairs (z_a, z_b) of the first rot_dim elements turned by angle = position * inv_freq[pair], the rest as it is
+//   dz: the pairs of dy turned back;  dw = sum over rows and heads of dz * xhat;  t = dz * w,  dx = rstd (t - xhat <t xhat>)
+//
+// Bound by HBM: every element is read once and written once (backward: two read, one written).  A warp takes a token and all
+// its heads (or a part of them, where there are few tokens), so that the angles of a token are formed once: a lane keeps the
+// cosine and sine of its four pairs and the eight weights that belong to them in registers, and a head takes head_dim / 8
+// lanes, two heads of 128 a warp at a time, four such steps in flight.  Both elements of a pair lie in one lane, so the
+// turn needs no exchange; the sum over a head is a shuffle.  Angles are formed in double and reduced by whole turns there: a position of
+// 10^6 leaves an fp32 angle off by 6e-2, and the reduced one by 1e-10 before it is rounded to fp32.
+// Heads or rows that are no whole vectors are read element by element, pair l + 32 i in lane l.
+#include "ls_internal.h"
+
+#include <math.h>
+
+namespace ls {
+namespace {
+
+constexpr int kNrMaxDim = 256;
+constexpr int kNrWarps = 8;              // of a CTA
+
+struct NrTensor { const void* p; int64_t row, replica; };
+struct NrArgs {
+  NrTensor x[2], dy[2];                  // q, k
+  NrTensor out[2];                       // y, or dx
+  const float* w[2];
+  int64_t w_stride;
+  const double* inv_freq;
+  const int32_t* positions;              // [m][tokens]
+  float* part;                           // backward: [m][ctas][2][head_dim]
+  int64_t tokens;
+  int m, heads[2], head_dim, rot_dim;
+  int parts;                             // warps that share a token's heads
+  float eps;
+};
+
+// Where the four pairs of a lane are.  Vectors: A and B are runs of four elements; pairs are (A_i, B_i), or neighbours.
+struct Slots {
+  int a, b;                              // first elements of the runs (VEC), or unused
+  bool live;                             // the lane has elements
+};
+
+template <typename T, bool VEC, bool INTER>
+struct Row {
+  // lo[i], hi[i]: the pair i of this lane
+  static __device__ __forceinline__ void load(const T* p, const Slots& s, int lane, int hd, int rot, float (&lo)[4], float (&hi)[4]) {
+    if constexpr (VEC) {
+      float a[4], b[4];
+      load4(p + s.a, a);
+      load4(p + s.b, b);
+      if (INTER) {
+        lo[0] = a[0]; hi[0] = a[1]; lo[1] = a[2]; hi[1] = a[3];
+        lo[2] = b[0]; hi[2] = b[1]; lo[3] = b[2]; hi[3] = b[3];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { lo[i] = a[i]; hi[i] = b[i]; }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int x, y;
+        at(lane + 32 * i, hd, rot, x, y);
+        lo[i] = x < hd ? value(p[x]) : 0.f;
+        hi[i] = y < hd ? value(p[y]) : 0.f;
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(T* p, const Slots& s, int lane, int hd, int rot, const float (&lo)[4], const float (&hi)[4]) {
+    if constexpr (VEC) {
+      if (INTER) {
+        store4(p + s.a, lo[0], hi[0], lo[1], hi[1]);
+        store4(p + s.b, lo[2], hi[2], lo[3], hi[3]);
+      } else {
+        store4(p + s.a, lo[0], lo[1], lo[2], lo[3]);
+        store4(p + s.b, hi[0], hi[1], hi[2], hi[3]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int x, y;
+        at(lane + 32 * i, hd, rot, x, y);
+        if (x < hd) set(p[x], lo[i]);
+        if (y < hd) set(p[y], hi[i]);
+      }
+    }
+  }
+  // elements of pair p (hd: there is none)
+  static __device__ __forceinline__ void at(int p, int hd, int rot, int& x, int& y) {
+    const int half = rot / 2;
+    if (p < half) {
+      x = INTER ? 2 * p : p;
+      y = INTER ? x + 1 : p + half;
+    } else {
+      x = min(2 * p, hd);
+      y = min(2 * p + 1, hd);
+    }
+  }
+  static __device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
+    const float4 t = *reinterpret_cast<const float4*>(p);
+    v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+  }
+  static __device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&v)[4]) {
+    const uint2 t = *reinterpret_cast<const uint2*>(p);
+    v[0] = __uint_as_float(t.x << 16); v[1] = __uint_as_float(t.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(t.y << 16); v[3] = __uint_as_float(t.y & 0xFFFF0000u);
+  }
+  static __device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
+    *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+  }
+  static __device__ __forceinline__ void store4(__nv_bfloat16* p, float a, float b, float c, float d) {
+    const __nv_bfloat162 u = __floats2bfloat162_rn(a, b), v = __floats2bfloat162_rn(c, d);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
+  }
+  static __device__ __forceinline__ float value(float x) { return x; }
+  static __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
+  static __device__ __forceinline__ void set(float& p, float x) { p = x; }
+  static __device__ __forceinline__ void set(__nv_bfloat16& p, float x) { p = __float2bfloat16_rn(x); }
+};
+
+template <int LPR>
+__device__ __forceinline__ float head_sum(float x) {
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// cosines and sines of this lane's pairs at a position (1 and 0 for pairs that are not turned)
+template <bool VEC>
+__device__ __forceinline__ void angles(const double (&turns)[4], int position, float (&c)[4], float (&s)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const double t = (double)position * turns[i];
+    sincospif(2.f * (float)(t - rint(t)), &s[i], &c[i]);
+  }
+}
+
+// LPR lanes to a head, 32 / LPR heads of a token at a time, U such steps in flight.
+template <typename T, bool VEC, bool INTER, int LPR, bool GRAD>
+__global__ void __launch_bounds__(kNrWarps * 32)
+qk_norm_rope_kernel(const __grid_constant__ NrArgs a) {
+  using R = Row<T, VEC, INTER>;
+  constexpr int H = 32 / LPR, U = GRAD ? 2 : 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / LPR, slot = lane % LPR;
+  const int hd = a.head_dim, rot = a.rot_dim, half = rot / 2;
+  const int rep = blockIdx.y;
+  Slots s{};
+  s.live = true;
+  if (VEC) {
+    s.live = slot * 8 < hd;
+    const bool split = !INTER && slot * 4 < half;
+    s.a = split ? slot * 4 : slot * 8;
+    s.b = split ? half + slot * 4 : slot * 8 + 4;
+    if (!s.live) s.a = s.b = 0;
+  }
+  grid_dep_wait();
+  grid_dep_launch();
+  double turns[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int p = VEC ? slot * 4 + i : lane + 32 * i;
+    turns[i] = p < half && s.live ? a.inv_freq[p] * 0.15915494309189533577 : 0.0;
+  }
+  float wl[2][4], wh[2][4], dwl[2][4] = {}, dwh[2][4] = {};
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const float* w = a.w[t] + rep * a.w_stride;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int x, y;
+      Row<T, false, INTER>::at(VEC ? slot * 4 + i : lane + 32 * i, hd, rot, x, y);
+      if (VEC && !INTER && slot * 4 >= half) { x = s.a + i; y = s.b + i; }       // (the rest's pairs are (A_i, B_i), too)
+      wl[t][i] = s.live && x < hd ? w[x] : 0.f;
+      wh[t][i] = s.live && y < hd ? w[y] : 0.f;
+    }
+  }
+  const float inv = 1.f / (float)hd;
+  const int64_t units = a.tokens * a.parts;
+  for (int64_t u = (int64_t)blockIdx.x * kNrWarps + warp; u < units; u += (int64_t)gridDim.x * kNrWarps) {
+    const int64_t token = u / a.parts;
+    const int part = (int)(u - token * a.parts);
+    float c[4], sn[4];
+    angles<VEC>(turns, half > 0 ? a.positions[rep * a.tokens + token] : 0, c, sn);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const T* x = static_cast<const T*>(a.x[t].p) + rep * a.x[t].replica + token * a.x[t].row;
+      const T* dy = GRAD ? static_cast<const T*>(a.dy[t].p) + rep * a.dy[t].replica + token * a.dy[t].row : nullptr;
+      T* out = const_cast<T*>(static_cast<const T*>(a.out[t].p)) + rep * a.out[t].replica + token * a.out[t].row;
+      const int groups = (a.heads[t] + H - 1) / H;
+      const int g0 = (int)((int64_t)groups * part / a.parts), g1 = (int)((int64_t)groups * (part + 1) / a.parts);
+      for (int g = g0; g < g1; g += U) {
+        float lo[U][4], hi[U][4], gl[U][4], gh[U][4];
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+          const int head = (g + v) * H + sub;
+          const bool in = s.live && g + v < g1 && head < a.heads[t];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { lo[v][i] = hi[v][i] = 0.f; gl[v][i] = gh[v][i] = 0.f; }
+          if (in) {
+            R::load(x + head * hd, s, lane, hd, rot, lo[v], hi[v]);
+            if (GRAD) R::load(dy + head * hd, s, lane, hd, rot, gl[v], gh[v]);
+          }
+        }
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+          const int head = (g + v) * H + sub;
+          const bool in = s.live && g + v < g1 && head < a.heads[t];
+          float sq = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sq = fmaf(lo[v][i], lo[v][i], fmaf(hi[v][i], hi[v][i], sq));
+          const float rstd = 1.f / sqrtf(fmaf(head_sum<LPR>(sq), inv, a.eps));
+          if (!GRAD) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float p = lo[v][i] * rstd * wl[t][i], q = hi[v][i] * rstd * wh[t][i];
+              lo[v][i] = fmaf(p, c[i], -(q * sn[i]));
+              hi[v][i] = fmaf(p, sn[i], q * c[i]);
+            }
+          } else {
+            float along = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              lo[v][i] *= rstd;
+              hi[v][i] *= rstd;
+              const float p = fmaf(gl[v][i], c[i], gh[v][i] * sn[i]), q = fmaf(gh[v][i], c[i], -(gl[v][i] * sn[i]));
+              if (in) {                    // (outside, eps = 0 makes xhat 0 / 0)
+                dwl[t][i] = fmaf(p, lo[v][i], dwl[t][i]);
+                dwh[t][i] = fmaf(q, hi[v][i], dwh[t][i]);
+              }
+              gl[v][i] = p * wl[t][i];
+              gh[v][i] = q * wh[t][i];
+              along = fmaf(gl[v][i], lo[v][i], fmaf(gh[v][i], hi[v][i], along));
+            }
+            along = head_sum<LPR>(along) * inv;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              lo[v][i] = rstd * fmaf(-lo[v][i], along, gl[v][i]);
+              hi[v][i] = rstd * fmaf(-hi[v][i], along, gh[v][i]);
+            }
+          }
+          if (in) R::store(out + head * hd, s, lane, hd, rot, lo[v], hi[v]);
+        }
+      }
+    }
+  }
+  if constexpr (GRAD) {
+    // this CTA's part of dw: the lanes that share a pair, then the warps, in order
+    __shared__ float sum[kNrWarps][kNrMaxDim];
+    float* part = a.part + ((int64_t)rep * gridDim.x + blockIdx.x) * 2 * hd;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int o = LPR; o < 32; o <<= 1) {
+          dwl[t][i] += __shfl_xor_sync(0xffffffffu, dwl[t][i], o);
+          dwh[t][i] += __shfl_xor_sync(0xffffffffu, dwh[t][i], o);
+        }
+        int x, y;
+        Row<T, false, INTER>::at(VEC ? slot * 4 + i : lane + 32 * i, hd, rot, x, y);
+        if (VEC && !INTER && slot * 4 >= half) { x = s.a + i; y = s.b + i; }
+        if (sub == 0 && s.live) {
+          if (x < hd) sum[warp][x] = dwl[t][i];
+          if (y < hd) sum[warp][y] = dwh[t][i];
+        }
+      }
+      __syncthreads();
+      if ((int)threadIdx.x < hd) {
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < kNrWarps; ++w) total += sum[w][threadIdx.x];
+        part[t * hd + threadIdx.x] = total;
+      }
+    }
+  }
+}
+
+// dw = sum of the CTAs' parts, every 32nd by one warp, then the warps in order.  (Columns of dw_q and dw_k are one axis.)
+__global__ void __launch_bounds__(1024)
+qk_norm_fold_kernel(const float* __restrict__ part, int parts, int hd, float* __restrict__ dwq, float* __restrict__ dwk, int64_t stride) {
+  __shared__ float slice[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+  const int64_t rep = blockIdx.y;
+  grid_dep_wait();
+  grid_dep_launch();
+  float s = 0.f;
+  if (col < 2 * hd) {
+    const float* p = part + rep * parts * 2 * hd + col;
+#pragma unroll 8
+    for (int i = warp; i < parts; i += 32) s += __ldcg(p + (int64_t)i * 2 * hd);
+  }
+  slice[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && col < 2 * hd) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t += slice[i][lane];
+    if (col < hd) dwq[rep * stride + col] = t;
+    else dwk[rep * stride + col - hd] = t;
+  }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------
+
+// CTAs of a replica in the backward pass: its share of two an SM, and no more than there are warps' tokens for
+unsigned nr_ctas(int m, int64_t tokens) {
+  const int64_t most = (tokens + kNrWarps - 1) / kNrWarps;
+  int64_t n = (148 * 2 + m - 1) / m;
+  n = n > most ? most : n;
+  return (unsigned)(n < 1 ? 1 : n);
+}
+
+template <typename T, bool VEC, bool INTER, int LPR>
+cudaError_t nr_launch(NrArgs& a, bool grad, unsigned ctas, cudaStream_t st) {
+  if (grad) return launch_dep(qk_norm_rope_kernel<T, VEC, INTER, LPR, true>, dim3(ctas, (unsigned)a.m), dim3(kNrWarps * 32), 0, st, 1, a);
+  return launch_dep(qk_norm_rope_kernel<T, VEC, INTER, LPR, false>, dim3(ctas, (unsigned)a.m), dim3(kNrWarps * 32), 0, st, 1, a);
+}
+template <typename T, bool INTER>
+cudaError_t nr_pick(NrArgs& a, bool vec, bool grad, unsigned ctas, cudaStream_t st) {
+  if (!vec) return nr_launch<T, false, INTER, 32>(a, grad, ctas, st);
+  const int slots = a.head_dim / 8;
+  if (slots <= 4) return nr_launch<T, true, INTER, 4>(a, grad, ctas, st);
+  if (slots <= 8) return nr_launch<T, true, INTER, 8>(a, grad, ctas, st);
+  if (slots <= 16) return nr_launch<T, true, INTER, 16>(a, grad, ctas, st);
+  return nr_launch<T, true, INTER, 32>(a, grad, ctas, st);
+}
+
+int nr_check(int m, int64_t tokens, int heads, int kv_heads, int head_dim, int rot_dim, int dtype) {
+  if (m < 1 || tokens < 0 || heads < 1 || kv_heads < 1 || head_dim < 1 || rot_dim < 0 || rot_dim > head_dim || rot_dim % 2 != 0)
+    return LS_ERR_INVALID_ARG;
+  if (dtype != LS_DTYPE_FP32 && dtype != LS_DTYPE_BF16) return LS_ERR_INVALID_ARG;
+  if (m > 65535 || tokens > (1ll << 30) || heads > 65536 || kv_heads > 65536 || head_dim > kNrMaxDim) return LS_ERR_TOO_LARGE;
+  return LS_OK;
+}
+bool nr_bad(const NrArgs& a, const NrTensor& t, int heads, int dtype) {
+  const int64_t width = (int64_t)heads * a.head_dim;
+  if (reinterpret_cast<uintptr_t>(t.p) % (dtype == LS_DTYPE_BF16 ? 2 : 4) != 0) return true;
+  if (a.tokens == 0) return false;
+  if (t.p == nullptr || (a.tokens > 1 && t.row < width) || t.row > (1ll << 40) / a.tokens) return true;
+  return a.m > 1 && t.replica < (a.tokens - 1) * (a.tokens > 1 ? t.row : 0) + width;
+}
+// runs of four elements need every row of every tensor to start on their boundary, and the pairs to come in fours
+bool nr_vec(const NrArgs& a, int dtype, bool grad) {
+  if (a.head_dim % 8 != 0 || a.rot_dim % 8 != 0) return false;
+  const uintptr_t bytes = dtype == LS_DTYPE_BF16 ? 8 : 16;
+  for (int t = 0; t < 2; ++t)
+    for (const NrTensor* x : {&a.x[t], &a.out[t], grad ? &a.dy[t] : &a.x[t]})
+      if (reinterpret_cast<uintptr_t>(x->p) % bytes != 0 || (a.tokens > 1 && x->row % 4 != 0) || (a.m > 1 && x->replica % 4 != 0))
+        return false;
+  return true;
+}
+cudaError_t nr_run(NrArgs& a, int dtype, bool interleaved, bool grad, unsigned ctas, cudaStream_t st) {
+  const bool vec = nr_vec(a, dtype, grad);
+  if (dtype == LS_DTYPE_BF16)
+    return interleaved ? nr_pick<__nv_bfloat16, true>(a, vec, grad, ctas, st) : nr_pick<__nv_bfloat16, false>(a, vec, grad, ctas, st);
+  return interleaved ? nr_pick<float, true>(a, vec, grad, ctas, st) : nr_pick<float, false>(a, vec, grad, ctas, st);
+}
+bool nr_misaligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+}  // namespace
+}  // namespace ls
+
+extern "C" int ls_qk_norm_rope(const void* q_dev, const void* k_dev, const float* q_weight_dev, const float* k_weight_dev,
+                               const int32_t* positions_dev, const double* inv_freq_dev, int m, int64_t tokens, int heads,
+                               int kv_heads, int head_dim, int rot_dim, int interleaved, int64_t q_row, int64_t k_row,
+                               int64_t q_stride, int64_t k_stride, int64_t weight_stride, int dtype, float eps, void* q_out_dev,
+                               void* k_out_dev, int64_t q_out_row, int64_t k_out_row, int64_t q_out_stride, int64_t k_out_stride,
+                               void* cuda_stream) {
+  using namespace ls;
+  int rc = nr_check(m, tokens, heads, kv_heads, head_dim, rot_dim, dtype);
+  if (rc != LS_OK) return rc;
+  NrArgs a{};
+  a.m = m; a.tokens = tokens; a.heads[0] = heads; a.heads[1] = kv_heads; a.head_dim = head_dim; a.rot_dim = rot_dim; a.eps = eps;
+  a.x[0] = NrTensor{q_dev, q_row, q_stride};
+  a.x[1] = NrTensor{k_dev, k_row, k_stride};
+  a.out[0] = NrTensor{q_out_dev, q_out_row, q_out_stride};
+  a.out[1] = NrTensor{k_out_dev, k_out_row, k_out_stride};
+  a.w[0] = q_weight_dev; a.w[1] = k_weight_dev; a.w_stride = m > 1 ? weight_stride : 0;
+  a.positions = positions_dev; a.inv_freq = inv_freq_dev;
+  if (!(eps >= 0.f) || !isfinite(eps) || interleaved < 0 || interleaved > 1 || q_weight_dev == nullptr || k_weight_dev == nullptr ||
+      (m > 1 && weight_stride < head_dim) || (rot_dim > 0 && (positions_dev == nullptr || inv_freq_dev == nullptr)))
+    return LS_ERR_INVALID_ARG;
+  for (int t = 0; t < 2; ++t)
+    if (nr_bad(a, a.x[t], a.heads[t], dtype) || nr_bad(a, a.out[t], a.heads[t], dtype)) return LS_ERR_INVALID_ARG;
+  if (nr_misaligned(q_weight_dev, 4) || nr_misaligned(k_weight_dev, 4) || nr_misaligned(positions_dev, 4) || nr_misaligned(inv_freq_dev, 8))
+    return LS_ERR_INVALID_ARG;
+  if (tokens == 0) return LS_OK;
+  // few tokens: their heads are shared out over several warps, up to eight
+  a.parts = 1;
+  while (a.parts < 8 && m * tokens * a.parts < 148 * 16) a.parts *= 2;
+  const int64_t ctas = (tokens * a.parts + kNrWarps - 1) / kNrWarps;
+  return nr_run(a, dtype, interleaved != 0, false, (unsigned)ctas, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LS_OK : LS_ERR_CUDA;
+}
+
+extern "C" int ls_qk_norm_rope_grad_ws_bytes(int m, int64_t tokens, int head_dim, size_t* bytes) {
+  using namespace ls;
+  const int rc = nr_check(m, tokens, 1, 1, head_dim, 0, LS_DTYPE_FP32);
+  if (rc != LS_OK) return rc;
+  if (bytes == nullptr) return LS_ERR_INVALID_ARG;
+  *bytes = (size_t)m * nr_ctas(m, tokens) * 2 * (size_t)head_dim * sizeof(float);
+  return LS_OK;
+}
+
+extern "C" int ls_qk_norm_rope_grad(const void* dq_out_dev, const void* dk_out_dev, const void* q_dev, const void* k_dev,
+                                    const float* q_weight_dev, const float* k_weight_dev, const int32_t* positions_dev,
+                                    const double* inv_freq_dev, int m, int64_t tokens, int heads, int kv_heads, int head_dim,
+                                    int rot_dim, int interleaved, int64_t dq_out_row, int64_t dk_out_row, int64_t q_row, int64_t k_row,
+                                    int64_t dq_out_stride, int64_t dk_out_stride, int64_t q_stride, int64_t k_stride,
+                                    int64_t weight_stride, int dtype, float eps, void* dq_dev, void* dk_dev, int64_t dq_row,
+                                    int64_t dk_row, int64_t dq_stride, int64_t dk_stride, float* dq_weight_dev, float* dk_weight_dev,
+                                    int64_t dweight_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  using namespace ls;
+  int rc = nr_check(m, tokens, heads, kv_heads, head_dim, rot_dim, dtype);
+  if (rc != LS_OK) return rc;
+  NrArgs a{};
+  a.m = m; a.tokens = tokens; a.heads[0] = heads; a.heads[1] = kv_heads; a.head_dim = head_dim; a.rot_dim = rot_dim; a.eps = eps;
+  a.dy[0] = NrTensor{dq_out_dev, dq_out_row, dq_out_stride};
+  a.dy[1] = NrTensor{dk_out_dev, dk_out_row, dk_out_stride};
+  a.x[0] = NrTensor{q_dev, q_row, q_stride};
+  a.x[1] = NrTensor{k_dev, k_row, k_stride};
+  a.out[0] = NrTensor{dq_dev, dq_row, dq_stride};
+  a.out[1] = NrTensor{dk_dev, dk_row, dk_stride};
+  a.w[0] = q_weight_dev; a.w[1] = k_weight_dev; a.w_stride = m > 1 ? weight_stride : 0;
+  a.positions = positions_dev; a.inv_freq = inv_freq_dev;
+  if (!(eps >= 0.f) || !isfinite(eps) || interleaved < 0 || interleaved > 1 || q_weight_dev == nullptr || k_weight_dev == nullptr ||
+      dq_weight_dev == nullptr || dk_weight_dev == nullptr || ws_dev == nullptr ||
+      (m > 1 && (weight_stride < head_dim || dweight_stride < head_dim)) ||
+      (rot_dim > 0 && (positions_dev == nullptr || inv_freq_dev == nullptr)))
+    return LS_ERR_INVALID_ARG;
+  for (int t = 0; t < 2; ++t)
+    if (nr_bad(a, a.x[t], a.heads[t], dtype) || nr_bad(a, a.dy[t], a.heads[t], dtype) || nr_bad(a, a.out[t], a.heads[t], dtype))
+      return LS_ERR_INVALID_ARG;
+  if (nr_misaligned(q_weight_dev, 4) || nr_misaligned(k_weight_dev, 4) || nr_misaligned(positions_dev, 4) ||
+      nr_misaligned(inv_freq_dev, 8) || nr_misaligned(dq_weight_dev, 4) || nr_misaligned(dk_weight_dev, 4))
+    return LS_ERR_INVALID_ARG;
+  size_t need = 0;
+  rc = ls_qk_norm_rope_grad_ws_bytes(m, tokens, head_dim, &need);
+  if (rc != LS_OK) return rc;
+  if (ws_bytes < need || reinterpret_cast<uintptr_t>(ws_dev) % 256 != 0) return LS_ERR_STATE_SIZE;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  a.part = static_cast<float*>(ws_dev);
+  a.parts = 1;
+  const unsigned ctas = nr_ctas(m, tokens);
+  // (no tokens: the sums are those of no parts)
+  if (tokens > 0 && nr_run(a, dtype, interleaved != 0, true, ctas, st) != cudaSuccess) return LS_ERR_CUDA;
+  const cudaError_t e = launch_dep(qk_norm_fold_kernel, dim3((unsigned)((2 * head_dim + 31) / 32), (unsigned)m), dim3(1024), 0, st, 1,
+                                   static_cast<const float*>(a.part), tokens > 0 ? (int)ctas : 0, head_dim, dq_weight_dev,
+                                   dk_weight_dev, dweight_stride);
+  return e == cudaSuccess ? LS_OK : LS_ERR_CUDA;
+}
