@@ -533,6 +533,8 @@ int ls_qk_norm_rope_grad(const void* dq_out_dev, const void* dk_out_dev, const v
  * last) get out = 0 and lse = 0, and whatever they hold reaches no other row; nor does a NaN reach another sequence or an
  * earlier row of its own.  (Boundaries that do not ascend or leave [0, tokens] give wrong results, but no access outside.)
  * lse: float [m][heads][tokens], dense.  A row whose scores are all -inf, or one +inf, has no softmax: its out is NaN.
+ * bf16 on the tensor cores (head_dim a multiple of 8 up to 128, every row of every tensor on a 16-byte boundary, scale > 0):
+ * probabilities are rounded to bf16 as the operand of the second product, their sum is not.  Other calls run on the CUDA cores.
  * head_dim <= 256, tokens <= 2^30. */
 int ls_attention(const void* q_dev, const void* k_dev, const void* v_dev, const int32_t* seq_start_dev, int m, int64_t tokens,
                  int n_seqs, int heads, int kv_heads, int head_dim, int64_t q_row, int64_t k_row, int64_t v_row, int64_t q_stride,

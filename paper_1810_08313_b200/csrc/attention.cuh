@@ -1,4 +1,4 @@
-// What the attention kernels (attention_simt.cu) share: the arguments of a call, where the sequence of a
+// What the attention kernels (attention_simt.cu, attention_tc.cu) share: the arguments of a call, where the sequence of a
 // row starts and ends, and the rows computed one by one from the formulas.
 //
 //   s_ij = scale q_i . k_j  for start(i) <= j <= i,   p_i = softmax(s_i),   out_i = sum_j p_ij v_j,   lse_i = log sum_j exp s_ij
@@ -204,6 +204,11 @@ __device__ __noinline__ void dkv_row(const Args& a, int rep, int kvh, int j) {
   lane_store(head_ptr<T>(a.dk, rep, kvh, hd) + j * a.dk.row, hd, lane, dk, a.scale);
   lane_store(head_ptr<T>(a.dv, rep, kvh, hd) + j * a.dv.row, hd, lane, dv, 1.f);
 }
+
+// Whether the tensor-core kernels take a call: bf16, heads of whole 16 bytes up to 128 elements, every row on a 16-byte
+// boundary (TMA), and a positive scale (the running maximum is that of the products, and what is masked stays -inf).
+bool tc_takes(const Args& a, int dtype);
+cudaError_t tc_forward(const Args& a, cudaStream_t st);
 
 }  // namespace attn
 }  // namespace ls

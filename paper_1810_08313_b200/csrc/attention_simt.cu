@@ -1,4 +1,5 @@
-// Attention over packed sequences and its gradient on the CUDA cores (see attention.cuh for the formulas), and the entry points.
+// Attention over packed sequences and its gradient on the CUDA cores: fp32 tensors, and the bf16 ones that the tensor-core
+// kernels do not take (see attention.cuh for the formulas and attention_tc.cu for the others).  The entry points are here, too.
 //
 // One CTA of 256 threads per tile of 64 rows (32 for heads of more than 128) of one head; tiles of 64 keys pass through shared
 // memory once each, and scores never leave the SM.  Thread (ty, tx) of 16 x 16 has the rows ty R .. + R - 1 and the keys
@@ -460,7 +461,8 @@ extern "C" int ls_attention(const void* q_dev, const void* k_dev, const void* v_
   settle(a, &a.v, kv_heads);
   a.err = gop::device_error_word();
   if (a.err == nullptr) return LS_ERR_CUDA;
-  return run(a, dtype, false, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LS_OK : LS_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return (tc_takes(a, dtype) ? tc_forward(a, st) : run(a, dtype, false, st)) == cudaSuccess ? LS_OK : LS_ERR_CUDA;
 }
 
 extern "C" int ls_attention_grad_ws_bytes(int m, int64_t tokens, int heads, int kv_heads, int head_dim, size_t* bytes) {

@@ -65,6 +65,20 @@ int make_output_map(CUtensorMap* out, void* base, MapType type, int64_t rows, in
   return make_map(out, base, type, rows, cols, planes, ld, plane, row_bytes, 32, !transposed);
 }
 
+int make_heads_map(CUtensorMap* out, const void* base, int64_t head_dim, int64_t heads, int64_t tokens, int64_t m, int64_t row,
+                   int64_t replica, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return cudaErrorNotSupported;
+  cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)m};
+  cuuint64_t strides[3] = {(cuuint64_t)(head_dim * 2), (cuuint64_t)(row * 2), (cuuint64_t)(replica * 2)};
+  cuuint32_t box[4] = {64, 1, (cuuint32_t)box_rows, 1};
+  cuuint32_t es[4] = {1, 1, 1, 1};
+  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 }  // namespace gop
 }  // namespace ls
 

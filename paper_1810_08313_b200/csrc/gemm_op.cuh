@@ -709,6 +709,10 @@ int make_operand_map(CUtensorMap* out, const void* base, MapType type, int64_t r
                      int64_t plane, int box_rows = 64);
 int make_output_map(CUtensorMap* out, void* base, MapType type, int64_t rows, int64_t cols, int64_t planes, int64_t ld,
                     int64_t plane, int row_bytes, bool transposed = false);
+// A bf16 tensor [m][tokens][heads][head_dim] (distances in elements, 16-byte multiples) in boxes of 64 elements of a head x
+// box_rows tokens, 128-byte swizzle; coordinates (element, head, token, replica).
+int make_heads_map(CUtensorMap* out, const void* base, int64_t head_dim, int64_t heads, int64_t tokens, int64_t m, int64_t row,
+                   int64_t replica, int box_rows);
 // where a bounded wait that runs out is recorded (one word per device, read by ls_device_status); null on failure
 int* device_error_word();
 
