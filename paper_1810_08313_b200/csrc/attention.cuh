@@ -209,6 +209,7 @@ __device__ __noinline__ void dkv_row(const Args& a, int rep, int kvh, int j) {
 // boundary (TMA), and a positive scale (the running maximum is that of the products, and what is masked stays -inf).
 bool tc_takes(const Args& a, int dtype);
 cudaError_t tc_forward(const Args& a, cudaStream_t st);
+cudaError_t tc_backward(const Args& a, cudaStream_t st);
 
 }  // namespace attn
 }  // namespace ls

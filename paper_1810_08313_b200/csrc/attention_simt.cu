@@ -514,5 +514,6 @@ extern "C" int ls_attention_grad(const void* dout_dev, const void* q_dev, const 
   a.dot = static_cast<float*>(ws_dev);
   a.err = gop::device_error_word();
   if (a.err == nullptr) return LS_ERR_CUDA;
-  return run(a, dtype, true, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LS_OK : LS_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return (tc_takes(a, dtype) ? tc_backward(a, st) : run(a, dtype, true, st)) == cudaSuccess ? LS_OK : LS_ERR_CUDA;
 }

@@ -8,7 +8,8 @@
 //              the tensor core works for one while the other's softmax runs
 //   warps 2-5, 6-9   the softmax of a tile, a thread a row: 128 scores in registers, running maximum, exponentials, sum, P in
 //              bf16 back to tensor memory
-// A commit arrives when everything issued before it is complete, so S of a block also says that the PV before it is done.
+// A commit arrives when everything issued before it is complete, so S of a block also says that the PV before it is done: S is
+// issued only then, because it overwrites P.
 // O stays in tensor memory over all blocks and is rescaled only where a row's maximum has grown by more than 2^8 since its
 // reference was taken: P then lies below 2^8 instead of 1, which costs bf16 and fp32 no precision, and most blocks need no
 // pass over O.  P is rounded to bf16 (2^-8 of each term, signs at random), its sum is taken before the rounding.
@@ -64,7 +65,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   uint64_t* q_full = empty + SLOTS;      // [2]
   uint64_t* s_full = q_full + 2;         // [2] S of the next block is there, and the PV before it done
   uint64_t* p_ready = s_full + 2;        // [2] four warps have left P
-  uint64_t* o_done = p_ready + 2;        // [2] the last PV is done
+  uint64_t* o_done = p_ready + 2;        // [2] a PV is done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_done + 2);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -165,11 +166,14 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
 #pragma unroll
             for (int k = 0; k < kB / 16; ++k)
               mma_bf16_ts(to, ts + k * 8, make_smem_desc(vb + k * 2048, kB * 128, 1024), idesc_o, j - 1 > sp.lo || k > 0);
-            if (j - 1 == sp.hi) mma_commit(&o_done[x]);
+            mma_commit(&o_done[x]);
           }
           __syncwarp();
         }
         if (has_k && j >= sp.lo && j <= sp.hi) {
+          // S goes where P lies: the product that reads it has to be complete (products of other shapes or accumulators are not
+          // known to keep their order)
+          if (j > sp.lo && !__all_sync(0xffffffffu, mbar_wait(&o_done[x], (j - 1 - sp.lo) & 1))) { failed = true; break; }
           tc_fence_after_sync();
           if (lead) {
             const uint32_t qb = base + x * L::kTile, kb = base + L::kRing + kslot * L::kTile;
@@ -263,7 +267,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     }
     const bool none = start > row;       // in no sequence, or behind the tensor
     if (sp.lo <= sp.hi && !failed) {
-      if (!__all_sync(0xffffffffu, mbar_wait(&o_done[x], 0))) failed = true;
+      if (!__all_sync(0xffffffffu, mbar_wait(&o_done[x], (sp.hi - sp.lo) & 1))) failed = true;
       __syncwarp();
       tc_fence_after_sync();
     }
@@ -332,6 +336,644 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   }
 }
 
+// ---- backward ----------------------------------------------------------------------------------------------------
+//
+// Two kernels, so that no sum depends on an order of arrival and dq needs no fp32 copy in memory: seven products of a block
+// instead of five, scores and exponentials twice.  Both have a producer warp, a warp that issues the MMAs, and eight warps for
+// the elements, two a TMEM quadrant: half 0 has the columns 0-63 of a tile, half 1 the others.
+
+constexpr int kBwdThreads = 320;
+
+// the named barrier of the eight element warps
+__device__ __forceinline__ void elements_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// D += A B^T, both in shared memory, K-major, `ksteps` of 16
+template <int HD>
+__device__ __forceinline__ void product_ss(uint32_t d, uint32_t sa, uint32_t sb, uint32_t idesc, int ksteps) {
+#pragma unroll
+  for (int k = 0; k < HD / 16; ++k) {
+    if (k >= ksteps) break;
+    const uint32_t off = (k >> 2) * (kB * 128) + (k & 3) * 32;
+    mma_bf16(d, make_smem_desc(sa + off, 16, 1024), make_smem_desc(sb + off, 16, 1024), idesc, k > 0);
+  }
+}
+// D += A B, A 128 columns of bf16 in tensor memory (64 of them at `a`, the others `step` columns on), B [128][N] in shared memory
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t ta, uint32_t step, uint32_t sb, uint32_t idesc, bool add) {
+#pragma unroll
+  for (int k = 0; k < kB / 16; ++k)
+    mma_bf16_ts(d, ta + (k >> 2) * step + (k & 3) * 8, make_smem_desc(sb + k * 2048, kB * 128, 1024), idesc, add || k > 0);
+}
+
+// This warp's 32 rows of a result [128][HD] in tensor memory, times `by`, in bf16 into `box` (the rows' place in a tile of panels)
+// and out.  Half h of the columns.  Returns whether the lane's numbers are finite; `zero`: zeros instead.
+template <int HD>
+__device__ __forceinline__ bool result_rows(uint32_t ta, int half, int cols, bool any, bool zero, float by, uint8_t* box, int lane) {
+  bool fine = true;
+#pragma unroll
+  for (int g = 0; g < HD / 32; ++g) {
+    const int c = half * (HD / 2) + g * 16;
+    uint32_t o[16], w[8];
+    if (c < cols && any) {
+      tmem_ld_32x16(ta + c, o);
+      tmem_ld_wait();
+    }
+    if (c < cols && any && !zero) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float e = __uint_as_float(o[2 * i]) * by, f = __uint_as_float(o[2 * i + 1]) * by;
+        fine = fine && fabsf(e) < INFINITY && fabsf(f) < INFINITY;
+        w[i] = pack2(e, f);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = 0u;
+    }
+    uint8_t* panel = box + (c >> 6) * (kB * 128);
+    *gop::box_piece<128>(panel, lane, (c & 63) >> 3) = make_uint4(w[0], w[1], w[2], w[3]);
+    *gop::box_piece<128>(panel, lane, ((c & 63) >> 3) + 1) = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+  return fine;
+}
+
+// dq, a tile of 128 rows of one head: S = Q K^T and dP = dO V^T of the next block run while the elements of this one become
+// dS = P (dP - D), and dq += dS K follows.  S and dP are free as soon as they are in registers; dS, in bf16 (2^-8 of each term), has two
+// places of its own.  D is formed here from dout and out, and left for the other kernel.
+template <int HD>
+struct Dq {
+  static constexpr int kTile = kB * HD * 2;
+  static constexpr int kK = 3, kV = 2;                      // slots
+  static constexpr int kBars = (2 + kK + kV) * kTile;       // behind Q, dO, the K and V slots
+  static constexpr int kTotal = 1024 + kBars + 2 * kB * 4 + 16 + (2 * kK + 2 * kV + 8) * 8 + 16;
+  static constexpr uint32_t kS = 0, kP = 128, kO = 256, kDs = 384;
+};
+struct DqMaps { CUtensorMap q, dout, k, v, dq; };
+
+template <int HD>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constant__ Args a) {
+  using L = Dq<HD>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  float* dpart = reinterpret_cast<float*>(smem + L::kBars);          // [2][128]
+  uint32_t* bad = reinterpret_cast<uint32_t*>(dpart + 2 * kB);       // [4]
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(bad + 4);
+  uint64_t* k_empty = k_full + L::kK;
+  uint64_t* v_full = k_empty + L::kK;
+  uint64_t* v_empty = v_full + L::kV;
+  uint64_t* q_full = v_empty + L::kV;    // [2] Q, dO
+  uint64_t* s_full = q_full + 2;         // S and dP of a block
+  uint64_t* s_free = s_full + 1;         // eight warps have them in registers
+  uint64_t* ds_ready = s_free + 1;       // [2] eight warps have left dS (two, because a warp may be a block ahead of another)
+  uint64_t* done = ds_ready + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  uint8_t* sk = smem + 2 * L::kTile;
+  uint8_t* sv = sk + L::kK * L::kTile;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  bool failed = false;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < L::kK; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
+    for (int i = 0; i < L::kV; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
+    mbar_init(&q_full[0], 1);
+    mbar_init(&q_full[1], 1);
+    mbar_init(s_full, 1);
+    mbar_init(s_free, 8);
+    mbar_init(&ds_ready[0], 8);
+    mbar_init(&ds_ready[1], 8);
+    mbar_init(done, 1);
+    fence_mbar_init();
+    for (int i = 0; i < 4; ++i) bad[i] = 0u;
+    prefetch_tmap(&maps.q);
+    prefetch_tmap(&maps.k);
+    prefetch_tmap(&maps.v);
+    prefetch_tmap(&maps.dout);
+    prefetch_tmap(&maps.dq);
+  }
+  __syncwarp();
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  grid_dep_wait();
+  grid_dep_launch();
+
+  const int tiles = (int)((a.tokens + kB - 1) / kB);
+  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
+  const int r0 = (tiles - 1 - rest / a.m) * kB;
+  const int kvh = head / (a.heads / a.kv_heads);
+  const Span sp = key_blocks(a, rep, r0);
+  const int n = sp.hi - sp.lo + 1;       // blocks (none: n <= 0)
+  const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
+
+  if (warp == 0) {
+    const bool lead = elect_one();
+    const uint64_t pol = l2_policy(0);
+    auto load = [&](const CUtensorMap* m, uint8_t* dst, uint64_t* bar, int h, int token) {
+      mbar_expect_tx(bar, panels * kB * 128);
+      for (int c = 0; c < panels; ++c) tma_load_4d_hint(dst + c * kB * 128, m, bar, c * 64, h, token, rep, pol);
+    };
+    for (int i = 0; i < n && !failed; ++i) {
+      const int ks = i % L::kK, vs = i % L::kV;
+      if (i == 0 && lead) load(&maps.q, smem, &q_full[0], head, r0);
+      if (i >= L::kK && !__all_sync(0xffffffffu, mbar_wait(&k_empty[ks], (i / L::kK - 1) & 1))) { failed = true; break; }
+      if (lead) load(&maps.k, sk + ks * L::kTile, &k_full[ks], kvh, (sp.lo + i) * kB);
+      __syncwarp();
+      if (i == 0 && lead) load(&maps.dout, smem + L::kTile, &q_full[1], head, r0);
+      if (i >= L::kV && !__all_sync(0xffffffffu, mbar_wait(&v_empty[vs], (i / L::kV - 1) & 1))) { failed = true; break; }
+      if (lead) load(&maps.v, sv + vs * L::kTile, &v_full[vs], kvh, (sp.lo + i) * kB);
+      __syncwarp();
+    }
+    // the releases of the last slots arrive here: wait for them before leaving
+    for (int i = 0; i < L::kK && i < n && !failed; ++i)
+      if (!__all_sync(0xffffffffu, mbar_wait(&k_empty[i], ((n - 1 - i) / L::kK) & 1))) failed = true;
+    for (int i = 0; i < L::kV && i < n && !failed; ++i)
+      if (!__all_sync(0xffffffffu, mbar_wait(&v_empty[i], ((n - 1 - i) / L::kV) & 1))) failed = true;
+    if (failed && lane == 0) atomicExch(a.err, 44);
+  } else if (warp == 1) {
+    const bool lead = elect_one();
+    const uint32_t idesc_s = make_idesc(1, false, false, kB, kB);
+    const uint32_t idesc_o = make_idesc(1, false, true, kB, (uint32_t)cols);
+    const uint32_t qb = smem_u32(smem), gb = qb + L::kTile, kb = smem_u32(sk), vb = smem_u32(sv);
+    auto scores = [&](int i) {           // S and dP of block i
+      const int ks = i % L::kK, vs = i % L::kV;
+      bool got = mbar_wait(&k_full[ks], (i / L::kK) & 1);
+      if (i == 0) got = got && mbar_wait(&q_full[0], 0);
+      if (!__all_sync(0xffffffffu, got)) return false;
+      tc_fence_after_sync();
+      if (lead) product_ss<HD>(tmem + L::kS, qb, kb + ks * L::kTile, idesc_s, ksteps);
+      __syncwarp();
+      got = mbar_wait(&v_full[vs], (i / L::kV) & 1);
+      if (i == 0) got = got && mbar_wait(&q_full[1], 0);
+      if (!__all_sync(0xffffffffu, got)) return false;
+      tc_fence_after_sync();
+      if (lead) {
+        product_ss<HD>(tmem + L::kP, gb, vb + vs * L::kTile, idesc_s, ksteps);
+        mma_commit(s_full);
+        mma_commit(&v_empty[vs]);
+      }
+      __syncwarp();
+      return true;
+    };
+    if (n > 0 && !scores(0)) failed = true;
+    for (int i = 0; i < n && !failed; ++i) {
+      if (i + 1 < n) {
+        if (!__all_sync(0xffffffffu, mbar_wait(s_free, i & 1)) || !scores(i + 1)) { failed = true; break; }
+      }
+      if (!__all_sync(0xffffffffu, mbar_wait(&ds_ready[i & 1], (i >> 1) & 1))) { failed = true; break; }
+      tc_fence_after_sync();
+      if (lead) {
+        product_ts(tmem + L::kO, tmem + L::kDs + (i & 1) * 64, 32, kb + (i % L::kK) * L::kTile, idesc_o, i > 0);
+        mma_commit(&k_empty[i % L::kK]);
+        if (i == n - 1) mma_commit(done);
+      }
+      __syncwarp();
+    }
+    if (failed && lane == 0) atomicExch(a.err, 45);
+  } else {
+    const int half = (warp - 2) >> 2, q = warp & 3, r = q * 32 + lane, row = r0 + r;
+    const uint32_t lanes = (uint32_t)(q * 32) << 16;
+    const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens + row;
+    const int start = row_start(a, rep, row);
+    float part = 0.f, nl2 = 0.f;
+    if (row < a.tokens) {
+      const __nv_bfloat16* g = head_ptr<const __nv_bfloat16>(a.dout, rep, head, a.head_dim) + row * a.dout.row;
+      const __nv_bfloat16* o = head_ptr<const __nv_bfloat16>(a.out, rep, head, a.head_dim) + row * a.out.row;
+#pragma unroll
+      for (int c = 0; c < HD / 16; ++c) {
+        const int e = (2 * c + half) * 8;
+        if (e < a.head_dim) {
+          const uint4 x = __ldg(reinterpret_cast<const uint4*>(g + e)), y = __ldg(reinterpret_cast<const uint4*>(o + e));
+          const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            part = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), part);
+            part = fmaf(__uint_as_float(u[i] & 0xFFFF0000u), __uint_as_float(v[i] & 0xFFFF0000u), part);
+          }
+        }
+      }
+      nl2 = -a.lse[stat] * kLog2e;
+    }
+    dpart[half * kB + r] = part;
+    elements_sync();
+    const float dot = dpart[r] + dpart[kB + r];
+    if (half == 0 && row < a.tokens) a.dot[stat] = dot;
+    const float scale2 = a.scale * kLog2e;
+    for (int i = 0; i < n; ++i) {
+      if (!__all_sync(0xffffffffu, mbar_wait(s_full, i & 1))) { failed = true; break; }
+      __syncwarp();
+      tc_fence_after_sync();
+      uint32_t s[2][32], g[2][32];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) tmem_ld_32x32(tmem + L::kS + lanes + half * 64 + c * 32, s[c]);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) tmem_ld_32x32(tmem + L::kP + lanes + half * 64 + c * 32, g[c]);
+      tmem_ld_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_free);
+      const int at = (sp.lo + i) * kB + half * 64;
+      const int from = start - at, to = row - at;          // visible columns [from, to]
+      const bool cut = __any_sync(0xffffffffu, from > 0 || to < 63);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t w[16];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float p = ex2(fmaf(__uint_as_float(s[c][e]), scale2, nl2));
+          g[c][e] = __float_as_uint(p * (__uint_as_float(g[c][e]) - dot));
+        }
+        if (cut) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (c * 32 + e < from || c * 32 + e > to) g[c][e] = 0u;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = pack2(__uint_as_float(g[c][2 * e]), __uint_as_float(g[c][2 * e + 1]));
+        tmem_st_32x16(tmem + L::kDs + (i & 1) * 64 + lanes + half * 32 + c * 16, w);
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ds_ready[i & 1]);
+      __syncwarp();
+    }
+    if (n > 0 && !failed) {
+      if (!__all_sync(0xffffffffu, mbar_wait(done, 0))) failed = true;
+      __syncwarp();
+      tc_fence_after_sync();
+    }
+    if (failed && lane == 0) atomicExch(a.err, 46);
+    if (!failed && r0 + q * 32 < a.tokens) {
+      const bool none = start > row;
+      uint8_t* box = smem + q * 32 * 128;
+      const bool fine = result_rows<HD>(tmem + L::kO + lanes, half, cols, n > 0, none, a.scale, box, lane);
+      const uint32_t ill = __ballot_sync(0xffffffffu, !fine);
+      if (ill != 0u && lane == 0) atomicOr(&bad[q], ill);
+      fence_proxy_async_smem();
+    }
+    elements_sync();                     // (half a panel each, where there is one)
+    if (!failed && half == 0 && r0 + q * 32 < a.tokens) {
+      if (lane == 0) {
+        for (int c = 0; c < panels; ++c) store_heads(&maps.dq, smem + q * 32 * 128 + c * kB * 128, c * 64, head, r0 + q * 32, rep);
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+      }
+      __syncwarp();
+      uint32_t ill = bad[q];
+      while (ill != 0u) {
+        const int e = __ffs(ill) - 1;
+        ill &= ill - 1;
+        dq_row<__nv_bfloat16>(a, rep, head, r0 + q * 32 + e);
+      }
+    }
+    tc_fence_before_sync();
+  }
+  __syncwarp();
+  if (failed) {
+    // a wait ran out: give the loads in flight time to land before the shared memory is released
+    const long long t0 = clock64();
+    while (clock64() - t0 < 4000000ll) {}
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// dk and dv, a tile of 128 keys (rows of S^T = K Q^T and dP^T = V dO^T) over all tiles of queries of its group's heads.  The elements
+// take turns: while those of P are formed, dk of the step before and the next dP are; while those of dS are, dv of this step and
+// the next S.  Heads of 128 fill the tensor memory with S, dP, dk and dv: P takes the place of S there, and dS that of dP, so the
+// next S (dP) waits for the product that reads P (dS).  Smaller ones have places of their own for P and dS, which the elements
+// fill again when that product is done.  A key is seen by the queries from itself to the end of its sequence.  P and dS are
+// rounded to bf16 (2^-8 of each term).
+template <int HD>
+struct Dkv {
+  static constexpr int kTile = kB * HD * 2;
+  static constexpr int kQ = 3, kG = 2;                      // slots of Q and dO; the rows' lse and D have two
+  static constexpr int kStats = (2 + kQ + kG) * kTile;      // behind K, V, the Q and dO slots
+  static constexpr int kBars = kStats + 2 * 2 * kB * 4;
+  static constexpr int kTotal = kBars + 16 + (2 * kQ + 2 * kG + 8) * 8 + 16;
+  static constexpr bool kShared = HD == 128;                // P and dS in the places of S and dP
+  static constexpr uint32_t kS = 0, kDp = 128, kDk = 256, kDv = 256 + HD;
+  // the bf16 of P and dS: half h of the columns at + h * kHalf
+  static constexpr uint32_t kP = kShared ? kS : 384, kDs = kShared ? kDp : 448, kHalf = kShared ? 64 : 32;
+};
+struct DkvMaps { CUtensorMap q, dout, k, v, dk, dv; };
+
+template <int HD>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_constant__ Args a) {
+  using L = Dkv<HD>;
+  extern __shared__ __align__(1024) uint8_t smem[];                  // (no room to round its start up)
+  if ((smem_u32(smem) & 1023) != 0) {
+    if (threadIdx.x == 0) atomicExch(a.err, 40);
+    return;
+  }
+  float* stats = reinterpret_cast<float*>(smem + L::kStats);         // [slot][-lse * log2(e), D][128]
+  uint32_t* bad = reinterpret_cast<uint32_t*>(smem + L::kBars);      // [4]
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(bad + 4);
+  uint64_t* q_empty = q_full + L::kQ;
+  uint64_t* g_full = q_empty + L::kQ;
+  uint64_t* g_empty = g_full + L::kG;
+  uint64_t* kv_full = g_empty + L::kG;   // [2] K, V
+  uint64_t* st_full = kv_full + 2;       // [2] lse and D
+  uint64_t* s_full = st_full + 2;        // S of a step
+  uint64_t* dp_full = s_full + 1;
+  uint64_t* p_ready = dp_full + 1;       // eight warps have left P
+  uint64_t* ds_ready = p_ready + 1;      // ... and dS
+  uint64_t* done = ds_ready + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  uint8_t* sq = smem + 2 * L::kTile;
+  uint8_t* sg = sq + L::kQ * L::kTile;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  bool failed = false;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < L::kQ; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); }
+    for (int i = 0; i < L::kG; ++i) { mbar_init(&g_full[i], 1); mbar_init(&g_empty[i], 1); }
+    mbar_init(&kv_full[0], 1);
+    mbar_init(&kv_full[1], 1);
+    mbar_init(&st_full[0], 1);
+    mbar_init(&st_full[1], 1);
+    mbar_init(s_full, 1);
+    mbar_init(dp_full, 1);
+    mbar_init(p_ready, 8);
+    mbar_init(ds_ready, 8);
+    mbar_init(done, 1);
+    fence_mbar_init();
+    for (int i = 0; i < 4; ++i) bad[i] = 0u;
+    prefetch_tmap(&maps.q);
+    prefetch_tmap(&maps.k);
+    prefetch_tmap(&maps.v);
+    prefetch_tmap(&maps.dout);
+    prefetch_tmap(&maps.dk);
+    prefetch_tmap(&maps.dv);
+  }
+  __syncwarp();
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  grid_dep_wait();
+  grid_dep_launch();
+
+  // the keys with the most queries first
+  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, rep = rest % a.m;
+  const int kt = rest / a.m, k0 = kt * kB, group = a.heads / a.kv_heads;
+  const int end = last_query(a, rep, (int)min((int64_t)k0 + kB, a.tokens) - 1);
+  const int per = end > k0 ? (end - 1) / kB - kt + 1 : 0;            // tiles of queries of a head
+  const int n = per * group;
+  const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
+
+  if (warp == 0) {
+    const bool lead = elect_one();
+    const uint64_t pol = l2_policy(0);
+    auto load = [&](const CUtensorMap* m, uint8_t* dst, uint64_t* bar, int h, int token) {
+      mbar_expect_tx(bar, panels * kB * 128);
+      for (int c = 0; c < panels; ++c) tma_load_4d_hint(dst + c * kB * 128, m, bar, c * 64, h, token, rep, pol);
+    };
+    int head = kvh * group, tile = kt;
+    for (int i = 0; i < n && !failed; ++i) {
+      const int qs = i % L::kQ, gs = i % L::kG;
+      if (i == 0 && lead) load(&maps.k, smem, &kv_full[0], kvh, k0);
+      if (i >= L::kQ && !__all_sync(0xffffffffu, mbar_wait(&q_empty[qs], (i / L::kQ - 1) & 1))) { failed = true; break; }
+      if (lead) load(&maps.q, sq + qs * L::kTile, &q_full[qs], head, tile * kB);
+      __syncwarp();
+      if (i == 0 && lead) load(&maps.v, smem + L::kTile, &kv_full[1], kvh, k0);
+      if (i >= L::kG && !__all_sync(0xffffffffu, mbar_wait(&g_empty[gs], (i / L::kG - 1) & 1))) { failed = true; break; }
+      if (lead) load(&maps.dout, sg + gs * L::kTile, &g_full[gs], head, tile * kB);
+      __syncwarp();
+      // the rows' numbers, into the place of the step before the last, whose elements are done when its Q is let go of
+      const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens;
+      float l[kB / 32], d[kB / 32];
+#pragma unroll
+      for (int e = 0; e < kB / 32; ++e) {
+        const int row = tile * kB + e * 32 + lane;
+        const bool in = row < a.tokens;
+        l[e] = in ? -a.lse[stat + row] * kLog2e : 0.f;
+        d[e] = in ? a.dot[stat + row] : 0.f;
+      }
+      if (i >= 2 && !__all_sync(0xffffffffu, mbar_wait(&q_empty[(i - 2) % L::kQ], ((i - 2) / L::kQ) & 1))) { failed = true; break; }
+      float* st = stats + (i & 1) * 2 * kB;
+#pragma unroll
+      for (int e = 0; e < kB / 32; ++e) {
+        st[e * 32 + lane] = l[e];
+        st[kB + e * 32 + lane] = d[e];
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&st_full[i & 1]);
+      __syncwarp();
+      if (++tile == kt + per) { tile = kt; ++head; }
+    }
+    // the releases of the last slots arrive here: wait for them before leaving
+    for (int i = 0; i < L::kQ && i < n && !failed; ++i)
+      if (!__all_sync(0xffffffffu, mbar_wait(&q_empty[i], ((n - 1 - i) / L::kQ) & 1))) failed = true;
+    for (int i = 0; i < L::kG && i < n && !failed; ++i)
+      if (!__all_sync(0xffffffffu, mbar_wait(&g_empty[i], ((n - 1 - i) / L::kG) & 1))) failed = true;
+    if (failed && lane == 0) atomicExch(a.err, 47);
+  } else if (warp == 1) {
+    const bool lead = elect_one();
+    const uint32_t idesc_s = make_idesc(1, false, false, kB, kB);
+    const uint32_t idesc_o = make_idesc(1, false, true, kB, (uint32_t)cols);
+    const uint32_t kb = smem_u32(smem), vb = kb + L::kTile, qb = smem_u32(sq), gb = smem_u32(sg);
+    auto scores = [&](int i) {
+      const int qs = i % L::kQ;
+      bool got = mbar_wait(&q_full[qs], (i / L::kQ) & 1);
+      if (i == 0) got = got && mbar_wait(&kv_full[0], 0);
+      if (!__all_sync(0xffffffffu, got)) return false;
+      tc_fence_after_sync();
+      if (lead) {
+        product_ss<HD>(tmem + L::kS, kb, qb + qs * L::kTile, idesc_s, ksteps);
+        mma_commit(s_full);
+      }
+      __syncwarp();
+      return true;
+    };
+    auto dots = [&](int i) {
+      const int gs = i % L::kG;
+      bool got = mbar_wait(&g_full[gs], (i / L::kG) & 1);
+      if (i == 0) got = got && mbar_wait(&kv_full[1], 0);
+      if (!__all_sync(0xffffffffu, got)) return false;
+      tc_fence_after_sync();
+      if (lead) {
+        product_ss<HD>(tmem + L::kDp, vb, gb + gs * L::kTile, idesc_s, ksteps);
+        mma_commit(dp_full);
+      }
+      __syncwarp();
+      return true;
+    };
+    if (n > 0 && !(scores(0) && dots(0))) failed = true;
+    for (int i = 0; i < n && !failed; ++i) {
+      const int qs = i % L::kQ, gs = i % L::kG;
+      auto dv = [&]() {
+        if (lead) {
+          product_ts(tmem + L::kDv, tmem + L::kP, L::kHalf, gb + gs * L::kTile, idesc_o, i > 0);
+          mma_commit(&g_empty[gs]);
+        }
+        __syncwarp();
+      };
+      auto dk = [&]() {
+        if (lead) {
+          product_ts(tmem + L::kDk, tmem + L::kDs, L::kHalf, qb + qs * L::kTile, idesc_o, i > 0);
+          mma_commit(&q_empty[qs]);
+          if (i == n - 1) mma_commit(done);
+        }
+        __syncwarp();
+      };
+      if (!__all_sync(0xffffffffu, mbar_wait(p_ready, i & 1))) { failed = true; break; }
+      tc_fence_after_sync();
+      if (L::kShared) {
+        dv();
+        if (i + 1 < n && (!__all_sync(0xffffffffu, mbar_wait(&g_empty[gs], (i / L::kG) & 1)) || !scores(i + 1))) { failed = true; break; }
+      } else {
+        if (i + 1 < n && !scores(i + 1)) { failed = true; break; }
+        dv();
+      }
+      if (!__all_sync(0xffffffffu, mbar_wait(ds_ready, i & 1))) { failed = true; break; }
+      tc_fence_after_sync();
+      if (L::kShared) {
+        dk();
+        if (i + 1 < n && (!__all_sync(0xffffffffu, mbar_wait(&q_empty[qs], (i / L::kQ) & 1)) || !dots(i + 1))) { failed = true; break; }
+      } else {
+        if (i + 1 < n && !dots(i + 1)) { failed = true; break; }
+        dk();
+      }
+    }
+    if (failed && lane == 0) atomicExch(a.err, 48);
+  } else {
+    const int half = (warp - 2) >> 2, q = warp & 3, r = q * 32 + lane, key = k0 + r;
+    const uint32_t lanes = (uint32_t)(q * 32) << 16, mine = lanes + half * 64, left = lanes + half * L::kHalf;
+    const int seq_end = row_end(a, rep, key);
+    const float scale2 = a.scale * kLog2e;
+    int tile = kt;
+    for (int i = 0; i < n; ++i) {
+      const float* st = stats + (i & 1) * 2 * kB + half * 64;
+      const int at = tile * kB + half * 64;
+      const int from = key - at, to = seq_end - 1 - at;    // visible columns [from, to]
+      const bool cut = __any_sync(0xffffffffu, from > 0 || to < 63);
+      float p[64];
+      if (!__all_sync(0xffffffffu, mbar_wait(&st_full[i & 1], (i >> 1) & 1) && mbar_wait(s_full, i & 1))) { failed = true; break; }
+      __syncwarp();
+      tc_fence_after_sync();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t s[32], w[16];
+        tmem_ld_32x32(tmem + L::kS + mine + c * 32, s);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(st + c * 32 + e);
+          p[c * 32 + e] = ex2(fmaf(__uint_as_float(s[e]), scale2, l.x));
+          p[c * 32 + e + 1] = ex2(fmaf(__uint_as_float(s[e + 1]), scale2, l.y));
+          p[c * 32 + e + 2] = ex2(fmaf(__uint_as_float(s[e + 2]), scale2, l.z));
+          p[c * 32 + e + 3] = ex2(fmaf(__uint_as_float(s[e + 3]), scale2, l.w));
+        }
+        if (cut) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (c * 32 + e < from || c * 32 + e > to) p[c * 32 + e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = pack2(p[c * 32 + 2 * e], p[c * 32 + 2 * e + 1]);
+        if (!L::kShared && c == 0 && i > 0 && !__all_sync(0xffffffffu, mbar_wait(&g_empty[(i - 1) % L::kG], ((i - 1) / L::kG) & 1))) failed = true;
+        tmem_st_32x16(tmem + L::kP + left + c * 16, w);
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_ready);
+      if (failed) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(dp_full, i & 1))) { failed = true; break; }
+      __syncwarp();
+      tc_fence_after_sync();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t g[32], w[16];
+        tmem_ld_32x32(tmem + L::kDp + mine + c * 32, g);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          const float4 d = *reinterpret_cast<const float4*>(st + kB + c * 32 + e);
+          g[e] = __float_as_uint(p[c * 32 + e] * (__uint_as_float(g[e]) - d.x));
+          g[e + 1] = __float_as_uint(p[c * 32 + e + 1] * (__uint_as_float(g[e + 1]) - d.y));
+          g[e + 2] = __float_as_uint(p[c * 32 + e + 2] * (__uint_as_float(g[e + 2]) - d.z));
+          g[e + 3] = __float_as_uint(p[c * 32 + e + 3] * (__uint_as_float(g[e + 3]) - d.w));
+        }
+        if (cut) {                         // (0 times NaN)
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (c * 32 + e < from || c * 32 + e > to) g[e] = 0u;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = pack2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1]));
+        if (!L::kShared && c == 0 && i > 0 && !__all_sync(0xffffffffu, mbar_wait(&q_empty[(i - 1) % L::kQ], ((i - 1) / L::kQ) & 1))) failed = true;
+        tmem_st_32x16(tmem + L::kDs + left + c * 16, w);
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ds_ready);
+      if (failed) break;
+      __syncwarp();
+      if (++tile == kt + per) tile = kt;
+    }
+    if (n > 0 && !failed) {
+      if (!__all_sync(0xffffffffu, mbar_wait(done, 0))) failed = true;
+      __syncwarp();
+      tc_fence_after_sync();
+    }
+    if (failed && lane == 0) atomicExch(a.err, 49);
+    if (!failed && k0 + q * 32 < a.tokens) {
+      const bool none = seq_end <= key;
+      uint8_t* box = smem + q * 32 * 128;
+      bool fine = result_rows<HD>(tmem + L::kDk + lanes, half, cols, n > 0, none, a.scale, box, lane);
+      fine = result_rows<HD>(tmem + L::kDv + lanes, half, cols, n > 0, none, 1.f, box + L::kTile, lane) && fine;
+      const uint32_t ill = __ballot_sync(0xffffffffu, !fine);
+      if (ill != 0u && lane == 0) atomicOr(&bad[q], ill);
+      fence_proxy_async_smem();
+    }
+    elements_sync();
+    if (!failed && half == 0 && k0 + q * 32 < a.tokens) {
+      if (lane == 0) {
+        for (int c = 0; c < panels; ++c) {
+          store_heads(&maps.dk, smem + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
+          store_heads(&maps.dv, smem + L::kTile + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
+        }
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+      }
+      __syncwarp();
+      uint32_t ill = bad[q];
+      while (ill != 0u) {
+        const int e = __ffs(ill) - 1;
+        ill &= ill - 1;
+        dkv_row<__nv_bfloat16>(a, rep, kvh, k0 + q * 32 + e);
+      }
+    }
+    tc_fence_before_sync();
+  }
+  __syncwarp();
+  if (failed) {
+    // a wait ran out: give the loads in flight time to land before the shared memory is released
+    const long long t0 = clock64();
+    while (clock64() - t0 < 4000000ll) {}
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
 // ---- host side ---------------------------------------------------------------------------------------------------
 
 template <int HD>
@@ -342,6 +984,20 @@ cudaError_t launch_forward(const FwdMaps& maps, const Args& a, cudaStream_t st) 
   if (e != cudaSuccess) return e;
   const int64_t tiles = (a.tokens + 2 * kB - 1) / (2 * kB);
   return launch_dep(attention_tc_kernel<HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kFwdThreads), Fwd<HD>::kTotal, st, 1, maps, a);
+}
+
+template <int HD>
+cudaError_t launch_backward(const DqMaps& dq, const DkvMaps& dkv, const Args& a, cudaStream_t st) {
+  static uint64_t done[2] = {0, 0};      // one bit per device
+  static_assert(Dq<HD>::kTotal <= 227 * 1024 && Dkv<HD>::kTotal <= 227 * 1024, "shared memory budget");
+  cudaError_t e = allow_dynamic_smem(attention_dq_tc_kernel<HD>, Dq<HD>::kTotal, &done[0]);
+  if (e == cudaSuccess) e = allow_dynamic_smem(attention_dkv_tc_kernel<HD>, Dkv<HD>::kTotal, &done[1]);
+  const int64_t tiles = (a.tokens + kB - 1) / kB;
+  if (e == cudaSuccess)
+    e = launch_dep(attention_dq_tc_kernel<HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kBwdThreads), Dq<HD>::kTotal, st, 1, dq, a);
+  if (e == cudaSuccess)
+    e = launch_dep(attention_dkv_tc_kernel<HD>, dim3((unsigned)(tiles * a.kv_heads * a.m)), dim3(kBwdThreads), Dkv<HD>::kTotal, st, 1, dkv, a);
+  return e;
 }
 
 int head_map(CUtensorMap* map, const Args& a, const Tensor& t, int heads, int box_rows) {
@@ -366,6 +1022,21 @@ cudaError_t tc_forward(const Args& a, cudaStream_t st) {
       head_map(&maps.v, a, a.v, a.kv_heads, kB) != cudaSuccess || head_map(&maps.out, a, a.out, a.heads, 32) != cudaSuccess)
     return cudaErrorInvalidValue;
   return a.head_dim <= 64 ? launch_forward<64>(maps, a, st) : launch_forward<128>(maps, a, st);
+}
+
+cudaError_t tc_backward(const Args& a, cudaStream_t st) {
+  DqMaps dq;
+  DkvMaps dkv;
+  if (head_map(&dq.q, a, a.q, a.heads, kB) != cudaSuccess || head_map(&dq.dout, a, a.dout, a.heads, kB) != cudaSuccess ||
+      head_map(&dq.k, a, a.k, a.kv_heads, kB) != cudaSuccess || head_map(&dq.v, a, a.v, a.kv_heads, kB) != cudaSuccess ||
+      head_map(&dq.dq, a, a.dq, a.heads, 32) != cudaSuccess || head_map(&dkv.dk, a, a.dk, a.kv_heads, 32) != cudaSuccess ||
+      head_map(&dkv.dv, a, a.dv, a.kv_heads, 32) != cudaSuccess)
+    return cudaErrorInvalidValue;
+  dkv.q = dq.q;
+  dkv.dout = dq.dout;
+  dkv.k = dq.k;
+  dkv.v = dq.v;
+  return a.head_dim <= 64 ? launch_backward<64>(dq, dkv, a, st) : launch_backward<128>(dq, dkv, a, st);
 }
 
 }  // namespace attn
