@@ -38,48 +38,86 @@ struct Args {
   int* err;
 };
 
-// the number of boundaries that are <= t; t lies in sequence (this - 1) unless that is -1 or n_seqs
-__device__ __forceinline__ int bounds_upto(const int32_t* b, int n_seqs, int t) {
-  int lo = 0, hi = n_seqs + 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (b[mid] <= t) lo = mid + 1;
-    else hi = mid;
+// The boundaries of a replica's sequences, as a whole warp sees them: up to 32 are loaded once, one a lane, and searched with
+// ballots; more are searched 32 at a time.  (A binary search of 24 boundaries is six loads one after another, some 2 us of a CTA
+// that has 10 us of work.)  Whatever the boundaries hold, the results stay within the rows.
+struct Bounds {
+  const int32_t* b;                      // null: one sequence of all rows
+  int n, tokens;                         // sequences, rows
+  int held;                              // lane l: boundary l, or none
+
+  __device__ __forceinline__ Bounds(const Args& a, int rep) {
+    n = a.n_seqs;
+    tokens = (int)a.tokens;
+    b = a.seq_start == nullptr ? nullptr : a.seq_start + (int64_t)rep * (n + 1);
+    const int lane = threadIdx.x & 31;
+    held = b != nullptr && lane <= n ? b[lane] : 0x7fffffff;
   }
-  return lo;
-}
-// First row of the sequence of row t, or t + 1 if it is in none.  (Whatever the boundaries hold, 0 <= start <= t + 1.)
-__device__ __forceinline__ int row_start(const Args& a, int rep, int t) {
-  if (t >= a.tokens) return t + 1;
-  if (a.seq_start == nullptr) return 0;
-  const int32_t* b = a.seq_start + (int64_t)rep * (a.n_seqs + 1);
-  const int s = bounds_upto(b, a.n_seqs, t) - 1;
-  return s < 0 || s >= a.n_seqs ? t + 1 : min(max(b[s], 0), t);
-}
-// End of the sequence of row t, or t if it is in none.
-__device__ __forceinline__ int row_end(const Args& a, int rep, int t) {
-  const int tokens = (int)a.tokens;
-  if (t >= tokens) return t;
-  if (a.seq_start == nullptr) return tokens;
-  const int32_t* b = a.seq_start + (int64_t)rep * (a.n_seqs + 1);
-  const int s = bounds_upto(b, a.n_seqs, t) - 1;
-  return s < 0 || s >= a.n_seqs ? t : min(max(b[s + 1], t + 1), tokens);
-}
-// The first key that any row from t on needs (tokens if there is none).
-__device__ __forceinline__ int first_key(const Args& a, int rep, int t) {
-  const int tokens = (int)a.tokens;
-  if (a.seq_start == nullptr) return 0;
-  const int32_t* b = a.seq_start + (int64_t)rep * (a.n_seqs + 1);
-  const int s = bounds_upto(b, a.n_seqs, t) - 1;
-  return s >= a.n_seqs ? tokens : min(max(b[max(s, 0)], 0), tokens);
-}
-// The end of the rows that any key up to t is needed by (0 if there is none).
-__device__ __forceinline__ int last_query(const Args& a, int rep, int t) {
-  const int tokens = (int)a.tokens;
-  if (a.seq_start == nullptr) return tokens;
-  const int32_t* b = a.seq_start + (int64_t)rep * (a.n_seqs + 1);
-  const int s = bounds_upto(b, a.n_seqs, t) - 1;
-  return s < 0 ? 0 : min(max(b[min(s + 1, a.n_seqs)], 0), tokens);
+  __device__ __forceinline__ int at(int i) const { return n < 32 ? __shfl_sync(0xffffffffu, held, i) : b[i]; }
+  // the number of boundaries that are <= t (one t for the warp)
+  __device__ __forceinline__ int upto(int t) const {
+    if (n < 32) return __popc(__ballot_sync(0xffffffffu, held <= t));
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n + 1;
+    while (lo < hi) {
+      const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+      const int before = __popc(__ballot_sync(0xffffffffu, i < hi && b[min(i, n)] <= t));
+      if (step == 1) return lo + before;
+      if (before == 0) return lo;
+      hi = min(hi, lo + before * step);
+      lo += (before - 1) * step + 1;
+    }
+    return lo;
+  }
+  // The first key that any row from t on needs (tokens if there is none).
+  __device__ __forceinline__ int first_key(int t) const {
+    if (b == nullptr) return 0;
+    const int s = upto(t) - 1;
+    return s >= n ? tokens : min(max(at(max(s, 0)), 0), tokens);
+  }
+  // The end of the rows that any key up to t is needed by (0 if there is none).
+  __device__ __forceinline__ int last_query(int t) const {
+    if (b == nullptr) return tokens;
+    const int s = upto(t) - 1;
+    return s < 0 ? 0 : min(max(at(min(s + 1, n)), 0), tokens);
+  }
+  // The sequence of row t0 + lane: its rows are [start, end).  In none: start = row + 1, end = row.
+  __device__ __forceinline__ void rows(int t0, int* start, int* end) const {
+    const int lane = threadIdx.x & 31, t = t0 + lane;
+    if (b == nullptr) {
+      *start = t < tokens ? 0 : t + 1;
+      *end = t < tokens ? tokens : t;
+      return;
+    }
+    // one bit for each of the warp's rows that a boundary after t0 lies at, and the first boundary behind them
+    const int c = upto(t0);
+    uint32_t starts = 0;
+    int next = 0x7fffffff;
+    for (int i = c; ; i += 32) {
+      const int v = n < 32 ? held : i + lane <= n ? b[i + lane] : 0x7fffffff;
+      starts |= __reduce_or_sync(0xffffffffu, v > t0 && v - t0 < 32 ? 1u << (v - t0) : 0u);
+      next = min(next, __reduce_min_sync(0xffffffffu, v > t0 && v - t0 >= 32 ? v : 0x7fffffff));
+      if (n < 32 || i + 32 > n || next != 0x7fffffff) break;
+    }
+    const uint32_t upto_me = 0xffffffffu >> (31 - lane);
+    const uint32_t mine = starts & upto_me, later = starts & ~upto_me;
+    const int before = c > 0 ? at(c - 1) : 0, last = at(n);          // (the whole warp's, so not inside what lanes decide)
+    int s = mine != 0u ? t0 + 31 - __clz(mine) : before;
+    int e = later != 0u ? t0 + __ffs(later) - 1 : next;
+    const bool none = t >= tokens || (mine == 0u && c == 0) || t >= last;
+    s = none ? t + 1 : min(max(s, 0), t);
+    e = none ? t : min(max(e, t + 1), tokens);
+    *start = s;
+    *end = e;
+  }
+};
+// The same of one row, for the kernels' rare ways.
+__device__ __forceinline__ void row_bounds(const Args& a, int rep, int t, int* start, int* end) {
+  const Bounds bounds(a, rep);
+  int s, e;
+  bounds.rows(t, &s, &e);
+  *start = __shfl_sync(0xffffffffu, s, 0);
+  *end = __shfl_sync(0xffffffffu, e, 0);
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -123,7 +161,8 @@ __device__ __forceinline__ float lane_dot(const float (&x)[kLaneMost], const flo
 template <typename T>
 __device__ __noinline__ void forward_row(const Args& a, int rep, int head, int i) {
   const int lane = threadIdx.x & 31, hd = a.head_dim, kvh = head / (a.heads / a.kv_heads);
-  const int from = row_start(a, rep, i);
+  int from, end;
+  row_bounds(a, rep, i, &from, &end);
   float q[kLaneMost], x[kLaneMost], acc[kLaneMost] = {};
   lane_load(head_ptr<const T>(a.q, rep, head, hd) + i * a.q.row, hd, lane, q);
   const T* k = head_ptr<const T>(a.k, rep, kvh, hd);
@@ -156,7 +195,8 @@ __device__ __noinline__ void forward_row(const Args& a, int rep, int head, int i
 template <typename T>
 __device__ __noinline__ void dq_row(const Args& a, int rep, int head, int i) {
   const int lane = threadIdx.x & 31, hd = a.head_dim, kvh = head / (a.heads / a.kv_heads);
-  const int from = row_start(a, rep, i);
+  int from, end;
+  row_bounds(a, rep, i, &from, &end);
   const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens + i;
   float q[kLaneMost], g[kLaneMost], x[kLaneMost], y[kLaneMost], acc[kLaneMost] = {};
   lane_load(head_ptr<const T>(a.q, rep, head, hd) + i * a.q.row, hd, lane, q);
@@ -178,7 +218,8 @@ __device__ __noinline__ void dq_row(const Args& a, int rep, int head, int i) {
 template <typename T>
 __device__ __noinline__ void dkv_row(const Args& a, int rep, int kvh, int j) {
   const int lane = threadIdx.x & 31, hd = a.head_dim, group = a.heads / a.kv_heads;
-  const int end = row_end(a, rep, j);
+  int start, end;
+  row_bounds(a, rep, j, &start, &end);
   float k[kLaneMost], v[kLaneMost], x[kLaneMost], g[kLaneMost], dk[kLaneMost] = {}, dv[kLaneMost] = {};
   lane_load(head_ptr<const T>(a.k, rep, kvh, hd) + j * a.k.row, hd, lane, k);
   lane_load(head_ptr<const T>(a.v, rep, kvh, hd) + j * a.v.row, hd, lane, v);

@@ -154,9 +154,11 @@ attention_kernel(const __grid_constant__ Args a) {
   const int64_t r0 = (int64_t)(tiles - 1 - rest / a.m) * W::B;
   const int kvh = head / (a.heads / a.kv_heads);
   load_tile<T, HD>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd);
-  if (tid < W::B) {
+  const Bounds bounds(a, rep);
+  if (tid < W::B) {                        // (whole warps)
+    int end;
     bad[tid] = 0u;
-    start[tid] = row_start(a, rep, (int)r0 + tid);
+    bounds.rows((int)r0 + (tid & ~31), &start[tid], &end);
   }
   __syncthreads();
   const float scale2 = a.scale * kLog2e;
@@ -164,7 +166,7 @@ attention_kernel(const __grid_constant__ Args a) {
 #pragma unroll
   for (int r = 0; r < W::R; ++r) { top[r] = -INFINITY; sum[r] = 0.f; }
   const int64_t end = min(r0 + W::B, a.tokens);
-  for (int64_t j0 = first_key(a, rep, (int)r0) / W::B * W::B; j0 < end; j0 += W::B) {
+  for (int64_t j0 = bounds.first_key((int)r0) / W::B * W::B; j0 < end; j0 += W::B) {
     load_tile<T, HD>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd);
     load_tile<T, HD>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd);
     __syncthreads();
@@ -242,9 +244,11 @@ attention_dq_kernel(const __grid_constant__ Args a) {
   load_tile<T, HD>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd);
   load_tile<T, HD>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, r0, a.tokens, hd);
   load_tile<T, HD>(sk, head_ptr<const T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd);
-  if (tid < W::B) {
+  const Bounds bounds(a, rep);
+  if (tid < W::B) {                        // (whole warps)
+    int end;
     bad[tid] = 0u;
-    start[tid] = row_start(a, rep, (int)r0 + tid);
+    bounds.rows((int)r0 + (tid & ~31), &start[tid], &end);
   }
   __syncthreads();
   float lse2[W::R], dot[W::R];
@@ -261,7 +265,7 @@ attention_dq_kernel(const __grid_constant__ Args a) {
   const float scale2 = a.scale * kLog2e;
   float acc[W::R][W::C] = {};
   const int64_t end = min(r0 + W::B, a.tokens);
-  for (int64_t j0 = first_key(a, rep, (int)r0) / W::B * W::B; j0 < end; j0 += W::B) {
+  for (int64_t j0 = bounds.first_key((int)r0) / W::B * W::B; j0 < end; j0 += W::B) {
     load_tile<T, HD>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd);
     load_tile<T, HD>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd);
     __syncthreads();
@@ -323,7 +327,8 @@ attention_dkv_kernel(const __grid_constant__ Args a) {
   if (tid < W::B) bad[tid] = 0u;
   const float scale2 = a.scale * kLog2e;
   float dk[W::R][W::C] = {}, dv[W::R][W::C] = {};
-  const int64_t end = last_query(a, rep, (int)min(k0 + W::B, a.tokens) - 1);
+  const Bounds bounds(a, rep);
+  const int64_t end = bounds.last_query((int)min(k0 + W::B, a.tokens) - 1);
   for (int head = kvh * group; head < (kvh + 1) * group; ++head) {
     const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens;
     for (int64_t i0 = k0; i0 < end; i0 += W::B) {
@@ -334,7 +339,8 @@ attention_dkv_kernel(const __grid_constant__ Args a) {
         const bool in = i0 + tid < a.tokens;
         lse2[tid] = in ? a.lse[stat + i0 + tid] * kLog2e : 0.f;
         dot[tid] = in ? a.dot[stat + i0 + tid] : 0.f;
-        start[tid] = row_start(a, rep, (int)i0 + tid);
+        int stop;
+        bounds.rows((int)i0 + (tid & ~31), &start[tid], &stop);
       }
       __syncthreads();
       float s[W::R][W::R], g[W::R][W::R];

@@ -30,7 +30,7 @@ struct Fwd {
   static constexpr int kSlots = HD == 128 ? 4 : 6;
   static constexpr int kRing = 2 * kTile;                   // offset of the ring, behind Q
   static constexpr int kBars = kRing + kSlots * kTile;
-  static constexpr int kTotal = 1024 + kBars + (2 * kSlots + 8) * 8 + 16;
+  static constexpr int kTotal = 1024 + kBars + (2 * kSlots + 10) * 8 + 16;
   static constexpr uint32_t kO = 256;                       // first TMEM column of O (tile X: + X HD); S: 0 and 128
 };
 
@@ -39,11 +39,38 @@ struct FwdMaps { CUtensorMap q, k, v, out; };
 __device__ __forceinline__ float ex2(float x) { return gop::ex2(x); }
 __device__ __forceinline__ uint32_t pack2(float a, float b) { return gop::pack_bf16(a, b); }
 
+// two fp32 numbers in one instruction, each rounded as on its own
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t two(uint32_t a, uint32_t b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float2 parts(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // key blocks [lo, hi] that the tile of rows from r0 on needs (lo > hi: none)
 struct Span { int lo, hi; };
-__device__ __forceinline__ Span key_blocks(const Args& a, int rep, int r0) {
-  if (r0 >= a.tokens) return Span{1, 0};
-  return Span{first_key(a, rep, r0) / kB, r0 / kB};
+__device__ __forceinline__ Span key_blocks(const Bounds& b, int r0) {
+  if (r0 >= b.tokens) return Span{1, 0};
+  return Span{b.first_key(r0) / kB, r0 / kB};
 }
 
 __device__ __forceinline__ void store_heads(const CUtensorMap* m, const void* src, int x, int head, int token, int rep) {
@@ -51,6 +78,12 @@ __device__ __forceinline__ void store_heads(const CUtensorMap* m, const void* sr
                    reinterpret_cast<uint64_t>(m)),
                "r"(smem_u32(src)), "r"(x), "r"(head), "r"(token), "r"(rep)
                : "memory");
+}
+
+// This thread's bulk stores have read their shared memory; or, where their rows are to be written once more, are complete.
+__device__ __forceinline__ void stores_read(bool complete) {
+  if (complete) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
 template <int HD>
@@ -64,7 +97,8 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   uint64_t* empty = full + SLOTS;
   uint64_t* q_full = empty + SLOTS;      // [2]
   uint64_t* s_full = q_full + 2;         // [2] S of the next block is there, and the PV before it done
-  uint64_t* p_ready = s_full + 2;        // [2] four warps have left P
+  uint64_t* p_half = s_full + 2;         // [2] four warps have left P of the first 64 keys
+  uint64_t* p_ready = p_half + 2;        // [2] ... of all
   uint64_t* o_done = p_ready + 2;        // [2] a PV is done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_done + 2);
 
@@ -72,7 +106,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   bool failed = false;
   if (threadIdx.x == 0) {
     for (int s = 0; s < SLOTS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int x = 0; x < 2; ++x) { mbar_init(&q_full[x], 1); mbar_init(&s_full[x], 1); mbar_init(&p_ready[x], 4); mbar_init(&o_done[x], 1); }
+    for (int x = 0; x < 2; ++x) { mbar_init(&q_full[x], 1); mbar_init(&s_full[x], 1); mbar_init(&p_half[x], 4); mbar_init(&p_ready[x], 4); mbar_init(&o_done[x], 1); }
     fence_mbar_init();
     prefetch_tmap(&maps.q);
     prefetch_tmap(&maps.k);
@@ -96,7 +130,8 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
   const int r0 = (tiles - 1 - rest / a.m) * 2 * kB;
   const int kvh = head / (a.heads / a.kv_heads);
-  const Span sa = key_blocks(a, rep, r0), sb = key_blocks(a, rep, r0 + kB);
+  const Bounds bounds(a, rep);
+  const Span sa = key_blocks(bounds, r0), sb = key_blocks(bounds, r0 + kB);
   const bool has_a = sa.lo <= sa.hi, has_b = sb.lo <= sb.hi;
   const int lo = has_a ? sa.lo : sb.lo, hi = has_b ? sb.hi : sa.hi;        // (lo > hi if neither has any)
   const int panels = (a.head_dim + 63) / 64;
@@ -159,16 +194,21 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
         const Span sp = x == 0 ? sa : sb;
         const uint32_t ts = tmem + x * kB, to = tmem + L::kO + x * HD;
         if (has_v && j - 1 >= sp.lo && j - 1 <= sp.hi) {
-          if (!__all_sync(0xffffffffu, mbar_wait(&p_ready[x], (j - 1 - sp.lo) & 1))) { failed = true; break; }
-          tc_fence_after_sync();
-          if (lead) {
-            const uint32_t vb = base + L::kRing + vslot * L::kTile;
+          const uint32_t vb = base + L::kRing + vslot * L::kTile;
+          for (int h = 0; h < 2; ++h) {
+            if (!__all_sync(0xffffffffu, mbar_wait(h == 0 ? &p_half[x] : &p_ready[x], (j - 1 - sp.lo) & 1))) { failed = true; break; }
+            tc_fence_after_sync();
+            if (lead) {
 #pragma unroll
-            for (int k = 0; k < kB / 16; ++k)
-              mma_bf16_ts(to, ts + k * 8, make_smem_desc(vb + k * 2048, kB * 128, 1024), idesc_o, j - 1 > sp.lo || k > 0);
-            mma_commit(&o_done[x]);
+              for (int e = 0; e < kB / 32; ++e) {
+                const int k = h * (kB / 32) + e;
+                mma_bf16_ts(to, ts + k * 8, make_smem_desc(vb + k * 2048, kB * 128, 1024), idesc_o, j - 1 > sp.lo || k > 0);
+              }
+              if (h == 1) mma_commit(&o_done[x]);
+            }
+            __syncwarp();
           }
-          __syncwarp();
+          if (failed) break;
         }
         if (has_k && j >= sp.lo && j <= sp.hi) {
           // S goes where P lies: the product that reads it has to be complete (products of other shapes or accumulators are not
@@ -198,7 +238,8 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     const int x = (warp - 2) >> 2, q = warp & 3;
     const Span sp = x == 0 ? sa : sb;
     const int row = r0 + x * kB + q * 32 + lane;
-    const int start = row_start(a, rep, row);
+    int start, end;
+    bounds.rows(r0 + x * kB + q * 32, &start, &end);
     const uint32_t ts = tmem + ((uint32_t)(q * 32) << 16) + x * kB;
     const uint32_t to = tmem + ((uint32_t)(q * 32) << 16) + L::kO + x * HD;
     const float scale2 = a.scale * kLog2e;
@@ -220,12 +261,17 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
           for (int i = 0; i < 32; ++i)
             if (c * 32 + i < from || c * 32 + i > to_col) s[c][i] = 0xff800000u;
       }
-      float most = -INFINITY;
+      // eight chains: one would take a row's 128 scores one after another
+      float m8[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m8[i] = __uint_as_float(s[0][i]);
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int i = 0; i < 32; i += 2)
-          most = fmaxf(most, fmaxf(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])));
+        for (int i = 0; i < 32; i += 16)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m8[e] = fmaxf(fmaxf(m8[e], __uint_as_float(s[c][i + e])), __uint_as_float(s[c][i + 8 + e]));
+      const float most = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])), fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
       // (top = -inf: the difference is infinite, and the factor zero)
       const bool far = most > top && (most - top) * scale2 > 8.f;
       if (__any_sync(0xffffffffu, far)) {
@@ -245,24 +291,29 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
         }
       }
       const float ref = top == -INFINITY ? 0.f : top * scale2;
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint64_t by2 = two(scale2, scale2), ref2 = two(-ref, -ref);
+      uint64_t part[2] = {0, 0};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         uint32_t p[16];
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-          const float e = ex2(fmaf(__uint_as_float(s[c][i]), scale2, -ref)), f = ex2(fmaf(__uint_as_float(s[c][i + 1]), scale2, -ref));
-          part[i & 2] += e;
-          part[(i & 2) + 1] += f;
-          p[i >> 1] = pack2(e, f);
+          float2 e = parts(fma2(two(s[c][i], s[c][i + 1]), by2, ref2));
+          e.x = ex2(e.x);
+          e.y = ex2(e.y);
+          part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], two(e.x, e.y));
+          p[i >> 1] = pack2(e.x, e.y);
         }
         tmem_st_32x16(ts + c * 16, p);
+        if (c & 1) {                       // PV may start with the first half of the keys
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(c == 1 ? &p_half[x] : &p_ready[x]);
+        }
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
-      tmem_st_wait();
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&p_ready[x]);
+      const float2 total = parts(add2(part[0], part[1]));
+      sum += total.x + total.y;
       __syncwarp();
     }
     const bool none = start > row;       // in no sequence, or behind the tensor
@@ -309,12 +360,13 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       if (lane == 0) {
         for (int c = 0; c < panels; ++c) store_heads(&maps.out, box + c * kB * 128, c * 64, head, r0 + x * kB + q * 32, rep);
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
       }
       if (row < a.tokens)
         a.lse[((int64_t)rep * a.heads + head) * a.tokens + row] = none ? 0.f : fmaf(top * scale2, kLn2, logf(sum));
       __syncwarp();
       uint32_t bad = __ballot_sync(0xffffffffu, !none && !fine);
+      if (lane == 0) stores_read(bad != 0u);
+      __syncwarp();
       while (bad != 0u) {
         const int r = __ffs(bad) - 1;
         bad &= bad - 1;
@@ -465,7 +517,8 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
   const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
   const int r0 = (tiles - 1 - rest / a.m) * kB;
   const int kvh = head / (a.heads / a.kv_heads);
-  const Span sp = key_blocks(a, rep, r0);
+  const Bounds bounds(a, rep);
+  const Span sp = key_blocks(bounds, r0);
   const int n = sp.hi - sp.lo + 1;       // blocks (none: n <= 0)
   const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
 
@@ -537,7 +590,8 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     const int half = (warp - 2) >> 2, q = warp & 3, r = q * 32 + lane, row = r0 + r;
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens + row;
-    const int start = row_start(a, rep, row);
+    int start, end;
+    bounds.rows(r0 + q * 32, &start, &end);
     float part = 0.f, nl2 = 0.f;
     if (row < a.tokens) {
       const __nv_bfloat16* g = head_ptr<const __nv_bfloat16>(a.dout, rep, head, a.head_dim) + row * a.dout.row;
@@ -620,7 +674,7 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
       if (lane == 0) {
         for (int c = 0; c < panels; ++c) store_heads(&maps.dq, smem + q * 32 * 128 + c * kB * 128, c * 64, head, r0 + q * 32, rep);
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        stores_read(bad[q] != 0u);
       }
       __syncwarp();
       uint32_t ill = bad[q];
@@ -729,7 +783,8 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
   // the keys with the most queries first
   const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, rep = rest % a.m;
   const int kt = rest / a.m, k0 = kt * kB, group = a.heads / a.kv_heads;
-  const int end = last_query(a, rep, (int)min((int64_t)k0 + kB, a.tokens) - 1);
+  const Bounds bounds(a, rep);
+  const int end = bounds.last_query((int)min((int64_t)k0 + kB, a.tokens) - 1);
   const int per = end > k0 ? (end - 1) / kB - kt + 1 : 0;            // tiles of queries of a head
   const int n = per * group;
   const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
@@ -852,7 +907,8 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
   } else {
     const int half = (warp - 2) >> 2, q = warp & 3, r = q * 32 + lane, key = k0 + r;
     const uint32_t lanes = (uint32_t)(q * 32) << 16, mine = lanes + half * 64, left = lanes + half * L::kHalf;
-    const int seq_end = row_end(a, rep, key);
+    int start, seq_end;
+    bounds.rows(k0 + q * 32, &start, &seq_end);
     const float scale2 = a.scale * kLog2e;
     int tile = kt;
     for (int i = 0; i < n; ++i) {
@@ -949,7 +1005,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
           store_heads(&maps.dv, smem + L::kTile + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
         }
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        stores_read(bad[q] != 0u);
       }
       __syncwarp();
       uint32_t ill = bad[q];
