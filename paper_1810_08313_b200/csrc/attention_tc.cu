@@ -3,11 +3,13 @@
 // Forward.  A CTA takes 256 consecutive rows of one head as two tiles of 128 (rows of S are TMEM lanes) and passes over the keys in
 // blocks of 128, once:
 //   warp 0     TMA producer: both tiles of Q, then K and V blocks through a ring
-//   warp 1     issues the MMAs: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory, where it
-//              takes the place of S).  Per block and tile: PV of the block before, then S of this one; the tiles alternate, so that
-//              the tensor core works for one while the other's softmax runs
-//   warps 2-5, 6-9   the softmax of a tile, a thread a row: 128 scores in registers, running maximum, exponentials, sum, P in
-//              bf16 back to tensor memory
+//   warps 1, 2 issue the MMAs of a tile: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory, where it
+//              takes the place of S).  Per block: PV of the block before, then S of this one
+//   warps 3-6, 7-10   the softmax of a tile, a thread a row: 128 scores in registers, maximum, exponentials, sum, P in bf16 back
+//              to tensor memory in two halves, on the first of which PV starts
+// The tensor core works for one tile while the other's softmax runs.  For that the two have to stay half a block apart: S of a tile
+// waits until the other one is past its maxima.  (Without, both end in step: 994 us instead of 945 for 16384 rows of 16
+// heads of 128.  With two threads a row, and twice the warps: 1013 us.)
 // A commit arrives when everything issued before it is complete, so S of a block also says that the PV before it is done: S is
 // issued only then, because it overwrites P.
 // O stays in tensor memory over all blocks and is rescaled only where a row's maximum has grown by more than 2^8 since its
@@ -22,15 +24,15 @@ namespace {
 using namespace ptx;
 
 constexpr int kB = 128;                  // rows of a tile, keys of a block
-constexpr int kFwdThreads = 320;
+constexpr int kFwdThreads = 352;
 
 template <int HD>
 struct Fwd {
   static constexpr int kTile = kB * HD * 2;                 // bytes: HD / 64 panels of 128 rows x 128 bytes
-  static constexpr int kSlots = HD == 128 ? 4 : 6;
+  static constexpr int kSlots = HD == 128 ? 2 : 3;          // of a K and a V block
   static constexpr int kRing = 2 * kTile;                   // offset of the ring, behind Q
-  static constexpr int kBars = kRing + kSlots * kTile;
-  static constexpr int kTotal = 1024 + kBars + (2 * kSlots + 10) * 8 + 16;
+  static constexpr int kBars = kRing + kSlots * 2 * kTile;
+  static constexpr int kTotal = 1024 + kBars + (2 * kSlots + 12) * 8 + 16;
   static constexpr uint32_t kO = 256;                       // first TMEM column of O (tile X: + X HD); S: 0 and 128
 };
 
@@ -66,6 +68,36 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 2^x of two numbers on the FMA units (Cody and Waite's reduction: x = n + f, |f| <= 1/2, and a polynomial of degree 5 for 2^f,
+// fitted to the least relative error, 9e-8, 1.9e-7 with its roundings).  x of -127 or less, -inf included, gives 0, and
+// between that and -126 something below the smallest normal number.  No infinities, no NaN.
+__device__ __forceinline__ float2 exp2_fma(uint64_t x2) {
+  float2 x = parts(x2);
+  x.x = fmaxf(x.x, -127.f);
+  x.y = fmaxf(x.y, -127.f);
+  x2 = two(x.x, x.y);
+  constexpr float kRound = 12582912.f;   // 1.5 * 2^23: the sum's last bits are the nearest whole number
+  const uint64_t t = add2(x2, two(kRound, kRound));
+  const uint64_t f = add2(x2, fma2(t, two(-1.f, -1.f), two(kRound, kRound)));
+  uint64_t p = fma2(f, two(0.001326472731307149f, 0.001326472731307149f), two(0.009671512991189957f, 0.009671512991189957f));
+  p = fma2(p, f, two(0.05550733581185341f, 0.05550733581185341f));
+  p = fma2(p, f, two(0.24022242426872253f, 0.24022242426872253f));
+  p = fma2(p, f, two(0.6931470036506653f, 0.6931470036506653f));
+  p = fma2(p, f, two(1.f, 1.f));
+  const float2 n = parts(t), y = parts(p);
+  return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(n.x) << 23)),
+                     __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23)));
+}
+// Which of 16 pairs of exponentials the FMA units take.  The special-function unit's 16 a clock and SM take as long as the tensor
+// cores' two products of a 128 x 128 block with heads of 128, but every instruction of a softmax thread is on the critical
+// path, and the polynomial has more: 16384 rows of 16 heads took 979 us with none, 893 us with three, 920 us with five.
+constexpr uint32_t kFmaOf16 = 0x1084;
+
 // key blocks [lo, hi] that the tile of rows from r0 on needs (lo > hi: none)
 struct Span { int lo, hi; };
 __device__ __forceinline__ Span key_blocks(const Bounds& b, int r0) {
@@ -78,6 +110,33 @@ __device__ __forceinline__ void store_heads(const CUtensorMap* m, const void* sr
                    reinterpret_cast<uint64_t>(m)),
                "r"(smem_u32(src)), "r"(x), "r"(head), "r"(token), "r"(rep)
                : "memory");
+}
+
+// Operands are tiles of 128 rows in panels of 64 columns (128 bytes a row, 128-byte swizzle, a panel 16 KB), given by the low words
+// of their descriptors: K-major (row = M or N) or MN-major (row = K).
+constexpr uint32_t kDescHi = smem_desc_hi(1024);
+__device__ __forceinline__ uint32_t k_major(uint32_t addr) { return smem_desc_lo(addr, 16); }
+__device__ __forceinline__ uint32_t mn_major(uint32_t addr) { return smem_desc_lo(addr, kB * 128); }
+// D = A B^T, both K-major, `ksteps` of 16
+template <int HD>
+__device__ __forceinline__ void product_ss(bool lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int ksteps) {
+#pragma unroll
+  for (int k = 0; k < HD / 16; ++k) {
+    const uint32_t off = (k >> 2) * (kB * 128 / 16) + (k & 3) * 2;
+    mma_f16_if(lead && k < ksteps, d, a + off, b + off, kDescHi, idesc, k > 0);
+  }
+}
+// D += A B, 64 columns of A in bf16 in tensor memory, B their 64 rows, MN-major
+__device__ __forceinline__ void product_ts(bool lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) mma_f16_ts_if(lead, d, a + k * 8, b + k * (2048 / 16), kDescHi, idesc, add || k > 0);
+}
+constexpr uint32_t kHalfRows = 4 * 2048 / 16;              // from the first 64 rows of an MN-major tile to the others
+
+// A bounded wait in a loop whose lanes stay together: every lane waits, and the warp looks at `ok` once a round.  After one that
+// ran out no other one waits.
+__device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, bool& ok) {
+  if (!mbar_wait(bar, parity, ok ? kSpinLimit : 0)) ok = false;
 }
 
 // This thread's bulk stores have read their shared memory; or, where their rows are to be written once more, are complete.
@@ -97,16 +156,16 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   uint64_t* empty = full + SLOTS;
   uint64_t* q_full = empty + SLOTS;      // [2]
   uint64_t* s_full = q_full + 2;         // [2] S of the next block is there, and the PV before it done
-  uint64_t* p_half = s_full + 2;         // [2] four warps have left P of the first 64 keys
-  uint64_t* p_ready = p_half + 2;        // [2] ... of all
-  uint64_t* o_done = p_ready + 2;        // [2] a PV is done
+  uint64_t* p_half = s_full + 2;         // [half][tile] four warps have left P of the first 64 keys, of the others
+  uint64_t* past_max = p_half + 4;       // [2] four warps have a block's maxima
+  uint64_t* o_done = past_max + 2;        // [2] a PV is done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_done + 2);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool failed = false;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < SLOTS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int x = 0; x < 2; ++x) { mbar_init(&q_full[x], 1); mbar_init(&s_full[x], 1); mbar_init(&p_half[x], 4); mbar_init(&p_ready[x], 4); mbar_init(&o_done[x], 1); }
+    for (int s = 0; s < SLOTS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 2); }
+    for (int x = 0; x < 2; ++x) { mbar_init(&q_full[x], 1); mbar_init(&s_full[x], 1); mbar_init(&p_half[x], 4); mbar_init(&p_half[2 + x], 4); mbar_init(&past_max[x], 4); mbar_init(&o_done[x], 1); }
     fence_mbar_init();
     prefetch_tmap(&maps.q);
     prefetch_tmap(&maps.k);
@@ -148,19 +207,20 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       }
     }
     __syncwarp();
+    // slot t: K of block t and V of the block before
     int s = 0, round = 0;
-    for (int j = lo; j <= hi && !failed; ++j) {
-      for (int kv = 0; kv < 2; ++kv) {
-        if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[s], (round - 1) & 1))) { failed = true; break; }
-        if (lead) {
-          uint8_t* dst = smem + L::kRing + s * L::kTile;
-          mbar_expect_tx(&full[s], panels * kB * 128);
-          for (int c = 0; c < panels; ++c)
-            tma_load_4d_hint(dst + c * kB * 128, kv == 0 ? &maps.k : &maps.v, &full[s], c * 64, kvh, j * kB, rep, pol);
-        }
-        __syncwarp();
-        if (++s == SLOTS) { s = 0; ++round; }
+    for (int j = lo; j <= hi + 1 && lo <= hi && !failed; ++j) {
+      if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[s], (round - 1) & 1))) { failed = true; break; }
+      if (lead) {
+        uint8_t* dst = smem + L::kRing + s * 2 * L::kTile;
+        mbar_expect_tx(&full[s], ((j <= hi) + (j > lo)) * panels * kB * 128);
+        for (int c = 0; c < panels && j <= hi; ++c)
+          tma_load_4d_hint(dst + c * kB * 128, &maps.k, &full[s], c * 64, kvh, j * kB, rep, pol);
+        for (int c = 0; c < panels && j > lo; ++c)
+          tma_load_4d_hint(dst + L::kTile + c * kB * 128, &maps.v, &full[s], c * 64, kvh, (j - 1) * kB, rep, pol);
       }
+      __syncwarp();
+      if (++s == SLOTS) { s = 0; ++round; }
     }
     // the releases of the last slots arrive here: wait for them before leaving
     for (int i = 0; i < SLOTS && !failed; ++i) {
@@ -168,74 +228,51 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       if (uses > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[i], (uses - 1) & 1))) failed = true;
     }
     if (failed && lane == 0) atomicExch(a.err, 41);
-  } else if (warp == 1) {
+  } else if (warp <= 2) {
+    const int x = warp - 1;
     const bool lead = elect_one();
     const int ksteps = (a.head_dim + 15) / 16;
     const uint32_t idesc_s = make_idesc(1, false, false, kB, kB);
     const uint32_t idesc_o = make_idesc(1, false, true, kB, (uint32_t)ksteps * 16);
-    const uint32_t base = smem_u32(smem);
-    for (int x = 0; x < 2; ++x)
-      if ((x == 0 ? has_a : has_b) && !__all_sync(0xffffffffu, mbar_wait(&q_full[x], 0))) failed = true;
+    constexpr uint32_t T = L::kTile / 16;
+    const uint32_t q_lo = k_major(smem_u32(smem)) + x * T, k_lo = k_major(smem_u32(smem) + L::kRing);
+    const uint32_t v_lo = mn_major(smem_u32(smem) + L::kRing + L::kTile);
+    const uint32_t ts = tmem + x * kB, to = tmem + L::kO + x * HD;
+    const int from = x == 0 ? sa.lo : sb.lo, upto = x == 0 ? sa.hi : sb.hi;
+    bool ok = true;
+    if (from <= upto) wait(&q_full[x], 0, ok);
     int s = 0, round = 0;
-    int vslot = 0;
-    for (int j = lo; j <= hi + 1 && lo <= hi && !failed; ++j) {
-      const bool has_v = j > lo, has_k = j <= hi;
-      if (has_v) {                       // V of the block before
-        vslot = s;
-        if (!__all_sync(0xffffffffu, mbar_wait(&full[s], round & 1))) { failed = true; break; }
-        if (++s == SLOTS) { s = 0; ++round; }
-      }
-      const int kslot = s;
-      if (has_k) {
-        if (!__all_sync(0xffffffffu, mbar_wait(&full[s], round & 1))) { failed = true; break; }
-        if (++s == SLOTS) { s = 0; ++round; }
-      }
-      for (int x = 0; x < 2 && !failed; ++x) {
-        const Span sp = x == 0 ? sa : sb;
-        const uint32_t ts = tmem + x * kB, to = tmem + L::kO + x * HD;
-        if (has_v && j - 1 >= sp.lo && j - 1 <= sp.hi) {
-          const uint32_t vb = base + L::kRing + vslot * L::kTile;
-          for (int h = 0; h < 2; ++h) {
-            if (!__all_sync(0xffffffffu, mbar_wait(h == 0 ? &p_half[x] : &p_ready[x], (j - 1 - sp.lo) & 1))) { failed = true; break; }
-            tc_fence_after_sync();
-            if (lead) {
+    for (int j = lo; j <= hi + 1 && lo <= hi; ++j) {
+      const uint32_t turn = (uint32_t)(j - 1 - from) & 1;
+      const bool pv = j > from && j <= upto + 1, qk = j >= from && j <= upto;
+      wait(&full[s], round & 1, ok);     // (a slot that this tile does not need is let go of in its turn all the same)
+      if (pv) {
 #pragma unroll
-              for (int e = 0; e < kB / 32; ++e) {
-                const int k = h * (kB / 32) + e;
-                mma_bf16_ts(to, ts + k * 8, make_smem_desc(vb + k * 2048, kB * 128, 1024), idesc_o, j - 1 > sp.lo || k > 0);
-              }
-              if (h == 1) mma_commit(&o_done[x]);
-            }
-            __syncwarp();
-          }
-          if (failed) break;
-        }
-        if (has_k && j >= sp.lo && j <= sp.hi) {
-          // S goes where P lies: the product that reads it has to be complete (products of other shapes or accumulators are not
-          // known to keep their order)
-          if (j > sp.lo && !__all_sync(0xffffffffu, mbar_wait(&o_done[x], (j - 1 - sp.lo) & 1))) { failed = true; break; }
+        for (int h = 0; h < 2; ++h) {
+          wait(&p_half[2 * h + x], turn, ok);
           tc_fence_after_sync();
-          if (lead) {
-            const uint32_t qb = base + x * L::kTile, kb = base + L::kRing + kslot * L::kTile;
-            for (int k = 0; k < ksteps; ++k) {
-              const uint32_t off = (k >> 2) * (kB * 128) + (k & 3) * 32;
-              mma_bf16(ts, make_smem_desc(qb + off, 16, 1024), make_smem_desc(kb + off, 16, 1024), idesc_s, k > 0);
-            }
-            mma_commit(&s_full[x]);
-          }
-          __syncwarp();
+          product_ts(lead, to, ts + h * 32, v_lo + s * 2 * T + h * kHalfRows, idesc_o, j - 1 > from || h > 0);
         }
+        mma_commit_if(lead, &o_done[x]);
       }
-      if (failed) break;
-      if (lead) {
-        if (has_v) mma_commit(&empty[vslot]);
-        if (has_k) mma_commit(&empty[kslot]);
+      if (qk) {
+        // S goes where P lies: the product that reads it has to be complete (products of other shapes or accumulators are not
+        // known to keep their order)
+        if (pv) wait(&o_done[x], turn, ok);
+        // the other tile is past its maximum: its exponentials and this product run together
+        const int b = x == 1 ? j : j - 1, b_from = x == 1 ? sa.lo : sb.lo, b_upto = x == 1 ? sa.hi : sb.hi;
+        if (b >= b_from && b <= b_upto) wait(&past_max[1 - x], (uint32_t)(b - b_from) & 1, ok);
+        tc_fence_after_sync();
+        product_ss<HD>(lead, ts, q_lo, k_lo + s * 2 * T, idesc_s, ksteps);
+        mma_commit_if(lead, &s_full[x]);
       }
-      __syncwarp();
+      mma_commit_if(lead, &empty[s]);
+      if (++s == SLOTS) { s = 0; ++round; }
+      if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
     }
     if (failed && lane == 0) atomicExch(a.err, 42);
   } else {
-    const int x = (warp - 2) >> 2, q = warp & 3;
+    const int x = (warp - 3) >> 2, q = warp & 3;
     const Span sp = x == 0 ? sa : sb;
     const int row = r0 + x * kB + q * 32 + lane;
     int start, end;
@@ -245,38 +282,45 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     const float scale2 = a.scale * kLog2e;
     const int cols = (a.head_dim + 15) / 16 * 16;
     float top = -INFINITY, sum = 0.f;    // the reference of the exponentials (a product, not scaled), and their sum
+    bool ok = true;
     for (int j = sp.lo; j <= sp.hi; ++j) {
-      if (!__all_sync(0xffffffffu, mbar_wait(&s_full[x], (j - sp.lo) & 1))) { failed = true; break; }
-      __syncwarp();
+      wait(&s_full[x], (j - sp.lo) & 1, ok);
       tc_fence_after_sync();
+      // columns [from, to_col] are visible; one bit each in a mask of 32
+      const int from = start - j * kB, to_col = row - j * kB;
+      const bool cut = __any_sync(0xffffffffu, from > 0 || to_col < kB - 1);
+      auto hide = [&](int c, uint32_t (&v)[32]) {
+        const int a0 = from - c * 32, a1 = to_col - c * 32;
+        const uint32_t seen = (a0 > 31 ? 0u : a0 > 0 ? 0xffffffffu << a0 : 0xffffffffu) & (a1 < 0 ? 0u : a1 < 31 ? (2u << a1) - 1 : 0xffffffffu);
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if ((seen >> i & 1) == 0) v[i] = 0xff800000u;
+      };
       uint32_t s[4][32];
 #pragma unroll
       for (int c = 0; c < 4; ++c) tmem_ld_32x32(ts + c * 32, s[c]);
       tmem_ld_wait();
-      const int from = start - j * kB, to_col = row - j * kB;                // visible columns [from, to_col]
-      if (__any_sync(0xffffffffu, from > 0 || to_col < kB - 1)) {
+      if (__builtin_expect(cut, 0)) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (c * 32 + i < from || c * 32 + i > to_col) s[c][i] = 0xff800000u;
+        for (int c = 0; c < 4; ++c) hide(c, s[c]);
       }
-      // eight chains: one would take a row's 128 scores one after another
-      float m8[8];
+      // four chains of three-input maxima: one would take them one after another.  A NaN stays.
+      float m4[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m8[i] = __uint_as_float(s[0][i]);
+      for (int e = 0; e < 4; ++e) {
+        float m = max3(__uint_as_float(s[0][e]), __uint_as_float(s[0][e + 4]), __uint_as_float(s[0][e]));
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int i = 0; i < 32; i += 16)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) m8[e] = fmaxf(fmaxf(m8[e], __uint_as_float(s[c][i + e])), __uint_as_float(s[c][i + 8 + e]));
-      const float most = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])), fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
-      // (top = -inf: the difference is infinite, and the factor zero)
-      const bool far = most > top && (most - top) * scale2 > 8.f;
-      if (__any_sync(0xffffffffu, far)) {
-        const float next = fmaxf(most, top);
-        const float keep = next > top ? ex2((top - next) * scale2) : 1.f;
+        for (int i = 8; i < 128; i += 8) m = max3(m, __uint_as_float(s[i >> 5][(i & 31) + e]), __uint_as_float(s[i >> 5][(i & 31) + 4 + e]));
+        m4[e] = m;
+      }
+      const float most = max3(max3(m4[0], m4[1], m4[2]), m4[3], m4[3]);
+      __syncwarp();
+      mbar_arrive_if(lane == 0, &past_max[x]);
+      // (top = -inf: the difference is infinite, and the factor zero; a NaN goes on into the reference)
+      const bool far = !((most - top) * scale2 <= 8.f) && !(most == -INFINITY);
+      if (__builtin_expect(__any_sync(0xffffffffu, far), 0)) {
+        const float next = max3(most, top, top);
+        const float keep = next == top ? 1.f : ex2((top - next) * scale2);
         top = next;
         sum *= keep;
         if (j > sp.lo) {
@@ -297,24 +341,30 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       for (int c = 0; c < 4; ++c) {
         uint32_t p[16];
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          float2 e = parts(fma2(two(s[c][i], s[c][i + 1]), by2, ref2));
-          e.x = ex2(e.x);
-          e.y = ex2(e.y);
-          part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], two(e.x, e.y));
-          p[i >> 1] = pack2(e.x, e.y);
+        for (int i = 0; i < 16; ++i) {
+          const uint64_t t = fma2(two(s[c][2 * i], s[c][2 * i + 1]), by2, ref2);
+          float2 e;
+          if (kFmaOf16 >> i & 1) {
+            e = exp2_fma(t);
+          } else {
+            e = parts(t);
+            e.x = ex2(e.x);
+            e.y = ex2(e.y);
+          }
+          part[i & 1] = add2(part[i & 1], two(e.x, e.y));
+          p[i] = pack2(e.x, e.y);
         }
         tmem_st_32x16(ts + c * 16, p);
         if (c & 1) {                       // PV may start with the first half of the keys
           tmem_st_wait();
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive(c == 1 ? &p_half[x] : &p_ready[x]);
+          mbar_arrive_if(lane == 0, &p_half[(c & 2) + x]);
         }
       }
       const float2 total = parts(add2(part[0], part[1]));
       sum += total.x + total.y;
-      __syncwarp();
+      if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
     }
     const bool none = start > row;       // in no sequence, or behind the tensor
     if (sp.lo <= sp.hi && !failed) {
@@ -326,7 +376,8 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       if (lane == 0) atomicExch(a.err, 43);
     } else if (r0 + x * kB + q * 32 < a.tokens) {
       // this warp's 32 rows leave through its part of the tile's place for Q
-      const float by = none ? 0.f : 1.f / sum;
+      // (a row with a NaN or +inf, or of -inf only, is computed once more: exp2_fma has no infinities)
+      const float by = none ? 0.f : fabsf(top) < INFINITY ? 1.f / sum : NAN;
       bool fine = true;
       uint8_t* box = smem + x * L::kTile + q * 32 * 128;
 #pragma unroll
@@ -398,23 +449,6 @@ constexpr int kBwdThreads = 320;
 
 // the named barrier of the eight element warps
 __device__ __forceinline__ void elements_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
-// D += A B^T, both in shared memory, K-major, `ksteps` of 16
-template <int HD>
-__device__ __forceinline__ void product_ss(uint32_t d, uint32_t sa, uint32_t sb, uint32_t idesc, int ksteps) {
-#pragma unroll
-  for (int k = 0; k < HD / 16; ++k) {
-    if (k >= ksteps) break;
-    const uint32_t off = (k >> 2) * (kB * 128) + (k & 3) * 32;
-    mma_bf16(d, make_smem_desc(sa + off, 16, 1024), make_smem_desc(sb + off, 16, 1024), idesc, k > 0);
-  }
-}
-// D += A B, A 128 columns of bf16 in tensor memory (64 of them at `a`, the others `step` columns on), B [128][N] in shared memory
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t ta, uint32_t step, uint32_t sb, uint32_t idesc, bool add) {
-#pragma unroll
-  for (int k = 0; k < kB / 16; ++k)
-    mma_bf16_ts(d, ta + (k >> 2) * step + (k & 3) * 8, make_smem_desc(sb + k * 2048, kB * 128, 1024), idesc, add || k > 0);
-}
 
 // This warp's 32 rows of a result [128][HD] in tensor memory, times `by`, in bf16 into `box` (the rows' place in a tile of panels)
 // and out.  Half h of the columns.  Returns whether the lane's numbers are finite; `zero`: zeros instead.
@@ -550,25 +584,22 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     const bool lead = elect_one();
     const uint32_t idesc_s = make_idesc(1, false, false, kB, kB);
     const uint32_t idesc_o = make_idesc(1, false, true, kB, (uint32_t)cols);
-    const uint32_t qb = smem_u32(smem), gb = qb + L::kTile, kb = smem_u32(sk), vb = smem_u32(sv);
+    constexpr uint32_t T = L::kTile / 16;
+    const uint32_t qb = k_major(smem_u32(smem)), gb = qb + T, kb = k_major(smem_u32(sk)), vb = k_major(smem_u32(sv)), kmn = mn_major(smem_u32(sk));
     auto scores = [&](int i) {           // S and dP of block i
       const int ks = i % L::kK, vs = i % L::kV;
       bool got = mbar_wait(&k_full[ks], (i / L::kK) & 1);
       if (i == 0) got = got && mbar_wait(&q_full[0], 0);
       if (!__all_sync(0xffffffffu, got)) return false;
       tc_fence_after_sync();
-      if (lead) product_ss<HD>(tmem + L::kS, qb, kb + ks * L::kTile, idesc_s, ksteps);
-      __syncwarp();
+      product_ss<HD>(lead, tmem + L::kS, qb, kb + ks * T, idesc_s, ksteps);
       got = mbar_wait(&v_full[vs], (i / L::kV) & 1);
       if (i == 0) got = got && mbar_wait(&q_full[1], 0);
       if (!__all_sync(0xffffffffu, got)) return false;
       tc_fence_after_sync();
-      if (lead) {
-        product_ss<HD>(tmem + L::kP, gb, vb + vs * L::kTile, idesc_s, ksteps);
-        mma_commit(s_full);
-        mma_commit(&v_empty[vs]);
-      }
-      __syncwarp();
+      product_ss<HD>(lead, tmem + L::kP, gb, vb + vs * T, idesc_s, ksteps);
+      mma_commit_if(lead, s_full);
+      mma_commit_if(lead, &v_empty[vs]);
       return true;
     };
     if (n > 0 && !scores(0)) failed = true;
@@ -578,12 +609,11 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
       }
       if (!__all_sync(0xffffffffu, mbar_wait(&ds_ready[i & 1], (i >> 1) & 1))) { failed = true; break; }
       tc_fence_after_sync();
-      if (lead) {
-        product_ts(tmem + L::kO, tmem + L::kDs + (i & 1) * 64, 32, kb + (i % L::kK) * L::kTile, idesc_o, i > 0);
-        mma_commit(&k_empty[i % L::kK]);
-        if (i == n - 1) mma_commit(done);
-      }
-      __syncwarp();
+      const uint32_t ds = tmem + L::kDs + (i & 1) * 64, k0 = kmn + (i % L::kK) * T;
+      product_ts(lead, tmem + L::kO, ds, k0, idesc_o, i > 0);
+      product_ts(lead, tmem + L::kO, ds + 32, k0 + kHalfRows, idesc_o, true);
+      mma_commit_if(lead, &k_empty[i % L::kK]);
+      mma_commit_if(lead && i == n - 1, done);
     }
     if (failed && lane == 0) atomicExch(a.err, 45);
   } else {
@@ -839,18 +869,17 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     const bool lead = elect_one();
     const uint32_t idesc_s = make_idesc(1, false, false, kB, kB);
     const uint32_t idesc_o = make_idesc(1, false, true, kB, (uint32_t)cols);
-    const uint32_t kb = smem_u32(smem), vb = kb + L::kTile, qb = smem_u32(sq), gb = smem_u32(sg);
+    constexpr uint32_t T = L::kTile / 16;
+    const uint32_t kb = k_major(smem_u32(smem)), vb = kb + T, qb = k_major(smem_u32(sq)), gb = k_major(smem_u32(sg));
+    const uint32_t qmn = mn_major(smem_u32(sq)), gmn = mn_major(smem_u32(sg));
     auto scores = [&](int i) {
       const int qs = i % L::kQ;
       bool got = mbar_wait(&q_full[qs], (i / L::kQ) & 1);
       if (i == 0) got = got && mbar_wait(&kv_full[0], 0);
       if (!__all_sync(0xffffffffu, got)) return false;
       tc_fence_after_sync();
-      if (lead) {
-        product_ss<HD>(tmem + L::kS, kb, qb + qs * L::kTile, idesc_s, ksteps);
-        mma_commit(s_full);
-      }
-      __syncwarp();
+      product_ss<HD>(lead, tmem + L::kS, kb, qb + qs * T, idesc_s, ksteps);
+      mma_commit_if(lead, s_full);
       return true;
     };
     auto dots = [&](int i) {
@@ -859,30 +888,23 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
       if (i == 0) got = got && mbar_wait(&kv_full[1], 0);
       if (!__all_sync(0xffffffffu, got)) return false;
       tc_fence_after_sync();
-      if (lead) {
-        product_ss<HD>(tmem + L::kDp, vb, gb + gs * L::kTile, idesc_s, ksteps);
-        mma_commit(dp_full);
-      }
-      __syncwarp();
+      product_ss<HD>(lead, tmem + L::kDp, vb, gb + gs * T, idesc_s, ksteps);
+      mma_commit_if(lead, dp_full);
       return true;
     };
     if (n > 0 && !(scores(0) && dots(0))) failed = true;
     for (int i = 0; i < n && !failed; ++i) {
       const int qs = i % L::kQ, gs = i % L::kG;
       auto dv = [&]() {
-        if (lead) {
-          product_ts(tmem + L::kDv, tmem + L::kP, L::kHalf, gb + gs * L::kTile, idesc_o, i > 0);
-          mma_commit(&g_empty[gs]);
-        }
-        __syncwarp();
+        product_ts(lead, tmem + L::kDv, tmem + L::kP, gmn + gs * T, idesc_o, i > 0);
+        product_ts(lead, tmem + L::kDv, tmem + L::kP + L::kHalf, gmn + gs * T + kHalfRows, idesc_o, true);
+        mma_commit_if(lead, &g_empty[gs]);
       };
       auto dk = [&]() {
-        if (lead) {
-          product_ts(tmem + L::kDk, tmem + L::kDs, L::kHalf, qb + qs * L::kTile, idesc_o, i > 0);
-          mma_commit(&q_empty[qs]);
-          if (i == n - 1) mma_commit(done);
-        }
-        __syncwarp();
+        product_ts(lead, tmem + L::kDk, tmem + L::kDs, qmn + qs * T, idesc_o, i > 0);
+        product_ts(lead, tmem + L::kDk, tmem + L::kDs + L::kHalf, qmn + qs * T + kHalfRows, idesc_o, true);
+        mma_commit_if(lead, &q_empty[qs]);
+        mma_commit_if(lead && i == n - 1, done);
       };
       if (!__all_sync(0xffffffffu, mbar_wait(p_ready, i & 1))) { failed = true; break; }
       tc_fence_after_sync();
