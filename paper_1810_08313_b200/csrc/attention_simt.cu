@@ -1,13 +1,15 @@
 // Attention over packed sequences and its gradient on the CUDA cores: fp32 tensors, and the bf16 ones that the tensor-core
 // kernels do not take (see attention.cuh for the formulas and attention_tc.cu for the others).  The entry points are here, too.
 //
-// One CTA of 256 threads per tile of 64 rows (32 for heads of more than 128) of one head; tiles of 64 keys pass through shared
-// memory once each, and scores never leave the SM.  Thread (ty, tx) of 16 x 16 has the rows ty R .. + R - 1 and the keys
-// tx + 16 c of a tile of scores; operands are read four elements of a head at a time, rows padded by four floats, so that
-// the reads of a quarter warp fall into distinct banks and R x R x 4 multiply-adds need 2 R reads of 16 bytes.  The
-// second products read the scores back from shared memory the same way.  Forward: a running maximum and sum a row; the backward
-// pass has one kernel for dq (and D), tiles of queries, and one for dk and dv, tiles of keys which take all the queries of
-// their group's heads: the scores are formed twice, and no sum depends on an order of arrival.
+// One CTA of 256 threads per tile of 64 rows of one head, or of 32 where those are too few for the SMs; blocks of 64 keys pass
+// through shared memory once each, and scores never leave the SM.  (Heads of more than 128: 32 rows and 32 keys.)  Thread (ty, tx)
+// of 16 x 16 has the rows ty R .. + R - 1 and the keys tx + 16 c of a block of scores; operands are read four elements of a head at
+// a time, rows padded by four floats, so that the reads of a quarter warp fall into distinct banks and 4 x 4 x 4 multiply-adds
+// need 8 reads of 16 bytes.  The second products read the scores back from shared memory the same way.  Forward: a running
+// maximum and sum a row.  Backward: one launch with CTAs for dk and dv, tiles of keys which take all the queries of their group's
+// heads, and others for dq, tiles of queries: the scores are formed twice, and no sum depends on an order of arrival.  Where
+// there are few tiles of keys, a cluster of CTAs shares the queries of a tile, and its first one adds up the parts, in order, out
+// of the others' shared memory.
 #include "attention.cuh"
 
 namespace ls {
@@ -16,45 +18,69 @@ namespace {
 
 constexpr int kNT = 256;
 
-template <int HD>
+// HD: head_dim at most; RB: rows of a tile
+template <int HD, int RB>
 struct Way {
-  static constexpr int R = HD > 128 ? 2 : 4;      // rows and keys of a thread
-  static constexpr int B = 16 * R;                // of a tile
+  static constexpr int B = RB, R = RB / 16;       // rows of a tile, of a thread
+  static constexpr int K = HD > 128 ? 2 : 4;      // keys of a thread
+  static constexpr int N = 16 * K;                // of a block
   static constexpr int P = HD + 4;                // floats between rows of an operand
-  static constexpr int PS = B + 4;                // of the scores
+  static constexpr int PS = N + 4;                // of the scores
   static constexpr int C = HD / 16;               // result columns of a thread: 4 tx + 64 c .. + 3, or tx + 16 c below 64
-  static constexpr int tile = B * P, scores = B * PS;
+  static constexpr int rows = B * P, block = N * P, scores = B * PS;
 };
 
-// rows [r0, r0 + B) of a head into shared memory as floats; zeros outside the tensor and the head
-template <typename T, int HD>
-__device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t row, int64_t r0, int64_t rows, int hd) {
-  using W = Way<HD>;
-  for (int i = threadIdx.x; i < W::B * HD; i += kNT) {
+__device__ __forceinline__ float4 four(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 four(const __nv_bfloat16* p) {
+  const uint2 t = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xFFFF0000u), __uint_as_float(t.y << 16),
+                     __uint_as_float(t.y & 0xFFFF0000u));
+}
+// rows [r0, r0 + ROWS) of a head into shared memory as floats; zeros outside the tensor and the head.  quads: rows are whole fours of
+// elements that start on their boundary
+template <typename T, int HD, int ROWS>
+__device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t row, int64_t r0, int64_t rows, int hd, bool quads) {
+  constexpr int P = HD + 4;
+  if (quads) {
+    constexpr int Q = HD / 4, N = ROWS * Q / kNT;
+    static_assert(ROWS * Q % kNT == 0, "whole rounds");
+    float4 v[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = n * kNT + threadIdx.x, r = i / Q, c = (i - r * Q) * 4;
+      v[n] = r0 + r < rows && c < hd ? four(src + (r0 + r) * row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = n * kNT + threadIdx.x, r = i / Q, c = (i - r * Q) * 4;
+      *reinterpret_cast<float4*>(dst + r * P + c) = v[n];
+    }
+    return;
+  }
+  for (int i = threadIdx.x; i < ROWS * HD; i += kNT) {
     const int r = i / HD, c = i - r * HD;
-    dst[r * W::P + c] = r0 + r < rows && c < hd ? to_f32(src[(r0 + r) * row + c]) : 0.f;
+    dst[r * P + c] = r0 + r < rows && c < hd ? to_f32(src[(r0 + r) * row + c]) : 0.f;
   }
 }
 
 // s[r][c] = x row (ty R + r) . y row (tx + 16 c)
-template <int HD>
-__device__ __forceinline__ void dots(const float* x, const float* y, int ty, int tx, float (&s)[Way<HD>::R][Way<HD>::R]) {
-  using W = Way<HD>;
+template <typename W, int HD>
+__device__ __forceinline__ void dots(const float* x, const float* y, int ty, int tx, float (&s)[W::R][W::K]) {
 #pragma unroll
   for (int r = 0; r < W::R; ++r)
 #pragma unroll
-    for (int c = 0; c < W::R; ++c) s[r][c] = 0.f;
+    for (int c = 0; c < W::K; ++c) s[r][c] = 0.f;
 #pragma unroll 4
   for (int d = 0; d < HD; d += 4) {
-    float4 a[W::R], b[W::R];
+    float4 a[W::R], b[W::K];
 #pragma unroll
     for (int r = 0; r < W::R; ++r) a[r] = *reinterpret_cast<const float4*>(x + (ty * W::R + r) * W::P + d);
 #pragma unroll
-    for (int c = 0; c < W::R; ++c) b[c] = *reinterpret_cast<const float4*>(y + (tx + 16 * c) * W::P + d);
+    for (int c = 0; c < W::K; ++c) b[c] = *reinterpret_cast<const float4*>(y + (tx + 16 * c) * W::P + d);
 #pragma unroll
     for (int r = 0; r < W::R; ++r)
 #pragma unroll
-      for (int c = 0; c < W::R; ++c)
+      for (int c = 0; c < W::K; ++c)
         s[r][c] = fmaf(a[r].w, b[c].w, fmaf(a[r].z, b[c].z, fmaf(a[r].y, b[c].y, fmaf(a[r].x, b[c].x, s[r][c]))));
   }
 }
@@ -65,11 +91,10 @@ __device__ __forceinline__ int column(int tx, int c) {
   return HD >= 64 ? (c & ~3) * 16 + tx * 4 + (c & 3) : tx + 16 * c;
 }
 // acc[r][c] += sum over j of s[ty R + r][j] y[j][column c]
-template <int HD>
-__device__ __forceinline__ void accumulate(const float* s, const float* y, int ty, int tx, float (&acc)[Way<HD>::R][Way<HD>::C]) {
-  using W = Way<HD>;
+template <typename W, int HD>
+__device__ __forceinline__ void accumulate(const float* s, const float* y, int ty, int tx, float (&acc)[W::R][W::C]) {
 #pragma unroll 2
-  for (int j = 0; j < W::B; j += 4) {
+  for (int j = 0; j < W::N; j += 4) {
     float4 a[W::R];
 #pragma unroll
     for (int r = 0; r < W::R; ++r) a[r] = *reinterpret_cast<const float4*>(s + (ty * W::R + r) * W::PS + j);
@@ -98,11 +123,9 @@ __device__ __forceinline__ void accumulate(const float* s, const float* y, int t
 }
 
 // Writes acc[r][c] * by[r] to the rows r0 + ty R + r of the tensor; returns whether all of the thread's numbers are finite.
-template <typename T, int HD>
+template <typename T, typename W, int HD>
 __device__ __forceinline__ bool write_rows(T* dst, int64_t row, int64_t r0, int64_t rows, int hd, int ty, int tx,
-                                           const float (&acc)[Way<HD>::R][Way<HD>::C], const float (&by)[Way<HD>::R],
-                                           uint32_t* bad) {
-  using W = Way<HD>;
+                                           const float (&acc)[W::R][W::C], const float (&by)[W::R], uint32_t* bad) {
   bool good = true;
 #pragma unroll
   for (int r = 0; r < W::R; ++r) {
@@ -134,15 +157,15 @@ __device__ __forceinline__ float row_max(float x) {
   return x;
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int RB>
 __global__ void __launch_bounds__(kNT)
-attention_kernel(const __grid_constant__ Args a) {
-  using W = Way<HD>;
+attention_kernel(const __grid_constant__ Args a, const bool quads) {
+  using W = Way<HD, RB>;
   extern __shared__ __align__(16) float sm[];
   float* sq = sm;
-  float* sk = sq + W::tile;
-  float* sv = sk + W::tile;
-  float* sp = sv + W::tile;
+  float* sk = sq + W::rows;
+  float* sv = sk + W::block;
+  float* sp = sv + W::block;
   __shared__ uint32_t bad[W::B];
   __shared__ int start[W::B];
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, hd = a.head_dim;
@@ -153,7 +176,7 @@ attention_kernel(const __grid_constant__ Args a) {
   const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
   const int64_t r0 = (int64_t)(tiles - 1 - rest / a.m) * W::B;
   const int kvh = head / (a.heads / a.kv_heads);
-  load_tile<T, HD>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd);
+  load_tile<T, HD, W::B>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd, quads);
   const Bounds bounds(a, rep);
   if (tid < W::B) {                        // (whole warps)
     int end;
@@ -166,18 +189,18 @@ attention_kernel(const __grid_constant__ Args a) {
 #pragma unroll
   for (int r = 0; r < W::R; ++r) { top[r] = -INFINITY; sum[r] = 0.f; }
   const int64_t end = min(r0 + W::B, a.tokens);
-  for (int64_t j0 = bounds.first_key((int)r0) / W::B * W::B; j0 < end; j0 += W::B) {
-    load_tile<T, HD>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd);
-    load_tile<T, HD>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd);
+  for (int64_t j0 = bounds.first_key((int)r0); j0 < end; j0 += W::N) {
+    load_tile<T, HD, W::N>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd, quads);
+    load_tile<T, HD, W::N>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd, quads);
     __syncthreads();
-    float s[W::R][W::R];
-    dots<HD>(sq, sk, ty, tx, s);
+    float s[W::R][W::K];
+    dots<W, HD>(sq, sk, ty, tx, s);
 #pragma unroll
     for (int r = 0; r < W::R; ++r) {
       const int row = ty * W::R + r;
       float most = -INFINITY;
 #pragma unroll
-      for (int c = 0; c < W::R; ++c) {
+      for (int c = 0; c < W::K; ++c) {
         const int64_t j = j0 + tx + 16 * c;
         s[r][c] = j >= start[row] && j <= r0 + row ? s[r][c] * scale2 : -INFINITY;
         most = fmaxf(most, s[r][c]);
@@ -188,7 +211,7 @@ attention_kernel(const __grid_constant__ Args a) {
       top[r] = most;
       float part = 0.f;
 #pragma unroll
-      for (int c = 0; c < W::R; ++c) {
+      for (int c = 0; c < W::K; ++c) {
         const float p = exp2f(s[r][c] - ref);
         part += p;
         sp[row * W::PS + tx + 16 * c] = p;
@@ -198,7 +221,7 @@ attention_kernel(const __grid_constant__ Args a) {
       for (int c = 0; c < W::C; ++c) acc[r][c] *= keep;
     }
     __syncthreads();
-    accumulate<HD>(sp, sv, ty, tx, acc);
+    accumulate<W, HD>(sp, sv, ty, tx, acc);
     __syncthreads();
   }
   float by[W::R];
@@ -215,75 +238,82 @@ attention_kernel(const __grid_constant__ Args a) {
     if (tx == 0 && i < a.tokens)
       a.lse[((int64_t)rep * a.heads + head) * a.tokens + i] = none ? 0.f : fmaf(top[r], kLn2, logf(sum[r]));
   }
-  const bool good = write_rows<T, HD>(head_ptr<T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
+  const bool good = write_rows<T, W, HD>(head_ptr<T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
   if (__syncthreads_and(good)) return;
   for (int r = tid >> 5; r < W::B; r += kNT / 32)
     if (bad[r] != 0u) forward_row<T>(a, rep, head, (int)r0 + r);
 }
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(kNT)
-attention_dq_kernel(const __grid_constant__ Args a) {
-  using W = Way<HD>;
-  extern __shared__ __align__(16) float sm[];
+// dot[r] = dout . out of the tile's rows, dout from shared memory
+template <typename T, int HD, int ROWS>
+__device__ __forceinline__ void row_dots(float* dot, const float* sg, const T* out, int64_t row, int64_t r0, int64_t rows, int hd, bool quads) {
+  constexpr int N = kNT / ROWS, P = HD + 4;          // neighbouring threads of a row
+  const int r = threadIdx.x / N, part = threadIdx.x % N;
+  float d = 0.f;
+  if (r0 + r < rows) {
+    const T* o = out + (r0 + r) * row;
+    if (quads) {
+#pragma unroll 4
+      for (int e = part * 4; e < hd; e += N * 4) {
+        const float4 x = four(o + e), g = *reinterpret_cast<const float4*>(sg + r * P + e);
+        d = fmaf(x.x, g.x, fmaf(x.y, g.y, fmaf(x.z, g.z, fmaf(x.w, g.w, d))));
+      }
+    } else {
+      for (int e = part; e < hd; e += N) d = fmaf(to_f32(o[e]), sg[r * P + e], d);
+    }
+  }
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+  if (part == 0) dot[r] = d;
+}
+
+template <typename T, int HD, int RB>
+__device__ __forceinline__ void grad_queries(const Args& a, bool quads, float* sm, uint32_t* bad, int* start, float* lse2, float* dot, int unit) {
+  using W = Way<HD, RB>;
   float* sq = sm;
-  float* sg = sq + W::tile;
-  float* sk = sg + W::tile;
-  float* sv = sk + W::tile;
-  float* sp = sv + W::tile;
-  __shared__ uint32_t bad[W::B];
-  __shared__ int start[W::B];
+  float* sg = sq + W::rows;
+  float* sk = sg + W::rows;
+  float* sv = sk + W::block;
+  float* sp = sv + W::block;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, hd = a.head_dim;
-  grid_dep_wait();
-  grid_dep_launch();
   const int tiles = (int)((a.tokens + W::B - 1) / W::B);
-  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
+  const int head = unit % a.heads, rest = unit / a.heads, rep = rest % a.m;
   const int64_t r0 = (int64_t)(tiles - 1 - rest / a.m) * W::B;
   const int kvh = head / (a.heads / a.kv_heads);
   const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens;
-  load_tile<T, HD>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd);
-  load_tile<T, HD>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, r0, a.tokens, hd);
-  load_tile<T, HD>(sk, head_ptr<const T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd);
+  load_tile<T, HD, W::B>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd, quads);
+  load_tile<T, HD, W::B>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, r0, a.tokens, hd, quads);
   const Bounds bounds(a, rep);
   if (tid < W::B) {                        // (whole warps)
     int end;
     bad[tid] = 0u;
     bounds.rows((int)r0 + (tid & ~31), &start[tid], &end);
+    lse2[tid] = r0 + tid < a.tokens ? a.lse[stat + r0 + tid] * kLog2e : 0.f;
   }
   __syncthreads();
-  float lse2[W::R], dot[W::R];
-#pragma unroll
-  for (int r = 0; r < W::R; ++r) {
-    const int row = ty * W::R + r;
-    float d = 0.f;
-    for (int e = tx; e < HD; e += 16) d = fmaf(sg[row * W::P + e], sk[row * W::P + e], d);
-    dot[r] = row_total(d);
-    lse2[r] = r0 + row < a.tokens ? a.lse[stat + r0 + row] * kLog2e : 0.f;
-    if (tx == 0 && r0 + row < a.tokens) a.dot[stat + r0 + row] = dot[r];
-  }
-  __syncthreads();
+  row_dots<T, HD, W::B>(dot, sg, head_ptr<const T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd, quads);
   const float scale2 = a.scale * kLog2e;
   float acc[W::R][W::C] = {};
   const int64_t end = min(r0 + W::B, a.tokens);
-  for (int64_t j0 = bounds.first_key((int)r0) / W::B * W::B; j0 < end; j0 += W::B) {
-    load_tile<T, HD>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd);
-    load_tile<T, HD>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd);
+  for (int64_t j0 = bounds.first_key((int)r0); j0 < end; j0 += W::N) {
+    load_tile<T, HD, W::N>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd, quads);
+    load_tile<T, HD, W::N>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd, quads);
     __syncthreads();
-    float s[W::R][W::R], g[W::R][W::R];
-    dots<HD>(sq, sk, ty, tx, s);
-    dots<HD>(sg, sv, ty, tx, g);
+    float s[W::R][W::K], g[W::R][W::K];
+    dots<W, HD>(sq, sk, ty, tx, s);
+    dots<W, HD>(sg, sv, ty, tx, g);
 #pragma unroll
     for (int r = 0; r < W::R; ++r) {
       const int row = ty * W::R + r;
 #pragma unroll
-      for (int c = 0; c < W::R; ++c) {
+      for (int c = 0; c < W::K; ++c) {
         const int64_t j = j0 + tx + 16 * c;
         const bool seen = j >= start[row] && j <= r0 + row;
-        sp[row * W::PS + tx + 16 * c] = seen ? exp2f(fmaf(s[r][c], scale2, -lse2[r])) * (g[r][c] - dot[r]) : 0.f;
+        sp[row * W::PS + tx + 16 * c] = seen ? exp2f(fmaf(s[r][c], scale2, -lse2[row])) * (g[r][c] - dot[row]) : 0.f;
       }
     }
-    __syncthreads();
-    accumulate<HD>(sp, sk, ty, tx, acc);
+    __syncwarp();                          // (a row of scores is one half warp's)
+    accumulate<W, HD>(sp, sk, ty, tx, acc);
     __syncthreads();
   }
   float by[W::R];
@@ -295,115 +325,185 @@ attention_dq_kernel(const __grid_constant__ Args a) {
       for (int c = 0; c < W::C; ++c) acc[r][c] = 0.f;
     }
   }
-  const bool good = write_rows<T, HD>(head_ptr<T>(a.dq, rep, head, hd), a.dq.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
+  const bool good = write_rows<T, W, HD>(head_ptr<T>(a.dq, rep, head, hd), a.dq.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
   if (__syncthreads_and(good)) return;
   for (int r = tid >> 5; r < W::B; r += kNT / 32)
     if (bad[r] != 0u) dq_row<T>(a, rep, head, (int)r0 + r);
 }
 
-// Tiles of keys: scores with the keys as rows and the queries as columns.
-template <typename T, int HD>
-__global__ void __launch_bounds__(kNT)
-attention_dkv_kernel(const __grid_constant__ Args a) {
-  using W = Way<HD>;
-  extern __shared__ __align__(16) float sm[];
+// Tiles of keys: scores with the keys as rows and the queries as columns.  `rank` of the `split` CTAs that share the queries.
+template <typename T, int HD, int RB>
+__device__ __forceinline__ void grad_keys(const Args& a, bool quads, float* sm, uint32_t* bad, int* start, float* lse2, float* dot, int unit,
+                                          int rank, int split) {
+  using W = Way<HD, RB>;
   float* sk = sm;
-  float* sv = sk + W::tile;
-  float* sq = sv + W::tile;
-  float* sg = sq + W::tile;
-  float* sp = sg + W::tile;
-  __shared__ uint32_t bad[W::B];
-  __shared__ float lse2[W::B], dot[W::B];
-  __shared__ int start[W::B];
+  float* sv = sk + W::rows;
+  float* sq = sv + W::rows;
+  float* sg = sq + W::block;
+  float* sp = sg + W::block;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, hd = a.head_dim;
-  grid_dep_wait();
-  grid_dep_launch();
-  // the keys with the most queries first
-  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, rep = rest % a.m;
+  const int kvh = unit % a.kv_heads, rest = unit / a.kv_heads, rep = rest % a.m;
   const int64_t k0 = (int64_t)(rest / a.m) * W::B;
   const int group = a.heads / a.kv_heads;
-  load_tile<T, HD>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, k0, a.tokens, hd);
-  load_tile<T, HD>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, k0, a.tokens, hd);
+  load_tile<T, HD, W::B>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, k0, a.tokens, hd, quads);
+  load_tile<T, HD, W::B>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, k0, a.tokens, hd, quads);
   if (tid < W::B) bad[tid] = 0u;
   const float scale2 = a.scale * kLog2e;
   float dk[W::R][W::C] = {}, dv[W::R][W::C] = {};
   const Bounds bounds(a, rep);
   const int64_t end = bounds.last_query((int)min(k0 + W::B, a.tokens) - 1);
-  for (int head = kvh * group; head < (kvh + 1) * group; ++head) {
-    const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens;
-    for (int64_t i0 = k0; i0 < end; i0 += W::B) {
-      __syncthreads();
-      load_tile<T, HD>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, i0, a.tokens, hd);
-      load_tile<T, HD>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, i0, a.tokens, hd);
-      if (tid < W::B) {
-        const bool in = i0 + tid < a.tokens;
-        lse2[tid] = in ? a.lse[stat + i0 + tid] * kLog2e : 0.f;
-        dot[tid] = in ? a.dot[stat + i0 + tid] : 0.f;
-        int stop;
-        bounds.rows((int)i0 + (tid & ~31), &start[tid], &stop);
-      }
-      __syncthreads();
-      float s[W::R][W::R], g[W::R][W::R];
-      dots<HD>(sk, sq, ty, tx, s);
-      dots<HD>(sv, sg, ty, tx, g);
+  // steps are tiles of queries, head by head; this CTA has its part of them
+  const int per = end > k0 ? (int)((end - k0 + W::N - 1) / W::N) : 0;
+  const int64_t all = (int64_t)per * group;
+  for (int64_t step = all * rank / split; step < all * (rank + 1) / split; ++step) {
+    const int head = kvh * group + (int)(step / per);
+    const int64_t i0 = k0 + step % per * W::N, stat = ((int64_t)rep * a.heads + head) * a.tokens;
+    __syncthreads();
+    load_tile<T, HD, W::N>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, i0, a.tokens, hd, quads);
+    load_tile<T, HD, W::N>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, i0, a.tokens, hd, quads);
+    if (tid < W::N) {
+      int stop;
+      lse2[tid] = i0 + tid < a.tokens ? a.lse[stat + i0 + tid] * kLog2e : 0.f;
+      bounds.rows((int)i0 + (tid & ~31), &start[tid], &stop);
+    }
+    __syncthreads();
+    row_dots<T, HD, W::N>(dot, sg, head_ptr<const T>(a.out, rep, head, hd), a.out.row, i0, a.tokens, hd, quads);
+    float s[W::R][W::K], g[W::R][W::K];
+    dots<W, HD>(sk, sq, ty, tx, s);
+    dots<W, HD>(sv, sg, ty, tx, g);
+    __syncthreads();
 #pragma unroll
-      for (int r = 0; r < W::R; ++r) {
-        const int64_t j = k0 + ty * W::R + r;
+    for (int r = 0; r < W::R; ++r) {
+      const int64_t j = k0 + ty * W::R + r;
 #pragma unroll
-        for (int c = 0; c < W::R; ++c) {
-          const int col = tx + 16 * c;
-          const bool seen = j >= start[col] && j <= i0 + col;
-          const float p = seen ? exp2f(fmaf(s[r][c], scale2, -lse2[col])) : 0.f;
-          sp[(ty * W::R + r) * W::PS + col] = p;
-          s[r][c] = seen ? p * (g[r][c] - dot[col]) : 0.f;
-        }
+      for (int c = 0; c < W::K; ++c) {
+        const int col = tx + 16 * c;
+        const bool seen = j >= start[col] && j <= i0 + col;
+        const float p = seen ? exp2f(fmaf(s[r][c], scale2, -lse2[col])) : 0.f;
+        sp[(ty * W::R + r) * W::PS + col] = p;
+        s[r][c] = seen ? p * (g[r][c] - dot[col]) : 0.f;
       }
-      __syncwarp();                        // (a row of scores is one half warp's)
-      accumulate<HD>(sp, sg, ty, tx, dv);
-      __syncwarp();
+    }
+    __syncwarp();                        // (a row of scores is one half warp's)
+    accumulate<W, HD>(sp, sg, ty, tx, dv);
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < W::R; ++r)
+#pragma unroll
+      for (int c = 0; c < W::K; ++c) sp[(ty * W::R + r) * W::PS + tx + 16 * c] = s[r][c];
+    __syncwarp();
+    accumulate<W, HD>(sp, sq, ty, tx, dk);
+  }
+  if (split > 1) {
+    // a thread's numbers beside those of the other threads, so that neighbours read neighbouring words
+    __syncthreads();
+    if (rank > 0) {
 #pragma unroll
       for (int r = 0; r < W::R; ++r)
 #pragma unroll
-        for (int c = 0; c < W::R; ++c) sp[(ty * W::R + r) * W::PS + tx + 16 * c] = s[r][c];
-      __syncwarp();
-      accumulate<HD>(sp, sq, ty, tx, dk);
+        for (int c = 0; c < W::C; ++c) {
+          sm[(r * W::C + c) * kNT + tid] = dk[r][c];
+          sm[((W::R + r) * W::C + c) * kNT + tid] = dv[r][c];
+        }
     }
+    ptx::cluster_sync_all();
+    if (rank == 0) {
+      for (int p = 1; p < split; ++p) {
+        const uint32_t at = ptx::map_to_rank(ptx::smem_u32(sm + tid), p);
+#pragma unroll
+        for (int r = 0; r < W::R; ++r)
+#pragma unroll
+          for (int c = 0; c < W::C; ++c) {
+            dk[r][c] += ptx::ld_cluster_f32(at + (r * W::C + c) * kNT * 4);
+            dv[r][c] += ptx::ld_cluster_f32(at + ((W::R + r) * W::C + c) * kNT * 4);
+          }
+      }
+    }
+    ptx::cluster_sync_all();               // (the others' shared memory has been read)
+    if (rank > 0) return;
   }
   float one[W::R], scale[W::R];
 #pragma unroll
   for (int r = 0; r < W::R; ++r) { one[r] = 1.f; scale[r] = a.scale; }
-  bool good = write_rows<T, HD>(head_ptr<T>(a.dk, rep, kvh, hd), a.dk.row, k0, a.tokens, hd, ty, tx, dk, scale, bad);
-  good = write_rows<T, HD>(head_ptr<T>(a.dv, rep, kvh, hd), a.dv.row, k0, a.tokens, hd, ty, tx, dv, one, bad) && good;
+  bool good = write_rows<T, W, HD>(head_ptr<T>(a.dk, rep, kvh, hd), a.dk.row, k0, a.tokens, hd, ty, tx, dk, scale, bad);
+  good = write_rows<T, W, HD>(head_ptr<T>(a.dv, rep, kvh, hd), a.dv.row, k0, a.tokens, hd, ty, tx, dv, one, bad) && good;
   if (__syncthreads_and(good)) return;
   for (int r = tid >> 5; r < W::B; r += kNT / 32)
     if (bad[r] != 0u) dkv_row<T>(a, rep, kvh, (int)k0 + r);
 }
 
-template <typename T, int HD>
-cudaError_t launch(const Args& a, bool grad, cudaStream_t st) {
-  using W = Way<HD>;
-  const int fwd = (3 * W::tile + W::scores) * 4, bwd = (4 * W::tile + W::scores) * 4;
-  static_assert((4 * W::tile + W::scores) * 4 <= 220 * 1024, "shared memory budget");
-  static uint64_t done[3] = {0, 0, 0};   // one bit per device
-  const int64_t tiles = (a.tokens + W::B - 1) / W::B;
-  if (!grad) {
-    const cudaError_t e = allow_dynamic_smem(attention_kernel<T, HD>, fwd, &done[0]);
-    if (e != cudaSuccess) return e;
-    return launch_dep(attention_kernel<T, HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kNT), fwd, st, 1, a);
+// The first `key_units` times `split` CTAs have tiles of keys (those with the most queries first), the others tiles of queries (those
+// with the most keys first).
+template <typename T, int HD, int RB>
+__global__ void __launch_bounds__(kNT)
+attention_grad_kernel(const __grid_constant__ Args a, const bool quads, const int key_units, const int query_units, const int split) {
+  using W = Way<HD, RB>;
+  extern __shared__ __align__(16) float sm[];
+  __shared__ uint32_t bad[W::B];
+  constexpr int M = W::B > W::N ? W::B : W::N;
+  __shared__ float lse2[M], dot[M];
+  __shared__ int start[M];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int unit = (int)blockIdx.x / split;
+  if (unit < key_units) {
+    grad_keys<T, HD, RB>(a, quads, sm, bad, start, lse2, dot, unit, (int)blockIdx.x % split, split);
+  } else {
+    const int query = (int)blockIdx.x - key_units * split;
+    if (query < query_units) grad_queries<T, HD, RB>(a, quads, sm, bad, start, lse2, dot, query);
   }
-  cudaError_t e = allow_dynamic_smem(attention_dq_kernel<T, HD>, bwd, &done[1]);
-  if (e == cudaSuccess) e = allow_dynamic_smem(attention_dkv_kernel<T, HD>, bwd, &done[2]);
-  if (e == cudaSuccess) e = launch_dep(attention_dq_kernel<T, HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kNT), bwd, st, 1, a);
-  if (e == cudaSuccess)
-    e = launch_dep(attention_dkv_kernel<T, HD>, dim3((unsigned)(tiles * a.kv_heads * a.m)), dim3(kNT), bwd, st, 1, a);
-  return e;
+}
+
+// fours of elements: their rows, heads and replicas start on a boundary of 16 (bf16: 8) bytes
+template <typename T>
+bool whole_quads(const Args& a) {
+  if (a.head_dim % 4 != 0) return false;
+  for (const Tensor* t : {&a.q, &a.k, &a.v, &a.out, &a.dout})
+    if (t->p != nullptr && (reinterpret_cast<uintptr_t>(t->p) % (4 * sizeof(T)) != 0 || t->row % 4 != 0 || t->replica % 4 != 0)) return false;
+  return true;
+}
+// How many CTAs share the queries of a tile of keys: as many, up to eight, as still find an SM, two to each.
+int query_split(int64_t key_units) {
+  int split = 1;
+  while (split < 8 && key_units * split * 2 <= 2 * 148) split *= 2;
+  return split;
+}
+
+template <typename T, int HD, int RB>
+cudaError_t launch(const Args& a, bool grad, cudaStream_t st) {
+  using W = Way<HD, RB>;
+  constexpr int fwd = (W::rows + 2 * W::block + W::scores) * 4, bwd = (2 * W::rows + 2 * W::block + W::scores) * 4;
+  static_assert(bwd <= 220 * 1024, "shared memory budget");
+  static_assert(2 * W::R * W::C * kNT <= 2 * W::rows + 2 * W::block, "the parts of a cluster");
+  static uint64_t done[2] = {0, 0};      // one bit per device
+  const int64_t tiles = (a.tokens + W::B - 1) / W::B;
+  const bool quads = whole_quads<T>(a);
+  if (!grad) {
+    const cudaError_t e = allow_dynamic_smem(attention_kernel<T, HD, RB>, fwd, &done[0]);
+    if (e != cudaSuccess) return e;
+    return launch_dep(attention_kernel<T, HD, RB>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kNT), fwd, st, 1, a, quads);
+  }
+  const cudaError_t e = allow_dynamic_smem(attention_grad_kernel<T, HD, RB>, bwd, &done[1]);
+  if (e != cudaSuccess) return e;
+  const int64_t key_units = tiles * a.kv_heads * a.m, query_units = tiles * a.heads * a.m;
+  const int split = query_split(key_units);
+  const int64_t ctas = key_units * split + (query_units + split - 1) / split * split;
+  return launch_dep(attention_grad_kernel<T, HD, RB>, dim3((unsigned)ctas), dim3(kNT), bwd, st, (unsigned)split, a, quads,
+                    (int)key_units, (int)query_units, split);
+}
+// Tiles of 64 rows, or of 32 where those would leave SMs without one: a tile's blocks of keys follow one another, and half the rows
+// take about half the time.
+template <typename T, int HD>
+cudaError_t pick_rows(const Args& a, bool grad, cudaStream_t st) {
+  const bool few = (a.tokens + 63) / 64 * a.heads * a.m <= 148;
+  return few ? launch<T, HD, 32>(a, grad, st) : launch<T, HD, 64>(a, grad, st);
 }
 template <typename T>
 cudaError_t pick(const Args& a, bool grad, cudaStream_t st) {
-  if (a.head_dim <= 32) return launch<T, 32>(a, grad, st);
-  if (a.head_dim <= 64) return launch<T, 64>(a, grad, st);
-  if (a.head_dim <= 128) return launch<T, 128>(a, grad, st);
-  return launch<T, 256>(a, grad, st);
+  if (a.head_dim <= 32) return pick_rows<T, 32>(a, grad, st);
+  if (a.head_dim <= 64) return pick_rows<T, 64>(a, grad, st);
+  if (a.head_dim <= 128) return pick_rows<T, 128>(a, grad, st);
+  return launch<T, 256, 32>(a, grad, st);
 }
 cudaError_t run(const Args& a, int dtype, bool grad, cudaStream_t st) {
   return dtype == LS_DTYPE_BF16 ? pick<__nv_bfloat16>(a, grad, st) : pick<float>(a, grad, st);
@@ -415,8 +515,8 @@ int check_sizes(int m, int64_t tokens, int heads, int kv_heads, int head_dim, in
   if (m < 1 || tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || head_dim < 1) return LS_ERR_INVALID_ARG;
   if (dtype != LS_DTYPE_FP32 && dtype != LS_DTYPE_BF16) return LS_ERR_INVALID_ARG;
   if (m > 65535 || tokens > (1ll << 30) || heads > 65536 || head_dim > 256) return LS_ERR_TOO_LARGE;
-  // (tiles of 32 rows, all heads, all replicas: blocks of one launch)
-  if ((tokens + 31) / 32 * heads > 2147483647ll / m) return LS_ERR_TOO_LARGE;
+  // (tiles of 32 rows, all heads, all replicas, of queries and keys: blocks of one launch)
+  if ((tokens + 31) / 32 * heads > 1073741823ll / m) return LS_ERR_TOO_LARGE;
   return LS_OK;
 }
 // distances that no element uses, as the kernels' tensor maps take them
