@@ -559,35 +559,36 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     const uint32_t idesc_o = make_idesc(1, false, true, kB, (uint32_t)cols);
     constexpr uint32_t T = L::kTile / 16;
     const uint32_t qb = k_major(smem_u32(smem)), gb = qb + T, kb = k_major(smem_u32(sk)), vb = k_major(smem_u32(sv)), kmn = mn_major(smem_u32(sk));
+    bool ok = true;
     auto scores = [&](int i) {           // S and dP of block i
       const int ks = i % L::kK, vs = i % L::kV;
-      bool got = mbar_wait(&k_full[ks], (i / L::kK) & 1);
-      if (i == 0) got = got && mbar_wait(&q_full[0], 0);
-      if (!__all_sync(0xffffffffu, got)) return false;
+      wait(&k_full[ks], (i / L::kK) & 1, ok);
+      if (i == 0) wait(&q_full[0], 0, ok);
       tc_fence_after_sync();
       product_ss<HD>(lead, tmem + L::kS, qb, kb + ks * T, idesc_s, ksteps);
-      got = mbar_wait(&v_full[vs], (i / L::kV) & 1);
-      if (i == 0) got = got && mbar_wait(&q_full[1], 0);
-      if (!__all_sync(0xffffffffu, got)) return false;
+      wait(&v_full[vs], (i / L::kV) & 1, ok);
+      if (i == 0) wait(&q_full[1], 0, ok);
       tc_fence_after_sync();
       product_ss<HD>(lead, tmem + L::kP, gb, vb + vs * T, idesc_s, ksteps);
       mma_commit_if(lead, s_full);
       mma_commit_if(lead, &v_empty[vs]);
-      return true;
     };
-    if (n > 0 && !scores(0)) failed = true;
-    for (int i = 0; i < n && !failed; ++i) {
+    if (n > 0) scores(0);
+    for (int i = 0; i < n; ++i) {
       if (i + 1 < n) {
-        if (!__all_sync(0xffffffffu, mbar_wait(s_free, i & 1)) || !scores(i + 1)) { failed = true; break; }
+        wait(s_free, i & 1, ok);
+        scores(i + 1);
       }
-      if (!__all_sync(0xffffffffu, mbar_wait(&ds_ready[i & 1], (i >> 1) & 1))) { failed = true; break; }
+      wait(&ds_ready[i & 1], (i >> 1) & 1, ok);
       tc_fence_after_sync();
       const uint32_t ds = tmem + L::kDs + (i & 1) * 64, k0 = kmn + (i % L::kK) * T;
       product_ts(lead, tmem + L::kO, ds, k0, idesc_o, i > 0);
       product_ts(lead, tmem + L::kO, ds + 32, k0 + kHalfRows, idesc_o, true);
       mma_commit_if(lead, &k_empty[i % L::kK]);
       mma_commit_if(lead && i == n - 1, done);
+      if (!__all_sync(0xffffffffu, ok)) break;
     }
+    if (!__all_sync(0xffffffffu, ok)) failed = true;
     if (failed && lane == 0) atomicExch(a.err, 45);
   } else {
     const int half = (warp - 2) >> 2, q = warp & 3, r = q * 32 + lane, row = r0 + r;
@@ -619,9 +620,9 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     const float dot = dpart[r] + dpart[kB + r];
     if (half == 0 && row < a.tokens) a.dot[stat] = dot;
     const float scale2 = a.scale * kLog2e;
+    bool ok = true;
     for (int i = 0; i < n; ++i) {
-      if (!__all_sync(0xffffffffu, mbar_wait(s_full, i & 1))) { failed = true; break; }
-      __syncwarp();
+      wait(s_full, i & 1, ok);
       tc_fence_after_sync();
       uint32_t s[2][32], g[2][32];
 #pragma unroll
@@ -631,7 +632,7 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
       tmem_ld_wait();
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(s_free);
+      mbar_arrive_if(lane == 0, s_free);
       const int at = (sp.lo + i) * kB + half * 64;
       const int from = start - at, to = row - at;          // visible columns [from, to]
       const bool cut = __any_sync(0xffffffffu, from > 0 || to < 63);
@@ -655,14 +656,12 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
       tmem_st_wait();
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&ds_ready[i & 1]);
-      __syncwarp();
+      mbar_arrive_if(lane == 0, &ds_ready[i & 1]);
+      if (!__all_sync(0xffffffffu, ok)) break;
     }
-    if (n > 0 && !failed) {
-      if (!__all_sync(0xffffffffu, mbar_wait(done, 0))) failed = true;
-      __syncwarp();
-      tc_fence_after_sync();
-    }
+    if (n > 0) wait(done, 0, ok);
+    if (!__all_sync(0xffffffffu, ok)) failed = true;
+    tc_fence_after_sync();
     if (failed && lane == 0) atomicExch(a.err, 46);
     if (!failed && r0 + q * 32 < a.tokens) {
       const bool none = start > row;
@@ -845,28 +844,28 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     constexpr uint32_t T = L::kTile / 16;
     const uint32_t kb = k_major(smem_u32(smem)), vb = kb + T, qb = k_major(smem_u32(sq)), gb = k_major(smem_u32(sg));
     const uint32_t qmn = mn_major(smem_u32(sq)), gmn = mn_major(smem_u32(sg));
+    bool ok = true;
     auto scores = [&](int i) {
       const int qs = i % L::kQ;
-      bool got = mbar_wait(&q_full[qs], (i / L::kQ) & 1);
-      if (i == 0) got = got && mbar_wait(&kv_full[0], 0);
-      if (!__all_sync(0xffffffffu, got)) return false;
+      wait(&q_full[qs], (i / L::kQ) & 1, ok);
+      if (i == 0) wait(&kv_full[0], 0, ok);
       tc_fence_after_sync();
       product_ss<HD>(lead, tmem + L::kS, kb, qb + qs * T, idesc_s, ksteps);
       mma_commit_if(lead, s_full);
-      return true;
     };
     auto dots = [&](int i) {
       const int gs = i % L::kG;
-      bool got = mbar_wait(&g_full[gs], (i / L::kG) & 1);
-      if (i == 0) got = got && mbar_wait(&kv_full[1], 0);
-      if (!__all_sync(0xffffffffu, got)) return false;
+      wait(&g_full[gs], (i / L::kG) & 1, ok);
+      if (i == 0) wait(&kv_full[1], 0, ok);
       tc_fence_after_sync();
       product_ss<HD>(lead, tmem + L::kDp, vb, gb + gs * T, idesc_s, ksteps);
       mma_commit_if(lead, dp_full);
-      return true;
     };
-    if (n > 0 && !(scores(0) && dots(0))) failed = true;
-    for (int i = 0; i < n && !failed; ++i) {
+    if (n > 0) {
+      scores(0);
+      dots(0);
+    }
+    for (int i = 0; i < n; ++i) {
       const int qs = i % L::kQ, gs = i % L::kG;
       auto dv = [&]() {
         product_ts(lead, tmem + L::kDv, tmem + L::kP, gmn + gs * T, idesc_o, i > 0);
@@ -879,25 +878,29 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         mma_commit_if(lead, &q_empty[qs]);
         mma_commit_if(lead && i == n - 1, done);
       };
-      if (!__all_sync(0xffffffffu, mbar_wait(p_ready, i & 1))) { failed = true; break; }
+      wait(p_ready, i & 1, ok);
       tc_fence_after_sync();
       if (L::kShared) {
         dv();
-        if (i + 1 < n && (!__all_sync(0xffffffffu, mbar_wait(&g_empty[gs], (i / L::kG) & 1)) || !scores(i + 1))) { failed = true; break; }
+        if (i + 1 < n) wait(&g_empty[gs], (i / L::kG) & 1, ok);
+        if (i + 1 < n) scores(i + 1);
       } else {
-        if (i + 1 < n && !scores(i + 1)) { failed = true; break; }
+        if (i + 1 < n) scores(i + 1);
         dv();
       }
-      if (!__all_sync(0xffffffffu, mbar_wait(ds_ready, i & 1))) { failed = true; break; }
+      wait(ds_ready, i & 1, ok);
       tc_fence_after_sync();
       if (L::kShared) {
         dk();
-        if (i + 1 < n && (!__all_sync(0xffffffffu, mbar_wait(&q_empty[qs], (i / L::kQ) & 1)) || !dots(i + 1))) { failed = true; break; }
+        if (i + 1 < n) wait(&q_empty[qs], (i / L::kQ) & 1, ok);
+        if (i + 1 < n) dots(i + 1);
       } else {
-        if (i + 1 < n && !dots(i + 1)) { failed = true; break; }
+        if (i + 1 < n) dots(i + 1);
         dk();
       }
+      if (!__all_sync(0xffffffffu, ok)) break;
     }
+    if (!__all_sync(0xffffffffu, ok)) failed = true;
     if (failed && lane == 0) atomicExch(a.err, 48);
   } else {
     const int half = (warp - 2) >> 2, q = warp & 3, r = q * 32 + lane, key = k0 + r;
@@ -906,14 +909,15 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     bounds.rows(k0 + q * 32, &start, &seq_end);
     const float scale2 = a.scale * kLog2e;
     int tile = kt;
+    bool ok = true;
     for (int i = 0; i < n; ++i) {
       const float* st = stats + (i & 1) * 2 * kB + half * 64;
       const int at = tile * kB + half * 64;
       const int from = key - at, to = seq_end - 1 - at;    // visible columns [from, to]
       const bool cut = __any_sync(0xffffffffu, from > 0 || to < 63);
       float p[64];
-      if (!__all_sync(0xffffffffu, mbar_wait(&st_full[i & 1], (i >> 1) & 1) && mbar_wait(s_full, i & 1))) { failed = true; break; }
-      __syncwarp();
+      wait(&st_full[i & 1], (i >> 1) & 1, ok);
+      wait(s_full, i & 1, ok);
       tc_fence_after_sync();
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -935,16 +939,14 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = pack2(p[c * 32 + 2 * e], p[c * 32 + 2 * e + 1]);
-        if (!L::kShared && c == 0 && i > 0 && !__all_sync(0xffffffffu, mbar_wait(&g_empty[(i - 1) % L::kG], ((i - 1) / L::kG) & 1))) failed = true;
+        if (!L::kShared && c == 0 && i > 0) wait(&g_empty[(i - 1) % L::kG], ((i - 1) / L::kG) & 1, ok);
         tmem_st_32x16(tmem + L::kP + left + c * 16, w);
       }
       tmem_st_wait();
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(p_ready);
-      if (failed) break;
-      if (!__all_sync(0xffffffffu, mbar_wait(dp_full, i & 1))) { failed = true; break; }
-      __syncwarp();
+      mbar_arrive_if(lane == 0, p_ready);
+      wait(dp_full, i & 1, ok);
       tc_fence_after_sync();
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -966,22 +968,19 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = pack2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1]));
-        if (!L::kShared && c == 0 && i > 0 && !__all_sync(0xffffffffu, mbar_wait(&q_empty[(i - 1) % L::kQ], ((i - 1) / L::kQ) & 1))) failed = true;
+        if (!L::kShared && c == 0 && i > 0) wait(&q_empty[(i - 1) % L::kQ], ((i - 1) / L::kQ) & 1, ok);
         tmem_st_32x16(tmem + L::kDs + left + c * 16, w);
       }
       tmem_st_wait();
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(ds_ready);
-      if (failed) break;
-      __syncwarp();
+      mbar_arrive_if(lane == 0, ds_ready);
+      if (!__all_sync(0xffffffffu, ok)) break;
       if (++tile == kt + per) tile = kt;
     }
-    if (n > 0 && !failed) {
-      if (!__all_sync(0xffffffffu, mbar_wait(done, 0))) failed = true;
-      __syncwarp();
-      tc_fence_after_sync();
-    }
+    if (n > 0) wait(done, 0, ok);
+    if (!__all_sync(0xffffffffu, ok)) failed = true;
+    tc_fence_after_sync();
     if (failed && lane == 0) atomicExch(a.err, 49);
     if (!failed && k0 + q * 32 < a.tokens) {
       const bool none = seq_end <= key;
