@@ -455,15 +455,17 @@ __device__ __forceinline__ bool result_rows(uint32_t ta, int half, int cols, boo
 }
 
 // dq, a tile of 128 rows of one head: S = Q K^T and dP = dO V^T of the next block run while the elements of this one become
-// dS = P (dP - D), and dq += dS K follows.  S and dP are free as soon as they are in registers; dS, in bf16 (2^-8 of each term), has two
-// places of its own.  D is formed here from dout and out, and left for the other kernel.
+// dS = P (dP - D), and dq += dS K follows.  S and dP are free as soon as they are in registers.  A row's dS add up to zero, so what
+// its keys have in common cancels, but not in the roundings of dS: it goes to the product in two bf16 pieces (2^-17 of each
+// term; with one, dq was off by 2.65e-3 of its norm, 1.66e-3 of which its own rounding is).  D is formed here from dout and
+// out, and left for the other kernel.
 template <int HD>
 struct Dq {
   static constexpr int kTile = kB * HD * 2;
   static constexpr int kK = 3, kV = 2;                      // slots
   static constexpr int kBars = (2 + kK + kV) * kTile;       // behind Q, dO, the K and V slots
   static constexpr int kTotal = 1024 + kBars + 2 * kB * 4 + 16 + (2 * kK + 2 * kV + 8) * 8 + 16;
-  static constexpr uint32_t kS = 0, kP = 128, kO = 256, kDs = 384;
+  static constexpr uint32_t kS = 0, kP = 128, kO = 256, kDs = 384;     // (dS: 64 columns of first pieces, 64 of second ones)
 };
 struct DqMaps { CUtensorMap q, dout, k, v, dq; };
 
@@ -482,8 +484,8 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
   uint64_t* q_full = v_empty + L::kV;    // [2] Q, dO
   uint64_t* s_full = q_full + 2;         // S and dP of a block
   uint64_t* s_free = s_full + 1;         // eight warps have them in registers
-  uint64_t* ds_ready = s_free + 1;       // [2] eight warps have left dS (two, because a warp may be a block ahead of another)
-  uint64_t* done = ds_ready + 2;
+  uint64_t* ds_ready = s_free + 1;       // eight warps have left dS
+  uint64_t* done = ds_ready + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
   uint8_t* sk = smem + 2 * L::kTile;
   uint8_t* sv = sk + L::kK * L::kTile;
@@ -497,8 +499,7 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     mbar_init(&q_full[1], 1);
     mbar_init(s_full, 1);
     mbar_init(s_free, 8);
-    mbar_init(&ds_ready[0], 8);
-    mbar_init(&ds_ready[1], 8);
+    mbar_init(ds_ready, 8);
     mbar_init(done, 1);
     fence_mbar_init();
     for (int i = 0; i < 4; ++i) bad[i] = 0u;
@@ -579,11 +580,12 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
         wait(s_free, i & 1, ok);
         scores(i + 1);
       }
-      wait(&ds_ready[i & 1], (i >> 1) & 1, ok);
+      wait(ds_ready, i & 1, ok);
       tc_fence_after_sync();
-      const uint32_t ds = tmem + L::kDs + (i & 1) * 64, k0 = kmn + (i % L::kK) * T;
-      product_ts(lead, tmem + L::kO, ds, k0, idesc_o, i > 0);
-      product_ts(lead, tmem + L::kO, ds + 32, k0 + kHalfRows, idesc_o, true);
+      const uint32_t ds = tmem + L::kDs, k0 = kmn + (i % L::kK) * T;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)          // the small pieces first
+        product_ts(lead, tmem + L::kO, ds + (e < 2 ? 64 : 0) + (e & 1) * 32, k0 + (e & 1) * kHalfRows, idesc_o, i > 0 || e > 0);
       mma_commit_if(lead, &k_empty[i % L::kK]);
       mma_commit_if(lead && i == n - 1, done);
       if (!__all_sync(0xffffffffu, ok)) break;
@@ -620,6 +622,7 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     const float dot = dpart[r] + dpart[kB + r];
     if (half == 0 && row < a.tokens) a.dot[stat] = dot;
     const float scale2 = a.scale * kLog2e;
+    const uint64_t by2 = two(scale2, scale2), less2 = two(nl2, nl2), minus_dot = two(-dot, -dot), minus_one = two(-1.f, -1.f);
     bool ok = true;
     for (int i = 0; i < n; ++i) {
       wait(s_full, i & 1, ok);
@@ -638,25 +641,34 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
       const bool cut = __any_sync(0xffffffffu, from > 0 || to < 63);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        uint32_t w[16];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float p = ex2(fmaf(__uint_as_float(s[c][e]), scale2, nl2));
-          g[c][e] = __float_as_uint(p * (__uint_as_float(g[c][e]) - dot));
+        for (int e = 0; e < 32; e += 2) {
+          const float2 x = parts(fma2(two(s[c][e], s[c][e + 1]), by2, less2));
+          const float2 d = parts(mul2(two(ex2(x.x), ex2(x.y)), add2(two(g[c][e], g[c][e + 1]), minus_dot)));
+          g[c][e] = __float_as_uint(d.x);
+          g[c][e + 1] = __float_as_uint(d.y);
         }
-        if (cut) {
+        if (__builtin_expect(cut, 0)) {
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             if (c * 32 + e < from || c * 32 + e > to) g[c][e] = 0u;
         }
+        uint32_t w[16], low[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = pack2(__uint_as_float(g[c][2 * e]), __uint_as_float(g[c][2 * e + 1]));
-        tmem_st_32x16(tmem + L::kDs + (i & 1) * 64 + lanes + half * 32 + c * 16, w);
+        for (int e = 0; e < 16; ++e) {
+          w[e] = pack2(__uint_as_float(g[c][2 * e]), __uint_as_float(g[c][2 * e + 1]));
+          const float2 rest = parts(fma2(two(w[e] << 16, w[e] & 0xFFFF0000u), minus_one, two(g[c][2 * e], g[c][2 * e + 1])));
+          low[e] = pack2(rest.x, rest.y);
+        }
+        // (dS of the block before has been read)
+        if (c == 0 && i > 0) wait(&k_empty[(i - 1) % L::kK], ((i - 1) / L::kK) & 1, ok);
+        tmem_st_32x16(tmem + L::kDs + lanes + half * 32 + c * 16, w);
+        tmem_st_32x16(tmem + L::kDs + 64 + lanes + half * 32 + c * 16, low);
       }
       tmem_st_wait();
       tc_fence_before_sync();
       __syncwarp();
-      mbar_arrive_if(lane == 0, &ds_ready[i & 1]);
+      mbar_arrive_if(lane == 0, ds_ready);
       if (!__all_sync(0xffffffffu, ok)) break;
     }
     if (n > 0) wait(done, 0, ok);
@@ -730,7 +742,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     if (threadIdx.x == 0) atomicExch(a.err, 40);
     return;
   }
-  float* stats = reinterpret_cast<float*>(smem + L::kStats);         // [slot][-lse * log2(e), D][128]
+  float* stats = reinterpret_cast<float*>(smem + L::kStats);         // [slot][-lse * log2(e), -D][128]
   uint32_t* bad = reinterpret_cast<uint32_t*>(smem + L::kBars);      // [4]
   uint64_t* q_full = reinterpret_cast<uint64_t*>(bad + 4);
   uint64_t* q_empty = q_full + L::kQ;
@@ -817,7 +829,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         const int row = tile * kB + e * 32 + lane;
         const bool in = row < a.tokens;
         l[e] = in ? -a.lse[stat + row] * kLog2e : 0.f;
-        d[e] = in ? a.dot[stat + row] : 0.f;
+        d[e] = in ? -a.dot[stat + row] : 0.f;
       }
       if (i >= 2 && !__all_sync(0xffffffffu, mbar_wait(&q_empty[(i - 2) % L::kQ], ((i - 2) / L::kQ) & 1))) { failed = true; break; }
       float* st = stats + (i & 1) * 2 * kB;
@@ -908,6 +920,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     int start, seq_end;
     bounds.rows(k0 + q * 32, &start, &seq_end);
     const float scale2 = a.scale * kLog2e;
+    const uint64_t by2 = two(scale2, scale2);
     int tile = kt;
     bool ok = true;
     for (int i = 0; i < n; ++i) {
@@ -926,13 +939,14 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         tmem_ld_wait();
 #pragma unroll
         for (int e = 0; e < 32; e += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(st + c * 32 + e);
-          p[c * 32 + e] = ex2(fmaf(__uint_as_float(s[e]), scale2, l.x));
-          p[c * 32 + e + 1] = ex2(fmaf(__uint_as_float(s[e + 1]), scale2, l.y));
-          p[c * 32 + e + 2] = ex2(fmaf(__uint_as_float(s[e + 2]), scale2, l.z));
-          p[c * 32 + e + 3] = ex2(fmaf(__uint_as_float(s[e + 3]), scale2, l.w));
+          const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(st + c * 32 + e);
+          const float2 x = parts(fma2(two(s[e], s[e + 1]), by2, l.x)), y = parts(fma2(two(s[e + 2], s[e + 3]), by2, l.y));
+          p[c * 32 + e] = ex2(x.x);
+          p[c * 32 + e + 1] = ex2(x.y);
+          p[c * 32 + e + 2] = ex2(y.x);
+          p[c * 32 + e + 3] = ex2(y.y);
         }
-        if (cut) {
+        if (__builtin_expect(cut, 0)) {
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             if (c * 32 + e < from || c * 32 + e > to) p[c * 32 + e] = 0.f;
@@ -955,13 +969,15 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         tmem_ld_wait();
 #pragma unroll
         for (int e = 0; e < 32; e += 4) {
-          const float4 d = *reinterpret_cast<const float4*>(st + kB + c * 32 + e);
-          g[e] = __float_as_uint(p[c * 32 + e] * (__uint_as_float(g[e]) - d.x));
-          g[e + 1] = __float_as_uint(p[c * 32 + e + 1] * (__uint_as_float(g[e + 1]) - d.y));
-          g[e + 2] = __float_as_uint(p[c * 32 + e + 2] * (__uint_as_float(g[e + 2]) - d.z));
-          g[e + 3] = __float_as_uint(p[c * 32 + e + 3] * (__uint_as_float(g[e + 3]) - d.w));
+          const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(st + kB + c * 32 + e);
+          const float2 x = parts(mul2(two(p[c * 32 + e], p[c * 32 + e + 1]), add2(two(g[e], g[e + 1]), d.x)));
+          const float2 y = parts(mul2(two(p[c * 32 + e + 2], p[c * 32 + e + 3]), add2(two(g[e + 2], g[e + 3]), d.y)));
+          g[e] = __float_as_uint(x.x);
+          g[e + 1] = __float_as_uint(x.y);
+          g[e + 2] = __float_as_uint(y.x);
+          g[e + 3] = __float_as_uint(y.y);
         }
-        if (cut) {                         // (0 times NaN)
+        if (__builtin_expect(cut, 0)) {    // (0 times NaN)
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             if (c * 32 + e < from || c * 32 + e > to) g[e] = 0u;
