@@ -3,15 +3,15 @@
 // Forward.  A CTA takes 256 consecutive rows of one head as two tiles of 128 (rows of S are TMEM lanes) and passes over the keys in
 // blocks of 128, once:
 //   warp 0     TMA producer: both tiles of Q, then K and V blocks through a ring
-//   warps 1, 2 issue the MMAs of a tile: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory, where it
-//              takes the place of S).  Per block: PV of the block before, then S of this one
+//   warps 1, 2 issue the MMAs of a tile: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory)
 //   warps 3-6, 7-10   the softmax of a tile, a thread a row: 128 scores in registers, maximum, exponentials, sum, P in bf16 back
 //              to tensor memory in two halves, on the first of which PV starts
 // The tensor core works for one tile while the other's softmax runs.  For that the two have to stay half a block apart: S of a tile
 // waits until the other one is past its maxima.  (Without, both end in step: 994 us instead of 945 for 16384 rows of 16
 // heads of 128.  With two threads a row, and twice the warps: 1013 us.)
-// A commit arrives when everything issued before it is complete, so S of a block also says that the PV before it is done: S is
-// issued only then, because it overwrites P.
+// Heads of 128 fill the tensor memory with S and O, and P takes the place of S: S of a block is issued when the PV before it is
+// done.  Smaller ones have a place for P, and S of the next block is issued as soon as this one's is in registers (8192 rows of
+// 16 heads of 64: 240 us with P in the place of S).
 // O stays in tensor memory over all blocks and is rescaled only where a row's maximum has grown by more than 2^8 since its
 // reference was taken: P then lies below 2^8 instead of 1, which costs bf16 and fp32 no precision, and most blocks need no
 // pass over O.  P is rounded to bf16 (2^-8 of each term, signs at random), its sum is taken before the rounding.
@@ -32,8 +32,10 @@ struct Fwd {
   static constexpr int kSlots = HD == 128 ? 2 : 3;          // of a K and a V block
   static constexpr int kRing = 2 * kTile;                   // offset of the ring, behind Q
   static constexpr int kBars = kRing + kSlots * 2 * kTile;
-  static constexpr int kTotal = 1024 + kBars + (2 * kSlots + 12) * 8 + 16;
-  static constexpr uint32_t kO = 256;                       // first TMEM column of O (tile X: + X HD); S: 0 and 128
+  static constexpr int kTotal = 1024 + kBars + (2 * kSlots + 14) * 8 + 16;
+  // TMEM columns: S at 0 and 128, O from 256 on (tile x: + x HD); P, 64 columns, in the place of S, or behind O where that ends early
+  static constexpr bool kShared = HD == 128;
+  static constexpr uint32_t kO = 256, kP = kShared ? 0 : 384, kPStep = kShared ? kB : 64;
 };
 
 struct FwdMaps { CUtensorMap q, k, v, out; };
@@ -131,14 +133,15 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   uint64_t* s_full = q_full + 2;         // [2] S of the next block is there, and the PV before it done
   uint64_t* p_half = s_full + 2;         // [half][tile] four warps have left P of the first 64 keys, of the others
   uint64_t* past_max = p_half + 4;       // [2] four warps have a block's maxima
-  uint64_t* o_done = past_max + 2;        // [2] a PV is done
+  uint64_t* s_free = past_max + 2;       // [2] four warps have S in registers
+  uint64_t* o_done = s_free + 2;        // [2] a PV is done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_done + 2);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool failed = false;
   if (threadIdx.x == 0) {
     for (int s = 0; s < SLOTS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 2); }
-    for (int x = 0; x < 2; ++x) { mbar_init(&q_full[x], 1); mbar_init(&s_full[x], 1); mbar_init(&p_half[x], 4); mbar_init(&p_half[2 + x], 4); mbar_init(&past_max[x], 4); mbar_init(&o_done[x], 1); }
+    for (int x = 0; x < 2; ++x) { mbar_init(&q_full[x], 1); mbar_init(&s_full[x], 1); mbar_init(&p_half[x], 4); mbar_init(&p_half[2 + x], 4); mbar_init(&past_max[x], 4); mbar_init(&s_free[x], 4); mbar_init(&o_done[x], 1); }
     fence_mbar_init();
     prefetch_tmap(&maps.q);
     prefetch_tmap(&maps.k);
@@ -210,7 +213,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     constexpr uint32_t T = L::kTile / 16;
     const uint32_t q_lo = k_major(smem_u32(smem)) + x * T, k_lo = k_major(smem_u32(smem) + L::kRing);
     const uint32_t v_lo = mn_major(smem_u32(smem) + L::kRing + L::kTile);
-    const uint32_t ts = tmem + x * kB, to = tmem + L::kO + x * HD;
+    const uint32_t ts = tmem + x * kB, tp = tmem + L::kP + x * L::kPStep, to = tmem + L::kO + x * HD;
     const int from = x == 0 ? sa.lo : sb.lo, upto = x == 0 ? sa.hi : sb.hi;
     bool ok = true;
     if (from <= upto) wait(&q_full[x], 0, ok);
@@ -219,25 +222,32 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       const uint32_t turn = (uint32_t)(j - 1 - from) & 1;
       const bool pv = j > from && j <= upto + 1, qk = j >= from && j <= upto;
       wait(&full[s], round & 1, ok);     // (a slot that this tile does not need is let go of in its turn all the same)
+      auto scores = [&]() {
+        tc_fence_after_sync();
+        product_ss<HD>(lead, ts, q_lo, k_lo + s * 2 * T, idesc_s, ksteps);
+        mma_commit_if(lead, &s_full[x]);
+      };
+      if (!L::kShared && qk) {
+        if (j > from) wait(&s_free[x], turn, ok);
+        scores();
+      }
       if (pv) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           wait(&p_half[2 * h + x], turn, ok);
           tc_fence_after_sync();
-          product_ts(lead, to, ts + h * 32, v_lo + s * 2 * T + h * kHalfRows, idesc_o, j - 1 > from || h > 0);
+          product_ts(lead, to, tp + h * 32, v_lo + s * 2 * T + h * kHalfRows, idesc_o, j - 1 > from || h > 0);
         }
         mma_commit_if(lead, &o_done[x]);
       }
-      if (qk) {
+      if (L::kShared && qk) {
         // S goes where P lies: the product that reads it has to be complete (products of other shapes or accumulators are not
         // known to keep their order)
         if (pv) wait(&o_done[x], turn, ok);
         // the other tile is past its maximum: its exponentials and this product run together
         const int b = x == 1 ? j : j - 1, b_from = x == 1 ? sa.lo : sb.lo, b_upto = x == 1 ? sa.hi : sb.hi;
         if (b >= b_from && b <= b_upto) wait(&past_max[1 - x], (uint32_t)(b - b_from) & 1, ok);
-        tc_fence_after_sync();
-        product_ss<HD>(lead, ts, q_lo, k_lo + s * 2 * T, idesc_s, ksteps);
-        mma_commit_if(lead, &s_full[x]);
+        scores();
       }
       mma_commit_if(lead, &empty[s]);
       if (++s == SLOTS) { s = 0; ++round; }
@@ -252,6 +262,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     bounds.rows(r0 + x * kB + q * 32, &start, &end);
     const uint32_t ts = tmem + ((uint32_t)(q * 32) << 16) + x * kB;
     const uint32_t to = tmem + ((uint32_t)(q * 32) << 16) + L::kO + x * HD;
+    const uint32_t tp = tmem + ((uint32_t)(q * 32) << 16) + L::kP + x * L::kPStep;
     const float scale2 = a.scale * kLog2e;
     const int cols = (a.head_dim + 15) / 16 * 16;
     float top = -INFINITY, sum = 0.f;    // the reference of the exponentials (a product, not scaled), and their sum
@@ -273,6 +284,11 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
 #pragma unroll
       for (int c = 0; c < 4; ++c) tmem_ld_32x32(ts + c * 32, s[c]);
       tmem_ld_wait();
+      if (!L::kShared) {
+        tc_fence_before_sync();
+        __syncwarp();
+        mbar_arrive_if(lane == 0, &s_free[x]);
+      }
       if (__builtin_expect(cut, 0)) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) hide(c, s[c]);
@@ -287,8 +303,13 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
         m4[e] = m;
       }
       const float most = max3(max3(m4[0], m4[1], m4[2]), m4[3], m4[3]);
-      __syncwarp();
-      mbar_arrive_if(lane == 0, &past_max[x]);
+      if (L::kShared) {
+        __syncwarp();
+        mbar_arrive_if(lane == 0, &past_max[x]);
+      } else if (j > sp.lo) {            // (PV of the block before is long done: O may be rescaled, and P written)
+        wait(&o_done[x], (j - 1 - sp.lo) & 1, ok);
+        tc_fence_after_sync();
+      }
       // (top = -inf: the difference is infinite, and the factor zero; a NaN goes on into the reference)
       const bool far = !((most - top) * scale2 <= 8.f) && !(most == -INFINITY);
       if (__builtin_expect(__any_sync(0xffffffffu, far), 0)) {
@@ -327,7 +348,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
           part[i & 1] = add2(part[i & 1], two(e.x, e.y));
           p[i] = pack2(e.x, e.y);
         }
-        tmem_st_32x16(ts + c * 16, p);
+        tmem_st_32x16(tp + c * 16, p);
         if (c & 1) {                       // PV may start with the first half of the keys
           tmem_st_wait();
           tc_fence_before_sync();
