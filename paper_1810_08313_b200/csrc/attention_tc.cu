@@ -90,8 +90,9 @@ __device__ __forceinline__ void store_heads(const CUtensorMap* m, const void* sr
 // Operands are tiles of 128 rows in panels of 64 columns (128 bytes a row, 128-byte swizzle, a panel 16 KB), given by the low words
 // of their descriptors: K-major (row = M or N) or MN-major (row = K).
 constexpr uint32_t kDescHi = smem_desc_hi(1024);
-__device__ __forceinline__ uint32_t k_major(uint32_t addr) { return smem_desc_lo(addr, 16); }
-__device__ __forceinline__ uint32_t mn_major(uint32_t addr) { return smem_desc_lo(addr, kB * 128); }
+// (In a cluster, a shared-memory address has the CTA's rank above its 18 bits, where a descriptor has the distance of panels.)
+__device__ __forceinline__ uint32_t k_major(uint32_t addr) { return smem_desc_lo(addr & 0x3FFFF, 16); }
+__device__ __forceinline__ uint32_t mn_major(uint32_t addr) { return smem_desc_lo(addr & 0x3FFFF, kB * 128); }
 // D = A B^T, both K-major, `ksteps` of 16
 template <int HD>
 __device__ __forceinline__ void product_ss(bool lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int ksteps) {
@@ -740,6 +741,9 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
 // next S (dP) waits for the product that reads P (dS).  Smaller ones have places of their own for P and dS, which the elements
 // fill again when that product is done.  A key is seen by the queries from itself to the end of its sequence.  P and dS are
 // rounded to bf16 (2^-8 of each term).
+//
+// Where there are few tiles of keys, a cluster of `split` CTAs shares a tile's queries.  Each leaves its sums in shared memory, and adds
+// up a slice of the columns over all of them, in order (2048 rows of 8 heads on 1 of 128: 16 tiles).
 template <int HD>
 struct Dkv {
   static constexpr int kTile = kB * HD * 2;
@@ -756,10 +760,10 @@ struct DkvMaps { CUtensorMap q, dout, k, v, dk, dv; };
 
 template <int HD>
 __global__ void __launch_bounds__(kBwdThreads, 1)
-attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_constant__ Args a) {
+attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_constant__ Args a, const int split) {
   using L = Dkv<HD>;
   extern __shared__ __align__(1024) uint8_t smem[];                  // (no room to round its start up)
-  if ((smem_u32(smem) & 1023) != 0) {
+  if ((smem_u32(smem) & 1023) != 0) {                                  // (then it is so for every CTA)
     if (threadIdx.x == 0) atomicExch(a.err, 40);
     return;
   }
@@ -816,12 +820,15 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
   grid_dep_launch();
 
   // the keys with the most queries first
-  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, rep = rest % a.m;
+  const int unit = blockIdx.x / split, rank = blockIdx.x % split;
+  const int kvh = unit % a.kv_heads, rest = unit / a.kv_heads, rep = rest % a.m;
   const int kt = rest / a.m, k0 = kt * kB, group = a.heads / a.kv_heads;
   const Bounds bounds(a, rep);
   const int end = bounds.last_query((int)min((int64_t)k0 + kB, a.tokens) - 1);
   const int per = end > k0 ? (end - 1) / kB - kt + 1 : 0;            // tiles of queries of a head
-  const int n = per * group;
+  // this CTA's steps of all: tiles of queries, head by head
+  const int64_t all = (int64_t)per * group;
+  const int first = (int)(all * rank / split), n = (int)(all * (rank + 1) / split) - first;
   const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
 
   if (warp == 0) {
@@ -831,7 +838,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
       mbar_expect_tx(bar, panels * kB * 128);
       for (int c = 0; c < panels; ++c) tma_load_4d_hint(dst + c * kB * 128, m, bar, c * 64, h, token, rep, pol);
     };
-    int head = kvh * group, tile = kt;
+    int head = kvh * group + (per > 0 ? first / per : 0), tile = kt + (per > 0 ? first % per : 0);
     for (int i = 0; i < n && !failed; ++i) {
       const int qs = i % L::kQ, gs = i % L::kG;
       if (i == 0 && lead) load(&maps.k, smem, &kv_full[0], kvh, k0);
@@ -942,7 +949,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     bounds.rows(k0 + q * 32, &start, &seq_end);
     const float scale2 = a.scale * kLog2e;
     const uint64_t by2 = two(scale2, scale2);
-    int tile = kt;
+    int tile = kt + (per > 0 ? first % per : 0);
     bool ok = true;
     for (int i = 0; i < n; ++i) {
       const float* st = stats + (i & 1) * 2 * kB + half * 64;
@@ -1019,34 +1026,99 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     if (!__all_sync(0xffffffffu, ok)) failed = true;
     tc_fence_after_sync();
     if (failed && lane == 0) atomicExch(a.err, 49);
-    if (!failed && k0 + q * 32 < a.tokens) {
-      const bool none = seq_end <= key;
-      uint8_t* box = smem + q * 32 * 128;
-      bool fine = result_rows<HD>(tmem + L::kDk + lanes, half, cols, n > 0, none, a.scale, box, lane);
-      fine = result_rows<HD>(tmem + L::kDv + lanes, half, cols, n > 0, none, 1.f, box + L::kTile, lane) && fine;
-      const uint32_t ill = __ballot_sync(0xffffffffu, !fine);
-      if (ill != 0u && lane == 0) atomicOr(&bad[q], ill);
-      fence_proxy_async_smem();
-    }
-    elements_sync();
-    if (!failed && half == 0 && k0 + q * 32 < a.tokens) {
-      if (lane == 0) {
-        for (int c = 0; c < panels; ++c) {
-          store_heads(&maps.dk, smem + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
-          store_heads(&maps.dv, smem + L::kTile + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
-        }
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        stores_read(bad[q] != 0u);
+    if (split == 1) {
+      if (!failed && k0 + q * 32 < a.tokens) {
+        const bool none = seq_end <= key;
+        uint8_t* box = smem + q * 32 * 128;
+        bool fine = result_rows<HD>(tmem + L::kDk + lanes, half, cols, n > 0, none, a.scale, box, lane);
+        fine = result_rows<HD>(tmem + L::kDv + lanes, half, cols, n > 0, none, 1.f, box + L::kTile, lane) && fine;
+        const uint32_t ill = __ballot_sync(0xffffffffu, !fine);
+        if (ill != 0u && lane == 0) atomicOr(&bad[q], ill);
+        fence_proxy_async_smem();
       }
-      __syncwarp();
-      uint32_t ill = bad[q];
-      while (ill != 0u) {
-        const int e = __ffs(ill) - 1;
-        ill &= ill - 1;
-        dkv_row<__nv_bfloat16>(a, rep, kvh, k0 + q * 32 + e);
+      elements_sync();
+      if (!failed && half == 0 && k0 + q * 32 < a.tokens) {
+        if (lane == 0) {
+          for (int c = 0; c < panels; ++c) {
+            store_heads(&maps.dk, smem + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
+            store_heads(&maps.dv, smem + L::kTile + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
+          }
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          stores_read(bad[q] != 0u);
+        }
+        __syncwarp();
+        uint32_t ill = bad[q];
+        while (ill != 0u) {
+          const int e = __ffs(ill) - 1;
+          ill &= ill - 1;
+          dkv_row<__nv_bfloat16>(a, rep, kvh, k0 + q * 32 + e);
+        }
+      }
+    } else {
+      // [dk, dv][column][row], neighbouring lanes beside each other
+      float* sums = reinterpret_cast<float*>(smem) + r;
+#pragma unroll
+      for (int g = 0; g < 2 * HD / 32; ++g) {
+        const int c = half * HD + g * 16;  // (half 0 has dk, half 1 dv)
+        uint32_t o[16];
+        if (n > 0 && !failed) {
+          tmem_ld_32x16(tmem + L::kDk + lanes + c, o);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = 0u;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[(c + e) * kB] = __uint_as_float(o[e]);
       }
     }
     tc_fence_before_sync();
+  }
+  if (split > 1) {
+    __syncwarp();
+    cluster_sync_all();
+    if (warp >= 2) {
+      constexpr int kMost = 8;             // columns at a time
+      const int t = (warp - 2) * 32 + lane, r = t & (kB - 1), mat = t >> 7, key = k0 + r;
+      const int width = HD / split, from = rank * width;
+      int start, seq_end;
+      bounds.rows(k0 + (r & ~31), &start, &seq_end);
+      const bool none = seq_end <= key;
+      const Tensor& d = mat == 0 ? a.dk : a.dv;
+      __nv_bfloat16* row = head_ptr<__nv_bfloat16>(d, rep, kvh, a.head_dim) + (int64_t)key * d.row;
+      bool fine = true;
+      for (int c = from; c < from + width && c < a.head_dim; c += kMost) {
+        float v[kMost];
+#pragma unroll
+        for (int e = 0; e < kMost; ++e) v[e] = 0.f;
+        for (int p = 0; p < split; ++p) {
+          const uint32_t at = map_to_rank(smem_u32(smem), p) + ((mat * HD + c) * kB + r) * 4;
+#pragma unroll
+          for (int e = 0; e < kMost; ++e) v[e] += ld_cluster_f32(at + e * kB * 4);
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float by = mat == 0 ? a.scale : 1.f, x = v[2 * e] * by, y = v[2 * e + 1] * by;
+          fine = fine && fabsf(x) < INFINITY && fabsf(y) < INFINITY;
+          w[e] = none ? 0u : pack2(x, y);
+        }
+        if (key < a.tokens) *reinterpret_cast<uint4*>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      if (!fine && key < a.tokens) atomicOr(&bad[r >> 5], 1u << (r & 31));
+    }
+    __syncwarp();
+    cluster_sync_all();                    // (all columns written, all rows looked at)
+    if (warp >= 2 && rank == 0) {
+      for (int g = 0; g < 4; ++g) {
+        uint32_t ill = 0;
+        for (int p = 0; p < split; ++p) ill |= __float_as_uint(ld_cluster_f32(map_to_rank(smem_u32(&bad[g]), p)));
+        for (int e = warp - 2; e < 32; e += 8)
+          if (ill >> e & 1) dkv_row<__nv_bfloat16>(a, rep, kvh, k0 + g * 32 + e);
+      }
+    }
+    __syncwarp();
+    cluster_sync_all();                    // (nobody's shared memory is read any more)
   }
   __syncwarp();
   if (failed) {
@@ -1082,8 +1154,13 @@ cudaError_t launch_backward(const DqMaps& dq, const DkvMaps& dkv, const Args& a,
   const int64_t tiles = (a.tokens + kB - 1) / kB;
   if (e == cudaSuccess)
     e = launch_dep(attention_dq_tc_kernel<HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kBwdThreads), Dq<HD>::kTotal, st, 1, dq, a);
+  // as many CTAs to a tile of keys, up to eight, as still find an SM
+  const int64_t units = tiles * a.kv_heads * a.m;
+  int split = 1;
+  while (split < 8 && units * split * 2 <= 148) split *= 2;
   if (e == cudaSuccess)
-    e = launch_dep(attention_dkv_tc_kernel<HD>, dim3((unsigned)(tiles * a.kv_heads * a.m)), dim3(kBwdThreads), Dkv<HD>::kTotal, st, 1, dkv, a);
+    e = launch_dep(attention_dkv_tc_kernel<HD>, dim3((unsigned)(units * split)), dim3(kBwdThreads), Dkv<HD>::kTotal, st, (unsigned)split, dkv, a,
+                   split);
   return e;
 }
 

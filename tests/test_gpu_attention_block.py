@@ -376,6 +376,21 @@ def test_attention_flat_and_sharp(sharp, dtype):
     _attn_run(1, 700, [0, 700], 2, 1, 64, dtype, sharp=sharp)
 
 
+@pytest.mark.parametrize("dtype,hd", [("fp32", 64), ("bf16", 64), ("bf16", 128)])
+def test_attention_many_tiles(hd, dtype):
+    """Enough tiles of keys for all SMs: no cluster shares one."""
+    _attn_run(3, 1100, [0, 500, 1093], 4, 4, hd, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("count", [31, 32, 40, 1400])
+def test_attention_many_sequences(count, dtype):
+    """More boundaries than a warp holds, in one and two levels of the search; some sequences are empty."""
+    import random
+    cuts = sorted(random.Random(count).choices(range(0, 1500), k=count + 1))
+    _attn_run(1, 1500, cuts, 2, 1, 64, dtype)
+
+
 def test_attention_rising_scores():
     """Keys that grow along the sequence: every tile has a new maximum."""
     import torch
