@@ -38,7 +38,7 @@ struct Fwd {
   static constexpr uint32_t kO = 256, kP = kShared ? 0 : 384, kPStep = kShared ? kB : 64;
 };
 
-struct FwdMaps { CUtensorMap q, k, v, out; };
+struct FwdMaps { CUtensorMap q, k, v; };
 
 __device__ __forceinline__ float ex2(float x) { return gop::ex2(x); }
 __device__ __forceinline__ uint32_t pack2(float a, float b) { return gop::pack_bf16(a, b); }
@@ -73,18 +73,16 @@ __device__ __forceinline__ float2 exp2_fma(uint64_t x2) {
 // path, and the polynomial has more: 16384 rows of 16 heads took 979 us with none, 893 us with three, 920 us with five.
 constexpr uint32_t kFmaOf16 = 0x1084;
 
+// Of 32 columns, a bit for each one in [from, to].
+__device__ __forceinline__ uint32_t visible(int from, int to) {
+  return (from > 31 ? 0u : from > 0 ? 0xffffffffu << from : 0xffffffffu) & (to < 0 ? 0u : to < 31 ? (2u << to) - 1 : 0xffffffffu);
+}
+
 // key blocks [lo, hi] that the tile of rows from r0 on needs (lo > hi: none)
 struct Span { int lo, hi; };
 __device__ __forceinline__ Span key_blocks(const Bounds& b, int r0) {
   if (r0 >= b.tokens) return Span{1, 0};
   return Span{b.first_key(r0) / kB, r0 / kB};
-}
-
-__device__ __forceinline__ void store_heads(const CUtensorMap* m, const void* src, int x, int head, int token, int rep) {
-  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(
-                   reinterpret_cast<uint64_t>(m)),
-               "r"(smem_u32(src)), "r"(x), "r"(head), "r"(token), "r"(rep)
-               : "memory");
 }
 
 // Operands are tiles of 128 rows in panels of 64 columns (128 bytes a row, 128-byte swizzle, a panel 16 KB), given by the low words
@@ -115,17 +113,49 @@ __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, bool& ok) {
   if (!mbar_wait(bar, parity, ok ? kSpinLimit : 0)) ok = false;
 }
 
-// This thread's bulk stores have read their shared memory; or, where their rows are to be written once more, are complete.
-__device__ __forceinline__ void stores_read(bool complete) {
-  if (complete) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-  else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+// A tile of 128 rows (tokens) of a head, `panels` of 64 elements.
+__device__ __forceinline__ void load_tile(const CUtensorMap* m, uint8_t* dst, uint64_t* bar, int panels, int head, int token, int rep, uint64_t pol) {
+  mbar_expect_tx(bar, panels * kB * 128);
+  for (int c = 0; c < panels; ++c) tma_load_4d_hint(dst + c * kB * 128, m, bar, c * 64, head, token, rep, pol);
+}
+
+// COLS columns from c0 on of this lane's row of a result in tensor memory, times `by`, in bf16 to `row` (of head_dim elements, or null).
+// Returns whether they are finite; `any`: there is a result; `zero`: zeros instead.  (Rows leave from registers: by way of
+// shared memory and a bulk store the end of a tile took 1000 cycles more, which nothing else runs under.)
+template <int COLS>
+__device__ __forceinline__ bool result_row(uint32_t ta, int c0, int cols, bool any, bool zero, float by, __nv_bfloat16* row, int head_dim) {
+  bool fine = true;
+#pragma unroll
+  for (int g = 0; g < COLS; g += 32) {
+    const int c = c0 + g;
+    uint32_t o[32];
+    if (c < cols && any) {
+      tmem_ld_32x32(ta + c, o);
+      tmem_ld_wait();
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (c + u * 8 >= head_dim) continue;
+      uint32_t w[4] = {0u, 0u, 0u, 0u};
+      if (any && !zero) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = __uint_as_float(o[u * 8 + 2 * e]) * by, y = __uint_as_float(o[u * 8 + 2 * e + 1]) * by;
+          fine = fine && fabsf(x) < INFINITY && fabsf(y) < INFINITY;
+          w[e] = pack2(x, y);
+        }
+      }
+      if (row != nullptr) *reinterpret_cast<uint4*>(row + c + u * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  return fine;
 }
 
 template <int HD>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant__ Args a) {
   using L = Fwd<HD>;
-  constexpr int PANELS = HD / 64, SLOTS = L::kSlots;
+  constexpr int SLOTS = L::kSlots;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
@@ -138,16 +168,25 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   uint64_t* o_done = s_free + 2;        // [2] a PV is done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_done + 2);
 
+  // the rows with the most keys first; heads of a group beside each other
+  const int tiles = (int)((a.tokens + 2 * kB - 1) / (2 * kB));
+  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
+  const int r0 = (tiles - 1 - rest / a.m) * 2 * kB;
+  const int kvh = head / (a.heads / a.kv_heads);
+  const int panels = (a.head_dim + 63) / 64;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool failed = false;
   if (threadIdx.x == 0) {
     for (int s = 0; s < SLOTS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 2); }
     for (int x = 0; x < 2; ++x) { mbar_init(&q_full[x], 1); mbar_init(&s_full[x], 1); mbar_init(&p_half[x], 4); mbar_init(&p_half[2 + x], 4); mbar_init(&past_max[x], 4); mbar_init(&s_free[x], 4); mbar_init(&o_done[x], 1); }
     fence_mbar_init();
-    prefetch_tmap(&maps.q);
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
-    prefetch_tmap(&maps.out);
+    // Q is on its way while the tensor memory is allocated and the boundaries are read
+    fence_proxy_async_smem();
+    grid_dep_wait();
+    for (int x = 0; x < 2; ++x)
+      if (r0 + x * kB < a.tokens) load_tile(&maps.q, smem + x * L::kTile, &q_full[x], panels, head, r0 + x * kB, rep, l2_policy(0));
   }
   __syncwarp();
   if (warp == 1) {
@@ -161,29 +200,14 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   grid_dep_wait();
   grid_dep_launch();
 
-  // the rows with the most keys first; heads of a group beside each other
-  const int tiles = (int)((a.tokens + 2 * kB - 1) / (2 * kB));
-  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
-  const int r0 = (tiles - 1 - rest / a.m) * 2 * kB;
-  const int kvh = head / (a.heads / a.kv_heads);
   const Bounds bounds(a, rep);
   const Span sa = key_blocks(bounds, r0), sb = key_blocks(bounds, r0 + kB);
   const bool has_a = sa.lo <= sa.hi, has_b = sb.lo <= sb.hi;
   const int lo = has_a ? sa.lo : sb.lo, hi = has_b ? sb.hi : sa.hi;        // (lo > hi if neither has any)
-  const int panels = (a.head_dim + 63) / 64;
 
   if (warp == 0) {
     const bool lead = elect_one();
     const uint64_t pol = l2_policy(0);
-    if (lead) {
-      for (int x = 0; x < 2; ++x) {
-        if (!(x == 0 ? has_a : has_b)) continue;
-        mbar_expect_tx(&q_full[x], panels * kB * 128);
-        for (int c = 0; c < panels; ++c)
-          tma_load_4d_hint(smem + x * L::kTile + c * kB * 128, &maps.q, &q_full[x], c * 64, head, r0 + x * kB, rep, pol);
-      }
-    }
-    __syncwarp();
     // slot t: K of block t and V of the block before
     int s = 0, round = 0;
     for (int j = lo; j <= hi + 1 && lo <= hi && !failed; ++j) {
@@ -199,7 +223,9 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       __syncwarp();
       if (++s == SLOTS) { s = 0; ++round; }
     }
-    // the releases of the last slots arrive here: wait for them before leaving
+    // Q that no product needs, and the releases of the last slots, arrive here: wait for them before leaving
+    for (int x = 0; x < 2; ++x)
+      if (r0 + x * kB < a.tokens && !(x == 0 ? has_a : has_b) && !__all_sync(0xffffffffu, mbar_wait(&q_full[x], 0))) failed = true;
     for (int i = 0; i < SLOTS && !failed; ++i) {
       const int uses = round + (i < s ? 1 : 0);
       if (uses > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[i], (uses - 1) & 1))) failed = true;
@@ -275,8 +301,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       const int from = start - j * kB, to_col = row - j * kB;
       const bool cut = __any_sync(0xffffffffu, from > 0 || to_col < kB - 1);
       auto hide = [&](int c, uint32_t (&v)[32]) {
-        const int a0 = from - c * 32, a1 = to_col - c * 32;
-        const uint32_t seen = (a0 > 31 ? 0u : a0 > 0 ? 0xffffffffu << a0 : 0xffffffffu) & (a1 < 0 ? 0u : a1 < 31 ? (2u << a1) - 1 : 0xffffffffu);
+        const uint32_t seen = visible(from - c * 32, to_col - c * 32);
 #pragma unroll
         for (int i = 0; i < 32; ++i)
           if ((seen >> i & 1) == 0) v[i] = 0xff800000u;
@@ -370,48 +395,14 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     if (failed) {
       if (lane == 0) atomicExch(a.err, 43);
     } else if (r0 + x * kB + q * 32 < a.tokens) {
-      // this warp's 32 rows leave through its part of the tile's place for Q
       // (a row with a NaN or +inf, or of -inf only, is computed once more: exp2_fma has no infinities)
       const float by = none ? 0.f : fabsf(top) < INFINITY ? 1.f / sum : NAN;
-      bool fine = true;
-      uint8_t* box = smem + x * L::kTile + q * 32 * 128;
-#pragma unroll
-      for (int c = 0; c < PANELS; ++c) {
-        if (c * 64 >= a.head_dim) break;
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          uint32_t o[16];
-          if (c * 64 + h * 16 < cols && sp.lo <= sp.hi) {
-            tmem_ld_32x16(to + c * 64 + h * 16, o);
-            tmem_ld_wait();
-          }
-          uint32_t w[8];
-          if (c * 64 + h * 16 < cols && !none) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float e = __uint_as_float(o[2 * i]) * by, f = __uint_as_float(o[2 * i + 1]) * by;
-              fine = fine && fabsf(e) < INFINITY && fabsf(f) < INFINITY;
-              w[i] = pack2(e, f);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = 0u;
-          }
-          *gop::box_piece<128>(box + c * kB * 128, lane, h * 2) = make_uint4(w[0], w[1], w[2], w[3]);
-          *gop::box_piece<128>(box + c * kB * 128, lane, h * 2 + 1) = make_uint4(w[4], w[5], w[6], w[7]);
-        }
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        for (int c = 0; c < panels; ++c) store_heads(&maps.out, box + c * kB * 128, c * 64, head, r0 + x * kB + q * 32, rep);
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-      }
+      __nv_bfloat16* dst = row < a.tokens ? head_ptr<__nv_bfloat16>(a.out, rep, head, a.head_dim) + row * a.out.row : nullptr;
+      const bool fine = result_row<HD>(to, 0, cols, sp.lo <= sp.hi, none, by, dst, a.head_dim);
       if (row < a.tokens)
         a.lse[((int64_t)rep * a.heads + head) * a.tokens + row] = none ? 0.f : fmaf(top * scale2, kLn2, logf(sum));
       __syncwarp();
       uint32_t bad = __ballot_sync(0xffffffffu, !none && !fine);
-      if (lane == 0) stores_read(bad != 0u);
       __syncwarp();
       while (bad != 0u) {
         const int r = __ffs(bad) - 1;
@@ -445,37 +436,6 @@ constexpr int kBwdThreads = 320;
 // the named barrier of the eight element warps
 __device__ __forceinline__ void elements_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-// This warp's 32 rows of a result [128][HD] in tensor memory, times `by`, in bf16 into `box` (the rows' place in a tile of panels)
-// and out.  Half h of the columns.  Returns whether the lane's numbers are finite; `zero`: zeros instead.
-template <int HD>
-__device__ __forceinline__ bool result_rows(uint32_t ta, int half, int cols, bool any, bool zero, float by, uint8_t* box, int lane) {
-  bool fine = true;
-#pragma unroll
-  for (int g = 0; g < HD / 32; ++g) {
-    const int c = half * (HD / 2) + g * 16;
-    uint32_t o[16], w[8];
-    if (c < cols && any) {
-      tmem_ld_32x16(ta + c, o);
-      tmem_ld_wait();
-    }
-    if (c < cols && any && !zero) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float e = __uint_as_float(o[2 * i]) * by, f = __uint_as_float(o[2 * i + 1]) * by;
-        fine = fine && fabsf(e) < INFINITY && fabsf(f) < INFINITY;
-        w[i] = pack2(e, f);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = 0u;
-    }
-    uint8_t* panel = box + (c >> 6) * (kB * 128);
-    *gop::box_piece<128>(panel, lane, (c & 63) >> 3) = make_uint4(w[0], w[1], w[2], w[3]);
-    *gop::box_piece<128>(panel, lane, ((c & 63) >> 3) + 1) = make_uint4(w[4], w[5], w[6], w[7]);
-  }
-  return fine;
-}
-
 // dq, a tile of 128 rows of one head: S = Q K^T and dP = dO V^T of the next block run while the elements of this one become
 // dS = P (dP - D), and dq += dS K follows.  S and dP are free as soon as they are in registers.  A row's dS add up to zero, so what
 // its keys have in common cancels, but not in the roundings of dS: it goes to the product in two bf16 pieces (2^-17 of each
@@ -486,10 +446,10 @@ struct Dq {
   static constexpr int kTile = kB * HD * 2;
   static constexpr int kK = 3, kV = 2;                      // slots
   static constexpr int kBars = (2 + kK + kV) * kTile;       // behind Q, dO, the K and V slots
-  static constexpr int kTotal = 1024 + kBars + 2 * kB * 4 + 16 + (2 * kK + 2 * kV + 8) * 8 + 16;
+  static constexpr int kTotal = 1024 + kBars + kB * 4 + 16 + (2 * kK + 2 * kV + 8) * 8 + 16;
   static constexpr uint32_t kS = 0, kP = 128, kO = 256, kDs = 384;     // (dS: 64 columns of first pieces, 64 of second ones)
 };
-struct DqMaps { CUtensorMap q, dout, k, v, dq; };
+struct DqMaps { CUtensorMap q, dout, k, v; };
 
 template <int HD>
 __global__ void __launch_bounds__(kBwdThreads, 1)
@@ -497,8 +457,8 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
   using L = Dq<HD>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  float* dpart = reinterpret_cast<float*>(smem + L::kBars);          // [2][128]
-  uint32_t* bad = reinterpret_cast<uint32_t*>(dpart + 2 * kB);       // [4]
+  float* dots = reinterpret_cast<float*>(smem + L::kBars);           // [128]
+  uint32_t* bad = reinterpret_cast<uint32_t*>(dots + kB);            // [4]
   uint64_t* k_full = reinterpret_cast<uint64_t*>(bad + 4);
   uint64_t* k_empty = k_full + L::kK;
   uint64_t* v_full = k_empty + L::kK;
@@ -512,6 +472,11 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
   uint8_t* sk = smem + 2 * L::kTile;
   uint8_t* sv = sk + L::kK * L::kTile;
 
+  const int tiles = (int)((a.tokens + kB - 1) / kB);
+  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
+  const int r0 = (tiles - 1 - rest / a.m) * kB;
+  const int kvh = head / (a.heads / a.kv_heads);
+  const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool failed = false;
   if (threadIdx.x == 0) {
@@ -525,11 +490,13 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     mbar_init(done, 1);
     fence_mbar_init();
     for (int i = 0; i < 4; ++i) bad[i] = 0u;
-    prefetch_tmap(&maps.q);
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
-    prefetch_tmap(&maps.dout);
-    prefetch_tmap(&maps.dq);
+    // Q and dO are on their way while the tensor memory is allocated and the boundaries are read
+    fence_proxy_async_smem();
+    grid_dep_wait();
+    load_tile(&maps.q, smem, &q_full[0], panels, head, r0, rep, l2_policy(0));
+    load_tile(&maps.dout, smem + L::kTile, &q_full[1], panels, head, r0, rep, l2_policy(0));
   }
   __syncwarp();
   if (warp == 1) {
@@ -543,34 +510,25 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
   grid_dep_wait();
   grid_dep_launch();
 
-  const int tiles = (int)((a.tokens + kB - 1) / kB);
-  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
-  const int r0 = (tiles - 1 - rest / a.m) * kB;
-  const int kvh = head / (a.heads / a.kv_heads);
   const Bounds bounds(a, rep);
   const Span sp = key_blocks(bounds, r0);
   const int n = sp.hi - sp.lo + 1;       // blocks (none: n <= 0)
-  const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
 
   if (warp == 0) {
     const bool lead = elect_one();
     const uint64_t pol = l2_policy(0);
-    auto load = [&](const CUtensorMap* m, uint8_t* dst, uint64_t* bar, int h, int token) {
-      mbar_expect_tx(bar, panels * kB * 128);
-      for (int c = 0; c < panels; ++c) tma_load_4d_hint(dst + c * kB * 128, m, bar, c * 64, h, token, rep, pol);
-    };
     for (int i = 0; i < n && !failed; ++i) {
       const int ks = i % L::kK, vs = i % L::kV;
-      if (i == 0 && lead) load(&maps.q, smem, &q_full[0], head, r0);
       if (i >= L::kK && !__all_sync(0xffffffffu, mbar_wait(&k_empty[ks], (i / L::kK - 1) & 1))) { failed = true; break; }
-      if (lead) load(&maps.k, sk + ks * L::kTile, &k_full[ks], kvh, (sp.lo + i) * kB);
+      if (lead) load_tile(&maps.k, sk + ks * L::kTile, &k_full[ks], panels, kvh, (sp.lo + i) * kB, rep, pol);
       __syncwarp();
-      if (i == 0 && lead) load(&maps.dout, smem + L::kTile, &q_full[1], head, r0);
       if (i >= L::kV && !__all_sync(0xffffffffu, mbar_wait(&v_empty[vs], (i / L::kV - 1) & 1))) { failed = true; break; }
-      if (lead) load(&maps.v, sv + vs * L::kTile, &v_full[vs], kvh, (sp.lo + i) * kB);
+      if (lead) load_tile(&maps.v, sv + vs * L::kTile, &v_full[vs], panels, kvh, (sp.lo + i) * kB, rep, pol);
       __syncwarp();
     }
-    // the releases of the last slots arrive here: wait for them before leaving
+    // tiles that no product needs, and the releases of the last slots, arrive here: wait for them before leaving
+    for (int i = 0; i < 2; ++i)
+      if (n <= 0 && !__all_sync(0xffffffffu, mbar_wait(&q_full[i], 0))) failed = true;
     for (int i = 0; i < L::kK && i < n && !failed; ++i)
       if (!__all_sync(0xffffffffu, mbar_wait(&k_empty[i], ((n - 1 - i) / L::kK) & 1))) failed = true;
     for (int i = 0; i < L::kV && i < n && !failed; ++i)
@@ -620,28 +578,38 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens + row;
     int start, end;
     bounds.rows(r0 + q * 32, &start, &end);
-    float part = 0.f, nl2 = 0.f;
-    if (row < a.tokens) {
-      const __nv_bfloat16* g = head_ptr<const __nv_bfloat16>(a.dout, rep, head, a.head_dim) + row * a.dout.row;
-      const __nv_bfloat16* o = head_ptr<const __nv_bfloat16>(a.out, rep, head, a.head_dim) + row * a.out.row;
+    const float nl2 = row < a.tokens ? -a.lse[stat] * kLog2e : 0.f;
+    {
+      // D of 16 rows a warp, a row's 16-byte pieces in neighbouring lanes (a lane to a row, each of its loads would touch 32 lines,
+      // and the first block waited 4500 cycles for D)
+      constexpr int N = HD / 8, ROWS = 32 / N;
+      const int piece = lane % N, e = piece * 8;
+      const __nv_bfloat16* g = head_ptr<const __nv_bfloat16>(a.dout, rep, head, a.head_dim) + e;
+      const __nv_bfloat16* o = head_ptr<const __nv_bfloat16>(a.out, rep, head, a.head_dim) + e;
+      uint4 x[16 / ROWS], y[16 / ROWS];
 #pragma unroll
-      for (int c = 0; c < HD / 16; ++c) {
-        const int e = (2 * c + half) * 8;
-        if (e < a.head_dim) {
-          const uint4 x = __ldg(reinterpret_cast<const uint4*>(g + e)), y = __ldg(reinterpret_cast<const uint4*>(o + e));
-          const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            part = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), part);
-            part = fmaf(__uint_as_float(u[i] & 0xFFFF0000u), __uint_as_float(v[i] & 0xFFFF0000u), part);
-          }
-        }
+      for (int i = 0; i < 16 / ROWS; ++i) {
+        const int64_t at = r0 + q * 32 + half * 16 + i * ROWS + lane / N;
+        const bool in = at < a.tokens && e < a.head_dim;
+        x[i] = in ? __ldg(reinterpret_cast<const uint4*>(g + at * a.dout.row)) : make_uint4(0u, 0u, 0u, 0u);
+        y[i] = in ? __ldg(reinterpret_cast<const uint4*>(o + at * a.out.row)) : make_uint4(0u, 0u, 0u, 0u);
       }
-      nl2 = -a.lse[stat] * kLog2e;
+#pragma unroll
+      for (int i = 0; i < 16 / ROWS; ++i) {
+        const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, v[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+        float part = 0.f;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          part = fmaf(__uint_as_float(u[f] << 16), __uint_as_float(v[f] << 16), part);
+          part = fmaf(__uint_as_float(u[f] & 0xFFFF0000u), __uint_as_float(v[f] & 0xFFFF0000u), part);
+        }
+#pragma unroll
+        for (int f = N / 2; f > 0; f >>= 1) part += __shfl_xor_sync(0xffffffffu, part, f);
+        if (piece == 0) dots[q * 32 + half * 16 + i * ROWS + lane / N] = part;
+      }
     }
-    dpart[half * kB + r] = part;
     elements_sync();
-    const float dot = dpart[r] + dpart[kB + r];
+    const float dot = dots[r];
     if (half == 0 && row < a.tokens) a.dot[stat] = dot;
     const float scale2 = a.scale * kLog2e;
     const uint64_t by2 = two(scale2, scale2), less2 = two(nl2, nl2), minus_dot = two(-dot, -dot), minus_one = two(-1.f, -1.f);
@@ -671,9 +639,10 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
           g[c][e + 1] = __float_as_uint(d.y);
         }
         if (__builtin_expect(cut, 0)) {
+          const uint32_t seen = visible(from - c * 32, to - c * 32);
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (c * 32 + e < from || c * 32 + e > to) g[c][e] = 0u;
+            if ((seen >> e & 1) == 0) g[c][e] = 0u;
         }
         uint32_t w[16], low[16];
 #pragma unroll
@@ -697,22 +666,14 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
     if (!__all_sync(0xffffffffu, ok)) failed = true;
     tc_fence_after_sync();
     if (failed && lane == 0) atomicExch(a.err, 46);
-    if (!failed && r0 + q * 32 < a.tokens) {
-      const bool none = start > row;
-      uint8_t* box = smem + q * 32 * 128;
-      const bool fine = result_rows<HD>(tmem + L::kO + lanes, half, cols, n > 0, none, a.scale, box, lane);
-      const uint32_t ill = __ballot_sync(0xffffffffu, !fine);
+    if (!failed) {
+      __nv_bfloat16* dst = row < a.tokens ? head_ptr<__nv_bfloat16>(a.dq, rep, head, a.head_dim) + row * a.dq.row : nullptr;
+      const bool fine = result_row<HD / 2>(tmem + L::kO + lanes, half * (HD / 2), cols, n > 0, start > row, a.scale, dst, a.head_dim);
+      const uint32_t ill = __ballot_sync(0xffffffffu, !fine && row < a.tokens);
       if (ill != 0u && lane == 0) atomicOr(&bad[q], ill);
-      fence_proxy_async_smem();
     }
-    elements_sync();                     // (half a panel each, where there is one)
-    if (!failed && half == 0 && r0 + q * 32 < a.tokens) {
-      if (lane == 0) {
-        for (int c = 0; c < panels; ++c) store_heads(&maps.dq, smem + q * 32 * 128 + c * kB * 128, c * 64, head, r0 + q * 32, rep);
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        stores_read(bad[q] != 0u);
-      }
-      __syncwarp();
+    elements_sync();
+    if (!failed && half == 0) {
       uint32_t ill = bad[q];
       while (ill != 0u) {
         const int e = __ffs(ill) - 1;
@@ -756,7 +717,7 @@ struct Dkv {
   // the bf16 of P and dS: half h of the columns at + h * kHalf
   static constexpr uint32_t kP = kShared ? kS : 384, kDs = kShared ? kDp : 448, kHalf = kShared ? 64 : 32;
 };
-struct DkvMaps { CUtensorMap q, dout, k, v, dk, dv; };
+struct DkvMaps { CUtensorMap q, dout, k, v; };
 
 template <int HD>
 __global__ void __launch_bounds__(kBwdThreads, 1)
@@ -784,6 +745,11 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
   uint8_t* sq = smem + 2 * L::kTile;
   uint8_t* sg = sq + L::kQ * L::kTile;
 
+  // the keys with the most queries first
+  const int unit = blockIdx.x / split, rank = blockIdx.x % split;
+  const int kvh = unit % a.kv_heads, rest = unit / a.kv_heads, rep = rest % a.m;
+  const int kt = rest / a.m, k0 = kt * kB, group = a.heads / a.kv_heads;
+  const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool failed = false;
   if (threadIdx.x == 0) {
@@ -801,11 +767,12 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     fence_mbar_init();
     for (int i = 0; i < 4; ++i) bad[i] = 0u;
     prefetch_tmap(&maps.q);
-    prefetch_tmap(&maps.k);
-    prefetch_tmap(&maps.v);
     prefetch_tmap(&maps.dout);
-    prefetch_tmap(&maps.dk);
-    prefetch_tmap(&maps.dv);
+    // K and V are on their way while the tensor memory is allocated and the boundaries are read
+    fence_proxy_async_smem();
+    grid_dep_wait();
+    load_tile(&maps.k, smem, &kv_full[0], panels, kvh, k0, rep, l2_policy(0));
+    load_tile(&maps.v, smem + L::kTile, &kv_full[1], panels, kvh, k0, rep, l2_policy(0));
   }
   __syncwarp();
   if (warp == 1) {
@@ -819,35 +786,24 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
   grid_dep_wait();
   grid_dep_launch();
 
-  // the keys with the most queries first
-  const int unit = blockIdx.x / split, rank = blockIdx.x % split;
-  const int kvh = unit % a.kv_heads, rest = unit / a.kv_heads, rep = rest % a.m;
-  const int kt = rest / a.m, k0 = kt * kB, group = a.heads / a.kv_heads;
   const Bounds bounds(a, rep);
   const int end = bounds.last_query((int)min((int64_t)k0 + kB, a.tokens) - 1);
   const int per = end > k0 ? (end - 1) / kB - kt + 1 : 0;            // tiles of queries of a head
   // this CTA's steps of all: tiles of queries, head by head
   const int64_t all = (int64_t)per * group;
   const int first = (int)(all * rank / split), n = (int)(all * (rank + 1) / split) - first;
-  const int panels = (a.head_dim + 63) / 64, ksteps = (a.head_dim + 15) / 16, cols = ksteps * 16;
 
   if (warp == 0) {
     const bool lead = elect_one();
     const uint64_t pol = l2_policy(0);
-    auto load = [&](const CUtensorMap* m, uint8_t* dst, uint64_t* bar, int h, int token) {
-      mbar_expect_tx(bar, panels * kB * 128);
-      for (int c = 0; c < panels; ++c) tma_load_4d_hint(dst + c * kB * 128, m, bar, c * 64, h, token, rep, pol);
-    };
     int head = kvh * group + (per > 0 ? first / per : 0), tile = kt + (per > 0 ? first % per : 0);
     for (int i = 0; i < n && !failed; ++i) {
       const int qs = i % L::kQ, gs = i % L::kG;
-      if (i == 0 && lead) load(&maps.k, smem, &kv_full[0], kvh, k0);
       if (i >= L::kQ && !__all_sync(0xffffffffu, mbar_wait(&q_empty[qs], (i / L::kQ - 1) & 1))) { failed = true; break; }
-      if (lead) load(&maps.q, sq + qs * L::kTile, &q_full[qs], head, tile * kB);
+      if (lead) load_tile(&maps.q, sq + qs * L::kTile, &q_full[qs], panels, head, tile * kB, rep, pol);
       __syncwarp();
-      if (i == 0 && lead) load(&maps.v, smem + L::kTile, &kv_full[1], kvh, k0);
       if (i >= L::kG && !__all_sync(0xffffffffu, mbar_wait(&g_empty[gs], (i / L::kG - 1) & 1))) { failed = true; break; }
-      if (lead) load(&maps.dout, sg + gs * L::kTile, &g_full[gs], head, tile * kB);
+      if (lead) load_tile(&maps.dout, sg + gs * L::kTile, &g_full[gs], panels, head, tile * kB, rep, pol);
       __syncwarp();
       // the rows' numbers, into the place of the step before the last, whose elements are done when its Q is let go of
       const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens;
@@ -871,7 +827,9 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
       __syncwarp();
       if (++tile == kt + per) { tile = kt; ++head; }
     }
-    // the releases of the last slots arrive here: wait for them before leaving
+    // tiles that no product needs, and the releases of the last slots, arrive here: wait for them before leaving
+    for (int i = 0; i < 2; ++i)
+      if (n <= 0 && !__all_sync(0xffffffffu, mbar_wait(&kv_full[i], 0))) failed = true;
     for (int i = 0; i < L::kQ && i < n && !failed; ++i)
       if (!__all_sync(0xffffffffu, mbar_wait(&q_empty[i], ((n - 1 - i) / L::kQ) & 1))) failed = true;
     for (int i = 0; i < L::kG && i < n && !failed; ++i)
@@ -956,6 +914,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
       const int at = tile * kB + half * 64;
       const int from = key - at, to = seq_end - 1 - at;    // visible columns [from, to]
       const bool cut = __any_sync(0xffffffffu, from > 0 || to < 63);
+      const uint32_t seen[2] = {visible(from, to), visible(from - 32, to - 32)};
       float p[64];
       wait(&st_full[i & 1], (i >> 1) & 1, ok);
       wait(s_full, i & 1, ok);
@@ -977,7 +936,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         if (__builtin_expect(cut, 0)) {
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (c * 32 + e < from || c * 32 + e > to) p[c * 32 + e] = 0.f;
+            if ((seen[c] >> e & 1) == 0) p[c * 32 + e] = 0.f;
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = pack2(p[c * 32 + 2 * e], p[c * 32 + 2 * e + 1]);
@@ -1008,7 +967,7 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         if (__builtin_expect(cut, 0)) {    // (0 times NaN)
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (c * 32 + e < from || c * 32 + e > to) g[e] = 0u;
+            if ((seen[c] >> e & 1) == 0) g[e] = 0u;
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = pack2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1]));
@@ -1027,26 +986,17 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
     tc_fence_after_sync();
     if (failed && lane == 0) atomicExch(a.err, 49);
     if (split == 1) {
-      if (!failed && k0 + q * 32 < a.tokens) {
-        const bool none = seq_end <= key;
-        uint8_t* box = smem + q * 32 * 128;
-        bool fine = result_rows<HD>(tmem + L::kDk + lanes, half, cols, n > 0, none, a.scale, box, lane);
-        fine = result_rows<HD>(tmem + L::kDv + lanes, half, cols, n > 0, none, 1.f, box + L::kTile, lane) && fine;
-        const uint32_t ill = __ballot_sync(0xffffffffu, !fine);
+      if (!failed) {
+        const bool none = seq_end <= key, in = key < a.tokens;
+        __nv_bfloat16* dk = in ? head_ptr<__nv_bfloat16>(a.dk, rep, kvh, a.head_dim) + key * a.dk.row : nullptr;
+        __nv_bfloat16* dv = in ? head_ptr<__nv_bfloat16>(a.dv, rep, kvh, a.head_dim) + key * a.dv.row : nullptr;
+        bool fine = result_row<HD / 2>(tmem + L::kDk + lanes, half * (HD / 2), cols, n > 0, none, a.scale, dk, a.head_dim);
+        fine = result_row<HD / 2>(tmem + L::kDv + lanes, half * (HD / 2), cols, n > 0, none, 1.f, dv, a.head_dim) && fine;
+        const uint32_t ill = __ballot_sync(0xffffffffu, !fine && in);
         if (ill != 0u && lane == 0) atomicOr(&bad[q], ill);
-        fence_proxy_async_smem();
       }
       elements_sync();
-      if (!failed && half == 0 && k0 + q * 32 < a.tokens) {
-        if (lane == 0) {
-          for (int c = 0; c < panels; ++c) {
-            store_heads(&maps.dk, smem + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
-            store_heads(&maps.dv, smem + L::kTile + q * 32 * 128 + c * kB * 128, c * 64, kvh, k0 + q * 32, rep);
-          }
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          stores_read(bad[q] != 0u);
-        }
-        __syncwarp();
+      if (!failed && half == 0) {
         uint32_t ill = bad[q];
         while (ill != 0u) {
           const int e = __ffs(ill) - 1;
@@ -1055,7 +1005,11 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         }
       }
     } else {
-      // [dk, dv][column][row], neighbouring lanes beside each other
+      // [dk, dv][column][row], neighbouring lanes beside each other (over K and V, which have to have landed)
+      if (n <= 0) {
+        wait(&kv_full[0], 0, ok);
+        wait(&kv_full[1], 0, ok);
+      }
       float* sums = reinterpret_cast<float*>(smem) + r;
 #pragma unroll
       for (int g = 0; g < 2 * HD / 32; ++g) {
@@ -1183,7 +1137,7 @@ bool tc_takes(const Args& a, int dtype) {
 cudaError_t tc_forward(const Args& a, cudaStream_t st) {
   FwdMaps maps;
   if (head_map(&maps.q, a, a.q, a.heads, kB) != cudaSuccess || head_map(&maps.k, a, a.k, a.kv_heads, kB) != cudaSuccess ||
-      head_map(&maps.v, a, a.v, a.kv_heads, kB) != cudaSuccess || head_map(&maps.out, a, a.out, a.heads, 32) != cudaSuccess)
+      head_map(&maps.v, a, a.v, a.kv_heads, kB) != cudaSuccess)
     return cudaErrorInvalidValue;
   return a.head_dim <= 64 ? launch_forward<64>(maps, a, st) : launch_forward<128>(maps, a, st);
 }
@@ -1192,9 +1146,7 @@ cudaError_t tc_backward(const Args& a, cudaStream_t st) {
   DqMaps dq;
   DkvMaps dkv;
   if (head_map(&dq.q, a, a.q, a.heads, kB) != cudaSuccess || head_map(&dq.dout, a, a.dout, a.heads, kB) != cudaSuccess ||
-      head_map(&dq.k, a, a.k, a.kv_heads, kB) != cudaSuccess || head_map(&dq.v, a, a.v, a.kv_heads, kB) != cudaSuccess ||
-      head_map(&dq.dq, a, a.dq, a.heads, 32) != cudaSuccess || head_map(&dkv.dk, a, a.dk, a.kv_heads, 32) != cudaSuccess ||
-      head_map(&dkv.dv, a, a.dv, a.kv_heads, 32) != cudaSuccess)
+      head_map(&dq.k, a, a.k, a.kv_heads, kB) != cudaSuccess || head_map(&dq.v, a, a.v, a.kv_heads, kB) != cudaSuccess)
     return cudaErrorInvalidValue;
   dkv.q = dq.q;
   dkv.dout = dq.dout;
