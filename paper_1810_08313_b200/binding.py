@@ -6,6 +6,7 @@ or loaded this module raises; there is no other implementation to fall back to.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 import math
@@ -408,9 +409,9 @@ class _Op:
             raise ValueError(f"{name} must be contiguous")
         return self.stack(t, name, shape[1:], shape[0], dtype)[0]
 
-    def heads(self, t, name: str, m: Optional[int], tokens: Optional[int], heads: Optional[int], hd: Optional[int], dtype):
-        """t as [m][tokens][heads][head_dim] with the heads of a token dense (None: from t); returns (pointer, distance between
-        tokens, distance between replicas)."""
+    def heads(self, t, name: str, m: int, tokens: int, heads: int, hd: int, dtype):
+        """t as [m][tokens][heads][head_dim] with the heads of a token dense; returns (pointer, distance between tokens, distance
+        between replicas)."""
         torch = self.torch
         if not isinstance(t, torch.Tensor) or t.device != self.device:
             raise ValueError(f"{name} must be a tensor on {self.device}")
@@ -419,10 +420,9 @@ class _Op:
         shape, step = t.shape, t.stride()
         if len(shape) == 3:
             shape, step = (1, *shape), (0, *step)
-        if len(shape) != 4 or (m is not None and shape[0] != m) or (tokens is not None and shape[1] != tokens) or \
-                (heads is not None and shape[2] != heads) or (hd is not None and shape[3] != hd):
+        if shape != (m, tokens, heads, hd):
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [m = {m}][tokens = {tokens}][heads = {heads}][head_dim = {hd}]")
-        if (step[3] != 1 and shape[3] > 1) or (step[2] != shape[3] and shape[2] > 1):
+        if (step[3] != 1 and hd > 1) or (step[2] != hd and heads > 1):
             raise ValueError(f"{name}: the heads of a token must be dense")
         if self.stream is not None:
             t.record_stream(self.stream)
@@ -431,7 +431,11 @@ class _Op:
     def heads_out(self, given, like, name: str, m, tokens, heads, hd, dtype):
         """An output [m][tokens][heads][head_dim]: the caller's tensor, or a new dense one.  (tensor, pointer, row, stride)"""
         if given is None:
-            t = self.new(like, (m, tokens, heads, hd), dtype)
+            shape = (m, tokens, heads, hd)
+            if self.stream is None and like.shape == shape and like.is_contiguous():
+                t = self.torch.empty_like(like)
+            else:
+                t = self.new(like, shape, dtype)
             return t, t.data_ptr(), heads * hd, tokens * heads * hd
         return (given, *self.heads(given, name, m, tokens, heads, hd, dtype))
 
@@ -691,11 +695,10 @@ def _head_shapes(q, k, what: str):
     """(m, tokens, heads, kv_heads, head_dim) of q [m][tokens][heads][head_dim] and k (either without m)."""
     if q.dim() not in (3, 4) or k.dim() != q.dim():
         raise ValueError(f"{what}: q and k must be [m][tokens][heads][head_dim] or [tokens][heads][head_dim]")
-    m = q.shape[0] if q.dim() == 4 else 1
-    tokens, heads, hd = q.shape[-3:]
+    m, tokens, heads, hd = q.shape if q.dim() == 4 else (1, *q.shape)
     kv = k.shape[-2]
-    for v in (m, tokens, heads, kv, hd):
-        _int32(v, LS_ERR_TOO_LARGE, what)
+    if max(m, tokens, heads, kv, hd) >= 2 ** 31:
+        raise LsError(LS_ERR_TOO_LARGE, what)
     return m, tokens, heads, kv, hd
 
 
@@ -857,38 +860,47 @@ def clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, stre
         raise ValueError("out must have as many tensors as grads")
 
     def table(tensors, name, like):
-        ptrs, sizes, steps, types = [], [], [], []
+        # (a pass for each property: a model has hundreds of tensors, and this is what a call on small ones costs)
         for i, t in enumerate(tensors):
-            if not isinstance(t, torch.Tensor) or t.device != op.device:
+            if not isinstance(t, torch.Tensor):
                 raise ValueError(f"{name}[{i}] must be a tensor on {op.device}")
-            dt = _OP_DTYPE.get(t.dtype)
-            if dt is None:
-                raise ValueError(f"{name}[{i}] must be float32 or bfloat16, not {t.dtype}")
-            shape = t.shape
-            if len(shape) < 1 or shape[0] != m or (like is not None and shape != like[i].shape):
-                raise ValueError(f"{name}[{i}] has shape {tuple(shape)}" + (f", expected [{m}][...]" if like is None else
-                                                                           f", expected {tuple(like[i].shape)}"))
-            n = t.numel() // m if m else 0
-            step = n
-            if not t.is_contiguous():
-                _, _, step = op.stack(t, f"{name}[{i}]", tuple(shape[1:]), m)
-            elif op.stream is not None:
-                t.record_stream(op.stream)
-            ptrs.append(t.data_ptr())
-            sizes.append(n)
-            steps.append(step)
-            types.append(dt)
-        return (C.c_void_p * count)(*ptrs), (C.c_int64 * count)(*sizes), (C.c_int64 * count)(*steps), (C.c_int32 * count)(*types)
+        if {t.device for t in tensors} != {op.device}:
+            raise ValueError(f"{name}: every tensor must be on {op.device}")
+        types = [_OP_DTYPE.get(t.dtype) for t in tensors]
+        if None in types:
+            i = types.index(None)
+            raise ValueError(f"{name}[{i}] must be float32 or bfloat16, not {tensors[i].dtype}")
+        if like is None and min(t.dim() for t in tensors) < 1:
+            raise ValueError(f"{name} must be [m][...]")
+        if like is None and {t.size(0) for t in tensors} != {m}:
+            raise ValueError(f"{name}: every tensor must be [{m}][...]")
+        if like is not None:
+            for i, (t, g) in enumerate(zip(tensors, like)):
+                if t.shape != g.shape:
+                    raise ValueError(f"{name}[{i}] has shape {tuple(t.shape)}, expected {tuple(g.shape)}")
+        sizes = [t.numel() // m if m else 0 for t in tensors]
+        steps = list(sizes)
+        if op.stream is not None or not all([t.is_contiguous() for t in tensors]):
+            for i, t in enumerate(tensors):
+                steps[i] = op.stack(t, f"{name}[{i}]", tuple(t.shape[1:]), m)[2]
+        return (array.array("Q", [t.data_ptr() for t in tensors]), array.array("q", sizes), array.array("q", steps),
+                array.array("i", types))
 
-    gp, sizes, gs, gt = table(grads, "grads", None)
-    op_, os_, ot = None, None, None
+    gp, sizes, gs, gt = lists = table(grads, "grads", None)
     if outs is not None:
-        op_, _, os_, ot = table(outs, "out", grads)
+        op_, _, os_, ot = more = table(outs, "out", grads)
+        more = [a.buffer_info()[0] for a in (op_, os_, ot)]
+    else:
+        more = [None, None, None]
+    live = [p for p, n in zip(gp if outs is None else op_, sizes) if n]
+    if len(set(live)) != len(live):
+        raise ValueError("a tensor is there twice")            # (it would be scaled twice, at the same time)
+    gp, sizes, gs, gt = (a.buffer_info()[0] for a in lists)
     norm_t, np_ = op.out_dense(norm, first, "norm", (m,), torch.float32)
     need = C.c_size_t()
     _check(_lib().ls_clip_grads_ws_bytes(sizes, count, m, C.byref(need)), what)
     base, nbytes, keep = op.workspace(first, workspace, need.value)
-    op.call(what, gp, sizes, gs, gt, count, m, float(max_norm), op_, os_, ot, np_, base, nbytes)
+    op.call(what, gp, sizes, gs, gt, count, m, float(max_norm), *more, np_, base, nbytes)
     return norm_t
 
 

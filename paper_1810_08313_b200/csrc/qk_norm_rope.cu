@@ -457,7 +457,7 @@ extern "C" int ls_qk_norm_rope(const void* q_dev, const void* k_dev, const float
   a.w[0] = q_weight_dev; a.w[1] = k_weight_dev; a.w_stride = m > 1 ? weight_stride : 0;
   a.positions = positions_dev; a.inv_freq = inv_freq_dev;
   if (!(eps >= 0.f) || !isfinite(eps) || interleaved < 0 || interleaved > 1 || q_weight_dev == nullptr || k_weight_dev == nullptr ||
-      (m > 1 && weight_stride < head_dim) || (rot_dim > 0 && (positions_dev == nullptr || inv_freq_dev == nullptr)))
+      (m > 1 && weight_stride < head_dim) || (rot_dim > 0 && tokens > 0 && (positions_dev == nullptr || inv_freq_dev == nullptr)))
     return LS_ERR_INVALID_ARG;
   for (int t = 0; t < 2; ++t)
     if (nr_bad(a, a.x[t], a.heads[t], dtype) || nr_bad(a, a.out[t], a.heads[t], dtype)) return LS_ERR_INVALID_ARG;
@@ -503,7 +503,7 @@ extern "C" int ls_qk_norm_rope_grad(const void* dq_out_dev, const void* dk_out_d
   if (!(eps >= 0.f) || !isfinite(eps) || interleaved < 0 || interleaved > 1 || q_weight_dev == nullptr || k_weight_dev == nullptr ||
       dq_weight_dev == nullptr || dk_weight_dev == nullptr || ws_dev == nullptr ||
       (m > 1 && (weight_stride < head_dim || dweight_stride < head_dim)) ||
-      (rot_dim > 0 && (positions_dev == nullptr || inv_freq_dev == nullptr)))
+      (rot_dim > 0 && tokens > 0 && (positions_dev == nullptr || inv_freq_dev == nullptr)))
     return LS_ERR_INVALID_ARG;
   for (int t = 0; t < 2; ++t)
     if (nr_bad(a, a.x[t], a.heads[t], dtype) || nr_bad(a, a.dy[t], a.heads[t], dtype) || nr_bad(a, a.out[t], a.heads[t], dtype))

@@ -358,6 +358,42 @@ def test_attention_sequences_heads_of_128(tokens, starts):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_attention_of_nothing(dtype):
+    """No sequences, and no tokens."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    q, k, v = _attn_case(2, 200, 2, 1, 64, dtype)
+    seq = torch.full((2, 1), 50, dtype=torch.int32, device="cuda")
+    out, lse = b.attention(q, k, v, seq)
+    assert not bool(out.any()) and not bool(lse.any())
+    assert not any(bool(t.any()) for t in b.attention_grad(torch.ones_like(q), q, k, v, out, lse, seq))
+    out, lse = b.attention(q[:, :0], k[:, :0], v[:, :0])
+    assert out.shape == (2, 0, 2, 64) and lse.shape == (2, 2, 0)
+    assert [t.numel() for t in b.attention_grad(out, q[:, :0], k[:, :0], v[:, :0], out, lse)] == [0, 0, 0]
+    pos = torch.zeros(2, 0, dtype=torch.int32, device="cuda")
+    w = torch.ones(2, 64, device="cuda")
+    got = b.qk_norm_rope_grad(q[:, :0], k[:, :0], q[:, :0], k[:, :0], w, w, pos, b.rope_frequencies(64))
+    assert not bool(got[2].any()) and not bool(got[3].any())
+
+
+def test_attention_refusals():
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    q, k, v = _attn_case(2, 20, 4, 2, 16, "bf16")
+    seq = torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+    for call in (lambda: b.attention(q, k.float(), v), lambda: b.attention(q, k, v[:, :19]), lambda: b.attention(q, k[..., :8], v),
+                 lambda: b.attention(q[0], k, v), lambda: b.attention(q, k, v, seq[:1]), lambda: b.attention(q, k, v, seq.long()),
+                 lambda: b.attention(q, k, v.transpose(2, 3).contiguous().transpose(2, 3)), lambda: b.attention(q, k, v, out=q[:, :, :2]),
+                 lambda: b.attention(q.half(), k.half(), v.half()), lambda: b.attention(q, k, v, lse=torch.zeros(2, 4, 19, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: b.attention(q[:, :, :3], k, v), lambda: b.attention(q, k, v, scale=math.inf),
+                 lambda: b.attention(q, k[:, :1].expand(-1, 20, -1, -1), v)):
+        with pytest.raises(b.LsError):
+            call()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("hd", [1, 7, 8, 16, 24, 32, 33, 40, 48, 72, 80, 96, 104, 112, 120, 128, 130, 136, 200, 256])
 def test_attention_head_sizes(hd, dtype):
     _attn_run(1, 275, [0, 100, 275], 4, 2, hd, dtype)
@@ -686,6 +722,20 @@ def test_clip_grads_of_views(dtype):
     used = torch.zeros(60001, dtype=torch.bool, device="cuda")
     used[1:20001] = used[20008:20008 + 96 * 200] = used[50000:50003] = True
     assert torch.equal(base[:, ~used], keep[:, ~used])
+
+
+def test_clip_grads_refusals():
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    x, y = torch.ones(2, 5, device="cuda"), torch.ones(2, 5, device="cuda")
+    for call in (lambda: b.clip_grads([x, x], 1.0), lambda: b.clip_grads([x, y], 1.0, out=[y, y]), lambda: b.clip_grads([x], 1.0, out=[]),
+                 lambda: b.clip_grads([x, x.double()], 1.0), lambda: b.clip_grads([x, y[:1]], 1.0), lambda: b.clip_grads([x, y.cpu()], 1.0),
+                 lambda: b.clip_grads([x.t()], 1.0), lambda: b.clip_grads([x], 1.0, out=[y[:, :3]]), lambda: b.clip_grads([x[0, 0]], 1.0)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(b.LsError):
+        b.clip_grads([x], 0.0)
+    assert bool((x == 1).all()) and bool((y == 1).all())
 
 
 def test_clip_grads_is_repeatable_and_captured():
