@@ -1,17 +1,19 @@
 // Attention over packed sequences on the tensor cores: bf16 heads of up to 128 elements (see attention.cuh for the formulas).
 //
-// Forward.  A CTA takes 256 consecutive rows of one head as two tiles of 128 (rows of S are TMEM lanes) and passes over the keys in
-// blocks of 128, once:
-//   warp 0     TMA producer: both tiles of Q, then K and V blocks through a ring
-//   warps 1, 2 issue the MMAs of a tile: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory)
-//   warps 3-6, 7-10   the softmax of a tile, a thread a row: 128 scores in registers, maximum, exponentials, sum, P in bf16 back
-//              to tensor memory in two halves, on the first of which PV starts
-// The tensor core works for one tile while the other's softmax runs.  For that the two have to stay half a block apart: S of a tile
-// waits until the other one is past its maxima.  (Without, both end in step: 994 us instead of 945 for 16384 rows of 16
-// heads of 128.  With two threads a row, and twice the warps: 1013 us.)
-// Heads of 128 fill the tensor memory with S and O, and P takes the place of S: S of a block is issued when the PV before it is
-// done.  Smaller ones have a place for P, and S of the next block is issued as soon as this one's is in registers (8192 rows of
-// 16 heads of 64: 240 us with P in the place of S).
+// Forward.  An SM has two tiles of 128 rows of a head each (rows of S are TMEM lanes), and each passes over the keys in blocks of 128,
+// once.  The tensor core works for one tile while the other's softmax runs.  A CTA has
+//   a TMA producer: Q, then K and V blocks through a ring
+//   a warp for each tile that issues its MMAs: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory)
+//   four warps for each tile's softmax, a thread a row: 128 scores in registers, maximum, exponentials, sum, P in bf16 back to
+//              tensor memory in two halves, on the first of which PV starts
+// Heads of up to 64: a CTA has one tile, and the SM two CTAs, of which one starts and ends while the other works (16 heads of 64,
+// two tiles a CTA: 251 us for 8192 rows instead of 231, 53.1 us for 23 packed sequences instead of 48.6).  P has a place of its own,
+// and S of the next block is issued as soon as this one's is in registers.
+// Larger heads: a CTA has both tiles, 256 consecutive rows, and they share every K and V block, which one CTA a tile would draw from
+// the L2 faster than it gives them (64 KB a block, twice in the 1700 cycles that two softmaxes take).  S and O fill the tensor memory,
+// P takes the place of S, and S of a block is issued when the PV before it is done.  So the two tiles have to stay half a block
+// apart: S of a tile waits until the other one is past its maxima.  (Without, both end in step: 994 us instead of 945 for 16384
+// rows of 16 heads of 128.  With two threads a row, and twice the warps: 1013 us.)
 // O stays in tensor memory over all blocks and is rescaled only where a row's maximum has grown by more than 2^8 since its
 // reference was taken: P then lies below 2^8 instead of 1, which costs bf16 and fp32 no precision, and most blocks need no
 // pass over O.  P is rounded to bf16 (2^-8 of each term, signs at random), its sum is taken before the rounding.
@@ -24,18 +26,19 @@ namespace {
 using namespace ptx;
 
 constexpr int kB = 128;                  // rows of a tile, keys of a block
-constexpr int kFwdThreads = 352;
 
 template <int HD>
 struct Fwd {
+  static constexpr bool kShared = HD == 128;                // P in the place of S
+  static constexpr int kTiles = HD == 128 ? 2 : 1;          // of 128 rows
   static constexpr int kTile = kB * HD * 2;                 // bytes: HD / 64 panels of 128 rows x 128 bytes
-  static constexpr int kSlots = HD == 128 ? 2 : 3;          // of a K and a V block
-  static constexpr int kRing = 2 * kTile;                   // offset of the ring, behind Q
+  static constexpr int kSlots = 2;                          // of a K and a V block
+  static constexpr int kRing = kTiles * kTile;              // offset of the ring, behind Q
   static constexpr int kBars = kRing + kSlots * 2 * kTile;
   static constexpr int kTotal = 1024 + kBars + (2 * kSlots + 14) * 8 + 16;
-  // TMEM columns: S at 0 and 128, O from 256 on (tile x: + x HD); P, 64 columns, in the place of S, or behind O where that ends early
-  static constexpr bool kShared = HD == 128;
-  static constexpr uint32_t kO = 256, kP = kShared ? 0 : 384, kPStep = kShared ? kB : 64;
+  // TMEM columns: S, 128 a tile, then O (tile x: + x HD); P, 64 columns, in the place of S, or behind O where that ends early
+  static constexpr uint32_t kColumns = kTiles * 256, kO = kTiles * kB, kP = kShared ? 0 : kO + kTiles * HD, kPStep = kShared ? kB : 64;
+  static constexpr int kThreads = 32 * (1 + 5 * kTiles), kPerSm = HD == 128 ? 1 : 2;
 };
 
 struct FwdMaps { CUtensorMap q, k, v; };
@@ -152,10 +155,10 @@ __device__ __forceinline__ bool result_row(uint32_t ta, int c0, int cols, bool a
 }
 
 template <int HD>
-__global__ void __launch_bounds__(kFwdThreads, 1)
+__global__ void __launch_bounds__(Fwd<HD>::kThreads, Fwd<HD>::kPerSm)
 attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant__ Args a) {
   using L = Fwd<HD>;
-  constexpr int SLOTS = L::kSlots;
+  constexpr int SLOTS = L::kSlots, TILES = L::kTiles;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
@@ -169,15 +172,15 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_done + 2);
 
   // the rows with the most keys first; heads of a group beside each other
-  const int tiles = (int)((a.tokens + 2 * kB - 1) / (2 * kB));
+  const int tiles = (int)((a.tokens + TILES * kB - 1) / (TILES * kB));
   const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
-  const int r0 = (tiles - 1 - rest / a.m) * 2 * kB;
+  const int r0 = (tiles - 1 - rest / a.m) * TILES * kB;
   const int kvh = head / (a.heads / a.kv_heads);
   const int panels = (a.head_dim + 63) / 64;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool failed = false;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < SLOTS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 2); }
+    for (int s = 0; s < SLOTS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], TILES); }
     for (int x = 0; x < 2; ++x) { mbar_init(&q_full[x], 1); mbar_init(&s_full[x], 1); mbar_init(&p_half[x], 4); mbar_init(&p_half[2 + x], 4); mbar_init(&past_max[x], 4); mbar_init(&s_free[x], 4); mbar_init(&o_done[x], 1); }
     fence_mbar_init();
     prefetch_tmap(&maps.k);
@@ -185,12 +188,12 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     // Q is on its way while the tensor memory is allocated and the boundaries are read
     fence_proxy_async_smem();
     grid_dep_wait();
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < TILES; ++x)
       if (r0 + x * kB < a.tokens) load_tile(&maps.q, smem + x * L::kTile, &q_full[x], panels, head, r0 + x * kB, rep, l2_policy(0));
   }
   __syncwarp();
   if (warp == 1) {
-    tmem_alloc(tmem_slot, 512);
+    tmem_alloc(tmem_slot, L::kColumns);
     tmem_relinquish();
   }
   tc_fence_before_sync();
@@ -201,9 +204,9 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   grid_dep_launch();
 
   const Bounds bounds(a, rep);
-  const Span sa = key_blocks(bounds, r0), sb = key_blocks(bounds, r0 + kB);
+  const Span sa = key_blocks(bounds, r0), sb = TILES == 2 ? key_blocks(bounds, r0 + kB) : Span{1, 0};
   const bool has_a = sa.lo <= sa.hi, has_b = sb.lo <= sb.hi;
-  const int lo = has_a ? sa.lo : sb.lo, hi = has_b ? sb.hi : sa.hi;        // (lo > hi if neither has any)
+  const int lo = has_a ? sa.lo : sb.lo, hi = has_b ? sb.hi : has_a ? sa.hi : lo - 1;
 
   if (warp == 0) {
     const bool lead = elect_one();
@@ -224,14 +227,14 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       if (++s == SLOTS) { s = 0; ++round; }
     }
     // Q that no product needs, and the releases of the last slots, arrive here: wait for them before leaving
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < TILES; ++x)
       if (r0 + x * kB < a.tokens && !(x == 0 ? has_a : has_b) && !__all_sync(0xffffffffu, mbar_wait(&q_full[x], 0))) failed = true;
     for (int i = 0; i < SLOTS && !failed; ++i) {
       const int uses = round + (i < s ? 1 : 0);
       if (uses > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty[i], (uses - 1) & 1))) failed = true;
     }
     if (failed && lane == 0) atomicExch(a.err, 41);
-  } else if (warp <= 2) {
+  } else if (warp <= TILES) {
     const int x = warp - 1;
     const bool lead = elect_one();
     const int ksteps = (a.head_dim + 15) / 16;
@@ -282,7 +285,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     }
     if (failed && lane == 0) atomicExch(a.err, 42);
   } else {
-    const int x = (warp - 3) >> 2, q = warp & 3;
+    const int x = (warp - 1 - TILES) >> 2, q = warp & 3;
     const Span sp = x == 0 ? sa : sb;
     const int row = r0 + x * kB + q * 32 + lane;
     int start, end;
@@ -421,7 +424,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   __syncthreads();
   if (warp == 1) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, L::kColumns);
   }
 }
 
@@ -1091,30 +1094,34 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
 
 template <int HD>
 cudaError_t launch_forward(const FwdMaps& maps, const Args& a, cudaStream_t st) {
+  using L = Fwd<HD>;
   static uint64_t done = 0;              // one bit per device
-  static_assert(Fwd<HD>::kTotal <= 227 * 1024, "shared memory budget");
-  const cudaError_t e = allow_dynamic_smem(attention_tc_kernel<HD>, Fwd<HD>::kTotal, &done);
+  static_assert(L::kTotal <= 227 * 1024, "shared memory budget");
+  const cudaError_t e = allow_dynamic_smem(attention_tc_kernel<HD>, L::kTotal, &done);
   if (e != cudaSuccess) return e;
-  const int64_t tiles = (a.tokens + 2 * kB - 1) / (2 * kB);
-  return launch_dep(attention_tc_kernel<HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kFwdThreads), Fwd<HD>::kTotal, st, 1, maps, a);
+  const int64_t tiles = (a.tokens + L::kTiles * kB - 1) / (L::kTiles * kB);
+  return launch_dep(attention_tc_kernel<HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(L::kThreads), L::kTotal, st, 1, maps, a);
 }
+
+constexpr int kAlone = 227 * 1024;       // shared memory beside which no other kernel with tensor memory fits
 
 template <int HD>
 cudaError_t launch_backward(const DqMaps& dq, const DkvMaps& dkv, const Args& a, cudaStream_t st) {
   static uint64_t done[2] = {0, 0};      // one bit per device
   static_assert(Dq<HD>::kTotal <= 227 * 1024 && Dkv<HD>::kTotal <= 227 * 1024, "shared memory budget");
   cudaError_t e = allow_dynamic_smem(attention_dq_tc_kernel<HD>, Dq<HD>::kTotal, &done[0]);
-  if (e == cudaSuccess) e = allow_dynamic_smem(attention_dkv_tc_kernel<HD>, Dkv<HD>::kTotal, &done[1]);
+  if (e == cudaSuccess) e = allow_dynamic_smem(attention_dkv_tc_kernel<HD>, kAlone, &done[1]);
   const int64_t tiles = (a.tokens + kB - 1) / kB;
   if (e == cudaSuccess)
     e = launch_dep(attention_dq_tc_kernel<HD>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kBwdThreads), Dq<HD>::kTotal, st, 1, dq, a);
-  // as many CTAs to a tile of keys, up to eight, as still find an SM
+  // As many CTAs to a tile of keys, up to eight, as still find an SM.  Those of a cluster have an SM for themselves: a CTA that waited
+  // there for another kernel's tensor memory, while that one's cluster waited for a CTA that waits for this one's, would wait for good.
   const int64_t units = tiles * a.kv_heads * a.m;
   int split = 1;
   while (split < 8 && units * split * 2 <= 148) split *= 2;
   if (e == cudaSuccess)
-    e = launch_dep(attention_dkv_tc_kernel<HD>, dim3((unsigned)(units * split)), dim3(kBwdThreads), Dkv<HD>::kTotal, st, (unsigned)split, dkv, a,
-                   split);
+    e = launch_dep(attention_dkv_tc_kernel<HD>, dim3((unsigned)(units * split)), dim3(kBwdThreads), split > 1 ? kAlone : Dkv<HD>::kTotal, st,
+                   (unsigned)split, dkv, a, split);
   return e;
 }
 
