@@ -740,7 +740,7 @@ def qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, eps: float = 1e-
     qp, qr, qs = op.heads(q, "q", m, tokens, heads, hd, q.dtype)
     kp, kr, ks = op.heads(k, "k", m, tokens, kv, hd, q.dtype)
     qo, qop, qor, qos = op.heads_out(q_out, q, "q_out", m, tokens, heads, hd, q.dtype)
-    ko, kop, kor, kos = op.heads_out(k_out, q, "k_out", m, tokens, kv, hd, q.dtype)
+    ko, kop, kor, kos = op.heads_out(k_out, k, "k_out", m, tokens, kv, hd, q.dtype)
     op.call("ls_qk_norm_rope", qp, kp, qw, kw, pp, fp, m, tokens, heads, kv, hd, rot, int(bool(interleaved)), qr, kr, qs, ks, ws, dt, eps,
             qop, kop, qor, kor, qos, kos)
     return qo if q_out is not None else _like(q, 4, qo), ko if k_out is not None else _like(q, 4, ko)
@@ -762,10 +762,10 @@ def qk_norm_rope_grad(dq_out, dk_out, q, k, q_weight, k_weight, positions, inv_f
     qp, qr, qs = op.heads(q, "q", m, tokens, heads, hd, q.dtype)
     kp, kr, ks = op.heads(k, "k", m, tokens, kv, hd, q.dtype)
     dq_t, dqp, dqr, dqs = op.heads_out(dq, q, "dq", m, tokens, heads, hd, q.dtype)
-    dk_t, dkp, dkr, dks = op.heads_out(dk, q, "dk", m, tokens, kv, hd, q.dtype)
+    dk_t, dkp, dkr, dks = op.heads_out(dk, k, "dk", m, tokens, kv, hd, q.dtype)
     f32 = op.torch.float32
-    dqw_t, dqw, dws = op.out(dq_weight, q, "dq_weight", (m, hd), f32)
-    dkw_t, dkw, dkws = op.out(dk_weight, q, "dk_weight", (m, hd), f32)
+    dqw_t, dqw, dws = op.out(dq_weight, q_weight, "dq_weight", (m, hd), f32)
+    dkw_t, dkw, dkws = op.out(dk_weight, k_weight, "dk_weight", (m, hd), f32)
     if m > 1 and dws != dkws:
         raise ValueError("dq_weight and dk_weight must have the same distance between replicas")
     base, nbytes, keep = op.workspace(q, workspace, _ws_bytes("ls_qk_norm_rope_grad_ws_bytes", m, tokens, hd))
@@ -822,8 +822,8 @@ def attention_grad(dout, q, k, v, out, lse, seq_start=None, scale: Optional[floa
     lp = op.dense(lse, "lse", (m, heads, tokens), op.torch.float32)
     sp, n = _sequences(op, seq_start, m)
     dq_t, dqp, dqr, dqs = op.heads_out(dq, q, "dq", m, tokens, heads, hd, q.dtype)
-    dk_t, dkp, dkr, dks = op.heads_out(dk, q, "dk", m, tokens, kv, hd, q.dtype)
-    dv_t, dvp, dvr, dvs = op.heads_out(dv, q, "dv", m, tokens, kv, hd, q.dtype)
+    dk_t, dkp, dkr, dks = op.heads_out(dk, k, "dk", m, tokens, kv, hd, q.dtype)
+    dv_t, dvp, dvr, dvs = op.heads_out(dv, v, "dv", m, tokens, kv, hd, q.dtype)
     base, nbytes, keep = op.workspace(q, workspace, _ws_bytes("ls_attention_grad_ws_bytes", m, tokens, heads, kv, hd))
     op.call("ls_attention_grad", gp, qp, kp, vp, outp, lp, sp, m, tokens, n, heads, kv, hd, gr, qr, kr, vr, outr, gs, qs, ks, vs, outs,
             dt, 1.0 / math.sqrt(hd) if scale is None else scale, dqp, dkp, dvp, dqr, dkr, dvr, dqs, dks, dvs, base, nbytes)
@@ -859,22 +859,27 @@ def clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, stre
     if outs is not None and len(outs) != count:
         raise ValueError("out must have as many tensors as grads")
 
+    here = {op.device.index}
+
     def table(tensors, name, like):
         # (a pass for each property: a model has hundreds of tensors, and this is what a call on small ones costs)
         for i, t in enumerate(tensors):
             if not isinstance(t, torch.Tensor):
                 raise ValueError(f"{name}[{i}] must be a tensor on {op.device}")
-        if {t.device for t in tensors} != {op.device}:
+        if {t.get_device() for t in tensors} != here:
             raise ValueError(f"{name}: every tensor must be on {op.device}")
         types = [_OP_DTYPE.get(t.dtype) for t in tensors]
         if None in types:
             i = types.index(None)
             raise ValueError(f"{name}[{i}] must be float32 or bfloat16, not {tensors[i].dtype}")
-        if like is None and min(t.dim() for t in tensors) < 1:
-            raise ValueError(f"{name} must be [m][...]")
-        if like is None and {t.size(0) for t in tensors} != {m}:
-            raise ValueError(f"{name}: every tensor must be [{m}][...]")
-        if like is not None:
+        if like is None:
+            try:
+                lead = {t.size(0) for t in tensors}
+            except IndexError:
+                lead = None
+            if lead != {m}:
+                raise ValueError(f"{name}: every tensor must be [{m}][...]")
+        else:
             for i, (t, g) in enumerate(zip(tensors, like)):
                 if t.shape != g.shape:
                     raise ValueError(f"{name}[{i}] has shape {tuple(t.shape)}, expected {tuple(g.shape)}")

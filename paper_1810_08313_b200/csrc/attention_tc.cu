@@ -305,6 +305,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
       const bool cut = __any_sync(0xffffffffu, from > 0 || to_col < kB - 1);
       auto hide = [&](int c, uint32_t (&v)[32]) {
         const uint32_t seen = visible(from - c * 32, to_col - c * 32);
+        if (__all_sync(0xffffffffu, seen == 0xffffffffu)) return;
 #pragma unroll
         for (int i = 0; i < 32; ++i)
           if ((seen >> i & 1) == 0) v[i] = 0xff800000u;
@@ -377,12 +378,18 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
           part[i & 1] = add2(part[i & 1], two(e.x, e.y));
           p[i] = pack2(e.x, e.y);
         }
-        tmem_st_32x16(tp + c * 16, p);
-        if (c & 1) {                       // PV may start with the first half of the keys
+        if (c == 2) {                      // PV may start with the first half of the keys, whose stores are done by now
           tmem_st_wait();
           tc_fence_before_sync();
           __syncwarp();
-          mbar_arrive_if(lane == 0, &p_half[(c & 2) + x]);
+          mbar_arrive_if(lane == 0, &p_half[x]);
+        }
+        tmem_st_32x16(tp + c * 16, p);
+        if (c == 3) {
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          mbar_arrive_if(lane == 0, &p_half[2 + x]);
         }
       }
       const float2 total = parts(add2(part[0], part[1]));
