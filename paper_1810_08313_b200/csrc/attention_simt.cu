@@ -16,12 +16,11 @@ namespace ls {
 namespace attn {
 namespace {
 
-constexpr int kNT = 256;
-
 // HD: head_dim at most; RB: rows of a tile
 template <int HD, int RB>
 struct Way {
-  static constexpr int B = RB, R = RB / 16;       // rows of a tile, of a thread
+  static constexpr int NT = RB == 32 && HD <= 128 ? 128 : 256;       // threads
+  static constexpr int B = RB, R = RB * 16 / NT;  // rows of a tile, of a thread
   static constexpr int K = HD > 128 ? 2 : 4;      // keys of a thread
   static constexpr int N = 16 * K;                // of a block
   static constexpr int P = HD + 4;                // floats between rows of an operand
@@ -38,28 +37,54 @@ __device__ __forceinline__ float4 four(const __nv_bfloat16* p) {
 }
 // rows [r0, r0 + ROWS) of a head into shared memory as floats; zeros outside the tensor and the head.  quads: rows are whole fours of
 // elements that start on their boundary
-template <typename T, int HD, int ROWS>
+template <typename T, typename W, int HD, int ROWS>
 __device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t row, int64_t r0, int64_t rows, int hd, bool quads) {
   constexpr int P = HD + 4;
   if (quads) {
-    constexpr int Q = HD / 4, N = ROWS * Q / kNT;
-    static_assert(ROWS * Q % kNT == 0, "whole rounds");
+    constexpr int Q = HD / 4, N = ROWS * Q / W::NT;
+    static_assert(ROWS * Q % W::NT == 0, "whole rounds");
     float4 v[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int i = n * kNT + threadIdx.x, r = i / Q, c = (i - r * Q) * 4;
+      const int i = n * W::NT + threadIdx.x, r = i / Q, c = (i - r * Q) * 4;
       v[n] = r0 + r < rows && c < hd ? four(src + (r0 + r) * row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int i = n * kNT + threadIdx.x, r = i / Q, c = (i - r * Q) * 4;
+      const int i = n * W::NT + threadIdx.x, r = i / Q, c = (i - r * Q) * 4;
       *reinterpret_cast<float4*>(dst + r * P + c) = v[n];
     }
     return;
   }
-  for (int i = threadIdx.x; i < ROWS * HD; i += kNT) {
+  for (int i = threadIdx.x; i < ROWS * HD; i += W::NT) {
     const int r = i / HD, c = i - r * HD;
     dst[r * P + c] = r0 + r < rows && c < hd ? to_f32(src[(r0 + r) * row + c]) : 0.f;
+  }
+}
+
+// two tiles at once, so that all their loads are on their way together
+template <typename T, typename W, int HD, int ROWS>
+__device__ __forceinline__ void load_two(float* d1, const T* s1, int64_t row1, float* d2, const T* s2, int64_t row2, int64_t r0, int64_t rows,
+                                         int hd, bool quads) {
+  if (!quads) {
+    load_tile<T, W, HD, ROWS>(d1, s1, row1, r0, rows, hd, false);
+    load_tile<T, W, HD, ROWS>(d2, s2, row2, r0, rows, hd, false);
+    return;
+  }
+  constexpr int P = HD + 4, Q = HD / 4, N = ROWS * Q / W::NT;
+  float4 v[N], w[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = n * W::NT + threadIdx.x, r = i / Q, c = (i - r * Q) * 4;
+    const bool in = r0 + r < rows && c < hd;
+    v[n] = in ? four(s1 + (r0 + r) * row1 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    w[n] = in ? four(s2 + (r0 + r) * row2 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = n * W::NT + threadIdx.x, r = i / Q, c = (i - r * Q) * 4;
+    *reinterpret_cast<float4*>(d1 + r * P + c) = v[n];
+    *reinterpret_cast<float4*>(d2 + r * P + c) = w[n];
   }
 }
 
@@ -158,7 +183,7 @@ __device__ __forceinline__ float row_max(float x) {
 }
 
 template <typename T, int HD, int RB>
-__global__ void __launch_bounds__(kNT)
+__global__ void __launch_bounds__(Way<HD, RB>::NT)
 attention_kernel(const __grid_constant__ Args a, const bool quads) {
   using W = Way<HD, RB>;
   extern __shared__ __align__(16) float sm[];
@@ -176,7 +201,7 @@ attention_kernel(const __grid_constant__ Args a, const bool quads) {
   const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, rep = rest % a.m;
   const int64_t r0 = (int64_t)(tiles - 1 - rest / a.m) * W::B;
   const int kvh = head / (a.heads / a.kv_heads);
-  load_tile<T, HD, W::B>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd, quads);
+  load_tile<T, W, HD, W::B>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd, quads);
   const Bounds bounds(a, rep);
   if (tid < W::B) {                        // (whole warps)
     int end;
@@ -190,8 +215,8 @@ attention_kernel(const __grid_constant__ Args a, const bool quads) {
   for (int r = 0; r < W::R; ++r) { top[r] = -INFINITY; sum[r] = 0.f; }
   const int64_t end = min(r0 + W::B, a.tokens);
   for (int64_t j0 = bounds.first_key((int)r0); j0 < end; j0 += W::N) {
-    load_tile<T, HD, W::N>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd, quads);
-    load_tile<T, HD, W::N>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd, quads);
+    load_two<T, W, HD, W::N>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens,
+                             hd, quads);
     __syncthreads();
     float s[W::R][W::K];
     dots<W, HD>(sq, sk, ty, tx, s);
@@ -240,32 +265,43 @@ attention_kernel(const __grid_constant__ Args a, const bool quads) {
   }
   const bool good = write_rows<T, W, HD>(head_ptr<T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
   if (__syncthreads_and(good)) return;
-  for (int r = tid >> 5; r < W::B; r += kNT / 32)
+  for (int r = tid >> 5; r < W::B; r += W::NT / 32)
     if (bad[r] != 0u) forward_row<T>(a, rep, head, (int)r0 + r);
 }
 
-// dot[r] = dout . out of the tile's rows, dout from shared memory
-template <typename T, int HD, int ROWS>
-__device__ __forceinline__ void row_dots(float* dot, const float* sg, const T* out, int64_t row, int64_t r0, int64_t rows, int hd, bool quads) {
-  constexpr int N = kNT / ROWS, P = HD + 4;          // neighbouring threads of a row
-  const int r = threadIdx.x / N, part = threadIdx.x % N;
-  float d = 0.f;
-  if (r0 + r < rows) {
-    const T* o = out + (r0 + r) * row;
-    if (quads) {
-#pragma unroll 4
-      for (int e = part * 4; e < hd; e += N * 4) {
-        const float4 x = four(o + e), g = *reinterpret_cast<const float4*>(sg + r * P + e);
-        d = fmaf(x.x, g.x, fmaf(x.y, g.y, fmaf(x.z, g.z, fmaf(x.w, g.w, d))));
-      }
-    } else {
-      for (int e = part; e < hd; e += N) d = fmaf(to_f32(o[e]), sg[r * P + e], d);
+// dot[r] = dout . out of the tile's rows: neighbouring threads share a row; out is loaded before, dout taken from shared memory
+template <typename T, typename W, int HD, int ROWS>
+struct RowDots {
+  static constexpr int N = W::NT / ROWS, M = HD / 4 / N, P = HD + 4;
+  float4 o[M];
+  const T* row;
+  __device__ __forceinline__ void fetch(const T* out, int64_t step, int64_t r0, int64_t rows, int hd, bool quads) {
+    const int64_t i = r0 + threadIdx.x / N;
+    row = i < rows ? out + i * step : nullptr;
+    if (!quads) return;
+#pragma unroll
+    for (int n = 0; n < M; ++n) {
+      const int e = (n * N + threadIdx.x % N) * 4;
+      o[n] = row != nullptr && e < hd ? four(row + e) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
   }
+  __device__ __forceinline__ void finish(float* dot, const float* sg, int hd, bool quads) const {
+    const int r = threadIdx.x / N, part = threadIdx.x % N;
+    float d = 0.f;
+    if (quads) {
 #pragma unroll
-  for (int o = N / 2; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-  if (part == 0) dot[r] = d;
-}
+      for (int n = 0; n < M; ++n) {        // (dout is zeros behind the tensor and the head)
+        const float4 g = *reinterpret_cast<const float4*>(sg + r * P + (n * N + part) * 4);
+        d = fmaf(o[n].x, g.x, fmaf(o[n].y, g.y, fmaf(o[n].z, g.z, fmaf(o[n].w, g.w, d))));
+      }
+    } else if (row != nullptr) {
+      for (int e = part; e < hd; e += N) d = fmaf(to_f32(row[e]), sg[r * P + e], d);
+    }
+#pragma unroll
+    for (int m = N / 2; m > 0; m >>= 1) d += __shfl_xor_sync(0xffffffffu, d, m);
+    if (part == 0) dot[r] = d;
+  }
+};
 
 template <typename T, int HD, int RB>
 __device__ __forceinline__ void grad_queries(const Args& a, bool quads, float* sm, uint32_t* bad, int* start, float* lse2, float* dot, int unit) {
@@ -281,8 +317,10 @@ __device__ __forceinline__ void grad_queries(const Args& a, bool quads, float* s
   const int64_t r0 = (int64_t)(tiles - 1 - rest / a.m) * W::B;
   const int kvh = head / (a.heads / a.kv_heads);
   const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens;
-  load_tile<T, HD, W::B>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, r0, a.tokens, hd, quads);
-  load_tile<T, HD, W::B>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, r0, a.tokens, hd, quads);
+  RowDots<T, W, HD, W::B> dots_of_rows;
+  dots_of_rows.fetch(head_ptr<const T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd, quads);
+  load_two<T, W, HD, W::B>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, r0,
+                           a.tokens, hd, quads);
   const Bounds bounds(a, rep);
   if (tid < W::B) {                        // (whole warps)
     int end;
@@ -291,13 +329,13 @@ __device__ __forceinline__ void grad_queries(const Args& a, bool quads, float* s
     lse2[tid] = r0 + tid < a.tokens ? a.lse[stat + r0 + tid] * kLog2e : 0.f;
   }
   __syncthreads();
-  row_dots<T, HD, W::B>(dot, sg, head_ptr<const T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd, quads);
+  dots_of_rows.finish(dot, sg, hd, quads);
   const float scale2 = a.scale * kLog2e;
   float acc[W::R][W::C] = {};
   const int64_t end = min(r0 + W::B, a.tokens);
   for (int64_t j0 = bounds.first_key((int)r0); j0 < end; j0 += W::N) {
-    load_tile<T, HD, W::N>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, j0, a.tokens, hd, quads);
-    load_tile<T, HD, W::N>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens, hd, quads);
+    load_two<T, W, HD, W::N>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, j0, a.tokens,
+                             hd, quads);
     __syncthreads();
     float s[W::R][W::K], g[W::R][W::K];
     dots<W, HD>(sq, sk, ty, tx, s);
@@ -327,7 +365,7 @@ __device__ __forceinline__ void grad_queries(const Args& a, bool quads, float* s
   }
   const bool good = write_rows<T, W, HD>(head_ptr<T>(a.dq, rep, head, hd), a.dq.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
   if (__syncthreads_and(good)) return;
-  for (int r = tid >> 5; r < W::B; r += kNT / 32)
+  for (int r = tid >> 5; r < W::B; r += W::NT / 32)
     if (bad[r] != 0u) dq_row<T>(a, rep, head, (int)r0 + r);
 }
 
@@ -345,8 +383,8 @@ __device__ __forceinline__ void grad_keys(const Args& a, bool quads, float* sm, 
   const int kvh = unit % a.kv_heads, rest = unit / a.kv_heads, rep = rest % a.m;
   const int64_t k0 = (int64_t)(rest / a.m) * W::B;
   const int group = a.heads / a.kv_heads;
-  load_tile<T, HD, W::B>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, k0, a.tokens, hd, quads);
-  load_tile<T, HD, W::B>(sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, k0, a.tokens, hd, quads);
+  load_two<T, W, HD, W::B>(sk, head_ptr<const T>(a.k, rep, kvh, hd), a.k.row, sv, head_ptr<const T>(a.v, rep, kvh, hd), a.v.row, k0, a.tokens,
+                           hd, quads);
   if (tid < W::B) bad[tid] = 0u;
   const float scale2 = a.scale * kLog2e;
   float dk[W::R][W::C] = {}, dv[W::R][W::C] = {};
@@ -359,15 +397,18 @@ __device__ __forceinline__ void grad_keys(const Args& a, bool quads, float* sm, 
     const int head = kvh * group + (int)(step / per);
     const int64_t i0 = k0 + step % per * W::N, stat = ((int64_t)rep * a.heads + head) * a.tokens;
     __syncthreads();
-    load_tile<T, HD, W::N>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, i0, a.tokens, hd, quads);
-    load_tile<T, HD, W::N>(sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, i0, a.tokens, hd, quads);
+    const float of_row = tid < W::N && i0 + tid < a.tokens ? a.lse[stat + i0 + tid] : 0.f;
+    RowDots<T, W, HD, W::N> dots_of_rows;
+    dots_of_rows.fetch(head_ptr<const T>(a.out, rep, head, hd), a.out.row, i0, a.tokens, hd, quads);
+    load_two<T, W, HD, W::N>(sq, head_ptr<const T>(a.q, rep, head, hd), a.q.row, sg, head_ptr<const T>(a.dout, rep, head, hd), a.dout.row, i0,
+                             a.tokens, hd, quads);
     if (tid < W::N) {
       int stop;
-      lse2[tid] = i0 + tid < a.tokens ? a.lse[stat + i0 + tid] * kLog2e : 0.f;
+      lse2[tid] = of_row * kLog2e;
       bounds.rows((int)i0 + (tid & ~31), &start[tid], &stop);
     }
     __syncthreads();
-    row_dots<T, HD, W::N>(dot, sg, head_ptr<const T>(a.out, rep, head, hd), a.out.row, i0, a.tokens, hd, quads);
+    dots_of_rows.finish(dot, sg, hd, quads);
     float s[W::R][W::K], g[W::R][W::K];
     dots<W, HD>(sk, sq, ty, tx, s);
     dots<W, HD>(sv, sg, ty, tx, g);
@@ -402,8 +443,8 @@ __device__ __forceinline__ void grad_keys(const Args& a, bool quads, float* sm, 
       for (int r = 0; r < W::R; ++r)
 #pragma unroll
         for (int c = 0; c < W::C; ++c) {
-          sm[(r * W::C + c) * kNT + tid] = dk[r][c];
-          sm[((W::R + r) * W::C + c) * kNT + tid] = dv[r][c];
+          sm[(r * W::C + c) * W::NT + tid] = dk[r][c];
+          sm[((W::R + r) * W::C + c) * W::NT + tid] = dv[r][c];
         }
     }
     ptx::cluster_sync_all();
@@ -414,8 +455,8 @@ __device__ __forceinline__ void grad_keys(const Args& a, bool quads, float* sm, 
         for (int r = 0; r < W::R; ++r)
 #pragma unroll
           for (int c = 0; c < W::C; ++c) {
-            dk[r][c] += ptx::ld_cluster_f32(at + (r * W::C + c) * kNT * 4);
-            dv[r][c] += ptx::ld_cluster_f32(at + ((W::R + r) * W::C + c) * kNT * 4);
+            dk[r][c] += ptx::ld_cluster_f32(at + (r * W::C + c) * W::NT * 4);
+            dv[r][c] += ptx::ld_cluster_f32(at + ((W::R + r) * W::C + c) * W::NT * 4);
           }
       }
     }
@@ -428,14 +469,14 @@ __device__ __forceinline__ void grad_keys(const Args& a, bool quads, float* sm, 
   bool good = write_rows<T, W, HD>(head_ptr<T>(a.dk, rep, kvh, hd), a.dk.row, k0, a.tokens, hd, ty, tx, dk, scale, bad);
   good = write_rows<T, W, HD>(head_ptr<T>(a.dv, rep, kvh, hd), a.dv.row, k0, a.tokens, hd, ty, tx, dv, one, bad) && good;
   if (__syncthreads_and(good)) return;
-  for (int r = tid >> 5; r < W::B; r += kNT / 32)
+  for (int r = tid >> 5; r < W::B; r += W::NT / 32)
     if (bad[r] != 0u) dkv_row<T>(a, rep, kvh, (int)k0 + r);
 }
 
 // The first `key_units` times `split` CTAs have tiles of keys (those with the most queries first), the others tiles of queries (those
 // with the most keys first).
 template <typename T, int HD, int RB>
-__global__ void __launch_bounds__(kNT)
+__global__ void __launch_bounds__(Way<HD, RB>::NT)
 attention_grad_kernel(const __grid_constant__ Args a, const bool quads, const int key_units, const int query_units, const int split) {
   using W = Way<HD, RB>;
   extern __shared__ __align__(16) float sm[];
@@ -462,10 +503,11 @@ bool whole_quads(const Args& a) {
     if (t->p != nullptr && (reinterpret_cast<uintptr_t>(t->p) % (4 * sizeof(T)) != 0 || t->row % 4 != 0 || t->replica % 4 != 0)) return false;
   return true;
 }
-// How many CTAs share the queries of a tile of keys: as many, up to eight, as still find an SM, two to each.
-int query_split(int64_t key_units) {
+// How many CTAs share the queries of a tile of keys: as many, up to eight, as still find an SM, two to each, or one where the shared
+// memory leaves room for one (1000 rows of 4 heads of 200 on 1: 604 us with 256 such CTAs, 468 with 128).
+int query_split(int64_t key_units, int per_sm) {
   int split = 1;
-  while (split < 8 && key_units * split * 2 <= 2 * 148) split *= 2;
+  while (split < 8 && key_units * split * 2 <= per_sm * 148) split *= 2;
   return split;
 }
 
@@ -474,21 +516,21 @@ cudaError_t launch(const Args& a, bool grad, cudaStream_t st) {
   using W = Way<HD, RB>;
   constexpr int fwd = (W::rows + 2 * W::block + W::scores) * 4, bwd = (2 * W::rows + 2 * W::block + W::scores) * 4;
   static_assert(bwd <= 220 * 1024, "shared memory budget");
-  static_assert(2 * W::R * W::C * kNT <= 2 * W::rows + 2 * W::block, "the parts of a cluster");
+  static_assert(2 * W::R * W::C * W::NT <= 2 * W::rows + 2 * W::block, "the parts of a cluster");
   static uint64_t done[2] = {0, 0};      // one bit per device
   const int64_t tiles = (a.tokens + W::B - 1) / W::B;
   const bool quads = whole_quads<T>(a);
   if (!grad) {
     const cudaError_t e = allow_dynamic_smem(attention_kernel<T, HD, RB>, fwd, &done[0]);
     if (e != cudaSuccess) return e;
-    return launch_dep(attention_kernel<T, HD, RB>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(kNT), fwd, st, 1, a, quads);
+    return launch_dep(attention_kernel<T, HD, RB>, dim3((unsigned)(tiles * a.heads * a.m)), dim3(W::NT), fwd, st, 1, a, quads);
   }
   const cudaError_t e = allow_dynamic_smem(attention_grad_kernel<T, HD, RB>, bwd, &done[1]);
   if (e != cudaSuccess) return e;
   const int64_t key_units = tiles * a.kv_heads * a.m, query_units = tiles * a.heads * a.m;
-  const int split = query_split(key_units);
+  const int split = query_split(key_units, HD > 128 ? 1 : 2);
   const int64_t ctas = key_units * split + (query_units + split - 1) / split * split;
-  return launch_dep(attention_grad_kernel<T, HD, RB>, dim3((unsigned)ctas), dim3(kNT), bwd, st, (unsigned)split, a, quads,
+  return launch_dep(attention_grad_kernel<T, HD, RB>, dim3((unsigned)ctas), dim3(W::NT), bwd, st, (unsigned)split, a, quads,
                     (int)key_units, (int)query_units, split);
 }
 // Tiles of 64 rows, or of 32 where those would leave SMs without one: a tile's blocks of keys follow one another, and half the rows
