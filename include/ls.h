@@ -505,7 +505,8 @@ int ls_muon_step_layer(ls_handle* h, int layer, const void* g_dev, int64_t g_str
  * elements between tokens of a tensor, *_stride that between replicas (ignored for one token, one replica), the heads of a
  * token are dense, so that q and k may be parts of one projection.  weights: float [m][head_dim], weight_stride apart.
  * inv_freq: double [rot_dim / 2], positions: int32 [m][tokens], dense (either may be NULL if rot_dim == 0).  Angles
- * are formed in double.  rot_dim is even.  head_dim <= 256, tokens <= 2^30, heads <= 65536. */
+ * are formed in double, squares and their mean in fp32 (elements of up to 10^18).  rot_dim is even.  head_dim <= 256, tokens <=
+ * 2^30, heads <= 65536. */
 int ls_qk_norm_rope(const void* q_dev, const void* k_dev, const float* q_weight_dev, const float* k_weight_dev,
                     const int32_t* positions_dev, const double* inv_freq_dev, int m, int64_t tokens, int heads, int kv_heads,
                     int head_dim, int rot_dim, int interleaved, int64_t q_row, int64_t k_row, int64_t q_stride, int64_t k_stride,
@@ -544,7 +545,8 @@ int ls_attention(const void* q_dev, const void* k_dev, const void* v_dev, const 
 /* Its gradient, from dout, the inputs, and the out and lse that the forward call wrote:
  *   P_ij = exp(s_ij - lse_i),  dS_ij = P_ij (dout_i . v_j - dout_i . out_i),
  *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
- * dk and dv sum over the query heads of their group.  Zero for rows in no sequence, whose dout may hold anything. */
+ * dk and dv sum over the query heads of their group.  Zero for rows in no sequence, whose dout may hold anything.  Where the
+ * tensor cores take the call (see above), P and dS are rounded to bf16 as operands of dv and dk; of dq, dS is two bf16 pieces. */
 int ls_attention_grad_ws_bytes(int m, int64_t tokens, int heads, int kv_heads, int head_dim, size_t* bytes);
 int ls_attention_grad(const void* dout_dev, const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
                       const float* lse_dev, const int32_t* seq_start_dev, int m, int64_t tokens, int n_seqs, int heads, int kv_heads,

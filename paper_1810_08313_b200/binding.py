@@ -324,7 +324,7 @@ def linear_loss_static(W, bias, x, y, chunk_rows: int, chunk_loss, loss: str = "
            "ls_linear_loss_static")
 
 
-# ---- operators of a language model's last layers and its weight update ---------------------------------------
+# ---- operators of a language model's blocks, last layers and weight update ------------------------------------
 # Every tensor takes the replicas first ([m][rows][d], ...); one replica may leave that axis out.  A replica is dense,
 # the distance between replicas is free (views into packed replica vectors are fine).  Outputs that are not given are
 # allocated.  `workspace`: a uint8 tensor of the size the matching *_workspace function names, for callers that keep
