@@ -637,6 +637,57 @@ def test_attention_is_repeatable_and_captured(dtype, hd):
     b.device_status()
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_replayed_with_other_boundaries(hd):
+    """A captured pair of calls reads its boundaries when it runs."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    m, tokens = 2, 900
+    q, k, v = _attn_case(m, tokens, 4, 2, hd, "bf16")
+    dout = _randn(_gen(5), m, tokens, 4, hd).bfloat16()
+    tables = [_starts(s, m)[1] for s in ([0, 900, 900, 900], [0, 1, 450, 880], [100, 100, 100, 101], [7, 300, 301, 900])]
+
+    def both(seq):
+        out, lse = b.attention(q, k, v, seq)
+        return (out, lse, *b.attention_grad(dout, q, k, v, out, lse, seq))
+
+    want = [both(s) for s in tables]
+    seq = tables[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both(seq)
+    for i in (1, 2, 0, 3):
+        seq.copy_(tables[i])
+        graph.replay()
+        assert all(torch.equal(p, w) for p, w in zip(got, want[i]))
+    b.device_status()
+
+
+def test_attention_on_several_streams_at_once():
+    """Calls of different shapes and types that share the SMs give what they give alone."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    cases = [(1, 1000, 4, 1, 64, "bf16"), (1, 2048, 8, 1, 128, "bf16"), (2, 513, 6, 2, 64, "fp32"), (1, 1000, 4, 1, 64, "bf16")]
+    data = []
+    for i, (m, tokens, heads, kv, hd, dtype) in enumerate(cases):
+        x = _attn_case(m, tokens, heads, kv, hd, dtype, seed=i)
+        data.append((*x, _randn(_gen(10 + i), m, tokens, heads, hd).to(_t(dtype)), _starts([3, tokens // 2, tokens], m)[1]))
+
+    def both(q, k, v, dout, seq, **kw):
+        out, lse = b.attention(q, k, v, seq, **kw)
+        return (out, lse, *b.attention_grad(dout, q, k, v, out, lse, seq, **kw))
+
+    want = [both(*d) for d in data]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = [both(*d, stream=s) for d, s in zip(data, streams)]
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(p, r) for p, r in zip(g, w))
+    b.device_status()
+
+
 # ---- gradient clipping ----------------------------------------------------------------------------------------------
 
 def _clip_check(grads, max_norm, norm, got, before):
