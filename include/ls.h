@@ -532,7 +532,7 @@ int ls_qk_norm_rope_grad(const void* dq_out_dev, const void* dk_out_dev, const v
  * seq_start: int32 [m][n_seqs + 1], dense, ascending: sequence s of a replica is the rows [seq_start[s], seq_start[s + 1]), of any
  * length, none included.  NULL with n_seqs == 1: one sequence of all rows.  Rows in no sequence (before the first, behind the
  * last) get out = 0 and lse = 0, and whatever they hold reaches no other row; nor does a NaN reach another sequence or an
- * earlier row of its own.  (Boundaries that do not ascend or leave [0, tokens] give wrong results, but no access outside.)
+ * earlier row of its own.  (Boundaries that do not ascend or leave [0, tokens] give wrong results, but no access outside, and no wait runs out.)
  * lse: float [m][heads][tokens], dense.  A row whose scores are all -inf, or one +inf, has no softmax: its out is NaN.
  * bf16 on the tensor cores (head_dim a multiple of 8 up to 128, every row of every tensor on a 16-byte boundary, scale > 0):
  * probabilities are rounded to bf16 as the operand of the second product, their sum is not.  Other calls run on the CUDA cores.

@@ -208,7 +208,11 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
   grid_dep_launch();
 
   const Bounds bounds(a, rep);
-  const Span sa = key_blocks(bounds, r0), sb = TILES == 2 ? key_blocks(bounds, r0 + kB) : Span{1, 0};
+  const Span sa = key_blocks(bounds, r0);
+  Span sb = TILES == 2 ? key_blocks(bounds, r0 + kB) : Span{1, 0};
+  // The second tile never starts before the first one, as its rows lie behind.  Boundaries that do not ascend may say otherwise; the
+  // hand-over below counts on it: the pair passes over the blocks from the first tile's on, and each tile waits for the other's maxima.
+  if (sa.lo <= sa.hi) sb.lo = max(sb.lo, sa.lo);
   const bool has_a = sa.lo <= sa.hi, has_b = sb.lo <= sb.hi;
   const int lo = has_a ? sa.lo : sb.lo, hi = has_b ? sb.hi : has_a ? sa.hi : lo - 1;
 
