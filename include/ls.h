@@ -560,6 +560,7 @@ int ls_attention_grad(const void* dout_dev, const void* q_dev, const void* k_dev
  * Host arrays of n_tensors entries: tensor i has sizes[i] elements a replica, of dtypes[i], strides[i] apart (dense within a
  * replica; strides may be NULL for m == 1).  outs NULL: in place; else the results go to outs[i] (of out_dtypes[i], rounded once,
  * out_strides[i] apart; grads[i] itself, with its type and stride, is allowed) and gradients that are not their own outputs stay.
+ * An output that shares memory with another output, or with a gradient that is not its own, is refused (LS_ERR_INVALID_ARG).
  * norm: float [m].  max_norm > 0; INFINITY: the norm, and nothing is scaled.  A norm of NaN makes the replica's results NaN;
  * an infinite one makes them 0, and NaN where a gradient is infinite.  Sums are formed in double over fp32 sums of 32 squares; no square
  * overflows or underflows.  The arrays are read before the call returns.  n_tensors <= 65536. */

@@ -844,7 +844,8 @@ def clip_grads_workspace(sizes: Sequence[int], m: int) -> int:
 def clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, stream=None):
     """The global norm [m] (float32) of every replica's gradients, a sequence of tensors [m][...] (float32 or bfloat16, a replica
     dense), which are scaled in place so that no replica's norm exceeds max_norm (ls_clip_grads).  out: a sequence of tensors of
-    the same shapes (of either type) that take the results instead.  max_norm = inf: the norm only."""
+    the same shapes (of either type) that take the results instead; one that shares memory with another, or with a gradient that
+    is not its own, is refused.  max_norm = inf: the norm only."""
     grads = list(grads)
     if not grads:
         raise ValueError("no gradients")

@@ -16,6 +16,10 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+#include <new>
+#include <vector>
+
 namespace ls {
 namespace {
 
@@ -275,6 +279,80 @@ int clip_run(const ClipList& l, float max_norm, float* norm, double* part, int p
   return LS_OK;
 }
 
+// Where a tensor's replicas lie: m pieces of `bytes`, `step` apart, from `at` on.  `out`: it is written.
+struct ClipSpan {
+  uint64_t at, step, bytes;
+  bool out;
+};
+// Pieces in the order of their addresses, one after another: whether one that is written shares memory with another one.
+struct ClipSweep {
+  uint64_t read_end = 0, written_end = 0;
+  bool meets(uint64_t at, const ClipSpan& s) {
+    const bool hit = at < written_end || (s.out && at < read_end);
+    uint64_t& end = s.out ? written_end : read_end;
+    end = std::max(end, at + s.bytes);
+    return hit;
+  }
+};
+// Whether spans [from, to), in the order of their first pieces and within `extent` bytes, have a piece that is written and meets another.
+bool clip_meet(const ClipSpan* from, const ClipSpan* to, uint64_t extent, int m) {
+  const uint64_t step = from->step;
+  bool same = true;
+  for (const ClipSpan* s = from; s < to; ++s) same = same && s->step == step && s->at - from->at + s->bytes <= step;
+  if (m == 1 || (same && extent <= step * (uint64_t)m)) {                    // views of replica vectors: replicas lie alike
+    ClipSweep sweep;
+    for (const ClipSpan* s = from; s < to; ++s)
+      if (sweep.meets(s->at, *s)) return true;
+    return false;
+  }
+  // others: all pieces, by a heap of every span's next one
+  struct Next { uint64_t at; const ClipSpan* s; int rep; };
+  std::vector<Next> heap;
+  const auto later = [](const Next& a, const Next& b) { return a.at > b.at; };
+  for (const ClipSpan* s = from; s < to; ++s) heap.push_back(Next{s->at, s, 0});
+  std::make_heap(heap.begin(), heap.end(), later);
+  ClipSweep sweep;
+  while (!heap.empty()) {
+    std::pop_heap(heap.begin(), heap.end(), later);
+    Next& n = heap.back();
+    if (sweep.meets(n.at, *n.s)) return true;
+    if (++n.rep == m) {
+      heap.pop_back();
+    } else {
+      n.at += n.s->step;
+      std::push_heap(heap.begin(), heap.end(), later);
+    }
+  }
+  return false;
+}
+// Whether an output shares memory with another output, or with a gradient that is not its own: CTAs would write what others still read.
+// A gradient that is its own output, as it lies, is one span.  Spans whose extents do not overlap (tensors of their own) are
+// told apart by one sort: 1 us for 38 tensors.  May throw std::bad_alloc.
+bool clip_overlap(const ClipList& l) {
+  std::vector<ClipSpan> spans;
+  spans.reserve(2 * (size_t)l.count);
+  const auto add = [&](const void* p, int64_t n, int64_t stride, int32_t dtype, bool out) {
+    const uint64_t e = dtype == LS_DTYPE_BF16 ? 2 : 4;
+    spans.push_back(ClipSpan{reinterpret_cast<uintptr_t>(p), l.m > 1 ? (uint64_t)std::min<int64_t>(stride, 1ll << 44) * e : 0, (uint64_t)n * e, out});
+  };
+  for (int i = 0; i < l.count; ++i) {
+    if (l.n[i] == 0) continue;
+    const bool own = l.out == nullptr || l.out[i] == l.in[i];
+    add(l.in[i], l.n[i], l.m > 1 ? l.in_stride[i] : 0, l.in_dtype[i], own);
+    if (!own) add(l.out[i], l.n[i], l.m > 1 ? l.out_stride[i] : 0, l.out_dtype[i], true);
+  }
+  std::sort(spans.begin(), spans.end(), [](const ClipSpan& a, const ClipSpan& b) { return a.at < b.at; });
+  const auto end_of = [&](const ClipSpan& s) { return s.at + (uint64_t)(l.m - 1) * s.step + s.bytes; };
+  for (size_t i = 0; i < spans.size();) {
+    uint64_t end = end_of(spans[i]);
+    size_t j = i + 1;
+    for (; j < spans.size() && spans[j].at < end; ++j) end = std::max(end, end_of(spans[j]));
+    if (j > i + 1 && clip_meet(&spans[i], &spans[i] + (j - i), end - spans[i].at, l.m)) return true;
+    i = j;
+  }
+  return false;
+}
+
 // CTAs' sums of a replica over all launches, or a refusal
 int clip_parts(const int64_t* n, int count, int m, int* parts) {
   if (m < 1 || count < 0 || (count > 0 && n == nullptr)) return LS_ERR_INVALID_ARG;
@@ -334,6 +412,12 @@ extern "C" int ls_clip_grads(const void* const* grads_dev, const int64_t* sizes,
   if (ws_bytes < (size_t)m * (size_t)parts * sizeof(double) || reinterpret_cast<uintptr_t>(ws_dev) % 256 != 0) return LS_ERR_STATE_SIZE;
   while (n_tensors > 0 && sizes[n_tensors - 1] == 0) --n_tensors;          // (so that every launch has a tensor to read)
   const ClipList l{grads_dev, outs_dev, sizes, strides, out_strides, dtypes, out_dtypes, n_tensors, m};
+  const bool only_norm = isinf(max_norm) && outs_dev == nullptr;             // (nothing is written, and tensors may share memory)
+  try {
+    if (!only_norm && clip_overlap(l)) return LS_ERR_INVALID_ARG;
+  } catch (const std::bad_alloc&) {
+    return LS_ERR_TOO_LARGE;
+  }
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   double* part = static_cast<double*>(ws_dev);
   // the sums of all launches, whose CTAs may be fewer than there is room for
