@@ -9,9 +9,9 @@
 // its own sequence to itself, so a tile of rows needs the keys from its first row's start on.  Short sequences share tiles, and
 // the host needs to know no lengths.
 //
-// A product of a whole tile multiplies what the mask leaves out by zero, and zero times an infinity or NaN is NaN.  So a row
-// of the result that is not finite is computed once more, alone, over the rows that it depends on: a NaN in one sequence, or in
-// the rows behind the last one, reaches no other.
+// A product of a whole tile multiplies what the mask leaves out by zero, and zero times an infinity or NaN is NaN.  So what is
+// not finite in a row of the result, and not so because of a row that it depends on, is computed once more from those rows alone: a
+// NaN in one sequence, or in the rows behind the last one, reaches no other.
 #pragma once
 
 #include "gemm_op.cuh"
@@ -134,116 +134,368 @@ __device__ __forceinline__ T* head_ptr(const Tensor& t, int rep, int head, int h
   return static_cast<T*>(t.p) + rep * t.replica + (int64_t)head * head_dim;
 }
 
-// ---- rows by themselves, one warp each: lane l has the elements l, l + 32, ... of a head (256 at most) --------------------
-constexpr int kLaneMost = 8;
+// ---- rows by themselves, a few to a warp: lane l has the elements l, l + 32, ... of a head, L of them ------------------------
+// Results that a warp forms together, which share the rows they depend on, and how many of those it reads together: the loads and
+// the sums over lanes of one hide those of the others.
+template <int L> constexpr int kRows = L > 4 ? 2 : 4;
+constexpr int kStep = 2;
 
-template <typename T>
-__device__ __forceinline__ void lane_load(const T* p, int hd, int lane, float (&x)[kLaneMost]) {
+template <int L, typename T>
+__device__ __forceinline__ void lane_load(const T* p, int hd, int lane, float (&x)[L]) {
 #pragma unroll
-  for (int e = 0; e < kLaneMost; ++e) x[e] = lane + 32 * e < hd ? to_f32(p[lane + 32 * e]) : 0.f;
+  for (int e = 0; e < L; ++e) x[e] = lane + 32 * e < hd ? to_f32(p[lane + 32 * e]) : 0.f;
 }
-template <typename T>
-__device__ __forceinline__ void lane_store(T* p, int hd, int lane, const float (&x)[kLaneMost], float by) {
-#pragma unroll
-  for (int e = 0; e < kLaneMost; ++e)
-    if (lane + 32 * e < hd) p[lane + 32 * e] = from_f32<T>(x[e] * by);
-}
-__device__ __forceinline__ float lane_dot(const float (&x)[kLaneMost], const float (&y)[kLaneMost], int hd, int lane) {
+// (elements behind the head are zeros)
+template <int L>
+__device__ __forceinline__ float lane_dot(const float (&x)[L], const float (&y)[L]) {
   float s = 0.f;
 #pragma unroll
-  for (int e = 0; e < kLaneMost; ++e)
-    if (lane + 32 * e < hd) s = fmaf(x[e], y[e], s);
+  for (int e = 0; e < L; ++e) s = fmaf(x[e], y[e], s);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return s;
 }
-
-template <typename T>
-__device__ __noinline__ void forward_row(const Args& a, int rep, int head, int i) {
-  const int lane = threadIdx.x & 31, hd = a.head_dim, kvh = head / (a.heads / a.kv_heads);
-  int from, end;
-  row_bounds(a, rep, i, &from, &end);
-  float q[kLaneMost], x[kLaneMost], acc[kLaneMost] = {};
-  lane_load(head_ptr<const T>(a.q, rep, head, hd) + i * a.q.row, hd, lane, q);
-  const T* k = head_ptr<const T>(a.k, rep, kvh, hd);
-  const T* v = head_ptr<const T>(a.v, rep, kvh, hd);
-  float top = -INFINITY, sum = 0.f;
-  for (int64_t j = from; j <= i; ++j) {
-    lane_load(k + j * a.k.row, hd, lane, x);
-    const float s = lane_dot(q, x, hd, lane) * a.scale;
-    top = s > top || s != s ? s : top;
-    if (top != top) break;
-  }
-  if (fabsf(top) < INFINITY) {
-    for (int64_t j = from; j <= i; ++j) {
-      lane_load(k + j * a.k.row, hd, lane, x);
-      const float p = expf(lane_dot(q, x, hd, lane) * a.scale - top);
-      sum += p;
-      lane_load(v + j * a.v.row, hd, lane, x);
+// rows i, i + 1, ... of a tensor, none from `to` on: the last one again
+template <int L, typename T>
+__device__ __forceinline__ void lane_rows(const T* p, int64_t row, int i, int to, int hd, int lane, float (&x)[kStep][L]) {
 #pragma unroll
-      for (int e = 0; e < kLaneMost; ++e) acc[e] = fmaf(p, x[e], acc[e]);
+  for (int u = 0; u < kStep; ++u) lane_load(p + min(i + u, to - 1) * row, hd, lane, x[u]);
+}
+// A bit for each element of a stored row that is not finite.
+template <int L, typename T>
+__device__ __forceinline__ uint32_t lane_ill(const T* p, int hd, int lane) {
+  float x[L];
+  lane_load(p, hd, lane, x);
+  uint32_t ill = 0;
+#pragma unroll
+  for (int e = 0; e < L; ++e)
+    if (!(fabsf(x[e]) < INFINITY)) ill |= 1u << e;
+  return ill;
+}
+template <int L, typename T>
+__device__ __forceinline__ void lane_store(T* p, int lane, const float (&x)[L], float by, uint32_t ill) {
+#pragma unroll
+  for (int e = 0; e < L; ++e)
+    if ((ill >> e & 1) != 0) p[lane + 32 * e] = from_f32<T>(x[e] * by);
+}
+// Whether an element in `ill` is not NaN yet, so that further terms may change it.
+template <int L>
+__device__ __forceinline__ bool lane_open(const float (&x)[L], uint32_t ill) {
+  bool open = false;
+#pragma unroll
+  for (int e = 0; e < L; ++e) open = open || ((ill >> e & 1) != 0 && x[e] == x[e]);
+  return open;
+}
+// What the rows that a result depends on hold of NaN, +inf and -inf: a bit for each of the lane's columns.  The results of a warp are taken
+// in an order in which those of a sequence depend on more and more rows, so that each row is looked at once for all.  (When every
+// result was formed again from all of its rows, one NaN in v, in the middle of 16384 rows of 16 heads of 128, took 714 ms, now 14.)
+struct Held {
+  uint32_t nan = 0, up = 0, down = 0;
+  // rows [i, to)
+  template <int L, typename T>
+  __device__ __forceinline__ void add_rows(const T* p, int64_t row, int i, int to, int hd, int lane) {
+    constexpr int N = 4;
+    for (; i < to; i += N) {
+      float x[N][L];
+#pragma unroll
+      for (int u = 0; u < N; ++u) lane_load(p + min(i + u, to - 1) * row, hd, lane, x[u]);
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int e = 0; e < L; ++e) {
+          if (x[u][e] != x[u][e]) nan |= 1u << e;
+          if (x[u][e] == INFINITY) up |= 1u << e;
+          if (x[u][e] == -INFINITY) down |= 1u << e;
+        }
     }
-  } else {                               // NaN, or infinite scores only: the softmax has no value
-#pragma unroll
-    for (int e = 0; e < kLaneMost; ++e) acc[e] = NAN;
-    sum = NAN;
   }
-  lane_store(head_ptr<T>(a.out, rep, head, hd) + i * a.out.row, hd, lane, acc, 1.f / sum);
-  if (lane == 0) a.lse[((int64_t)rep * a.heads + head) * a.tokens + i] = fabsf(top) == INFINITY ? top : logf(sum) + top;
-}
+  // Sums of those rows with positive factors: sets the elements that are not finite for that reason, and returns the others of `ill`.
+  template <int L, typename T>
+  __device__ __forceinline__ uint32_t mark(T* p, int lane, uint32_t ill) const {
+    const uint32_t none = nan | (up & down), all = none | up | down;
+#pragma unroll
+    for (int e = 0; e < L; ++e)
+      if ((ill & all) >> e & 1) p[lane + 32 * e] = from_f32<T>(none >> e & 1 ? NAN : up >> e & 1 ? INFINITY : -INFINITY);
+    return ill & ~all;
+  }
+};
 
-template <typename T>
-__device__ __noinline__ void dq_row(const Args& a, int rep, int head, int i) {
+// Rows r0 + the bits of `rows`.  A row whose lse is not finite has no softmax: all of its elements are NaN, and stay so.  Those of the
+// others have it as the reference of their exponentials.
+template <typename T, int L>
+__device__ __noinline__ void forward_rows(const Args& a, int rep, int head, int r0, uint32_t rows) {
+  constexpr int R = kRows<L>;
   const int lane = threadIdx.x & 31, hd = a.head_dim, kvh = head / (a.heads / a.kv_heads);
-  int from, end;
-  row_bounds(a, rep, i, &from, &end);
-  const int64_t stat = ((int64_t)rep * a.heads + head) * a.tokens + i;
-  float q[kLaneMost], g[kLaneMost], x[kLaneMost], y[kLaneMost], acc[kLaneMost] = {};
-  lane_load(head_ptr<const T>(a.q, rep, head, hd) + i * a.q.row, hd, lane, q);
-  lane_load(head_ptr<const T>(a.dout, rep, head, hd) + i * a.dout.row, hd, lane, g);
-  lane_load(head_ptr<const T>(a.out, rep, head, hd) + i * a.out.row, hd, lane, x);
-  const float lse = a.lse[stat], dot = lane_dot(g, x, hd, lane);
+  const T* q = head_ptr<const T>(a.q, rep, head, hd);
   const T* k = head_ptr<const T>(a.k, rep, kvh, hd);
   const T* v = head_ptr<const T>(a.v, rep, kvh, hd);
-  for (int64_t j = from; j <= i; ++j) {
-    lane_load(k + j * a.k.row, hd, lane, x);
-    lane_load(v + j * a.v.row, hd, lane, y);
-    const float ds = expf(lane_dot(q, x, hd, lane) * a.scale - lse) * (lane_dot(g, y, hd, lane) - dot);
+  T* out = head_ptr<T>(a.out, rep, head, hd);
+  Held held;
+  int first = -1, next = 0;              // of the keys that were looked at
+  while (rows != 0u) {
+    float x[R][L], acc[R][L], sum[R], lse[R];
+    int from[R], upto[R], lo = 0x7fffffff, hi = 0;
+    uint32_t ill[R];
 #pragma unroll
-    for (int e = 0; e < kLaneMost; ++e) acc[e] = fmaf(ds, x[e], acc[e]);
+    for (int r = 0; r < R; ++r) {
+      const int i = r0 + max(__ffs(rows) - 1, 0);
+      const float l = a.lse[((int64_t)rep * a.heads + head) * a.tokens + i];
+      const bool has = rows != 0u && fabsf(l) < INFINITY;
+      rows &= rows - 1;
+      ill[r] = 0u;
+      from[r] = upto[r] = 0;             // [from, upto): its keys
+      lse[r] = l;
+      sum[r] = 0.f;
+#pragma unroll
+      for (int e = 0; e < L; ++e) x[r][e] = acc[r][e] = 0.f;
+      if (!has) continue;
+      int start, end;
+      row_bounds(a, rep, i, &start, &end);
+      if (start != first) {
+        held = Held{};
+        first = next = start;
+      }
+      held.add_rows<L>(v, a.v.row, next, i + 1, hd, lane);
+      next = i + 1;
+      ill[r] = held.mark<L>(out + i * a.out.row, lane, lane_ill<L>(out + i * a.out.row, hd, lane));
+      if (!__any_sync(0xffffffffu, ill[r] != 0u)) continue;
+      lane_load(q + i * a.q.row, hd, lane, x[r]);
+      from[r] = start;
+      upto[r] = i + 1;
+      lo = min(lo, start);
+      hi = max(hi, i + 1);
+    }
+    for (int j = lo; j < hi; j += kStep) {
+      bool open = false;
+#pragma unroll
+      for (int r = 0; r < R; ++r) open = open || (upto[r] > j && lane_open(acc[r], ill[r]));
+      if (!__any_sync(0xffffffffu, open)) break;
+      float kk[kStep][L], vv[kStep][L], s[R][kStep];
+      lane_rows(k, a.k.row, j, hi, hd, lane, kk);
+      lane_rows(v, a.v.row, j, hi, hd, lane, vv);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int u = 0; u < kStep; ++u) s[r][u] = lane_dot(x[r], kk[u]);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int u = 0; u < kStep; ++u)
+          if (j + u >= from[r] && j + u < upto[r]) {
+            const float p = expf(s[r][u] * a.scale - lse[r]);
+            sum[r] += p;
+#pragma unroll
+            for (int e = 0; e < L; ++e) acc[r][e] = fmaf(p, vv[u][e], acc[r][e]);
+          }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) lane_store(out + (upto[r] - 1) * a.out.row, lane, acc[r], 1.f / sum[r], ill[r]);
   }
-  lane_store(head_ptr<T>(a.dq, rep, head, hd) + i * a.dq.row, hd, lane, acc, a.scale);
 }
 
-template <typename T>
-__device__ __noinline__ void dkv_row(const Args& a, int rep, int kvh, int j) {
-  const int lane = threadIdx.x & 31, hd = a.head_dim, group = a.heads / a.kv_heads;
-  int start, end;
-  row_bounds(a, rep, j, &start, &end);
-  float k[kLaneMost], v[kLaneMost], x[kLaneMost], g[kLaneMost], dk[kLaneMost] = {}, dv[kLaneMost] = {};
-  lane_load(head_ptr<const T>(a.k, rep, kvh, hd) + j * a.k.row, hd, lane, k);
-  lane_load(head_ptr<const T>(a.v, rep, kvh, hd) + j * a.v.row, hd, lane, v);
-  for (int head = kvh * group; head < (kvh + 1) * group; ++head) {
-    const T* q = head_ptr<const T>(a.q, rep, head, hd);
-    const T* d = head_ptr<const T>(a.dout, rep, head, hd);
-    const T* o = head_ptr<const T>(a.out, rep, head, hd);
-    const float* lse = a.lse + ((int64_t)rep * a.heads + head) * a.tokens;
-    for (int64_t i = j; i < end; ++i) {
-      lane_load(d + i * a.dout.row, hd, lane, g);
-      lane_load(o + i * a.out.row, hd, lane, x);
-      const float dot = lane_dot(g, x, hd, lane);
-      lane_load(q + i * a.q.row, hd, lane, x);
-      const float p = expf(lane_dot(k, x, hd, lane) * a.scale - lse[i]);
-      const float ds = p * (lane_dot(g, v, hd, lane) - dot);
+// Rows r0 + the bits of `rows`.  Where lse or D is not finite, neither is any element of the row.
+template <typename T, int L>
+__device__ __noinline__ void dq_rows(const Args& a, int rep, int head, int r0, uint32_t rows) {
+  constexpr int R = kRows<L>;
+  const int lane = threadIdx.x & 31, hd = a.head_dim, kvh = head / (a.heads / a.kv_heads);
+  const T* q = head_ptr<const T>(a.q, rep, head, hd);
+  const T* g = head_ptr<const T>(a.dout, rep, head, hd);
+  const T* o = head_ptr<const T>(a.out, rep, head, hd);
+  const T* k = head_ptr<const T>(a.k, rep, kvh, hd);
+  const T* v = head_ptr<const T>(a.v, rep, kvh, hd);
+  T* dq = head_ptr<T>(a.dq, rep, head, hd);
+  while (rows != 0u) {
+    float x[R][L], y[R][L], acc[R][L], lse[R], dot[R];
+    int from[R], upto[R], lo = 0x7fffffff, hi = 0;
+    uint32_t ill[R];
 #pragma unroll
-      for (int e = 0; e < kLaneMost; ++e) {
-        dk[e] = fmaf(ds, x[e], dk[e]);
-        dv[e] = fmaf(p, g[e], dv[e]);
+    for (int r = 0; r < R; ++r) {
+      const int i = r0 + max(__ffs(rows) - 1, 0);
+      lane_load(g + i * a.dout.row, hd, lane, y[r]);
+      lane_load(o + i * a.out.row, hd, lane, x[r]);
+      lse[r] = a.lse[((int64_t)rep * a.heads + head) * a.tokens + i];
+      dot[r] = lane_dot(x[r], y[r]);
+      const bool has = rows != 0u && fabsf(lse[r]) < INFINITY && fabsf(dot[r]) < INFINITY;
+      rows &= rows - 1;
+      lane_load(q + i * a.q.row, hd, lane, x[r]);
+      ill[r] = 0u;
+      from[r] = upto[r] = 0;
+#pragma unroll
+      for (int e = 0; e < L; ++e) acc[r][e] = 0.f;
+      if (!has) continue;
+      int end;
+      row_bounds(a, rep, i, &from[r], &end);
+      ill[r] = lane_ill<L>(dq + i * a.dq.row, hd, lane);
+      upto[r] = i + 1;
+      lo = min(lo, from[r]);
+      hi = max(hi, i + 1);
+    }
+    for (int j = lo; j < hi; j += kStep) {
+      bool open = false;
+#pragma unroll
+      for (int r = 0; r < R; ++r) open = open || (upto[r] > j && lane_open(acc[r], ill[r]));
+      if (!__any_sync(0xffffffffu, open)) break;
+      float kk[kStep][L], vv[kStep][L], s[R][kStep], d[R][kStep];
+      lane_rows(k, a.k.row, j, hi, hd, lane, kk);
+      lane_rows(v, a.v.row, j, hi, hd, lane, vv);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int u = 0; u < kStep; ++u) {
+          s[r][u] = lane_dot(x[r], kk[u]);
+          d[r][u] = lane_dot(y[r], vv[u]);
+        }
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int u = 0; u < kStep; ++u)
+          if (j + u >= from[r] && j + u < upto[r]) {
+            const float ds = expf(s[r][u] * a.scale - lse[r]) * (d[r][u] - dot[r]);
+#pragma unroll
+            for (int e = 0; e < L; ++e) acc[r][e] = fmaf(ds, kk[u][e], acc[r][e]);
+          }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) lane_store(dq + (upto[r] - 1) * a.dq.row, lane, acc[r], a.scale, ill[r]);
+  }
+}
+
+// Keys k0 + the bits of `rows`, the last one first.  A query whose lse is NaN or -inf leaves nothing finite, one whose D is not finite
+// nothing of dk.  dots: every row's D, or null where nobody has left it.
+template <typename T, int L>
+__device__ __noinline__ void dkv_rows(const Args& a, int rep, int kvh, int k0, uint32_t rows, const float* dots) {
+  constexpr int R = L > 2 ? 2 : 4;       // (four keys of 128 elements take more registers than the tiles)
+  const int lane = threadIdx.x & 31, hd = a.head_dim, group = a.heads / a.kv_heads;
+  const int64_t stats = ((int64_t)rep * a.heads + kvh * group) * a.tokens;
+  const T* k = head_ptr<const T>(a.k, rep, kvh, hd);
+  const T* v = head_ptr<const T>(a.v, rep, kvh, hd);
+  T* to_k = head_ptr<T>(a.dk, rep, kvh, hd);
+  T* to_v = head_ptr<T>(a.dv, rep, kvh, hd);
+  Held held;                             // of dout
+  bool no_p = false, no_ds = false;
+  int last = -1, low = 0, low_g = 0;     // of the queries that were looked at, and from where on
+  while (rows != 0u) {
+    float x[R][L], y[R][L], dk[R][L], dv[R][L];
+    int from[R], upto[R], lo = 0x7fffffff, hi = 0;
+    uint32_t ill_k[R], ill_v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int bit = 31 - __clz(rows), j = k0 + max(bit, 0);
+      ill_k[r] = ill_v[r] = 0u;
+      from[r] = upto[r] = 0;             // [from, upto): its queries
+#pragma unroll
+      for (int e = 0; e < L; ++e) x[r][e] = y[r][e] = dk[r][e] = dv[r][e] = 0.f;
+      if (rows == 0u) continue;
+      rows &= ~(1u << bit);
+      int start, end;
+      row_bounds(a, rep, j, &start, &end);
+      if (end != last) {
+        held = Held{};
+        no_p = no_ds = false;
+        last = low = low_g = end;
+      }
+      for (int h = 0; h < group; ++h)
+        for (int i = j; i < low; i += 32) {
+          const bool in = i + lane < low;
+          const float l = in ? a.lse[stats + h * a.tokens + i + lane] : 0.f, d = dots != nullptr && in ? dots[stats + h * a.tokens + i + lane] : 0.f;
+          no_p = __any_sync(0xffffffffu, !(l > -INFINITY)) || no_p;
+          no_ds = __any_sync(0xffffffffu, !(fabsf(d) < INFINITY)) || no_ds;
+        }
+      low = j;
+      if (no_p) continue;
+      const uint32_t of_k = lane_ill<L>(to_k + j * a.dk.row, hd, lane), of_v = lane_ill<L>(to_v + j * a.dv.row, hd, lane);
+      if (dots == nullptr || __any_sync(0xffffffffu, of_v != 0u)) {
+        for (int h = 0; h < group; ++h) {
+          const T* g = head_ptr<const T>(a.dout, rep, kvh * group + h, hd);
+          held.add_rows<L>(g, a.dout.row, j, low_g, hd, lane);
+          if (dots != nullptr) continue;
+          const T* o = head_ptr<const T>(a.out, rep, kvh * group + h, hd);
+          for (int i = j; i < low_g; i += kStep) {
+            float gg[kStep][L], oo[kStep][L];
+            lane_rows(g, a.dout.row, i, low_g, hd, lane, gg);
+            lane_rows(o, a.out.row, i, low_g, hd, lane, oo);
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) no_ds = !(fabsf(lane_dot(gg[u], oo[u])) < INFINITY) || no_ds;
+          }
+        }
+        low_g = j;
+      }
+      ill_k[r] = no_ds ? 0u : of_k;
+      ill_v[r] = held.mark<L>(to_v + j * a.dv.row, lane, of_v);
+      from[r] = j;
+      if (!__any_sync(0xffffffffu, (ill_k[r] | ill_v[r]) != 0u)) continue;
+      lane_load(k + j * a.k.row, hd, lane, x[r]);
+      lane_load(v + j * a.v.row, hd, lane, y[r]);
+      upto[r] = end;
+      lo = min(lo, j);
+      hi = max(hi, end);
+    }
+    uint32_t any_k = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) any_k |= ill_k[r];
+    const bool of_dk = __any_sync(0xffffffffu, any_k != 0u);
+    for (int h = 0; h < group; ++h) {
+      const T* q = head_ptr<const T>(a.q, rep, kvh * group + h, hd);
+      const T* g = head_ptr<const T>(a.dout, rep, kvh * group + h, hd);
+      const T* o = head_ptr<const T>(a.out, rep, kvh * group + h, hd);
+      const int64_t stat = stats + h * a.tokens;
+      for (int i = lo; i < hi; i += kStep) {
+        bool open = false;
+#pragma unroll
+        for (int r = 0; r < R; ++r) open = open || lane_open(dk[r], ill_k[r]) || lane_open(dv[r], ill_v[r]);
+        if (!__any_sync(0xffffffffu, open)) break;
+        float qq[kStep][L], gg[kStep][L], lse[kStep], dot[kStep];
+        lane_rows(q, a.q.row, i, hi, hd, lane, qq);
+        lane_rows(g, a.dout.row, i, hi, hd, lane, gg);
+#pragma unroll
+        for (int u = 0; u < kStep; ++u) {
+          lse[u] = a.lse[stat + min(i + u, hi - 1)];
+          dot[u] = dots != nullptr ? dots[stat + min(i + u, hi - 1)] : 0.f;
+        }
+        if (dots == nullptr) {
+          float oo[kStep][L];
+          lane_rows(o, a.out.row, i, hi, hd, lane, oo);
+#pragma unroll
+          for (int u = 0; u < kStep; ++u) dot[u] = lane_dot(gg[u], oo[u]);
+        }
+        float s[R][kStep], d[R][kStep] = {};
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int u = 0; u < kStep; ++u) s[r][u] = lane_dot(x[r], qq[u]);
+        if (of_dk) {
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) d[r][u] = lane_dot(y[r], gg[u]);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int u = 0; u < kStep; ++u)
+            if (i + u >= from[r] && i + u < upto[r]) {
+              const float p = expf(s[r][u] * a.scale - lse[u]), ds = p * (d[r][u] - dot[u]);
+#pragma unroll
+              for (int e = 0; e < L; ++e) {
+                dk[r][e] = fmaf(ds, qq[u][e], dk[r][e]);
+                dv[r][e] = fmaf(p, gg[u][e], dv[r][e]);
+              }
+            }
       }
     }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      lane_store(to_k + from[r] * a.dk.row, lane, dk[r], a.scale, ill_k[r]);
+      lane_store(to_v + from[r] * a.dv.row, lane, dv[r], 1.f, ill_v[r]);
+    }
   }
-  lane_store(head_ptr<T>(a.dk, rep, kvh, hd) + j * a.dk.row, hd, lane, dk, a.scale);
-  lane_store(head_ptr<T>(a.dv, rep, kvh, hd) + j * a.dv.row, hd, lane, dv, 1.f);
+}
+
+// The larger of two numbers, NaN if one is.
+__device__ __forceinline__ float max_nan(float x, float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
 }
 
 // Whether the tensor-core kernels take a call: bf16, heads of whole 16 bytes up to 128 elements, every row on a 16-byte

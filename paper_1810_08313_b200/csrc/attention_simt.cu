@@ -173,6 +173,17 @@ __device__ __forceinline__ bool write_rows(T* dst, int64_t row, int64_t r0, int6
   return good;
 }
 
+// The tile's rows that are not finite, shared out over the warps: this warp's, from row first_bad() on.
+template <typename W>
+__device__ __forceinline__ int first_bad() { return (threadIdx.x >> 5) * (W::B * 32 / W::NT); }
+template <typename W>
+__device__ __forceinline__ uint32_t bad_rows(const uint32_t* bad) {
+  constexpr int N = W::B * 32 / W::NT;
+  static_assert(N <= 32, "bits of a word");
+  const int lane = threadIdx.x & 31;
+  return __ballot_sync(0xffffffffu, lane < N && bad[first_bad<W>() + lane % N] != 0u);
+}
+
 // sum or maximum over the 16 threads of a row
 __device__ __forceinline__ float row_total(float x) {
 #pragma unroll
@@ -181,12 +192,17 @@ __device__ __forceinline__ float row_total(float x) {
 }
 __device__ __forceinline__ float row_max(float x) {
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  for (int o = 8; o > 0; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
   return x;
 }
 
+// CTAs of an SM that registers have to leave room for: with heads of up to 32 the rare ways (forward_rows and the others) would take more
+// than the tiles do.  (0: as the compiler sees fit.)
+template <int HD, int RB>
+constexpr int least_ctas(bool grad) { return HD > 32 ? 0 : RB == 64 ? 2 : grad ? 3 : 5; }
+
 template <typename T, int HD, int RB>
-__global__ void __launch_bounds__(Way<HD, RB>::NT)
+__global__ void __launch_bounds__(Way<HD, RB>::NT, least_ctas<HD, RB>(false))
 attention_kernel(const __grid_constant__ Args a, const bool quads) {
   using W = Way<HD, RB>;
   extern __shared__ __align__(16) float sm[];
@@ -231,9 +247,9 @@ attention_kernel(const __grid_constant__ Args a, const bool quads) {
       for (int c = 0; c < W::K; ++c) {
         const int64_t j = j0 + tx + 16 * c;
         s[r][c] = j >= start[row] && j <= r0 + row ? s[r][c] * scale2 : -INFINITY;
-        most = fmaxf(most, s[r][c]);
+        most = max_nan(most, s[r][c]);
       }
-      most = fmaxf(row_max(most), top[r]);
+      most = max_nan(row_max(most), top[r]);
       const float ref = most == -INFINITY ? 0.f : most;
       const float keep = exp2f(top[r] - ref);
       top[r] = most;
@@ -262,14 +278,16 @@ attention_kernel(const __grid_constant__ Args a, const bool quads) {
 #pragma unroll
       for (int c = 0; c < W::C; ++c) acc[r][c] = 0.f;
     }
-    by[r] = none ? 0.f : 1.f / sum[r];
+    // (scores with a NaN or +inf, or of -inf only, have no softmax)
+    const bool has = fabsf(top[r]) < INFINITY;
+    by[r] = none ? 0.f : has ? 1.f / sum[r] : NAN;
     if (tx == 0 && i < a.tokens)
-      a.lse[((int64_t)rep * a.heads + head) * a.tokens + i] = none ? 0.f : fmaf(top[r], kLn2, logf(sum[r]));
+      a.lse[((int64_t)rep * a.heads + head) * a.tokens + i] = none ? 0.f : has ? fmaf(top[r], kLn2, logf(sum[r])) : top[r];
   }
   const bool good = write_rows<T, W, HD>(head_ptr<T>(a.out, rep, head, hd), a.out.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
   if (__syncthreads_and(good)) return;
-  for (int r = tid >> 5; r < W::B; r += W::NT / 32)
-    if (bad[r] != 0u) forward_row<T>(a, rep, head, (int)r0 + r);
+  const uint32_t ill = bad_rows<W>(bad);
+  if (ill != 0u) forward_rows<T, HD / 32>(a, rep, head, (int)r0 + first_bad<W>(), ill);
 }
 
 // dot[r] = dout . out of the tile's rows: neighbouring threads share a row; out is loaded before, dout taken from shared memory
@@ -368,8 +386,8 @@ __device__ __forceinline__ void grad_queries(const Args& a, bool quads, float* s
   }
   const bool good = write_rows<T, W, HD>(head_ptr<T>(a.dq, rep, head, hd), a.dq.row, r0, a.tokens, hd, ty, tx, acc, by, bad);
   if (__syncthreads_and(good)) return;
-  for (int r = tid >> 5; r < W::B; r += W::NT / 32)
-    if (bad[r] != 0u) dq_row<T>(a, rep, head, (int)r0 + r);
+  const uint32_t ill = bad_rows<W>(bad);
+  if (ill != 0u) dq_rows<T, HD / 32>(a, rep, head, (int)r0 + first_bad<W>(), ill);
 }
 
 // Tiles of keys: scores with the keys as rows and the queries as columns.  `rank` of the `split` CTAs that share the queries.
@@ -472,14 +490,14 @@ __device__ __forceinline__ void grad_keys(const Args& a, bool quads, float* sm, 
   bool good = write_rows<T, W, HD>(head_ptr<T>(a.dk, rep, kvh, hd), a.dk.row, k0, a.tokens, hd, ty, tx, dk, scale, bad);
   good = write_rows<T, W, HD>(head_ptr<T>(a.dv, rep, kvh, hd), a.dv.row, k0, a.tokens, hd, ty, tx, dv, one, bad) && good;
   if (__syncthreads_and(good)) return;
-  for (int r = tid >> 5; r < W::B; r += W::NT / 32)
-    if (bad[r] != 0u) dkv_row<T>(a, rep, kvh, (int)k0 + r);
+  const uint32_t ill = bad_rows<W>(bad);
+  if (ill != 0u) dkv_rows<T, HD / 32>(a, rep, kvh, (int)k0 + first_bad<W>(), ill, nullptr);
 }
 
 // The first `key_units` times `split` CTAs have tiles of keys (those with the most queries first), the others tiles of queries (those
 // with the most keys first).
 template <typename T, int HD, int RB>
-__global__ void __launch_bounds__(Way<HD, RB>::NT)
+__global__ void __launch_bounds__(Way<HD, RB>::NT, least_ctas<HD, RB>(true))
 attention_grad_kernel(const __grid_constant__ Args a, const bool quads, const int key_units, const int query_units, const int split) {
   using W = Way<HD, RB>;
   extern __shared__ __align__(16) float sm[];

@@ -413,20 +413,17 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     if (failed) {
       if (lane == 0) atomicExch(a.err, 43);
     } else if (r0 + x * kB + q * 32 < a.tokens) {
-      // (a row with a NaN or +inf, or of -inf only, is computed once more: exp2_fma has no infinities)
-      const float by = none ? 0.f : fabsf(top) < INFINITY ? 1.f / sum : NAN;
+      // (scores with a NaN or +inf, or of -inf only, have no softmax: exp2_fma has no infinities)
+      const bool has = fabsf(top) < INFINITY;
+      const float by = none ? 0.f : has ? 1.f / sum : NAN;
       __nv_bfloat16* dst = row < a.tokens ? head_ptr<__nv_bfloat16>(a.out, rep, head, a.head_dim) + row * a.out.row : nullptr;
       const bool fine = result_row<HD>(to, 0, cols, sp.lo <= sp.hi, none, by, dst, a.head_dim);
       if (row < a.tokens)
-        a.lse[((int64_t)rep * a.heads + head) * a.tokens + row] = none ? 0.f : fmaf(top * scale2, kLn2, logf(sum));
+        a.lse[((int64_t)rep * a.heads + head) * a.tokens + row] = none ? 0.f : has ? fmaf(top * scale2, kLn2, logf(sum)) : top;
       __syncwarp();
-      uint32_t bad = __ballot_sync(0xffffffffu, !none && !fine);
+      const uint32_t bad = __ballot_sync(0xffffffffu, !none && has && !fine);
       __syncwarp();
-      while (bad != 0u) {
-        const int r = __ffs(bad) - 1;
-        bad &= bad - 1;
-        forward_row<__nv_bfloat16>(a, rep, head, r0 + x * kB + q * 32 + r);
-      }
+      if (bad != 0u) forward_rows<__nv_bfloat16, HD / 32>(a, rep, head, r0 + x * kB + q * 32, bad);
     }
     tc_fence_before_sync();
   }
@@ -693,13 +690,9 @@ attention_dq_tc_kernel(const __grid_constant__ DqMaps maps, const __grid_constan
       if (ill != 0u && lane == 0) atomicOr(&bad[q], ill);
     }
     elements_sync();
-    if (!failed && half == 0) {
-      uint32_t ill = bad[q];
-      while (ill != 0u) {
-        const int e = __ffs(ill) - 1;
-        ill &= ill - 1;
-        dq_row<__nv_bfloat16>(a, rep, head, r0 + q * 32 + e);
-      }
+    if (!failed) {
+      const uint32_t ill = bad[q] & 0xFFFFu << half * 16;
+      if (ill != 0u) dq_rows<__nv_bfloat16, HD / 32>(a, rep, head, r0 + q * 32, ill);
     }
     tc_fence_before_sync();
   }
@@ -1016,13 +1009,9 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
         if (ill != 0u && lane == 0) atomicOr(&bad[q], ill);
       }
       elements_sync();
-      if (!failed && half == 0) {
-        uint32_t ill = bad[q];
-        while (ill != 0u) {
-          const int e = __ffs(ill) - 1;
-          ill &= ill - 1;
-          dkv_row<__nv_bfloat16>(a, rep, kvh, k0 + q * 32 + e);
-        }
+      if (!failed) {
+        const uint32_t ill = bad[q] & 0xFFFFu << half * 16;
+        if (ill != 0u) dkv_rows<__nv_bfloat16, HD / 32>(a, rep, kvh, k0 + q * 32, ill, a.dot);
       }
     } else {
       // [dk, dv][column][row], neighbouring lanes beside each other (over K and V, which have to have landed)
@@ -1087,8 +1076,8 @@ attention_dkv_tc_kernel(const __grid_constant__ DkvMaps maps, const __grid_const
       for (int g = 0; g < 4; ++g) {
         uint32_t ill = 0;
         for (int p = 0; p < split; ++p) ill |= __float_as_uint(ld_cluster_f32(map_to_rank(smem_u32(&bad[g]), p)));
-        for (int e = warp - 2; e < 32; e += 8)
-          if (ill >> e & 1) dkv_row<__nv_bfloat16>(a, rep, kvh, k0 + g * 32 + e);
+        ill &= 0xFu << (warp - 2) * 4;
+        if (ill != 0u) dkv_rows<__nv_bfloat16, HD / 32>(a, rep, kvh, k0 + g * 32, ill, a.dot);
       }
     }
     __syncwarp();
