@@ -180,3 +180,41 @@ def test_values_that_are_not_finite_take_bounded_time(case):
     stop.record()
     stop.synchronize()
     assert start.elapsed_time(stop) < 60.0
+
+
+# ---- what keys have in common ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hd", [64, 72, 128])
+def test_gradient_of_queries_whose_keys_have_much_in_common(hd):
+    """A row's dS add up to dout . (exact out - out), nearly zero, so that what the keys share (16 in column 0, where q is zero) must
+    not come back from the roundings of dS: two bf16 pieces keep 2^-17 of a term, one would keep 2^-9.
+
+    Bounds per term: the exponent (16 truncated MMAs of 2^-22 of the product's absolute sum, hd roundings, log-sum-exp), the
+    product dout . v and D the same, 2^-16 of dS for its pieces, sums of n keys in MMAs of 16, the result's rounding."""
+    import torch
+    from paper_1810_08313_b200 import binding as b
+    tokens, cuts, scale = 300, [0, 9, 30, 64, 130, 300], 1.0 / hd ** 0.5
+    q, k, v, dout = (_randn(s, 1, tokens, 1, hd) for s in (1, 2, 3, 4))
+    q[..., 0], k[..., 0] = 0.0, 16.0
+    seq = torch.tensor([cuts], dtype=torch.int32, device="cuda")
+    out, lse = b.attention(q, k, v, seq)
+    dq = b.attention_grad(dout, q, k, v, out, lse, seq)[0][0, :, 0].double()
+    q, k, v, dout, out = (t[0, :, 0].double() for t in (q, k, v, dout, out))
+    lse = lse[0, 0].double()[:, None]
+    i = torch.arange(tokens, device="cuda")
+    of = torch.bucketize(i, torch.tensor(cuts, device="cuda"), right=True)
+    see = (of[:, None] == of[None, :]) & (i[None, :] <= i[:, None])
+    s = (q @ k.T) * scale
+    p = torch.where(see, (s - lse).exp(), 0.0)
+    dot = (dout * out).sum(1, keepdim=True)
+    ds = p * (dout @ v.T - dot)
+    mma, n = hd * U + 16 * 2.0 ** -22, see.sum(1, keepdim=True)
+    d = mma * (q.abs() @ k.abs().T) * scale + 4 * U * (s.abs() + lse.abs()) + 2.0 ** -22
+    term = d * ds.abs() + p * mma * (dout.abs() @ v.abs().T + (dout * out).abs().sum(1, keepdim=True)) + (2.0 ** -16 + 4 * U) * ds.abs()
+    keys = (n + 64) * U + (n / 16 + 8) * 2.0 ** -22
+    want = (ds @ k) * scale
+    tol = 1.05 * scale * (term @ k.abs() + keys * (ds.abs() @ k.abs())) + (2.0 ** -8 + 2 * U) * want.abs() + 2.0 ** -126
+    assert bool(((dq - want).abs() <= tol).all())
+    # with one piece, column 0 of many rows would lie outside
+    one = (ds.float().bfloat16().double() @ k) * scale
+    assert int(((one - want).abs() > tol)[:, 0].sum()) > tokens // 4
