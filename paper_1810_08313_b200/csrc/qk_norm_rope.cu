@@ -186,7 +186,7 @@ qk_norm_rope_kernel(const __grid_constant__ NrArgs a) {
   }
   grid_dep_wait();
   grid_dep_launch();
-  __shared__ float weight[2][kNrMaxDim];
+  __shared__ __align__(16) float weight[2][kNrMaxDim];                  // (read four at a time)
   for (int i = threadIdx.x; i < 2 * kNrMaxDim; i += kNrWarps * 32)
     if ((i & (kNrMaxDim - 1)) < hd) weight[i / kNrMaxDim][i & (kNrMaxDim - 1)] = a.w[i / kNrMaxDim][rep * a.w_stride + (i & (kNrMaxDim - 1))];
   // Units are tokens, or parts of them: the parts of a token go to neighbouring warps, so a warp has the same part of every one.
