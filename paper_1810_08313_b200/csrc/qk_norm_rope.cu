@@ -29,9 +29,10 @@ using ptx::two;
 
 constexpr int kNrMaxDim = 256;
 constexpr int kNrWarps = 8;              // of a CTA
-// CTAs of an SM.  The forward pass of vectors has registers for three (16384 x 40 heads of 128 bf16: 67 us, 78 with two CTAs and loads
-// eight steps ahead, 74 with four CTAs and two); the backward pass spills with three (107 us, 145).
-constexpr int nr_per_sm(bool vec, bool grad) { return vec && !grad ? 3 : 2; }
+// CTAs of an SM.  The forward pass of bf16 vectors has registers for three (16384 x 40 heads of 128: 68 us, 74 with two; 78 with two and loads
+// eight steps ahead, 74 with four CTAs and two).  That of fp32 spills with three (4096 x 40 heads of 128: 38 us, 32 with two; 16384
+// tokens 119 and 120, in neighbouring pairs 133 and 124), and so does the backward pass (bf16 145 us, 107 with two).
+constexpr int nr_per_sm(bool vec, bool grad, bool bf16) { return vec && !grad && bf16 ? 3 : 2; }
 
 struct NrTensor { const void* p; int64_t row, replica; };
 struct NrArgs {
@@ -169,7 +170,7 @@ __device__ __forceinline__ void angles(const double (&turns)[4], int position, f
 
 // LPR lanes to a head, 32 / LPR heads of a token at a time, U such steps loaded ahead.
 template <typename T, bool VEC, bool INTER, int LPR, bool GRAD>
-__global__ void __launch_bounds__(kNrWarps * 32, nr_per_sm(VEC, GRAD))
+__global__ void __launch_bounds__(kNrWarps * 32, nr_per_sm(VEC, GRAD, sizeof(T) == 2))
 qk_norm_rope_kernel(const __grid_constant__ NrArgs a) {
   constexpr int H = 32 / LPR, U = GRAD && (sizeof(T) == 4 || !VEC) ? 2 : 4;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / LPR, slot = lane % LPR;
@@ -466,7 +467,7 @@ extern "C" int ls_qk_norm_rope(const void* q_dev, const void* k_dev, const float
   if (tokens == 0) return LS_OK;
   // few tokens: their heads are shared out over several warps, up to eight
   while (a.parts_log2 < 3 && (m * tokens << a.parts_log2) < 148 * 16) ++a.parts_log2;
-  const unsigned ctas = nr_ctas(m, tokens << a.parts_log2, nr_per_sm(nr_vec(a, dtype, false), false));
+  const unsigned ctas = nr_ctas(m, tokens << a.parts_log2, nr_per_sm(nr_vec(a, dtype, false), false, dtype == LS_DTYPE_BF16));
   return nr_run(a, dtype, interleaved != 0, false, ctas, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LS_OK : LS_ERR_CUDA;
 }
 
@@ -475,7 +476,7 @@ extern "C" int ls_qk_norm_rope_grad_ws_bytes(int m, int64_t tokens, int head_dim
   const int rc = nr_check(m, tokens, 1, 1, head_dim, 0, LS_DTYPE_FP32);
   if (rc != LS_OK) return rc;
   if (bytes == nullptr) return LS_ERR_INVALID_ARG;
-  *bytes = (size_t)m * nr_ctas(m, tokens, nr_per_sm(true, true)) * 2 * (size_t)head_dim * sizeof(float);
+  *bytes = (size_t)m * nr_ctas(m, tokens, nr_per_sm(true, true, true)) * 2 * (size_t)head_dim * sizeof(float);
   return LS_OK;
 }
 
@@ -517,7 +518,7 @@ extern "C" int ls_qk_norm_rope_grad(const void* dq_out_dev, const void* dk_out_d
   if (ws_bytes < need || reinterpret_cast<uintptr_t>(ws_dev) % 256 != 0) return LS_ERR_STATE_SIZE;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   a.part = static_cast<float*>(ws_dev);
-  const unsigned ctas = nr_ctas(m, tokens, nr_per_sm(true, true));
+  const unsigned ctas = nr_ctas(m, tokens, nr_per_sm(true, true, true));
   // (no tokens: the sums are those of no parts)
   if (tokens > 0 && nr_run(a, dtype, interleaved != 0, true, ctas, st) != cudaSuccess) return LS_ERR_CUDA;
   const cudaError_t e = launch_dep(qk_norm_fold_kernel, dim3((unsigned)((2 * head_dim + 31) / 32), (unsigned)m), dim3(1024), 0, st, 1,
