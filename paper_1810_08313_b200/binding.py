@@ -725,7 +725,7 @@ def _rope_args(op, q, k, q_weight, k_weight, positions, inv_freq, what):
     kw, _, kws = op.stack(k_weight, "k_weight", (hd,), m, f32)
     if m > 1 and ws != kws:
         raise ValueError("q_weight and k_weight must have the same distance between replicas")
-    return dt, m, tokens, heads, kv, hd, 2 * inv_freq.shape[0], qw, kw, ws, pp, fp
+    return dt, m, tokens, heads, kv, hd, _int32(2 * inv_freq.shape[0], LS_ERR_TOO_LARGE, what), qw, kw, ws, pp, fp
 
 
 def qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, eps: float = 1e-6, interleaved: bool = False, q_out=None, k_out=None,
@@ -781,7 +781,7 @@ def _sequences(op, seq_start, m):
     n = seq_start.shape[-1] - 1 if isinstance(seq_start, op.torch.Tensor) and seq_start.dim() else 0
     if n < 0:
         raise ValueError("seq_start must be an int32 tensor [m][sequences + 1]")
-    return op.dense(seq_start, "seq_start", (m, n + 1), op.torch.int32), n
+    return op.dense(seq_start, "seq_start", (m, n + 1), op.torch.int32), _int32(n, LS_ERR_TOO_LARGE, "seq_start")
 
 
 def attention(q, k, v, seq_start=None, scale: Optional[float] = None, out=None, lse=None, stream=None):
@@ -799,7 +799,7 @@ def attention(q, k, v, seq_start=None, scale: Optional[float] = None, out=None, 
     o, outp, outr, outs = op.heads_out(out, q, "out", m, tokens, heads, hd, q.dtype)
     lse_t, lp = op.out_dense(lse, q, "lse", (m, heads, tokens), op.torch.float32)
     op.call("ls_attention", qp, kp, vp, sp, m, tokens, n, heads, kv, hd, qr, kr, vr, qs, ks, vs, dt,
-            1.0 / math.sqrt(hd) if scale is None else scale, outp, outr, outs, lp)
+            1.0 / math.sqrt(max(hd, 1)) if scale is None else scale, outp, outr, outs, lp)
     return o if out is not None else _like(q, 4, o), lse_t if lse is not None else _like(q, 4, lse_t)
 
 
@@ -826,7 +826,7 @@ def attention_grad(dout, q, k, v, out, lse, seq_start=None, scale: Optional[floa
     dv_t, dvp, dvr, dvs = op.heads_out(dv, v, "dv", m, tokens, kv, hd, q.dtype)
     base, nbytes, keep = op.workspace(q, workspace, _ws_bytes("ls_attention_grad_ws_bytes", m, tokens, heads, kv, hd))
     op.call("ls_attention_grad", gp, qp, kp, vp, outp, lp, sp, m, tokens, n, heads, kv, hd, gr, qr, kr, vr, outr, gs, qs, ks, vs, outs,
-            dt, 1.0 / math.sqrt(hd) if scale is None else scale, dqp, dkp, dvp, dqr, dkr, dvr, dqs, dks, dvs, base, nbytes)
+            dt, 1.0 / math.sqrt(max(hd, 1)) if scale is None else scale, dqp, dkp, dvp, dqr, dkr, dvr, dqs, dks, dvs, base, nbytes)
     return (dq_t if dq is not None else _like(q, 4, dq_t), dk_t if dk is not None else _like(q, 4, dk_t),
             dv_t if dv is not None else _like(q, 4, dv_t))
 
