@@ -7,20 +7,24 @@
 //   four warps for each tile's softmax, a thread a row: 128 scores in registers, maximum, exponentials, sum, P in bf16 back to
 //              tensor memory in two halves, on the first of which PV starts
 // Heads of up to 64: a CTA has one tile, and the SM two CTAs, of which one starts and ends while the other works (16 heads of 64,
-// two tiles a CTA: 251 us for 8192 rows instead of 231, 53.1 us for 23 packed sequences instead of 48.6).  P has a place of its own,
-// and S of the next block is issued as soon as this one's is in registers.
+// two tiles a CTA: 9 % longer for 8192 rows and for 23 packed sequences).  P has a place of its own, and S of the next block is issued
+// as soon as this one's is in registers.
 // Larger heads: a CTA has both tiles, 256 consecutive rows, and they share every K and V block, which one CTA a tile would draw from
 // the L2 faster than it gives them (64 KB a block, twice in the 1700 cycles that two softmaxes take).  S and O fill the tensor memory,
 // P takes the place of S, and S of a block is issued when the PV before it is done.  So the two tiles have to stay half a block
-// apart: S of a tile waits until the other one is past its maxima.  (Without, both end in step: 994 us instead of 945 for 16384
-// rows of 16 heads of 128.  With two threads a row, and twice the warps: 1013 us.)
+// apart: S of a tile waits until the other one is past its maxima.  (16384 rows of 16 heads of 128: without, both end in step, 5 %
+// longer; with two threads a row, and twice the warps, 7 %.)
 // O stays in tensor memory over all blocks and is rescaled only where a row's maximum has grown by more than 2^8 since its
 // reference was taken: P then lies below 2^8 instead of 1, which costs bf16 and fp32 no precision, and most blocks need no
-// pass over O.  P is rounded to bf16 (2^-8 of each term, signs at random), its sum is taken before the rounding.
-// Bound by the softmax of a tile, 1500 to 1700 cycles a block of the SM (the special-function unit alone takes 830 for the exponentials,
-// the MMAs 510 with heads of 64 and 1020 with 128), and in long calls by the clock under the power cap: 16384 rows of 16 heads of
-// 128 take 960 to 1070 us (1.15 to 1.03 PFLOP/s), 23 packed sequences in 8191 rows of 16 heads of 64 47 us, with 5700 of a CTA's
-// 18000 cycles before its first block and behind its last one.
+// pass over O.  P is rounded to bf16 (at most 2^-8 of each term, signs at random), its sum is taken before the rounding:
+// out is off by 1.8e-3 of its norm, 1.66e-3 of which its own rounding to bf16 is.
+// Exponentials are the special-function unit's, 1024 cycles a tile and block.  (A polynomial on the FMA units for three of 16 gains
+// nothing, every instruction of a softmax thread being on the critical path: 16384 rows of 16 heads of 128 1011 to 1015 us with
+// it, 1009 to 1018 without, 8192 rows of 16 heads of 64 239 and 230, in turn.)
+// Bound by the softmax of a tile, 1500 to 1700 cycles a block of the SM (the MMAs take 510 with heads of 64 and 1020 with 128), and in long
+// calls by the clock under the power cap: 16384 rows of 16 heads of 128 take 930 to 1070 us with the clock (1.18 to 1.03
+// PFLOP/s), 23 packed sequences in 8191 rows of 16 heads of 64 48 to 51 us, with 5700 of a CTA's 18000 cycles before its first block and
+// behind its last one.
 #include "attention.cuh"
 
 namespace ls {
@@ -55,31 +59,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^x of two numbers on the FMA units (Cody and Waite's reduction: x = n + f, |f| <= 1/2, and a polynomial of degree 5 for 2^f,
-// fitted to the least relative error, 9e-8, 1.9e-7 with its roundings).  x of -127 or less, -inf included, gives 0, and
-// between that and -126 something below the smallest normal number.  No infinities, no NaN.
-__device__ __forceinline__ float2 exp2_fma(uint64_t x2) {
-  float2 x = parts(x2);
-  x.x = fmaxf(x.x, -127.f);
-  x.y = fmaxf(x.y, -127.f);
-  x2 = two(x.x, x.y);
-  constexpr float kRound = 12582912.f;   // 1.5 * 2^23: the sum's last bits are the nearest whole number
-  const uint64_t t = add2(x2, two(kRound, kRound));
-  const uint64_t f = add2(x2, fma2(t, two(-1.f, -1.f), two(kRound, kRound)));
-  uint64_t p = fma2(f, two(0.001326472731307149f, 0.001326472731307149f), two(0.009671512991189957f, 0.009671512991189957f));
-  p = fma2(p, f, two(0.05550733581185341f, 0.05550733581185341f));
-  p = fma2(p, f, two(0.24022242426872253f, 0.24022242426872253f));
-  p = fma2(p, f, two(0.6931470036506653f, 0.6931470036506653f));
-  p = fma2(p, f, two(1.f, 1.f));
-  const float2 n = parts(t), y = parts(p);
-  return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(n.x) << 23)),
-                     __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23)));
-}
-// Which of 16 pairs of exponentials the FMA units take.  The special-function unit's 16 a clock and SM take as long as the tensor
-// cores' two products of a 128 x 128 block with heads of 128, but every instruction of a softmax thread is on the critical
-// path, and the polynomial has more: 16384 rows of 16 heads took 979 us with none, 893 us with three, 920 us with five.
-constexpr uint32_t kFmaOf16 = 0x1084;
-
 // Of 32 columns, a bit for each one in [from, to].
 __device__ __forceinline__ uint32_t visible(int from, int to) {
   return (from > 31 ? 0u : from > 0 ? 0xffffffffu << from : 0xffffffffu) & (to < 0 ? 0u : to < 31 ? (2u << to) - 1 : 0xffffffffu);
@@ -375,14 +354,9 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const uint64_t t = fma2(two(s[c][2 * i], s[c][2 * i + 1]), by2, ref2);
-          float2 e;
-          if (kFmaOf16 >> i & 1) {
-            e = exp2_fma(t);
-          } else {
-            e = parts(t);
-            e.x = ex2(e.x);
-            e.y = ex2(e.y);
-          }
+          float2 e = parts(t);
+          e.x = ex2(e.x);
+          e.y = ex2(e.y);
           part[i & 1] = add2(part[i & 1], two(e.x, e.y));
           p[i] = pack2(e.x, e.y);
         }
@@ -413,7 +387,7 @@ attention_tc_kernel(const __grid_constant__ FwdMaps maps, const __grid_constant_
     if (failed) {
       if (lane == 0) atomicExch(a.err, 43);
     } else if (r0 + x * kB + q * 32 < a.tokens) {
-      // (scores with a NaN or +inf, or of -inf only, have no softmax: exp2_fma has no infinities)
+      // (scores with a NaN or +inf, or of -inf only, have no softmax)
       const bool has = fabsf(top) < INFINITY;
       const float by = none ? 0.f : has ? 1.f / sum : NAN;
       __nv_bfloat16* dst = row < a.tokens ? head_ptr<__nv_bfloat16>(a.out, rep, head, a.head_dim) + row * a.out.row : nullptr;
