@@ -502,7 +502,7 @@ int ls_muon_step_layer(ls_handle* h, int layer, const void* g_dev, int64_t g_str
  *   (a, b) -> (a cos - b sin, a sin + b cos),  angle = positions[token] * inv_freq[pair]
  * Pair p is the elements (p, p + rot_dim / 2), or (2 p, 2 p + 1) when interleaved; the other elements stay as they are.
  * q [m][tokens][heads][head_dim], k [m][tokens][kv_heads][head_dim], and their outputs, of dtype: *_row is the distance in
- * elements between tokens of a tensor, *_stride that between replicas (ignored for one token, one replica), the heads of a
+ * elements between tokens of a tensor, *_stride that between replicas, one behind the other (ignored for one token, one replica), the heads of a
  * token are dense, so that q and k may be parts of one projection.  weights: float [m][head_dim], weight_stride apart.
  * inv_freq: double [rot_dim / 2], positions: int32 [m][tokens], dense (either may be NULL if rot_dim == 0).  Angles
  * are formed in double, squares and their mean in fp32 (elements of up to 10^18).  rot_dim is even.  head_dim <= 256, tokens <=
@@ -562,8 +562,8 @@ int ls_attention_grad(const void* dout_dev, const void* q_dev, const void* k_dev
  * out_strides[i] apart; grads[i] itself, with its type and stride, is allowed) and gradients that are not their own outputs stay.
  * An output that shares memory with another output, or with a gradient that is not its own, is refused (LS_ERR_INVALID_ARG).
  * norm: float [m].  max_norm > 0; INFINITY: the norm, and nothing is scaled.  A norm of NaN makes the replica's results NaN;
- * an infinite one makes them 0, and NaN where a gradient is infinite.  Sums are formed in double over fp32 sums of 32 squares; no square
- * overflows or underflows.  The arrays are read before the call returns.  n_tensors <= 65536. */
+ * that of an infinite gradient makes them 0, and NaN where a gradient is infinite.  Sums are formed in double over fp32 sums of 32 squares; no
+ * square overflows or underflows, and a finite norm beyond fp32's largest number is written as infinity, but clips as what it is.  The arrays are read before the call returns.  n_tensors <= 65536. */
 int ls_clip_grads_ws_bytes(const int64_t* sizes, int n_tensors, int m, size_t* bytes);
 int ls_clip_grads(const void* const* grads_dev, const int64_t* sizes, const int64_t* strides, const int32_t* dtypes, int n_tensors,
                   int m, float max_norm, void* const* outs_dev, const int64_t* out_strides, const int32_t* out_dtypes,

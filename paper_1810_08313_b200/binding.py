@@ -328,7 +328,8 @@ def linear_loss_static(W, bias, x, y, chunk_rows: int, chunk_loss, loss: str = "
 # Every tensor takes the replicas first ([m][rows][d], ...); one replica may leave that axis out.  A replica is dense,
 # the distance between replicas is free (views into packed replica vectors are fine).  Outputs that are not given are
 # allocated.  `workspace`: a uint8 tensor of the size the matching *_workspace function names, for callers that keep
-# one; calls that may overlap on the GPU need their own.  `stream`: a torch stream, the current one by default.
+# one; calls that may overlap on the GPU need their own.  `stream`: a torch stream, the current one by default.  An output shares
+# no memory with inputs or other outputs, unless its function says so.
 
 _TORCH = None
 _OP_DTYPE = {}
@@ -731,7 +732,7 @@ def _rope_args(op, q, k, q_weight, k_weight, positions, inv_freq, what):
 def qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, eps: float = 1e-6, interleaved: bool = False, q_out=None, k_out=None,
                  stream=None):
     """RMS norm of every head of q [m][tokens][heads][head_dim] and k [m][tokens][kv_heads][head_dim] (float32 or bfloat16; the
-    heads of a token dense, tokens and replicas any distance apart) with float32 weights [m][head_dim], and rotation of the
+    heads of a token dense, tokens any distance apart, each replica behind the one before) with float32 weights [m][head_dim], and rotation of the
     first 2 len(inv_freq) elements by positions (int32 [m][tokens]) times inv_freq (float64, rope_frequencies()), in one
     pass (ls_qk_norm_rope).  Returns the two results."""
     op = _Op(q, stream)
@@ -786,7 +787,7 @@ def _sequences(op, seq_start, m):
 
 def attention(q, k, v, seq_start=None, scale: Optional[float] = None, out=None, lse=None, stream=None):
     """Causal attention with grouped heads over packed sequences: q [m][tokens][heads][head_dim], k and v
-    [m][tokens][kv_heads][head_dim] (float32 or bfloat16; the heads of a token dense, tokens and replicas any distance apart),
+    [m][tokens][kv_heads][head_dim] (float32 or bfloat16; the heads of a token dense, tokens any distance apart, each replica behind the one before),
     seq_start int32 [m][sequences + 1] (None: one sequence of all tokens), scale 1 / sqrt(head_dim) if None (ls_attention).
     Returns (out like q, log-sum-exp float32 [m][heads][tokens]); rows in no sequence are zero in both."""
     op = _Op(q, stream)
