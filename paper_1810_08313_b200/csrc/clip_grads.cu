@@ -6,7 +6,7 @@
 // sum a CTA, the second adds the CTAs' sums in index order, redundantly in every CTA (a few hundred numbers), and scales.
 // Where nothing is clipped in place it ends there.  Bound by HBM.  A replica's tensors are one sequence of chunks of 8192
 // elements, of which every CTA takes a run; the second launch takes its run backwards, so that what the first one read last is
-// still in the L2 (126 MB): two replicas of 332 million fp32 elements into bf16 in 379 + 631 us, 7.0 and 6.3 TB/s of what each launch
+// still in the L2 (126 MB): two replicas of 332 million fp32 elements into bf16 in 383 + 631 us, 7.0 and 6.3 TB/s of what each launch
 // reads and writes; 38 tensors of four small replicas, whose second launch has nothing to scale, in 23 + 5 us.
 //
 // Squares are added in fp32 over the 32 elements that a thread has of a chunk, and in double beyond.  Where such a sum
