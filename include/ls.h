@@ -566,7 +566,7 @@ int ls_attention_grad(const void* dout_dev, const void* q_dev, const void* k_dev
  * square overflows or underflows, and a finite norm beyond fp32's largest number is written as infinity, but clips as what it is.  The arrays are read before the call returns.  n_tensors <= 65536. */
 int ls_clip_grads_ws_bytes(const int64_t* sizes, int n_tensors, int m, size_t* bytes);
 int ls_clip_grads(const void* const* grads_dev, const int64_t* sizes, const int64_t* strides, const int32_t* dtypes, int n_tensors,
-                  int m, float max_norm, void* const* outs_dev, const int64_t* out_strides, const int32_t* out_dtypes,
+                  int m, double max_norm, void* const* outs_dev, const int64_t* out_strides, const int32_t* out_dtypes,
                   float* norm_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream);
 
 /* Per-kernel device timing.  Between ls_profile_begin() and ls_profile_end()

@@ -144,7 +144,7 @@ def _lib():
         "ls_attention_grad": (C.c_int, [vp] * 7 + [C.c_int, i64] + [C.c_int] * 4 + [i64] * 10 + [C.c_int, f32, vp, vp, vp] + [i64] * 6 +
                               [vp, C.c_size_t, vp]),
         "ls_clip_grads_ws_bytes": (C.c_int, [vp, C.c_int, C.c_int, P(C.c_size_t)]),
-        "ls_clip_grads": (C.c_int, [vp, vp, vp, vp, C.c_int, C.c_int, f32, vp, vp, vp, vp, vp, C.c_size_t, vp]),
+        "ls_clip_grads": (C.c_int, [vp, vp, vp, vp, C.c_int, C.c_int, C.c_double, vp, vp, vp, vp, vp, C.c_size_t, vp]),
         "ls_shard_buffer_floats": (C.c_int, [vp, P(i64)]),
         "ls_set_shard": (C.c_int, [vp, C.c_int, C.c_int, vp, vp, EXCHANGE_FN, vp]),
         "ls_shard_partial_sum": (C.c_int, [vp, vp]),

@@ -248,11 +248,11 @@ int clip_fill(const ClipList& l, int from, ClipArgs<MOST>* a) {
 }
 
 template <int MOST>
-int clip_run(const ClipList& l, float max_norm, float* norm, double* part, int parts, cudaStream_t st) {
+int clip_run(const ClipList& l, double max_norm, float* norm, double* part, int parts, cudaStream_t st) {
   ClipArgs<MOST> a;
   a.parts = parts;
   a.part = part;
-  a.max_norm = (double)max_norm;
+  a.max_norm = max_norm;
   a.norm = norm;
   const bool only_norm = isinf(max_norm) && l.out == nullptr;
   for (int pass = 0; pass < 2; ++pass) {
@@ -387,13 +387,13 @@ extern "C" int ls_clip_grads_ws_bytes(const int64_t* sizes, int n_tensors, int m
 }
 
 extern "C" int ls_clip_grads(const void* const* grads_dev, const int64_t* sizes, const int64_t* strides, const int32_t* dtypes,
-                             int n_tensors, int m, float max_norm, void* const* outs_dev, const int64_t* out_strides,
+                             int n_tensors, int m, double max_norm, void* const* outs_dev, const int64_t* out_strides,
                              const int32_t* out_dtypes, float* norm_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
   using namespace ls;
   int parts = 0;
   const int rc = clip_parts(sizes, n_tensors, m, &parts);
   if (rc != LS_OK) return rc;
-  if (!(max_norm > 0.f) || norm_dev == nullptr || reinterpret_cast<uintptr_t>(norm_dev) % 4 != 0 || ws_dev == nullptr) return LS_ERR_INVALID_ARG;
+  if (!(max_norm > 0.0) || norm_dev == nullptr || reinterpret_cast<uintptr_t>(norm_dev) % 4 != 0 || ws_dev == nullptr) return LS_ERR_INVALID_ARG;
   if (n_tensors > 0 && (grads_dev == nullptr || dtypes == nullptr || (m > 1 && strides == nullptr))) return LS_ERR_INVALID_ARG;
   if (n_tensors > 0 && outs_dev != nullptr && (out_dtypes == nullptr || (m > 1 && out_strides == nullptr))) return LS_ERR_INVALID_ARG;
   auto bad = [&](const void* p, int64_t n, int32_t dtype, int64_t stride) {
